@@ -419,6 +419,130 @@ int artopk_get_profile(artopk_ctx* ctx, float* ms_out, int32_t count);
  */
 int artopk_select_info(artopk_ctx* ctx, int32_t* info_out, int32_t count);
 
+/* ------------------------------------------------------------------------------------------
+ * What a training step does on either side of the compressed exchange: layer norm, whose weight
+ * gradients land in a worker's flat gradient vector, and the update of weight matrices that lie
+ * in a flat weight vector.  Both have handles of their own, made once like a context: bound to
+ * one stream and the current device, all device memory allocated at creation, calls only enqueue
+ * kernels (no synchronisation, no memset; they can be recorded into a HIP graph and replayed),
+ * calls on one handle must not overlap.  Buffers of these calls need only be aligned to their
+ * elements; at 16-byte aligned places the loads are wider.  As everywhere, a buffer that a call
+ * writes must not overlap any other of that call.
+ * Element types are ARTOPK_G_F32, ARTOPK_G_BF16 and ARTOPK_G_F16; weights of a layer norm, its
+ * statistics, momentum and updates are float32 whatever the elements' type.
+ * ------------------------------------------------------------------------------------------ */
+
+typedef struct artopk_norm artopk_norm;
+
+/*
+ * A handle for layer norms of up to max_rows rows of up to max_cols elements (each in
+ * [1, 2^31)).  It allocates artopk_norm_scratch_bytes(max_rows, max_cols) (the shares of the
+ * weight gradients, at most 128 MiB up to 16384 columns; -1 for limits that create refuses).
+ * On failure *out is left alone and artopk_last_error(NULL) tells why.
+ */
+int artopk_norm_create(artopk_norm** out, int64_t max_rows, int64_t max_cols, void* hip_stream);
+int64_t artopk_norm_scratch_bytes(int64_t max_rows, int64_t max_cols);
+/* Free the scratch.  The caller must have synchronised the stream. */
+int artopk_norm_destroy(artopk_norm* norm);
+/* Text of the last error on this handle (never NULL; norm = NULL: as artopk_last_error(NULL)). */
+const char* artopk_norm_last_error(const artopk_norm* norm);
+
+/*
+ * Layer norm of each row:  mean = sum(x) / cols,  rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps),
+ * y = (x - mean) rstd gamma + beta.  Sums are float32, y is rounded once.
+ *   x, y       device, rows of `cols` elements of `type`; rows lie x_stride / y_stride elements apart
+ *              (at least cols where there is more than one).  Elements between rows stay untouched
+ *   gamma      device, cols float32, or NULL for ones;  beta the same, or NULL for zeros
+ *   eps        finite, >= 0
+ *   mean_out, rstd_out   device, rows float32 each, for the backward pass; may be NULL
+ * rows may be 0: nothing is enqueued.
+ */
+int artopk_layernorm_forward(artopk_norm* norm, const void* x, int64_t x_stride, int32_t type, int64_t rows,
+                             int64_t cols, const float* gamma, const float* beta, float eps, void* y,
+                             int64_t y_stride, float* mean_out, float* rstd_out);
+
+/*
+ * Its gradient.  With h = (x - mean) rstd and d = dy gamma, row by row
+ *   dx = rstd (d - sum(d) / cols - h sum(d h) / cols),
+ * and summed over the rows  dgamma = sum(dy h),  dbeta = sum(dy).  Sums are float32, and their
+ * order depends on the sizes alone: the same inputs give the same bits.
+ *   dy, x, dx  device, rows of `type` as above; dx may be NULL where only the weights' gradients are wanted
+ *   mean, rstd device, rows float32, as the forward pass left them
+ *   dgamma, dbeta   device, cols elements of grad_type each, or NULL; they may lie anywhere in a
+ *              worker's flat gradient vector, of either type that artopk_step or artopk_step_g16 takes
+ *   accumulate 0: they are overwritten; otherwise added to, in float32 (a further micro-batch)
+ * rows may be 0: dgamma and dbeta become zeros, or stay as they are with accumulate.
+ */
+int artopk_layernorm_backward(artopk_norm* norm, const void* dy, int64_t dy_stride, const void* x,
+                              int64_t x_stride, int32_t type, int64_t rows, int64_t cols, const float* gamma,
+                              const float* mean, const float* rstd, void* dx, int64_t dx_stride, void* dgamma,
+                              void* dbeta, int32_t grad_type, int32_t accumulate);
+
+/* One matrix of a flat vector: rows x cols elements, row by row, from `offset` on. */
+typedef struct artopk_matrix {
+  int64_t offset;
+  int32_t rows, cols;
+  float scale; /* the orthogonalised matrix is multiplied by it, e.g. sqrt(max(1, rows / cols)) */
+} artopk_matrix;
+
+typedef struct artopk_matrices artopk_matrices;
+
+/* How many bits the operands of the matrix products keep.  HALF: 11 (float16, scaled by powers of
+ * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32. */
+enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1 };
+
+#define ARTOPK_MAX_POLAR_STEPS 32
+
+/*
+ * A handle for the matrices of a flat vector of n elements (1 <= n < 2^31) of `type`.  `mats` is a
+ * host array of `count` matrices (1 .. 65535), each within the vector, none overlapping another,
+ * rows and cols in [1, 65536], scale finite; it is read before the call returns.  The iterates' memory
+ * is allocated here: artopk_matrices_scratch_bytes(..) bytes, 6 for each element of a matrix and 4 for each of its
+ * Gram matrix with HALF, of sides padded to whole tiles, and twice that with SPLIT (-1 for arguments that create
+ * refuses).  The tables are copied
+ * to the device synchronously.  On failure *out is left alone and artopk_last_error(NULL) tells why.
+ */
+int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int32_t count, int64_t n,
+                           int32_t type, int32_t products, void* hip_stream);
+int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
+                                      int32_t products);
+int artopk_matrices_destroy(artopk_matrices* m);
+const char* artopk_matrices_last_error(const artopk_matrices* m);
+
+/*
+ * Orthogonalises every matrix G of x by Newton-Schulz steps:  X = G / (||G|| + eps) (Frobenius norm,
+ * summed in float64), then `steps` times  A = X X^T,  X <- a X + (b A + c A^2) X  (of the transpose where
+ * there are more rows than columns), out = scale X.  Each step takes every singular value s to
+ * a s + b s^3 + c s^5.
+ *   x     device, n elements of the handle's type (read only)
+ *   out   device, n elements; elements of no matrix stay as they are
+ *   steps 0 .. ARTOPK_MAX_POLAR_STEPS
+ *   coefficients   host, steps x 3 float32 (a, b, c), or NULL for the usual (3.4445, -4.7750, 2.0315) in
+ *         every step.  Refused where they would take singular values in [0, 1] beyond 2, or |a + b s^2 + c s^4|
+ *         beyond 15, in any step: the iterates would leave the operands' range
+ *   eps   finite, > 0
+ * A matrix of zeros gives zeros; NaN or infinity in a matrix gives NaN throughout that matrix and
+ * touches no other.
+ */
+int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t steps, const float* coefficients,
+                         float eps);
+
+/*
+ * The model update behind an exchange (Alg. 1's update of w, with the direction of each matrix
+ * orthogonalised):
+ *   momentum <- mu momentum + update_scale update              (all n elements, float32)
+ *   v = nesterov ? mu momentum + update_scale update : momentum
+ *   matrices  w <- w (1 - eta decay) - eta scale X(v),  X as in artopk_orthogonalize
+ *   the rest  w <- w - eta_rest v    (left alone where eta_rest is 0)
+ *   weights   device, n elements of the handle's type, updated in place (each rounded once)
+ *   momentum  device, n float32, updated in place
+ *   update    device, n float32: the step's update_out; update_scale 1 / W makes its sum a mean
+ *   mu, eta, decay, eta_rest, update_scale   finite
+ */
+int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const float* update, float update_scale,
+                     float mu, int32_t nesterov, float eta, float decay, float eta_rest, int32_t steps,
+                     const float* coefficients, float eps);
+
 /* Library version, major*10000 + minor*100 + patch. */
 int32_t artopk_version(void);
 

@@ -17,6 +17,7 @@ ARTOPK_STAR_COUNTER = 5
 ARTOPK_G_F32, ARTOPK_G_BF16, ARTOPK_G_F16 = 0, 1, 2
 ARTOPK_OPT_GUESS_MIN_N, ARTOPK_OPT_UPDATE_TILES_MIN_N, ARTOPK_OPT_LEADER_FIRST, ARTOPK_OPT_NONTEMPORAL = 0, 1, 2, 3
 ARTOPK_OPT_STAGE_TILES, ARTOPK_OPT_SHORT_MAX_N = 4, 5
+ARTOPK_PRODUCTS_HALF, ARTOPK_PRODUCTS_SPLIT = 0, 1
 PROF_NAMES = ("pass_a", "select", "gather", "update", "total")
 
 _SYMBOLS = (
@@ -26,6 +27,10 @@ _SYMBOLS = (
     "artopk_apply_update", "artopk_topk_workers", "artopk_select_info", "artopk_step_g16",
     "artopk_set_option", "artopk_get_option", "artopk_variance_static", "artopk_set_step_counter",
     "artopk_scratch_bytes",
+    "artopk_norm_create", "artopk_norm_scratch_bytes", "artopk_norm_destroy", "artopk_norm_last_error",
+    "artopk_layernorm_forward", "artopk_layernorm_backward",
+    "artopk_matrices_create", "artopk_matrices_scratch_bytes", "artopk_matrices_destroy",
+    "artopk_matrices_last_error", "artopk_orthogonalize", "artopk_muon_step",
 )
 
 
@@ -59,7 +64,6 @@ def load_library():
     lib.artopk_create.argtypes = [C.POINTER(vp), i32, i64, i64, i32, vp]
     lib.artopk_destroy.argtypes = [vp]
     lib.artopk_last_error.argtypes = [vp]
-    lib.artopk_last_error.restype = C.c_char_p
     lib.artopk_status.argtypes = [vp]
     lib.artopk_variance.argtypes = [vp, vp, i32, i64, vp, vp]
     lib.artopk_select_topk.argtypes = [vp, vp, i64, i32, vp, vp, i64, vp]
@@ -79,10 +83,26 @@ def load_library():
     lib.artopk_variance_static.argtypes = [vp, i32, i64, vp, vp, vp]
     lib.artopk_set_step_counter.argtypes = [vp, C.c_uint64]
     lib.artopk_scratch_bytes.argtypes = [i32, i64, i64, i32]
+    f32 = C.c_float
+    lib.artopk_norm_create.argtypes = [C.POINTER(vp), i64, i64, vp]
+    lib.artopk_norm_scratch_bytes.argtypes = [i64, i64]
+    lib.artopk_norm_destroy.argtypes = [vp]
+    lib.artopk_norm_last_error.argtypes = [vp]
+    lib.artopk_layernorm_forward.argtypes = [vp, vp, i64, i32, i64, i64, vp, vp, f32, vp, i64, vp, vp]
+    lib.artopk_layernorm_backward.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, vp, vp, vp, i64, vp, vp, i32, i32]
+    lib.artopk_matrices_create.argtypes = [C.POINTER(vp), vp, i32, i64, i32, i32, vp]
+    lib.artopk_matrices_scratch_bytes.argtypes = [vp, i32, i64, i32, i32]
+    lib.artopk_matrices_destroy.argtypes = [vp]
+    lib.artopk_matrices_last_error.argtypes = [vp]
+    lib.artopk_orthogonalize.argtypes = [vp, vp, vp, i32, vp, f32]
+    lib.artopk_muon_step.argtypes = [vp, vp, vp, vp, f32, f32, i32, f32, f32, f32, i32, vp, f32]
     lib.artopk_version.restype = i32
-    lib.artopk_scratch_bytes.restype = i64
     for name in _SYMBOLS:
-        if name not in ("artopk_last_error", "artopk_version", "artopk_scratch_bytes"):
+        if name.endswith("_scratch_bytes"):
+            getattr(lib, name).restype = i64
+        elif name.endswith("_last_error"):
+            getattr(lib, name).restype = C.c_char_p
+        elif name != "artopk_version":
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -241,3 +261,184 @@ class Context:
                                               _i64_array(seg_off), _i64_array(seg_k), k, mode, step, fixed_leader,
                                               _ptr(leader_out), _ptr(var_out), _ptr(idx_out), _ptr(vals_out),
                                               _ptr(sum_out), _ptr(update_out)))
+
+
+def _elem_type(t) -> int:
+    """ARTOPK_G_* of a tensor's elements."""
+    import torch
+
+    types = {torch.float32: ARTOPK_G_F32, torch.bfloat16: ARTOPK_G_BF16, torch.float16: ARTOPK_G_F16}
+    if t.dtype not in types:
+        raise ArTopkError(-1, f"elements of type {t.dtype} are not taken")
+    return types[t.dtype]
+
+
+def _rows(t, name: str):
+    """(address, distance of rows, rows, cols) of a matrix whose columns lie side by side."""
+    if t.dim() != 2:
+        raise ArTopkError(-1, f"{name} has {t.dim()} dimensions, not 2")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ArTopkError(-1, f"{name}'s columns do not lie side by side")
+    return _ptr(t), (t.stride(0) if rows > 1 else cols), rows, cols
+
+
+def _vector(t, name: str, length: int, dtype=None) -> Optional[int]:
+    """Address of a contiguous vector of `length` elements (of `dtype`), or None for None."""
+    if t is None:
+        return None
+    if t.numel() != length or not t.is_contiguous():
+        raise ArTopkError(-1, f"{name} is not a contiguous vector of {length} elements")
+    if dtype is not None and t.dtype != dtype:
+        raise ArTopkError(-1, f"{name} is {t.dtype}, not {dtype}")
+    return _ptr(t)
+
+
+def _coefficients(steps: int, coefficients):
+    """steps x 3 floats from None, one (a, b, c) for all steps, or one for each."""
+    if coefficients is None:
+        return None
+    rows = [coefficients] * steps if len(coefficients) == 3 and not hasattr(coefficients[0], "__len__") else coefficients
+    if len(rows) != steps or any(len(r) != 3 for r in rows):
+        raise ArTopkError(-1, f"coefficients are not (a, b, c) or {steps} of these")
+    return (C.c_float * (3 * max(steps, 1)))(*[float(v) for r in rows for v in r])
+
+
+class _Handle:
+    """A library handle bound to the current torch stream of the current device."""
+
+    _name = ""
+
+    def _open(self, stream: Optional[int], *args):
+        import torch
+
+        if not torch.cuda.is_available():
+            raise RuntimeError("the AR-Topk library needs a GPU; there is no CPU path")
+        self._lib = load_library()
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        h = C.c_void_p()
+        rc = getattr(self._lib, f"artopk_{self._name}_create")(C.byref(h), *args, C.c_void_p(stream))
+        if rc != 0:
+            raise ArTopkError(rc, self._lib.artopk_last_error(None).decode())
+        self._h = h
+
+    def _check(self, rc: int):
+        if rc != 0:
+            raise ArTopkError(rc, getattr(self._lib, f"artopk_{self._name}_last_error")(self._h).decode())
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            getattr(self._lib, f"artopk_{self._name}_destroy")(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def artopk_norm_scratch_bytes(max_rows: int, max_cols: int) -> int:
+    """Device bytes a NormContext of these limits allocates (-1: limits refused); needs no GPU."""
+    return int(load_library().artopk_norm_scratch_bytes(int(max_rows), int(max_cols)))
+
+
+class NormContext(_Handle):
+    """Owns one artopk_norm: layer norms of up to max_rows rows of up to max_cols elements."""
+
+    _name = "norm"
+
+    def __init__(self, max_rows: int, max_cols: int, stream: Optional[int] = None):
+        self._open(stream, int(max_rows), int(max_cols))
+
+    def artopk_layernorm_forward(self, x, gamma, beta, y, mean_out=None, rstd_out=None, eps: float = 1e-5):
+        import torch
+
+        px, sx, rows, cols = _rows(x, "x")
+        py, sy, *shape = _rows(y, "y")
+        if shape != [rows, cols] or y.dtype != x.dtype:
+            raise ArTopkError(-1, "y's shape or type is not x's")
+        self._check(self._lib.artopk_layernorm_forward(
+            self._h, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, torch.float32),
+            _vector(beta, "beta", cols, torch.float32), C.c_float(eps), py, sy,
+            _vector(mean_out, "mean_out", rows, torch.float32), _vector(rstd_out, "rstd_out", rows, torch.float32)))
+
+    def artopk_layernorm_backward(self, dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, accumulate: bool = False):
+        import torch
+
+        px, sx, rows, cols = _rows(x, "x")
+        pd, sd, *shape = _rows(dy, "dy")
+        if shape != [rows, cols] or dy.dtype != x.dtype:
+            raise ArTopkError(-1, "dy's shape or type is not x's")
+        po, so = None, cols
+        if dx is not None:
+            po, so, *shape = _rows(dx, "dx")
+            if shape != [rows, cols] or dx.dtype != x.dtype:
+                raise ArTopkError(-1, "dx's shape or type is not x's")
+        grads = [g for g in (dgamma, dbeta) if g is not None]
+        if len(grads) == 2 and grads[0].dtype != grads[1].dtype:
+            raise ArTopkError(-1, "dgamma and dbeta are of different types")
+        self._check(self._lib.artopk_layernorm_backward(
+            self._h, pd, sd, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, torch.float32),
+            _vector(mean, "mean", rows, torch.float32), _vector(rstd, "rstd", rows, torch.float32), po, so,
+            _vector(dgamma, "dgamma", cols), _vector(dbeta, "dbeta", cols),
+            _elem_type(grads[0]) if grads else ARTOPK_G_F32, int(accumulate)))
+
+
+class _Matrix(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32), ("scale", C.c_float)]
+
+
+def _matrix_table(matrices: Sequence):
+    table = (_Matrix * max(1, len(matrices)))()
+    for i, m in enumerate(matrices):
+        offset, rows, cols = (int(v) for v in m[:3])
+        table[i] = _Matrix(offset, rows, cols, float(m[3]) if len(m) > 3 else 1.0)
+    return table
+
+
+def artopk_matrices_scratch_bytes(matrices: Sequence, n: int, elem_type: int = ARTOPK_G_F32,
+                                  products: Optional[int] = None) -> int:
+    """Device bytes a MatrixContext of these arguments allocates (-1: refused); needs no GPU."""
+    return int(load_library().artopk_matrices_scratch_bytes(_matrix_table(matrices), len(matrices), int(n),
+                                                            int(elem_type), _products(elem_type, products)))
+
+
+def _products(elem_type: int, products: Optional[int]) -> int:
+    """SPLIT for float32 elements, HALF for 16-bit ones (whose own rounding is as large), unless told."""
+    if products is not None:
+        return int(products)
+    return ARTOPK_PRODUCTS_SPLIT if elem_type == ARTOPK_G_F32 else ARTOPK_PRODUCTS_HALF
+
+
+class MatrixContext(_Handle):
+    """Owns one artopk_matrices: matrices (offset, rows, cols[, scale]) of a flat vector of n elements."""
+
+    _name = "matrices"
+
+    def __init__(self, matrices: Sequence, n: int, elem_type: int = ARTOPK_G_F32, products: Optional[int] = None,
+                 stream: Optional[int] = None):
+        self.n, self.elem_type = int(n), int(elem_type)
+        self._open(stream, _matrix_table(matrices), len(matrices), self.n, self.elem_type,
+                   _products(self.elem_type, products))
+
+    def _flat(self, t, name: str) -> Optional[int]:
+        if t is not None and _elem_type(t) != self.elem_type:
+            raise ArTopkError(-1, f"{name} is {t.dtype}, which is not the handle's type")
+        return _vector(t, name, self.n)
+
+    def artopk_orthogonalize(self, x, out, steps: int = 5, coefficients=None, eps: float = 1e-7):
+        self._check(self._lib.artopk_orthogonalize(self._h, self._flat(x, "x"), self._flat(out, "out"), int(steps),
+                                                   _coefficients(int(steps), coefficients), C.c_float(eps)))
+
+    def artopk_muon_step(self, weights, momentum, update, eta: float, mu: float = 0.95, nesterov: bool = True,
+                         decay: float = 0.0, eta_rest: float = 0.0, update_scale: float = 1.0, steps: int = 5,
+                         coefficients=None, eps: float = 1e-7):
+        import torch
+
+        self._check(self._lib.artopk_muon_step(
+            self._h, self._flat(weights, "weights"), _vector(momentum, "momentum", self.n, torch.float32),
+            _vector(update, "update", self.n, torch.float32), C.c_float(update_scale), C.c_float(mu), int(nesterov),
+            C.c_float(eta), C.c_float(decay), C.c_float(eta_rest), int(steps), _coefficients(int(steps), coefficients),
+            C.c_float(eps)))

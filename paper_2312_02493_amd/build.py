@@ -22,24 +22,44 @@ HIPCC_FLAGS = [
 ]
 
 
-def build(verbose: bool = False) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    src = os.path.join(HERE, "csrc", "artopk.hip")
-    runs = []
-    for path, flags in ((LIB_PATH, []), (HELD_PATH, ["-DARTOPK_HELD_BLOCKS"])):
-        cmd = [hipcc, *HIPCC_FLAGS, *flags, "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-               src, "-o", path + ".tmp"]
+# operators around the step, in both libraries
+PART_SOURCES = ("norm.hip", "matrices.hip")
+
+
+def _run_all(runs, verbose: bool):
+    """Runs the commands side by side; raises if one fails."""
+    procs = []
+    for name, cmd in runs:
         if verbose:
             print(" ".join(cmd), flush=True)
-        runs.append((path, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)))
-    for path, proc in runs:
+        procs.append((name, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)))
+    failed = []
+    for name, proc in procs:
         out, err = proc.communicate()
         if proc.returncode != 0:
             sys.stderr.write(out + err)
-            raise RuntimeError(f"hipcc failed building {os.path.basename(path)}")
-        if verbose and err.strip():
+            failed.append(name)
+        elif verbose and err.strip():
             sys.stderr.write(err)
-    for path, _ in runs:
+    if failed:
+        raise RuntimeError(f"hipcc failed building {', '.join(failed)}")
+
+
+def build(verbose: bool = False) -> str:
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    src = os.path.join(HERE, "csrc", "artopk.hip")
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"] + ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+    objects = os.path.join(HERE, "csrc", "_build")
+    os.makedirs(objects, exist_ok=True)
+    parts = [os.path.join(objects, name.replace(".hip", ".o")) for name in PART_SOURCES]
+    mains = [(path, os.path.join(objects, os.path.basename(path).replace(".so", ".o")), more)
+             for path, more in ((LIB_PATH, []), (HELD_PATH, ["-DARTOPK_HELD_BLOCKS"]))]
+    _run_all([(name, [hipcc, *flags, "-c", os.path.join(HERE, "csrc", name), "-o", obj])
+              for name, obj in zip(PART_SOURCES, parts)] +
+             [(os.path.basename(path), [hipcc, *flags, *more, "-c", src, "-o", obj]) for path, obj, more in mains], verbose)
+    _run_all([(os.path.basename(path), [hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", obj, *parts, "-o", path + ".tmp"])
+              for path, obj, _ in mains], verbose)
+    for path, _, _ in mains:
         os.replace(path + ".tmp", path)
     build_abi_client(hipcc, verbose)
     return LIB_PATH

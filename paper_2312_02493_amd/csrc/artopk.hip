@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "artopk_kernels.h"
+#include "host_common.h"
 
 using namespace artopk;
 
@@ -187,20 +188,22 @@ struct artopk_ctx {
   int cur = 0;          // ring slot of the call being recorded
   char err[512] = {0};
 };
-static_assert(sizeof(artopk_ctx::err) == 512, "fail() writes up to 512 bytes");
-
-namespace {
+static_assert(sizeof(artopk_ctx::err) == kErrText, "fail() writes up to this many bytes");
 
 // error text of calls that have no context (artopk_last_error(NULL) returns it)
-thread_local char g_noctx_err[512] = {0};
+__thread char artopk::g_noctx_err[artopk::kErrText] = {0};
+
+namespace {
 
 int fail(artopk_ctx* c, int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(c ? c->err : g_noctx_err, sizeof(g_noctx_err), fmt, ap);
+  vsnprintf(c ? c->err : g_noctx_err, kErrText, fmt, ap);
   va_end(ap);
   return code;
 }
+
+char* err_of(artopk_ctx* c) { return c ? c->err : g_noctx_err; }
 
 #define HIP_TRY(ctx, expr)                                                                   \
   do {                                                                                       \
@@ -209,10 +212,6 @@ int fail(artopk_ctx* c, int code, const char* fmt, ...) {
       return fail((ctx), ARTOPK_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), \
                   __FILE__, __LINE__);                                                       \
   } while (0)
-
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int check_ptr_table(artopk_ctx* c, const float* const* tab, int32_t w, const char* name, int align = 16) {
   if (!tab) return fail(c, ARTOPK_EINVAL, "%s is NULL", name);
@@ -255,54 +254,6 @@ int check_segments(artopk_ctx* c, int64_t n, int32_t nseg, const int64_t* seg_of
   if (ksum != k) return fail(c, ARTOPK_EINVAL, "sum of seg_k (%lld) differs from k (%lld)", (long long)ksum, (long long)k);
   return ARTOPK_OK;
 }
-
-// The buffers of one call as byte ranges.  Ranges that are only read may overlap each other
-// (two workers may share a gradient buffer); a range that is written must not overlap any other.
-class RangeSet {
- public:
-  void add(const void* p, size_t bytes, bool written, const char* name, int index = -1) {
-    if (!p || bytes == 0 || n_ >= kCap) return;
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-    r_[n_++] = Range{lo, lo + bytes, written, name, index};
-  }
-  void add_table(const void* const* tab, int32_t w, size_t bytes, bool written, const char* name) {
-    for (int i = 0; i < w; ++i) add(tab[i], bytes, written, name, i);
-  }
-  // ARTOPK_OK, or ARTOPK_EINVAL with the first offending pair in the context's error text
-  int check(artopk_ctx* c) {
-    std::sort(r_, r_ + n_, [](const Range& a, const Range& b) { return a.lo < b.lo; });
-    int far_any = -1, far_written = -1;  // ranges seen so far that reach furthest: any, written ones
-    for (int i = 0; i < n_; ++i) {
-      const int other = r_[i].written ? far_any : far_written;
-      if (other >= 0 && r_[i].lo < r_[other].hi) {
-        char a[48], b[48];
-        label(r_[other], a, sizeof(a));
-        label(r_[i], b, sizeof(b));
-        return fail(c, ARTOPK_EINVAL, "buffers %s and %s overlap", a, b);
-      }
-      if (far_any < 0 || r_[i].hi > r_[far_any].hi) far_any = i;
-      if (r_[i].written && (far_written < 0 || r_[i].hi > r_[far_written].hi)) far_written = i;
-    }
-    return ARTOPK_OK;
-  }
-
- private:
-  struct Range {
-    uintptr_t lo, hi;
-    bool written;
-    const char* name;
-    int index;
-  };
-  static void label(const Range& r, char* out, size_t cap) {
-    if (r.index >= 0)
-      snprintf(out, cap, "%s[%d]", r.name, r.index);
-    else
-      snprintf(out, cap, "%s", r.name);
-  }
-  static constexpr int kCap = 2 * kMaxW + 8;
-  Range r_[kCap];
-  int n_ = 0;
-};
 
 PtrTable make_table(const float* const* tab, int32_t w) {
   PtrTable t;
@@ -1709,7 +1660,7 @@ int artopk_variance(artopk_ctx* ctx, const float* const* x, int32_t w, int64_t n
     rs.add_table(reinterpret_cast<const void* const*>(x), w, (size_t)n * 4, false, "x");
     rs.add(var_out, (size_t)w * 8, true, "var_out");
     rs.add(argmax_out, 4, true, "argmax_out");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   const PtrTable tab = make_table(x, w);
   const int nblk = stats_blocks(ctx->num_cu, w, n);
@@ -1774,7 +1725,7 @@ int artopk_variance_static(const float* const* x, int32_t w, int64_t n, double* 
     rs.add_table(reinterpret_cast<const void* const*>(x), w, (size_t)n * 4, false, "x");
     rs.add(var_out, (size_t)w * 8, true, "var_out");
     rs.add(argmax_out, 4, true, "argmax_out");
-    if ((rc = rs.check(nullptr))) return rc;
+    if ((rc = rs.check(err_of(nullptr)))) return rc;
   }
   const StaticDevice* sd = nullptr;
   if ((rc = static_device(&sd))) return rc;
@@ -1804,7 +1755,7 @@ int artopk_select_topk(artopk_ctx* ctx, const float* acc, int64_t n, int32_t nse
     RangeSet rs;
     rs.add(acc, (size_t)n * 4, false, "acc");
     rs.add(idx_out, (size_t)k * 4, true, "idx_out");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   const float* one[1] = {acc};
   const PtrTable tab = make_table(one, 1);
@@ -1838,7 +1789,7 @@ int artopk_gather_sum(artopk_ctx* ctx, const float* const* acc, int32_t w, int64
     rs.add(idx, (size_t)k * 4, false, "idx");
     rs.add(vals_out, (size_t)w * (size_t)k * 4, true, "vals_out");
     rs.add(sum_out, (size_t)k * 4, true, "sum_out");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   const PtrTable tab = make_table(acc, w);
   return enqueue_gather(ctx, tab, w, n, idx, k, vals_out, sum_out, false);
@@ -1857,7 +1808,7 @@ int artopk_scatter_residual(artopk_ctx* ctx, float* const* residual, int32_t w, 
     rs.add(idx, (size_t)k * 4, false, "idx");
     rs.add(sum, (size_t)k * 4, false, "sum");
     rs.add(update, (size_t)n * 4, true, "update");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   const PtrTable tab = make_table(residual, w);
   const int blocks = (int)((k + 255) / 256);
@@ -1879,7 +1830,7 @@ int artopk_topk_workers(artopk_ctx* ctx, const float* const* acc, int32_t w, int
     rs.add(vals_out, (size_t)w * (size_t)k * 4, true, "vals_out");
     rs.add(sqnorm_out, (size_t)w * 8, true, "sqnorm_out");
     rs.add(argmax_out, 4, true, "argmax_out");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   const PtrTable tab = make_table(acc, w);
   return enqueue_topk_workers(ctx, tab, w, n, k, idx_out, vals_out ? vals_out : ctx->s.vals, sqnorm_out,
@@ -1897,7 +1848,7 @@ int artopk_compression_gain(artopk_ctx* ctx, const float* const* residual, int32
     rs.add_table(reinterpret_cast<const void* const*>(residual), w, (size_t)n * 4, false, "residual");
     rs.add(vals, (size_t)w * (size_t)k * 4, false, "vals");
     rs.add(gain_out, (size_t)w * 8, true, "gain_out");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   Scratch& s = ctx->s;
   const PtrTable rtab = make_table(residual, w);
@@ -1934,7 +1885,7 @@ int artopk_apply_update(artopk_ctx* ctx, float* weights, int64_t n, const int32_
     rs.add(weights, (size_t)n * 4, true, "weights");
     rs.add(idx, (size_t)k * 4, false, "idx");
     rs.add(sum, (size_t)k * 4, false, "sum");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   const int blocks = (int)((k + 255) / 256);
   hipLaunchKernelGGL(k_apply_update, dim3(blocks), dim3(256), 0, ctx->stream, weights, n, idx, sum, k, eta,
@@ -1984,7 +1935,7 @@ int step_impl(artopk_ctx* ctx, const float* const* g, int32_t g_type, float* con
     rs.add(vals_out, (size_t)w * (size_t)k * 4, true, "vals_out");
     rs.add(sum_out, (size_t)k * 4, true, "sum_out");
     rs.add(update_out, (size_t)n * 4, true, "update_out");
-    if ((rc = rs.check(ctx))) return rc;
+    if ((rc = rs.check(err_of(ctx)))) return rc;
   }
   int leader_host = -1;
   if (mode == ARTOPK_STAR) {

@@ -1,0 +1,431 @@
+// Host side of the entry points on matrices of a flat vector: argument checks, layout of the iterates' memory,
+// tables of tiles, launches.
+
+#include "artopk.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "host_common.h"
+#include "matrices_kernels.h"
+
+using namespace artopk;
+
+namespace {
+
+constexpr int kTileClasses = 3;
+constexpr int kTileOf[kTileClasses] = {64, 128, 256};
+constexpr int32_t kMaxMatrices = 65535;
+constexpr int32_t kMaxSide = 65536;
+constexpr float kUsual[3] = {3.4445f, -4.7750f, 2.0315f};
+
+// A list of blocks' work in the tables.
+struct Span {
+  size_t at = 0;  // entries from the table's start
+  int count = 0;
+};
+
+// What creation works out on the host: where everything lies, and the tables.
+struct MatPlan {
+  std::vector<MatDesc> mats;
+  std::vector<MatChunk> chunks;
+  std::vector<MatTile> tiles;
+  Span begin;
+  Span symmetric[kTileClasses], apply[kTileClasses], final_[kTileClasses];
+  int64_t halves = 0;  // of the iterates' memory
+  int32_t sums = 0;
+  // places in the slab
+  size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_mem = 0, total = 0;
+};
+
+int tile_class(int m, int n) {
+  if (m > 512 && n > 512) return 2;
+  if (m > 128) return 1;
+  return 0;
+}
+
+// ARTOPK_OK, or ARTOPK_EINVAL with the reason in `err`.  Throws std::bad_alloc.
+int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products, MatPlan* plan, char* err) {
+  if (!mats) return fail_text(err, ARTOPK_EINVAL, "mats is NULL");
+  if (count < 1 || count > kMaxMatrices) return fail_text(err, ARTOPK_EINVAL, "count=%d outside [1, %d]", count, kMaxMatrices);
+  if (n < 1 || n >= (1ll << 31)) return fail_text(err, ARTOPK_EINVAL, "n=%lld outside [1, 2^31)", (long long)n);
+  if (type != ARTOPK_G_F32 && type != ARTOPK_G_BF16 && type != ARTOPK_G_F16)
+    return fail_text(err, ARTOPK_EINVAL, "unknown element type %d", type);
+  if (products != ARTOPK_PRODUCTS_HALF && products != ARTOPK_PRODUCTS_SPLIT)
+    return fail_text(err, ARTOPK_EINVAL, "unknown kind of products %d", products);
+  const int parts = products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
+  std::vector<int32_t> order(count);
+  for (int i = 0; i < count; ++i) {
+    const artopk_matrix& m = mats[i];
+    if (m.rows < 1 || m.rows > kMaxSide || m.cols < 1 || m.cols > kMaxSide)
+      return fail_text(err, ARTOPK_EINVAL, "matrix %d is %d x %d; sides have to be in [1, %d]", i, m.rows, m.cols, kMaxSide);
+    const int64_t size = (int64_t)m.rows * m.cols;
+    if (m.offset < 0 || size > n || m.offset > n - size)
+      return fail_text(err, ARTOPK_EINVAL, "matrix %d does not lie within the vector", i);
+    if (!std::isfinite(m.scale)) return fail_text(err, ARTOPK_EINVAL, "matrix %d's scale is not finite", i);
+    order[i] = i;
+  }
+  std::sort(order.begin(), order.end(), [&](int a, int b) { return mats[a].offset < mats[b].offset; });
+  for (int i = 1; i < count; ++i) {
+    const artopk_matrix& m = mats[order[i - 1]];
+    if (m.offset + (int64_t)m.rows * m.cols > mats[order[i]].offset)
+      return fail_text(err, ARTOPK_EINVAL, "matrices %d and %d overlap", order[i - 1], order[i]);
+  }
+
+  plan->mats.resize(count);
+  std::vector<int> cls(count);
+  for (int i = 0; i < count; ++i) {
+    const artopk_matrix& m = mats[i];
+    MatDesc& d = plan->mats[i];
+    d.at = m.offset;
+    d.tall = m.rows > m.cols;
+    d.m = std::min(m.rows, m.cols);
+    d.n = std::max(m.rows, m.cols);
+    d.scale = m.scale;
+    cls[i] = tile_class(d.m, d.n);
+    const int tile = kTileOf[cls[i]];
+    d.mp = (d.m + tile - 1) / tile * tile;
+    d.np = (d.n + tile - 1) / tile * tile;
+    const int64_t mn = (int64_t)d.mp * d.np * parts, mm = (int64_t)d.mp * d.mp * parts;
+    d.x = plan->halves;
+    d.xt[0] = d.x + mn;
+    d.xt[1] = d.xt[0] + mn;
+    d.a = d.xt[1] + mn;
+    d.q = d.a + mm;
+    plan->halves = d.q + mm;
+  }
+
+  // pieces of the vector, those of a matrix side by side; at most 512 a matrix, so that every block that needs its norm
+  // can add them up
+  int64_t done = 0;
+  auto loose = [&](int64_t end) {
+    for (; done < end; done += 16384) plan->chunks.push_back(MatChunk{done, std::min(end, done + 16384), -1, 0});
+    done = end;
+  };
+  for (int k = 0; k < count; ++k) {
+    const int i = order[k];
+    MatDesc& d = plan->mats[i];
+    loose(d.at);
+    const int64_t size = (int64_t)d.m * d.n, end = d.at + size;
+    int64_t each = (size + 511) / 512;
+    each = (std::max<int64_t>(each, 8192) + 63) / 64 * 64;
+    d.part = plan->sums;
+    for (; done < end; done += each) plan->chunks.push_back(MatChunk{done, std::min(end, done + each), i, plan->sums++});
+    done = end;
+    d.parts = plan->sums - d.part;
+  }
+  loose(n);
+
+  auto add = [&](int mat, int i, int j) { plan->tiles.push_back(MatTile{(uint32_t)mat, (uint16_t)i, (uint16_t)j}); };
+  auto list = [&](Span* s, auto&& each) {
+    s->at = plan->tiles.size();
+    each();
+    s->count = (int)(plan->tiles.size() - s->at);
+  };
+  list(&plan->begin, [&] {
+    for (int i = 0; i < count; ++i)
+      for (int a = 0; a < plan->mats[i].mp / 64; ++a)
+        for (int b = 0; b < plan->mats[i].np / 64; ++b) add(i, a, b);
+  });
+  for (int c = 0; c < kTileClasses; ++c) {
+    const int tile = kTileOf[c];
+    list(&plan->symmetric[c], [&] {
+      for (int i = 0; i < count; ++i)
+        if (cls[i] == c)
+          for (int a = 0; a < plan->mats[i].mp / tile; ++a)
+            for (int b = 0; b <= a; ++b) add(i, a, b);
+    });
+    list(&plan->apply[c], [&] {
+      for (int i = 0; i < count; ++i)
+        if (cls[i] == c)
+          for (int a = 0; a < plan->mats[i].mp / tile; ++a)
+            for (int b = 0; b < plan->mats[i].np / tile; ++b) add(i, a, b);
+    });
+    list(&plan->final_[c], [&] {
+      for (int i = 0; i < count; ++i)
+        if (cls[i] == c)
+          for (int a = 0; a < plan->mats[i].mp / tile; ++a)
+            for (int b = 0; b < plan->mats[i].np / tile; ++b) {
+              if (plan->mats[i].tall)
+                add(i, b, a);
+              else
+                add(i, a, b);
+            }
+    });
+  }
+  if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
+
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at = align_up(at + bytes, 256);
+    return o;
+  };
+  plan->o_mats = take(plan->mats.size() * sizeof(MatDesc));
+  plan->o_chunks = take(plan->chunks.size() * sizeof(MatChunk));
+  plan->o_tiles = take(plan->tiles.size() * sizeof(MatTile));
+  plan->o_sums = take((size_t)plan->sums * sizeof(double));
+  plan->o_mem = take((size_t)plan->halves * 2);
+  plan->total = at;
+  return ARTOPK_OK;
+}
+
+}  // namespace
+
+struct artopk_matrices {
+  hipStream_t stream = nullptr;
+  int64_t n = 0;
+  int32_t type = 0, parts = 1;
+  int nchunks = 0;
+  Span begin, symmetric[kTileClasses], apply[kTileClasses], final_[kTileClasses];
+  char* slab = nullptr;
+  const MatDesc* mats = nullptr;
+  const MatChunk* chunks = nullptr;
+  const MatTile* tiles = nullptr;
+  double* sums = nullptr;
+  _Float16* mem = nullptr;
+  char err[kErrText] = {0};
+};
+
+namespace {
+
+#define MAT_TRY(h, expr)                                                                                       \
+  do {                                                                                                         \
+    hipError_t e_ = (expr);                                                                                    \
+    if (e_ != hipSuccess)                                                                                      \
+      return fail_text((h)->err, ARTOPK_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, \
+                       __LINE__);                                                                              \
+  } while (0)
+
+// The coefficients of every step, or ARTOPK_EINVAL where the iterates could leave the operands' range: with singular
+// values of at most `most` before a step, the largest of |s (a + b s^2 + c s^4)| and of |a + b s^2 + c s^4| over
+// [0, most] lie at an end or where a derivative is zero.
+int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficients, float (*out)[3]) {
+  if (steps < 0 || steps > ARTOPK_MAX_POLAR_STEPS)
+    return fail_text(h->err, ARTOPK_EINVAL, "steps=%d outside [0, %d]", steps, ARTOPK_MAX_POLAR_STEPS);
+  double most = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    for (int i = 0; i < 3; ++i) out[k][i] = coefficients ? coefficients[3 * k + i] : kUsual[i];
+    const double a = out[k][0], b = out[k][1], c = out[k][2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c))
+      return fail_text(h->err, ARTOPK_EINVAL, "coefficients of step %d are not finite", k);
+    double next = 0.0, factor = std::fabs(a);
+    auto look = [&](double y) {  // y = s^2
+      if (!(y >= 0.0 && y <= most * most)) return;
+      const double q = a + y * (b + c * y);
+      factor = std::max(factor, std::fabs(q));
+      next = std::max(next, std::sqrt(y) * std::fabs(q));
+    };
+    look(most * most);
+    if (c != 0.0) {
+      look(-b / (2.0 * c));
+      const double disc = 9.0 * b * b - 20.0 * a * c;  // of a + 3 b y + 5 c y^2
+      if (disc >= 0.0) {
+        look((-3.0 * b + std::sqrt(disc)) / (10.0 * c));
+        look((-3.0 * b - std::sqrt(disc)) / (10.0 * c));
+      }
+    }
+    if (b != 0.0) look(-a / (3.0 * b));  // (c = 0; an extra point otherwise)
+    if (next > 2.0 || factor > 15.0)
+      return fail_text(h->err, ARTOPK_EINVAL,
+                       "step %d would take singular values up to %.4g to %.4g, with a factor of %.4g; at most 2 and 15 are taken", k,
+                       most, next, factor);
+    most = std::max(next, 1e-30);
+  }
+  return ARTOPK_OK;
+}
+
+template <int TILE, int PARTS, int MODE>
+void product(artopk_matrices* h, const Span& s, int from, const float* co, const FinishArgs& f) {
+  if (s.count)
+    k_mat_product<TILE, PARTS, MODE><<<s.count, product_threads<TILE>(), 0, h->stream>>>(h->mats, h->tiles + s.at, h->mem, from,
+                                                                                        co[0], co[1], co[2], f);
+}
+
+template <int PARTS, int MODE>
+void products(artopk_matrices* h, const Span (&s)[kTileClasses], int from, const float* co, const FinishArgs& f) {
+  product<256, PARTS, MODE>(h, s[2], from, co, f);
+  product<128, PARTS, MODE>(h, s[1], from, co, f);
+  product<64, PARTS, MODE>(h, s[0], from, co, f);
+}
+
+template <int PARTS, class From>
+void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], float eps, const FinishArgs& f) {
+  if (steps == 0) {
+    k_mat_scaled<From><<<h->nchunks, 256, 0, h->stream>>>(from, h->mats, h->chunks, h->sums, eps, f);
+    return;
+  }
+  k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->mats, h->tiles + h->begin.at, h->sums, eps, h->mem);
+  for (int k = 0; k < steps; ++k) {
+    products<PARTS, kGram>(h, h->symmetric, k & 1, co[k], f);
+    products<PARTS, kSquare>(h, h->symmetric, k & 1, co[k], f);
+    if (k + 1 < steps)
+      products<PARTS, kApply>(h, h->apply, k & 1, co[k], f);
+    else
+      products<PARTS, kFinal>(h, h->final_, k & 1, co[k], f);
+  }
+}
+
+template <class From>
+void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], float eps, const FinishArgs& f) {
+  if (h->parts == 2)
+    polar<2>(h, from, steps, co, eps, f);
+  else
+    polar<1>(h, from, steps, co, eps, f);
+}
+
+// Calls f with a null pointer of the handle's element type.
+template <class F>
+void with_type(int32_t type, F&& f) {
+  if (type == ARTOPK_G_F32) f((float*)nullptr);
+  else if (type == ARTOPK_G_BF16) f((__bf16*)nullptr);
+  else f((_Float16*)nullptr);
+}
+
+size_t elem_size(int32_t type) { return type == ARTOPK_G_F32 ? 4 : 2; }
+
+int check_vector(artopk_matrices* h, const char* name, const void* p, size_t size) {
+  if (!p) return fail_text(h->err, ARTOPK_EINVAL, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % size) return fail_text(h->err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
+  return ARTOPK_OK;
+}
+
+int check_eps(artopk_matrices* h, float eps) {
+  if (!(eps > 0.0f) || !std::isfinite(eps)) return fail_text(h->err, ARTOPK_EINVAL, "eps has to be positive and finite");
+  return ARTOPK_OK;
+}
+
+}  // namespace
+
+int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products) {
+  try {
+    MatPlan plan;
+    if (make_plan(mats, count, n, type, products, &plan, g_noctx_err)) return -1;
+    return (int64_t)plan.total;
+  } catch (const std::exception&) {
+    return -1;
+  }
+}
+
+int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
+                           int32_t products, void* hip_stream) {
+  if (!out) return fail_text(g_noctx_err, ARTOPK_EINVAL, "out is NULL");
+  MatPlan plan;
+  try {
+    const int rc = make_plan(mats, count, n, type, products, &plan, g_noctx_err);
+    if (rc) return rc;
+  } catch (const std::exception&) {
+    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "out of host memory");
+  }
+  artopk_matrices* h = new (std::nothrow) artopk_matrices();
+  if (!h) return fail_text(g_noctx_err, ARTOPK_ENOMEM, "out of host memory");
+  h->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  h->n = n;
+  h->type = type;
+  h->parts = products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
+  h->nchunks = (int)plan.chunks.size();
+  h->begin = plan.begin;
+  for (int c = 0; c < kTileClasses; ++c) {
+    h->symmetric[c] = plan.symmetric[c];
+    h->apply[c] = plan.apply[c];
+    h->final_[c] = plan.final_[c];
+  }
+  void* p = nullptr;
+  hipError_t e = hipMalloc(&p, plan.total);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "hipMalloc of %lld bytes failed: %s", (long long)plan.total, hipGetErrorString(e));
+  }
+  h->slab = static_cast<char*>(p);
+  h->mats = reinterpret_cast<const MatDesc*>(h->slab + plan.o_mats);
+  h->chunks = reinterpret_cast<const MatChunk*>(h->slab + plan.o_chunks);
+  h->tiles = reinterpret_cast<const MatTile*>(h->slab + plan.o_tiles);
+  h->sums = reinterpret_cast<double*>(h->slab + plan.o_sums);
+  h->mem = reinterpret_cast<_Float16*>(h->slab + plan.o_mem);
+  e = hipMemcpy(h->slab + plan.o_mats, plan.mats.data(), plan.mats.size() * sizeof(MatDesc), hipMemcpyHostToDevice);
+  if (e == hipSuccess)
+    e = hipMemcpy(h->slab + plan.o_chunks, plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk), hipMemcpyHostToDevice);
+  if (e == hipSuccess)
+    e = hipMemcpy(h->slab + plan.o_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MatTile), hipMemcpyHostToDevice);
+  if (e != hipSuccess) {
+    (void)hipFree(h->slab);
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "hipMemcpy failed: %s", hipGetErrorString(e));
+  }
+  *out = h;
+  return ARTOPK_OK;
+}
+
+int artopk_matrices_destroy(artopk_matrices* m) {
+  if (!m) return ARTOPK_EINVAL;
+  if (m->slab) (void)hipFree(m->slab);
+  delete m;
+  return ARTOPK_OK;
+}
+
+const char* artopk_matrices_last_error(const artopk_matrices* m) { return m ? m->err : g_noctx_err; }
+
+int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t steps, const float* coefficients, float eps) {
+  if (!m) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_orthogonalize: m is NULL");
+  int rc;
+  float co[ARTOPK_MAX_POLAR_STEPS][3];
+  const size_t size = elem_size(m->type);
+  if ((rc = check_vector(m, "x", x, size)) || (rc = check_vector(m, "out", out, size))) return rc;
+  if ((rc = take_coefficients(m, steps, coefficients, co)) || (rc = check_eps(m, eps))) return rc;
+  {
+    RangeSet rs;
+    rs.add(x, (size_t)m->n * size, false, "x");
+    rs.add(out, (size_t)m->n * size, true, "out");
+    if ((rc = rs.check(m->err))) return rc;
+  }
+  FinishArgs f = {};
+  f.out = out;
+  f.type = m->type;
+  with_type(m->type, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    k_mat_squares<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), m->chunks, m->sums);
+    polar(m, FromVector<T>{static_cast<const T*>(x)}, steps, co, eps, f);
+  });
+  MAT_TRY(m, hipGetLastError());
+  return ARTOPK_OK;
+}
+
+int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const float* update, float update_scale, float mu,
+                     int32_t nesterov, float eta, float decay, float eta_rest, int32_t steps, const float* coefficients,
+                     float eps) {
+  if (!m) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_muon_step: m is NULL");
+  int rc;
+  float co[ARTOPK_MAX_POLAR_STEPS][3];
+  const size_t size = elem_size(m->type);
+  if ((rc = check_vector(m, "weights", weights, size)) || (rc = check_vector(m, "momentum", momentum, 4)) ||
+      (rc = check_vector(m, "update", update, 4)))
+    return rc;
+  if (!std::isfinite(update_scale) || !std::isfinite(mu) || !std::isfinite(eta) || !std::isfinite(decay) ||
+      !std::isfinite(eta_rest))
+    return fail_text(m->err, ARTOPK_EINVAL, "update_scale, mu, eta, decay or eta_rest is not finite");
+  if ((rc = take_coefficients(m, steps, coefficients, co)) || (rc = check_eps(m, eps))) return rc;
+  {
+    RangeSet rs;
+    rs.add(weights, (size_t)m->n * size, true, "weights");
+    rs.add(momentum, (size_t)m->n * 4, true, "momentum");
+    rs.add(update, (size_t)m->n * 4, false, "update");
+    if ((rc = rs.check(m->err))) return rc;
+  }
+  FinishArgs f = {};
+  f.out = weights;
+  f.type = m->type;
+  f.muon = 1;
+  f.a = MuonArgs{mu, update_scale, nesterov != 0, eta, (float)(1.0 - (double)eta * (double)decay), eta_rest};
+  with_type(m->type, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    k_mat_momentum<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<T*>(weights), momentum, update, f.a, m->chunks, m->sums);
+  });
+  polar(m, FromMomentum{momentum, update, f.a}, steps, co, eps, f);
+  MAT_TRY(m, hipGetLastError());
+  return ARTOPK_OK;
+}

@@ -1,0 +1,297 @@
+// Host side of the layer norm entry points: argument checks, the choice of a kernel's shape, launches.
+
+#include "artopk.h"
+
+#include <hip/hip_runtime.h>
+
+#include <new>
+
+#include "host_common.h"
+#include "norm_kernels.h"
+
+using namespace artopk;
+
+struct artopk_norm {
+  hipStream_t stream = nullptr;
+  int num_cu = 256;
+  int64_t max_rows = 0, max_cols = 0;
+  float* part = nullptr;  // the blocks' shares of the weight gradients
+  char err[kErrText] = {0};
+};
+
+namespace {
+
+constexpr int64_t kRegisterCols = 16384;  // longest row that a block's registers hold
+constexpr int kMaxShares = 1024;          // blocks of a backward pass, at most
+constexpr int kLongShares = 64;
+
+#define NORM_TRY(h, expr)                                                                                      \
+  do {                                                                                                         \
+    hipError_t e_ = (expr);                                                                                    \
+    if (e_ != hipSuccess)                                                                                      \
+      return fail_text((h)->err, ARTOPK_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, \
+                       __LINE__);                                                                              \
+  } while (0)
+
+bool valid_limits(int64_t max_rows, int64_t max_cols) {
+  return max_rows >= 1 && max_rows < (1ll << 31) && max_cols >= 1 && max_cols < (1ll << 31);
+}
+
+int64_t shares_limit(int64_t max_rows, int64_t max_cols) {
+  const int64_t most = max_cols > kRegisterCols ? kLongShares : kMaxShares;
+  return max_rows < most ? max_rows : most;
+}
+
+// Floats of scratch; shorter rows than max_cols have more shares, but no more floats than the longest kept in registers.
+int64_t part_floats(int64_t max_rows, int64_t max_cols) {
+  const int64_t in_regs = max_cols < kRegisterCols ? max_cols : kRegisterCols;
+  int64_t f = 2 * shares_limit(max_rows, in_regs) * in_regs;
+  if (max_cols > kRegisterCols) {
+    const int64_t g = 2 * shares_limit(max_rows, max_cols) * max_cols;
+    if (g > f) f = g;
+  }
+  return f;
+}
+
+size_t elem_size(int32_t type) { return type == ARTOPK_G_F32 ? 4 : 2; }
+
+bool known_type(int32_t type) { return type == ARTOPK_G_F32 || type == ARTOPK_G_BF16 || type == ARTOPK_G_F16; }
+
+int check_rows(artopk_norm* h, const char* name, const void* p, int64_t stride, int32_t type, int64_t rows, int64_t cols) {
+  if (!p && rows > 0) return fail_text(h->err, ARTOPK_EINVAL, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % elem_size(type))
+    return fail_text(h->err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
+  if (rows > 1 && stride < cols)
+    return fail_text(h->err, ARTOPK_EINVAL, "%s's rows are %lld apart and %lld long", name, (long long)stride, (long long)cols);
+  if (stride < 0 || stride >= (1ll << 40)) return fail_text(h->err, ARTOPK_EINVAL, "%s's stride is outside [0, 2^40)", name);
+  return ARTOPK_OK;
+}
+
+int check_problem(artopk_norm* h, int32_t type, int64_t rows, int64_t cols) {
+  if (!known_type(type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type %d", type);
+  if (rows < 0 || rows > h->max_rows)
+    return fail_text(h->err, ARTOPK_EINVAL, "rows=%lld outside [0, %lld]", (long long)rows, (long long)h->max_rows);
+  if (cols < 1 || cols > h->max_cols)
+    return fail_text(h->err, ARTOPK_EINVAL, "cols=%lld outside [1, %lld]", (long long)cols, (long long)h->max_cols);
+  return ARTOPK_OK;
+}
+
+int check_floats(artopk_norm* h, const char* name, const void* p, size_t size = 4) {
+  if (reinterpret_cast<uintptr_t>(p) % size)
+    return fail_text(h->err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
+  return ARTOPK_OK;
+}
+
+size_t rows_bytes(int64_t stride, int64_t rows, int64_t cols, int32_t type) {
+  return rows ? ((size_t)(rows - 1) * (size_t)stride + (size_t)cols) * elem_size(type) : 0;
+}
+
+// Whether rows at p can be read sixteen bytes at a time.
+bool wide_rows(const void* p, int64_t stride, int64_t rows, size_t size) {
+  return aligned16(p) && (rows <= 1 || stride * (int64_t)size % 16 == 0);
+}
+
+// Calls f(V, threads of a row, elements of a thread) as compile-time constants: the fewest threads that hold the row, a
+// wave where it does.
+template <int V, class F>
+void with_shape(int64_t cols, F&& f) {
+  if (cols <= 512) return f(std::integral_constant<int, V>(), std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
+  if (cols <= 1024) return f(std::integral_constant<int, V>(), std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+  if (cols <= 2048) return f(std::integral_constant<int, V>(), std::integral_constant<int, 256>(), std::integral_constant<int, 8>());
+  if (cols <= 4096) return f(std::integral_constant<int, V>(), std::integral_constant<int, 256>(), std::integral_constant<int, 16>());
+  if (cols <= 8192) return f(std::integral_constant<int, V>(), std::integral_constant<int, 512>(), std::integral_constant<int, 16>());
+  return f(std::integral_constant<int, V>(), std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
+}
+
+template <class T>
+void forward(artopk_norm* h, const T* x, int64_t x_stride, int64_t rows, int64_t cols, const float* gamma,
+             const float* beta, float eps, T* y, int64_t y_stride, float* mean, float* rstd) {
+  if (cols > kRegisterCols) {
+    const int blocks = (int)std::min<int64_t>(rows, 2 * h->num_cu);
+    k_norm_forward_long<T><<<blocks, 1024, 0, h->stream>>>(x, x_stride, rows, cols, gamma, beta, eps, y, y_stride, mean, rstd);
+    return;
+  }
+  auto go = [&](auto V, auto TPR, auto E) {
+    using S = NormShape<TPR()>;
+    const int64_t units = (rows + S::kRows - 1) / S::kRows;
+    const int blocks = (int)std::min<int64_t>(units, (int64_t)h->num_cu * (2048 / S::kThreads) * 4);
+    k_norm_forward<T, V(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(x, x_stride, rows, (int)cols, gamma, beta, eps,
+                                                                              y, y_stride, mean, rstd);
+  };
+  constexpr int kWide = 16 / sizeof(T);
+  if (cols % kWide == 0 && wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(y, y_stride, rows, sizeof(T)))
+    with_shape<kWide>(cols, go);
+  else
+    with_shape<1>(cols, go);
+}
+
+// Returns the number of shares of the weight gradients.
+template <class T>
+int backward(artopk_norm* h, const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int64_t cols,
+             const float* gamma, const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* part) {
+  int shares = 0;
+  if (cols > kRegisterCols) {
+    if (dx) {
+      const int blocks = (int)std::min<int64_t>(rows, 2 * h->num_cu);
+      k_norm_backward_long<T><<<blocks, 1024, 0, h->stream>>>(dy, dy_stride, x, x_stride, rows, cols, gamma, mean, rstd, dx,
+                                                              dx_stride);
+    }
+    shares = (int)std::min<int64_t>(rows, kLongShares);
+    if (part)
+      k_norm_backward_cols<T><<<dim3((unsigned)((cols + 255) / 256), shares), 256, 0, h->stream>>>(
+          dy, dy_stride, x, x_stride, rows, cols, mean, rstd, part);
+    return shares;
+  }
+  auto go = [&](auto V, auto TPR, auto E) {
+    using S = NormShape<TPR()>;
+    const int64_t units = (rows + S::kRows - 1) / S::kRows;
+    shares = (int)std::min<int64_t>(units, std::min<int64_t>(kMaxShares, (int64_t)h->num_cu * (1024 / S::kThreads)));
+    k_norm_backward<T, V(), TPR(), E()><<<shares, S::kThreads, 0, h->stream>>>(dy, dy_stride, x, x_stride, rows, (int)cols, gamma,
+                                                                               mean, rstd, dx, dx_stride, part);
+  };
+  constexpr int kWide = 16 / sizeof(T);
+  if (cols % kWide == 0 && wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(dy, dy_stride, rows, sizeof(T)) &&
+      (!dx || wide_rows(dx, dx_stride, rows, sizeof(T))))
+    with_shape<kWide>(cols, go);
+  else
+    with_shape<1>(cols, go);
+  return shares;
+}
+
+}  // namespace
+
+int64_t artopk_norm_scratch_bytes(int64_t max_rows, int64_t max_cols) {
+  if (!valid_limits(max_rows, max_cols)) return -1;
+  return 4 * part_floats(max_rows, max_cols);
+}
+
+int artopk_norm_create(artopk_norm** out, int64_t max_rows, int64_t max_cols, void* hip_stream) {
+  if (!out) return fail_text(g_noctx_err, ARTOPK_EINVAL, "out is NULL");
+  if (!valid_limits(max_rows, max_cols))
+    return fail_text(g_noctx_err, ARTOPK_EINVAL, "max_rows=%lld and max_cols=%lld have to be in [1, 2^31)", (long long)max_rows,
+                     (long long)max_cols);
+  artopk_norm* h = new (std::nothrow) artopk_norm();
+  if (!h) return fail_text(g_noctx_err, ARTOPK_ENOMEM, "out of host memory");
+  h->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  h->max_rows = max_rows;
+  h->max_cols = max_cols;
+  int dev = 0, cus = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) {
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "no device: %s", hipGetErrorString(e));
+  }
+  if (cus > 0) h->num_cu = cus;
+  void* p = nullptr;
+  e = hipMalloc(&p, (size_t)part_floats(max_rows, max_cols) * 4);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "hipMalloc failed: %s", hipGetErrorString(e));
+  }
+  h->part = static_cast<float*>(p);
+  *out = h;
+  return ARTOPK_OK;
+}
+
+int artopk_norm_destroy(artopk_norm* norm) {
+  if (!norm) return ARTOPK_EINVAL;
+  if (norm->part) (void)hipFree(norm->part);
+  delete norm;
+  return ARTOPK_OK;
+}
+
+const char* artopk_norm_last_error(const artopk_norm* norm) { return norm ? norm->err : g_noctx_err; }
+
+int artopk_layernorm_forward(artopk_norm* norm, const void* x, int64_t x_stride, int32_t type, int64_t rows,
+                             int64_t cols, const float* gamma, const float* beta, float eps, void* y, int64_t y_stride,
+                             float* mean_out, float* rstd_out) {
+  if (!norm) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_layernorm_forward: norm is NULL");
+  int rc;
+  if ((rc = check_problem(norm, type, rows, cols))) return rc;
+  if (!(eps >= 0.0f) || eps > 1e30f) return fail_text(norm->err, ARTOPK_EINVAL, "eps is negative or not finite");
+  if ((rc = check_rows(norm, "x", x, x_stride, type, rows, cols))) return rc;
+  if ((rc = check_rows(norm, "y", y, y_stride, type, rows, cols))) return rc;
+  if ((rc = check_floats(norm, "gamma", gamma)) || (rc = check_floats(norm, "beta", beta)) ||
+      (rc = check_floats(norm, "mean_out", mean_out)) || (rc = check_floats(norm, "rstd_out", rstd_out)))
+    return rc;
+  {
+    RangeSet rs;
+    rs.add(x, rows_bytes(x_stride, rows, cols, type), false, "x");
+    rs.add(y, rows_bytes(y_stride, rows, cols, type), true, "y");
+    rs.add(gamma, (size_t)cols * 4, false, "gamma");
+    rs.add(beta, (size_t)cols * 4, false, "beta");
+    rs.add(mean_out, (size_t)rows * 4, true, "mean_out");
+    rs.add(rstd_out, (size_t)rows * 4, true, "rstd_out");
+    if ((rc = rs.check(norm->err))) return rc;
+  }
+  if (rows == 0) return ARTOPK_OK;
+  auto go = [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    forward<T>(norm, static_cast<const T*>(x), x_stride, rows, cols, gamma, beta, eps, static_cast<T*>(y), y_stride, mean_out,
+               rstd_out);
+  };
+  if (type == ARTOPK_G_F32) go((float*)nullptr);
+  else if (type == ARTOPK_G_BF16) go((__bf16*)nullptr);
+  else go((_Float16*)nullptr);
+  NORM_TRY(norm, hipGetLastError());
+  return ARTOPK_OK;
+}
+
+int artopk_layernorm_backward(artopk_norm* norm, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                              int32_t type, int64_t rows, int64_t cols, const float* gamma, const float* mean,
+                              const float* rstd, void* dx, int64_t dx_stride, void* dgamma, void* dbeta,
+                              int32_t grad_type, int32_t accumulate) {
+  if (!norm) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_layernorm_backward: norm is NULL");
+  int rc;
+  if ((rc = check_problem(norm, type, rows, cols))) return rc;
+  if (!known_type(grad_type)) return fail_text(norm->err, ARTOPK_EINVAL, "unknown gradient element type %d", grad_type);
+  if (!dx && !dgamma && !dbeta) return fail_text(norm->err, ARTOPK_EINVAL, "dx, dgamma and dbeta are all NULL");
+  if ((rc = check_rows(norm, "dy", dy, dy_stride, type, rows, cols))) return rc;
+  if ((rc = check_rows(norm, "x", x, x_stride, type, rows, cols))) return rc;
+  if (dx && (rc = check_rows(norm, "dx", dx, dx_stride, type, rows, cols))) return rc;
+  if (rows > 0 && (!mean || !rstd)) return fail_text(norm->err, ARTOPK_EINVAL, "mean or rstd is NULL");
+  const size_t gsize = elem_size(grad_type);
+  if ((rc = check_floats(norm, "gamma", gamma)) || (rc = check_floats(norm, "mean", mean)) ||
+      (rc = check_floats(norm, "rstd", rstd)) || (rc = check_floats(norm, "dgamma", dgamma, gsize)) ||
+      (rc = check_floats(norm, "dbeta", dbeta, gsize)))
+    return rc;
+  {
+    RangeSet rs;
+    rs.add(dy, rows_bytes(dy_stride, rows, cols, type), false, "dy");
+    rs.add(x, rows_bytes(x_stride, rows, cols, type), false, "x");
+    rs.add(gamma, (size_t)cols * 4, false, "gamma");
+    rs.add(mean, (size_t)rows * 4, false, "mean");
+    rs.add(rstd, (size_t)rows * 4, false, "rstd");
+    rs.add(dx, rows_bytes(dx_stride, rows, cols, type), true, "dx");
+    rs.add(dgamma, (size_t)cols * gsize, true, "dgamma");
+    rs.add(dbeta, (size_t)cols * gsize, true, "dbeta");
+    if ((rc = rs.check(norm->err))) return rc;
+  }
+  float* part = dgamma || dbeta ? norm->part : nullptr;
+  int shares = 0;
+  if (rows > 0) {
+    auto go = [&](auto* tag) {
+      using T = std::remove_pointer_t<decltype(tag)>;
+      shares = backward<T>(norm, static_cast<const T*>(dy), dy_stride, static_cast<const T*>(x), x_stride, rows, cols, gamma, mean,
+                           rstd, static_cast<T*>(dx), dx_stride, part);
+    };
+    if (type == ARTOPK_G_F32) go((float*)nullptr);
+    else if (type == ARTOPK_G_BF16) go((__bf16*)nullptr);
+    else go((_Float16*)nullptr);
+  }
+  if (part) {
+    const dim3 grid((unsigned)((cols + 63) / 64), 2);
+    auto go = [&](auto* tag) {
+      using G = std::remove_pointer_t<decltype(tag)>;
+      k_norm_join<G><<<grid, 256, 0, norm->stream>>>(part, shares, cols, static_cast<G*>(dgamma), static_cast<G*>(dbeta),
+                                                     accumulate != 0);
+    };
+    if (grad_type == ARTOPK_G_F32) go((float*)nullptr);
+    else if (grad_type == ARTOPK_G_BF16) go((__bf16*)nullptr);
+    else go((_Float16*)nullptr);
+  }
+  NORM_TRY(norm, hipGetLastError());
+  return ARTOPK_OK;
+}

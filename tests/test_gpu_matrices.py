@@ -1,0 +1,323 @@
+"""Orthogonalised updates of matrices in a flat vector against the definition in 64 bits.
+
+Tolerance of an orthogonalised matrix, relative in the Frobenius norm.  A perturbation E of an iterate X_k changes the
+result by at most L_k ||E||, L_k the largest slope of the steps still to come, a^(5 - k) for the usual coefficients
+(3.4445 each, at zero).  In a step X, A (twice) and Q are each rounded to within u, which perturbs the next iterate by
+no more than about 4 u of the previous one's norm times a; float32 sums add a few 2^-24 of the same.  So
+    off = sum over k of 4 (u + 2^-22) a^(5 - k) ||X_k|| / ||X_5||,
+with the norms from the reference; u = 2^-11 for HALF, 2^-21 for SPLIT.  That is a worst case; indexing is held to more by
+matrices whose result is known element by element.
+"""
+
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+USUAL = (3.4445, -4.7750, 2.0315)
+OUT_U = {"f32": 2.0 ** -24, "bf16": 2.0 ** -9, "f16": 2.0 ** -12}
+OPERAND_U = {0: 2.0 ** -11, 1: 2.0 ** -21}
+EPS = 1e-7
+
+
+def _dtype(t):
+    import torch
+
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[t]
+
+
+def _code(t):
+    import paper_2312_02493_amd as lib
+
+    return {"f32": lib.ARTOPK_G_F32, "bf16": lib.ARTOPK_G_BF16, "f16": lib.ARTOPK_G_F16}[t]
+
+
+def reference(g, steps=5, coefficients=USUAL, eps=EPS):
+    """(result, norms of the iterates before each step and after the last) in 64 bits."""
+    tall = g.shape[0] > g.shape[1]
+    x = g.T if tall else g
+    x = x / (np.sqrt((x * x).sum()) + eps)
+    norms = [np.linalg.norm(x)]
+    rows = [coefficients] * steps if np.ndim(coefficients) == 1 else coefficients
+    for a, b, c in rows:
+        s = x @ x.T
+        x = a * x + (b * s + c * (s @ s)) @ x
+        norms.append(np.linalg.norm(x))
+    return (x.T if tall else x), norms
+
+
+def tolerance(norms, u, slope=USUAL[0]):
+    steps = len(norms) - 1
+    return sum(4 * (u + 2.0 ** -22) * slope ** (steps - k) * norms[k] for k in range(steps)) / norms[-1]
+
+
+def layout(shapes, gap=3):
+    """[(offset, rows, cols, scale)] with `gap` loose elements before, between and behind."""
+    at, out = gap, []
+    for i, (r, c) in enumerate(shapes):
+        out.append((at, r, c, math.sqrt(max(1.0, r / c)) if i % 2 else 1.0))
+        at += r * c + gap
+    return out, at
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (5, 3), (64, 64), (65, 63), (63, 200), (129, 130), (300, 77), (257, 520), (1, 1000), (700, 2),
+          (128, 128), (513, 700), (40, 41), (600, 530), (1040, 130)]
+
+
+def _gradients(rng, shapes, n):
+    v = rng.standard_normal(n) * 1e-3
+    mats, _ = layout(shapes)
+    for at, r, c, _ in mats:
+        k = max(1, min(r, c) // 8)
+        v[at:at + r * c] += 1e-3 * (rng.standard_normal((r, k)) @ rng.standard_normal((k, c))).ravel()
+    return v.astype(np.float32)
+
+
+@pytest.mark.parametrize("t,products", [("f32", 1), ("f32", 0), ("bf16", 0), ("f16", 0), ("bf16", 1)])
+def test_orthogonalize(t, products):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(21)
+    mats, n = layout(SHAPES)
+    x = torch.from_numpy(_gradients(rng, SHAPES, n)).cuda().to(_dtype(t))
+    out = torch.full_like(x, 7.0)
+    ctx = lib.MatrixContext(mats, n, _code(t), products)
+    ctx.artopk_orthogonalize(x, out)
+    got, xs = out.cpu().double().numpy(), x.cpu().double().numpy()
+    inside = np.zeros(n, bool)
+    for at, r, c, scale in mats:
+        inside[at:at + r * c] = True
+        want, norms = reference(xs[at:at + r * c].reshape(r, c))
+        off = np.linalg.norm(got[at:at + r * c].reshape(r, c) - scale * want) / np.linalg.norm(scale * want)
+        assert off <= tolerance(norms, OPERAND_U[products]) + OUT_U[t], (r, c, off, tolerance(norms, OPERAND_U[products]))
+    assert (got[~inside] == 7.0).all()
+    again = torch.zeros_like(out)
+    ctx.artopk_orthogonalize(x, again)
+    ctx.artopk_orthogonalize(x, out)
+    for at, r, c, _ in mats:
+        assert torch.equal(again[at:at + r * c], out[at:at + r * c])
+
+
+@pytest.mark.parametrize("t,products", [("f32", 1), ("bf16", 0)])
+@pytest.mark.parametrize("shape", [(200, 320), (320, 200), (700, 900), (1500, 600), (64, 3000), (1025, 1025), (30, 2000)])
+def test_every_element_in_its_place(shape, t, products):
+    """One entry to each row and column: the result has the same pattern, each entry the polynomial of its own value, and
+    exact zeros everywhere else."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(shape[0])
+    r, c = shape
+    m = min(r, c)
+    g = np.zeros((r, c))
+    rows, cols = rng.permutation(r)[:m], rng.permutation(c)[:m]
+    g[rows, cols] = rng.choice([-1.0, 1.0], m) * rng.integers(64, 256, m)  # exact in every type
+    x = torch.from_numpy(g.astype(np.float32)).cuda().to(_dtype(t)).view(-1)
+    out = torch.full_like(x, 7.0)
+    lib.MatrixContext([(0, r, c, 1.0)], r * c, _code(t), products).artopk_orthogonalize(x, out)
+    got = out.cpu().double().numpy().reshape(r, c)
+    v = g[rows, cols] / (np.sqrt((g * g).sum()) + EPS)
+    off = np.zeros(m)
+    u = OPERAND_U[products] + 2.0 ** -22
+    for _ in range(5):
+        p = v * (USUAL[0] + USUAL[1] * v ** 2 + USUAL[2] * v ** 4)
+        slope = np.abs(USUAL[0] + 3 * USUAL[1] * v ** 2 + 5 * USUAL[2] * v ** 4)
+        # what it was off by, and the roundings of x, of a = x^2 (twice) and of q
+        off = (slope + 0.1) * off + u * np.abs(v) * (slope + 2 * np.abs(USUAL[1]) * v ** 2 + 4 * USUAL[2] * v ** 4 + 4)
+        v = p
+    assert (np.abs(got[rows, cols] - v) <= off + OUT_U[t] * np.abs(v)).all(), np.abs(got[rows, cols] - v).max()
+    got[rows, cols] = 0.0
+    assert not got.any()
+
+
+def test_steps_and_coefficients():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(4)
+    mats, n = layout([(70, 150), (150, 70), (3, 2)])
+    x = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda()
+    out = torch.zeros_like(x)
+    ctx = lib.MatrixContext(mats, n)
+    third = [(1.5, -0.5, 0.0)] * 3 + [(1.875, -1.25, 0.375)] * 2
+    for steps, co in ((0, None), (1, None), (2, (1.5, -0.5, 0.0)), (5, third), (12, (1.5, -0.5, 0.0))):
+        ctx.artopk_orthogonalize(x, out, steps=steps, coefficients=co)
+        got, xs = out.cpu().double().numpy(), x.cpu().double().numpy()
+        for at, r, c, scale in mats:
+            want, norms = reference(xs[at:at + r * c].reshape(r, c), steps, USUAL if co is None else co)
+            tol = tolerance(norms, OPERAND_U[1], 3.4445 if co is None else 1.875) + 4 * 2.0 ** -24
+            off = np.linalg.norm(got[at:at + r * c].reshape(r, c) - scale * want) / np.linalg.norm(scale * want)
+            assert off <= tol, (steps, r, c, off, tol)
+
+
+def test_special_values_stay_in_their_matrix():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    mats, n = layout([(70, 150), (90, 40), (130, 130), (20, 20), (33, 65)])
+    x = torch.randn(n, device="cuda")
+    zero, nan, inf = (slice(m[0], m[0] + m[1] * m[2]) for m in mats[:3])
+    x[zero] = 0.0
+    x[nan.start + 17] = float("nan")
+    x[inf.start + 4000] = float("-inf")
+    big, small = (slice(m[0], m[0] + m[1] * m[2]) for m in mats[3:])
+    x[big] *= 1e30   # its squares pass float32's range
+    x[small] *= 1e-30
+    out = torch.full_like(x, 7.0)
+    lib.MatrixContext(mats, n).artopk_orthogonalize(x, out, eps=1e-37)
+    assert not bool(out[zero].any())
+    assert bool(torch.isnan(out[nan]).all()) and bool(torch.isnan(out[inf]).all())
+    got, xs = out.cpu().double().numpy(), x.cpu().double().numpy()
+    for at, r, c, scale in mats[3:]:
+        want, norms = reference(xs[at:at + r * c].reshape(r, c), eps=1e-37)
+        off = np.linalg.norm(got[at:at + r * c].reshape(r, c) - scale * want) / np.linalg.norm(scale * want)
+        assert off <= tolerance(norms, OPERAND_U[1])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_muon_steps(t, nesterov):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(8)
+    shapes = [(70, 150), (300, 77), (1, 5), (128, 64), (513, 520)]
+    mats, n = layout(shapes)
+    eta, mu, decay, rest, by = 0.02, 0.9, 0.1, 0.5, 0.25
+    w = torch.from_numpy((0.05 * rng.standard_normal(n)).astype(np.float32)).cuda().to(_dtype(t))
+    m = torch.from_numpy(_gradients(rng, shapes, n)).cuda()
+    ctx = lib.MatrixContext(mats, n, _code(t))
+    u32 = 2.0 ** -24
+    for turn in range(2):
+        u = torch.from_numpy(4.0 * _gradients(rng, shapes, n)).cuda()
+        w0, m0, u0 = (v.cpu().double().numpy() for v in (w, m, u))
+        ctx.artopk_muon_step(w, m, u, eta=eta, mu=mu, nesterov=nesterov, decay=decay, eta_rest=rest, update_scale=by)
+        m1 = mu * m0 + by * u0
+        mo = 2 * u32 * (np.abs(mu * m0) + np.abs(by * u0)) + 2.0 ** -24 * np.abs(m0)  # mu itself is rounded
+        assert (np.abs(m.cpu().double().numpy() - m1) <= mo).all()
+        v = mu * m1 + by * u0 if nesterov else m1
+        vo = mo + 3 * u32 * (np.abs(m1) + np.abs(by * u0))
+        got = w.cpu().double().numpy()
+        out_u = OUT_U[t] + 2 * u32
+        loose = np.ones(n, bool)
+        for at, r, c, scale in mats:
+            s = slice(at, at + r * c)
+            loose[s] = False
+            o, norms = reference(v[s].reshape(r, c))
+            want = w0[s].reshape(r, c) * (1 - eta * decay) - eta * scale * o
+            # v's own roundings reach the result as a perturbation of the first iterate
+            tol = tolerance(norms, OPERAND_U[1 if t == "f32" else 0]) + \
+                USUAL[0] ** 5 * np.linalg.norm(vo[s]) / np.linalg.norm(v[s]) / norms[-1]
+            off = np.linalg.norm(got[s].reshape(r, c) - want)
+            assert off <= eta * scale * tol * norms[-1] + out_u * (np.linalg.norm(want) + np.linalg.norm(w0[s])), (r, c)
+        want = w0 - rest * v
+        tol = rest * vo + out_u * (np.abs(w0) + np.abs(want)) + (2.0 ** -25 if t == "f16" else 0.0)
+        assert (np.abs(got - want) <= tol)[loose].all()
+    before = w.clone()
+    ctx.artopk_muon_step(w, m, u, eta=0.0, mu=mu, nesterov=nesterov)
+    assert torch.equal(before, w)  # eta and eta_rest zero: nothing moves but the momentum
+
+
+def test_large_matrices():
+    """Sizes of several tiles each way, odd ones, checked by the definition with torch's float64 products."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for r, c, t in ((1500, 2111, "f32"), (2304, 1100, "f32"), (2049, 4097, "bf16"), (3000, 100, "f16")):
+        x = torch.randn(r, c, generator=g, device="cuda").to(_dtype(t))
+        out = torch.empty_like(x)
+        ctx = lib.MatrixContext([(0, r, c)], r * c, _code(t))
+        ctx.artopk_orthogonalize(x.view(-1), out.view(-1))
+        y = x.double()
+        y = (y.t() if r > c else y).contiguous()
+        y = y / (y.norm() + EPS)
+        norms = [float(y.norm())]
+        for _ in range(5):
+            s = y @ y.t().contiguous()
+            y = USUAL[0] * y + (USUAL[1] * s + USUAL[2] * (s @ s)) @ y
+            norms.append(float(y.norm()))
+        y = y.t() if r > c else y
+        off = float((out.double() - y).norm() / y.norm())
+        assert off <= tolerance(norms, OPERAND_U[1 if t == "f32" else 0]) + OUT_U[t], (r, c, t, off)
+
+
+def test_refusals():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    def refused(text, f, *a, **k):
+        with pytest.raises(lib.ArTopkError, match=text) as e:
+            f(*a, **k)
+        assert e.value.code == -1
+
+    for text, mats, n in (("count", [], 10), ("within", [(0, 3, 4)], 11), ("within", [(-1, 3, 3)], 11), ("overlap", [(5, 2, 3), (0, 2, 3)], 20),
+                          ("sides", [(0, 0, 3)], 9), ("sides", [(0, 1, 65537)], 70000), ("n=0", [(0, 1, 1)], 0),
+                          ("n=2147483648", [(0, 1, 1)], 1 << 31), ("scale", [(0, 1, 1, float("inf"))], 1)):
+        refused(text, lib.MatrixContext, mats, n)
+    refused("element type", lib.MatrixContext, [(0, 1, 1)], 1, 7)
+    refused("products", lib.MatrixContext, [(0, 1, 1)], 1, 0, 5)
+    ctx = lib.MatrixContext([(0, 4, 5)], 24)
+    x, out = torch.ones(24, device="cuda"), torch.zeros(24, device="cuda")
+    orth, muon = ctx.artopk_orthogonalize, ctx.artopk_muon_step
+    refused("overlap", orth, x, x)
+    refused("24 elements", orth, x[:23], out)
+    refused("handle's type", orth, x.half(), out.half())
+    refused("steps=-1", orth, x, out, steps=-1)
+    refused("steps=33", orth, x, out, steps=33)
+    refused("eps", orth, x, out, eps=0.0)
+    refused("eps", orth, x, out, eps=float("inf"))
+    refused("coefficients", orth, x, out, coefficients=[(1.5, -0.5, 0.0)] * 2)
+    refused("not finite", orth, x, out, coefficients=(float("nan"), 0.0, 0.0))
+    refused("singular values", orth, x, out, coefficients=(3.0, 0.0, 0.0), steps=1)
+    refused("singular values", orth, x, out, coefficients=(16.0, -16.0, 0.0), steps=1)
+    refused("step 1", orth, x, out, coefficients=(1.9, 0.0, 0.0), steps=2)
+    w, m, u = torch.ones(24, device="cuda"), torch.ones(24, device="cuda"), torch.ones(24, device="cuda")
+    refused("overlap", muon, w, m, m, eta=0.1)
+    refused("overlap", muon, w, w, u, eta=0.1)
+    refused("finite", muon, w, m, u, eta=float("nan"))
+    refused("momentum is torch.float16", muon, w, m.half(), u, eta=0.1)
+    refused("update is NULL", muon, w, m, None, eta=0.1)
+    raw = lib.load_library()
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    assert raw.artopk_orthogonalize(None, p(x), p(out), 5, None, 1e-7) == -1
+    assert raw.artopk_orthogonalize(ctx._h, None, p(out), 5, None, 1e-7) == -1
+    assert raw.artopk_orthogonalize(ctx._h, C.c_void_p(x.data_ptr() + 2), p(out), 5, None, 1e-7) == -1
+    assert not bool(out.any()) and bool((w == 1).all()) and bool((m == 1).all())
+    orth(x, out)
+    torch.cuda.synchronize()
+
+
+def test_on_its_own_stream_and_in_a_graph():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    mats, n = layout([(70, 150), (300, 310), (520, 513)])
+    stream = torch.cuda.Stream()
+    w0, m0, u = torch.randn(n, device="cuda"), torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        ctx = lib.MatrixContext(mats, n)
+        w, m = w0.clone(), m0.clone()
+
+        def go():
+            ctx.artopk_muon_step(w, m, u, eta=0.02, decay=0.01, eta_rest=0.1)
+
+        eager = []
+        for _ in range(3):
+            go()
+            eager.append((w.clone(), m.clone()))
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            go()
+        w.copy_(w0)
+        m.copy_(m0)
+        for turn in range(3):
+            graph.replay()
+            stream.synchronize()
+            assert torch.equal(w, eager[turn][0]) and torch.equal(m, eager[turn][1]), turn
