@@ -17,8 +17,8 @@ using namespace artopk;
 
 namespace {
 
-constexpr int kTileClasses = 3;
-constexpr int kTileOf[kTileClasses] = {64, 128, 256};
+constexpr int kTileClasses = 4;
+constexpr int kTileOf[kTileClasses] = {64, 128, 192, 256};
 constexpr int32_t kMaxMatrices = 65535;
 constexpr int32_t kMaxSide = 65536;
 constexpr float kUsual[3] = {3.4445f, -4.7750f, 2.0315f};
@@ -29,23 +29,136 @@ struct Span {
   int count = 0;
 };
 
+// A product's blocks, and the tile they take.
+struct Product {
+  Span tiles;
+  int cls = 0;
+};
+
 // What creation works out on the host: where everything lies, and the tables.
 struct MatPlan {
   std::vector<MatDesc> mats;
   std::vector<MatChunk> chunks;
   std::vector<MatTile> tiles;
   Span begin;
-  Span symmetric[kTileClasses], apply[kTileClasses], final_[kTileClasses];
+  Product gram, square, apply, final_;
   int64_t halves = 0;  // of the iterates' memory
   int32_t sums = 0;
+  int64_t slots = 0;   // partial sums of the Gram products' shares
   // places in the slab
-  size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_mem = 0, total = 0;
+  size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_arrived = 0, o_partial = 0, o_mem = 0, total = 0;
 };
 
-int tile_class(int m, int n) {
-  if (m > 512 && n > 512) return 2;
-  if (m > 128) return 1;
-  return 0;
+// What a product costs, in us, by tile class: a block alone on its compute unit for each 64 of the summed index, and the
+// whole chip's time for each 64 of one of very many blocks.
+struct TileCost {
+  double alone, among, fixed;
+};
+constexpr TileCost kCost[2][kTileClasses] = {
+    {{0.21, 0.00072, 3.0}, {0.53, 0.00197, 4.0}, {0.85, 0.0043, 5.0}, {1.25, 0.0070, 6.0}},
+    {{0.42, 0.0023, 3.0}, {1.10, 0.0055, 4.0}, {2.0, 0.0115, 5.0}, {3.15, 0.0185, 6.0}}};
+constexpr double kJoinCost = 4.0;  // of sums that meet in memory
+
+int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
+
+// One kind of product over all matrices.
+struct ProductKind {
+  bool symmetric, long_sum;  // the result is, and n is summed over, not m
+};
+
+int64_t product_tiles(const MatDesc& d, const ProductKind& k, int tile) {
+  const int64_t a = tiles_of(d.mp, tile), b = tiles_of(d.np, tile);
+  return k.symmetric ? a * (a + 1) / 2 : a * b;
+}
+
+int product_shares(const MatDesc& d, const ProductKind& k, int each) {  // `each`: 64s of the summed index a share, 0: whole
+  const int units = (k.long_sum ? d.np : d.mp) / 64;
+  return each == 0 ? 1 : std::max(1, (units + each / 2) / each);
+}
+
+double product_cost(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, int cls, int each) {
+  const TileCost& c = kCost[parts - 1][cls];
+  double sum = 0.0, longest = 0.0;
+  bool cut = false;
+  for (const MatDesc& d : mats) {
+    const double units = (k.long_sum ? d.np : d.mp) / 64;
+    const int shares = product_shares(d, k, each);
+    sum += units * (double)product_tiles(d, k, kTileOf[cls]);
+    longest = std::max(longest, std::ceil(units / shares));
+    cut |= shares > 1;
+  }
+  return std::max(c.alone * longest, c.among * sum) + c.fixed + (cut ? kJoinCost : 0.0);
+}
+
+// The tile and, for the Gram products, the length of a share that cost least.
+void choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, Product* p, int* each_out) {
+  double best = 1e300;
+  for (int cls = 0; cls < kTileClasses; ++cls)
+    for (int each : {0, 32, 16, 8, 4}) {
+      if (each && (!k.long_sum || cls > 1)) continue;
+      const double cost = product_cost(mats, k, parts, cls, each);
+      if (cost < best) {
+        best = cost;
+        p->cls = cls;
+        if (each_out) *each_out = each;
+      }
+    }
+}
+
+// The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
+// each die has a cache of its own: every matrix's tiles are cut into eight runs of neighbours, one for each die, and the
+// matrices with the longest sums come first.
+void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each, bool swap_tall) {
+  const int tile = kTileOf[p->cls];
+  std::vector<int> order(plan->mats.size());
+  for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
+  auto units = [&](int i) {
+    const MatDesc& d = plan->mats[i];
+    return (k.long_sum ? d.np : d.mp) / 64 / product_shares(d, k, each);
+  };
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return units(a) > units(b); });
+  std::vector<MatTile> die[8];
+  std::vector<MatTile> own;
+  int first = 0;
+  for (int i : order) {
+    const MatDesc& d = plan->mats[i];
+    const int a = tiles_of(d.mp, tile), b = tiles_of(d.np, tile);
+    const int shares = product_shares(d, k, each);
+    own.clear();
+    constexpr int kBand = 4;  // rows of tiles taken together
+    for (int a0 = 0; a0 < a; a0 += kBand)
+      for (int y = 0; y < (k.symmetric ? std::min(a, a0 + kBand) : b); ++y)
+        for (int x = a0; x < std::min(a, a0 + kBand); ++x) {
+          if (k.symmetric && y > x) continue;
+          MatTile t = {};
+          t.mat = (uint32_t)i;
+          t.i = (uint16_t)(swap_tall && d.tall ? y : x);
+          t.j = (uint16_t)(swap_tall && d.tall ? x : y);
+          t.shares = (uint16_t)shares;
+          t.slot = (uint32_t)plan->slots;
+          if (shares > 1) plan->slots += shares;
+          for (int s = 0; s < shares; ++s) {
+            t.share = (uint16_t)s;
+            own.push_back(t);
+          }
+        }
+    const int64_t total = (int64_t)own.size(), per = total / 8, more = total % 8;
+    int64_t at = 0;
+    for (int x = 0; x < 8; ++x) {
+      const int64_t count = per + (x < more);
+      std::vector<MatTile>& to = die[(first + x) % 8];
+      to.insert(to.end(), own.begin() + at, own.begin() + at + count);
+      at += count;
+    }
+    first = (int)((first + more) % 8);
+  }
+  p->tiles.at = plan->tiles.size();
+  size_t longest = 0;
+  for (const auto& v : die) longest = std::max(longest, v.size());
+  for (size_t r = 0; r < longest; ++r)
+    for (const auto& v : die)
+      if (r < v.size()) plan->tiles.push_back(v[r]);
+  p->tiles.count = (int)(plan->tiles.size() - p->tiles.at);
 }
 
 // ARTOPK_OK, or ARTOPK_EINVAL with the reason in `err`.  Throws std::bad_alloc.
@@ -77,7 +190,6 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   }
 
   plan->mats.resize(count);
-  std::vector<int> cls(count);
   for (int i = 0; i < count; ++i) {
     const artopk_matrix& m = mats[i];
     MatDesc& d = plan->mats[i];
@@ -86,10 +198,8 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
     d.m = std::min(m.rows, m.cols);
     d.n = std::max(m.rows, m.cols);
     d.scale = m.scale;
-    cls[i] = tile_class(d.m, d.n);
-    const int tile = kTileOf[cls[i]];
-    d.mp = (d.m + tile - 1) / tile * tile;
-    d.np = (d.n + tile - 1) / tile * tile;
+    d.mp = (d.m + 63) / 64 * 64;
+    d.np = (d.n + 63) / 64 * 64;
     const int64_t mn = (int64_t)d.mp * d.np * parts, mm = (int64_t)d.mp * d.mp * parts;
     d.x = plan->halves;
     d.xt[0] = d.x + mn;
@@ -120,43 +230,21 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   }
   loose(n);
 
-  auto add = [&](int mat, int i, int j) { plan->tiles.push_back(MatTile{(uint32_t)mat, (uint16_t)i, (uint16_t)j}); };
-  auto list = [&](Span* s, auto&& each) {
-    s->at = plan->tiles.size();
-    each();
-    s->count = (int)(plan->tiles.size() - s->at);
-  };
-  list(&plan->begin, [&] {
-    for (int i = 0; i < count; ++i)
-      for (int a = 0; a < plan->mats[i].mp / 64; ++a)
-        for (int b = 0; b < plan->mats[i].np / 64; ++b) add(i, a, b);
-  });
-  for (int c = 0; c < kTileClasses; ++c) {
-    const int tile = kTileOf[c];
-    list(&plan->symmetric[c], [&] {
-      for (int i = 0; i < count; ++i)
-        if (cls[i] == c)
-          for (int a = 0; a < plan->mats[i].mp / tile; ++a)
-            for (int b = 0; b <= a; ++b) add(i, a, b);
-    });
-    list(&plan->apply[c], [&] {
-      for (int i = 0; i < count; ++i)
-        if (cls[i] == c)
-          for (int a = 0; a < plan->mats[i].mp / tile; ++a)
-            for (int b = 0; b < plan->mats[i].np / tile; ++b) add(i, a, b);
-    });
-    list(&plan->final_[c], [&] {
-      for (int i = 0; i < count; ++i)
-        if (cls[i] == c)
-          for (int a = 0; a < plan->mats[i].mp / tile; ++a)
-            for (int b = 0; b < plan->mats[i].np / tile; ++b) {
-              if (plan->mats[i].tall)
-                add(i, b, a);
-              else
-                add(i, a, b);
-            }
-    });
-  }
+  for (int i = 0; i < count; ++i)
+    for (int a = 0; a < plan->mats[i].mp / 64; ++a)
+      for (int b = 0; b < plan->mats[i].np / 64; ++b)
+        plan->tiles.push_back(MatTile{(uint32_t)i, (uint16_t)a, (uint16_t)b, 0, 1, 0});
+  plan->begin.count = (int)plan->tiles.size();
+  const ProductKind gram = {true, true}, square = {true, false}, apply = {false, false};
+  int each = 0;
+  choose_product(plan->mats, gram, parts, &plan->gram, &each);
+  choose_product(plan->mats, square, parts, &plan->square, nullptr);
+  choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
+  plan->final_.cls = plan->apply.cls;
+  list_product(plan, gram, &plan->gram, each, false);
+  list_product(plan, square, &plan->square, 0, false);
+  list_product(plan, apply, &plan->apply, 0, false);
+  list_product(plan, apply, &plan->final_, 0, true);
   if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
 
   size_t at = 0;
@@ -169,6 +257,8 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   plan->o_chunks = take(plan->chunks.size() * sizeof(MatChunk));
   plan->o_tiles = take(plan->tiles.size() * sizeof(MatTile));
   plan->o_sums = take((size_t)plan->sums * sizeof(double));
+  plan->o_arrived = take((size_t)plan->slots * sizeof(uint32_t));
+  plan->o_partial = take((size_t)plan->slots * kTileOf[plan->gram.cls] * kTileOf[plan->gram.cls] * sizeof(float));
   plan->o_mem = take((size_t)plan->halves * 2);
   plan->total = at;
   return ARTOPK_OK;
@@ -181,7 +271,10 @@ struct artopk_matrices {
   int64_t n = 0;
   int32_t type = 0, parts = 1;
   int nchunks = 0;
-  Span begin, symmetric[kTileClasses], apply[kTileClasses], final_[kTileClasses];
+  Span begin;
+  Product gram, square, apply, final_;
+  uint32_t* arrived = nullptr;
+  float* partial = nullptr;
   char* slab = nullptr;
   const MatDesc* mats = nullptr;
   const MatChunk* chunks = nullptr;
@@ -241,16 +334,18 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 
 template <int TILE, int PARTS, int MODE>
 void product(artopk_matrices* h, const Span& s, int from, const float* co, const FinishArgs& f) {
-  if (s.count)
-    k_mat_product<TILE, PARTS, MODE><<<s.count, product_threads<TILE>(), 0, h->stream>>>(h->mats, h->tiles + s.at, h->mem, from,
-                                                                                        co[0], co[1], co[2], f);
+  k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
+      h->mats, h->tiles + s.at, h->mem, from, co[0], co[1], co[2], f, h->partial, h->arrived);
 }
 
 template <int PARTS, int MODE>
-void products(artopk_matrices* h, const Span (&s)[kTileClasses], int from, const float* co, const FinishArgs& f) {
-  product<256, PARTS, MODE>(h, s[2], from, co, f);
-  product<128, PARTS, MODE>(h, s[1], from, co, f);
-  product<64, PARTS, MODE>(h, s[0], from, co, f);
+void product(artopk_matrices* h, const Product& p, int from, const float* co, const FinishArgs& f) {
+  switch (p.cls) {
+    case 0: return product<64, PARTS, MODE>(h, p.tiles, from, co, f);
+    case 1: return product<128, PARTS, MODE>(h, p.tiles, from, co, f);
+    case 2: return product<192, PARTS, MODE>(h, p.tiles, from, co, f);
+    default: return product<256, PARTS, MODE>(h, p.tiles, from, co, f);
+  }
 }
 
 template <int PARTS, class From>
@@ -261,12 +356,12 @@ void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], f
   }
   k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->mats, h->tiles + h->begin.at, h->sums, eps, h->mem);
   for (int k = 0; k < steps; ++k) {
-    products<PARTS, kGram>(h, h->symmetric, k & 1, co[k], f);
-    products<PARTS, kSquare>(h, h->symmetric, k & 1, co[k], f);
+    product<PARTS, kGram>(h, h->gram, k & 1, co[k], f);
+    product<PARTS, kSquare>(h, h->square, k & 1, co[k], f);
     if (k + 1 < steps)
-      products<PARTS, kApply>(h, h->apply, k & 1, co[k], f);
+      product<PARTS, kApply>(h, h->apply, k & 1, co[k], f);
     else
-      products<PARTS, kFinal>(h, h->final_, k & 1, co[k], f);
+      product<PARTS, kFinal>(h, h->final_, k & 1, co[k], f);
   }
 }
 
@@ -329,11 +424,10 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->parts = products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
   h->nchunks = (int)plan.chunks.size();
   h->begin = plan.begin;
-  for (int c = 0; c < kTileClasses; ++c) {
-    h->symmetric[c] = plan.symmetric[c];
-    h->apply[c] = plan.apply[c];
-    h->final_[c] = plan.final_[c];
-  }
+  h->gram = plan.gram;
+  h->square = plan.square;
+  h->apply = plan.apply;
+  h->final_ = plan.final_;
   void* p = nullptr;
   hipError_t e = hipMalloc(&p, plan.total);
   if (e != hipSuccess) {
@@ -346,16 +440,20 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->chunks = reinterpret_cast<const MatChunk*>(h->slab + plan.o_chunks);
   h->tiles = reinterpret_cast<const MatTile*>(h->slab + plan.o_tiles);
   h->sums = reinterpret_cast<double*>(h->slab + plan.o_sums);
+  h->arrived = reinterpret_cast<uint32_t*>(h->slab + plan.o_arrived);
+  h->partial = reinterpret_cast<float*>(h->slab + plan.o_partial);
   h->mem = reinterpret_cast<_Float16*>(h->slab + plan.o_mem);
   e = hipMemcpy(h->slab + plan.o_mats, plan.mats.data(), plan.mats.size() * sizeof(MatDesc), hipMemcpyHostToDevice);
   if (e == hipSuccess)
     e = hipMemcpy(h->slab + plan.o_chunks, plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk), hipMemcpyHostToDevice);
   if (e == hipSuccess)
     e = hipMemcpy(h->slab + plan.o_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MatTile), hipMemcpyHostToDevice);
+  if (e == hipSuccess && plan.slots) e = hipMemset(h->slab + plan.o_arrived, 0, (size_t)plan.slots * sizeof(uint32_t));
+  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     (void)hipFree(h->slab);
     delete h;
-    return fail_text(g_noctx_err, ARTOPK_EHIP, "hipMemcpy failed: %s", hipGetErrorString(e));
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "filling the tables failed: %s", hipGetErrorString(e));
   }
   *out = h;
   return ARTOPK_OK;

@@ -23,7 +23,8 @@
 namespace artopk {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kOperandScale = 4096.0f;  // 2^12, of every stored operand
 
@@ -45,9 +46,13 @@ struct MatChunk {
   int32_t mat, slot;  // slot: where its sum of squares goes
 };
 
+// One block's tile of a product, or its share of the summed index where a tile's sum is cut (shares > 1): the shares
+// meet at `slot` of the memory for partial sums.
 struct MatTile {
   uint32_t mat;
   uint16_t i, j;  // in tiles
+  uint16_t share, shares;
+  uint32_t slot;
 };
 
 // What the elements of a step are made of.
@@ -200,18 +205,28 @@ struct FinishArgs {
   MuonArgs a;
 };
 
-template <class T>
-__device__ __forceinline__ void finish_as(T* p, const FinishArgs& f, float scaled) {
-  *p = static_cast<T>(f.muon ? fmaf(-f.a.eta, scaled, static_cast<float>(*p) * f.a.decay_by) : scaled);
+template <int N, class T>
+__device__ __forceinline__ void finish_as(T* p, const FinishArgs& f, const float (&scaled)[N]) {
+  struct alignas(N * sizeof(T)) Some {
+    T e[N];
+  };
+  Some v;
+  if (f.muon) v = *reinterpret_cast<const Some*>(p);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    v.e[e] = static_cast<T>(f.muon ? fmaf(-f.a.eta, scaled[e], static_cast<float>(v.e[e]) * f.a.decay_by) : scaled[e]);
+  *reinterpret_cast<Some*>(p) = v;
 }
 
-__device__ __forceinline__ void finish(const FinishArgs& f, int64_t i, float scaled) {
+// N elements side by side, at a place aligned to all of them.
+template <int N>
+__device__ __forceinline__ void finish(const FinishArgs& f, int64_t i, const float (&scaled)[N]) {
   if (f.type == kTypeF32)
-    finish_as(static_cast<float*>(f.out) + i, f, scaled);
+    finish_as<N>(static_cast<float*>(f.out) + i, f, scaled);
   else if (f.type == kTypeBf16)
-    finish_as(static_cast<__bf16*>(f.out) + i, f, scaled);
+    finish_as<N>(static_cast<__bf16*>(f.out) + i, f, scaled);
   else
-    finish_as(static_cast<_Float16*>(f.out) + i, f, scaled);
+    finish_as<N>(static_cast<_Float16*>(f.out) + i, f, scaled);
 }
 
 // No step at all: the scaled matrix itself.
@@ -224,198 +239,401 @@ __global__ __launch_bounds__(256) void k_mat_scaled(From from, const MatDesc* __
   if (c.mat < 0) return;
   const MatDesc d = mats[c.mat];
   const float by = inverse_norm(d, sums, eps, room);
-  for (int64_t i = c.begin + threadIdx.x; i < c.end; i += 256) finish(f, i, from(i) * by * d.scale);
+  for (int64_t i = c.begin + threadIdx.x; i < c.end; i += 256) {
+    const float v[1] = {from(i) * by * d.scale};
+    finish<1>(f, i, v);
+  }
 }
 
 enum { kGram = 0, kSquare = 1, kApply = 2, kFinal = 3 };
 
-// One tile of a product.  TILE x TILE elements, WM x WN waves.
-template <int TILE>
-struct ProductShape;
-template <>
-struct ProductShape<64> {
-  static constexpr int kWM = 2, kWN = 2;
+// The shape of a product's tile: TILE x TILE elements by WM x WN waves, the summed index in stages of kDepth, kStages of
+// them in LDS.  A stage is brought by loads that go to LDS without passing registers, two stages ahead of its use at most,
+// and every wave keeps the next 32 of the summed index in registers while it multiplies the present ones.
+template <int TILE_, int PARTS_>
+struct ProductShape {
+  static constexpr int TILE = TILE_, PARTS = PARTS_;
+  static constexpr int kWM = 2, kWN = TILE >= 192 ? 4 : 2;
+  static constexpr int kWaves = kWM * kWN, kThreads = kWaves * 64;
+  static constexpr int kDepth = PARTS == 2 ? 32 : 64;
+  static constexpr int kStages = TILE == 256 || TILE == 128 ? 2 : TILE == 192 ? 3 : 4;
+  static constexpr int kChunks = kDepth / 8;        // of 16 bytes in a row of a stage
+  static constexpr int kLoadRows = 64 / kChunks;    // rows that one load of a wave brings
+  static constexpr int kRowsM = TILE / kWM, kRowsN = TILE / kWN;  // of a wave
+  static constexpr int kFM = kRowsM / 16, kFN = kRowsN / 16;
+  static constexpr int kLoads = 2 * PARTS * TILE / kLoadRows / kWaves;  // of a wave, a stage
+  static constexpr int kPlane = TILE * kDepth, kStage = 2 * PARTS * kPlane;  // halves
+  static constexpr int kHalves = kStages * kStage;
+  // Two blocks of the smaller tiles share a compute unit.
+  static constexpr int kBlocks = TILE >= 192 ? 1 : 2;
+  // A second set of operands in registers has no room beside the sums of a 256 tile in two parts.
+  static constexpr bool kAhead = !(TILE == 256 && PARTS == 2);
 };
-template <>
-struct ProductShape<128> {
-  static constexpr int kWM = 2, kWN = 2;
-};
-template <>
-struct ProductShape<256> {
-  static constexpr int kWM = 2, kWN = 4;
-};
-template <int TILE>
-constexpr int product_threads() {
-  return ProductShape<TILE>::kWM * ProductShape<TILE>::kWN * 64;
+
+// Chunk c of row r of a stage lies at place c ^ (r & 7) of its row (with 32 halves a row: of the pair of rows), so that
+// the sixteen rows that a wave reads together lie in different banks.
+template <int CHUNKS>
+__device__ __forceinline__ int stage_place(int r, int c) {
+  if constexpr (CHUNKS == 8)
+    return r * 64 + ((c ^ (r & 7)) << 3);
+  else
+    return r * 32 + ((c ^ ((r >> 1) & 3)) << 3);
 }
-constexpr int product_depth(int parts) { return parts == 2 ? 32 : 64; }  // of the summed index, a stage
-template <int TILE, int PARTS>
-constexpr int product_lds() {
-  return 2 * PARTS * 2 * TILE * product_depth(PARTS) * 2;  // two stages of both operands, bytes
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N loads are outstanding, and LDS reads are through
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void block_barrier() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// acc += P Q^T for `steps` stages (two at least, an even number with two parts), P's and Q's rows `ld` apart.  Rows from
+// p_rows / q_rows on count as zeros, and so do stages behind the last: the loads' descriptors end there.
+template <class S>
+__device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int p_rows, const _Float16* q, int64_t q_plane,
+                                         int q_rows, int ld, int steps, _Float16* lds, f32x4 (&acc)[S::kFM][S::kFN]) {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the loads to LDS are unknown to the host's compiler)
+  constexpr int TILE = S::TILE, PARTS = S::PARTS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / S::kWN * S::kRowsM, wj = wave % S::kWN * S::kRowsN;
+  const int lr = lane / S::kChunks;
+  const int lc = S::kChunks == 8 ? (lane % 8) ^ (lr & 7) : (lane % 4) ^ ((lr >> 1) & 3);
+  const int voff = (lr * ld + lc * 8) * 2;
+  const int group_bytes = S::kLoadRows * ld * 2;
+  constexpr int G = TILE / S::kLoadRows;  // loads of one operand's part
+  auto fetch = [&](int k, int stage) {
+    const int there = k < steps ? -1 : 0;
+#pragma unroll
+    for (int l = 0; l < S::kLoads; ++l) {
+      const int u = l * S::kWaves + wave;  // P's parts, then Q's
+      const bool is_q = u >= PARTS * G;
+      const int v = is_q ? u - PARTS * G : u;
+      const int s = PARTS == 1 ? 0 : v / G, g = PARTS == 1 ? v : v % G;
+      const _Float16* base = is_q ? q + s * q_plane : p + s * p_plane;
+      const int bytes = ((is_q ? q_rows : p_rows) * ld * 2) & there;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(base), 0, bytes, 0x00027000),
+          (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + u * (S::kLoadRows * S::kDepth)), 16,
+          voff + (g * group_bytes + k * (S::kDepth * 2)), 0, 0, 0);
+    }
+  };
+  constexpr int KS = S::kDepth / 32;
+  constexpr int SETS = S::kAhead ? 2 : 1;
+  half8 fp[SETS][PARTS][S::kFM], fq[SETS][PARTS][S::kFN];
+  auto read = [&](int stage, int ks, int to) {
+    const _Float16* here = lds + stage * S::kStage;
+    const int c = ks * 4 + (lane >> 4);
+#pragma unroll
+    for (int s = 0; s < PARTS; ++s) {
+#pragma unroll
+      for (int i = 0; i < S::kFM; ++i)
+        fp[to][s][i] = *reinterpret_cast<const half8*>(here + s * S::kPlane + stage_place<S::kChunks>(wi + i * 16 + (lane & 15), c));
+#pragma unroll
+      for (int j = 0; j < S::kFN; ++j)
+        fq[to][s][j] =
+            *reinterpret_cast<const half8*>(here + (PARTS + s) * S::kPlane + stage_place<S::kChunks>(wj + j * 16 + (lane & 15), c));
+    }
+  };
+  auto mul = [&](int of) {
+#pragma unroll
+    for (int i = 0; i < S::kFM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::kFN; ++j) {
+        if constexpr (PARTS == 2) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[of][PARTS - 1][i], fq[of][0][j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[of][0][i], fq[of][PARTS - 1][j], acc[i][j], 0, 0, 0);
+        }
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[of][0][i], fq[of][0][j], acc[i][j], 0, 0, 0);
+      }
+  };
+  constexpr int N = S::kStages;
+#pragma unroll
+  for (int s = 0; s < (S::kAhead ? N : N - 1); ++s) fetch(s, s);
+  int st = 0;
+  if constexpr (S::kAhead) {
+    wait_loads<(N - 1) * S::kLoads>();
+    block_barrier();
+    read(0, 0, 0);
+    auto stage = [&](int k, int base, bool more) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int now = (base + ks) & 1;
+        if (ks + 1 < KS) {
+          read(st, ks + 1, now ^ 1);
+        } else if (more) {
+          const int next = st + 1 == N ? 0 : st + 1;
+          wait_loads<(N - 2) * S::kLoads>();  // the next stage is there, and this one read whole
+          block_barrier();
+          fetch(k + N, st);
+          read(next, 0, now ^ 1);
+          st = next;
+        }
+        mul(now);
+        __builtin_amdgcn_sched_barrier(0);  // (or the reads sink to their uses)
+      }
+    };
+    if constexpr (KS % 2 == 0) {
+      for (int k = 0; k + 1 < steps; ++k) stage(k, 0, true);
+      stage(steps - 1, 0, false);
+    } else {
+      for (int k = 0; k + 2 < steps; k += 2) {
+        stage(k, 0, true);
+        stage(k + 1, 1, true);
+      }
+      stage(steps - 2, 0, true);
+      stage(steps - 1, 1, false);
+    }
+  } else {
+    for (int k = 0; k < steps; ++k) {
+      wait_loads<(N - 2) * S::kLoads>();
+      block_barrier();
+      fetch(k + N - 1, st == 0 ? N - 1 : st - 1);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        read(st, ks, 0);
+        mul(0);
+      }
+      st = st + 1 == N ? 0 : st + 1;
+    }
+  }
+  wait_loads<0>();  // the loads behind the last stage still write
+  block_barrier();
+#endif
+}
+
+// One wave's rows of a tile, by way of its own part of LDS: `value(i, j)` are four sums of rows 16 i + 4 (lane / 16) ..
+// and column 16 j + lane % 16; they go as halves to out[row ld + col] and, `both`, to out_t[col ld_t + row].  Rows and
+// columns from `rows` and `cols` on are left out (whole chunks of eight: both are multiples of 64).
+template <int FM, int FN, int PARTS, class Value>
+__device__ __forceinline__ void store_halves(Value&& value, _Float16* room, int row0, int col0, int rows, int cols,
+                                             _Float16* out, int64_t ld, _Float16* out_t, int64_t ld_t, int64_t plane,
+                                             bool both) {
+  constexpr int CF = FM > 4 ? FM / 2 : FM;  // fragments of rows at a time
+  constexpr int CR = CF * 16, CC = FN * 16;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int h = 0; h < FM; h += CF) {
+    half4 v[PARTS][CF][FN];
+#pragma unroll
+    for (int i = 0; i < CF; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const f32x4 x = value(h + i, j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          _Float16 p[PARTS];
+          split_half<PARTS>(x[e], p);
+#pragma unroll
+          for (int s = 0; s < PARTS; ++s) v[s][i][j][e] = p[s];
+        }
+      }
+#pragma unroll
+    for (int s = 0; s < PARTS; ++s) {
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < CF; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            room[(i * 16 + (lane >> 4) * 4 + e) * (CC + 8) + j * 16 + (lane & 15)] = v[s][i][j][e];
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int u = 0; u < CR * CC / 8; u += 64) {
+        const int r = (u + lane) / (CC / 8), c = (u + lane) % (CC / 8) * 8;
+        if ((CR * CC / 8) % 64 && u + lane >= CR * CC / 8) continue;
+        const half8 x = *reinterpret_cast<const half8*>(room + r * (CC + 8) + c);
+        const int row = row0 + h * 16 + r, col = col0 + c;
+        if (row < rows && col < cols) *reinterpret_cast<half8*>(out + s * plane + row * ld + col) = x;
+      }
+      asm volatile("" ::: "memory");
+      if (!both) continue;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < CF; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          *reinterpret_cast<half4*>(room + (j * 16 + (lane & 15)) * (CR + 8) + i * 16 + (lane >> 4) * 4) = v[s][i][j];
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int u = 0; u < CR * CC / 8; u += 64) {
+        const int c = (u + lane) / (CR / 8), r = (u + lane) % (CR / 8) * 8;
+        if ((CR * CC / 8) % 64 && u + lane >= CR * CC / 8) continue;
+        const half8 x = *reinterpret_cast<const half8*>(room + c * (CR + 8) + r);
+        const int row = row0 + h * 16 + r, col = col0 + c;
+        if (row < rows && col < cols) *reinterpret_cast<half8*>(out_t + s * plane + col * ld_t + row) = x;
+      }
+      asm volatile("" ::: "memory");
+    }
+  }
+}
+
+// Halves of LDS that a wave's stores need: 16 bytes between rows beyond their length.
+template <int FM, int FN>
+constexpr int store_room() {
+  constexpr int CR = (FM > 4 ? FM / 2 : FM) * 16, CC = FN * 16;
+  constexpr int a = CR * (CC + 8), b = CC * (CR + 8), c = 2 * 32 * (CC + 4);  // c: 32 rows of floats
+  return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
 template <int TILE, int PARTS, int MODE>
-__global__ __launch_bounds__(product_threads<TILE>()) void k_mat_product(
+__global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShape<TILE, PARTS>::kBlocks)) void k_mat_product(
     const MatDesc* __restrict__ mats, const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, int from, float ca,
-    float cb, float cc, FinishArgs f) {
-  using S = ProductShape<TILE>;
-  constexpr int THREADS = product_threads<TILE>();
-  constexpr int BK = product_depth(PARTS);
-  constexpr int CH = BK / 8;                 // 16-byte chunks of a row
-  constexpr int FM = TILE / S::kWM / 32, FN = TILE / S::kWN / 32;
-  constexpr int LOADS = TILE * CH / THREADS;  // chunks of one operand's part a thread brings
-  __shared__ __align__(16) _Float16 lds[product_lds<TILE, PARTS>() / 2];
-  constexpr int PLANE = TILE * BK;            // halves of one operand's part in a stage
-  constexpr int STAGE = 2 * PARTS * PLANE;
+    float cb, float cc, FinishArgs f, float* __restrict__ partial, uint32_t* __restrict__ arrived) {
+  using S = ProductShape<TILE, PARTS>;
+  constexpr int FM = S::kFM, FN = S::kFN;
+  constexpr int kRoom = store_room<FM, FN>();
+  constexpr int kNeed = kRoom * S::kWaves > S::kHalves ? kRoom * S::kWaves : S::kHalves;
+  __shared__ __align__(16) _Float16 lds[kNeed];
 
   const MatTile t = tiles[blockIdx.x];
   const MatDesc& d = mats[t.mat];
   const bool swap = MODE == kFinal && d.tall;  // X^T wanted: its rows are X^T's, Q is symmetric
   const int64_t mm = (int64_t)d.mp * d.mp, mn = (int64_t)d.mp * d.np;
+  const int i0 = t.i * TILE, j0 = t.j * TILE;
+  const int rows = swap ? d.np : d.mp, cols = MODE == kApply || MODE == kFinal ? (swap ? d.mp : d.np) : d.mp;
   const _Float16 *p, *q;
   int64_t p_plane, q_plane;
-  int K;
+  int ld, begin = 0, end;
   if constexpr (MODE == kGram) {
     p = q = mem + d.x;
     p_plane = q_plane = mn;
-    K = d.np;
+    ld = d.np;
+    // a share is whole pieces of 64
+    begin = (int)((int64_t)(ld / 64) * t.share / t.shares) * 64;
+    end = (int)((int64_t)(ld / 64) * (t.share + 1) / t.shares) * 64;
   } else if constexpr (MODE == kSquare) {
     p = q = mem + d.a;
     p_plane = q_plane = mm;
-    K = d.mp;
+    ld = end = d.mp;
   } else {
     p = mem + (swap ? d.xt[from] : d.q);
     q = mem + (swap ? d.q : d.xt[from]);
     p_plane = swap ? mn : mm;
     q_plane = swap ? mm : mn;
-    K = d.mp;
+    ld = end = d.mp;
   }
-  const int i0 = t.i * TILE, j0 = t.j * TILE;
-  p += (int64_t)i0 * K;
-  q += (int64_t)j0 * K;
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wi = wave / S::kWN * (FM * 32), wj = wave % S::kWN * (FN * 32);
-
-  f32x16 acc[FM][FN];
+  f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    for (int j = 0; j < FN; ++j) acc[i][j] = 0.0f;
+  const int p_rows = rows - i0 < TILE ? rows - i0 : TILE;
+  const int q_all = MODE == kApply || MODE == kFinal ? cols : rows;
+  const int q_rows = q_all - j0 < TILE ? q_all - j0 : TILE;
+  multiply<S>(p + (int64_t)i0 * ld + begin, p_plane, p_rows, q + (int64_t)j0 * ld + begin, q_plane, q_rows, ld,
+              (end - begin) / S::kDepth, lds, acc);
 
-  // chunk c of row r lies at place c ^ (r & 7) of the row (with 32 halves a row: of two rows), so that the rows a wave
-  // reads side by side lie in different banks
-  auto place = [](int r, int c) {
-    if constexpr (CH == 8)
-      return r * BK + ((c ^ (r & 7)) << 3);
-    else
-      return r * BK + ((c ^ ((r >> 1) & 3)) << 3);
-  };
-  half8 held[2 * PARTS][LOADS];
-  auto fetch = [&](int k0) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = i0 + wave / S::kWN * S::kRowsM, col0 = j0 + wave % S::kWN * S::kRowsN;
+  _Float16* room = lds + wave * kRoom;
+  if constexpr (MODE == kGram) {
+    if (t.shares > 1) {
+      // Every share leaves its sums; the block that finds itself the last one adds them in their order and goes on.
+      // Nobody waits.
+      constexpr int kEach = TILE * TILE;
+      f32x4* mine = reinterpret_cast<f32x4*>(partial + ((int64_t)t.slot + t.share) * kEach) + threadIdx.x;
 #pragma unroll
-    for (int s = 0; s < PARTS; ++s)
+      for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int l = 0; l < LOADS; ++l) {
-        const int u = l * THREADS + threadIdx.x;
-        const int64_t at = (int64_t)(u / CH) * K + k0 + u % CH * 8;
-        held[s][l] = *reinterpret_cast<const half8*>(p + s * p_plane + at);
-        held[PARTS + s][l] = *reinterpret_cast<const half8*>(q + s * q_plane + at);
+        for (int j = 0; j < FN; ++j) mine[(i * FN + j) * S::kThreads] = acc[i][j];
+      __threadfence();
+      __syncthreads();
+      uint32_t* last = reinterpret_cast<uint32_t*>(lds);
+      if (threadIdx.x == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(arrived + t.slot, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        *last = before + 1 == t.shares;
+        if (*last) __hip_atomic_store(arrived + t.slot, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
-  };
-  auto put = [&](int stage) {
-#pragma unroll
-    for (int s = 0; s < 2 * PARTS; ++s)
-#pragma unroll
-      for (int l = 0; l < LOADS; ++l) {
-        const int u = l * THREADS + threadIdx.x;
-        *reinterpret_cast<half8*>(lds + stage * STAGE + s * PLANE + place(u / CH, u % CH)) = held[s][l];
-      }
-  };
-  fetch(0);
-  put(0);
-  __syncthreads();
-  const int steps = K / BK;
-  for (int k = 0; k < steps; ++k) {
-    if (k + 1 < steps) fetch((k + 1) * BK);
-    const _Float16* here = lds + (k & 1) * STAGE;
-#pragma unroll
-    for (int ks = 0; ks < BK / 16; ++ks) {
-      half8 fp[PARTS][FM], fq[PARTS][FN];
-      const int c = ks * 2 + (lane >> 5);
-#pragma unroll
-      for (int s = 0; s < PARTS; ++s) {
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-          fp[s][i] = *reinterpret_cast<const half8*>(here + s * PLANE + place(wi + i * 32 + (lane & 31), c));
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          fq[s][j] = *reinterpret_cast<const half8*>(here + (PARTS + s) * PLANE + place(wj + j * 32 + (lane & 31), c));
-      }
+      __syncthreads();
+      if (!*last) return;
+      __threadfence();
+      const f32x4* all = reinterpret_cast<const f32x4*>(partial + (int64_t)t.slot * kEach) + threadIdx.x;
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-          if constexpr (PARTS == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fp[1][i], fq[0][j], acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fp[0][i], fq[1][j], acc[i][j], 0, 0, 0);
-          }
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fp[0][i], fq[0][j], acc[i][j], 0, 0, 0);
+          f32x4 v = all[(i * FN + j) * S::kThreads];
+          for (int s = 1; s < t.shares; ++s) v += all[(int64_t)s * (kEach / 4) + (i * FN + j) * S::kThreads];
+          acc[i][j] = v;
         }
+      __syncthreads();  // `last` lies where the waves' rooms do
     }
-    if (k + 1 < steps) put((k + 1) & 1);
-    __syncthreads();
   }
-
-  // a lane has column lane & 31 and, of each 8 rows, the four from 4 (lane >> 5) on
+  if constexpr (MODE == kFinal) {
+    const int out_rows = d.tall ? d.n : d.m, out_cols = d.tall ? d.m : d.n;
+    const float by = d.scale * (1.0f / (kOperandScale * kOperandScale));
+    const int size = f.type == kTypeF32 ? 4 : 2;
+    const bool wide = out_cols % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * size) % (4 * size) == 0;
+    constexpr int CC = FN * 16;
+    float* fl = reinterpret_cast<float*>(room);
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+    for (int h = 0; h < FM; h += 2) {
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int row = i0 + wi + i * 32 + g * 8 + (lane >> 5) * 4, col = j0 + wj + j * 32 + (lane & 31);
-        if constexpr (MODE == kFinal) {
-          const int rows = d.tall ? d.n : d.m, cols = d.tall ? d.m : d.n;
-          if (col < cols) {
+        for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (row + e < rows)
-                finish(f, d.at + (int64_t)(row + e) * cols + col,
-                       acc[i][j][g * 4 + e] * (d.scale / (kOperandScale * kOperandScale)));
+          for (int e = 0; e < 4; ++e)
+            fl[(i * 16 + (lane >> 4) * 4 + e) * (CC + 4) + j * 16 + (lane & 15)] = acc[h + i][j][e] * by;
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+      if (wide) {
+#pragma unroll
+        for (int u = 0; u < 32 * CC / 4; u += 64) {
+          const int r = (u + lane) / (CC / 4), c = (u + lane) % (CC / 4) * 4;
+          const int row = row0 + h * 16 + r, col = col0 + c;
+          if (row < out_rows && col < out_cols) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fl[r * (CC + 4) + c + e];
+            finish<4>(f, d.at + (int64_t)row * out_cols + col, v);
           }
-        } else {
-          const int64_t ld = MODE == kApply ? d.np : d.mp, ldt = d.mp;
-          const int64_t plane = MODE == kApply ? mn : mm;
-          _Float16* out = mem + (MODE == kGram ? d.a : MODE == kSquare ? d.q : d.x);
-          _Float16* out_t = MODE == kApply ? mem + d.xt[from ^ 1] : out;
-          _Float16 h[4][PARTS];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float v = acc[i][j][g * 4 + e] * (1.0f / kOperandScale);
-            if constexpr (MODE == kSquare) {
-              const _Float16* pa = mem + d.a + (int64_t)(row + e) * ld + col;
-              float av = static_cast<float>(pa[0]);
-              if constexpr (PARTS == 2) av += static_cast<float>(pa[mm]);
-              v = fmaf(cc, v, cb * av);
-              if (row + e == col) v += ca * kOperandScale;
-            }
-            split_half<PARTS>(v, h[e]);
-          }
-#pragma unroll
-          for (int s = 0; s < PARTS; ++s) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[s * plane + (int64_t)(row + e) * ld + col] = h[e][s];
-            if (MODE == kApply || t.i != t.j) {  // (a tile on the diagonal holds its own transpose)
-              typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-              half4 v4 = {h[0][s], h[1][s], h[2][s], h[3][s]};
-              *reinterpret_cast<half4*>(out_t + s * plane + (int64_t)col * ldt + row) = v4;
-            }
+        }
+      } else {
+#pragma unroll 4
+        for (int u = 0; u < 32 * CC; u += 64) {
+          const int r = (u + lane) / CC, c = (u + lane) % CC;
+          const int row = row0 + h * 16 + r, col = col0 + c;
+          if (row < out_rows && col < out_cols) {
+            const float v[1] = {fl[r * (CC + 4) + c]};
+            finish<1>(f, d.at + (int64_t)row * out_cols + col, v);
           }
         }
       }
+      asm volatile("" ::: "memory");
+    }
+  } else if constexpr (MODE == kSquare) {
+    // (A is symmetric: four rows of one column lie side by side in that row)
+    auto value = [&](int i, int j) {
+      const int row = row0 + i * 16 + (lane >> 4) * 4, col = col0 + j * 16 + (lane & 15);
+      f32x4 v = acc[i][j] * (cc / kOperandScale);
+      if (row < rows && col < cols) {
+        const _Float16* pa = mem + d.a + (int64_t)col * d.mp + row;
+        const half4 hi = *reinterpret_cast<const half4*>(pa);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float av = static_cast<float>(hi[e]);
+          if constexpr (PARTS == 2) av += static_cast<float>(reinterpret_cast<const half4*>(pa + mm)[0][e]);
+          v[e] = fmaf(cb, av, v[e]);
+          if (row + e == col) v[e] += ca * kOperandScale;
+        }
+      }
+      return v;
+    };
+    store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.q, d.mp, mem + d.q, d.mp, mm, t.i != t.j);
+  } else {
+    auto value = [&](int i, int j) { return acc[i][j] * (1.0f / kOperandScale); };
+    if constexpr (MODE == kGram)
+      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.a, d.mp, mem + d.a, d.mp, mm, t.i != t.j);
+    else
+      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.x, d.np, mem + d.xt[from ^ 1], d.mp, mn, true);
+  }
 }
 
 }  // namespace artopk
