@@ -42,22 +42,35 @@ struct MatPlan {
   std::vector<MatTile> tiles;
   Span begin;
   Product gram, square, apply, final_;
+  Span join;  // the tiles of Gram matrices whose sums are cut
   int64_t halves = 0;  // of the iterates' memory
   int32_t sums = 0;
   int64_t slots = 0;   // partial sums of the Gram products' shares
   // places in the slab
-  size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_arrived = 0, o_partial = 0, o_mem = 0, total = 0;
+  size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_partial = 0, o_mem = 0, total = 0;
 };
 
-// What a product costs, in us, by tile class: a block alone on its compute unit for each 64 of the summed index, and the
-// whole chip's time for each 64 of one of very many blocks.
+// What a product's block costs, in us, by tile class: alone on its compute unit (`fixed` and `alone` for each 64 of the
+// summed index), and as the chip's time for one of very many blocks (`store` and `among` for each 64).  Fitted to products
+// timed one kind at a time, tile by tile: 4096 x 4096 (64 of 64), sixteen matrices of 1280 x 1280 and eight of 1280 x 5120
+// (20 of 64 where m is summed over), and the long sums of one 1280 x 5120 by itself.  What the rule has to get right (us,
+// HALF, tiles of 64 / 128 / 192 / 256): X X^T of 4096 x 4096 132 / 100 / 80 / 99, Q X of it 235 / 138 / 152 / 117, X X^T of
+// 2048 x 2048 22 / 24 / 33 / 48, of 1280 x 5120 19 / 54 / 72 / 108.
 struct TileCost {
-  double alone, among, fixed;
+  double fixed, alone, store, among;
+  int slots;  // blocks that the chip holds
 };
-constexpr TileCost kCost[2][kTileClasses] = {
-    {{0.21, 0.00072, 3.0}, {0.53, 0.00197, 4.0}, {0.85, 0.0043, 5.0}, {1.25, 0.0070, 6.0}},
-    {{0.42, 0.0023, 3.0}, {1.10, 0.0055, 4.0}, {2.0, 0.0115, 5.0}, {3.15, 0.0185, 6.0}}};
-constexpr double kJoinCost = 4.0;  // of sums that meet in memory
+constexpr TileCost kCost[2][kTileClasses] = {{{3.0, 0.20, 0.0043, 0.00083, 512},
+                                              {4.0, 0.63, 0.0258, 0.0017, 512},
+                                              {5.0, 0.84, 0.0325, 0.0044, 256},
+                                              {6.0, 1.28, 0.0890, 0.00575, 256}},
+                                             {{3.0, 0.55, 0.0047, 0.00231, 512},
+                                              {4.0, 1.60, 0.0470, 0.0047, 512},
+                                              {5.0, 1.93, 0.0820, 0.0100, 256},
+                                              {6.0, 3.80, 0.1890, 0.0160, 256}}};
+// Shares that meet in memory: a launch, the shares of one tile one after the other, and their bytes (36 tiles of 64 x 64 in 9
+// shares each 4.6, 10 of 128 x 128 in 18 9.1, one of 64 x 64 in 32 11.1).
+constexpr double kJoinLaunch = 3.5, kJoinShare = 0.22, kJoinBytes = 1.0 / 2.5e6;
 
 int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
 
@@ -78,23 +91,33 @@ int product_shares(const MatDesc& d, const ProductKind& k, int each) {  // `each
 
 double product_cost(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, int cls, int each) {
   const TileCost& c = kCost[parts - 1][cls];
-  double sum = 0.0, longest = 0.0;
-  bool cut = false;
+  double chip = 0.0, blocks = 0.0, units_in_all = 0.0, longest = 0.0, joined = 0.0;
+  int most_shares = 1;
   for (const MatDesc& d : mats) {
     const double units = (k.long_sum ? d.np : d.mp) / 64;
     const int shares = product_shares(d, k, each);
-    sum += units * (double)product_tiles(d, k, kTileOf[cls]);
+    const double tiles = (double)product_tiles(d, k, kTileOf[cls]);
+    chip += tiles * (shares * c.store + units * c.among);
+    blocks += tiles * shares;
+    units_in_all += tiles * units;
     longest = std::max(longest, std::ceil(units / shares));
-    cut |= shares > 1;
+    if (shares > 1) joined += tiles * shares * kTileOf[cls] * kTileOf[cls] * 8.0;
+    most_shares = std::max(most_shares, shares);
   }
-  return std::max(c.alone * longest, c.among * sum) + c.fixed + (cut ? kJoinCost : 0.0);
+  // whole rounds of blocks at the chip's rate, and a last one that takes a block's own time at least
+  const double rounds = std::floor(blocks / c.slots), rest = blocks - rounds * c.slots;
+  double cost = chip * (rounds * c.slots / blocks);
+  if (rest > 0.0) cost += std::max(c.fixed + c.alone * (units_in_all / blocks), chip * (rest / blocks));
+  cost = std::max(cost, c.fixed + c.alone * longest);
+  if (most_shares > 1) cost += kJoinLaunch + kJoinShare * most_shares + kJoinBytes * joined;
+  return cost;
 }
 
 // The tile and, for the Gram products, the length of a share that cost least.
 void choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, Product* p, int* each_out) {
   double best = 1e300;
   for (int cls = 0; cls < kTileClasses; ++cls)
-    for (int each : {0, 32, 16, 8, 4}) {
+    for (int each : {0, 64, 32, 16, 8}) {
       if (each && (!k.long_sum || cls > 1)) continue;
       const double cost = product_cost(mats, k, parts, cls, each);
       if (cost < best) {
@@ -242,6 +265,12 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
   plan->final_.cls = plan->apply.cls;
   list_product(plan, gram, &plan->gram, each, false);
+  plan->join.at = plan->tiles.size();
+  for (int i = 0; i < plan->gram.tiles.count; ++i) {
+    const MatTile t = plan->tiles[plan->gram.tiles.at + i];
+    if (t.shares > 1 && t.share == 0) plan->tiles.push_back(t);
+  }
+  plan->join.count = (int)(plan->tiles.size() - plan->join.at);
   list_product(plan, square, &plan->square, 0, false);
   list_product(plan, apply, &plan->apply, 0, false);
   list_product(plan, apply, &plan->final_, 0, true);
@@ -257,7 +286,6 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   plan->o_chunks = take(plan->chunks.size() * sizeof(MatChunk));
   plan->o_tiles = take(plan->tiles.size() * sizeof(MatTile));
   plan->o_sums = take((size_t)plan->sums * sizeof(double));
-  plan->o_arrived = take((size_t)plan->slots * sizeof(uint32_t));
   plan->o_partial = take((size_t)plan->slots * kTileOf[plan->gram.cls] * kTileOf[plan->gram.cls] * sizeof(float));
   plan->o_mem = take((size_t)plan->halves * 2);
   plan->total = at;
@@ -273,7 +301,7 @@ struct artopk_matrices {
   int nchunks = 0;
   Span begin;
   Product gram, square, apply, final_;
-  uint32_t* arrived = nullptr;
+  Span join;
   float* partial = nullptr;
   char* slab = nullptr;
   const MatDesc* mats = nullptr;
@@ -335,7 +363,7 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 template <int TILE, int PARTS, int MODE>
 void product(artopk_matrices* h, const Span& s, int from, const float* co, const FinishArgs& f) {
   k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
-      h->mats, h->tiles + s.at, h->mem, from, co[0], co[1], co[2], f, h->partial, h->arrived);
+      h->mats, h->tiles + s.at, h->mem, from, co[0], co[1], co[2], f, h->partial);
 }
 
 template <int PARTS, int MODE>
@@ -348,6 +376,12 @@ void product(artopk_matrices* h, const Product& p, int from, const float* co, co
   }
 }
 
+template <int TILE, int PARTS>
+void join_shares(artopk_matrices* h) {
+  k_mat_join<TILE, PARTS><<<dim3(h->join.count, 4), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
+      h->mats, h->tiles + h->join.at, h->mem, h->partial);
+}
+
 template <int PARTS, class From>
 void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], float eps, const FinishArgs& f) {
   if (steps == 0) {
@@ -357,6 +391,7 @@ void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], f
   k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->mats, h->tiles + h->begin.at, h->sums, eps, h->mem);
   for (int k = 0; k < steps; ++k) {
     product<PARTS, kGram>(h, h->gram, k & 1, co[k], f);
+    if (h->join.count) h->gram.cls == 0 ? join_shares<64, PARTS>(h) : join_shares<128, PARTS>(h);
     product<PARTS, kSquare>(h, h->square, k & 1, co[k], f);
     if (k + 1 < steps)
       product<PARTS, kApply>(h, h->apply, k & 1, co[k], f);
@@ -425,6 +460,7 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->nchunks = (int)plan.chunks.size();
   h->begin = plan.begin;
   h->gram = plan.gram;
+  h->join = plan.join;
   h->square = plan.square;
   h->apply = plan.apply;
   h->final_ = plan.final_;
@@ -440,7 +476,6 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->chunks = reinterpret_cast<const MatChunk*>(h->slab + plan.o_chunks);
   h->tiles = reinterpret_cast<const MatTile*>(h->slab + plan.o_tiles);
   h->sums = reinterpret_cast<double*>(h->slab + plan.o_sums);
-  h->arrived = reinterpret_cast<uint32_t*>(h->slab + plan.o_arrived);
   h->partial = reinterpret_cast<float*>(h->slab + plan.o_partial);
   h->mem = reinterpret_cast<_Float16*>(h->slab + plan.o_mem);
   e = hipMemcpy(h->slab + plan.o_mats, plan.mats.data(), plan.mats.size() * sizeof(MatDesc), hipMemcpyHostToDevice);
@@ -448,8 +483,6 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
     e = hipMemcpy(h->slab + plan.o_chunks, plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk), hipMemcpyHostToDevice);
   if (e == hipSuccess)
     e = hipMemcpy(h->slab + plan.o_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MatTile), hipMemcpyHostToDevice);
-  if (e == hipSuccess && plan.slots) e = hipMemset(h->slab + plan.o_arrived, 0, (size_t)plan.slots * sizeof(uint32_t));
-  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     (void)hipFree(h->slab);
     delete h;

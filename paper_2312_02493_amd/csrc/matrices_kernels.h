@@ -79,20 +79,39 @@ __device__ __forceinline__ double block_sum(double v, double* room) {
   return s;
 }
 
-// Sums of squares of the matrices' pieces.
+// Sums of squares of the matrices' pieces.  Sixteen bytes a load from the first aligned place on; a thread's sums are
+// float64.
 template <class T>
 __global__ __launch_bounds__(256) void k_mat_squares(const T* __restrict__ x, const MatChunk* __restrict__ chunks,
                                                      double* __restrict__ sums) {
+  constexpr int V = 16 / sizeof(T);
   __shared__ double room[4];
   const MatChunk c = chunks[blockIdx.x];
   if (c.mat < 0) return;
-  double s = 0.0;
-  for (int64_t i = c.begin + threadIdx.x; i < c.end; i += 256) {
-    const double v = static_cast<double>(static_cast<float>(x[i]));
-    s = fma(v, v, s);
+  double s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = 0.0;
+  auto add = [&](int i, float v) { s[i] = fma((double)v, (double)v, s[i]); };
+  const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(x + c.begin) / sizeof(T) % V);
+  const int64_t body = c.begin + (off ? V - off : 0);
+  if (body >= c.end) {
+    if (c.begin + (int64_t)threadIdx.x < c.end) add(0, static_cast<float>(x[c.begin + threadIdx.x]));
+  } else {
+    if (c.begin + (int64_t)threadIdx.x < body) add(0, static_cast<float>(x[c.begin + threadIdx.x]));
+    const int64_t whole = body + (c.end - body) / V * V;
+#pragma unroll 4
+    for (int64_t i = body + threadIdx.x * V; i < whole; i += 256 * V) {
+      float v[V];
+      load_elems<V>(v, x + i);
+#pragma unroll
+      for (int e = 0; e < V; ++e) add(e, v[e]);
+    }
+    if (whole + (int64_t)threadIdx.x < c.end) add(1, static_cast<float>(x[whole + threadIdx.x]));
   }
-  s = block_sum(s, room);
-  if (threadIdx.x == 0) sums[c.slot] = s;
+#pragma unroll
+  for (int i = 1; i < V; ++i) s[0] += s[i];
+  const double total = block_sum(s[0], room);
+  if (threadIdx.x == 0) sums[c.slot] = total;
 }
 
 // Momentum, the sums of squares of the direction v, and the weights of no matrix.
@@ -483,7 +502,7 @@ constexpr int store_room() {
 template <int TILE, int PARTS, int MODE>
 __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShape<TILE, PARTS>::kBlocks)) void k_mat_product(
     const MatDesc* __restrict__ mats, const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, int from, float ca,
-    float cb, float cc, FinishArgs f, float* __restrict__ partial, uint32_t* __restrict__ arrived) {
+    float cb, float cc, FinishArgs f, float* __restrict__ partial) {
   using S = ProductShape<TILE, PARTS>;
   constexpr int FM = S::kFM, FN = S::kFN;
   constexpr int kRoom = store_room<FM, FN>();
@@ -532,36 +551,13 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
   const int row0 = i0 + wave / S::kWN * S::kRowsM, col0 = j0 + wave % S::kWN * S::kRowsN;
   _Float16* room = lds + wave * kRoom;
   if constexpr (MODE == kGram) {
-    if (t.shares > 1) {
-      // Every share leaves its sums; the block that finds itself the last one adds them in their order and goes on.
-      // Nobody waits.
-      constexpr int kEach = TILE * TILE;
-      f32x4* mine = reinterpret_cast<f32x4*>(partial + ((int64_t)t.slot + t.share) * kEach) + threadIdx.x;
+    if (t.shares > 1) {  // the sums of this share, for k_mat_join
+      f32x4* mine = reinterpret_cast<f32x4*>(partial + ((int64_t)t.slot + t.share) * (TILE * TILE)) + threadIdx.x;
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) mine[(i * FN + j) * S::kThreads] = acc[i][j];
-      __threadfence();
-      __syncthreads();
-      uint32_t* last = reinterpret_cast<uint32_t*>(lds);
-      if (threadIdx.x == 0) {
-        const uint32_t before = __hip_atomic_fetch_add(arrived + t.slot, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        *last = before + 1 == t.shares;
-        if (*last) __hip_atomic_store(arrived + t.slot, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-      __syncthreads();
-      if (!*last) return;
-      __threadfence();
-      const f32x4* all = reinterpret_cast<const f32x4*>(partial + (int64_t)t.slot * kEach) + threadIdx.x;
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          f32x4 v = all[(i * FN + j) * S::kThreads];
-          for (int s = 1; s < t.shares; ++s) v += all[(int64_t)s * (kEach / 4) + (i * FN + j) * S::kThreads];
-          acc[i][j] = v;
-        }
-      __syncthreads();  // `last` lies where the waves' rooms do
+      return;
     }
   }
   if constexpr (MODE == kFinal) {
@@ -634,6 +630,41 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
     else
       store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.x, d.np, mem + d.xt[from ^ 1], d.mp, mn, true);
   }
+}
+
+// Adds the shares of a Gram matrix's tiles in their order and stores the tile, a quarter of each wave's fragments a block.
+// (The blocks of the product cannot do it themselves, the last one of a tile: that takes a write-back of a die's whole cache
+// by every block before it says that it is through.  480 blocks of 128 x 128 sums took 150 us so, 20 in two launches.)
+template <int TILE, int PARTS>
+__global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads)) void k_mat_join(
+    const MatDesc* __restrict__ mats, const MatTile* __restrict__ tiles, _Float16* __restrict__ mem,
+    const float* __restrict__ partial) {
+  using S = ProductShape<TILE, PARTS>;
+  constexpr int FM = S::kFM, FN = S::kFN;
+  constexpr int QM = FM / 2, QN = FN / 2;
+  constexpr int kRoom = store_room<QM, QN>();
+  __shared__ __align__(16) _Float16 lds[kRoom * S::kWaves];
+  const MatTile t = tiles[blockIdx.x];
+  const MatDesc& d = mats[t.mat];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qi = (blockIdx.y >> 1) * QM, qj = (blockIdx.y & 1) * QN;
+  const int row0 = t.i * TILE + wave / S::kWN * S::kRowsM + qi * 16;
+  const int col0 = t.j * TILE + wave % S::kWN * S::kRowsN + qj * 16;
+  const f32x4* all = reinterpret_cast<const f32x4*>(partial + (int64_t)t.slot * (TILE * TILE)) + threadIdx.x;
+  f32x4 sum[QM][QN];
+#pragma unroll
+  for (int i = 0; i < QM; ++i)
+#pragma unroll
+    for (int j = 0; j < QN; ++j) sum[i][j] = all[((qi + i) * FN + qj + j) * S::kThreads];
+  for (int s = 1; s < t.shares; ++s)
+#pragma unroll
+    for (int i = 0; i < QM; ++i)
+#pragma unroll
+      for (int j = 0; j < QN; ++j)
+        sum[i][j] += all[(int64_t)s * (TILE * TILE / 4) + ((qi + i) * FN + qj + j) * S::kThreads];
+  auto value = [&](int i, int j) { return sum[i][j] * (1.0f / kOperandScale); };
+  store_halves<QM, QN, PARTS>(value, lds + wave * kRoom, row0, col0, d.mp, d.mp, mem + d.a, d.mp, mem + d.a, d.mp,
+                              (int64_t)d.mp * d.mp, t.i != t.j);
 }
 
 }  // namespace artopk

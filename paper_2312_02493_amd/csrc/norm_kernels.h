@@ -65,6 +65,16 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
   __shared__ float room[2 * (TPR / 64) + 2];
   const int t = threadIdx.x % TPR;
   const float inv = 1.0f / static_cast<float>(cols);
+  float gm[R][V], bt[R][V];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int c = (r * TPR + t) * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      gm[r][i] = gamma && c < cols ? gamma[c + i] : 1.0f;
+      bt[r][i] = beta && c < cols ? beta[c + i] : 0.0f;
+    }
+  }
   for (int64_t row0 = (int64_t)blockIdx.x * NormShape<TPR>::kRows; row0 < rows;
        row0 += (int64_t)gridDim.x * NormShape<TPR>::kRows) {
     const int64_t row = row0 + threadIdx.x / TPR;
@@ -115,7 +125,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float h = v[r][i] * rstd;
-          o[i] = fmaf(h, gamma ? gamma[c + i] : 1.0f, beta ? beta[c + i] : 0.0f);
+          o[i] = fmaf(h, gm[r][i], bt[r][i]);
         }
         store_elems<V>(yr + c, o);
       }
