@@ -41,7 +41,7 @@ struct MatPlan {
   std::vector<MatChunk> chunks;
   std::vector<MatTile> tiles;
   Span begin;
-  Product gram, square, apply, final_;
+  Product gram, square, apply;
   Span join;  // the tiles of Gram matrices whose sums are cut
   int64_t halves = 0;  // of the iterates' memory
   int32_t sums = 0;
@@ -131,7 +131,7 @@ void choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int 
 // The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
 // each die has a cache of its own: every matrix's tiles are cut into eight runs of neighbours, one for each die, and the
 // matrices with the longest sums come first.
-void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each, bool swap_tall) {
+void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
   const int tile = kTileOf[p->cls];
   std::vector<int> order(plan->mats.size());
   for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
@@ -155,8 +155,8 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each, boo
           if (k.symmetric && y > x) continue;
           MatTile t = {};
           t.mat = (uint32_t)i;
-          t.i = (uint16_t)(swap_tall && d.tall ? y : x);
-          t.j = (uint16_t)(swap_tall && d.tall ? x : y);
+          t.i = (uint16_t)x;
+          t.j = (uint16_t)y;
           t.shares = (uint16_t)shares;
           t.slot = (uint32_t)plan->slots;
           if (shares > 1) plan->slots += shares;
@@ -224,10 +224,9 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
     d.mp = (d.m + 63) / 64 * 64;
     d.np = (d.n + 63) / 64 * 64;
     const int64_t mn = (int64_t)d.mp * d.np * parts, mm = (int64_t)d.mp * d.mp * parts;
-    d.x = plan->halves;
-    d.xt[0] = d.x + mn;
-    d.xt[1] = d.xt[0] + mn;
-    d.a = d.xt[1] + mn;
+    d.x[0] = plan->halves;
+    d.x[1] = d.x[0] + mn;
+    d.a = d.x[1] + mn;
     d.q = d.a + mm;
     plan->halves = d.q + mm;
   }
@@ -263,17 +262,15 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   choose_product(plan->mats, gram, parts, &plan->gram, &each);
   choose_product(plan->mats, square, parts, &plan->square, nullptr);
   choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
-  plan->final_.cls = plan->apply.cls;
-  list_product(plan, gram, &plan->gram, each, false);
+  list_product(plan, gram, &plan->gram, each);
   plan->join.at = plan->tiles.size();
   for (int i = 0; i < plan->gram.tiles.count; ++i) {
     const MatTile t = plan->tiles[plan->gram.tiles.at + i];
     if (t.shares > 1 && t.share == 0) plan->tiles.push_back(t);
   }
   plan->join.count = (int)(plan->tiles.size() - plan->join.at);
-  list_product(plan, square, &plan->square, 0, false);
-  list_product(plan, apply, &plan->apply, 0, false);
-  list_product(plan, apply, &plan->final_, 0, true);
+  list_product(plan, square, &plan->square, 0);
+  list_product(plan, apply, &plan->apply, 0);
   if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
 
   size_t at = 0;
@@ -300,7 +297,7 @@ struct artopk_matrices {
   int32_t type = 0, parts = 1;
   int nchunks = 0;
   Span begin;
-  Product gram, square, apply, final_;
+  Product gram, square, apply;
   Span join;
   float* partial = nullptr;
   char* slab = nullptr;
@@ -396,7 +393,7 @@ void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], f
     if (k + 1 < steps)
       product<PARTS, kApply>(h, h->apply, k & 1, co[k], f);
     else
-      product<PARTS, kFinal>(h, h->final_, k & 1, co[k], f);
+      product<PARTS, kFinal>(h, h->apply, k & 1, co[k], f);
   }
 }
 
@@ -463,7 +460,6 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->join = plan.join;
   h->square = plan.square;
   h->apply = plan.apply;
-  h->final_ = plan.final_;
   void* p = nullptr;
   hipError_t e = hipMalloc(&p, plan.total);
   if (e != hipSuccess) {

@@ -12,10 +12,11 @@
 // keeps 11 bits; with two (hi + lo, and hi hi + hi lo + lo hi for a product) 22, which leaves the result as exact as
 // float32 products do.
 //
-// Layout.  All products have the form P Q^T with both operands' rows along the summed index: X X^T from X, A A^T from
-// the symmetric A, and Q X = Q (X^T)^T from a second copy of X, transposed, which is written beside the first (a
-// product writes 4 bytes for every 2 m operations on them).  Everything is padded with zeros to whole tiles, so that
-// the products have no edges; only the final product, which writes the caller's buffer, knows the true sizes.
+// Layout.  X X^T and A A^T (A is symmetric) have both operands' rows along the summed index, as the matrix cores take
+// them; in Q X the second operand's lie across it, and are turned on their way from LDS to registers.  (A second copy of
+// X, transposed, would spare that, and cost more: every step would write it, and with few rows a step is bound by what it
+// writes.)  Everything is padded with zeros to multiples of 64, so that the products' summed index has no edge; the
+// final product, which writes the caller's buffer, knows the true sizes.
 #pragma once
 
 #include "elements.h"
@@ -36,7 +37,7 @@ struct MatDesc {
   int32_t mp, np;       // padded
   int32_t tall;         // the flat vector holds n rows of m
   float scale;
-  int64_t x, xt[2], a, q;
+  int64_t x[2], a, q;   // X before and after a step, in turn
   int32_t part, parts;  // its sums of squares
 };
 
@@ -138,12 +139,13 @@ __global__ __launch_bounds__(256) void k_mat_momentum(T* __restrict__ w, float* 
   if (threadIdx.x == 0) sums[c.slot] = s;
 }
 
-// 1 / (norm + eps) of a matrix, in every thread of a block of 256.
+// 1 / (norm + eps) of a matrix, in every thread of a block of 256; NaN where the norm is.
 __device__ __forceinline__ float inverse_norm(const MatDesc& d, const double* sums, float eps, double* room) {
   double s = 0.0;
   for (int i = threadIdx.x; i < d.parts; i += 256) s += sums[d.part + i];
   s = block_sum(s, room);
-  return static_cast<float>(1.0 / (sqrt(s) + (double)eps));
+  const double v = 1.0 / (sqrt(s) + (double)eps);
+  return static_cast<float>(v > 3.4028234e38 ? 3.4028234e38 : v);  // (not infinite, so that zeros stay zeros)
 }
 
 template <int PARTS>
@@ -167,7 +169,7 @@ struct FromMomentum {
   }
 };
 
-// X_0 and its transpose, 64 x 64 elements a block, zeros beyond the true sizes.
+// X_0, 64 x 64 elements a block, zeros beyond the true sizes.
 template <int PARTS, class From>
 __global__ __launch_bounds__(256) void k_mat_begin(From from, const MatDesc* __restrict__ mats,
                                                    const MatTile* __restrict__ tiles, const double* __restrict__ sums,
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(256) void k_mat_begin(From from, const MatDesc* __r
   const int rows = d.tall ? d.n : d.m, cols = d.tall ? d.m : d.n;  // as they lie
   const int r0 = (d.tall ? t.j : t.i) * 64, c0 = (d.tall ? t.i : t.j) * 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 4
+#pragma unroll 8
   for (int r = wave; r < 64; r += 4) {
     float v = 0.0f;
     if (r0 + r < rows && c0 + lane < cols) v = from(d.at + (int64_t)(r0 + r) * cols + c0 + lane) * by * kOperandScale;
@@ -196,24 +198,17 @@ __global__ __launch_bounds__(256) void k_mat_begin(From from, const MatDesc* __r
 #pragma unroll
   for (int half = 0; half < 64; half += 32) {
     const int r = at + half;
-    _Float16 p[8][PARTS], q[8][PARTS];
+    half8 u[PARTS];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      split_half<PARTS>(tile[r][k + e], p[e]);
-      split_half<PARTS>(tile[k + e][r], q[e]);
+      _Float16 p[PARTS];
+      split_half<PARTS>(tile[r][k + e], p);
+#pragma unroll
+      for (int s = 0; s < PARTS; ++s) u[s][e] = p[s];
     }
 #pragma unroll
-    for (int s = 0; s < PARTS; ++s) {
-      half8 u, v;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        u[e] = p[e][s];
-        v[e] = q[e][s];
-      }
-      const int64_t plane = (int64_t)s * d.mp * d.np;
-      *reinterpret_cast<half8*>(mem + d.x + plane + (int64_t)(i0 + r) * d.np + j0 + k) = u;
-      *reinterpret_cast<half8*>(mem + d.xt[0] + plane + (int64_t)(j0 + r) * d.mp + i0 + k) = v;
-    }
+    for (int s = 0; s < PARTS; ++s)
+      *reinterpret_cast<half8*>(mem + d.x[0] + (int64_t)s * d.mp * d.np + (int64_t)(i0 + r) * d.np + j0 + k) = u[s];
   }
 }
 
@@ -299,6 +294,17 @@ __device__ __forceinline__ int stage_place(int r, int c) {
     return r * 32 + ((c ^ ((r >> 1) & 3)) << 3);
 }
 
+// A stage of an operand whose rows lie across the summed index is kDepth rows of TILE; sixteen columns of row r, 32 bytes,
+// lie at their place with this flipped, so that the rows that a wave reads together lie in different banks: r, r + 8, r + 16
+// and r + 24 for four r side by side.
+template <int TILE>
+__device__ __forceinline__ int turned_flip(int r) {
+  if constexpr (TILE == 64) return ((r >> 1) & 1) | (((r >> 3) & 1) << 1);
+  if constexpr (TILE == 128) return (r & 3) | (((r >> 3) & 1) << 2);
+  if constexpr (TILE == 192) return r & 3;  // (twelve sixteens a row)
+  return (r & 3) | (((r >> 3) & 3) << 2);
+}
+
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most N loads are outstanding, and LDS reads are through
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
@@ -308,39 +314,66 @@ __device__ __forceinline__ void block_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// acc += P Q^T for `steps` stages (two at least, an even number with two parts), P's and Q's rows `ld` apart.  Rows from
-// p_rows / q_rows on count as zeros, and so do stages behind the last: the loads' descriptors end there.
-template <class S>
-__device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int p_rows, const _Float16* q, int64_t q_plane,
-                                         int q_rows, int ld, int steps, _Float16* lds, f32x4 (&acc)[S::kFM][S::kFN]) {
+// acc += P Q^T for `steps` stages (an even number with two parts), P's and Q's rows `ld` and `q_ld` apart.  With `TURNED`
+// acc += P Q instead: Q's rows lie across the summed index.  P's rows from p_rows on count as zeros (and Q's from q_rows on; of
+// a turned Q, columns from `q_rows` on may count as anything that lies in memory behind them up to the matrix's end, or as
+// zeros), and so do stages behind the last: the loads' descriptors end there.
+template <class S, bool TURNED>
+__device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int p_rows, int ld, const _Float16* q,
+                                         int64_t q_plane, int q_rows, int q_ld, int steps, _Float16* lds,
+                                         f32x4 (&acc)[S::kFM][S::kFN]) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the loads to LDS are unknown to the host's compiler)
   constexpr int TILE = S::TILE, PARTS = S::PARTS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / S::kWN * S::kRowsM, wj = wave % S::kWN * S::kRowsN;
   const int lr = lane / S::kChunks;
   const int lc = S::kChunks == 8 ? (lane % 8) ^ (lr & 7) : (lane % 4) ^ ((lr >> 1) & 3);
-  const int voff = (lr * ld + lc * 8) * 2;
-  const int group_bytes = S::kLoadRows * ld * 2;
-  constexpr int G = TILE / S::kLoadRows;  // loads of one operand's part
+  constexpr int G = TILE / S::kLoadRows;    // loads of one operand's part
+  constexpr int EACH = S::kLoads / 2;       // a wave's loads of one operand
+  int p_off[EACH], q_off[EACH];             // bytes from the stage's first element
+#pragma unroll
+  for (int l = 0; l < EACH; ++l) {
+    const int g = (l * S::kWaves + wave) % G;
+    p_off[l] = ((g * S::kLoadRows + lr) * ld + lc * 8) * 2;
+    if constexpr (TURNED) {
+      const int at = g * 64 + lane, r = at / (TILE / 8);
+      q_off[l] = (r * q_ld + ((at % (TILE / 8)) ^ (turned_flip<TILE>(r) << 1)) * 8) * 2;
+    } else {
+      q_off[l] = ((g * S::kLoadRows + lr) * q_ld + lc * 8) * 2;
+    }
+  }
   auto fetch = [&](int k, int stage) {
     const int there = k < steps ? -1 : 0;
 #pragma unroll
-    for (int l = 0; l < S::kLoads; ++l) {
-      const int u = l * S::kWaves + wave;  // P's parts, then Q's
-      const bool is_q = u >= PARTS * G;
-      const int v = is_q ? u - PARTS * G : u;
-      const int s = PARTS == 1 ? 0 : v / G, g = PARTS == 1 ? v : v % G;
-      const _Float16* base = is_q ? q + s * q_plane : p + s * p_plane;
-      const int bytes = ((is_q ? q_rows : p_rows) * ld * 2) & there;
+    for (int l = 0; l < EACH; ++l) {
+      const int u = l * S::kWaves + wave, s = PARTS == 1 ? 0 : u / G;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(base), 0, bytes, 0x00027000),
-          (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + u * (S::kLoadRows * S::kDepth)), 16,
-          voff + (g * group_bytes + k * (S::kDepth * 2)), 0, 0, 0);
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(p + s * p_plane), 0, (p_rows * ld * 2) & there, 0x00027000),
+          (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + u * 512), 16, p_off[l] + k * (S::kDepth * 2), 0, 0, 0);
+    }
+#pragma unroll
+    for (int l = 0; l < EACH; ++l) {
+      const int u = l * S::kWaves + wave, s = PARTS == 1 ? 0 : u / G;
+      const _Float16* base = q + s * q_plane;
+      int bytes = q_rows * q_ld * 2, more = k * (S::kDepth * 2);
+      if constexpr (TURNED) {
+        base += (int64_t)k * S::kDepth * q_ld;
+        bytes = ((S::kDepth - 1) * q_ld + q_rows) * 2;  // from the stage's first row to the last one's end
+        more = 0;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(base), 0, bytes & there, 0x00027000),
+          (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + PARTS * S::kPlane + u * 512), 16, q_off[l] + more, 0,
+          0, 0);
     }
   };
   constexpr int KS = S::kDepth / 32;
   constexpr int SETS = S::kAhead ? 2 : 1;
   half8 fp[SETS][PARTS][S::kFM], fq[SETS][PARTS][S::kFN];
+  // (of a turned operand a lane names four columns of one row and is given four rows of one column: in each sixteen lanes,
+  // lane i names row i / 4 and columns 4 (i % 4) .. and is given rows 0 .. 3 of column i)
+  const int tr = (lane >> 4) * 8 + ((lane & 15) >> 2);
+  const int flip = turned_flip<TILE>(tr);  // the same for r + 4 and r + 32
   auto read = [&](int stage, int ks, int to) {
     const _Float16* here = lds + stage * S::kStage;
     const int c = ks * 4 + (lane >> 4);
@@ -350,9 +383,18 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
       for (int i = 0; i < S::kFM; ++i)
         fp[to][s][i] = *reinterpret_cast<const half8*>(here + s * S::kPlane + stage_place<S::kChunks>(wi + i * 16 + (lane & 15), c));
 #pragma unroll
-      for (int j = 0; j < S::kFN; ++j)
-        fq[to][s][j] =
-            *reinterpret_cast<const half8*>(here + (PARTS + s) * S::kPlane + stage_place<S::kChunks>(wj + j * 16 + (lane & 15), c));
+      for (int j = 0; j < S::kFN; ++j) {
+        const _Float16* at = here + (PARTS + s) * S::kPlane;
+        if constexpr (TURNED) {
+          typedef short short4v __attribute__((ext_vector_type(4)));
+          at += (ks * 32 + tr) * TILE + ((((wj >> 4) + j) ^ flip) << 4) + (lane & 3) * 4;
+          const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+          const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at + 4 * TILE));
+          fq[to][s][j] = __builtin_shufflevector(__builtin_bit_cast(half4, a), __builtin_bit_cast(half4, b), 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+          fq[to][s][j] = *reinterpret_cast<const half8*>(at + stage_place<S::kChunks>(wj + j * 16 + (lane & 15), c));
+        }
+      }
     }
   };
   auto mul = [&](int of) {
@@ -495,7 +537,7 @@ __device__ __forceinline__ void store_halves(Value&& value, _Float16* room, int 
 template <int FM, int FN>
 constexpr int store_room() {
   constexpr int CR = (FM > 4 ? FM / 2 : FM) * 16, CC = FN * 16;
-  constexpr int a = CR * (CC + 8), b = CC * (CR + 8), c = 2 * 32 * (CC + 4);  // c: 32 rows of floats
+  constexpr int a = CR * (CC + 8), b = CC * (CR + 8), c = 2 * 36 * (CC + 4);  // c: 32 rows of floats, or as many columns
   return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
@@ -511,41 +553,29 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
 
   const MatTile t = tiles[blockIdx.x];
   const MatDesc& d = mats[t.mat];
-  const bool swap = MODE == kFinal && d.tall;  // X^T wanted: its rows are X^T's, Q is symmetric
   const int64_t mm = (int64_t)d.mp * d.mp, mn = (int64_t)d.mp * d.np;
   const int i0 = t.i * TILE, j0 = t.j * TILE;
-  const int rows = swap ? d.np : d.mp, cols = MODE == kApply || MODE == kFinal ? (swap ? d.mp : d.np) : d.mp;
-  const _Float16 *p, *q;
-  int64_t p_plane, q_plane;
-  int ld, begin = 0, end;
-  if constexpr (MODE == kGram) {
-    p = q = mem + d.x;
-    p_plane = q_plane = mn;
-    ld = d.np;
-    // a share is whole pieces of 64
-    begin = (int)((int64_t)(ld / 64) * t.share / t.shares) * 64;
-    end = (int)((int64_t)(ld / 64) * (t.share + 1) / t.shares) * 64;
-  } else if constexpr (MODE == kSquare) {
-    p = q = mem + d.a;
-    p_plane = q_plane = mm;
-    ld = end = d.mp;
-  } else {
-    p = mem + (swap ? d.xt[from] : d.q);
-    q = mem + (swap ? d.q : d.xt[from]);
-    p_plane = swap ? mn : mm;
-    q_plane = swap ? mm : mn;
-    ld = end = d.mp;
-  }
+  constexpr bool kTurned = MODE == kApply || MODE == kFinal;
+  const int rows = d.mp, cols = kTurned ? d.np : d.mp;
+  const int p_rows = rows - i0 < TILE ? rows - i0 : TILE, q_rows = cols - j0 < TILE ? cols - j0 : TILE;
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = 0.0f;
-  const int p_rows = rows - i0 < TILE ? rows - i0 : TILE;
-  const int q_all = MODE == kApply || MODE == kFinal ? cols : rows;
-  const int q_rows = q_all - j0 < TILE ? q_all - j0 : TILE;
-  multiply<S>(p + (int64_t)i0 * ld + begin, p_plane, p_rows, q + (int64_t)j0 * ld + begin, q_plane, q_rows, ld,
-              (end - begin) / S::kDepth, lds, acc);
+  if constexpr (kTurned) {
+    multiply<S, true>(mem + d.q + (int64_t)i0 * d.mp, mm, p_rows, d.mp, mem + d.x[from] + j0, mn, q_rows, d.np,
+                      d.mp / S::kDepth, lds, acc);
+  } else {
+    const _Float16* p = mem + (MODE == kGram ? d.x[from] : d.a);
+    const int ld = MODE == kGram ? d.np : d.mp;
+    // a share is whole pieces of 64
+    const int begin = MODE == kGram ? (int)((int64_t)(ld / 64) * t.share / t.shares) * 64 : 0;
+    const int end = MODE == kGram ? (int)((int64_t)(ld / 64) * (t.share + 1) / t.shares) * 64 : ld;
+    const int64_t plane = MODE == kGram ? mn : mm;
+    multiply<S, false>(p + (int64_t)i0 * ld + begin, plane, p_rows, ld, p + (int64_t)j0 * ld + begin, plane, q_rows, ld,
+                       (end - begin) / S::kDepth, lds, acc);
+  }
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = i0 + wave / S::kWN * S::kRowsM, col0 = j0 + wave % S::kWN * S::kRowsN;
@@ -561,10 +591,12 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
     }
   }
   if constexpr (MODE == kFinal) {
-    const int out_rows = d.tall ? d.n : d.m, out_cols = d.tall ? d.m : d.n;
+    // Elements of a tall matrix lie column by column of X.  32 rows of the wave's part at a time go through LDS as floats,
+    // in the order in which they lie.
+    const int lines = d.tall ? d.n : d.m, length = d.tall ? d.m : d.n;
     const float by = d.scale * (1.0f / (kOperandScale * kOperandScale));
     const int size = f.type == kTypeF32 ? 4 : 2;
-    const bool wide = out_cols % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * size) % (4 * size) == 0;
+    const bool wide = length % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * size) % (4 * size) == 0;
     constexpr int CC = FN * 16;
     float* fl = reinterpret_cast<float*>(room);
 #pragma unroll
@@ -573,32 +605,36 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int j = 0; j < FN; ++j) {
+          const f32x4 v = acc[h + i][j] * by;
+          if (d.tall) {
+            *reinterpret_cast<f32x4*>(fl + (j * 16 + (lane & 15)) * 36 + i * 16 + (lane >> 4) * 4) = v;
+          } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            fl[(i * 16 + (lane >> 4) * 4 + e) * (CC + 4) + j * 16 + (lane & 15)] = acc[h + i][j][e] * by;
+            for (int e = 0; e < 4; ++e) fl[(i * 16 + (lane >> 4) * 4 + e) * (CC + 4) + j * 16 + (lane & 15)] = v[e];
+          }
+        }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
+      const int line0 = d.tall ? col0 : row0 + h * 16, place0 = d.tall ? row0 + h * 16 : col0;
+      const int run = d.tall ? 32 : CC, pitch = run + 4;
       if (wide) {
-#pragma unroll
-        for (int u = 0; u < 32 * CC / 4; u += 64) {
-          const int r = (u + lane) / (CC / 4), c = (u + lane) % (CC / 4) * 4;
-          const int row = row0 + h * 16 + r, col = col0 + c;
-          if (row < out_rows && col < out_cols) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fl[r * (CC + 4) + c + e];
-            finish<4>(f, d.at + (int64_t)row * out_cols + col, v);
+#pragma unroll 4
+        for (int u = lane; u < 32 * CC / 4; u += 64) {
+          const int r = u / (run / 4), c = u % (run / 4) * 4;
+          if (line0 + r < lines && place0 + c < length) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(fl + r * pitch + c);
+            const float v[4] = {x[0], x[1], x[2], x[3]};
+            finish<4>(f, d.at + (int64_t)(line0 + r) * length + place0 + c, v);
           }
         }
       } else {
 #pragma unroll 4
-        for (int u = 0; u < 32 * CC; u += 64) {
-          const int r = (u + lane) / CC, c = (u + lane) % CC;
-          const int row = row0 + h * 16 + r, col = col0 + c;
-          if (row < out_rows && col < out_cols) {
-            const float v[1] = {fl[r * (CC + 4) + c]};
-            finish<1>(f, d.at + (int64_t)row * out_cols + col, v);
+        for (int u = lane; u < 32 * CC; u += 64) {
+          const int r = u / run, c = u % run;
+          if (line0 + r < lines && place0 + c < length) {
+            const float v[1] = {fl[r * pitch + c]};
+            finish<1>(f, d.at + (int64_t)(line0 + r) * length + place0 + c, v);
           }
         }
       }
@@ -628,7 +664,7 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
     if constexpr (MODE == kGram)
       store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.a, d.mp, mem + d.a, d.mp, mm, t.i != t.j);
     else
-      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.x, d.np, mem + d.xt[from ^ 1], d.mp, mn, true);
+      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.x[from ^ 1], d.np, nullptr, 0, mn, false);
   }
 }
 
