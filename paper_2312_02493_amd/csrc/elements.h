@@ -6,6 +6,8 @@
 
 namespace artopk {
 
+enum { kTypeF32 = 0, kTypeBf16 = 1, kTypeF16 = 2 };  // as ARTOPK_G_F32 ..
+
 // Sixteen bytes of elements; whole ones are read and written at 16-byte aligned places only.
 template <class T>
 struct alignas(16) Vec16 {

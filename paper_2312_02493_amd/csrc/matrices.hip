@@ -129,8 +129,9 @@ void choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int 
 }
 
 // The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
-// each die has a cache of its own: every matrix's tiles are cut into eight runs of neighbours, one for each die, and the
-// matrices with the longest sums come first.
+// each die has a cache of its own: the tiles of all matrices with equally long sums are cut into eight runs of neighbours,
+// one for each die, and the longest sums come first.  (Every matrix cut into eight instead: Q X of sixteen 1280 x 1280
+// and eight 1280 x 5120 234 us, so KRUNS.)
 void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
   const int tile = kTileOf[p->cls];
   std::vector<int> order(plan->mats.size());
@@ -143,28 +144,32 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
   std::vector<MatTile> die[8];
   std::vector<MatTile> own;
   int first = 0;
-  for (int i : order) {
-    const MatDesc& d = plan->mats[i];
-    const int a = tiles_of(d.mp, tile), b = tiles_of(d.np, tile);
-    const int shares = product_shares(d, k, each);
+  for (size_t o = 0; o < order.size();) {
     own.clear();
-    constexpr int kBand = 4;  // rows of tiles taken together
-    for (int a0 = 0; a0 < a; a0 += kBand)
-      for (int y = 0; y < (k.symmetric ? std::min(a, a0 + kBand) : b); ++y)
-        for (int x = a0; x < std::min(a, a0 + kBand); ++x) {
-          if (k.symmetric && y > x) continue;
-          MatTile t = {};
-          t.mat = (uint32_t)i;
-          t.i = (uint16_t)x;
-          t.j = (uint16_t)y;
-          t.shares = (uint16_t)shares;
-          t.slot = (uint32_t)plan->slots;
-          if (shares > 1) plan->slots += shares;
-          for (int s = 0; s < shares; ++s) {
-            t.share = (uint16_t)s;
-            own.push_back(t);
+    const int here = units(order[o]);
+    for (; o < order.size() && units(order[o]) == here; ++o) {
+      const int i = order[o];
+      const MatDesc& d = plan->mats[i];
+      const int a = tiles_of(d.mp, tile), b = tiles_of(d.np, tile);
+      const int shares = product_shares(d, k, each);
+      constexpr int kBand = 4;  // rows of tiles taken together
+      for (int a0 = 0; a0 < a; a0 += kBand)
+        for (int y = 0; y < (k.symmetric ? std::min(a, a0 + kBand) : b); ++y)
+          for (int x = a0; x < std::min(a, a0 + kBand); ++x) {
+            if (k.symmetric && y > x) continue;
+            MatTile t = {};
+            t.mat = (uint32_t)i;
+            t.i = (uint16_t)x;
+            t.j = (uint16_t)y;
+            t.shares = (uint16_t)shares;
+            t.slot = (uint32_t)plan->slots;
+            if (shares > 1) plan->slots += shares;
+            for (int s = 0; s < shares; ++s) {
+              t.share = (uint16_t)s;
+              own.push_back(t);
+            }
           }
-        }
+    }
     const int64_t total = (int64_t)own.size(), per = total / 8, more = total % 8;
     int64_t at = 0;
     for (int x = 0; x < 8; ++x) {

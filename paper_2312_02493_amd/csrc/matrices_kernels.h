@@ -63,8 +63,6 @@ struct MuonArgs {
   float eta, decay_by, eta_rest;  // decay_by = 1 - eta decay
 };
 
-enum { kTypeF32 = 0, kTypeBf16 = 1, kTypeF16 = 2 };
-
 __device__ __forceinline__ float muon_direction(const MuonArgs& a, float momentum, float update) {
   return a.nesterov ? fmaf(a.mu, momentum, a.scale * update) : momentum;
 }

@@ -24,6 +24,8 @@ namespace {
 constexpr int64_t kRegisterCols = 16384;  // longest row that a block's registers hold
 constexpr int kMaxShares = 1024;          // blocks of a backward pass, at most
 constexpr int kLongShares = 64;
+// Up to this many rows, and elements, the weight gradients are summed column by column beside the rows' blocks.
+constexpr int64_t kColumnRows = 512, kColumnElems = 1 << 20;
 
 #define NORM_TRY(h, expr)                                                                                      \
   do {                                                                                                         \
@@ -91,16 +93,20 @@ bool wide_rows(const void* p, int64_t stride, int64_t rows, size_t size) {
   return aligned16(p) && (rows <= 1 || stride * (int64_t)size % 16 == 0);
 }
 
-// Calls f(V, threads of a row, elements of a thread) as compile-time constants: the fewest threads that hold the row, a
-// wave where it does.
+// Calls f(V, threads of a row, elements of a thread) as compile-time constants: a wave where it holds the row, then the fewest
+// threads that do; with fewer rows than compute units twice as many, of half the elements.
 template <int V, class F>
-void with_shape(int64_t cols, F&& f) {
-  if (cols <= 512) return f(std::integral_constant<int, V>(), std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
-  if (cols <= 1024) return f(std::integral_constant<int, V>(), std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
-  if (cols <= 2048) return f(std::integral_constant<int, V>(), std::integral_constant<int, 256>(), std::integral_constant<int, 8>());
-  if (cols <= 4096) return f(std::integral_constant<int, V>(), std::integral_constant<int, 256>(), std::integral_constant<int, 16>());
-  if (cols <= 8192) return f(std::integral_constant<int, V>(), std::integral_constant<int, 512>(), std::integral_constant<int, 16>());
-  return f(std::integral_constant<int, V>(), std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
+void with_shape(int64_t cols, bool few, F&& f) {
+  auto go = [&](auto tpr, auto e) { f(std::integral_constant<int, V>(), tpr, e); };
+  using std::integral_constant;
+  if (cols <= 512) return go(integral_constant<int, 64>(), integral_constant<int, 8>());
+  if (cols <= 1024 && !few) return go(integral_constant<int, 64>(), integral_constant<int, 16>());
+  if (cols <= 2048) return go(integral_constant<int, 256>(), integral_constant<int, 8>());
+  if (cols <= 4096 && !few) return go(integral_constant<int, 256>(), integral_constant<int, 16>());
+  if (cols <= 4096) return go(integral_constant<int, 512>(), integral_constant<int, 8>());
+  if (cols <= 8192 && !few) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
+  if (cols <= 8192) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
+  return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
 }
 
 template <class T>
@@ -114,21 +120,23 @@ void forward(artopk_norm* h, const T* x, int64_t x_stride, int64_t rows, int64_t
   auto go = [&](auto V, auto TPR, auto E) {
     using S = NormShape<TPR()>;
     const int64_t units = (rows + S::kRows - 1) / S::kRows;
-    const int blocks = (int)std::min<int64_t>(units, (int64_t)h->num_cu * (2048 / S::kThreads) * 4);
+    const int blocks = (int)std::min<int64_t>(units, (int64_t)h->num_cu * (2048 / S::kThreads));
     k_norm_forward<T, V(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(x, x_stride, rows, (int)cols, gamma, beta, eps,
                                                                               y, y_stride, mean, rstd);
   };
   constexpr int kWide = 16 / sizeof(T);
-  if (cols % kWide == 0 && wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(y, y_stride, rows, sizeof(T)))
-    with_shape<kWide>(cols, go);
+  const bool few = rows <= h->num_cu;
+  if (wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(y, y_stride, rows, sizeof(T)))
+    with_shape<kWide>(cols, few, go);
   else
-    with_shape<1>(cols, go);
+    with_shape<1>(cols, few, go);
 }
 
-// Returns the number of shares of the weight gradients.
+// Returns the number of shares of the weight gradients to be added up, 0 if they are done.
 template <class T>
 int backward(artopk_norm* h, const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int64_t cols,
-             const float* gamma, const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* part) {
+             const float* gamma, const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* part,
+             const GradOut& grads) {
   int shares = 0;
   if (cols > kRegisterCols) {
     if (dx) {
@@ -142,19 +150,24 @@ int backward(artopk_norm* h, const T* dy, int64_t dy_stride, const T* x, int64_t
           dy, dy_stride, x, x_stride, rows, cols, mean, rstd, part);
     return shares;
   }
+  const bool columns = part && rows <= kColumnRows && rows * cols <= kColumnElems;
   auto go = [&](auto V, auto TPR, auto E) {
     using S = NormShape<TPR()>;
     const int64_t units = (rows + S::kRows - 1) / S::kRows;
     shares = (int)std::min<int64_t>(units, std::min<int64_t>(kMaxShares, (int64_t)h->num_cu * (1024 / S::kThreads)));
-    k_norm_backward<T, V(), TPR(), E()><<<shares, S::kThreads, 0, h->stream>>>(dy, dy_stride, x, x_stride, rows, (int)cols, gamma,
-                                                                               mean, rstd, dx, dx_stride, part);
+    const int row_blocks = columns && !dx ? 0 : shares;
+    const int blocks = row_blocks + (columns ? (int)((cols + 63) / 64) : 0);
+    k_norm_backward<T, V(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(
+        dy, dy_stride, x, x_stride, rows, (int)cols, gamma, mean, rstd, dx, dx_stride, columns ? nullptr : part, row_blocks, grads);
   };
   constexpr int kWide = 16 / sizeof(T);
-  if (cols % kWide == 0 && wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(dy, dy_stride, rows, sizeof(T)) &&
+  const bool few = rows <= h->num_cu;
+  if (wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(dy, dy_stride, rows, sizeof(T)) &&
       (!dx || wide_rows(dx, dx_stride, rows, sizeof(T))))
-    with_shape<kWide>(cols, go);
+    with_shape<kWide>(cols, few, go);
   else
-    with_shape<1>(cols, go);
+    with_shape<1>(cols, few, go);
+  if (columns) shares = 0;
   return shares;
 }
 
@@ -270,28 +283,20 @@ int artopk_layernorm_backward(artopk_norm* norm, const void* dy, int64_t dy_stri
     if ((rc = rs.check(norm->err))) return rc;
   }
   float* part = dgamma || dbeta ? norm->part : nullptr;
+  const GradOut grads = {{dgamma, dbeta}, grad_type, accumulate != 0};
   int shares = 0;
   if (rows > 0) {
     auto go = [&](auto* tag) {
       using T = std::remove_pointer_t<decltype(tag)>;
       shares = backward<T>(norm, static_cast<const T*>(dy), dy_stride, static_cast<const T*>(x), x_stride, rows, cols, gamma, mean,
-                           rstd, static_cast<T*>(dx), dx_stride, part);
+                           rstd, static_cast<T*>(dx), dx_stride, part, grads);
     };
     if (type == ARTOPK_G_F32) go((float*)nullptr);
     else if (type == ARTOPK_G_BF16) go((__bf16*)nullptr);
     else go((_Float16*)nullptr);
   }
-  if (part) {
-    const dim3 grid((unsigned)((cols + 63) / 64), 2);
-    auto go = [&](auto* tag) {
-      using G = std::remove_pointer_t<decltype(tag)>;
-      k_norm_join<G><<<grid, 256, 0, norm->stream>>>(part, shares, cols, static_cast<G*>(dgamma), static_cast<G*>(dbeta),
-                                                     accumulate != 0);
-    };
-    if (grad_type == ARTOPK_G_F32) go((float*)nullptr);
-    else if (grad_type == ARTOPK_G_BF16) go((__bf16*)nullptr);
-    else go((_Float16*)nullptr);
-  }
+  if (part && (shares || rows == 0))
+    k_norm_join<<<dim3((unsigned)((cols + 63) / 64), 2), 1024, 0, norm->stream>>>(part, shares, cols, grads);
   NORM_TRY(norm, hipGetLastError());
   return ARTOPK_OK;
 }

@@ -25,6 +25,27 @@ struct NormShape {
   static constexpr int kWaves = TPR / 64;  // of one row
 };
 
+// The weights' gradients as the caller wants them: dgamma (0) and dbeta (1), either of which may be missing, of one of the
+// three element types; `add` adds to what is there, in float32.
+struct GradOut {
+  void* out[2];
+  int32_t type, add;
+  __device__ __forceinline__ bool wanted(int which) const { return out[which] != nullptr; }
+  template <class G>
+  __device__ __forceinline__ void put_as(G* p, float s) const {
+    *p = static_cast<G>(add ? s + static_cast<float>(*p) : s);
+  }
+  __device__ __forceinline__ void put(int which, int64_t c, float s) const {
+    if (!out[which]) return;
+    if (type == kTypeF32)
+      put_as(static_cast<float*>(out[which]) + c, s);
+    else if (type == kTypeBf16)
+      put_as(static_cast<__bf16*>(out[which]) + c, s);
+    else
+      put_as(static_cast<_Float16*>(out[which]) + c, s);
+  }
+};
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
@@ -56,6 +77,48 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* room, int turn) {
   }
 }
 
+// V elements of a row as they lie; the last ones of a row whose length is no multiple of V one by one, zeros behind them.
+template <class T, int V>
+struct alignas(V * sizeof(T)) Piece {
+  T e[V];
+  __device__ __forceinline__ void load(const T* row, int c, int cols, bool there) {
+    if (there && c + V <= cols) {
+      *this = *reinterpret_cast<const Piece*>(row + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = there && c + i < cols ? row[c + i] : static_cast<T>(0.0f);
+    }
+  }
+  __device__ __forceinline__ void store(T* row, int c, int cols) const {
+    if (c + V <= cols) {
+      *reinterpret_cast<Piece*>(row + c) = *this;
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c + i < cols) row[c + i] = e[i];
+    }
+  }
+};
+
+// V float32 weights from column c on, `other` where there are none.  They may lie anywhere in a flat vector.
+template <int V>
+__device__ __forceinline__ void load_weights(float (&out)[V], const float* w, int c, int cols, float other) {
+  if (w && V % 4 == 0 && (reinterpret_cast<uintptr_t>(w) & 15) == 0 && c + V <= cols) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(w + c + i);
+      out[i] = v.x;
+      out[i + 1 < V ? i + 1 : 0] = v.y;
+      out[i + 2 < V ? i + 2 : 0] = v.z;
+      out[i + 3 < V ? i + 3 : 0] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = w && c + i < cols ? w[c + i] : other;
+  }
+}
+
+// Rows blockIdx.x, blockIdx.x + gridDim.x, .. (times the rows a block has); the next row is on its way while one is summed.
 template <class T, int V, int TPR, int E>
 __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
     const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, const float* __restrict__ gamma,
@@ -65,70 +128,61 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
   __shared__ float room[2 * (TPR / 64) + 2];
   const int t = threadIdx.x % TPR;
   const float inv = 1.0f / static_cast<float>(cols);
+  const int64_t step = (int64_t)gridDim.x * NormShape<TPR>::kRows;
+  int64_t row = (int64_t)blockIdx.x * NormShape<TPR>::kRows + threadIdx.x / TPR;
+  Piece<T, V> next[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) next[r].load(x + row * x_stride, (r * TPR + t) * V, cols, row < rows);
   float gm[R][V], bt[R][V];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int c = (r * TPR + t) * V;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      gm[r][i] = gamma && c < cols ? gamma[c + i] : 1.0f;
-      bt[r][i] = beta && c < cols ? beta[c + i] : 0.0f;
-    }
+    load_weights<V>(gm[r], gamma, (r * TPR + t) * V, cols, 1.0f);
+    load_weights<V>(bt[r], beta, (r * TPR + t) * V, cols, 0.0f);
   }
-  for (int64_t row0 = (int64_t)blockIdx.x * NormShape<TPR>::kRows; row0 < rows;
-       row0 += (int64_t)gridDim.x * NormShape<TPR>::kRows) {
-    const int64_t row = row0 + threadIdx.x / TPR;
-    const bool there = row < rows;  // (whole waves; with several waves to a row always)
-    const T* xr = x + row * x_stride;
+  // (the rows of a block's waves end together or one turn apart: nobody waits for a wave that has left, since several
+  // waves to a row share it)
+  for (; row < rows; row += step) {
     float v[R][V];
     float s[1] = {0.0f};
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int c = (r * TPR + t) * V;
-      if (there && c < cols) {
-        load_elems<V>(v[r], xr + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[r][i] = 0.0f;
-      }
-    }
-#pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[0] += v[r][i];
+      for (int i = 0; i < V; ++i) {
+        v[r][i] = static_cast<float>(next[r].e[i]);
+        s[0] += v[r][i];
+      }
+    if (row + step < rows) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) next[r].load(x + (row + step) * x_stride, (r * TPR + t) * V, cols, true);
+    }
     row_sums<TPR>(s, room, 0);
     const float mean = s[0] * inv;
     float q[1] = {0.0f};
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if ((r * TPR + t) * V < cols) {
+      const int c = (r * TPR + t) * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          v[r][i] -= mean;
-          q[0] = fmaf(v[r][i], v[r][i], q[0]);
-        }
+      for (int i = 0; i < V; ++i) v[r][i] -= mean;
+      if (c + V > cols) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (c + i >= cols) v[r][i] = 0.0f;
       }
+#pragma unroll
+      for (int i = 0; i < V; ++i) q[0] = fmaf(v[r][i], v[r][i], q[0]);
     }
     row_sums<TPR>(q, room, 1);
     const float rstd = 1.0f / sqrtf(fmaf(q[0], inv, eps));
-    if (!there) continue;
     if (t == 0) {
       if (mean_out) mean_out[row] = mean;
       if (rstd_out) rstd_out[row] = rstd;
     }
-    T* yr = y + row * y_stride;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int c = (r * TPR + t) * V;
-      if (c < cols) {
-        float o[V];
+      Piece<T, V> o;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float h = v[r][i] * rstd;
-          o[i] = fmaf(h, gm[r][i], bt[r][i]);
-        }
-        store_elems<V>(yr + c, o);
-      }
+      for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(fmaf(v[r][i] * rstd, gm[r][i], bt[r][i]));
+      o.store(y + row * y_stride, (r * TPR + t) * V, cols);
     }
   }
 }
@@ -165,79 +219,113 @@ __global__ __launch_bounds__(1024) void k_norm_forward_long(
   }
 }
 
-// The backward pass over rows blockIdx.x, blockIdx.x + gridDim.x, ..; the block's share of the weight gradients goes
-// to part[0][blockIdx.x][..] (dgamma) and part[1][blockIdx.x][..] (dbeta), rows of `cols`.
+// The weights' gradients of 64 columns over all rows, by one block of NT threads: its waves take every NT / 64-th row.
+template <class T, int NT>
+__device__ void norm_columns(int64_t c0, const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols,
+                             const float* mean, const float* rstd, const GradOut& g, float* room) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = c0 + lane;
+  float a = 0.0f, b = 0.0f;
+  if (c < cols)
+#pragma unroll 8
+    for (int64_t row = wave; row < rows; row += NT / 64) {
+      const float d = static_cast<float>(dy[row * dy_stride + c]);
+      a = fmaf(d, (static_cast<float>(x[row * x_stride + c]) - mean[row]) * rstd[row], a);
+      b += d;
+    }
+  room[wave * 128 + lane] = a;
+  room[wave * 128 + 64 + lane] = b;
+  __syncthreads();
+  if (wave < 2 && c < cols) {  // wave 0 dgamma, wave 1 dbeta
+    float s = 0.0f;
+    for (int i = 0; i < NT / 64; ++i) s += room[i * 128 + wave * 64 + lane];
+    g.put(wave, c, s);
+  }
+}
+
+// The backward pass over rows blockIdx.x, blockIdx.x + row_blocks, ..; the block's share of the weight gradients goes to
+// part[0][blockIdx.x][..] (dgamma) and part[1][blockIdx.x][..] (dbeta), rows of `cols`.  Blocks from row_blocks on, if there
+// are such, take 64 columns each instead and write their weights' gradients whole: few rows are read a second time sooner
+// than a second launch adds up shares (then `part` is NULL).
 template <class T, int V, int TPR, int E>
 __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols,
     const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
-    T* __restrict__ dx, int64_t dx_stride, float* __restrict__ part) {
+    T* __restrict__ dx, int64_t dx_stride, float* __restrict__ part, int row_blocks, GradOut grads) {
   constexpr int R = E / V;
   constexpr int kRows = NormShape<TPR>::kRows;
-  constexpr int kRoom = kRows > 1 ? 2 * kRows * TPR * E : 4 * (TPR / 64);
+  constexpr int kRoomRows = kRows > 1 ? 2 * kRows * TPR * E : 4 * (TPR / 64);
+  constexpr int kRoomCols = NormShape<TPR>::kThreads / 64 * 128;
+  constexpr int kRoom = kRoomRows > kRoomCols ? kRoomRows : kRoomCols;
   __shared__ float room[kRoom];
+  if ((int)blockIdx.x >= row_blocks) {
+    norm_columns<T, NormShape<TPR>::kThreads>((int64_t)(blockIdx.x - row_blocks) * 64, dy, dy_stride, x, x_stride, rows, cols,
+                                              mean, rstd, grads, room);
+    return;
+  }
   const int t = threadIdx.x % TPR;
   const float inv = 1.0f / static_cast<float>(cols);
+  const int64_t step = (int64_t)row_blocks * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+  Piece<T, V> next_x[R], next_d[R];
+  float next_mu = 0.0f, next_rs = 0.0f;
+  auto ask = [&](int64_t of) {
+    const bool there = of < rows;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      next_x[r].load(x + of * x_stride, (r * TPR + t) * V, cols, there);
+      next_d[r].load(dy + of * dy_stride, (r * TPR + t) * V, cols, there);
+    }
+    next_mu = there ? mean[of] : 0.0f;
+    next_rs = there ? rstd[of] : 0.0f;
+  };
+  ask(row);
   float dg[R][V], db[R][V], gm[R][V];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int c = (r * TPR + t) * V;
+    load_weights<V>(gm[r], gamma, (r * TPR + t) * V, cols, 1.0f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      dg[r][i] = db[r][i] = 0.0f;
-      gm[r][i] = c < cols ? (gamma ? gamma[c + i] : 1.0f) : 0.0f;
-    }
+    for (int i = 0; i < V; ++i) dg[r][i] = db[r][i] = 0.0f;
   }
   int turn = 0;
-  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < rows; row0 += (int64_t)gridDim.x * kRows) {
-    const int64_t row = row0 + threadIdx.x / TPR;
-    const bool there = row < rows;
+  for (; row < rows; row += step) {
     float h[R][V], d[R][V];
-    const float mu = there ? mean[row] : 0.0f, rs = there ? rstd[row] : 0.0f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int c = (r * TPR + t) * V;
-      if (there && c < cols) {
-        load_elems<V>(h[r], x + row * x_stride + c);
-        load_elems<V>(d[r], dy + row * dy_stride + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) h[r][i] = d[r][i] = 0.0f;
-      }
-    }
+    const float mu = next_mu, rs = next_rs;
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (there && (r * TPR + t) * V < cols) {
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          h[r][i] = (h[r][i] - mu) * rs;
-          dg[r][i] = fmaf(d[r][i], h[r][i], dg[r][i]);
-          db[r][i] += d[r][i];
-          d[r][i] *= gm[r][i];
-          s[0] += d[r][i];
-          s[1] = fmaf(d[r][i], h[r][i], s[1]);
-        }
+      for (int i = 0; i < V; ++i) {  // (behind the row's end d is zero)
+        d[r][i] = static_cast<float>(next_d[r].e[i]);
+        h[r][i] = (static_cast<float>(next_x[r].e[i]) - mu) * rs;
       }
-    }
+    if (row + step < rows) ask(row + step);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if ((r * TPR + t) * V + i >= cols) h[r][i] = 0.0f;  // (mean and rstd need not be finite)
+        dg[r][i] = fmaf(d[r][i], h[r][i], dg[r][i]);
+        db[r][i] += d[r][i];
+        d[r][i] *= gm[r][i];
+        s[0] += d[r][i];
+        s[1] = fmaf(d[r][i], h[r][i], s[1]);
+      }
     if (!dx) continue;
     row_sums<TPR>(s, room, turn);
     turn ^= 1;
     const float m1 = s[0] * inv, m2 = s[1] * inv;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int c = (r * TPR + t) * V;
-      if (there && c < cols) {
-        float o[V];
+      Piece<T, V> o;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = rs * (d[r][i] - fmaf(h[r][i], m2, m1));
-        store_elems<V>(dx + row * dx_stride + c, o);
-      }
+      for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(rs * (d[r][i] - fmaf(h[r][i], m2, m1)));
+      o.store(dx + row * dx_stride, (r * TPR + t) * V, cols);
     }
   }
   if (!part) return;
   float* pg = part + (int64_t)blockIdx.x * cols;
-  float* pb = pg + (int64_t)gridDim.x * cols;
+  float* pb = pg + (int64_t)row_blocks * cols;
   if constexpr (kRows > 1) {
     const int mine = threadIdx.x / TPR;
 #pragma unroll
@@ -263,13 +351,12 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int c = (r * TPR + t) * V;
-      if (c < cols) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+      for (int i = 0; i < V; ++i)
+        if (c + i < cols) {
           pg[c + i] = dg[r][i];
           pb[c + i] = db[r][i];
         }
-      }
     }
   }
 }
@@ -323,27 +410,24 @@ __global__ __launch_bounds__(256) void k_norm_backward_cols(
   part[((int64_t)gridDim.y + blockIdx.y) * cols + c] = b;
 }
 
-// Sums the blocks' shares column by column, blockIdx.y = 0 dgamma, 1 dbeta; 64 columns a block, whose four waves take
-// a quarter of the shares each.  `add` adds to what out holds, in float32.
-template <class G>
-__global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ part, int shares, int64_t cols,
-                                                   G* __restrict__ dgamma, G* __restrict__ dbeta, int add) {
-  __shared__ float room[4][64];
-  G* out = blockIdx.y ? dbeta : dgamma;
-  if (!out) return;
+// Sums the blocks' shares column by column, blockIdx.y = 0 dgamma, 1 dbeta; 64 columns a block, each of whose sixteen
+// waves takes every sixteenth share.
+__global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ part, int shares, int64_t cols, GradOut grads) {
+  __shared__ float room[16][64];
+  if (!grads.wanted(blockIdx.y)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   const float* p = part + (int64_t)blockIdx.y * shares * cols;
   float s = 0.0f;
   if (c < cols)
-#pragma unroll 8
-    for (int j = wave; j < shares; j += 4) s += p[(int64_t)j * cols + c];
+#pragma unroll 16
+    for (int j = wave; j < shares; j += 16) s += p[(int64_t)j * cols + c];
   room[wave][lane] = s;
   __syncthreads();
   if (wave == 0 && c < cols) {
-    s = (room[0][lane] + room[1][lane]) + (room[2][lane] + room[3][lane]);
-    if (add) s += static_cast<float>(out[c]);
-    out[c] = static_cast<G>(s);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += room[i][lane];
+    grads.put(blockIdx.y, c, s);
   }
 }
 
