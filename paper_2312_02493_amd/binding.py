@@ -263,35 +263,45 @@ class Context:
                                               _ptr(sum_out), _ptr(update_out)))
 
 
+_types = {}  # torch's element types -> ARTOPK_G_*, filled when torch is there
+
+
+def _elem_types():
+    if not _types:
+        import torch
+
+        _types.update({torch.float32: ARTOPK_G_F32, torch.bfloat16: ARTOPK_G_BF16, torch.float16: ARTOPK_G_F16})
+    return _types
+
+
 def _elem_type(t) -> int:
     """ARTOPK_G_* of a tensor's elements."""
-    import torch
-
-    types = {torch.float32: ARTOPK_G_F32, torch.bfloat16: ARTOPK_G_BF16, torch.float16: ARTOPK_G_F16}
-    if t.dtype not in types:
+    kind = _elem_types().get(t.dtype)
+    if kind is None:
         raise ArTopkError(-1, f"elements of type {t.dtype} are not taken")
-    return types[t.dtype]
+    return kind
 
 
 def _rows(t, name: str):
     """(address, distance of rows, rows, cols) of a matrix whose columns lie side by side."""
-    if t.dim() != 2:
-        raise ArTopkError(-1, f"{name} has {t.dim()} dimensions, not 2")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2:
+        raise ArTopkError(-1, f"{name} has {len(shape)} dimensions, not 2")
+    rows, cols = shape
+    if stride[1] != 1 and cols > 1:
         raise ArTopkError(-1, f"{name}'s columns do not lie side by side")
-    return _ptr(t), (t.stride(0) if rows > 1 else cols), rows, cols
+    return t.data_ptr(), (stride[0] if rows > 1 else cols), rows, cols
 
 
-def _vector(t, name: str, length: int, dtype=None) -> Optional[int]:
-    """Address of a contiguous vector of `length` elements (of `dtype`), or None for None."""
+def _vector(t, name: str, length: int, kind: Optional[int] = None) -> Optional[int]:
+    """Address of a contiguous vector of `length` elements (of type `kind`), or None for None."""
     if t is None:
         return None
     if t.numel() != length or not t.is_contiguous():
         raise ArTopkError(-1, f"{name} is not a contiguous vector of {length} elements")
-    if dtype is not None and t.dtype != dtype:
-        raise ArTopkError(-1, f"{name} is {t.dtype}, not {dtype}")
-    return _ptr(t)
+    if kind is not None and _types.get(t.dtype) != kind:
+        raise ArTopkError(-1, f"{name} is {t.dtype}, which is not what is taken")
+    return t.data_ptr()
 
 
 def _coefficients(steps: int, coefficients):
@@ -353,37 +363,33 @@ class NormContext(_Handle):
         self._open(stream, int(max_rows), int(max_cols))
 
     def artopk_layernorm_forward(self, x, gamma, beta, y, mean_out=None, rstd_out=None, eps: float = 1e-5):
-        import torch
-
         px, sx, rows, cols = _rows(x, "x")
-        py, sy, *shape = _rows(y, "y")
-        if shape != [rows, cols] or y.dtype != x.dtype:
+        py, sy, rows_y, cols_y = _rows(y, "y")
+        if rows_y != rows or cols_y != cols or y.dtype != x.dtype:
             raise ArTopkError(-1, "y's shape or type is not x's")
         self._check(self._lib.artopk_layernorm_forward(
-            self._h, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, torch.float32),
-            _vector(beta, "beta", cols, torch.float32), C.c_float(eps), py, sy,
-            _vector(mean_out, "mean_out", rows, torch.float32), _vector(rstd_out, "rstd_out", rows, torch.float32)))
+            self._h, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, ARTOPK_G_F32),
+            _vector(beta, "beta", cols, ARTOPK_G_F32), eps, py, sy,
+            _vector(mean_out, "mean_out", rows, ARTOPK_G_F32), _vector(rstd_out, "rstd_out", rows, ARTOPK_G_F32)))
 
     def artopk_layernorm_backward(self, dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, accumulate: bool = False):
-        import torch
-
         px, sx, rows, cols = _rows(x, "x")
-        pd, sd, *shape = _rows(dy, "dy")
-        if shape != [rows, cols] or dy.dtype != x.dtype:
+        pd, sd, rows_d, cols_d = _rows(dy, "dy")
+        if rows_d != rows or cols_d != cols or dy.dtype != x.dtype:
             raise ArTopkError(-1, "dy's shape or type is not x's")
         po, so = None, cols
         if dx is not None:
-            po, so, *shape = _rows(dx, "dx")
-            if shape != [rows, cols] or dx.dtype != x.dtype:
+            po, so, rows_d, cols_d = _rows(dx, "dx")
+            if rows_d != rows or cols_d != cols or dx.dtype != x.dtype:
                 raise ArTopkError(-1, "dx's shape or type is not x's")
-        grads = [g for g in (dgamma, dbeta) if g is not None]
-        if len(grads) == 2 and grads[0].dtype != grads[1].dtype:
+        grad = dbeta if dgamma is None else dgamma
+        if dgamma is not None and dbeta is not None and dgamma.dtype != dbeta.dtype:
             raise ArTopkError(-1, "dgamma and dbeta are of different types")
         self._check(self._lib.artopk_layernorm_backward(
-            self._h, pd, sd, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, torch.float32),
-            _vector(mean, "mean", rows, torch.float32), _vector(rstd, "rstd", rows, torch.float32), po, so,
+            self._h, pd, sd, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, ARTOPK_G_F32),
+            _vector(mean, "mean", rows, ARTOPK_G_F32), _vector(rstd, "rstd", rows, ARTOPK_G_F32), po, so,
             _vector(dgamma, "dgamma", cols), _vector(dbeta, "dbeta", cols),
-            _elem_type(grads[0]) if grads else ARTOPK_G_F32, int(accumulate)))
+            ARTOPK_G_F32 if grad is None else _elem_type(grad), int(accumulate)))
 
 
 class _Matrix(C.Structure):
@@ -430,15 +436,13 @@ class MatrixContext(_Handle):
 
     def artopk_orthogonalize(self, x, out, steps: int = 5, coefficients=None, eps: float = 1e-7):
         self._check(self._lib.artopk_orthogonalize(self._h, self._flat(x, "x"), self._flat(out, "out"), int(steps),
-                                                   _coefficients(int(steps), coefficients), C.c_float(eps)))
+                                                   _coefficients(int(steps), coefficients), eps))
 
     def artopk_muon_step(self, weights, momentum, update, eta: float, mu: float = 0.95, nesterov: bool = True,
                          decay: float = 0.0, eta_rest: float = 0.0, update_scale: float = 1.0, steps: int = 5,
                          coefficients=None, eps: float = 1e-7):
-        import torch
-
         self._check(self._lib.artopk_muon_step(
-            self._h, self._flat(weights, "weights"), _vector(momentum, "momentum", self.n, torch.float32),
-            _vector(update, "update", self.n, torch.float32), C.c_float(update_scale), C.c_float(mu), int(nesterov),
-            C.c_float(eta), C.c_float(decay), C.c_float(eta_rest), int(steps), _coefficients(int(steps), coefficients),
-            C.c_float(eps)))
+            self._h, self._flat(weights, "weights"), _vector(momentum, "momentum", self.n, ARTOPK_G_F32),
+            _vector(update, "update", self.n, ARTOPK_G_F32), update_scale, mu, int(nesterov),
+            eta, decay, eta_rest, int(steps), _coefficients(int(steps), coefficients),
+            eps))

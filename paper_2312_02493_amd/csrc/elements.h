@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace artopk {
 
 enum { kTypeF32 = 0, kTypeBf16 = 1, kTypeF16 = 2 };  // as ARTOPK_G_F32 ..

@@ -45,6 +45,8 @@ struct MatPlan {
   Span join;  // the tiles of Gram matrices whose sums are cut
   int64_t halves = 0;  // of the iterates' memory
   int32_t sums = 0;
+  bool small = false;  // every matrix on one compute unit, in one launch
+  size_t small_lds = 0;
   int64_t slots = 0;   // partial sums of the Gram products' shares
   // places in the slab
   size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_partial = 0, o_mem = 0, total = 0;
@@ -114,7 +116,7 @@ double product_cost(const std::vector<MatDesc>& mats, const ProductKind& k, int 
 }
 
 // The tile and, for the Gram products, the length of a share that cost least.
-void choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, Product* p, int* each_out) {
+double choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, Product* p, int* each_out) {
   double best = 1e300;
   for (int cls = 0; cls < kTileClasses; ++cls)
     for (int each : {0, 64, 32, 16, 8}) {
@@ -126,6 +128,19 @@ void choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, int 
         if (each_out) *each_out = each;
       }
     }
+  return best;
+}
+
+// What a step of small matrices costs, in us, one block each.
+constexpr int64_t kSmallLds = 156 * 1024;
+double small_cost(const std::vector<MatDesc>& mats, int parts) {
+  double longest = 0.0;
+  for (const MatDesc& d : mats) {
+    const double m = small_pad(d.m) / 16, n = small_pad(d.n) / 16;
+    const double mults = (m * (m + 1) / 2 * (n + m) + m * n * m) / 2 * (parts == 2 ? 3 : 1);
+    longest = std::max(longest, 2.0 + mults * 0.006);
+  }
+  return longest * std::ceil(mats.size() / 256.0);
 }
 
 // The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
@@ -158,7 +173,7 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
           for (int x = a0; x < std::min(a, a0 + kBand); ++x) {
             if (k.symmetric && y > x) continue;
             MatTile t = {};
-            t.mat = (uint32_t)i;
+            t.d = d;
             t.i = (uint16_t)x;
             t.j = (uint16_t)y;
             t.shares = (uint16_t)shares;
@@ -260,13 +275,28 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   for (int i = 0; i < count; ++i)
     for (int a = 0; a < plan->mats[i].mp / 64; ++a)
       for (int b = 0; b < plan->mats[i].np / 64; ++b)
-        plan->tiles.push_back(MatTile{(uint32_t)i, (uint16_t)a, (uint16_t)b, 0, 1, 0});
+        plan->tiles.push_back(MatTile{plan->mats[i], (uint16_t)a, (uint16_t)b, 0, 1, 0});
   plan->begin.count = (int)plan->tiles.size();
+  plan->small = true;
+  for (const MatDesc& d : plan->mats) {
+    const int64_t bytes = 2 * small_halves(d.m, d.n, parts);
+    plan->small &= bytes <= kSmallLds && (int64_t)small_pad(d.m) * small_pad(d.n) <= kSmallElems;
+    plan->small_lds = std::max(plan->small_lds, (size_t)bytes);
+  }
   const ProductKind gram = {true, true}, square = {true, false}, apply = {false, false};
   int each = 0;
-  choose_product(plan->mats, gram, parts, &plan->gram, &each);
-  choose_product(plan->mats, square, parts, &plan->square, nullptr);
-  choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
+  double cost = choose_product(plan->mats, gram, parts, &plan->gram, &each);
+  cost += choose_product(plan->mats, square, parts, &plan->square, nullptr);
+  cost += choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
+  if (plan->small) plan->small = small_cost(plan->mats, parts) < cost;
+  if (plan->small) {
+    plan->tiles.clear();
+    plan->begin.count = 0;
+    plan->halves = 0;
+  } else {
+    plan->small_lds = 0;
+  }
+  if (!plan->small) {
   list_product(plan, gram, &plan->gram, each);
   plan->join.at = plan->tiles.size();
   for (int i = 0; i < plan->gram.tiles.count; ++i) {
@@ -276,6 +306,7 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   plan->join.count = (int)(plan->tiles.size() - plan->join.at);
   list_product(plan, square, &plan->square, 0);
   list_product(plan, apply, &plan->apply, 0);
+  }
   if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
 
   size_t at = 0;
@@ -304,6 +335,8 @@ struct artopk_matrices {
   Span begin;
   Product gram, square, apply;
   Span join;
+  int count = 0;
+  size_t small_lds = 0;  // 0: not small
   float* partial = nullptr;
   char* slab = nullptr;
   const MatDesc* mats = nullptr;
@@ -365,7 +398,7 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 template <int TILE, int PARTS, int MODE>
 void product(artopk_matrices* h, const Span& s, int from, const float* co, const FinishArgs& f) {
   k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
-      h->mats, h->tiles + s.at, h->mem, from, co[0], co[1], co[2], f, h->partial);
+      h->tiles + s.at, h->mem, from, co[0], co[1], co[2], f, h->partial);
 }
 
 template <int PARTS, int MODE>
@@ -381,16 +414,24 @@ void product(artopk_matrices* h, const Product& p, int from, const float* co, co
 template <int TILE, int PARTS>
 void join_shares(artopk_matrices* h) {
   k_mat_join<TILE, PARTS><<<dim3(h->join.count, 4), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
-      h->mats, h->tiles + h->join.at, h->mem, h->partial);
+      h->tiles + h->join.at, h->mem, h->partial);
 }
 
+// What the squares' or the momentum's launch leaves to do.
 template <int PARTS, class From>
 void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], float eps, const FinishArgs& f) {
   if (steps == 0) {
     k_mat_scaled<From><<<h->nchunks, 256, 0, h->stream>>>(from, h->mats, h->chunks, h->sums, eps, f);
     return;
   }
-  k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->mats, h->tiles + h->begin.at, h->sums, eps, h->mem);
+  if (h->small_lds) {
+    PolarSteps st = {};
+    st.steps = steps;
+    memcpy(st.co, co, sizeof(float) * 3 * steps);
+    k_mat_small<PARTS, From><<<h->count, kSmallThreads, h->small_lds, h->stream>>>(from, h->mats, st, eps, f);
+    return;
+  }
+  k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->tiles + h->begin.at, h->sums, eps, h->mem);
   for (int k = 0; k < steps; ++k) {
     product<PARTS, kGram>(h, h->gram, k & 1, co[k], f);
     if (h->join.count) h->gram.cls == 0 ? join_shares<64, PARTS>(h) : join_shares<128, PARTS>(h);
@@ -431,6 +472,20 @@ int check_eps(artopk_matrices* h, float eps) {
   return ARTOPK_OK;
 }
 
+// Lets the kernels of small matrices have the handle's LDS.
+template <int PARTS>
+hipError_t allow_small(const artopk_matrices* h) {
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mat_small<PARTS, FromMomentum>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)kSmallLds);
+  with_type(h->type, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    if (e == hipSuccess)
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mat_small<PARTS, FromVector<T>>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)kSmallLds);
+  });
+  return e;
+}
+
 }  // namespace
 
 int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products) {
@@ -463,6 +518,8 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->begin = plan.begin;
   h->gram = plan.gram;
   h->join = plan.join;
+  h->count = (int)plan.mats.size();
+  h->small_lds = plan.small ? plan.small_lds : 0;
   h->square = plan.square;
   h->apply = plan.apply;
   void* p = nullptr;
@@ -484,6 +541,7 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
     e = hipMemcpy(h->slab + plan.o_chunks, plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk), hipMemcpyHostToDevice);
   if (e == hipSuccess)
     e = hipMemcpy(h->slab + plan.o_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MatTile), hipMemcpyHostToDevice);
+  if (e == hipSuccess && h->small_lds) e = h->parts == 2 ? allow_small<2>(h) : allow_small<1>(h);
   if (e != hipSuccess) {
     (void)hipFree(h->slab);
     delete h;
@@ -520,7 +578,7 @@ int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t s
   f.type = m->type;
   with_type(m->type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    k_mat_squares<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), m->chunks, m->sums);
+    if (!m->small_lds || steps == 0) k_mat_squares<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), m->chunks, m->sums);
     polar(m, FromVector<T>{static_cast<const T*>(x)}, steps, co, eps, f);
   });
   MAT_TRY(m, hipGetLastError());

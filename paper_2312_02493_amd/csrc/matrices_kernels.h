@@ -48,9 +48,10 @@ struct MatChunk {
 };
 
 // One block's tile of a product, or its share of the summed index where a tile's sum is cut (shares > 1): the shares
-// meet at `slot` of the memory for partial sums.
+// meet at `slot` of the memory for partial sums.  The matrix is described in every tile: a short product's time is that
+// of what it waits for one after the other, and so this is one load.
 struct MatTile {
-  uint32_t mat;
+  MatDesc d;
   uint16_t i, j;  // in tiles
   uint16_t share, shares;
   uint32_t slot;
@@ -137,13 +138,17 @@ __global__ __launch_bounds__(256) void k_mat_momentum(T* __restrict__ w, float* 
   if (threadIdx.x == 0) sums[c.slot] = s;
 }
 
-// 1 / (norm + eps) of a matrix, in every thread of a block of 256; NaN where the norm is.
+// 1 / (norm + eps) from a matrix's sum of squares; NaN where that is.
+__device__ __forceinline__ float inverse_of_norm(double squares, float eps) {
+  const double v = 1.0 / (sqrt(squares) + (double)eps);
+  return static_cast<float>(v > 3.4028234e38 ? 3.4028234e38 : v);  // (not infinite, so that zeros stay zeros)
+}
+
+// The same from the sums of the matrix's pieces, in every thread of a block of 256.
 __device__ __forceinline__ float inverse_norm(const MatDesc& d, const double* sums, float eps, double* room) {
   double s = 0.0;
   for (int i = threadIdx.x; i < d.parts; i += 256) s += sums[d.part + i];
-  s = block_sum(s, room);
-  const double v = 1.0 / (sqrt(s) + (double)eps);
-  return static_cast<float>(v > 3.4028234e38 ? 3.4028234e38 : v);  // (not infinite, so that zeros stay zeros)
+  return inverse_of_norm(block_sum(s, room), eps);
 }
 
 template <int PARTS>
@@ -169,13 +174,12 @@ struct FromMomentum {
 
 // X_0, 64 x 64 elements a block, zeros beyond the true sizes.
 template <int PARTS, class From>
-__global__ __launch_bounds__(256) void k_mat_begin(From from, const MatDesc* __restrict__ mats,
-                                                   const MatTile* __restrict__ tiles, const double* __restrict__ sums,
+__global__ __launch_bounds__(256) void k_mat_begin(From from, const MatTile* __restrict__ tiles, const double* __restrict__ sums,
                                                    float eps, _Float16* __restrict__ mem) {
   __shared__ float tile[64][65];
   __shared__ double room[4];
-  const MatTile t = tiles[blockIdx.x];
-  const MatDesc d = mats[t.mat];
+  const MatTile& t = tiles[blockIdx.x];
+  const MatDesc& d = t.d;
   const float by = inverse_norm(d, sums, eps, room);
   const int rows = d.tall ? d.n : d.m, cols = d.tall ? d.m : d.n;  // as they lie
   const int r0 = (d.tall ? t.j : t.i) * 64, c0 = (d.tall ? t.i : t.j) * 64;
@@ -541,7 +545,7 @@ constexpr int store_room() {
 
 template <int TILE, int PARTS, int MODE>
 __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShape<TILE, PARTS>::kBlocks)) void k_mat_product(
-    const MatDesc* __restrict__ mats, const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, int from, float ca,
+    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, int from, float ca,
     float cb, float cc, FinishArgs f, float* __restrict__ partial) {
   using S = ProductShape<TILE, PARTS>;
   constexpr int FM = S::kFM, FN = S::kFN;
@@ -549,8 +553,8 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
   constexpr int kNeed = kRoom * S::kWaves > S::kHalves ? kRoom * S::kWaves : S::kHalves;
   __shared__ __align__(16) _Float16 lds[kNeed];
 
-  const MatTile t = tiles[blockIdx.x];
-  const MatDesc& d = mats[t.mat];
+  const MatTile& t = tiles[blockIdx.x];
+  const MatDesc& d = t.d;
   const int64_t mm = (int64_t)d.mp * d.mp, mn = (int64_t)d.mp * d.np;
   const int i0 = t.i * TILE, j0 = t.j * TILE;
   constexpr bool kTurned = MODE == kApply || MODE == kFinal;
@@ -666,20 +670,200 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
   }
 }
 
+// Whole steps of small matrices, one block each, with everything on chip: X, A and Q lie in LDS as halves (rows padded by
+// eight), sums in registers.  A step's products of a matrix that one compute unit holds take some microseconds there, less
+// than the launches and the trips through memory that they would otherwise be.
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+constexpr int kSmallElems = kSmallWaves * 32 * 32;           // of X, padded, at most: a block of 32 x 32 for each wave
+constexpr int kSmallHeld = kSmallElems / kSmallThreads;      // that a thread brings
+struct PolarSteps {
+  int32_t steps;
+  float co[32][3];
+};
+__host__ __device__ constexpr int small_pad(int v) { return (v + 31) / 32 * 32; }
+__host__ __device__ constexpr int64_t small_halves(int m, int n, int parts) {
+  return (int64_t)parts * small_pad(m) * ((small_pad(n) + 8) + 2 * (small_pad(m) + 8));
+}
+
+template <int PARTS, class From>
+__global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const MatDesc* __restrict__ mats, PolarSteps st,
+                                                             float eps, FinishArgs f) {
+  extern __shared__ __align__(16) _Float16 small_lds[];
+  __shared__ double room[kSmallWaves];
+  const MatDesc d = mats[blockIdx.x];
+  const int mp = small_pad(d.m), np = small_pad(d.n), xp = np + 8;
+  _Float16* X = small_lds;
+  const int size = d.m * d.n, cols = d.tall ? d.m : d.n;
+  float held[kSmallHeld];
+#pragma unroll
+  for (int u = 0; u < kSmallHeld; ++u) {
+    const int i = threadIdx.x + u * kSmallThreads;
+    held[u] = i < size ? from(d.at + i) : 0.0f;
+  }
+  const half8 zeros = {};
+  for (int i = threadIdx.x * 8; i < PARTS * mp * xp; i += kSmallThreads * 8) *reinterpret_cast<half8*>(X + i) = zeros;
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < kSmallHeld; ++u) sum = fma((double)held[u], (double)held[u], sum);
+  const float by = inverse_of_norm(block_sum(sum, room), eps);
+#pragma unroll
+  for (int u = 0; u < kSmallHeld; ++u) {
+    const int i = threadIdx.x + u * kSmallThreads;
+    if (i < size) {
+      const int r = i / cols, c = i - r * cols;
+      _Float16 h[PARTS];
+      split_half<PARTS>(held[u] * by * kOperandScale, h);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) X[(p * mp + (d.tall ? c : r)) * xp + (d.tall ? r : c)] = h[p];
+    }
+  }
+  __syncthreads();
+
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ap = mp + 8;
+  _Float16* A = X + PARTS * mp * xp;
+  _Float16* Q = A + PARTS * mp * ap;
+  int l15 = lane & 15, l4 = lane >> 4;
+  const int am = mp / 32, an = np / 32;
+  // A wave takes a block of 32 x 32, whose four tiles share what is read: the sums of block (i, j) of P B^T, times 2^-12;
+  // with `turned` of P^T B^T.  P's rows are p_pitch apart.  A lane is given four rows of a column, that is, of the transposed
+  // block four columns side by side: so A and Q, which are symmetric, are stored as their transposes, whole (a wave with the
+  // mirrored block costs nothing where there are waves enough), and X' = Q X is worked out as X^T Q.
+  auto block = [&](const _Float16* P, int p_pitch, int i, const _Float16* B, int b_pitch, int j, int depth, auto turned,
+                   f32x4 (&out)[2][2]) {
+    f32x4 acc[2][2], low[2][2], low2[2][2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) acc[x >> 1][x & 1] = low[x >> 1][x & 1] = low2[x >> 1][x & 1] = 0.0f;
+    const int p_plane = mp * p_pitch, b_plane = mp * b_pitch;
+    // (turned as in multiply())
+    const _Float16* a = turned() ? P + (l4 * 8 + (l15 >> 2)) * p_pitch + i * 32 + (l15 & 3) * 4 : P + (i * 32 + l15) * p_pitch + l4 * 8;
+    const _Float16* b = B + (j * 32 + l15) * b_pitch + l4 * 8;
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    auto four = [&](const _Float16* at) {
+      return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at));
+    };
+#pragma clang loop unroll(disable)
+    for (int k = 0; k < depth; k += 32) {
+      half8 fa[PARTS][2], fb[PARTS][2];
+#pragma unroll
+      for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if constexpr (turned()) {
+            const _Float16* at = a + s * p_plane + k * p_pitch + x * 16;
+            fa[s][x] = __builtin_shufflevector(four(at), four(at + 4 * p_pitch), 0, 1, 2, 3, 4, 5, 6, 7);
+          } else {
+            fa[s][x] = *reinterpret_cast<const half8*>(a + s * p_plane + x * 16 * p_pitch + k);
+          }
+          fb[s][x] = *reinterpret_cast<const half8*>(b + s * b_plane + x * 16 * b_pitch + k);
+        }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int u = x >> 1, v = x & 1;
+        if constexpr (PARTS == 2) {
+          low[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[PARTS - 1][u], fb[0][v], low[u][v], 0, 0, 0);
+          low2[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0][u], fb[PARTS - 1][v], low2[u][v], 0, 0, 0);
+        }
+        acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0][u], fb[0][v], acc[u][v], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      out[x >> 1][x & 1] = (acc[x >> 1][x & 1] + (low[x >> 1][x & 1] + low2[x >> 1][x & 1])) * (1.0f / kOperandScale);
+  };
+  // the transpose of block (i, j) at block (j, i)
+  auto put = [&](_Float16* M, int pitch, int i, int j, const f32x4 (&v)[2][2]) {
+    _Float16* at = M + (j * 32 + l15) * pitch + i * 32 + l4 * 4;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      half4 t[PARTS];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        _Float16 h[PARTS];
+        split_half<PARTS>(v[x >> 1][x & 1][e], h);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) t[p][e] = h[p];
+      }
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p)
+        *reinterpret_cast<half4*>(at + (p * mp + (x & 1) * 16) * pitch + (x >> 1) * 16) = t[p];
+    }
+  };
+  const bool has_a = wave < am * am, has_x = wave < am * an;
+  const int ai = wave / am, aj = wave - ai * am;  // of A and Q
+  const int xj = wave / am, xi = wave - xj * am;  // of X
+  constexpr std::integral_constant<bool, true> kTurned;
+  constexpr std::integral_constant<bool, false> kStraight;
+  f32x4 v[2][2];
+  for (int step = 0; step < st.steps; ++step) {
+    asm volatile("" : "+v"(l15), "+v"(l4));  // (places worked out once for all steps would fill the registers)
+    const float ca = st.co[step][0], cb = st.co[step][1], cc = st.co[step][2];
+    if (has_a) {
+      block(X, xp, ai, X, xp, aj, np, kStraight, v);
+      put(A, ap, ai, aj, v);
+    }
+    __syncthreads();
+    if (has_a) {
+      block(A, ap, ai, A, ap, aj, mp, kStraight, v);
+      const _Float16* at = A + (aj * 32 + l15) * ap + ai * 32 + l4 * 4;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const half4 hi = *reinterpret_cast<const half4*>(at + (x & 1) * 16 * ap + (x >> 1) * 16);
+        half4 lo = {};
+        if constexpr (PARTS == 2) lo = *reinterpret_cast<const half4*>(at + (mp + (x & 1) * 16) * ap + (x >> 1) * 16);
+        const int row = ai * 32 + (x >> 1) * 16 + l4 * 4, col = aj * 32 + (x & 1) * 16 + l15;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float w = fmaf(cb, static_cast<float>(hi[e]) + static_cast<float>(lo[e]), v[x >> 1][x & 1][e] * cc);
+          if (row + e == col) w += ca * kOperandScale;
+          v[x >> 1][x & 1][e] = w;
+        }
+      }
+      put(Q, ap, ai, aj, v);
+    }
+    __syncthreads();
+    if (has_x) block(X, xp, xj, Q, ap, xi, mp, kTurned, v);
+    if (step + 1 == st.steps) break;
+    __syncthreads();
+    if (has_x) put(X, xp, xj, xi, v);
+    __syncthreads();
+  }
+  if (!has_x) return;
+  const bool wide = !d.tall && d.n % 4 == 0 && f.type == kTypeF32 && (reinterpret_cast<uintptr_t>(f.out) + d.at * 4) % 16 == 0;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int row = xi * 32 + (x & 1) * 16 + l15, col = xj * 32 + (x >> 1) * 16 + l4 * 4;
+    const float by = d.scale / kOperandScale;
+    const float w[4] = {v[x >> 1][x & 1][0] * by, v[x >> 1][x & 1][1] * by, v[x >> 1][x & 1][2] * by, v[x >> 1][x & 1][3] * by};
+    if (row >= d.m || col >= d.n) continue;
+    if (wide) {
+      finish_as<4>(static_cast<float*>(f.out) + d.at + (int64_t)row * d.n + col, f, w);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float one[1] = {w[e]};
+        if (col + e < d.n) finish<1>(f, d.at + (d.tall ? (int64_t)(col + e) * d.m + row : (int64_t)row * d.n + col + e), one);
+      }
+    }
+  }
+#endif
+}
+
 // Adds the shares of a Gram matrix's tiles in their order and stores the tile, a quarter of each wave's fragments a block.
 // (The blocks of the product cannot do it themselves, the last one of a tile: that takes a write-back of a die's whole cache
 // by every block before it says that it is through.  480 blocks of 128 x 128 sums took 150 us so, 20 in two launches.)
 template <int TILE, int PARTS>
 __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads)) void k_mat_join(
-    const MatDesc* __restrict__ mats, const MatTile* __restrict__ tiles, _Float16* __restrict__ mem,
+    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem,
     const float* __restrict__ partial) {
   using S = ProductShape<TILE, PARTS>;
   constexpr int FM = S::kFM, FN = S::kFN;
   constexpr int QM = FM / 2, QN = FN / 2;
   constexpr int kRoom = store_room<QM, QN>();
   __shared__ __align__(16) _Float16 lds[kRoom * S::kWaves];
-  const MatTile t = tiles[blockIdx.x];
-  const MatDesc& d = mats[t.mat];
+  const MatTile& t = tiles[blockIdx.x];
+  const MatDesc& d = t.d;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = (blockIdx.y >> 1) * QM, qj = (blockIdx.y & 1) * QN;
   const int row0 = t.i * TILE + wave / S::kWN * S::kRowsM + qi * 16;

@@ -279,7 +279,9 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     next_mu = there ? mean[of] : 0.0f;
     next_rs = there ? rstd[of] : 0.0f;
   };
-  ask(row);
+  // (with wide loads the second row's registers cost more waves than it gains: 32768 x 2048 bf16 95 us so, KWAIT without)
+  constexpr bool kAhead = V == 1;
+  if (kAhead) ask(row);
   float dg[R][V], db[R][V], gm[R][V];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -289,6 +291,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
   }
   int turn = 0;
   for (; row < rows; row += step) {
+    if (!kAhead) ask(row);
     float h[R][V], d[R][V];
     const float mu = next_mu, rs = next_rs;
     float s[2] = {0.0f, 0.0f};
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
         d[r][i] = static_cast<float>(next_d[r].e[i]);
         h[r][i] = (static_cast<float>(next_x[r].e[i]) - mu) * rs;
       }
-    if (row + step < rows) ask(row + step);
+    if (kAhead && row + step < rows) ask(row + step);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
