@@ -131,16 +131,19 @@ double choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, in
   return best;
 }
 
-// What a step of small matrices costs, in us, one block each.
+// What a step of small matrices costs, in us, by the 32 x 32 x 32 products of the largest (measured, five steps and some 6 us
+// besides, HALF / SPLIT: 64 x 64 15.6 / 20, 64 x 128 19.4 / 25, 96 x 160 32 / 43, 128 x 128 38 / too large; the same in
+// launches of their own 46 / 56, 51 / 63, 62 / 82, 60 / 76; 600 of 64 x 64 34 / 62 and 102 / 153).
 constexpr int64_t kSmallLds = 156 * 1024;
-double small_cost(const std::vector<MatDesc>& mats, int parts) {
+double small_cost(const std::vector<MatDesc>& mats, int parts, size_t lds) {
   double longest = 0.0;
   for (const MatDesc& d : mats) {
-    const double m = small_pad(d.m) / 16, n = small_pad(d.n) / 16;
-    const double mults = (m * (m + 1) / 2 * (n + m) + m * n * m) / 2 * (parts == 2 ? 3 : 1);
-    longest = std::max(longest, 2.0 + mults * 0.006);
+    const double m = small_pad(d.m) / 32, n = small_pad(d.n) / 32;
+    const double blocks = m * m * (n + m) + m * n * m;
+    longest = std::max(longest, parts == 2 ? 1.8 + 0.048 * blocks : 1.2 + 0.032 * blocks);
   }
-  return longest * std::ceil(mats.size() / 256.0);
+  const int64_t together = 256 * std::max<int64_t>(1, std::min<int64_t>(2, 160 * 1024 / (int64_t)lds));
+  return longest * std::ceil((double)mats.size() / (double)together);
 }
 
 // The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
@@ -288,7 +291,7 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   double cost = choose_product(plan->mats, gram, parts, &plan->gram, &each);
   cost += choose_product(plan->mats, square, parts, &plan->square, nullptr);
   cost += choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
-  if (plan->small) plan->small = small_cost(plan->mats, parts) < cost;
+  if (plan->small) plan->small = small_cost(plan->mats, parts, plan->small_lds) < cost;
   if (plan->small) {
     plan->tiles.clear();
     plan->begin.count = 0;
