@@ -93,11 +93,11 @@ bool wide_rows(const void* p, int64_t stride, int64_t rows, size_t size) {
   return aligned16(p) && (rows <= 1 || stride * (int64_t)size % 16 == 0);
 }
 
-// Calls f(V, threads of a row, elements of a thread) as compile-time constants: a wave where it holds the row, then the fewest
+// Calls f(V, whether rows end inside V elements, threads of a row, elements of a thread) as compile-time constants: a wave where it holds the row, then the fewest
 // threads that do; with fewer rows than compute units twice as many, of half the elements.
-template <int V, class F>
+template <int V, bool TAIL, class F>
 void with_shape(int64_t cols, bool few, F&& f) {
-  auto go = [&](auto tpr, auto e) { f(std::integral_constant<int, V>(), tpr, e); };
+  auto go = [&](auto tpr, auto e) { f(std::integral_constant<int, V>(), std::integral_constant<bool, TAIL>(), tpr, e); };
   using std::integral_constant;
   if (cols <= 512) return go(integral_constant<int, 64>(), integral_constant<int, 8>());
   if (cols <= 1024 && !few) return go(integral_constant<int, 64>(), integral_constant<int, 16>());
@@ -117,19 +117,19 @@ void forward(artopk_norm* h, const T* x, int64_t x_stride, int64_t rows, int64_t
     k_norm_forward_long<T><<<blocks, 1024, 0, h->stream>>>(x, x_stride, rows, cols, gamma, beta, eps, y, y_stride, mean, rstd);
     return;
   }
-  auto go = [&](auto V, auto TPR, auto E) {
+  auto go = [&](auto V, auto TAIL, auto TPR, auto E) {
     using S = NormShape<TPR()>;
     const int64_t units = (rows + S::kRows - 1) / S::kRows;
     const int blocks = (int)std::min<int64_t>(units, (int64_t)h->num_cu * (2048 / S::kThreads));
-    k_norm_forward<T, V(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(x, x_stride, rows, (int)cols, gamma, beta, eps,
+    k_norm_forward<T, V(), TAIL(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(x, x_stride, rows, (int)cols, gamma, beta, eps,
                                                                               y, y_stride, mean, rstd);
   };
   constexpr int kWide = 16 / sizeof(T);
   const bool few = rows <= h->num_cu;
   if (wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(y, y_stride, rows, sizeof(T)))
-    with_shape<kWide>(cols, few, go);
+    cols % kWide ? with_shape<kWide, true>(cols, few, go) : with_shape<kWide, false>(cols, few, go);
   else
-    with_shape<1>(cols, few, go);
+    with_shape<1, false>(cols, few, go);
 }
 
 // Returns the number of shares of the weight gradients to be added up, 0 if they are done.
@@ -151,22 +151,22 @@ int backward(artopk_norm* h, const T* dy, int64_t dy_stride, const T* x, int64_t
     return shares;
   }
   const bool columns = part && rows <= kColumnRows && rows * cols <= kColumnElems;
-  auto go = [&](auto V, auto TPR, auto E) {
+  auto go = [&](auto V, auto TAIL, auto TPR, auto E) {
     using S = NormShape<TPR()>;
     const int64_t units = (rows + S::kRows - 1) / S::kRows;
     shares = (int)std::min<int64_t>(units, std::min<int64_t>(kMaxShares, (int64_t)h->num_cu * (1024 / S::kThreads)));
     const int row_blocks = columns && !dx ? 0 : shares;
     const int blocks = row_blocks + (columns ? (int)((cols + 63) / 64) : 0);
-    k_norm_backward<T, V(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(
+    k_norm_backward<T, V(), TAIL(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(
         dy, dy_stride, x, x_stride, rows, (int)cols, gamma, mean, rstd, dx, dx_stride, columns ? nullptr : part, row_blocks, grads);
   };
   constexpr int kWide = 16 / sizeof(T);
   const bool few = rows <= h->num_cu;
   if (wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(dy, dy_stride, rows, sizeof(T)) &&
       (!dx || wide_rows(dx, dx_stride, rows, sizeof(T))))
-    with_shape<kWide>(cols, few, go);
+    cols % kWide ? with_shape<kWide, true>(cols, few, go) : with_shape<kWide, false>(cols, few, go);
   else
-    with_shape<1>(cols, few, go);
+    with_shape<1, false>(cols, few, go);
   if (columns) shares = 0;
   return shares;
 }

@@ -77,22 +77,30 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* room, int turn) {
   }
 }
 
-// V elements of a row as they lie; the last ones of a row whose length is no multiple of V one by one, zeros behind them.
-template <class T, int V>
+// V elements of a row as they lie, zeros behind its end.  With TAIL the row's length need not be a multiple of V, and its last
+// elements go one by one.  Without it a load stands in no branch, behind which it would be waited for: places behind the end
+// read the row's last ones instead (32768 x 2048 bf16 backward 93 us with a branch around each load, 78 so).
+template <class T, int V, bool TAIL>
 struct alignas(V * sizeof(T)) Piece {
   T e[V];
-  __device__ __forceinline__ void load(const T* row, int c, int cols, bool there) {
-    if (there && c + V <= cols) {
-      *this = *reinterpret_cast<const Piece*>(row + c);
-    } else {
+  __device__ __forceinline__ void load(const T* row, int c, int cols) {
+    if constexpr (TAIL) {
+      if (c + V <= cols) {
+        *this = *reinterpret_cast<const Piece*>(row + c);
+      } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) e[i] = there && c + i < cols ? row[c + i] : static_cast<T>(0.0f);
+        for (int i = 0; i < V; ++i) e[i] = c + i < cols ? row[c + i] : static_cast<T>(0.0f);
+      }
+    } else {
+      *this = *reinterpret_cast<const Piece*>(row + (c < cols ? c : cols - V));
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = c < cols ? e[i] : static_cast<T>(0.0f);
     }
   }
   __device__ __forceinline__ void store(T* row, int c, int cols) const {
     if (c + V <= cols) {
       *reinterpret_cast<Piece*>(row + c) = *this;
-    } else {
+    } else if constexpr (TAIL) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (c + i < cols) row[c + i] = e[i];
@@ -119,7 +127,7 @@ __device__ __forceinline__ void load_weights(float (&out)[V], const float* w, in
 }
 
 // Rows blockIdx.x, blockIdx.x + gridDim.x, .. (times the rows a block has); the next row is on its way while one is summed.
-template <class T, int V, int TPR, int E>
+template <class T, int V, bool TAIL, int TPR, int E>
 __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
     const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, const float* __restrict__ gamma,
     const float* __restrict__ beta, float eps, T* __restrict__ y, int64_t y_stride, float* __restrict__ mean_out,
@@ -130,9 +138,9 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
   const float inv = 1.0f / static_cast<float>(cols);
   const int64_t step = (int64_t)gridDim.x * NormShape<TPR>::kRows;
   int64_t row = (int64_t)blockIdx.x * NormShape<TPR>::kRows + threadIdx.x / TPR;
-  Piece<T, V> next[R];
+  Piece<T, V, TAIL> next[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) next[r].load(x + row * x_stride, (r * TPR + t) * V, cols, row < rows);
+  for (int r = 0; r < R; ++r) next[r].load(x + (row < rows ? row : rows - 1) * x_stride, (r * TPR + t) * V, cols);
   float gm[R][V], bt[R][V];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -151,9 +159,10 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
         v[r][i] = static_cast<float>(next[r].e[i]);
         s[0] += v[r][i];
       }
-    if (row + step < rows) {
+    {
+      const int64_t then = row + step < rows ? row + step : rows - 1;
 #pragma unroll
-      for (int r = 0; r < R; ++r) next[r].load(x + (row + step) * x_stride, (r * TPR + t) * V, cols, true);
+      for (int r = 0; r < R; ++r) next[r].load(x + then * x_stride, (r * TPR + t) * V, cols);
     }
     row_sums<TPR>(s, room, 0);
     const float mean = s[0] * inv;
@@ -179,7 +188,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      Piece<T, V> o;
+      Piece<T, V, TAIL> o;
 #pragma unroll
       for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(fmaf(v[r][i] * rstd, gm[r][i], bt[r][i]));
       o.store(y + row * y_stride, (r * TPR + t) * V, cols);
@@ -247,7 +256,7 @@ __device__ void norm_columns(int64_t c0, const T* dy, int64_t dy_stride, const T
 // part[0][blockIdx.x][..] (dgamma) and part[1][blockIdx.x][..] (dbeta), rows of `cols`.  Blocks from row_blocks on, if there
 // are such, take 64 columns each instead and write their weights' gradients whole: few rows are read a second time sooner
 // than a second launch adds up shares (then `part` is NULL).
-template <class T, int V, int TPR, int E>
+template <class T, int V, bool TAIL, int TPR, int E>
 __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols,
     const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
@@ -267,19 +276,19 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
   const float inv = 1.0f / static_cast<float>(cols);
   const int64_t step = (int64_t)row_blocks * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-  Piece<T, V> next_x[R], next_d[R];
+  Piece<T, V, TAIL> next_x[R], next_d[R];
   float next_mu = 0.0f, next_rs = 0.0f;
   auto ask = [&](int64_t of) {
-    const bool there = of < rows;
+    if (of >= rows) of = rows - 1;  // (not used)
+    next_mu = mean[of];
+    next_rs = rstd[of];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      next_x[r].load(x + of * x_stride, (r * TPR + t) * V, cols, there);
-      next_d[r].load(dy + of * dy_stride, (r * TPR + t) * V, cols, there);
+      next_x[r].load(x + of * x_stride, (r * TPR + t) * V, cols);
+      next_d[r].load(dy + of * dy_stride, (r * TPR + t) * V, cols);
     }
-    next_mu = there ? mean[of] : 0.0f;
-    next_rs = there ? rstd[of] : 0.0f;
   };
-  // (with wide loads the second row's registers cost more waves than it gains: 32768 x 2048 bf16 95 us so, KWAIT without)
+  // (with wide loads the second row's registers cost more waves than it gains: 32768 x 2048 bf16 81 us, 78 without)
   constexpr bool kAhead = V == 1;
   if (kAhead) ask(row);
   float dg[R][V], db[R][V], gm[R][V];
@@ -298,16 +307,15 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int i = 0; i < V; ++i) {  // (behind the row's end d is zero)
+      for (int i = 0; i < V; ++i) {  // (behind the row's end d is zero, and nothing comes of h)
         d[r][i] = static_cast<float>(next_d[r].e[i]);
         h[r][i] = (static_cast<float>(next_x[r].e[i]) - mu) * rs;
       }
-    if (kAhead && row + step < rows) ask(row + step);
+    if (kAhead) ask(row + step);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if ((r * TPR + t) * V + i >= cols) h[r][i] = 0.0f;  // (mean and rstd need not be finite)
         dg[r][i] = fmaf(d[r][i], h[r][i], dg[r][i]);
         db[r][i] += d[r][i];
         d[r][i] *= gm[r][i];
@@ -320,7 +328,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     const float m1 = s[0] * inv, m2 = s[1] * inv;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      Piece<T, V> o;
+      Piece<T, V, TAIL> o;
 #pragma unroll
       for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(rs * (d[r][i] - fmaf(h[r][i], m2, m1)));
       o.store(dx + row * dx_stride, (r * TPR + t) * V, cols);
