@@ -399,16 +399,17 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
       }
     }
   };
+  // The second operand goes first: so a lane is given four columns of one row side by side.
   auto mul = [&](int of) {
 #pragma unroll
     for (int i = 0; i < S::kFM; ++i)
 #pragma unroll
       for (int j = 0; j < S::kFN; ++j) {
         if constexpr (PARTS == 2) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[of][PARTS - 1][i], fq[of][0][j], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[of][0][i], fq[of][PARTS - 1][j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[of][0][j], fp[of][PARTS - 1][i], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[of][PARTS - 1][j], fp[of][0][i], acc[i][j], 0, 0, 0);
         }
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[of][0][i], fq[of][0][j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[of][0][j], fp[of][0][i], acc[i][j], 0, 0, 0);
       }
   };
   constexpr int N = S::kStages;
@@ -466,8 +467,8 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
 #endif
 }
 
-// One wave's rows of a tile, by way of its own part of LDS: `value(i, j)` are four sums of rows 16 i + 4 (lane / 16) ..
-// and column 16 j + lane % 16; they go as halves to out[row ld + col] and, `both`, to out_t[col ld_t + row].  Rows and
+// One wave's rows of a tile, by way of its own part of LDS: `value(i, j)` are four sums of row 16 i + lane % 16 and columns
+// 16 j + 4 (lane / 16) ..; they go as halves to out[row ld + col] and, `both`, to out_t[col ld_t + row].  Rows and
 // columns from `rows` and `cols` on are left out (whole chunks of eight: both are multiples of 64).
 template <int FM, int FN, int PARTS, class Value>
 __device__ __forceinline__ void store_halves(Value&& value, _Float16* room, int row0, int col0, int rows, int cols,
@@ -499,9 +500,7 @@ __device__ __forceinline__ void store_halves(Value&& value, _Float16* room, int 
       for (int i = 0; i < CF; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            room[(i * 16 + (lane >> 4) * 4 + e) * (CC + 8) + j * 16 + (lane & 15)] = v[s][i][j][e];
+          *reinterpret_cast<half4*>(room + (i * 16 + (lane & 15)) * (CC + 8) + j * 16 + (lane >> 4) * 4) = v[s][i][j];
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -519,7 +518,9 @@ __device__ __forceinline__ void store_halves(Value&& value, _Float16* room, int 
       for (int i = 0; i < CF; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-          *reinterpret_cast<half4*>(room + (j * 16 + (lane & 15)) * (CR + 8) + i * 16 + (lane >> 4) * 4) = v[s][i][j];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            room[(j * 16 + (lane >> 4) * 4 + e) * (CR + 8) + i * 16 + (lane & 15)] = v[s][i][j][e];
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -610,10 +611,10 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
         for (int j = 0; j < FN; ++j) {
           const f32x4 v = acc[h + i][j] * by;
           if (d.tall) {
-            *reinterpret_cast<f32x4*>(fl + (j * 16 + (lane & 15)) * 36 + i * 16 + (lane >> 4) * 4) = v;
-          } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) fl[(i * 16 + (lane >> 4) * 4 + e) * (CC + 4) + j * 16 + (lane & 15)] = v[e];
+            for (int e = 0; e < 4; ++e) fl[(j * 16 + (lane >> 4) * 4 + e) * 36 + i * 16 + (lane & 15)] = v[e];
+          } else {
+            *reinterpret_cast<f32x4*>(fl + (i * 16 + (lane & 15)) * (CC + 4) + j * 16 + (lane >> 4) * 4) = v;
           }
         }
       asm volatile("" ::: "memory");
@@ -643,19 +644,18 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
       asm volatile("" ::: "memory");
     }
   } else if constexpr (MODE == kSquare) {
-    // (A is symmetric: four rows of one column lie side by side in that row)
     auto value = [&](int i, int j) {
-      const int row = row0 + i * 16 + (lane >> 4) * 4, col = col0 + j * 16 + (lane & 15);
+      const int row = row0 + i * 16 + (lane & 15), col = col0 + j * 16 + (lane >> 4) * 4;
       f32x4 v = acc[i][j] * (cc / kOperandScale);
       if (row < rows && col < cols) {
-        const _Float16* pa = mem + d.a + (int64_t)col * d.mp + row;
+        const _Float16* pa = mem + d.a + (int64_t)row * d.mp + col;
         const half4 hi = *reinterpret_cast<const half4*>(pa);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float av = static_cast<float>(hi[e]);
           if constexpr (PARTS == 2) av += static_cast<float>(reinterpret_cast<const half4*>(pa + mm)[0][e]);
           v[e] = fmaf(cb, av, v[e]);
-          if (row + e == col) v[e] += ca * kOperandScale;
+          if (row == col + e) v[e] += ca * kOperandScale;
         }
       }
       return v;
