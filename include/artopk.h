@@ -497,7 +497,7 @@ enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1 };
  * A handle for the matrices of a flat vector of n elements (1 <= n < 2^31) of `type`.  `mats` is a
  * host array of `count` matrices (1 .. 65535), each within the vector, none overlapping another,
  * rows and cols in [1, 65536], scale finite; it is read before the call returns.  The iterates' memory
- * is allocated here: artopk_matrices_scratch_bytes(..) bytes, 4 for each element of a matrix and 4 for each of its
+ * is allocated here: artopk_matrices_scratch_bytes(..) bytes, 4 for each element of a matrix and 6 for each of its
  * Gram matrix with HALF, of sides padded to whole tiles, and twice that with SPLIT (-1 for arguments that create
  * refuses).  The tables are copied
  * to the device synchronously.  On failure *out is left alone and artopk_last_error(NULL) tells why.

@@ -45,6 +45,7 @@ struct MatPlan {
   Span join;  // the tiles of Gram matrices whose sums are cut
   int64_t halves = 0;  // of the iterates' memory
   int32_t sums = 0;
+  bool pairs = false;  // two steps at once
   bool small = false;  // every matrix on one compute unit, in one launch
   size_t small_lds = 0;
   int64_t slots = 0;   // partial sums of the Gram products' shares
@@ -62,14 +63,11 @@ struct TileCost {
   double fixed, alone, store, among;
   int slots;  // blocks that the chip holds
 };
-constexpr TileCost kCost[2][kTileClasses] = {{{3.0, 0.20, 0.0043, 0.00083, 512},
-                                              {4.0, 0.63, 0.0258, 0.0017, 512},
-                                              {5.0, 0.84, 0.0325, 0.0044, 256},
-                                              {6.0, 1.28, 0.0890, 0.00575, 256}},
-                                             {{3.0, 0.55, 0.0047, 0.00231, 512},
-                                              {4.0, 1.60, 0.0470, 0.0047, 512},
-                                              {5.0, 1.93, 0.0820, 0.0100, 256},
-                                              {6.0, 3.80, 0.1890, 0.0160, 256}}};
+constexpr TileCost kCost[2][2][kTileClasses] = {  // [Q X][two parts]
+    {{{3.0, 0.20, 0.0043, 0.00083, 512}, {4.0, 0.63, 0.0258, 0.0017, 512}, {5.0, 0.84, 0.0325, 0.0044, 256}, {6.0, 1.28, 0.0890, 0.00575, 256}},
+     {{3.0, 0.55, 0.0047, 0.00231, 512}, {4.0, 1.60, 0.0470, 0.0047, 512}, {5.0, 1.93, 0.0820, 0.0100, 256}, {6.0, 3.80, 0.1890, 0.0160, 256}}},
+    {{{3.0, 0.25, 0.0067, 0.00112, 512}, {4.0, 0.65, 0.0200, 0.0018, 512}, {5.0, 0.90, 0.0300, 0.0049, 256}, {6.0, 1.28, 0.0800, 0.0054, 256}},
+     {{3.0, 0.60, 0.0220, 0.00240, 512}, {4.0, 1.60, 0.0350, 0.0047, 512}, {5.0, 2.20, 0.0900, 0.0106, 256}, {6.0, 3.80, 0.1600, 0.0172, 256}}}};
 // Shares that meet in memory: a launch, the shares of one tile one after the other, and their bytes (36 tiles of 64 x 64 in 9
 // shares each 4.6, 10 of 128 x 128 in 18 9.1, one of 64 x 64 in 32 11.1).
 constexpr double kJoinLaunch = 3.5, kJoinShare = 0.22, kJoinBytes = 1.0 / 2.5e6;
@@ -92,7 +90,7 @@ int product_shares(const MatDesc& d, const ProductKind& k, int each) {  // `each
 }
 
 double product_cost(const std::vector<MatDesc>& mats, const ProductKind& k, int parts, int cls, int each) {
-  const TileCost& c = kCost[parts - 1][cls];
+  const TileCost& c = kCost[k.symmetric ? 0 : 1][parts - 1][cls];
   double chip = 0.0, blocks = 0.0, units_in_all = 0.0, longest = 0.0, joined = 0.0;
   int most_shares = 1;
   for (const MatDesc& d : mats) {
@@ -106,10 +104,12 @@ double product_cost(const std::vector<MatDesc>& mats, const ProductKind& k, int 
     if (shares > 1) joined += tiles * shares * kTileOf[cls] * kTileOf[cls] * 8.0;
     most_shares = std::max(most_shares, shares);
   }
-  // whole rounds of blocks at the chip's rate, and a last one that takes a block's own time at least
+  // whole rounds of blocks at the chip's rate, and a last one that takes a block's own time at least, or half of that where
+  // two blocks share a compute unit, since they do not end together
   const double rounds = std::floor(blocks / c.slots), rest = blocks - rounds * c.slots;
   double cost = chip * (rounds * c.slots / blocks);
-  if (rest > 0.0) cost += std::max(c.fixed + c.alone * (units_in_all / blocks), chip * (rest / blocks));
+  if (rest > 0.0)
+    cost += std::max((c.fixed + c.alone * (units_in_all / blocks)) * (rounds > 0.0 ? 256.0 / c.slots : 1.0), chip * (rest / blocks));
   cost = std::max(cost, c.fixed + c.alone * longest);
   if (most_shares > 1) cost += kJoinLaunch + kJoinShare * most_shares + kJoinBytes * joined;
   return cost;
@@ -249,9 +249,8 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
     const int64_t mn = (int64_t)d.mp * d.np * parts, mm = (int64_t)d.mp * d.mp * parts;
     d.x[0] = plan->halves;
     d.x[1] = d.x[0] + mn;
-    d.a = d.x[1] + mn;
-    d.q = d.a + mm;
-    plan->halves = d.q + mm;
+    for (int k = 0; k < 3; ++k) d.sq[k] = d.x[1] + mn + k * mm;
+    plan->halves = d.sq[2] + mm;
   }
 
   // pieces of the vector, those of a matrix side by side; at most 512 a matrix, so that every block that needs its norm
@@ -288,9 +287,11 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   }
   const ProductKind gram = {true, true}, square = {true, false}, apply = {false, false};
   int each = 0;
-  double cost = choose_product(plan->mats, gram, parts, &plan->gram, &each);
-  cost += choose_product(plan->mats, square, parts, &plan->square, nullptr);
-  cost += choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
+  const double cost_gram = choose_product(plan->mats, gram, parts, &plan->gram, &each);
+  const double cost_square = choose_product(plan->mats, square, parts, &plan->square, nullptr);
+  const double cost_apply = choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
+  const double cost = cost_gram + cost_square + cost_apply;
+  plan->pairs = cost_gram + 5.0 * cost_square + cost_apply < 2.0 * cost;
   if (plan->small) plan->small = small_cost(plan->mats, parts, plan->small_lds) < cost;
   if (plan->small) {
     plan->tiles.clear();
@@ -339,6 +340,7 @@ struct artopk_matrices {
   Product gram, square, apply;
   Span join;
   int count = 0;
+  bool pairs = false;
   size_t small_lds = 0;  // 0: not small
   float* partial = nullptr;
   char* slab = nullptr;
@@ -360,16 +362,25 @@ namespace {
                        __LINE__);                                                                              \
   } while (0)
 
+struct Steps {
+  int count = 0;
+  float co[ARTOPK_MAX_POLAR_STEPS][3];
+  double factor[ARTOPK_MAX_POLAR_STEPS];  // the largest |a + b s^2 + c s^4|
+};
+constexpr double kMostFactor = 15.0;
+
 // The coefficients of every step, or ARTOPK_EINVAL where the iterates could leave the operands' range: with singular
 // values of at most `most` before a step, the largest of |s (a + b s^2 + c s^4)| and of |a + b s^2 + c s^4| over
 // [0, most] lie at an end or where a derivative is zero.
-int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficients, float (*out)[3]) {
+int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficients, Steps* st) {
   if (steps < 0 || steps > ARTOPK_MAX_POLAR_STEPS)
     return fail_text(h->err, ARTOPK_EINVAL, "steps=%d outside [0, %d]", steps, ARTOPK_MAX_POLAR_STEPS);
   double most = 1.0;
+  st->count = steps;
   for (int k = 0; k < steps; ++k) {
-    for (int i = 0; i < 3; ++i) out[k][i] = coefficients ? coefficients[3 * k + i] : kUsual[i];
-    const double a = out[k][0], b = out[k][1], c = out[k][2];
+    float* out = st->co[k];
+    for (int i = 0; i < 3; ++i) out[i] = coefficients ? coefficients[3 * k + i] : kUsual[i];
+    const double a = out[0], b = out[1], c = out[2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c))
       return fail_text(h->err, ARTOPK_EINVAL, "coefficients of step %d are not finite", k);
     double next = 0.0, factor = std::fabs(a);
@@ -389,7 +400,8 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
       }
     }
     if (b != 0.0) look(-a / (3.0 * b));  // (c = 0; an extra point otherwise)
-    if (next > 2.0 || factor > 15.0)
+    st->factor[k] = factor;
+    if (next > 2.0 || factor > kMostFactor)
       return fail_text(h->err, ARTOPK_EINVAL,
                        "step %d would take singular values up to %.4g to %.4g, with a factor of %.4g; at most 2 and 15 are taken", k,
                        most, next, factor);
@@ -399,18 +411,18 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 }
 
 template <int TILE, int PARTS, int MODE>
-void product(artopk_matrices* h, const Span& s, int from, const float* co, const FinishArgs& f) {
-  k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
-      h->tiles + s.at, h->mem, from, co[0], co[1], co[2], f, h->partial);
+void product(artopk_matrices* h, const Span& s, const ProductArgs& a, const FinishArgs& f) {
+  k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(h->tiles + s.at, h->mem, a, f,
+                                                                                                  h->partial);
 }
 
 template <int PARTS, int MODE>
-void product(artopk_matrices* h, const Product& p, int from, const float* co, const FinishArgs& f) {
+void product(artopk_matrices* h, const Product& p, const ProductArgs& a, const FinishArgs& f) {
   switch (p.cls) {
-    case 0: return product<64, PARTS, MODE>(h, p.tiles, from, co, f);
-    case 1: return product<128, PARTS, MODE>(h, p.tiles, from, co, f);
-    case 2: return product<192, PARTS, MODE>(h, p.tiles, from, co, f);
-    default: return product<256, PARTS, MODE>(h, p.tiles, from, co, f);
+    case 0: return product<64, PARTS, MODE>(h, p.tiles, a, f);
+    case 1: return product<128, PARTS, MODE>(h, p.tiles, a, f);
+    case 2: return product<192, PARTS, MODE>(h, p.tiles, a, f);
+    default: return product<256, PARTS, MODE>(h, p.tiles, a, f);
   }
 }
 
@@ -422,36 +434,53 @@ void join_shares(artopk_matrices* h) {
 
 // What the squares' or the momentum's launch leaves to do.
 template <int PARTS, class From>
-void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], float eps, const FinishArgs& f) {
-  if (steps == 0) {
+void polar(artopk_matrices* h, From from, const Steps& st, float eps, const FinishArgs& f) {
+  if (st.count == 0) {
     k_mat_scaled<From><<<h->nchunks, 256, 0, h->stream>>>(from, h->mats, h->chunks, h->sums, eps, f);
     return;
   }
   if (h->small_lds) {
-    PolarSteps st = {};
-    st.steps = steps;
-    memcpy(st.co, co, sizeof(float) * 3 * steps);
-    k_mat_small<PARTS, From><<<h->count, kSmallThreads, h->small_lds, h->stream>>>(from, h->mats, st, eps, f);
+    PolarSteps ps = {};
+    ps.steps = st.count;
+    memcpy(ps.co, st.co, sizeof(float) * 3 * st.count);
+    k_mat_small<PARTS, From><<<h->count, kSmallThreads, h->small_lds, h->stream>>>(from, h->mats, ps, eps, f);
     return;
   }
   k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->tiles + h->begin.at, h->sums, eps, h->mem);
-  for (int k = 0; k < steps; ++k) {
-    product<PARTS, kGram>(h, h->gram, k & 1, co[k], f);
+  int x = 0;  // which X
+  auto square = [&](int k, int in, int out) {
+    product<PARTS, kSquare>(h, h->square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2]}, f);
+  };
+  auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, h->square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
+  for (int k = 0; k < st.count;) {
+    product<PARTS, kGram>(h, h->gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
     if (h->join.count) h->gram.cls == 0 ? join_shares<64, PARTS>(h) : join_shares<128, PARTS>(h);
-    product<PARTS, kSquare>(h, h->square, k & 1, co[k], f);
-    if (k + 1 < steps)
-      product<PARTS, kApply>(h, h->apply, k & 1, co[k], f);
+    square(k, 0, 1);
+    int q = 1;
+    if (h->pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {
+      times(1, 0, 2);      // Q_1 A_0
+      times(2, 1, 0);      // A_1
+      square(k + 1, 0, 2);  // Q_2
+      times(2, 1, 0);      // Q_2 Q_1
+      q = 0;
+      ++k;
+    }
+    ++k;
+    const ProductArgs a = {x, q, 0, 0, 0, 0, 0};
+    if (k < st.count)
+      product<PARTS, kApply>(h, h->apply, a, f);
     else
-      product<PARTS, kFinal>(h, h->apply, k & 1, co[k], f);
+      product<PARTS, kFinal>(h, h->apply, a, f);
+    x ^= 1;
   }
 }
 
 template <class From>
-void polar(artopk_matrices* h, From from, int32_t steps, const float (*co)[3], float eps, const FinishArgs& f) {
+void polar(artopk_matrices* h, From from, const Steps& st, float eps, const FinishArgs& f) {
   if (h->parts == 2)
-    polar<2>(h, from, steps, co, eps, f);
+    polar<2>(h, from, st, eps, f);
   else
-    polar<1>(h, from, steps, co, eps, f);
+    polar<1>(h, from, st, eps, f);
 }
 
 // Calls f with a null pointer of the handle's element type.
@@ -521,6 +550,7 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->begin = plan.begin;
   h->gram = plan.gram;
   h->join = plan.join;
+  h->pairs = plan.pairs;
   h->count = (int)plan.mats.size();
   h->small_lds = plan.small ? plan.small_lds : 0;
   h->square = plan.square;
@@ -566,10 +596,10 @@ const char* artopk_matrices_last_error(const artopk_matrices* m) { return m ? m-
 int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t steps, const float* coefficients, float eps) {
   if (!m) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_orthogonalize: m is NULL");
   int rc;
-  float co[ARTOPK_MAX_POLAR_STEPS][3];
+  Steps st;
   const size_t size = elem_size(m->type);
   if ((rc = check_vector(m, "x", x, size)) || (rc = check_vector(m, "out", out, size))) return rc;
-  if ((rc = take_coefficients(m, steps, coefficients, co)) || (rc = check_eps(m, eps))) return rc;
+  if ((rc = take_coefficients(m, steps, coefficients, &st)) || (rc = check_eps(m, eps))) return rc;
   {
     RangeSet rs;
     rs.add(x, (size_t)m->n * size, false, "x");
@@ -582,7 +612,7 @@ int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t s
   with_type(m->type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     if (!m->small_lds || steps == 0) k_mat_squares<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), m->chunks, m->sums);
-    polar(m, FromVector<T>{static_cast<const T*>(x)}, steps, co, eps, f);
+    polar(m, FromVector<T>{static_cast<const T*>(x)}, st, eps, f);
   });
   MAT_TRY(m, hipGetLastError());
   return ARTOPK_OK;
@@ -593,7 +623,7 @@ int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const f
                      float eps) {
   if (!m) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_muon_step: m is NULL");
   int rc;
-  float co[ARTOPK_MAX_POLAR_STEPS][3];
+  Steps st;
   const size_t size = elem_size(m->type);
   if ((rc = check_vector(m, "weights", weights, size)) || (rc = check_vector(m, "momentum", momentum, 4)) ||
       (rc = check_vector(m, "update", update, 4)))
@@ -601,7 +631,7 @@ int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const f
   if (!std::isfinite(update_scale) || !std::isfinite(mu) || !std::isfinite(eta) || !std::isfinite(decay) ||
       !std::isfinite(eta_rest))
     return fail_text(m->err, ARTOPK_EINVAL, "update_scale, mu, eta, decay or eta_rest is not finite");
-  if ((rc = take_coefficients(m, steps, coefficients, co)) || (rc = check_eps(m, eps))) return rc;
+  if ((rc = take_coefficients(m, steps, coefficients, &st)) || (rc = check_eps(m, eps))) return rc;
   {
     RangeSet rs;
     rs.add(weights, (size_t)m->n * size, true, "weights");
@@ -618,7 +648,7 @@ int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const f
     using T = std::remove_pointer_t<decltype(tag)>;
     k_mat_momentum<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<T*>(weights), momentum, update, f.a, m->chunks, m->sums);
   });
-  polar(m, FromMomentum{momentum, update, f.a}, steps, co, eps, f);
+  polar(m, FromMomentum{momentum, update, f.a}, st, eps, f);
   MAT_TRY(m, hipGetLastError());
   return ARTOPK_OK;
 }

@@ -4,6 +4,13 @@
 //   X_0 = G / (||G|| + eps),   A = X X^T,   Q = a I + b A + c A^2,   X <- Q X.
 // A and Q are symmetric, so only their tiles on and below the diagonal are computed, and each is stored twice.
 //
+// Two steps at once.  Every A and Q is a polynomial in the first A, so they commute and all their products are symmetric, too.
+// After X_1 = Q_1 X_0 the next A is Q_1 A_0 Q_1 and X_2 = (Q_2 Q_1) X_0: five products of m x m by halves and one of each that
+// is n long, instead of two and two.  With many more columns than rows that is up to twice as fast.  What it costs: A_1's
+// small eigenvalues keep the error of A_0's roundings times up to a^2, which Q_2, whose first term is a I, damps again
+// (errors of the result, simulated: 5e-7 to 7e-7 instead of 4e-7 to 6e-7 with two parts, 1.1e-3 to 1.9e-3 instead of 1.1e-3 to
+// 1.7e-3 with one).  Three steps at once would not do: the error grows by another a^2, and Q_3 Q_2 Q_1 passes the range below.
+//
 // Operands.  The products run on the matrix cores in float16 with float32 sums.  Entries of X are at most 2 in size,
 // those of A at most 4, those of Q at most 15 (the host refuses coefficients that would pass these bounds), so each is
 // stored times 2^12: 2^16 is never reached, and a matrix of 16384 x 16384 still has its first X's typical entry, 2^-14,
@@ -37,7 +44,8 @@ struct MatDesc {
   int32_t mp, np;       // padded
   int32_t tall;         // the flat vector holds n rows of m
   float scale;
-  int64_t x[2], a, q;   // X before and after a step, in turn
+  int64_t x[2];   // X before and after a step, in turn
+  int64_t sq[3];  // A, Q and their products, m x m
   int32_t part, parts;  // its sums of squares
 };
 
@@ -261,7 +269,15 @@ __global__ __launch_bounds__(256) void k_mat_scaled(From from, const MatDesc* __
   }
 }
 
-enum { kGram = 0, kSquare = 1, kApply = 2, kFinal = 3 };
+// kGram: sq[out] = X X^T;  kSquare: sq[out] = ca I + cb A + cc A^2, A = sq[in];  kTimes: sq[out] = sq[in] sq[in2], which commute;
+// kApply: the other X = sq[in] X;  kFinal: the same to the caller's buffer.
+enum { kGram = 0, kSquare = 1, kApply = 2, kFinal = 3, kTimes = 4 };
+
+struct ProductArgs {
+  int32_t from;  // which X
+  int32_t in, in2, out;
+  float ca, cb, cc;
+};
 
 // The shape of a product's tile: TILE x TILE elements by WM x WN waves, the summed index in stages of kDepth, kStages of
 // them in LDS.  A stage is brought by loads that go to LDS without passing registers, two stages ahead of its use at most,
@@ -546,8 +562,7 @@ constexpr int store_room() {
 
 template <int TILE, int PARTS, int MODE>
 __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShape<TILE, PARTS>::kBlocks)) void k_mat_product(
-    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, int from, float ca,
-    float cb, float cc, FinishArgs f, float* __restrict__ partial) {
+    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, ProductArgs a, FinishArgs f, float* __restrict__ partial) {
   using S = ProductShape<TILE, PARTS>;
   constexpr int FM = S::kFM, FN = S::kFN;
   constexpr int kRoom = store_room<FM, FN>();
@@ -567,16 +582,17 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = 0.0f;
   if constexpr (kTurned) {
-    multiply<S, true>(mem + d.q + (int64_t)i0 * d.mp, mm, p_rows, d.mp, mem + d.x[from] + j0, mn, q_rows, d.np,
+    multiply<S, true>(mem + d.sq[a.in] + (int64_t)i0 * d.mp, mm, p_rows, d.mp, mem + d.x[a.from] + j0, mn, q_rows, d.np,
                       d.mp / S::kDepth, lds, acc);
   } else {
-    const _Float16* p = mem + (MODE == kGram ? d.x[from] : d.a);
+    const _Float16* p = mem + (MODE == kGram ? d.x[a.from] : d.sq[a.in]);
+    const _Float16* q = MODE == kTimes ? mem + d.sq[a.in2] : p;
     const int ld = MODE == kGram ? d.np : d.mp;
     // a share is whole pieces of 64
     const int begin = MODE == kGram ? (int)((int64_t)(ld / 64) * t.share / t.shares) * 64 : 0;
     const int end = MODE == kGram ? (int)((int64_t)(ld / 64) * (t.share + 1) / t.shares) * 64 : ld;
     const int64_t plane = MODE == kGram ? mn : mm;
-    multiply<S, false>(p + (int64_t)i0 * ld + begin, plane, p_rows, ld, p + (int64_t)j0 * ld + begin, plane, q_rows, ld,
+    multiply<S, false>(p + (int64_t)i0 * ld + begin, plane, p_rows, ld, q + (int64_t)j0 * ld + begin, plane, q_rows, ld,
                        (end - begin) / S::kDepth, lds, acc);
   }
 
@@ -646,27 +662,28 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
   } else if constexpr (MODE == kSquare) {
     auto value = [&](int i, int j) {
       const int row = row0 + i * 16 + (lane & 15), col = col0 + j * 16 + (lane >> 4) * 4;
-      f32x4 v = acc[i][j] * (cc / kOperandScale);
+      f32x4 v = acc[i][j] * (a.cc / kOperandScale);
       if (row < rows && col < cols) {
-        const _Float16* pa = mem + d.a + (int64_t)row * d.mp + col;
+        const _Float16* pa = mem + d.sq[a.in] + (int64_t)row * d.mp + col;
         const half4 hi = *reinterpret_cast<const half4*>(pa);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float av = static_cast<float>(hi[e]);
           if constexpr (PARTS == 2) av += static_cast<float>(reinterpret_cast<const half4*>(pa + mm)[0][e]);
-          v[e] = fmaf(cb, av, v[e]);
-          if (row == col + e) v[e] += ca * kOperandScale;
+          v[e] = fmaf(a.cb, av, v[e]);
+          if (row == col + e) v[e] += a.ca * kOperandScale;
         }
       }
       return v;
     };
-    store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.q, d.mp, mem + d.q, d.mp, mm, t.i != t.j);
+    store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.sq[a.out], d.mp, mem + d.sq[a.out], d.mp, mm, t.i != t.j);
   } else {
     auto value = [&](int i, int j) { return acc[i][j] * (1.0f / kOperandScale); };
-    if constexpr (MODE == kGram)
-      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.a, d.mp, mem + d.a, d.mp, mm, t.i != t.j);
+    if constexpr (MODE == kGram || MODE == kTimes)
+      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.sq[a.out], d.mp, mem + d.sq[a.out], d.mp, mm,
+                                  t.i != t.j);
     else
-      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.x[from ^ 1], d.np, nullptr, 0, mn, false);
+      store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.x[a.from ^ 1], d.np, nullptr, 0, mn, false);
   }
 }
 
@@ -881,7 +898,7 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads)) void k_mat_j
       for (int j = 0; j < QN; ++j)
         sum[i][j] += all[(int64_t)s * (TILE * TILE / 4) + ((qi + i) * FN + qj + j) * S::kThreads];
   auto value = [&](int i, int j) { return sum[i][j] * (1.0f / kOperandScale); };
-  store_halves<QM, QN, PARTS>(value, lds + wave * kRoom, row0, col0, d.mp, d.mp, mem + d.a, d.mp, mem + d.a, d.mp,
+  store_halves<QM, QN, PARTS>(value, lds + wave * kRoom, row0, col0, d.mp, d.mp, mem + d.sq[0], d.mp, mem + d.sq[0], d.mp,
                               (int64_t)d.mp * d.mp, t.i != t.j);
 }
 

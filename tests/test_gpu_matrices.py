@@ -154,6 +154,30 @@ def test_steps_and_coefficients():
             assert off <= tol, (steps, r, c, off, tol)
 
 
+@pytest.mark.parametrize("t,products", [("f32", 1), ("bf16", 0)])
+def test_steps_in_pairs_and_alone(t, products):
+    """Many more columns than rows, where two steps are taken at once, with an odd step left over, and with factors too large
+    for that."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(14)
+    mats, n = layout([(130, 2000), (2500, 200), (64, 1111), (300, 3001)])
+    x = torch.from_numpy(_gradients(rng, [m[1:3] for m in mats], n)).cuda().to(_dtype(t))
+    out = torch.zeros_like(x)
+    ctx = lib.MatrixContext(mats, n, _code(t), products)
+    steep = [(3.9, -6.2, 2.9), (3.9, -6.2, 2.9)]  # 3.9^2 > 15: one at a time
+    for steps, co in ((1, USUAL), (2, USUAL), (3, USUAL), (4, USUAL), (6, (1.875, -1.25, 0.375)), (2, steep)):
+        ctx.artopk_orthogonalize(x, out, steps=steps, coefficients=co)
+        got, xs = out.cpu().double().numpy(), x.cpu().double().numpy()
+        for at, r, c, scale in mats:
+            want, norms = reference(xs[at:at + r * c].reshape(r, c), steps, co)
+            slope = max(np.ravel(co))  # a is the largest slope
+            off = np.linalg.norm(got[at:at + r * c].reshape(r, c) - scale * want) / np.linalg.norm(scale * want)
+            # two steps at once: the second's A is worked out from rounded factors, three more roundings of size 4 u
+            assert off <= 2 * tolerance(norms, OPERAND_U[products], slope) + OUT_U[t], (steps, r, c, off)
+
+
 def test_special_values_stay_in_their_matrix():
     import torch
     import paper_2312_02493_amd as lib
