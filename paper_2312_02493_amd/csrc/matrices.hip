@@ -291,7 +291,7 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   const double cost_square = choose_product(plan->mats, square, parts, &plan->square, nullptr);
   const double cost_apply = choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
   const double cost = cost_gram + cost_square + cost_apply;
-  plan->pairs = cost_gram + 5.0 * cost_square + cost_apply < 2.0 * cost;
+  plan->pairs = cost_gram + 5.0 * cost_square + cost_apply < 0.9 * 2.0 * cost;  // (not for a little: it rounds more)
   if (plan->small) plan->small = small_cost(plan->mats, parts, plan->small_lds) < cost;
   if (plan->small) {
     plan->tiles.clear();
