@@ -17,8 +17,8 @@ using namespace artopk;
 
 namespace {
 
-constexpr int kTileClasses = 4;
-constexpr int kTileOf[kTileClasses] = {64, 128, 192, 256};
+constexpr int kTileClasses = 5;
+constexpr int kTileOf[kTileClasses] = {64, 128, 192, 256, 64};  // the last one deep
 constexpr int32_t kMaxMatrices = 65535;
 constexpr int32_t kMaxSide = 65536;
 constexpr float kUsual[3] = {3.4445f, -4.7750f, 2.0315f};
@@ -63,11 +63,28 @@ struct TileCost {
   double fixed, alone, store, among;
   int slots;  // blocks that the chip holds
 };
+constexpr TileCost kNever = {1e9, 1e9, 1e9, 1e9, 256};  // (one part is fed as fast without)
 constexpr TileCost kCost[2][2][kTileClasses] = {  // [Q X][two parts]
-    {{{3.0, 0.20, 0.0043, 0.00083, 512}, {4.0, 0.63, 0.0258, 0.0017, 512}, {5.0, 0.84, 0.0325, 0.0044, 256}, {6.0, 1.28, 0.0890, 0.00575, 256}},
-     {{3.0, 0.55, 0.0047, 0.00231, 512}, {4.0, 1.60, 0.0470, 0.0047, 512}, {5.0, 1.93, 0.0820, 0.0100, 256}, {6.0, 3.80, 0.1890, 0.0160, 256}}},
-    {{{3.0, 0.25, 0.0067, 0.00112, 512}, {4.0, 0.65, 0.0200, 0.0018, 512}, {5.0, 0.90, 0.0300, 0.0049, 256}, {6.0, 1.28, 0.0800, 0.0054, 256}},
-     {{3.0, 0.60, 0.0220, 0.00240, 512}, {4.0, 1.60, 0.0350, 0.0047, 512}, {5.0, 2.20, 0.0900, 0.0106, 256}, {6.0, 3.80, 0.1600, 0.0172, 256}}}};
+    {{{3.0, 0.20, 0.0043, 0.00083, 512},
+      {4.0, 0.63, 0.0258, 0.0017, 512},
+      {5.0, 0.84, 0.0325, 0.0044, 256},
+      {6.0, 1.28, 0.0890, 0.00575, 256},
+      kNever},
+     {{3.0, 0.60, 0.0050, 0.0019, 512},
+      {4.0, 1.60, 0.0470, 0.0047, 512},
+      {5.0, 1.93, 0.0820, 0.0100, 256},
+      {6.0, 3.80, 0.1890, 0.0160, 256},
+      {3.0, 0.38, 0.0060, 0.0019, 256}}},
+    {{{3.0, 0.25, 0.0067, 0.00112, 512},
+      {4.0, 0.65, 0.0200, 0.0018, 512},
+      {5.0, 0.90, 0.0300, 0.0049, 256},
+      {6.0, 1.28, 0.0800, 0.0054, 256},
+      kNever},
+     {{3.0, 0.60, 0.0057, 0.00183, 512},
+      {4.0, 1.60, 0.0350, 0.0047, 512},
+      {5.0, 2.20, 0.0900, 0.0106, 256},
+      {6.0, 3.80, 0.1600, 0.0172, 256},
+      {3.0, 0.40, 0.0090, 0.0027, 256}}}};
 // Shares that meet in memory: a launch, the shares of one tile one after the other, and their bytes (36 tiles of 64 x 64 in 9
 // shares each 4.6, 10 of 128 x 128 in 18 9.1, one of 64 x 64 in 32 11.1).
 constexpr double kJoinLaunch = 3.5, kJoinShare = 0.22, kJoinBytes = 1.0 / 2.5e6;
@@ -120,7 +137,7 @@ double choose_product(const std::vector<MatDesc>& mats, const ProductKind& k, in
   double best = 1e300;
   for (int cls = 0; cls < kTileClasses; ++cls)
     for (int each : {0, 64, 32, 16, 8}) {
-      if (each && (!k.long_sum || cls > 1)) continue;
+      if (each && (!k.long_sum || kTileOf[cls] > 128)) continue;
       const double cost = product_cost(mats, k, parts, cls, each);
       if (cost < best) {
         best = cost;
@@ -422,13 +439,14 @@ void product(artopk_matrices* h, const Product& p, const ProductArgs& a, const F
     case 0: return product<64, PARTS, MODE>(h, p.tiles, a, f);
     case 1: return product<128, PARTS, MODE>(h, p.tiles, a, f);
     case 2: return product<192, PARTS, MODE>(h, p.tiles, a, f);
-    default: return product<256, PARTS, MODE>(h, p.tiles, a, f);
+    case 3: return product<256, PARTS, MODE>(h, p.tiles, a, f);
+    default: return product<64 + (PARTS == 2 ? kDeep : 0), PARTS, MODE>(h, p.tiles, a, f);
   }
 }
 
 template <int TILE, int PARTS>
 void join_shares(artopk_matrices* h) {
-  k_mat_join<TILE, PARTS><<<dim3(h->join.count, 4), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
+  k_mat_join<TILE, PARTS><<<dim3(h->join.count, 2), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
       h->tiles + h->join.at, h->mem, h->partial);
 }
 
@@ -454,7 +472,7 @@ void polar(artopk_matrices* h, From from, const Steps& st, float eps, const Fini
   auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, h->square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
   for (int k = 0; k < st.count;) {
     product<PARTS, kGram>(h, h->gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
-    if (h->join.count) h->gram.cls == 0 ? join_shares<64, PARTS>(h) : join_shares<128, PARTS>(h);
+    if (h->join.count) kTileOf[h->gram.cls] == 64 ? join_shares<64, PARTS>(h) : join_shares<128, PARTS>(h);
     square(k, 0, 1);
     int q = 1;
     if (h->pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {

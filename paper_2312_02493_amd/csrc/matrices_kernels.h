@@ -281,22 +281,26 @@ struct ProductArgs {
 // The shape of a product's tile: TILE x TILE elements by WM x WN waves, the summed index in stages of kDepth, kStages of
 // them in LDS.  A stage is brought by loads that go to LDS without passing registers, two stages ahead of its use at most,
 // and every wave keeps the next 32 of the summed index in registers while it multiplies the present ones.
+constexpr int kDeep = 1;  // added to a TILE: more stages, and one block a compute unit
 template <int TILE_, int PARTS_>
 struct ProductShape {
-  static constexpr int TILE = TILE_, PARTS = PARTS_;
+  static constexpr int TILE = TILE_ & ~kDeep, PARTS = PARTS_;
   static constexpr int kWM = 2, kWN = TILE >= 192 ? 4 : 2;
-  static constexpr int kWaves = kWM * kWN, kThreads = kWaves * 64;
-  static constexpr int kDepth = PARTS == 2 ? 32 : 64;
-  static constexpr int kStages = TILE == 256 || TILE == 128 ? 2 : TILE == 192 ? 3 : 4;
+  // Two groups of waves take turns along the summed index and add up at the end, where a tile has little work for a stage.
+  static constexpr int kGroups = TILE == 64 && PARTS == 2 ? 2 : 1;
+  static constexpr int kWaves = kWM * kWN * kGroups, kThreads = kWaves * 64;
+  static constexpr int kDepth = PARTS == 2 ? 32 * kGroups : 64;
+  static constexpr int kStages = TILE == 256 || TILE == 128 ? 2 : TILE == 192 ? 3 : kGroups == 1 ? 4 : TILE_ & kDeep ? 3 : 2;
   static constexpr int kChunks = kDepth / 8;        // of 16 bytes in a row of a stage
   static constexpr int kLoadRows = 64 / kChunks;    // rows that one load of a wave brings
   static constexpr int kRowsM = TILE / kWM, kRowsN = TILE / kWN;  // of a wave
   static constexpr int kFM = kRowsM / 16, kFN = kRowsN / 16;
+  static constexpr int kOutM = kFM / kGroups;  // fragments of rows that a wave has in the end
   static constexpr int kLoads = 2 * PARTS * TILE / kLoadRows / kWaves;  // of a wave, a stage
   static constexpr int kPlane = TILE * kDepth, kStage = 2 * PARTS * kPlane;  // halves
   static constexpr int kHalves = kStages * kStage;
   // Two blocks of the smaller tiles share a compute unit.
-  static constexpr int kBlocks = TILE >= 192 ? 1 : 2;
+  static constexpr int kBlocks = TILE >= 192 || kHalves > 40960 ? 1 : 2;
   // A second set of operands in registers has no room beside the sums of a 256 tile in two parts.
   static constexpr bool kAhead = !(TILE == 256 && PARTS == 2);
   // Where there is room the small products of two parts are summed by themselves: a third of the roundings against the large
@@ -334,18 +338,19 @@ __device__ __forceinline__ void block_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// acc += P Q^T for `steps` stages (an even number with two parts), P's and Q's rows `ld` and `q_ld` apart.  With `TURNED`
-// acc += P Q instead: Q's rows lie across the summed index.  P's rows from p_rows on count as zeros (and Q's from q_rows on; of
+// out = P Q^T over `steps` stages (one at least), P's and Q's rows `ld` and `q_ld` apart.  With `TURNED`
+// out = P Q instead: Q's rows lie across the summed index.  P's rows from p_rows on count as zeros (and Q's from q_rows on; of
 // a turned Q, columns from `q_rows` on may count as anything that lies in memory behind them up to the matrix's end, or as
 // zeros), and so do stages behind the last: the loads' descriptors end there.
 template <class S, bool TURNED>
 __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int p_rows, int ld, const _Float16* q,
                                          int64_t q_plane, int q_rows, int q_ld, int steps, _Float16* lds,
-                                         f32x4 (&acc)[S::kFM][S::kFN]) {
+                                         f32x4 (&out)[S::kOutM][S::kFN]) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the loads to LDS are unknown to the host's compiler)
   constexpr int TILE = S::TILE, PARTS = S::PARTS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wi = wave / S::kWN * S::kRowsM, wj = wave % S::kWN * S::kRowsN;
+  const int group = wave / (S::kWM * S::kWN), wave2 = wave % (S::kWM * S::kWN);
+  const int wi = wave2 / S::kWN * S::kRowsM, wj = wave2 % S::kWN * S::kRowsN;
   const int lr = lane / S::kChunks;
   const int lc = S::kChunks == 8 ? (lane % 8) ^ (lr & 7) : (lane % 4) ^ ((lr >> 1) & 3);
   constexpr int G = TILE / S::kLoadRows;    // loads of one operand's part
@@ -387,7 +392,7 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
           0, 0);
     }
   };
-  constexpr int KS = S::kDepth / 32;
+  constexpr int KS = S::kDepth / 32 / S::kGroups;  // of a group
   constexpr int SETS = S::kAhead ? 2 : 1;
   half8 fp[SETS][PARTS][S::kFM], fq[SETS][PARTS][S::kFN];
   // (of a turned operand a lane names four columns of one row and is given four rows of one column: in each sixteen lanes,
@@ -395,6 +400,7 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
   const int tr = (lane >> 4) * 8 + ((lane & 15) >> 2);
   const int flip = turned_flip<TILE>(tr);  // the same for r + 4 and r + 32
   auto read = [&](int stage, int ks, int to) {
+    ks += group * KS;
     const _Float16* here = lds + stage * S::kStage;
     const int c = ks * 4 + (lane >> 4);
 #pragma unroll
@@ -417,6 +423,11 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
       }
     }
   };
+  f32x4 acc[S::kFM][S::kFN];
+#pragma unroll
+  for (int i = 0; i < S::kFM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::kFN; ++j) acc[i][j] = 0.0f;
   f32x4 low[S::kLow ? S::kFM : 1][S::kLow ? S::kFN : 1];
 #pragma unroll
   for (int i = 0; i < (S::kLow ? S::kFM : 1); ++i)
@@ -466,12 +477,17 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
       for (int k = 0; k + 1 < steps; ++k) stage(k, 0, true);
       stage(steps - 1, 0, false);
     } else {
-      for (int k = 0; k + 2 < steps; k += 2) {
+      int k = 0;
+      for (; k + 2 < steps; k += 2) {
         stage(k, 0, true);
         stage(k + 1, 1, true);
       }
-      stage(steps - 2, 0, true);
-      stage(steps - 1, 1, false);
+      if (steps - k == 2) {
+        stage(k, 0, true);
+        stage(k + 1, 1, false);
+      } else {
+        stage(k, 0, false);
+      }
     }
   } else {
     for (int k = 0; k < steps; ++k) {
@@ -493,6 +509,27 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
       for (int j = 0; j < S::kFN; ++j) acc[i][j] += low[i][j];
   wait_loads<0>();  // the loads behind the last stage still write
   block_barrier();
+  if constexpr (S::kGroups == 1) {
+#pragma unroll
+    for (int i = 0; i < S::kFM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::kFN; ++j) out[i][j] = acc[i][j];
+  } else {  // each group finishes half of the rows, with what the other has of them
+    f32x4* room = reinterpret_cast<f32x4*>(lds);
+    constexpr int H = S::kOutM, T = S::kWM * S::kWN * 64;
+    const int t = wave2 * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < S::kFN; ++j) room[((group * H + i) * S::kFN + j) * T + t] = group ? acc[i][j] : acc[H + i][j];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < S::kFN; ++j)
+        out[i][j] = (group ? acc[H + i][j] : acc[i][j]) + room[(((group ^ 1) * H + i) * S::kFN + j) * T + t];
+    __syncthreads();
+  }
 #endif
 }
 
@@ -573,11 +610,11 @@ constexpr int store_room() {
   return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
-template <int TILE, int PARTS, int MODE>
-__global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShape<TILE, PARTS>::kBlocks)) void k_mat_product(
+template <int SHAPE, int PARTS, int MODE>
+__global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductShape<SHAPE, PARTS>::kBlocks)) void k_mat_product(
     const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, ProductArgs a, FinishArgs f, float* __restrict__ partial) {
-  using S = ProductShape<TILE, PARTS>;
-  constexpr int FM = S::kFM, FN = S::kFN;
+  using S = ProductShape<SHAPE, PARTS>;
+  constexpr int TILE = S::TILE, FM = S::kOutM, FN = S::kFN;
   constexpr int kRoom = store_room<FM, FN>();
   constexpr int kNeed = kRoom * S::kWaves > S::kHalves ? kRoom * S::kWaves : S::kHalves;
   __shared__ __align__(16) _Float16 lds[kNeed];
@@ -590,10 +627,6 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
   const int rows = d.mp, cols = kTurned ? d.np : d.mp;
   const int p_rows = rows - i0 < TILE ? rows - i0 : TILE, q_rows = cols - j0 < TILE ? cols - j0 : TILE;
   f32x4 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = 0.0f;
   if constexpr (kTurned) {
     multiply<S, true>(mem + d.sq[a.in] + (int64_t)i0 * d.mp, mm, p_rows, d.mp, mem + d.x[a.from] + j0, mn, q_rows, d.np,
                       d.mp / S::kDepth, lds, acc);
@@ -610,7 +643,8 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
   }
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = i0 + wave / S::kWN * S::kRowsM, col0 = j0 + wave % S::kWN * S::kRowsN;
+  const int wave2 = wave % (S::kWM * S::kWN), group = wave / (S::kWM * S::kWN);
+  const int row0 = i0 + wave2 / S::kWN * S::kRowsM + group * (FM * 16), col0 = j0 + wave2 % S::kWN * S::kRowsN;
   _Float16* room = lds + wave * kRoom;
   if constexpr (MODE == kGram) {
     if (t.shares > 1) {  // the sums of this share, for k_mat_join
@@ -629,19 +663,19 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
     const float by = d.scale * (1.0f / (kOperandScale * kOperandScale));
     const int size = f.type == kTypeF32 ? 4 : 2;
     const bool wide = length % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * size) % (4 * size) == 0;
-    constexpr int CC = FN * 16;
+    constexpr int CC = FN * 16, HM = FM > 1 ? 2 : 1, HR = HM * 16;  // rows at a time
     float* fl = reinterpret_cast<float*>(room);
 #pragma unroll
-    for (int h = 0; h < FM; h += 2) {
+    for (int h = 0; h < FM; h += HM) {
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < HM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
           const f32x4 v = acc[h + i][j] * by;
           if (d.tall) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) fl[(j * 16 + (lane >> 4) * 4 + e) * 36 + i * 16 + (lane & 15)] = v[e];
+            for (int e = 0; e < 4; ++e) fl[(j * 16 + (lane >> 4) * 4 + e) * (HR + 4) + i * 16 + (lane & 15)] = v[e];
           } else {
             *reinterpret_cast<f32x4*>(fl + (i * 16 + (lane & 15)) * (CC + 4) + j * 16 + (lane >> 4) * 4) = v;
           }
@@ -649,10 +683,10 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
       const int line0 = d.tall ? col0 : row0 + h * 16, place0 = d.tall ? row0 + h * 16 : col0;
-      const int run = d.tall ? 32 : CC, pitch = run + 4;
+      const int run = d.tall ? HR : CC, pitch = run + 4;
       if (wide) {
 #pragma unroll 4
-        for (int u = lane; u < 32 * CC / 4; u += 64) {
+        for (int u = lane; u < HR * CC / 4; u += 64) {
           const int r = u / (run / 4), c = u % (run / 4) * 4;
           if (line0 + r < lines && place0 + c < length) {
             const f32x4 x = *reinterpret_cast<const f32x4*>(fl + r * pitch + c);
@@ -662,7 +696,7 @@ __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads), (ProductShap
         }
       } else {
 #pragma unroll 4
-        for (int u = lane; u < 32 * CC; u += 64) {
+        for (int u = lane; u < HR * CC; u += 64) {
           const int r = u / run, c = u % run;
           if (line0 + r < lines && place0 + c < length) {
             const float v[1] = {fl[r * pitch + c]};
@@ -880,38 +914,35 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
 #endif
 }
 
-// Adds the shares of a Gram matrix's tiles in their order and stores the tile, a quarter of each wave's fragments a block.
+// Adds the shares of a Gram matrix's tiles in their order and stores the tile, half of each wave's fragments a block.
 // (The blocks of the product cannot do it themselves, the last one of a tile: that takes a write-back of a die's whole cache
 // by every block before it says that it is through.  480 blocks of 128 x 128 sums took 150 us so, 20 in two launches.)
 template <int TILE, int PARTS>
 __global__ __launch_bounds__((ProductShape<TILE, PARTS>::kThreads)) void k_mat_join(
-    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem,
-    const float* __restrict__ partial) {
+    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, const float* __restrict__ partial) {
   using S = ProductShape<TILE, PARTS>;
-  constexpr int FM = S::kFM, FN = S::kFN;
-  constexpr int QM = FM / 2, QN = FN / 2;
-  constexpr int kRoom = store_room<QM, QN>();
+  constexpr int FM = S::kOutM, FN = S::kFN, QN = FN / 2;
+  constexpr int kRoom = store_room<FM, QN>();
   __shared__ __align__(16) _Float16 lds[kRoom * S::kWaves];
   const MatTile& t = tiles[blockIdx.x];
   const MatDesc& d = t.d;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int qi = (blockIdx.y >> 1) * QM, qj = (blockIdx.y & 1) * QN;
-  const int row0 = t.i * TILE + wave / S::kWN * S::kRowsM + qi * 16;
-  const int col0 = t.j * TILE + wave % S::kWN * S::kRowsN + qj * 16;
+  const int wave2 = wave % (S::kWM * S::kWN), group = wave / (S::kWM * S::kWN), qj = blockIdx.y * QN;
+  const int row0 = t.i * TILE + wave2 / S::kWN * S::kRowsM + group * (FM * 16);
+  const int col0 = t.j * TILE + wave2 % S::kWN * S::kRowsN + qj * 16;
   const f32x4* all = reinterpret_cast<const f32x4*>(partial + (int64_t)t.slot * (TILE * TILE)) + threadIdx.x;
-  f32x4 sum[QM][QN];
+  f32x4 sum[FM][QN];
 #pragma unroll
-  for (int i = 0; i < QM; ++i)
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < QN; ++j) sum[i][j] = all[((qi + i) * FN + qj + j) * S::kThreads];
+    for (int j = 0; j < QN; ++j) sum[i][j] = all[(i * FN + qj + j) * S::kThreads];
   for (int s = 1; s < t.shares; ++s)
 #pragma unroll
-    for (int i = 0; i < QM; ++i)
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < QN; ++j)
-        sum[i][j] += all[(int64_t)s * (TILE * TILE / 4) + ((qi + i) * FN + qj + j) * S::kThreads];
+      for (int j = 0; j < QN; ++j) sum[i][j] += all[(int64_t)s * (TILE * TILE / 4) + (i * FN + qj + j) * S::kThreads];
   auto value = [&](int i, int j) { return sum[i][j] * (1.0f / kOperandScale); };
-  store_halves<QM, QN, PARTS>(value, lds + wave * kRoom, row0, col0, d.mp, d.mp, mem + d.sq[0], d.mp, mem + d.sq[0], d.mp,
+  store_halves<FM, QN, PARTS>(value, lds + wave * kRoom, row0, col0, d.mp, d.mp, mem + d.sq[0], d.mp, mem + d.sq[0], d.mp,
                               (int64_t)d.mp * d.mp, t.i != t.j);
 }
 
