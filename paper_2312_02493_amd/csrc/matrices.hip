@@ -63,28 +63,28 @@ struct TileCost {
   double fixed, alone, store, among;
   int slots;  // blocks that the chip holds
 };
-constexpr TileCost kNever = {1e9, 1e9, 1e9, 1e9, 256};  // (one part is fed as fast without)
+constexpr TileCost kNever = {1e9, 1e9, 1e9, 1e9, 256};  // (one part is fed as fast without, and Q X has two stages)
 constexpr TileCost kCost[2][2][kTileClasses] = {  // [Q X][two parts]
     {{{3.0, 0.20, 0.0043, 0.00083, 512},
       {4.0, 0.63, 0.0258, 0.0017, 512},
       {5.0, 0.84, 0.0325, 0.0044, 256},
       {6.0, 1.28, 0.0890, 0.00575, 256},
       kNever},
-     {{3.0, 0.60, 0.0050, 0.0019, 512},
+     {{3.0, 0.60, 0.0110, 0.0018, 512},
       {4.0, 1.60, 0.0470, 0.0047, 512},
       {5.0, 1.93, 0.0820, 0.0100, 256},
       {6.0, 3.80, 0.1890, 0.0160, 256},
-      {3.0, 0.38, 0.0060, 0.0019, 256}}},
-    {{{3.0, 0.25, 0.0067, 0.00112, 512},
-      {4.0, 0.65, 0.0200, 0.0018, 512},
-      {5.0, 0.90, 0.0300, 0.0049, 256},
-      {6.0, 1.28, 0.0800, 0.0054, 256},
+      {3.0, 0.38, 0.0110, 0.0018, 256}}},
+    {{{3.0, 0.25, 0.0020, 0.00085, 1024},
+      {4.0, 0.65, 0.0155, 0.00186, 512},
+      {5.0, 0.90, 0.0330, 0.0049, 256},
+      {6.0, 1.28, 0.0600, 0.0060, 256},
       kNever},
-     {{3.0, 0.60, 0.0057, 0.00183, 512},
-      {4.0, 1.60, 0.0350, 0.0047, 512},
-      {5.0, 2.20, 0.0900, 0.0106, 256},
-      {6.0, 3.80, 0.1600, 0.0172, 256},
-      {3.0, 0.40, 0.0090, 0.0027, 256}}}};
+     {{3.0, 0.55, 0.0080, 0.0017, 512},
+      {4.0, 1.60, 0.0400, 0.0047, 512},
+      {5.0, 2.20, 0.0920, 0.0117, 256},
+      {6.0, 3.60, 0.1100, 0.0168, 256},
+      kNever}}};
 // Shares that meet in memory: a launch, the shares of one tile one after the other, and their bytes (36 tiles of 64 x 64 in 9
 // shares each 4.6, 10 of 128 x 128 in 18 9.1, one of 64 x 64 in 32 11.1).
 constexpr double kJoinLaunch = 3.5, kJoinShare = 0.22, kJoinBytes = 1.0 / 2.5e6;

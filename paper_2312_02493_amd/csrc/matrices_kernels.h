@@ -228,28 +228,51 @@ struct FinishArgs {
   MuonArgs a;
 };
 
-template <int N, class T>
-__device__ __forceinline__ void finish_as(T* p, const FinishArgs& f, const float (&scaled)[N]) {
-  struct alignas(N * sizeof(T)) Some {
-    T e[N];
-  };
-  Some v;
-  if (f.muon) v = *reinterpret_cast<const Some*>(p);
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    v.e[e] = static_cast<T>(f.muon ? fmaf(-f.a.eta, scaled[e], static_cast<float>(v.e[e]) * f.a.decay_by) : scaled[e]);
-  *reinterpret_cast<Some*>(p) = v;
+__device__ __forceinline__ float updated(const FinishArgs& f, float weight, float scaled) {
+  return fmaf(-f.a.eta, scaled, weight * f.a.decay_by);
 }
 
-// N elements side by side, at a place aligned to all of them.
-template <int N>
-__device__ __forceinline__ void finish(const FinishArgs& f, int64_t i, const float (&scaled)[N]) {
+template <class T>
+__device__ __forceinline__ void finish_one(T* p, const FinishArgs& f, float scaled) {
+  *p = static_cast<T>(f.muon ? updated(f, static_cast<float>(*p), scaled) : scaled);
+}
+
+__device__ __forceinline__ void finish(const FinishArgs& f, int64_t i, float scaled) {
   if (f.type == kTypeF32)
-    finish_as<N>(static_cast<float*>(f.out) + i, f, scaled);
+    finish_one(static_cast<float*>(f.out) + i, f, scaled);
   else if (f.type == kTypeBf16)
-    finish_as<N>(static_cast<__bf16*>(f.out) + i, f, scaled);
+    finish_one(static_cast<__bf16*>(f.out) + i, f, scaled);
   else
-    finish_as<N>(static_cast<_Float16*>(f.out) + i, f, scaled);
+    finish_one(static_cast<_Float16*>(f.out) + i, f, scaled);
+}
+
+// Four elements side by side, at a place aligned to all of them.
+template <class T>
+struct alignas(4 * sizeof(T)) Four {
+  T e[4];
+};
+template <class T>
+__device__ __forceinline__ float4 read_four_of(const T* p) {
+  const Four<T> v = *reinterpret_cast<const Four<T>*>(p);
+  return float4{static_cast<float>(v.e[0]), static_cast<float>(v.e[1]), static_cast<float>(v.e[2]), static_cast<float>(v.e[3])};
+}
+template <class T>
+__device__ __forceinline__ void write_four_of(T* p, const float (&v)[4]) {
+  const Four<T> o = {{static_cast<T>(v[0]), static_cast<T>(v[1]), static_cast<T>(v[2]), static_cast<T>(v[3])}};
+  *reinterpret_cast<Four<T>*>(p) = o;
+}
+__device__ __forceinline__ float4 read_four(const FinishArgs& f, int64_t i) {
+  if (f.type == kTypeF32) return read_four_of(static_cast<const float*>(f.out) + i);
+  if (f.type == kTypeBf16) return read_four_of(static_cast<const __bf16*>(f.out) + i);
+  return read_four_of(static_cast<const _Float16*>(f.out) + i);
+}
+__device__ __forceinline__ void write_four(const FinishArgs& f, int64_t i, const float (&v)[4]) {
+  if (f.type == kTypeF32)
+    write_four_of(static_cast<float*>(f.out) + i, v);
+  else if (f.type == kTypeBf16)
+    write_four_of(static_cast<__bf16*>(f.out) + i, v);
+  else
+    write_four_of(static_cast<_Float16*>(f.out) + i, v);
 }
 
 // No step at all: the scaled matrix itself.
@@ -263,8 +286,7 @@ __global__ __launch_bounds__(256) void k_mat_scaled(From from, const MatDesc* __
   const MatDesc d = mats[c.mat];
   const double by = inverse_norm(d, sums, eps, room);
   for (int64_t i = c.begin + threadIdx.x; i < c.end; i += 256) {
-    const float v[1] = {normalised(from(i), by) * d.scale};
-    finish<1>(f, i, v);
+    finish(f, i, normalised(from(i), by) * d.scale);
   }
 }
 
@@ -393,21 +415,34 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
     }
   };
   constexpr int KS = S::kDepth / 32 / S::kGroups;  // of a group
-  constexpr int SETS = S::kAhead ? 2 : 1;
-  half8 fp[SETS][PARTS][S::kFM], fq[SETS][PARTS][S::kFN];
+  constexpr int N = TURNED ? 2 : S::kStages;
+  constexpr int SETS = S::kAhead ? 2 : 1, Q_SETS = TURNED && KS == 2 ? 3 : SETS;
+  half8 fp[SETS][PARTS][S::kFM], fq[Q_SETS][PARTS][S::kFN];
   // (of a turned operand a lane names four columns of one row and is given four rows of one column: in each sixteen lanes,
   // lane i names row i / 4 and columns 4 (i % 4) .. and is given rows 0 .. 3 of column i)
   const int tr = (lane >> 4) * 8 + ((lane & 15) >> 2);
   const int flip = turned_flip<TILE>(tr);  // the same for r + 4 and r + 32
-  auto read = [&](int stage, int ks, int to) {
-    ks += group * KS;
-    const _Float16* here = lds + stage * S::kStage;
-    const int c = ks * 4 + (lane >> 4);
+  // (a stage's place is worked out anew for every read: all of them at hand would fill the registers)
+  auto stage_at = [&](int stage) {
+    int at = stage * S::kStage;
+    asm volatile("" : "+s"(at));
+    return lds + at;
+  };
+  auto read_p = [&](int stage, int ks, int to) {
+    const _Float16* here = stage_at(stage);
+    const int c = (ks + group * KS) * 4 + (lane >> 4);
 #pragma unroll
-    for (int s = 0; s < PARTS; ++s) {
+    for (int s = 0; s < PARTS; ++s)
 #pragma unroll
       for (int i = 0; i < S::kFM; ++i)
         fp[to][s][i] = *reinterpret_cast<const half8*>(here + s * S::kPlane + stage_place<S::kChunks>(wi + i * 16 + (lane & 15), c));
+  };
+  auto read_q = [&](int stage, int ks, int to) {
+    ks += group * KS;
+    const _Float16* here = stage_at(stage);
+    const int c = ks * 4 + (lane >> 4);
+#pragma unroll
+    for (int s = 0; s < PARTS; ++s)
 #pragma unroll
       for (int j = 0; j < S::kFN; ++j) {
         const _Float16* at = here + (PARTS + s) * S::kPlane;
@@ -421,7 +456,6 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
           fq[to][s][j] = *reinterpret_cast<const half8*>(at + stage_place<S::kChunks>(wj + j * 16 + (lane & 15), c));
         }
       }
-    }
   };
   f32x4 acc[S::kFM][S::kFN];
 #pragma unroll
@@ -434,72 +468,91 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
 #pragma unroll
     for (int j = 0; j < (S::kLow ? S::kFN : 1); ++j) low[i][j] = 0.0f;
   // The second operand goes first: so a lane is given four columns of one row side by side.
-  auto mul = [&](int of) {
+  auto mul = [&](int of, int q_of) {
 #pragma unroll
     for (int i = 0; i < S::kFM; ++i)
 #pragma unroll
       for (int j = 0; j < S::kFN; ++j) {
         if constexpr (PARTS == 2) {
           f32x4& to = S::kLow ? low[i][j] : acc[i][j];
-          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[of][0][j], fp[of][PARTS - 1][i], to, 0, 0, 0);
-          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[of][PARTS - 1][j], fp[of][0][i], to, 0, 0, 0);
+          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][0][j], fp[of][PARTS - 1][i], to, 0, 0, 0);
+          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][PARTS - 1][j], fp[of][0][i], to, 0, 0, 0);
         }
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[of][0][j], fp[of][0][i], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][0][j], fp[of][0][i], acc[i][j], 0, 0, 0);
       }
   };
-  constexpr int N = S::kStages;
-#pragma unroll
-  for (int s = 0; s < (S::kAhead ? N : N - 1); ++s) fetch(s, s);
+  // A turned operand is read before the next stage is asked for, both halves of it where a stage has two: the compiler lets no
+  // such read pass a load to LDS that is on its way, whatever stage it is for.  (So two stages do for it.)
   int st = 0;
+  auto ask_and_read = [&](int k, int next, int to, int q_to, int q_to2) {
+    wait_loads<(N - 2) * S::kLoads>();  // the next stage is there, and this one read whole
+    block_barrier();
+    if constexpr (!TURNED) fetch(k + N, st);
+    read_p(next, 0, to);
+    read_q(next, 0, q_to);
+    if constexpr (TURNED) {
+      if constexpr (KS == 2) read_q(next, 1, q_to2);
+      fetch(k + N, st);
+    }
+    st = next;
+  };
+  auto after = [&](int of) { return of + 1 == N ? 0 : of + 1; };
   if constexpr (S::kAhead) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) fetch(s, s);
     wait_loads<(N - 1) * S::kLoads>();
     block_barrier();
-    read(0, 0, 0);
-    auto stage = [&](int k, int base, bool more) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int now = (base + ks) & 1;
-        if (ks + 1 < KS) {
-          read(st, ks + 1, now ^ 1);
-        } else if (more) {
-          const int next = st + 1 == N ? 0 : st + 1;
-          wait_loads<(N - 2) * S::kLoads>();  // the next stage is there, and this one read whole
-          block_barrier();
-          fetch(k + N, st);
-          read(next, 0, now ^ 1);
-          st = next;
-        }
-        mul(now);
+    read_p(0, 0, 0);
+    read_q(0, 0, 0);
+    if constexpr (TURNED && KS == 2) read_q(0, 1, 1);
+    auto stage = [&](int k, int odd, bool more) {
+      if constexpr (KS == 2) {
+        read_p(st, 1, 1);
+        if constexpr (!TURNED) read_q(st, 1, 1);
+        mul(0, 0);
         __builtin_amdgcn_sched_barrier(0);  // (or the reads sink to their uses)
+        if (more) ask_and_read(k, after(st), 0, 0, 2);
+        mul(1, 1);
+        if constexpr (TURNED) {
+          if (more)
+#pragma unroll
+            for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+              for (int j = 0; j < S::kFN; ++j) fq[1][s][j] = fq[Q_SETS - 1][s][j];
+        }
+      } else {
+        if (more) ask_and_read(k, after(st), odd ^ 1, odd ^ 1, 0);
+        mul(odd, odd);
       }
+      __builtin_amdgcn_sched_barrier(0);
     };
-    if constexpr (KS % 2 == 0) {
-      for (int k = 0; k + 1 < steps; ++k) stage(k, 0, true);
-      stage(steps - 1, 0, false);
+    int k = 0;
+    if constexpr (KS == 2) {
+      for (; k + 1 < steps; ++k) stage(k, 0, true);
     } else {
-      int k = 0;
       for (; k + 2 < steps; k += 2) {
         stage(k, 0, true);
         stage(k + 1, 1, true);
       }
-      if (steps - k == 2) {
-        stage(k, 0, true);
-        stage(k + 1, 1, false);
-      } else {
-        stage(k, 0, false);
-      }
+    }
+    if (KS == 1 && steps - k == 2) {
+      stage(k, 0, true);
+      stage(k + 1, 1, false);
+    } else {
+      stage(k, 0, false);
     }
   } else {
+    static_assert(N == 2 && KS == 1, "");
+    fetch(0, 0);
     for (int k = 0; k < steps; ++k) {
-      wait_loads<(N - 2) * S::kLoads>();
+      wait_loads<0>();
       block_barrier();
-      fetch(k + N - 1, st == 0 ? N - 1 : st - 1);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        read(st, ks, 0);
-        mul(0);
-      }
-      st = st + 1 == N ? 0 : st + 1;
+      if constexpr (!TURNED) fetch(k + 1, st ^ 1);
+      read_p(st, 0, 0);
+      read_q(st, 0, 0);
+      if constexpr (TURNED) fetch(k + 1, st ^ 1);
+      mul(0, 0);
+      st ^= 1;
     }
   }
   if constexpr (S::kLow)
@@ -610,13 +663,82 @@ constexpr int store_room() {
   return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
+// The same for the caller's buffer, as floats: out = scale X, or the weights' update, whose old values are asked for before the
+// sums pass through LDS (asked for one by one where they are needed, 78.6 M bf16 weights took 324 us instead of KFIN).
+template <int FM, int FN, bool TALL>
+__device__ __forceinline__ void finish_rows(const f32x4 (&acc)[FM][FN], float* fl, int row0, int col0, const MatDesc& d,
+                                            const FinishArgs& f) {
+  const int lane = threadIdx.x & 63;
+  constexpr int CC = FN * 16, HM = FM > 1 ? 2 : 1, HR = HM * 16;  // rows at a time
+  constexpr int RUN = TALL ? HR : CC, PITCH = RUN + 4;            // as they lie
+  constexpr int EACH = HR * CC / 4 / 64;                          // fours of a lane
+  const int lines = TALL ? d.n : d.m, length = TALL ? d.m : d.n;
+  const float by = d.scale * (1.0f / (kOperandScale * kOperandScale));
+  const int size = f.type == kTypeF32 ? 4 : 2;
+  const bool wide = length % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * size) % (4 * size) == 0;
+#pragma unroll
+  for (int h = 0; h < FM; h += HM) {
+    const int line0 = TALL ? col0 : row0 + h * 16, place0 = TALL ? row0 + h * 16 : col0;
+    int64_t at[EACH];
+    float4 old[EACH];
+    if (wide) {
+#pragma unroll
+      for (int u = 0; u < EACH; ++u) {
+        const int r = (u * 64 + lane) / (RUN / 4), c = (u * 64 + lane) % (RUN / 4) * 4;
+        const bool there = line0 + r < lines && place0 + c < length;
+        at[u] = there ? d.at + (int64_t)(line0 + r) * length + place0 + c : -1;
+        if (f.muon && there) old[u] = read_four(f, at[u]);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < HM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const f32x4 v = acc[h + i][j] * by;
+        if constexpr (TALL) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) fl[(j * 16 + (lane >> 4) * 4 + e) * PITCH + i * 16 + (lane & 15)] = v[e];
+        } else {
+          *reinterpret_cast<f32x4*>(fl + (i * 16 + (lane & 15)) * PITCH + j * 16 + (lane >> 4) * 4) = v;
+        }
+      }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    if (wide) {
+#pragma unroll
+      for (int u = 0; u < EACH; ++u) {
+        const int r = (u * 64 + lane) / (RUN / 4), c = (u * 64 + lane) % (RUN / 4) * 4;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(fl + r * PITCH + c);
+        float v[4] = {x[0], x[1], x[2], x[3]};
+        if (f.muon) {
+          const float w[4] = {old[u].x, old[u].y, old[u].z, old[u].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = updated(f, w[e], v[e]);
+        }
+        if (at[u] >= 0) write_four(f, at[u], v);
+      }
+    } else {
+#pragma unroll 4
+      for (int u = lane; u < HR * CC; u += 64) {
+        const int r = u / RUN, c = u % RUN;
+        if (line0 + r < lines && place0 + c < length) {
+          finish(f, d.at + (int64_t)(line0 + r) * length + place0 + c, fl[r * PITCH + c]);
+        }
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
 template <int SHAPE, int PARTS, int MODE>
 __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductShape<SHAPE, PARTS>::kBlocks)) void k_mat_product(
     const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, ProductArgs a, FinishArgs f, float* __restrict__ partial) {
   using S = ProductShape<SHAPE, PARTS>;
   constexpr int TILE = S::TILE, FM = S::kOutM, FN = S::kFN;
   constexpr int kRoom = store_room<FM, FN>();
-  constexpr int kNeed = kRoom * S::kWaves > S::kHalves ? kRoom * S::kWaves : S::kHalves;
+  constexpr int kStaged = MODE == kApply || MODE == kFinal ? 2 * S::kStage : S::kHalves;
+  constexpr int kNeed = kRoom * S::kWaves > kStaged ? kRoom * S::kWaves : kStaged;
   __shared__ __align__(16) _Float16 lds[kNeed];
 
   const MatTile& t = tiles[blockIdx.x];
@@ -657,55 +779,12 @@ __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductSha
     }
   }
   if constexpr (MODE == kFinal) {
-    // Elements of a tall matrix lie column by column of X.  32 rows of the wave's part at a time go through LDS as floats,
-    // in the order in which they lie.
-    const int lines = d.tall ? d.n : d.m, length = d.tall ? d.m : d.n;
-    const float by = d.scale * (1.0f / (kOperandScale * kOperandScale));
-    const int size = f.type == kTypeF32 ? 4 : 2;
-    const bool wide = length % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * size) % (4 * size) == 0;
-    constexpr int CC = FN * 16, HM = FM > 1 ? 2 : 1, HR = HM * 16;  // rows at a time
-    float* fl = reinterpret_cast<float*>(room);
-#pragma unroll
-    for (int h = 0; h < FM; h += HM) {
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int i = 0; i < HM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const f32x4 v = acc[h + i][j] * by;
-          if (d.tall) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) fl[(j * 16 + (lane >> 4) * 4 + e) * (HR + 4) + i * 16 + (lane & 15)] = v[e];
-          } else {
-            *reinterpret_cast<f32x4*>(fl + (i * 16 + (lane & 15)) * (CC + 4) + j * 16 + (lane >> 4) * 4) = v;
-          }
-        }
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_wave_barrier();
-      const int line0 = d.tall ? col0 : row0 + h * 16, place0 = d.tall ? row0 + h * 16 : col0;
-      const int run = d.tall ? HR : CC, pitch = run + 4;
-      if (wide) {
-#pragma unroll 4
-        for (int u = lane; u < HR * CC / 4; u += 64) {
-          const int r = u / (run / 4), c = u % (run / 4) * 4;
-          if (line0 + r < lines && place0 + c < length) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(fl + r * pitch + c);
-            const float v[4] = {x[0], x[1], x[2], x[3]};
-            finish<4>(f, d.at + (int64_t)(line0 + r) * length + place0 + c, v);
-          }
-        }
-      } else {
-#pragma unroll 4
-        for (int u = lane; u < HR * CC; u += 64) {
-          const int r = u / run, c = u % run;
-          if (line0 + r < lines && place0 + c < length) {
-            const float v[1] = {fl[r * pitch + c]};
-            finish<1>(f, d.at + (int64_t)(line0 + r) * length + place0 + c, v);
-          }
-        }
-      }
-      asm volatile("" ::: "memory");
-    }
+    // Elements of a tall matrix lie column by column of X.  A few rows of the wave's part at a time go through LDS as floats, in
+    // the order in which they lie.
+    if (d.tall)
+      finish_rows<FM, FN, true>(acc, reinterpret_cast<float*>(room), row0, col0, d, f);
+    else
+      finish_rows<FM, FN, false>(acc, reinterpret_cast<float*>(room), row0, col0, d, f);
   } else if constexpr (MODE == kSquare) {
     auto value = [&](int i, int j) {
       const int row = row0 + i * 16 + (lane & 15), col = col0 + j * 16 + (lane >> 4) * 4;
@@ -894,7 +973,8 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
     __syncthreads();
   }
   if (!has_x) return;
-  const bool wide = !d.tall && d.n % 4 == 0 && f.type == kTypeF32 && (reinterpret_cast<uintptr_t>(f.out) + d.at * 4) % 16 == 0;
+  const int size4 = f.type == kTypeF32 ? 16 : 8;
+  const bool wide = !d.tall && d.n % 4 == 0 && (reinterpret_cast<uintptr_t>(f.out) + d.at * (size4 / 4)) % size4 == 0;
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
     const int row = xi * 32 + (x & 1) * 16 + l15, col = xj * 32 + (x >> 1) * 16 + l4 * 4;
@@ -902,12 +982,17 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
     const float w[4] = {v[x >> 1][x & 1][0] * by, v[x >> 1][x & 1][1] * by, v[x >> 1][x & 1][2] * by, v[x >> 1][x & 1][3] * by};
     if (row >= d.m || col >= d.n) continue;
     if (wide) {
-      finish_as<4>(static_cast<float*>(f.out) + d.at + (int64_t)row * d.n + col, f, w);
+      const int64_t at = d.at + (int64_t)row * d.n + col;
+      float o[4] = {w[0], w[1], w[2], w[3]};
+      if (f.muon) {
+        const float4 old = read_four(f, at);
+        o[0] = updated(f, old.x, w[0]), o[1] = updated(f, old.y, w[1]), o[2] = updated(f, old.z, w[2]), o[3] = updated(f, old.w, w[3]);
+      }
+      write_four(f, at, o);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float one[1] = {w[e]};
-        if (col + e < d.n) finish<1>(f, d.at + (d.tall ? (int64_t)(col + e) * d.m + row : (int64_t)row * d.n + col + e), one);
+        if (col + e < d.n) finish(f, d.at + (d.tall ? (int64_t)(col + e) * d.m + row : (int64_t)row * d.n + col + e), w[e]);
       }
     }
   }
