@@ -377,47 +377,42 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
   const int lc = S::kChunks == 8 ? (lane % 8) ^ (lr & 7) : (lane % 4) ^ ((lr >> 1) & 3);
   constexpr int G = TILE / S::kLoadRows;    // loads of one operand's part
   constexpr int EACH = S::kLoads / 2;       // a wave's loads of one operand
-  int p_off[EACH], q_off[EACH];             // bytes from the stage's first element
+  static_assert(S::kLoadRows % (S::kChunks == 8 ? 8 : 16) == 0, "every load's rows lie alike");
+  const int p_off = (lr * ld + lc * 8) * 2, q_off = (lr * q_ld + lc * 8) * 2;  // bytes from a load's first row
+  int turned_off[TURNED ? EACH : 1];                                          // of a turned operand from the stage's
+  if constexpr (TURNED)
 #pragma unroll
-  for (int l = 0; l < EACH; ++l) {
-    const int g = (l * S::kWaves + wave) % G;
-    p_off[l] = ((g * S::kLoadRows + lr) * ld + lc * 8) * 2;
-    if constexpr (TURNED) {
-      const int at = g * 64 + lane, r = at / (TILE / 8);
-      q_off[l] = (r * q_ld + ((at % (TILE / 8)) ^ (turned_flip<TILE>(r) << 1)) * 8) * 2;
-    } else {
-      q_off[l] = ((g * S::kLoadRows + lr) * q_ld + lc * 8) * 2;
+    for (int l = 0; l < EACH; ++l) {
+      const int at = (l * S::kWaves + wave) % G * 64 + lane, r = at / (TILE / 8);
+      turned_off[l] = (r * q_ld + ((at % (TILE / 8)) ^ (turned_flip<TILE>(r) << 1)) * 8) * 2;
     }
-  }
-  auto fetch = [&](int k, int stage) {
+  // one of a wave's loads for stage k, to place `stage`: EACH of P, then EACH of Q
+  auto fetch_one = [&](int k, int stage, int piece) {
     const int there = k < steps ? -1 : 0;
-#pragma unroll
-    for (int l = 0; l < EACH; ++l) {
-      const int u = l * S::kWaves + wave, s = PARTS == 1 ? 0 : u / G;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(p + s * p_plane), 0, (p_rows * ld * 2) & there, 0x00027000),
-          (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + u * 512), 16, p_off[l] + k * (S::kDepth * 2), 0, 0, 0);
+    const bool is_q = piece >= EACH;
+    const int l = is_q ? piece - EACH : piece;
+    const int u = l * S::kWaves + wave, s = PARTS == 1 ? 0 : u / G;
+    const _Float16* base = is_q ? q + s * q_plane : p + s * p_plane;
+    int bytes = is_q ? q_rows * q_ld * 2 : p_rows * ld * 2;
+    int off = (is_q ? q_off : p_off) + (u % G * (S::kLoadRows * 2) * (is_q ? q_ld : ld) + k * (S::kDepth * 2));
+    if (TURNED && is_q) {
+      base += (int64_t)k * S::kDepth * q_ld;
+      bytes = ((S::kDepth - 1) * q_ld + q_rows) * 2;  // from the stage's first row to the last one's end
+      off = turned_off[TURNED ? l : 0];
     }
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(base), 0, bytes & there, 0x00027000),
+        (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + (is_q ? PARTS * S::kPlane : 0) + u * 512), 16,
+        off, 0, 0, 0);
+  };
+  auto fetch = [&](int k, int stage) {
 #pragma unroll
-    for (int l = 0; l < EACH; ++l) {
-      const int u = l * S::kWaves + wave, s = PARTS == 1 ? 0 : u / G;
-      const _Float16* base = q + s * q_plane;
-      int bytes = q_rows * q_ld * 2, more = k * (S::kDepth * 2);
-      if constexpr (TURNED) {
-        base += (int64_t)k * S::kDepth * q_ld;
-        bytes = ((S::kDepth - 1) * q_ld + q_rows) * 2;  // from the stage's first row to the last one's end
-        more = 0;
-      }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16*>(base), 0, bytes & there, 0x00027000),
-          (__attribute__((address_space(3))) void*)(lds + stage * S::kStage + PARTS * S::kPlane + u * 512), 16, q_off[l] + more, 0,
-          0, 0);
-    }
+    for (int i = 0; i < 2 * EACH; ++i) fetch_one(k, stage, i);
   };
   constexpr int KS = S::kDepth / 32 / S::kGroups;  // of a group
   constexpr int N = TURNED ? 2 : S::kStages;
   constexpr int SETS = S::kAhead ? 2 : 1, Q_SETS = TURNED && KS == 2 ? 3 : SETS;
-  half8 fp[SETS][PARTS][S::kFM], fq[Q_SETS][PARTS][S::kFN];
+  half8 fp[PARTS][S::kFM], fq[Q_SETS][PARTS][S::kFN];
   // (of a turned operand a lane names four columns of one row and is given four rows of one column: in each sixteen lanes,
   // lane i names row i / 4 and columns 4 (i % 4) .. and is given rows 0 .. 3 of column i)
   const int tr = (lane >> 4) * 8 + ((lane & 15) >> 2);
@@ -428,34 +423,37 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
     asm volatile("" : "+s"(at));
     return lds + at;
   };
-  auto read_p = [&](int stage, int ks, int to) {
-    const _Float16* here = stage_at(stage);
+  auto read_p = [&](const _Float16* here, int ks, int i) {
     const int c = (ks + group * KS) * 4 + (lane >> 4);
 #pragma unroll
     for (int s = 0; s < PARTS; ++s)
-#pragma unroll
-      for (int i = 0; i < S::kFM; ++i)
-        fp[to][s][i] = *reinterpret_cast<const half8*>(here + s * S::kPlane + stage_place<S::kChunks>(wi + i * 16 + (lane & 15), c));
+      fp[s][i] = *reinterpret_cast<const half8*>(here + s * S::kPlane + stage_place<S::kChunks>(wi + i * 16 + (lane & 15), c));
   };
-  auto read_q = [&](int stage, int ks, int to) {
+  auto read_q = [&](const _Float16* here, int ks, int to, int j) {
     ks += group * KS;
-    const _Float16* here = stage_at(stage);
     const int c = ks * 4 + (lane >> 4);
 #pragma unroll
-    for (int s = 0; s < PARTS; ++s)
-#pragma unroll
-      for (int j = 0; j < S::kFN; ++j) {
-        const _Float16* at = here + (PARTS + s) * S::kPlane;
-        if constexpr (TURNED) {
-          typedef short short4v __attribute__((ext_vector_type(4)));
-          at += (ks * 32 + tr) * TILE + ((((wj >> 4) + j) ^ flip) << 4) + (lane & 3) * 4;
-          const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
-          const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at + 4 * TILE));
-          fq[to][s][j] = __builtin_shufflevector(__builtin_bit_cast(half4, a), __builtin_bit_cast(half4, b), 0, 1, 2, 3, 4, 5, 6, 7);
-        } else {
-          fq[to][s][j] = *reinterpret_cast<const half8*>(at + stage_place<S::kChunks>(wj + j * 16 + (lane & 15), c));
-        }
+    for (int s = 0; s < PARTS; ++s) {
+      const _Float16* at = here + (PARTS + s) * S::kPlane;
+      if constexpr (TURNED) {
+        typedef short short4v __attribute__((ext_vector_type(4)));
+        at += (ks * 32 + tr) * TILE + ((((wj >> 4) + j) ^ flip) << 4) + (lane & 3) * 4;
+        const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+        const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at + 4 * TILE));
+        fq[to][s][j] = __builtin_shufflevector(__builtin_bit_cast(half4, a), __builtin_bit_cast(half4, b), 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        fq[to][s][j] = *reinterpret_cast<const half8*>(at + stage_place<S::kChunks>(wj + j * 16 + (lane & 15), c));
       }
+    }
+  };
+  auto read_all = [&](int stage, int ks, int q_to, bool of_p, bool of_q) {
+    const _Float16* here = stage_at(stage);
+    if (of_p)
+#pragma unroll
+      for (int i = 0; i < S::kFM; ++i) read_p(here, ks, i);
+    if (of_q)
+#pragma unroll
+      for (int j = 0; j < S::kFN; ++j) read_q(here, ks, q_to, j);
   };
   f32x4 acc[S::kFM][S::kFN];
 #pragma unroll
@@ -468,51 +466,78 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
 #pragma unroll
     for (int j = 0; j < (S::kLow ? S::kFN : 1); ++j) low[i][j] = 0.0f;
   // The second operand goes first: so a lane is given four columns of one row side by side.
-  auto mul = [&](int of, int q_of) {
+  auto mul_row = [&](int i, int q_of) {
 #pragma unroll
-    for (int i = 0; i < S::kFM; ++i)
-#pragma unroll
-      for (int j = 0; j < S::kFN; ++j) {
-        if constexpr (PARTS == 2) {
-          f32x4& to = S::kLow ? low[i][j] : acc[i][j];
-          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][0][j], fp[of][PARTS - 1][i], to, 0, 0, 0);
-          to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][PARTS - 1][j], fp[of][0][i], to, 0, 0, 0);
-        }
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][0][j], fp[of][0][i], acc[i][j], 0, 0, 0);
+    for (int j = 0; j < S::kFN; ++j) {
+      if constexpr (PARTS == 2) {
+        f32x4& to = S::kLow ? low[i][j] : acc[i][j];
+        to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][0][j], fp[PARTS - 1][i], to, 0, 0, 0);
+        to = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][PARTS - 1][j], fp[0][i], to, 0, 0, 0);
       }
-  };
-  // A turned operand is read before the next stage is asked for, both halves of it where a stage has two: the compiler lets no
-  // such read pass a load to LDS that is on its way, whatever stage it is for.  (So two stages do for it.)
-  int st = 0;
-  auto ask_and_read = [&](int k, int next, int to, int q_to, int q_to2) {
-    wait_loads<(N - 2) * S::kLoads>();  // the next stage is there, and this one read whole
-    block_barrier();
-    if constexpr (!TURNED) fetch(k + N, st);
-    read_p(next, 0, to);
-    read_q(next, 0, q_to);
-    if constexpr (TURNED) {
-      if constexpr (KS == 2) read_q(next, 1, q_to2);
-      fetch(k + N, st);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[q_of][0][j], fp[0][i], acc[i][j], 0, 0, 0);
     }
-    st = next;
   };
+  // What is read and asked for stands between the rows of products, P's next fragment where the last row's was: with all of it
+  // in front, the waves' loads wait for each other while nothing multiplies (4096 x 4096, HALF, tiles of 256: X X^T 92 us, Q X
+  // 114, so 89 and 110; sixteen 1280 x 1280 and eight 1280 x 5120, SPLIT, tiles of 128: Q X 671, so 610; but X X^T of four
+  // 512 x 4608, HALF, tiles of 64, alone on their units, 16.2, so 17.6).
+  auto rows = [&](int q_of, auto&& between) {
+#pragma unroll
+    for (int i = 0; i < S::kFM; ++i) {
+      between(i);
+      mul_row(i, q_of);
+      __builtin_amdgcn_sched_barrier(0);  // (or the reads sink to their uses)
+    }
+    between(S::kFM);
+  };
+  constexpr int ROW_LOADS = (2 * EACH + S::kFM - 1) / S::kFM;  // of a row
+  constexpr int ROW_Q = (S::kFN + S::kFM - 1) / S::kFM;
+  int st = 0;
   auto after = [&](int of) { return of + 1 == N ? 0 : of + 1; };
   if constexpr (S::kAhead) {
 #pragma unroll
     for (int s = 0; s < N; ++s) fetch(s, s);
     wait_loads<(N - 1) * S::kLoads>();
     block_barrier();
-    read_p(0, 0, 0);
-    read_q(0, 0, 0);
-    if constexpr (TURNED && KS == 2) read_q(0, 1, 1);
+    read_all(0, 0, 0, true, true);
+    if constexpr (TURNED && KS == 2) read_all(0, 1, 1, false, true);
+    // the products with Q's set `q_of` beside which the next stage's first operands come, Q's to `q_to`, and the loads of stage
+    // k + N go out
+    auto last_of_stage = [&](int k, bool more, int q_of, int q_to) {
+      if (!more) return rows(q_of, [](int) {});
+      wait_loads<(N - 2) * S::kLoads>();  // the next stage is there, and this one read whole
+      block_barrier();
+      const int next = after(st), here = st;
+      // A turned operand is read before the next loads go out, both halves of it where a stage has two: the compiler lets no such
+      // read pass a load to LDS that is on its way, whatever stage it is for.  (So two stages do for it.)
+      if constexpr (TURNED) {
+        read_all(next, 0, q_to, false, true);
+        if constexpr (KS == 2) read_all(next, 1, 2, false, true);
+      }
+      st = next;
+      const _Float16* at = stage_at(next);
+      rows(q_of, [&](int i) {
+#pragma unroll
+        for (int l = i * ROW_LOADS; l < (i + 1) * ROW_LOADS; ++l)
+          if (l < 2 * EACH) fetch_one(k + N, here, l);
+        if (i > 0) read_p(at, 0, i - 1);
+        if constexpr (!TURNED)
+#pragma unroll
+          for (int j = i * ROW_Q; j < (i + 1) * ROW_Q; ++j)
+            if (j < S::kFN) read_q(at, 0, q_to, j);
+      });
+    };
     auto stage = [&](int k, int odd, bool more) {
       if constexpr (KS == 2) {
-        read_p(st, 1, 1);
-        if constexpr (!TURNED) read_q(st, 1, 1);
-        mul(0, 0);
-        __builtin_amdgcn_sched_barrier(0);  // (or the reads sink to their uses)
-        if (more) ask_and_read(k, after(st), 0, 0, 2);
-        mul(1, 1);
+        const _Float16* at = stage_at(st);
+        rows(0, [&](int i) {
+          if (i > 0) read_p(at, 1, i - 1);
+          if constexpr (!TURNED)
+#pragma unroll
+            for (int j = i * ROW_Q; j < (i + 1) * ROW_Q; ++j)
+              if (j < S::kFN) read_q(at, 1, 1, j);
+        });
+        last_of_stage(k, more, 1, 0);
         if constexpr (TURNED) {
           if (more)
 #pragma unroll
@@ -521,10 +546,8 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
               for (int j = 0; j < S::kFN; ++j) fq[1][s][j] = fq[Q_SETS - 1][s][j];
         }
       } else {
-        if (more) ask_and_read(k, after(st), odd ^ 1, odd ^ 1, 0);
-        mul(odd, odd);
+        last_of_stage(k, more, odd, odd ^ 1);
       }
-      __builtin_amdgcn_sched_barrier(0);
     };
     int k = 0;
     if constexpr (KS == 2) {
@@ -548,10 +571,10 @@ __device__ __forceinline__ void multiply(const _Float16* p, int64_t p_plane, int
       wait_loads<0>();
       block_barrier();
       if constexpr (!TURNED) fetch(k + 1, st ^ 1);
-      read_p(st, 0, 0);
-      read_q(st, 0, 0);
+      read_all(st, 0, 0, true, true);
       if constexpr (TURNED) fetch(k + 1, st ^ 1);
-      mul(0, 0);
+#pragma unroll
+      for (int i = 0; i < S::kFM; ++i) mul_row(i, 0);
       st ^= 1;
     }
   }
