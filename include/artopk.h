@@ -488,8 +488,12 @@ typedef struct artopk_matrix {
 typedef struct artopk_matrices artopk_matrices;
 
 /* How many bits the operands of the matrix products keep.  HALF: 11 (float16, scaled by powers of
- * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32. */
-enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1 };
+ * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32.
+ * DEFAULT: as many as the result shows.  Five steps leave a matrix some 1e-3 off with HALF (4e-3 of 16
+ * rows) and 1e-6 with SPLIT, so it takes SPLIT for float32 everywhere, and in artopk_orthogonalize for
+ * float16 and for bfloat16 where no matrix has more than 64 rows or columns (the fewer of the two); HALF
+ * otherwise, in artopk_muon_step for all 16-bit weights (their own rounding is coarser than the step's error). */
+enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1, ARTOPK_PRODUCTS_DEFAULT = -1 };
 
 #define ARTOPK_MAX_POLAR_STEPS 32
 
@@ -498,8 +502,8 @@ enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1 };
  * host array of `count` matrices (1 .. 65535), each within the vector, none overlapping another,
  * rows and cols in [1, 65536], scale finite; it is read before the call returns.  The iterates' memory
  * is allocated here: artopk_matrices_scratch_bytes(..) bytes, 4 for each element of a matrix and 6 for each of its
- * Gram matrix with HALF, of sides padded to whole tiles, and twice that with SPLIT (-1 for arguments that create
- * refuses).  The tables are copied
+ * Gram matrix with HALF, of sides padded to multiples of 64, twice that where an entry point takes SPLIT, and the tables
+ * (-1 for arguments that create refuses).  The tables are copied
  * to the device synchronously.  On failure *out is left alone and artopk_last_error(NULL) tells why.
  */
 int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int32_t count, int64_t n,

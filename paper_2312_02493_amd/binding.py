@@ -17,7 +17,7 @@ ARTOPK_STAR_COUNTER = 5
 ARTOPK_G_F32, ARTOPK_G_BF16, ARTOPK_G_F16 = 0, 1, 2
 ARTOPK_OPT_GUESS_MIN_N, ARTOPK_OPT_UPDATE_TILES_MIN_N, ARTOPK_OPT_LEADER_FIRST, ARTOPK_OPT_NONTEMPORAL = 0, 1, 2, 3
 ARTOPK_OPT_STAGE_TILES, ARTOPK_OPT_SHORT_MAX_N = 4, 5
-ARTOPK_PRODUCTS_HALF, ARTOPK_PRODUCTS_SPLIT = 0, 1
+ARTOPK_PRODUCTS_HALF, ARTOPK_PRODUCTS_SPLIT, ARTOPK_PRODUCTS_DEFAULT = 0, 1, -1
 PROF_NAMES = ("pass_a", "select", "gather", "update", "total")
 
 _SYMBOLS = (
@@ -405,17 +405,10 @@ def _matrix_table(matrices: Sequence):
 
 
 def artopk_matrices_scratch_bytes(matrices: Sequence, n: int, elem_type: int = ARTOPK_G_F32,
-                                  products: Optional[int] = None) -> int:
+                                  products: int = ARTOPK_PRODUCTS_DEFAULT) -> int:
     """Device bytes a MatrixContext of these arguments allocates (-1: refused); needs no GPU."""
     return int(load_library().artopk_matrices_scratch_bytes(_matrix_table(matrices), len(matrices), int(n),
-                                                            int(elem_type), _products(elem_type, products)))
-
-
-def _products(elem_type: int, products: Optional[int]) -> int:
-    """SPLIT for float32 elements, HALF for 16-bit ones (whose own rounding is as large), unless told."""
-    if products is not None:
-        return int(products)
-    return ARTOPK_PRODUCTS_SPLIT if elem_type == ARTOPK_G_F32 else ARTOPK_PRODUCTS_HALF
+                                                            int(elem_type), int(products)))
 
 
 class MatrixContext(_Handle):
@@ -423,11 +416,10 @@ class MatrixContext(_Handle):
 
     _name = "matrices"
 
-    def __init__(self, matrices: Sequence, n: int, elem_type: int = ARTOPK_G_F32, products: Optional[int] = None,
+    def __init__(self, matrices: Sequence, n: int, elem_type: int = ARTOPK_G_F32, products: int = ARTOPK_PRODUCTS_DEFAULT,
                  stream: Optional[int] = None):
         self.n, self.elem_type = int(n), int(elem_type)
-        self._open(stream, _matrix_table(matrices), len(matrices), self.n, self.elem_type,
-                   _products(self.elem_type, products))
+        self._open(stream, _matrix_table(matrices), len(matrices), self.n, self.elem_type, int(products))
 
     def _flat(self, t, name: str) -> Optional[int]:
         if t is not None and _elem_type(t) != self.elem_type:

@@ -49,8 +49,7 @@ struct MatPlan {
   bool small = false;  // every matrix on one compute unit, in one launch
   size_t small_lds = 0;
   int64_t slots = 0;   // partial sums of the Gram products' shares
-  // places in the slab
-  size_t o_mats = 0, o_chunks = 0, o_tiles = 0, o_sums = 0, o_partial = 0, o_mem = 0, total = 0;
+  int parts = 1;       // of an operand
 };
 
 // What a product's block costs, in us, by tile class: alone on its compute unit (`fixed` and `alone` for each 64 of the
@@ -166,7 +165,7 @@ double small_cost(const std::vector<MatDesc>& mats, int parts, size_t lds) {
 // The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
 // each die has a cache of its own: the tiles of all matrices with equally long sums are cut into eight runs of neighbours,
 // one for each die, and the longest sums come first.  (Every matrix cut into eight instead: Q X of sixteen 1280 x 1280
-// and eight 1280 x 5120 234 us, so KRUNS.)
+// and eight 1280 x 5120 234 us, so 228.)
 void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
   const int tile = kTileOf[p->cls];
   std::vector<int> order(plan->mats.size());
@@ -225,15 +224,11 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
 }
 
 // ARTOPK_OK, or ARTOPK_EINVAL with the reason in `err`.  Throws std::bad_alloc.
-int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products, MatPlan* plan, char* err) {
-  if (!mats) return fail_text(err, ARTOPK_EINVAL, "mats is NULL");
-  if (count < 1 || count > kMaxMatrices) return fail_text(err, ARTOPK_EINVAL, "count=%d outside [1, %d]", count, kMaxMatrices);
+int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int parts, MatPlan* plan, char* err) {
   if (n < 1 || n >= (1ll << 31)) return fail_text(err, ARTOPK_EINVAL, "n=%lld outside [1, 2^31)", (long long)n);
   if (type != ARTOPK_G_F32 && type != ARTOPK_G_BF16 && type != ARTOPK_G_F16)
     return fail_text(err, ARTOPK_EINVAL, "unknown element type %d", type);
-  if (products != ARTOPK_PRODUCTS_HALF && products != ARTOPK_PRODUCTS_SPLIT)
-    return fail_text(err, ARTOPK_EINVAL, "unknown kind of products %d", products);
-  const int parts = products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
+  plan->parts = parts;
   std::vector<int32_t> order(count);
   for (int i = 0; i < count; ++i) {
     const artopk_matrix& m = mats[i];
@@ -318,31 +313,87 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
     plan->small_lds = 0;
   }
   if (!plan->small) {
-  list_product(plan, gram, &plan->gram, each);
-  plan->join.at = plan->tiles.size();
-  for (int i = 0; i < plan->gram.tiles.count; ++i) {
-    const MatTile t = plan->tiles[plan->gram.tiles.at + i];
-    if (t.shares > 1 && t.share == 0) plan->tiles.push_back(t);
-  }
-  plan->join.count = (int)(plan->tiles.size() - plan->join.at);
-  list_product(plan, square, &plan->square, 0);
-  list_product(plan, apply, &plan->apply, 0);
+    list_product(plan, gram, &plan->gram, each);
+    plan->join.at = plan->tiles.size();
+    for (int i = 0; i < plan->gram.tiles.count; ++i) {
+      const MatTile t = plan->tiles[plan->gram.tiles.at + i];
+      if (t.shares > 1 && t.share == 0) plan->tiles.push_back(t);
+    }
+    plan->join.count = (int)(plan->tiles.size() - plan->join.at);
+    list_product(plan, square, &plan->square, 0);
+    list_product(plan, apply, &plan->apply, 0);
   }
   if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
 
+  return ARTOPK_OK;
+}
+
+// What an entry point launches on, with its places in the handle's memory.
+struct Route {
+  int parts = 1;
+  int nchunks = 0;
+  Span begin;
+  Product gram, square, apply;
+  Span join;
+  int count = 0;
+  bool pairs = false;
+  size_t small_lds = 0;  // 0: not small
+  const MatDesc* mats = nullptr;
+  const MatChunk* chunks = nullptr;
+  const MatTile* tiles = nullptr;
+  double* sums = nullptr;
+  float* partial = nullptr;
+};
+
+// The parts of an operand, for the entry point that gives a matrix itself or the one that steps weights by it.  By default
+// the products' roundings stay below the result's own.  Against 64 bits HALF is 0.9e-3 to 1.8e-3 off, float16's own rounding
+// 0.2e-3 and bfloat16's 1.6e-3; of few rows the singular values lie so close that roundings go the same way (17 x 1300
+// 2.9e-3, 16 x 3662 4.1e-3), and SPLIT costs little there (64 x 64 20 us for 15.6).  A step of 16-bit weights moves them by a
+// small part of themselves, and HALF's share of that is below the rounding of the sum.
+int parts_for(const artopk_matrix* mats, int32_t count, int32_t type, int32_t products, bool weights) {
+  if (products != ARTOPK_PRODUCTS_DEFAULT) return products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
+  if (type == ARTOPK_G_F32) return 2;
+  if (weights) return 1;
+  if (type == ARTOPK_G_F16) return 2;
+  int32_t rows = 0;
+  for (int32_t i = 0; i < count; ++i) rows = std::max(rows, std::min(mats[i].rows, mats[i].cols));
+  return rows <= 64 ? 2 : 1;
+}
+
+// Both entry points' plans, and the places of their tables; the iterates' memory is used by one call at a time.
+struct Plans {
+  MatPlan plan[2];
+  int count = 1;  // 1: they are the same
+  size_t o_mats[2], o_chunks[2], o_tiles[2], o_sums[2], o_partial[2], o_mem = 0, total = 0;
+};
+
+int make_plans(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products, Plans* p, char* err) {
+  if (!mats) return fail_text(err, ARTOPK_EINVAL, "mats is NULL");
+  if (count < 1 || count > kMaxMatrices) return fail_text(err, ARTOPK_EINVAL, "count=%d outside [1, %d]", count, kMaxMatrices);
+  if (products != ARTOPK_PRODUCTS_HALF && products != ARTOPK_PRODUCTS_SPLIT && products != ARTOPK_PRODUCTS_DEFAULT)
+    return fail_text(err, ARTOPK_EINVAL, "unknown kind of products %d", products);
+  const int own = parts_for(mats, count, type, products, false), weights = parts_for(mats, count, type, products, true);
+  p->count = own == weights ? 1 : 2;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
     at = align_up(at + bytes, 256);
     return o;
   };
-  plan->o_mats = take(plan->mats.size() * sizeof(MatDesc));
-  plan->o_chunks = take(plan->chunks.size() * sizeof(MatChunk));
-  plan->o_tiles = take(plan->tiles.size() * sizeof(MatTile));
-  plan->o_sums = take((size_t)plan->sums * sizeof(double));
-  plan->o_partial = take((size_t)plan->slots * kTileOf[plan->gram.cls] * kTileOf[plan->gram.cls] * sizeof(float));
-  plan->o_mem = take((size_t)plan->halves * 2);
-  plan->total = at;
+  int64_t halves = 0;
+  for (int i = 0; i < p->count; ++i) {
+    MatPlan& plan = p->plan[i];
+    const int rc = make_plan(mats, count, n, type, i == 0 ? own : weights, &plan, err);
+    if (rc) return rc;
+    p->o_mats[i] = take(plan.mats.size() * sizeof(MatDesc));
+    p->o_chunks[i] = take(plan.chunks.size() * sizeof(MatChunk));
+    p->o_tiles[i] = take(plan.tiles.size() * sizeof(MatTile));
+    p->o_sums[i] = take((size_t)plan.sums * sizeof(double));
+    p->o_partial[i] = take((size_t)plan.slots * kTileOf[plan.gram.cls] * kTileOf[plan.gram.cls] * sizeof(float));
+    halves = std::max(halves, plan.halves);
+  }
+  p->o_mem = take((size_t)halves * 2);
+  p->total = at;
   return ARTOPK_OK;
 }
 
@@ -351,20 +402,9 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
 struct artopk_matrices {
   hipStream_t stream = nullptr;
   int64_t n = 0;
-  int32_t type = 0, parts = 1;
-  int nchunks = 0;
-  Span begin;
-  Product gram, square, apply;
-  Span join;
-  int count = 0;
-  bool pairs = false;
-  size_t small_lds = 0;  // 0: not small
-  float* partial = nullptr;
+  int32_t type = 0;
+  Route own, weights;  // of artopk_orthogonalize and of artopk_muon_step
   char* slab = nullptr;
-  const MatDesc* mats = nullptr;
-  const MatChunk* chunks = nullptr;
-  const MatTile* tiles = nullptr;
-  double* sums = nullptr;
   _Float16* mem = nullptr;
   char err[kErrText] = {0};
 };
@@ -428,54 +468,54 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 }
 
 template <int TILE, int PARTS, int MODE>
-void product(artopk_matrices* h, const Span& s, const ProductArgs& a, const FinishArgs& f) {
-  k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(h->tiles + s.at, h->mem, a, f,
-                                                                                                  h->partial);
+void product(const artopk_matrices* h, const Route& r, const Span& s, const ProductArgs& a, const FinishArgs& f) {
+  k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(r.tiles + s.at, h->mem, a, f,
+                                                                                                  r.partial);
 }
 
 template <int PARTS, int MODE>
-void product(artopk_matrices* h, const Product& p, const ProductArgs& a, const FinishArgs& f) {
+void product(const artopk_matrices* h, const Route& r, const Product& p, const ProductArgs& a, const FinishArgs& f) {
   switch (p.cls) {
-    case 0: return product<64, PARTS, MODE>(h, p.tiles, a, f);
-    case 1: return product<128, PARTS, MODE>(h, p.tiles, a, f);
-    case 2: return product<192, PARTS, MODE>(h, p.tiles, a, f);
-    case 3: return product<256, PARTS, MODE>(h, p.tiles, a, f);
-    default: return product<64 + (PARTS == 2 ? kDeep : 0), PARTS, MODE>(h, p.tiles, a, f);
+    case 0: return product<64, PARTS, MODE>(h, r, p.tiles, a, f);
+    case 1: return product<128, PARTS, MODE>(h, r, p.tiles, a, f);
+    case 2: return product<192, PARTS, MODE>(h, r, p.tiles, a, f);
+    case 3: return product<256, PARTS, MODE>(h, r, p.tiles, a, f);
+    default: return product<64 + (PARTS == 2 ? kDeep : 0), PARTS, MODE>(h, r, p.tiles, a, f);
   }
 }
 
 template <int TILE, int PARTS>
-void join_shares(artopk_matrices* h) {
-  k_mat_join<TILE, PARTS><<<dim3(h->join.count, 2), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
-      h->tiles + h->join.at, h->mem, h->partial);
+void join_shares(const artopk_matrices* h, const Route& r) {
+  k_mat_join<TILE, PARTS><<<dim3(r.join.count, 2), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
+      r.tiles + r.join.at, h->mem, r.partial);
 }
 
 // What the squares' or the momentum's launch leaves to do.
 template <int PARTS, class From>
-void polar(artopk_matrices* h, From from, const Steps& st, float eps, const FinishArgs& f) {
+void polar(const artopk_matrices* h, const Route& r, From from, const Steps& st, float eps, const FinishArgs& f) {
   if (st.count == 0) {
-    k_mat_scaled<From><<<h->nchunks, 256, 0, h->stream>>>(from, h->mats, h->chunks, h->sums, eps, f);
+    k_mat_scaled<From><<<r.nchunks, 256, 0, h->stream>>>(from, r.mats, r.chunks, r.sums, eps, f);
     return;
   }
-  if (h->small_lds) {
+  if (r.small_lds) {
     PolarSteps ps = {};
     ps.steps = st.count;
     memcpy(ps.co, st.co, sizeof(float) * 3 * st.count);
-    k_mat_small<PARTS, From><<<h->count, kSmallThreads, h->small_lds, h->stream>>>(from, h->mats, ps, eps, f);
+    k_mat_small<PARTS, From><<<r.count, kSmallThreads, r.small_lds, h->stream>>>(from, r.mats, ps, eps, f);
     return;
   }
-  k_mat_begin<PARTS, From><<<h->begin.count, 256, 0, h->stream>>>(from, h->tiles + h->begin.at, h->sums, eps, h->mem);
+  k_mat_begin<PARTS, From><<<r.begin.count, 256, 0, h->stream>>>(from, r.tiles + r.begin.at, r.sums, eps, h->mem);
   int x = 0;  // which X
   auto square = [&](int k, int in, int out) {
-    product<PARTS, kSquare>(h, h->square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2]}, f);
+    product<PARTS, kSquare>(h, r, r.square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2]}, f);
   };
-  auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, h->square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
+  auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, r, r.square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
   for (int k = 0; k < st.count;) {
-    product<PARTS, kGram>(h, h->gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
-    if (h->join.count) kTileOf[h->gram.cls] == 64 ? join_shares<64, PARTS>(h) : join_shares<128, PARTS>(h);
+    product<PARTS, kGram>(h, r, r.gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
+    if (r.join.count) kTileOf[r.gram.cls] == 64 ? join_shares<64, PARTS>(h, r) : join_shares<128, PARTS>(h, r);
     square(k, 0, 1);
     int q = 1;
-    if (h->pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {
+    if (r.pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {
       times(1, 0, 2);      // Q_1 A_0
       times(2, 1, 0);      // A_1
       square(k + 1, 0, 2);  // Q_2
@@ -486,19 +526,19 @@ void polar(artopk_matrices* h, From from, const Steps& st, float eps, const Fini
     ++k;
     const ProductArgs a = {x, q, 0, 0, 0, 0, 0};
     if (k < st.count)
-      product<PARTS, kApply>(h, h->apply, a, f);
+      product<PARTS, kApply>(h, r, r.apply, a, f);
     else
-      product<PARTS, kFinal>(h, h->apply, a, f);
+      product<PARTS, kFinal>(h, r, r.apply, a, f);
     x ^= 1;
   }
 }
 
 template <class From>
-void polar(artopk_matrices* h, From from, const Steps& st, float eps, const FinishArgs& f) {
-  if (h->parts == 2)
-    polar<2>(h, from, st, eps, f);
+void polar(const artopk_matrices* h, const Route& r, From from, const Steps& st, float eps, const FinishArgs& f) {
+  if (r.parts == 2)
+    polar<2>(h, r, from, st, eps, f);
   else
-    polar<1>(h, from, st, eps, f);
+    polar<1>(h, r, from, st, eps, f);
 }
 
 // Calls f with a null pointer of the handle's element type.
@@ -540,9 +580,9 @@ hipError_t allow_small(const artopk_matrices* h) {
 
 int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products) {
   try {
-    MatPlan plan;
-    if (make_plan(mats, count, n, type, products, &plan, g_noctx_err)) return -1;
-    return (int64_t)plan.total;
+    Plans plans;
+    if (make_plans(mats, count, n, type, products, &plans, g_noctx_err)) return -1;
+    return (int64_t)plans.total;
   } catch (const std::exception&) {
     return -1;
   }
@@ -551,9 +591,9 @@ int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, 
 int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
                            int32_t products, void* hip_stream) {
   if (!out) return fail_text(g_noctx_err, ARTOPK_EINVAL, "out is NULL");
-  MatPlan plan;
+  Plans plans;
   try {
-    const int rc = make_plan(mats, count, n, type, products, &plan, g_noctx_err);
+    const int rc = make_plans(mats, count, n, type, products, &plans, g_noctx_err);
     if (rc) return rc;
   } catch (const std::exception&) {
     return fail_text(g_noctx_err, ARTOPK_ENOMEM, "out of host memory");
@@ -563,36 +603,42 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   h->stream = reinterpret_cast<hipStream_t>(hip_stream);
   h->n = n;
   h->type = type;
-  h->parts = products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
-  h->nchunks = (int)plan.chunks.size();
-  h->begin = plan.begin;
-  h->gram = plan.gram;
-  h->join = plan.join;
-  h->pairs = plan.pairs;
-  h->count = (int)plan.mats.size();
-  h->small_lds = plan.small ? plan.small_lds : 0;
-  h->square = plan.square;
-  h->apply = plan.apply;
   void* p = nullptr;
-  hipError_t e = hipMalloc(&p, plan.total);
+  hipError_t e = hipMalloc(&p, plans.total);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     delete h;
-    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "hipMalloc of %lld bytes failed: %s", (long long)plan.total, hipGetErrorString(e));
+    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "hipMalloc of %lld bytes failed: %s", (long long)plans.total, hipGetErrorString(e));
   }
   h->slab = static_cast<char*>(p);
-  h->mats = reinterpret_cast<const MatDesc*>(h->slab + plan.o_mats);
-  h->chunks = reinterpret_cast<const MatChunk*>(h->slab + plan.o_chunks);
-  h->tiles = reinterpret_cast<const MatTile*>(h->slab + plan.o_tiles);
-  h->sums = reinterpret_cast<double*>(h->slab + plan.o_sums);
-  h->partial = reinterpret_cast<float*>(h->slab + plan.o_partial);
-  h->mem = reinterpret_cast<_Float16*>(h->slab + plan.o_mem);
-  e = hipMemcpy(h->slab + plan.o_mats, plan.mats.data(), plan.mats.size() * sizeof(MatDesc), hipMemcpyHostToDevice);
-  if (e == hipSuccess)
-    e = hipMemcpy(h->slab + plan.o_chunks, plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk), hipMemcpyHostToDevice);
-  if (e == hipSuccess)
-    e = hipMemcpy(h->slab + plan.o_tiles, plan.tiles.data(), plan.tiles.size() * sizeof(MatTile), hipMemcpyHostToDevice);
-  if (e == hipSuccess && h->small_lds) e = h->parts == 2 ? allow_small<2>(h) : allow_small<1>(h);
+  h->mem = reinterpret_cast<_Float16*>(h->slab + plans.o_mem);
+  for (int i = 0; i < plans.count && e == hipSuccess; ++i) {
+    const MatPlan& plan = plans.plan[i];
+    Route& r = i == 0 ? h->own : h->weights;
+    r.parts = plan.parts;
+    r.nchunks = (int)plan.chunks.size();
+    r.begin = plan.begin;
+    r.gram = plan.gram;
+    r.square = plan.square;
+    r.apply = plan.apply;
+    r.join = plan.join;
+    r.count = (int)plan.mats.size();
+    r.pairs = plan.pairs;
+    r.small_lds = plan.small ? plan.small_lds : 0;
+    r.mats = reinterpret_cast<const MatDesc*>(h->slab + plans.o_mats[i]);
+    r.chunks = reinterpret_cast<const MatChunk*>(h->slab + plans.o_chunks[i]);
+    r.tiles = reinterpret_cast<const MatTile*>(h->slab + plans.o_tiles[i]);
+    r.sums = reinterpret_cast<double*>(h->slab + plans.o_sums[i]);
+    r.partial = reinterpret_cast<float*>(h->slab + plans.o_partial[i]);
+    auto fill = [&](size_t to, const void* from, size_t bytes) {
+      if (e == hipSuccess && bytes) e = hipMemcpy(h->slab + to, from, bytes, hipMemcpyHostToDevice);
+    };
+    fill(plans.o_mats[i], plan.mats.data(), plan.mats.size() * sizeof(MatDesc));
+    fill(plans.o_chunks[i], plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk));
+    fill(plans.o_tiles[i], plan.tiles.data(), plan.tiles.size() * sizeof(MatTile));
+    if (e == hipSuccess && r.small_lds) e = r.parts == 2 ? allow_small<2>(h) : allow_small<1>(h);
+  }
+  if (plans.count == 1) h->weights = h->own;
   if (e != hipSuccess) {
     (void)hipFree(h->slab);
     delete h;
@@ -629,8 +675,9 @@ int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t s
   f.type = m->type;
   with_type(m->type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    if (!m->small_lds || steps == 0) k_mat_squares<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), m->chunks, m->sums);
-    polar(m, FromVector<T>{static_cast<const T*>(x)}, st, eps, f);
+    const Route& r = m->own;
+    if (!r.small_lds || steps == 0) k_mat_squares<T><<<r.nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), r.chunks, r.sums);
+    polar(m, r, FromVector<T>{static_cast<const T*>(x)}, st, eps, f);
   });
   MAT_TRY(m, hipGetLastError());
   return ARTOPK_OK;
@@ -662,11 +709,12 @@ int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const f
   f.type = m->type;
   f.muon = 1;
   f.a = MuonArgs{mu, update_scale, nesterov != 0, eta, (float)(1.0 - (double)eta * (double)decay), eta_rest};
+  const Route& r = m->weights;
   with_type(m->type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    k_mat_momentum<T><<<m->nchunks, 256, 0, m->stream>>>(static_cast<T*>(weights), momentum, update, f.a, m->chunks, m->sums);
+    k_mat_momentum<T><<<r.nchunks, 256, 0, m->stream>>>(static_cast<T*>(weights), momentum, update, f.a, r.chunks, r.sums);
   });
-  polar(m, FromMomentum{momentum, update, f.a}, st, eps, f);
+  polar(m, r, FromMomentum{momentum, update, f.a}, st, eps, f);
   MAT_TRY(m, hipGetLastError());
   return ARTOPK_OK;
 }

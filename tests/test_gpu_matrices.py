@@ -345,3 +345,46 @@ def test_on_its_own_stream_and_in_a_graph():
             graph.replay()
             stream.synchronize()
             assert torch.equal(w, eager[turn][0]) and torch.equal(m, eager[turn][1]), turn
+
+
+@pytest.mark.parametrize("t,shapes", [("f16", [(16, 700), (90, 333), (300, 77), (520, 530)]), ("bf16", [(16, 700), (24, 57), (333, 64)]),
+                                      ("f32", [(16, 700), (333, 64)])])
+def test_products_by_default_stay_below_the_result_s_own_rounding(t, shapes):
+    """Default products: off by no more than SPLIT may be, and the type's unit roundoff."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(33)
+    mats, n = layout(shapes)
+    x = torch.from_numpy(_gradients(rng, shapes, n)).cuda().to(_dtype(t))
+    out = torch.zeros_like(x)
+    lib.MatrixContext(mats, n, _code(t)).artopk_orthogonalize(x, out)
+    got, xs = out.cpu().double().numpy(), x.cpu().double().numpy()
+    for at, r, c, scale in mats:
+        want, norms = reference(xs[at:at + r * c].reshape(r, c))
+        off = np.linalg.norm(got[at:at + r * c].reshape(r, c) - scale * want) / np.linalg.norm(scale * want)
+        assert off <= tolerance(norms, OPERAND_U[1]) + {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[t], (r, c, off)
+
+
+def test_default_products_are_one_of_the_two():
+    """The same bits as the kind that the rule names, for both entry points of one handle, one after the other."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    half, split = lib.ARTOPK_PRODUCTS_HALF, lib.ARTOPK_PRODUCTS_SPLIT
+    for t, shapes, orth, muon in (("f16", [(70, 200), (64, 65)], split, half), ("bf16", [(70, 200), (64, 65)], half, half),
+                                  ("bf16", [(64, 200), (65, 64)], split, half), ("f32", [(70, 200)], split, split)):
+        mats, n = layout(shapes)
+        rng = np.random.default_rng(34)
+        x = torch.from_numpy(_gradients(rng, shapes, n)).cuda()
+        u = x * 2
+        own = lib.MatrixContext(mats, n, _code(t))
+        results = []
+        for ctx_orth, ctx_muon in ((own, own), (lib.MatrixContext(mats, n, _code(t), orth), lib.MatrixContext(mats, n, _code(t), muon))):
+            out, w, m = torch.zeros_like(x).to(_dtype(t)), x.to(_dtype(t)).clone(), torch.ones_like(x)
+            for _ in range(2):
+                ctx_orth.artopk_orthogonalize(x.to(_dtype(t)), out)
+                ctx_muon.artopk_muon_step(w, m, u, eta=0.1, decay=0.01, eta_rest=0.1)
+            results.append((out, w, m))
+        for a, b in zip(*results):
+            assert torch.equal(a, b), (t, shapes)

@@ -51,3 +51,13 @@ def test_no_cpu_fallback():
         lib.NormContext(4, 4)
     with pytest.raises(RuntimeError):
         lib.MatrixContext([(0, 2, 2)], 4)
+
+
+def test_matrices_scratch_of_both_kinds_of_products():
+    q = lib.artopk_matrices_scratch_bytes
+    mats, n = [(0, 512, 700)], 512 * 700
+    half, split = (q(mats, n, lib.ARTOPK_G_F16, p) for p in (lib.ARTOPK_PRODUCTS_HALF, lib.ARTOPK_PRODUCTS_SPLIT))
+    assert split <= q(mats, n, lib.ARTOPK_G_F16) < split + half // 4  # the iterates' memory serves one call at a time
+    assert q(mats, n, lib.ARTOPK_G_BF16) == half
+    assert q([(0, 64, 700)], n, lib.ARTOPK_G_BF16) > q([(0, 64, 700)], n, lib.ARTOPK_G_BF16, lib.ARTOPK_PRODUCTS_HALF)
+    assert q(mats, n, lib.ARTOPK_G_F16, -2) == -1
