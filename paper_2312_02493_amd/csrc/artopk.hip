@@ -1412,7 +1412,7 @@ Layout scratch_layout(int32_t max_w, int64_t max_n, int64_t max_k, int32_t max_s
 
 extern "C" {
 
-int32_t artopk_version(void) { return 200; }  // 0.2.0: options, counted round-robin leader, allocation-free variance
+int32_t artopk_version(void) { return 300; }  // 0.3.0: layer norm, orthogonalised updates
 
 const char* artopk_last_error(const artopk_ctx* ctx) { return ctx ? ctx->err : g_noctx_err; }
 
