@@ -22,6 +22,8 @@ struct artopk_norm {
 namespace {
 
 constexpr int64_t kRegisterCols = 16384;  // longest row that a block's registers hold
+constexpr int kWaveCols = 512;        // what a wave's eight elements a lane hold
+constexpr int kSingleCols = 8192;  // the same in the backward pass, taken one by one
 constexpr int kMaxShares = 1024;          // blocks of a backward pass, at most
 constexpr int kLongShares = 64;
 // Up to this many rows, and elements, the weight gradients are summed column by column beside the rows' blocks.
@@ -93,20 +95,22 @@ bool wide_rows(const void* p, int64_t stride, int64_t rows, size_t size) {
   return aligned16(p) && (rows <= 1 || stride * (int64_t)size % 16 == 0);
 }
 
-// Calls f(V, whether rows end inside V elements, threads of a row, elements of a thread) as compile-time constants: a wave where it holds the row, then the fewest
-// threads that do; with fewer rows than compute units twice as many, of half the elements.
-template <int V, bool TAIL, class F>
+// Calls f(V, whether rows may lie anywhere, threads of a row, elements of a thread) as compile-time constants: a wave where it
+// holds the row, then the fewest threads that do; with fewer rows than compute units twice as many, of half the elements.
+template <int V, bool ANY, int MOST, class F>  // at most MOST columns
 void with_shape(int64_t cols, bool few, F&& f) {
-  auto go = [&](auto tpr, auto e) { f(std::integral_constant<int, V>(), std::integral_constant<bool, TAIL>(), tpr, e); };
+  auto go = [&](auto tpr, auto e) { f(std::integral_constant<int, V>(), std::integral_constant<bool, ANY>(), tpr, e); };
   using std::integral_constant;
-  if (cols <= 512) return go(integral_constant<int, 64>(), integral_constant<int, 8>());
-  if (cols <= 1024 && !few) return go(integral_constant<int, 64>(), integral_constant<int, 16>());
-  if (cols <= 2048) return go(integral_constant<int, 256>(), integral_constant<int, 8>());
-  if (cols <= 4096 && !few) return go(integral_constant<int, 256>(), integral_constant<int, 16>());
-  if (cols <= 4096) return go(integral_constant<int, 512>(), integral_constant<int, 8>());
-  if (cols <= 8192 && !few) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
-  if (cols <= 8192) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
-  return go(integral_constant<int, 1024>(), integral_constant<int, 16>());
+  if (MOST <= kWaveCols || cols <= kWaveCols) return go(integral_constant<int, 64>(), integral_constant<int, 8>());
+  if constexpr (MOST > kWaveCols) {
+    if (cols <= 1024 && !few) return go(integral_constant<int, 64>(), integral_constant<int, 16>());
+    if (cols <= 2048) return go(integral_constant<int, 256>(), integral_constant<int, 8>());
+    if (cols <= 4096 && !few) return go(integral_constant<int, 256>(), integral_constant<int, 16>());
+    if (cols <= 4096) return go(integral_constant<int, 512>(), integral_constant<int, 8>());
+    if (cols <= 8192 && !few) return go(integral_constant<int, 512>(), integral_constant<int, 16>());
+    if (MOST <= 8192 || cols <= 8192) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
+    if constexpr (MOST > 8192) go(integral_constant<int, 1024>(), integral_constant<int, 16>());
+  }
 }
 
 template <class T>
@@ -117,19 +121,25 @@ void forward(artopk_norm* h, const T* x, int64_t x_stride, int64_t rows, int64_t
     k_norm_forward_long<T><<<blocks, 1024, 0, h->stream>>>(x, x_stride, rows, cols, gamma, beta, eps, y, y_stride, mean, rstd);
     return;
   }
-  auto go = [&](auto V, auto TAIL, auto TPR, auto E) {
+  auto go = [&](auto V, auto ANY, auto TPR, auto E) {
     using S = NormShape<TPR()>;
     const int64_t units = (rows + S::kRows - 1) / S::kRows;
     const int blocks = (int)std::min<int64_t>(units, (int64_t)h->num_cu * (2048 / S::kThreads));
-    k_norm_forward<T, V(), TAIL(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(x, x_stride, rows, (int)cols, gamma, beta, eps,
+    k_norm_forward<T, V(), ANY(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(x, x_stride, rows, (int)cols, gamma, beta, eps,
                                                                               y, y_stride, mean, rstd);
   };
   constexpr int kWide = 16 / sizeof(T);
   const bool few = rows <= h->num_cu;
-  if (wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(y, y_stride, rows, sizeof(T)))
-    cols % kWide ? with_shape<kWide, true>(cols, few, go) : with_shape<kWide, false>(cols, few, go);
+  const bool wide = wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(y, y_stride, rows, sizeof(T));
+  // Where sixteen bytes are not aligned they still move faster than one 16-bit element at a time (8191 x 2501 f16 25 us, so 22;
+  // 4000 x 10001 bf16 44, so 41), but not than one float32 (4099 x 1111 10.3, so 11.8), nor in a wave's row (30000 x 333 bf16
+  // 12.2, so 14.7).
+  if (wide && cols % kWide == 0)
+    with_shape<kWide, false, kRegisterCols>(cols, few, go);
+  else if (cols >= kWide && (wide || (sizeof(T) == 2 && cols > kWaveCols)))
+    with_shape<kWide, true, kRegisterCols>(cols, few, go);
   else
-    with_shape<1, false>(cols, few, go);
+    with_shape<1, false, sizeof(T) == 2 ? kWaveCols : kRegisterCols>(cols, few, go);
 }
 
 // Returns the number of shares of the weight gradients to be added up, 0 if they are done.
@@ -151,22 +161,27 @@ int backward(artopk_norm* h, const T* dy, int64_t dy_stride, const T* x, int64_t
     return shares;
   }
   const bool columns = part && rows <= kColumnRows && rows * cols <= kColumnElems;
-  auto go = [&](auto V, auto TAIL, auto TPR, auto E) {
+  auto go = [&](auto V, auto ANY, auto TPR, auto E) {
     using S = NormShape<TPR()>;
     const int64_t units = (rows + S::kRows - 1) / S::kRows;
     shares = (int)std::min<int64_t>(units, std::min<int64_t>(kMaxShares, (int64_t)h->num_cu * (1024 / S::kThreads)));
     const int row_blocks = columns && !dx ? 0 : shares;
     const int blocks = row_blocks + (columns ? (int)((cols + 63) / 64) : 0);
-    k_norm_backward<T, V(), TAIL(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(
+    k_norm_backward<T, V(), ANY(), TPR(), E()><<<blocks, S::kThreads, 0, h->stream>>>(
         dy, dy_stride, x, x_stride, rows, (int)cols, gamma, mean, rstd, dx, dx_stride, columns ? nullptr : part, row_blocks, grads);
   };
   constexpr int kWide = 16 / sizeof(T);
   const bool few = rows <= h->num_cu;
-  if (wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(dy, dy_stride, rows, sizeof(T)) &&
-      (!dx || wide_rows(dx, dx_stride, rows, sizeof(T))))
-    cols % kWide ? with_shape<kWide, true>(cols, few, go) : with_shape<kWide, false>(cols, few, go);
+  const bool wide = wide_rows(x, x_stride, rows, sizeof(T)) && wide_rows(dy, dy_stride, rows, sizeof(T)) &&
+                    (!dx || wide_rows(dx, dx_stride, rows, sizeof(T)));
+  // Where sixteen bytes are not aligned one element at a time is faster (8191 x 2501 f16 42 us, 54 by sixteen bytes) as long
+  // as its registers hold the row (4000 x 10001 bf16 290 and 86, f32 291 and 121).
+  if (wide && cols % kWide == 0)
+    with_shape<kWide, false, kRegisterCols>(cols, few, go);
+  else if (cols >= kWide && (wide || cols > kSingleCols))
+    with_shape<kWide, true, kRegisterCols>(cols, few, go);
   else
-    with_shape<1, false>(cols, few, go);
+    with_shape<1, false, kSingleCols>(cols, few, go);
   if (columns) shares = 0;
   return shares;
 }

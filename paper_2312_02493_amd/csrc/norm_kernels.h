@@ -77,30 +77,44 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* room, int turn) {
   }
 }
 
-// V elements of a row as they lie, zeros behind its end.  With TAIL the row's length need not be a multiple of V, and its last
-// elements go one by one.  Without it a load stands in no branch, behind which it would be waited for: places behind the end
-// read the row's last ones instead (32768 x 2048 bf16 backward 93 us with a branch around each load, 78 so).
-template <class T, int V, bool TAIL>
+// V elements of a row as they lie, zeros behind its end.  A load stands in no branch, behind which it would be waited for:
+// places behind the end read the row's last ones instead (32768 x 2048 bf16 backward 93 us with a branch around each load, 78
+// so).  With ANY rows may begin at any element and end inside V: sixteen bytes are then read and written wherever they lie,
+// over a row's end into what follows, but never beyond the last row's (`last`: its last V elements), and settle(), where
+// the elements are first needed, brings in order what lies there.
+template <class T, int V, bool ANY>
 struct alignas(V * sizeof(T)) Piece {
   T e[V];
-  __device__ __forceinline__ void load(const T* row, int c, int cols) {
-    if constexpr (TAIL) {
-      if (c + V <= cols) {
-        *this = *reinterpret_cast<const Piece*>(row + c);
-      } else {
+  __device__ __forceinline__ void load(const T* row, int c, int cols, const T* last) {
+    const T* at = row + (c < cols ? c : cols - V);
+    if constexpr (ANY)
+      __builtin_memcpy(e, at < last ? at : last, sizeof(e));
+    else
+      *this = *reinterpret_cast<const Piece*>(at);
+  }
+  __device__ __forceinline__ void settle(const T* row, int c, int cols, const T* last) {
+    if constexpr (ANY) {
+      if (c + V > cols) {
+        if (c < cols && row + c > last) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) e[i] = c + i < cols ? row[c + i] : static_cast<T>(0.0f);
+          for (int i = 0; i < V; ++i) e[i] = c + i < cols ? row[c + i] : static_cast<T>(0.0f);
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; ++i) e[i] = c + i < cols ? e[i] : static_cast<T>(0.0f);
+        }
       }
     } else {
-      *this = *reinterpret_cast<const Piece*>(row + (c < cols ? c : cols - V));
 #pragma unroll
       for (int i = 0; i < V; ++i) e[i] = c < cols ? e[i] : static_cast<T>(0.0f);
     }
   }
   __device__ __forceinline__ void store(T* row, int c, int cols) const {
     if (c + V <= cols) {
-      *reinterpret_cast<Piece*>(row + c) = *this;
-    } else if constexpr (TAIL) {
+      if constexpr (ANY)
+        __builtin_memcpy(row + c, e, sizeof(e));
+      else
+        *reinterpret_cast<Piece*>(row + c) = *this;
+    } else if constexpr (ANY) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (c + i < cols) row[c + i] = e[i];
@@ -127,7 +141,7 @@ __device__ __forceinline__ void load_weights(float (&out)[V], const float* w, in
 }
 
 // Rows blockIdx.x, blockIdx.x + gridDim.x, .. (times the rows a block has); the next row is on its way while one is summed.
-template <class T, int V, bool TAIL, int TPR, int E>
+template <class T, int V, bool ANY, int TPR, int E>
 __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
     const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, const float* __restrict__ gamma,
     const float* __restrict__ beta, float eps, T* __restrict__ y, int64_t y_stride, float* __restrict__ mean_out,
@@ -138,9 +152,10 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
   const float inv = 1.0f / static_cast<float>(cols);
   const int64_t step = (int64_t)gridDim.x * NormShape<TPR>::kRows;
   int64_t row = (int64_t)blockIdx.x * NormShape<TPR>::kRows + threadIdx.x / TPR;
-  Piece<T, V, TAIL> next[R];
+  const T* last = x + (rows - 1) * x_stride + cols - V;
+  Piece<T, V, ANY> next[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) next[r].load(x + (row < rows ? row : rows - 1) * x_stride, (r * TPR + t) * V, cols);
+  for (int r = 0; r < R; ++r) next[r].load(x + (row < rows ? row : rows - 1) * x_stride, (r * TPR + t) * V, cols, last);
   float gm[R][V], bt[R][V];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -153,16 +168,18 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
     float v[R][V];
     float s[1] = {0.0f};
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+      next[r].settle(x + row * x_stride, (r * TPR + t) * V, cols, last);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         v[r][i] = static_cast<float>(next[r].e[i]);
         s[0] += v[r][i];
       }
+    }
     {
       const int64_t then = row + step < rows ? row + step : rows - 1;
 #pragma unroll
-      for (int r = 0; r < R; ++r) next[r].load(x + then * x_stride, (r * TPR + t) * V, cols);
+      for (int r = 0; r < R; ++r) next[r].load(x + then * x_stride, (r * TPR + t) * V, cols, last);
     }
     row_sums<TPR>(s, room, 0);
     const float mean = s[0] * inv;
@@ -188,7 +205,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_forward(
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      Piece<T, V, TAIL> o;
+      Piece<T, V, ANY> o;
 #pragma unroll
       for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(fmaf(v[r][i] * rstd, gm[r][i], bt[r][i]));
       o.store(y + row * y_stride, (r * TPR + t) * V, cols);
@@ -256,7 +273,7 @@ __device__ void norm_columns(int64_t c0, const T* dy, int64_t dy_stride, const T
 // part[0][blockIdx.x][..] (dgamma) and part[1][blockIdx.x][..] (dbeta), rows of `cols`.  Blocks from row_blocks on, if there
 // are such, take 64 columns each instead and write their weights' gradients whole: few rows are read a second time sooner
 // than a second launch adds up shares (then `part` is NULL).
-template <class T, int V, bool TAIL, int TPR, int E>
+template <class T, int V, bool ANY, int TPR, int E>
 __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols,
     const float* __restrict__ gamma, const float* __restrict__ mean, const float* __restrict__ rstd,
@@ -276,7 +293,8 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
   const float inv = 1.0f / static_cast<float>(cols);
   const int64_t step = (int64_t)row_blocks * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-  Piece<T, V, TAIL> next_x[R], next_d[R];
+  const T *last_x = x + (rows - 1) * x_stride + cols - V, *last_d = dy + (rows - 1) * dy_stride + cols - V;
+  Piece<T, V, ANY> next_x[R], next_d[R];
   float next_mu = 0.0f, next_rs = 0.0f;
   auto ask = [&](int64_t of) {
     if (of >= rows) of = rows - 1;  // (not used)
@@ -284,8 +302,8 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     next_rs = rstd[of];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      next_x[r].load(x + of * x_stride, (r * TPR + t) * V, cols);
-      next_d[r].load(dy + of * dy_stride, (r * TPR + t) * V, cols);
+      next_x[r].load(x + of * x_stride, (r * TPR + t) * V, cols, last_x);
+      next_d[r].load(dy + of * dy_stride, (r * TPR + t) * V, cols, last_d);
     }
   };
   // (with wide loads the second row's registers cost more waves than it gains: 32768 x 2048 bf16 81 us, 78 without)
@@ -305,12 +323,15 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     const float mu = next_mu, rs = next_rs;
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+      next_x[r].settle(x + row * x_stride, (r * TPR + t) * V, cols, last_x);
+      next_d[r].settle(dy + row * dy_stride, (r * TPR + t) * V, cols, last_d);
 #pragma unroll
       for (int i = 0; i < V; ++i) {  // (behind the row's end d is zero, and nothing comes of h)
         d[r][i] = static_cast<float>(next_d[r].e[i]);
         h[r][i] = (static_cast<float>(next_x[r].e[i]) - mu) * rs;
       }
+    }
     if (kAhead) ask(row + step);
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -328,7 +349,7 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     const float m1 = s[0] * inv, m2 = s[1] * inv;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      Piece<T, V, TAIL> o;
+      Piece<T, V, ANY> o;
 #pragma unroll
       for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(rs * (d[r][i] - fmaf(h[r][i], m2, m1)));
       o.store(dx + row * dx_stride, (r * TPR + t) * V, cols);

@@ -331,3 +331,32 @@ def test_on_its_own_stream_and_in_a_graph():
             graph.replay()
             stream.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(want, (y, dx, dg))), turn
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,cols", [(3, 9), (2, 515), (3, 1111), (2, 10001)])
+def test_what_lies_between_rows_does_not_matter(t, rows, cols):
+    """The same bits with NaN between the rows as with zeros."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rng = np.random.default_rng(9)
+    ctx = lib.NormContext(rows, cols)
+    a, d = (rng.standard_normal((rows, cols)).astype(np.float32) for _ in range(2))
+    for pad in (1, 8, 23):
+        found = []
+        for between in (0.0, float("nan")):
+            views = []
+            for v in (a, d):
+                mem, view = _strided(v, pad, _dtype(t))
+                keep = view.clone()
+                mem.fill_(between)
+                view.copy_(keep)
+                views.append(view)
+            y, dx = torch.zeros(rows, cols, dtype=_dtype(t), device="cuda"), torch.zeros(rows, cols, dtype=_dtype(t), device="cuda")
+            mean, rstd, dg, db = (torch.zeros(k, device="cuda") for k in (rows, rows, cols, cols))
+            ctx.artopk_layernorm_forward(views[0], None, None, y, mean, rstd)
+            ctx.artopk_layernorm_backward(views[1], views[0], None, mean, rstd, dx, dg, db)
+            found.append((y, mean, rstd, dx, dg, db))
+        for u, v in zip(*found):
+            assert torch.equal(u, v) and not bool(u.isnan().any()), (pad, u.shape)
