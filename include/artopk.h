@@ -490,9 +490,10 @@ typedef struct artopk_matrices artopk_matrices;
 /* How many bits the operands of the matrix products keep.  HALF: 11 (float16, scaled by powers of
  * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32.
  * DEFAULT: as many as the result shows.  Five steps leave a matrix some 1e-3 off with HALF (4e-3 of 16
- * rows) and 1e-6 with SPLIT, so it takes SPLIT for float32 everywhere, and in artopk_orthogonalize for
- * float16 and for bfloat16 where no matrix has more than 64 rows or columns (the fewer of the two); HALF
- * otherwise, in artopk_muon_step for all 16-bit weights (their own rounding is coarser than the step's error). */
+ * rows) and 1e-6 with SPLIT, so it takes SPLIT for float32 and float16; for bfloat16 in
+ * artopk_orthogonalize where the matrices of at most 256 rows or columns (the fewer of the two) have more than
+ * half of all, and HALF otherwise and in artopk_muon_step (the weights' own rounding is coarser than the
+ * step's error). */
 enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1, ARTOPK_PRODUCTS_DEFAULT = -1 };
 
 #define ARTOPK_MAX_POLAR_STEPS 32

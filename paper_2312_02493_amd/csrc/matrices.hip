@@ -346,18 +346,25 @@ struct Route {
 };
 
 // The parts of an operand, for the entry point that gives a matrix itself or the one that steps weights by it.  By default
-// the products' roundings stay below the result's own.  Against 64 bits HALF is 0.9e-3 to 1.8e-3 off, float16's own rounding
-// 0.2e-3 and bfloat16's 1.6e-3; of few rows the singular values lie so close that roundings go the same way (17 x 1300
-// 2.9e-3, 16 x 3662 4.1e-3), and SPLIT costs little there (64 x 64 20 us for 15.6).  A step of 16-bit weights moves them by a
-// small part of themselves, and HALF's share of that is below the rounding of the sum.
+// the products' roundings stay below the result's own: float16's is 0.2e-3, bfloat16's 1.6e-3.  Against 64 bits HALF is
+// 0.9e-3 to 1.3e-3 off from some 600 rows on, 1.5e-3 of 64 to 256, and more of fewer, whose singular values lie so close that
+// roundings go the same way (24 x 200 2.2e-3, 17 x 1300 2.9e-3, 16 x 3662 4.1e-3).  SPLIT costs little there, where launches
+// and latency count (64 x 64 20 us for 15.6, four of 468 x 24 and one of 162 x 1065 110 for 80, 24 of 256 x 1024 195 for
+// 120); so bfloat16 takes it where most of the result (its squared norm is its matrices' rows) is of at most 256 rows, and
+// float16 always.  A step of bfloat16 weights moves them by a small part of themselves, and HALF's share of that is far below
+// the rounding of the sum (of float16 weights, which it left 0.34e-3 off, it is not).
+constexpr int32_t kFewRows = 256;
 int parts_for(const artopk_matrix* mats, int32_t count, int32_t type, int32_t products, bool weights) {
   if (products != ARTOPK_PRODUCTS_DEFAULT) return products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
-  if (type == ARTOPK_G_F32) return 2;
+  if (type != ARTOPK_G_BF16) return 2;
   if (weights) return 1;
-  if (type == ARTOPK_G_F16) return 2;
-  int32_t rows = 0;
-  for (int32_t i = 0; i < count; ++i) rows = std::max(rows, std::min(mats[i].rows, mats[i].cols));
-  return rows <= 64 ? 2 : 1;
+  int64_t all = 0, few = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    const int32_t rows = std::min(mats[i].rows, mats[i].cols);
+    all += rows;
+    if (rows <= kFewRows) few += rows;
+  }
+  return 2 * few > all ? 2 : 1;
 }
 
 // Both entry points' plans, and the places of their tables; the iterates' memory is used by one call at a time.

@@ -372,8 +372,8 @@ def test_default_products_are_one_of_the_two():
     import paper_2312_02493_amd as lib
 
     half, split = lib.ARTOPK_PRODUCTS_HALF, lib.ARTOPK_PRODUCTS_SPLIT
-    for t, shapes, orth, muon in (("f16", [(70, 200), (64, 65)], split, half), ("bf16", [(70, 200), (64, 65)], half, half),
-                                  ("bf16", [(64, 200), (65, 64)], split, half), ("f32", [(70, 200)], split, split)):
+    for t, shapes, orth, muon in (("f16", [(70, 200), (64, 65)], split, split), ("bf16", [(300, 520), (256, 257)], half, half),
+                                  ("bf16", [(300, 520), (64, 256), (257, 256)], split, half), ("f32", [(70, 200)], split, split)):
         mats, n = layout(shapes)
         rng = np.random.default_rng(34)
         x = torch.from_numpy(_gradients(rng, shapes, n)).cuda()
