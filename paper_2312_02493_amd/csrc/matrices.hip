@@ -56,8 +56,8 @@ struct MatPlan {
 // summed index), and as the chip's time for one of very many blocks (`store` and `among` for each 64).  Fitted to products
 // timed one kind at a time, tile by tile: 4096 x 4096 (64 of 64), sixteen matrices of 1280 x 1280 and eight of 1280 x 5120
 // (20 of 64 where m is summed over), and the long sums of one 1280 x 5120 by itself.  What the rule has to get right (us,
-// HALF, tiles of 64 / 128 / 192 / 256): X X^T of 4096 x 4096 132 / 100 / 80 / 99, Q X of it 235 / 138 / 152 / 117, X X^T of
-// 2048 x 2048 22 / 24 / 33 / 48, of 1280 x 5120 19 / 54 / 72 / 108.
+// HALF, tiles of 64 / 128 / 192 / 256): X X^T of 4096 x 4096 130 / 100 / 75 / 89, Q X of it 227 / 131 / 154 / 110, X X^T of
+// four 512 x 4608 18 / 44 / 54 / 87, Q X of the sixteen and eight 346 / 243 / 272 / 206.
 struct TileCost {
   double fixed, alone, store, among;
   int slots;  // blocks that the chip holds

@@ -302,7 +302,11 @@ struct ProductArgs {
 
 // The shape of a product's tile: TILE x TILE elements by WM x WN waves, the summed index in stages of kDepth, kStages of
 // them in LDS.  A stage is brought by loads that go to LDS without passing registers, two stages ahead of its use at most,
-// and every wave keeps the next 32 of the summed index in registers while it multiplies the present ones.
+// and every wave reads the next 32 of the summed index into registers while it multiplies the present ones.
+// What bounds it is the matrix cores' rate at the clock that the chip holds under them: 4096 x 4096, HALF, Q X in tiles of 256
+// 108 us = 1.27 PFLOP/s (a loop of matrix instructions alone reaches 1.5 to 1.6, a large library product 1.4), X X^T's half in
+// tiles of 192 70 us = 1.03 PFLOP/s (253 tiles on 256 units, each stored twice).  Larger tiles feed the cores from fewer reads
+// of LDS, smaller ones fill the chip; the host takes the class that its table of costs says is soonest done.
 constexpr int kDeep = 1;  // added to a TILE: more stages, and one block a compute unit
 template <int TILE_, int PARTS_>
 struct ProductShape {
