@@ -282,8 +282,10 @@ def _elem_type(t) -> int:
     return kind
 
 
-def _rows(t, name: str):
-    """(address, distance of rows, rows, cols) of a matrix whose columns lie side by side."""
+def _rows(t, name: str, device: int):
+    """(address, distance of rows, rows, cols) of a matrix on the device whose columns lie side by side."""
+    if t.get_device() != device:
+        raise ArTopkError(-1, f"{name} is on {t.device}, not on the handle's device {device}")
     shape, stride = t.shape, t.stride()
     if len(shape) != 2:
         raise ArTopkError(-1, f"{name} has {len(shape)} dimensions, not 2")
@@ -293,10 +295,12 @@ def _rows(t, name: str):
     return t.data_ptr(), (stride[0] if rows > 1 else cols), rows, cols
 
 
-def _vector(t, name: str, length: int, kind: Optional[int] = None) -> Optional[int]:
-    """Address of a contiguous vector of `length` elements (of type `kind`), or None for None."""
+def _vector(t, name: str, length: int, device: int, kind: Optional[int] = None) -> Optional[int]:
+    """Address of a contiguous vector of `length` elements (of type `kind`) on the device, or None for None."""
     if t is None:
         return None
+    if t.get_device() != device:
+        raise ArTopkError(-1, f"{name} is on {t.device}, not on the handle's device {device}")
     if t.numel() != length or not t.is_contiguous():
         raise ArTopkError(-1, f"{name} is not a contiguous vector of {length} elements")
     if kind is not None and _types.get(t.dtype) != kind:
@@ -327,6 +331,7 @@ class _Handle:
         self._lib = load_library()
         if stream is None:
             stream = torch.cuda.current_stream().cuda_stream
+        self._device = torch.cuda.current_device()
         h = C.c_void_p()
         rc = getattr(self._lib, f"artopk_{self._name}_create")(C.byref(h), *args, C.c_void_p(stream))
         if rc != 0:
@@ -363,32 +368,34 @@ class NormContext(_Handle):
         self._open(stream, int(max_rows), int(max_cols))
 
     def artopk_layernorm_forward(self, x, gamma, beta, y, mean_out=None, rstd_out=None, eps: float = 1e-5):
-        px, sx, rows, cols = _rows(x, "x")
-        py, sy, rows_y, cols_y = _rows(y, "y")
+        dev = self._device
+        px, sx, rows, cols = _rows(x, "x", dev)
+        py, sy, rows_y, cols_y = _rows(y, "y", dev)
         if rows_y != rows or cols_y != cols or y.dtype != x.dtype:
             raise ArTopkError(-1, "y's shape or type is not x's")
         self._check(self._lib.artopk_layernorm_forward(
-            self._h, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, ARTOPK_G_F32),
-            _vector(beta, "beta", cols, ARTOPK_G_F32), eps, py, sy,
-            _vector(mean_out, "mean_out", rows, ARTOPK_G_F32), _vector(rstd_out, "rstd_out", rows, ARTOPK_G_F32)))
+            self._h, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, dev, ARTOPK_G_F32),
+            _vector(beta, "beta", cols, dev, ARTOPK_G_F32), eps, py, sy,
+            _vector(mean_out, "mean_out", rows, dev, ARTOPK_G_F32), _vector(rstd_out, "rstd_out", rows, dev, ARTOPK_G_F32)))
 
     def artopk_layernorm_backward(self, dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, accumulate: bool = False):
-        px, sx, rows, cols = _rows(x, "x")
-        pd, sd, rows_d, cols_d = _rows(dy, "dy")
+        dev = self._device
+        px, sx, rows, cols = _rows(x, "x", dev)
+        pd, sd, rows_d, cols_d = _rows(dy, "dy", dev)
         if rows_d != rows or cols_d != cols or dy.dtype != x.dtype:
             raise ArTopkError(-1, "dy's shape or type is not x's")
         po, so = None, cols
         if dx is not None:
-            po, so, rows_d, cols_d = _rows(dx, "dx")
+            po, so, rows_d, cols_d = _rows(dx, "dx", dev)
             if rows_d != rows or cols_d != cols or dx.dtype != x.dtype:
                 raise ArTopkError(-1, "dx's shape or type is not x's")
         grad = dbeta if dgamma is None else dgamma
         if dgamma is not None and dbeta is not None and dgamma.dtype != dbeta.dtype:
             raise ArTopkError(-1, "dgamma and dbeta are of different types")
         self._check(self._lib.artopk_layernorm_backward(
-            self._h, pd, sd, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, ARTOPK_G_F32),
-            _vector(mean, "mean", rows, ARTOPK_G_F32), _vector(rstd, "rstd", rows, ARTOPK_G_F32), po, so,
-            _vector(dgamma, "dgamma", cols), _vector(dbeta, "dbeta", cols),
+            self._h, pd, sd, px, sx, _elem_type(x), rows, cols, _vector(gamma, "gamma", cols, dev, ARTOPK_G_F32),
+            _vector(mean, "mean", rows, dev, ARTOPK_G_F32), _vector(rstd, "rstd", rows, dev, ARTOPK_G_F32), po, so,
+            _vector(dgamma, "dgamma", cols, dev), _vector(dbeta, "dbeta", cols, dev),
             ARTOPK_G_F32 if grad is None else _elem_type(grad), int(accumulate)))
 
 
@@ -424,7 +431,7 @@ class MatrixContext(_Handle):
     def _flat(self, t, name: str) -> Optional[int]:
         if t is not None and _elem_type(t) != self.elem_type:
             raise ArTopkError(-1, f"{name} is {t.dtype}, which is not the handle's type")
-        return _vector(t, name, self.n)
+        return _vector(t, name, self.n, self._device)
 
     def artopk_orthogonalize(self, x, out, steps: int = 5, coefficients=None, eps: float = 1e-7):
         self._check(self._lib.artopk_orthogonalize(self._h, self._flat(x, "x"), self._flat(out, "out"), int(steps),
@@ -434,7 +441,7 @@ class MatrixContext(_Handle):
                          decay: float = 0.0, eta_rest: float = 0.0, update_scale: float = 1.0, steps: int = 5,
                          coefficients=None, eps: float = 1e-7):
         self._check(self._lib.artopk_muon_step(
-            self._h, self._flat(weights, "weights"), _vector(momentum, "momentum", self.n, ARTOPK_G_F32),
-            _vector(update, "update", self.n, ARTOPK_G_F32), update_scale, mu, int(nesterov),
+            self._h, self._flat(weights, "weights"), _vector(momentum, "momentum", self.n, self._device, ARTOPK_G_F32),
+            _vector(update, "update", self.n, self._device, ARTOPK_G_F32), update_scale, mu, int(nesterov),
             eta, decay, eta_rest, int(steps), _coefficients(int(steps), coefficients),
             eps))

@@ -360,3 +360,20 @@ def test_what_lies_between_rows_does_not_matter(t, rows, cols):
             found.append((y, mean, rstd, dx, dg, db))
         for u, v in zip(*found):
             assert torch.equal(u, v) and not bool(u.isnan().any()), (pad, u.shape)
+
+
+def test_tensors_of_the_host_are_refused():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    ctx = lib.NormContext(4, 8)
+    x, y, v, w = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(4, device="cuda")
+    ctx.artopk_layernorm_forward(x, v, v, y, w, w.clone())
+    for args in ((x.cpu(), v, v, y), (x, v.cpu(), v, y), (x, v, v.cpu(), y), (x, v, v, y.cpu()), (x, v, v, y, w.cpu()), (x, v, v, y, w, w.cpu())):
+        with pytest.raises(lib.ArTopkError, match="cpu"):
+            ctx.artopk_layernorm_forward(*args)
+    good = [y, x, v, w, w.clone(), torch.zeros_like(x), v.clone(), v.clone()]
+    ctx.artopk_layernorm_backward(*good)
+    for i in range(len(good)):
+        with pytest.raises(lib.ArTopkError, match="cpu"):
+            ctx.artopk_layernorm_backward(*good[:i], good[i].cpu(), *good[i + 1:])

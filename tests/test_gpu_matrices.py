@@ -388,3 +388,18 @@ def test_default_products_are_one_of_the_two():
             results.append((out, w, m))
         for a, b in zip(*results):
             assert torch.equal(a, b), (t, shapes)
+
+
+def test_tensors_of_the_host_are_refused():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    ctx = lib.MatrixContext([(0, 3, 4)], 12)
+    v = [torch.ones(12, device="cuda") for _ in range(3)]
+    for i in range(3):
+        with pytest.raises(lib.ArTopkError, match="cpu"):
+            ctx.artopk_muon_step(*v[:i], v[i].cpu(), *v[i + 1:], eta=0.1)
+    for i in range(2):
+        with pytest.raises(lib.ArTopkError, match="cpu"):
+            ctx.artopk_orthogonalize(*v[:i], v[i].cpu(), *v[i + 1:2])
+    assert all(bool((t == 1.0).all()) for t in v)
