@@ -488,12 +488,14 @@ typedef struct artopk_matrix {
 typedef struct artopk_matrices artopk_matrices;
 
 /* How many bits the operands of the matrix products keep.  HALF: 11 (float16, scaled by powers of
- * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32.
- * DEFAULT: as many as the result shows.  Five steps leave a matrix some 1e-3 off with HALF (4e-3 of 16
- * rows) and 1e-6 with SPLIT, so it takes SPLIT for float32 and float16; for bfloat16 in
- * artopk_orthogonalize where the matrices of at most 256 rows or columns (the fewer of the two) have more than
- * half of all, and HALF otherwise and in artopk_muon_step (the weights' own rounding is coarser than the
- * step's error). */
+ * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32.  Five steps leave a
+ * matrix some 1e-6 off with SPLIT; with HALF 1e-3 to 2e-3 (4e-3 where all singular values are the same), and up to 9e-3
+ * with fewer than 64 rows or columns (the fewer of the two).
+ * DEFAULT takes SPLIT for float32 and float16, and for bfloat16, whose own rounding is 1.7e-3, matrix by matrix: SPLIT for
+ * those of fewer than 64 rows or columns, HALF for the others; in artopk_orthogonalize SPLIT for all where the matrices of
+ * at most 256 rows or columns have more than half of all.  In artopk_muon_step HALF's part of the error is that of the
+ * step: next to weights much larger than their step it is lost in their rounding, but weights that start from zero show
+ * it whole.  Ask for SPLIT where that matters. */
 enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1, ARTOPK_PRODUCTS_DEFAULT = -1 };
 
 #define ARTOPK_MAX_POLAR_STEPS 32
@@ -503,7 +505,8 @@ enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1, ARTOPK_PRODUCTS_DEFA
  * host array of `count` matrices (1 .. 65535), each within the vector, none overlapping another,
  * rows and cols in [1, 65536], scale finite; it is read before the call returns.  The iterates' memory
  * is allocated here: artopk_matrices_scratch_bytes(..) bytes, 4 for each element of a matrix and 6 for each of its
- * Gram matrix with HALF, of sides padded to multiples of 64, twice that where an entry point takes SPLIT, and the tables
+ * Gram matrix with HALF, of sides padded to multiples of 64, twice that for matrices that take SPLIT in an entry point, the
+ * partial sums of Gram matrices that are summed in shares, and the tables
  * (-1 for arguments that create refuses).  The tables are copied
  * to the device synchronously.  On failure *out is left alone and artopk_last_error(NULL) tells why.
  */

@@ -35,21 +35,28 @@ struct Product {
   int cls = 0;
 };
 
-// What creation works out on the host: where everything lies, and the tables.
-struct MatPlan {
-  std::vector<MatDesc> mats;
-  std::vector<MatChunk> chunks;
-  std::vector<MatTile> tiles;
+// The matrices whose products are of one kind, and what their launches work on.
+struct Group {
+  int parts = 1;             // of an operand
+  int first = 0, count = 0;  // in the table of matrices
   Span begin;
   Product gram, square, apply;
   Span join;  // the tiles of Gram matrices whose sums are cut
+  bool pairs = false;    // two steps at once
+  size_t small_lds = 0;  // of every matrix on one compute unit, in one launch; 0: not so
+  int64_t partial = 0;   // where the sums of its Gram products' shares lie, in floats
+};
+
+// What creation works out on the host: where everything lies, and the tables.
+struct MatPlan {
+  std::vector<MatDesc> mats;  // group by group
+  std::vector<MatChunk> chunks;
+  std::vector<MatTile> tiles;
+  Group groups[2];
+  int ngroups = 0;
   int64_t halves = 0;  // of the iterates' memory
+  int64_t partial = 0;  // floats of the sums of shares
   int32_t sums = 0;
-  bool pairs = false;  // two steps at once
-  bool small = false;  // every matrix on one compute unit, in one launch
-  size_t small_lds = 0;
-  int64_t slots = 0;   // partial sums of the Gram products' shares
-  int parts = 1;       // of an operand
 };
 
 // What a product's block costs, in us, by tile class: alone on its compute unit (`fixed` and `alone` for each 64 of the
@@ -165,13 +172,13 @@ double small_cost(const std::vector<MatDesc>& mats, int parts, size_t lds) {
 // The blocks of one kind of product, in the order in which they start.  Blocks go to the chip's eight dies in turn, and
 // each die has a cache of its own: the tiles of all matrices with equally long sums are cut into eight runs of neighbours,
 // one for each die, and the longest sums come first.  (Every matrix cut into eight instead: Q X of sixteen 1280 x 1280
-// and eight 1280 x 5120 234 us, so 228.)
-void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
+// and eight 1280 x 5120 234 us, so 228.)  `slots` counts the places of shares' sums.
+void list_product(MatPlan* plan, const std::vector<MatDesc>& mats, const ProductKind& k, Product* p, int each, int64_t* slots) {
   const int tile = kTileOf[p->cls];
-  std::vector<int> order(plan->mats.size());
+  std::vector<int> order(mats.size());
   for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
   auto units = [&](int i) {
-    const MatDesc& d = plan->mats[i];
+    const MatDesc& d = mats[i];
     return (k.long_sum ? d.np : d.mp) / 64 / product_shares(d, k, each);
   };
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return units(a) > units(b); });
@@ -183,7 +190,7 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
     const int here = units(order[o]);
     for (; o < order.size() && units(order[o]) == here; ++o) {
       const int i = order[o];
-      const MatDesc& d = plan->mats[i];
+      const MatDesc& d = mats[i];
       const int a = tiles_of(d.mp, tile), b = tiles_of(d.np, tile);
       const int shares = product_shares(d, k, each);
       constexpr int kBand = 4;  // rows of tiles taken together
@@ -196,8 +203,8 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
             t.i = (uint16_t)x;
             t.j = (uint16_t)y;
             t.shares = (uint16_t)shares;
-            t.slot = (uint32_t)plan->slots;
-            if (shares > 1) plan->slots += shares;
+            t.slot = (uint32_t)*slots;
+            if (shares > 1) *slots += shares;
             for (int s = 0; s < shares; ++s) {
               t.share = (uint16_t)s;
               own.push_back(t);
@@ -223,12 +230,62 @@ void list_product(MatPlan* plan, const ProductKind& k, Product* p, int each) {
   p->tiles.count = (int)(plan->tiles.size() - p->tiles.at);
 }
 
-// ARTOPK_OK, or ARTOPK_EINVAL with the reason in `err`.  Throws std::bad_alloc.
-int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int parts, MatPlan* plan, char* err) {
+// Places of a group's matrices in the iterates' memory, and its lists of blocks; `mats` are those of the table from
+// group->first on.
+void plan_group(MatPlan* plan, Group* g) {
+  const std::vector<MatDesc> bare(plan->mats.begin() + g->first, plan->mats.begin() + g->first + g->count);
+  const ProductKind gram = {true, true}, square = {true, false}, apply = {false, false};
+  int each = 0;
+  const double cost_gram = choose_product(bare, gram, g->parts, &g->gram, &each);
+  const double cost_square = choose_product(bare, square, g->parts, &g->square, nullptr);
+  const double cost_apply = choose_product(bare, apply, g->parts, &g->apply, nullptr);
+  const double cost = cost_gram + cost_square + cost_apply;
+  g->pairs = cost_gram + 5.0 * cost_square + cost_apply < 0.9 * 2.0 * cost;  // (not for a little: it rounds more)
+  bool small = true;
+  size_t lds = 0;
+  for (const MatDesc& d : bare) {
+    const int64_t bytes = 2 * small_halves(d.m, d.n, g->parts);
+    small &= bytes <= kSmallLds && (int64_t)small_pad(d.m) * small_pad(d.n) <= kSmallElems;
+    lds = std::max(lds, (size_t)bytes);
+  }
+  if (small && small_cost(bare, g->parts, lds) < cost) {
+    g->small_lds = lds;
+    return;
+  }
+  for (int i = g->first; i < g->first + g->count; ++i) {
+    MatDesc& d = plan->mats[i];
+    const int64_t mn = (int64_t)d.mp * d.np * g->parts, mm = (int64_t)d.mp * d.mp * g->parts;
+    d.x[0] = plan->halves;
+    d.x[1] = d.x[0] + mn;
+    for (int k = 0; k < 3; ++k) d.sq[k] = d.x[1] + mn + k * mm;
+    plan->halves = d.sq[2] + mm;
+  }
+  const std::vector<MatDesc> mats(plan->mats.begin() + g->first, plan->mats.begin() + g->first + g->count);
+  g->begin.at = plan->tiles.size();
+  for (const MatDesc& d : mats)
+    for (int a = 0; a < d.mp / 64; ++a)
+      for (int b = 0; b < d.np / 64; ++b) plan->tiles.push_back(MatTile{d, (uint16_t)a, (uint16_t)b, 0, 1, 0});
+  g->begin.count = (int)(plan->tiles.size() - g->begin.at);
+  int64_t slots = 0;
+  list_product(plan, mats, gram, &g->gram, each, &slots);
+  g->join.at = plan->tiles.size();
+  for (int i = 0; i < g->gram.tiles.count; ++i) {
+    const MatTile t = plan->tiles[g->gram.tiles.at + i];
+    if (t.shares > 1 && t.share == 0) plan->tiles.push_back(t);
+  }
+  g->join.count = (int)(plan->tiles.size() - g->join.at);
+  g->partial = plan->partial;
+  plan->partial += slots * kTileOf[g->gram.cls] * kTileOf[g->gram.cls];
+  list_product(plan, mats, square, &g->square, 0, &slots);
+  list_product(plan, mats, apply, &g->apply, 0, &slots);
+}
+
+// `parts`: of each matrix's operands.  ARTOPK_OK, or ARTOPK_EINVAL with the reason in `err`.  Throws std::bad_alloc.
+int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, const std::vector<int>& parts, MatPlan* plan,
+              char* err) {
   if (n < 1 || n >= (1ll << 31)) return fail_text(err, ARTOPK_EINVAL, "n=%lld outside [1, 2^31)", (long long)n);
   if (type != ARTOPK_G_F32 && type != ARTOPK_G_BF16 && type != ARTOPK_G_F16)
     return fail_text(err, ARTOPK_EINVAL, "unknown element type %d", type);
-  plan->parts = parts;
   std::vector<int32_t> order(count);
   for (int i = 0; i < count; ++i) {
     const artopk_matrix& m = mats[i];
@@ -247,22 +304,27 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
       return fail_text(err, ARTOPK_EINVAL, "matrices %d and %d overlap", order[i - 1], order[i]);
   }
 
-  plan->mats.resize(count);
-  for (int i = 0; i < count; ++i) {
-    const artopk_matrix& m = mats[i];
-    MatDesc& d = plan->mats[i];
-    d.at = m.offset;
-    d.tall = m.rows > m.cols;
-    d.m = std::min(m.rows, m.cols);
-    d.n = std::max(m.rows, m.cols);
-    d.scale = m.scale;
-    d.mp = (d.m + 63) / 64 * 64;
-    d.np = (d.n + 63) / 64 * 64;
-    const int64_t mn = (int64_t)d.mp * d.np * parts, mm = (int64_t)d.mp * d.mp * parts;
-    d.x[0] = plan->halves;
-    d.x[1] = d.x[0] + mn;
-    for (int k = 0; k < 3; ++k) d.sq[k] = d.x[1] + mn + k * mm;
-    plan->halves = d.sq[2] + mm;
+  std::vector<int> place(count);  // of a matrix in the table
+  for (int kind = 1; kind <= 2; ++kind) {
+    Group g;
+    g.parts = kind;
+    g.first = (int)plan->mats.size();
+    for (int i = 0; i < count; ++i) {
+      if (parts[i] != kind) continue;
+      const artopk_matrix& m = mats[i];
+      MatDesc d = {};
+      d.at = m.offset;
+      d.tall = m.rows > m.cols;
+      d.m = std::min(m.rows, m.cols);
+      d.n = std::max(m.rows, m.cols);
+      d.scale = m.scale;
+      d.mp = (d.m + 63) / 64 * 64;
+      d.np = (d.n + 63) / 64 * 64;
+      place[i] = (int)plan->mats.size();
+      plan->mats.push_back(d);
+    }
+    g.count = (int)plan->mats.size() - g.first;
+    if (g.count) plan->groups[plan->ngroups++] = g;
   }
 
   // pieces of the vector, those of a matrix side by side; at most 512 a matrix, so that every block that needs its norm
@@ -273,7 +335,7 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
     done = end;
   };
   for (int k = 0; k < count; ++k) {
-    const int i = order[k];
+    const int i = place[order[k]];
     MatDesc& d = plan->mats[i];
     loose(d.at);
     const int64_t size = (int64_t)d.m * d.n, end = d.at + size;
@@ -286,58 +348,16 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   }
   loose(n);
 
-  for (int i = 0; i < count; ++i)
-    for (int a = 0; a < plan->mats[i].mp / 64; ++a)
-      for (int b = 0; b < plan->mats[i].np / 64; ++b)
-        plan->tiles.push_back(MatTile{plan->mats[i], (uint16_t)a, (uint16_t)b, 0, 1, 0});
-  plan->begin.count = (int)plan->tiles.size();
-  plan->small = true;
-  for (const MatDesc& d : plan->mats) {
-    const int64_t bytes = 2 * small_halves(d.m, d.n, parts);
-    plan->small &= bytes <= kSmallLds && (int64_t)small_pad(d.m) * small_pad(d.n) <= kSmallElems;
-    plan->small_lds = std::max(plan->small_lds, (size_t)bytes);
-  }
-  const ProductKind gram = {true, true}, square = {true, false}, apply = {false, false};
-  int each = 0;
-  const double cost_gram = choose_product(plan->mats, gram, parts, &plan->gram, &each);
-  const double cost_square = choose_product(plan->mats, square, parts, &plan->square, nullptr);
-  const double cost_apply = choose_product(plan->mats, apply, parts, &plan->apply, nullptr);
-  const double cost = cost_gram + cost_square + cost_apply;
-  plan->pairs = cost_gram + 5.0 * cost_square + cost_apply < 0.9 * 2.0 * cost;  // (not for a little: it rounds more)
-  if (plan->small) plan->small = small_cost(plan->mats, parts, plan->small_lds) < cost;
-  if (plan->small) {
-    plan->tiles.clear();
-    plan->begin.count = 0;
-    plan->halves = 0;
-  } else {
-    plan->small_lds = 0;
-  }
-  if (!plan->small) {
-    list_product(plan, gram, &plan->gram, each);
-    plan->join.at = plan->tiles.size();
-    for (int i = 0; i < plan->gram.tiles.count; ++i) {
-      const MatTile t = plan->tiles[plan->gram.tiles.at + i];
-      if (t.shares > 1 && t.share == 0) plan->tiles.push_back(t);
-    }
-    plan->join.count = (int)(plan->tiles.size() - plan->join.at);
-    list_product(plan, square, &plan->square, 0);
-    list_product(plan, apply, &plan->apply, 0);
-  }
+  for (int i = 0; i < plan->ngroups; ++i) plan_group(plan, &plan->groups[i]);
   if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
-
   return ARTOPK_OK;
 }
 
 // What an entry point launches on, with its places in the handle's memory.
 struct Route {
-  int parts = 1;
+  Group groups[2];
+  int ngroups = 0;
   int nchunks = 0;
-  Span begin;
-  Product gram, square, apply;
-  Span join;
-  int count = 0;
-  bool pairs = false;
-  size_t small_lds = 0;  // 0: not small
   const MatDesc* mats = nullptr;
   const MatChunk* chunks = nullptr;
   const MatTile* tiles = nullptr;
@@ -345,26 +365,28 @@ struct Route {
   float* partial = nullptr;
 };
 
-// The parts of an operand, for the entry point that gives a matrix itself or the one that steps weights by it.  By default
-// the products' roundings stay below the result's own: float16's is 0.2e-3, bfloat16's 1.6e-3.  Against 64 bits HALF is
-// 0.9e-3 to 1.3e-3 off from some 600 rows on, 1.5e-3 of 64 to 256, and more of fewer, whose singular values lie so close that
-// roundings go the same way (24 x 200 2.2e-3, 17 x 1300 2.9e-3, 16 x 3662 4.1e-3).  SPLIT costs little there, where launches
-// and latency count (64 x 64 20 us for 15.6, four of 468 x 24 and one of 162 x 1065 110 for 80, 24 of 256 x 1024 195 for
-// 120); so bfloat16 takes it where most of the result (its squared norm is its matrices' rows) is of at most 256 rows, and
-// float16 always.  A step of bfloat16 weights moves them by a small part of themselves, and HALF's share of that is far below
-// the rounding of the sum (of float16 weights, which it left 0.34e-3 off, it is not).
-constexpr int32_t kFewRows = 256;
-int parts_for(const artopk_matrix* mats, int32_t count, int32_t type, int32_t products, bool weights) {
-  if (products != ARTOPK_PRODUCTS_DEFAULT) return products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1;
-  if (type != ARTOPK_G_BF16) return 2;
-  if (weights) return 1;
+// The parts of each matrix's operands, for the entry point that gives a matrix itself or the one that steps weights by it.
+// float16's own rounding is 0.2e-3, and HALF would show in it: it takes SPLIT always.  bfloat16's is 1.7e-3.  Against 64 bits
+// HALF is 0.9e-3 to 2.3e-3 off from 64 rows on (the worst of Gaussian, low-rank and graded matrices; 3.6e-3 where all singular
+// values are the same, so that all roundings go the same way), and of fewer rows up to 9e-3 (4 x 4096), 7e-3 (48 x 4096), 4e-3
+// (24 x 384).  So matrices of fewer than 64 rows take SPLIT, whatever lies beside them in the vector: it costs little there,
+// where launches and latency count (a second group of launches, 20 us for 16 in one launch).  artopk_orthogonalize, whose
+// result is nothing but X, takes it for all matrices where most of the result (its squared norm is its matrices' rows) is of at
+// most 256 rows (24 of 256 x 1024 195 us for 120); weights are a sum, of which X is usually the smaller part.
+constexpr int32_t kFewRows = 256, kSplitBelow = 64;
+std::vector<int> parts_for(const artopk_matrix* mats, int32_t count, int32_t type, int32_t products, bool weights) {
+  if (products != ARTOPK_PRODUCTS_DEFAULT) return std::vector<int>(count, products == ARTOPK_PRODUCTS_SPLIT ? 2 : 1);
+  if (type != ARTOPK_G_BF16) return std::vector<int>(count, 2);
+  std::vector<int> parts(count);
   int64_t all = 0, few = 0;
   for (int32_t i = 0; i < count; ++i) {
     const int32_t rows = std::min(mats[i].rows, mats[i].cols);
+    parts[i] = rows < kSplitBelow ? 2 : 1;
     all += rows;
     if (rows <= kFewRows) few += rows;
   }
-  return 2 * few > all ? 2 : 1;
+  if (!weights && 2 * few > all) parts.assign(count, 2);
+  return parts;
 }
 
 // Both entry points' plans, and the places of their tables; the iterates' memory is used by one call at a time.
@@ -379,7 +401,7 @@ int make_plans(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type
   if (count < 1 || count > kMaxMatrices) return fail_text(err, ARTOPK_EINVAL, "count=%d outside [1, %d]", count, kMaxMatrices);
   if (products != ARTOPK_PRODUCTS_HALF && products != ARTOPK_PRODUCTS_SPLIT && products != ARTOPK_PRODUCTS_DEFAULT)
     return fail_text(err, ARTOPK_EINVAL, "unknown kind of products %d", products);
-  const int own = parts_for(mats, count, type, products, false), weights = parts_for(mats, count, type, products, true);
+  const std::vector<int> own = parts_for(mats, count, type, products, false), weights = parts_for(mats, count, type, products, true);
   p->count = own == weights ? 1 : 2;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -396,7 +418,7 @@ int make_plans(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type
     p->o_chunks[i] = take(plan.chunks.size() * sizeof(MatChunk));
     p->o_tiles[i] = take(plan.tiles.size() * sizeof(MatTile));
     p->o_sums[i] = take((size_t)plan.sums * sizeof(double));
-    p->o_partial[i] = take((size_t)plan.slots * kTileOf[plan.gram.cls] * kTileOf[plan.gram.cls] * sizeof(float));
+    p->o_partial[i] = take((size_t)plan.partial * sizeof(float));
     halves = std::max(halves, plan.halves);
   }
   p->o_mem = take((size_t)halves * 2);
@@ -475,54 +497,50 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 }
 
 template <int TILE, int PARTS, int MODE>
-void product(const artopk_matrices* h, const Route& r, const Span& s, const ProductArgs& a, const FinishArgs& f) {
+void product(const artopk_matrices* h, const Route& r, const Group& g, const Span& s, const ProductArgs& a, const FinishArgs& f) {
   k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(r.tiles + s.at, h->mem, a, f,
-                                                                                                  r.partial);
+                                                                                                  r.partial + g.partial);
 }
 
 template <int PARTS, int MODE>
-void product(const artopk_matrices* h, const Route& r, const Product& p, const ProductArgs& a, const FinishArgs& f) {
+void product(const artopk_matrices* h, const Route& r, const Group& g, const Product& p, const ProductArgs& a, const FinishArgs& f) {
   switch (p.cls) {
-    case 0: return product<64, PARTS, MODE>(h, r, p.tiles, a, f);
-    case 1: return product<128, PARTS, MODE>(h, r, p.tiles, a, f);
-    case 2: return product<192, PARTS, MODE>(h, r, p.tiles, a, f);
-    case 3: return product<256, PARTS, MODE>(h, r, p.tiles, a, f);
-    default: return product<64 + (PARTS == 2 ? kDeep : 0), PARTS, MODE>(h, r, p.tiles, a, f);
+    case 0: return product<64, PARTS, MODE>(h, r, g, p.tiles, a, f);
+    case 1: return product<128, PARTS, MODE>(h, r, g, p.tiles, a, f);
+    case 2: return product<192, PARTS, MODE>(h, r, g, p.tiles, a, f);
+    case 3: return product<256, PARTS, MODE>(h, r, g, p.tiles, a, f);
+    default: return product<64 + (PARTS == 2 ? kDeep : 0), PARTS, MODE>(h, r, g, p.tiles, a, f);
   }
 }
 
 template <int TILE, int PARTS>
-void join_shares(const artopk_matrices* h, const Route& r) {
-  k_mat_join<TILE, PARTS><<<dim3(r.join.count, 2), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
-      r.tiles + r.join.at, h->mem, r.partial);
+void join_shares(const artopk_matrices* h, const Route& r, const Group& g) {
+  k_mat_join<TILE, PARTS><<<dim3(g.join.count, 2), ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(
+      r.tiles + g.join.at, h->mem, r.partial + g.partial);
 }
 
-// What the squares' or the momentum's launch leaves to do.
+// All steps of a group's matrices.
 template <int PARTS, class From>
-void polar(const artopk_matrices* h, const Route& r, From from, const Steps& st, float eps, const FinishArgs& f) {
-  if (st.count == 0) {
-    k_mat_scaled<From><<<r.nchunks, 256, 0, h->stream>>>(from, r.mats, r.chunks, r.sums, eps, f);
-    return;
-  }
-  if (r.small_lds) {
+void polar(const artopk_matrices* h, const Route& r, const Group& g, From from, const Steps& st, float eps, const FinishArgs& f) {
+  if (g.small_lds) {
     PolarSteps ps = {};
     ps.steps = st.count;
     memcpy(ps.co, st.co, sizeof(float) * 3 * st.count);
-    k_mat_small<PARTS, From><<<r.count, kSmallThreads, r.small_lds, h->stream>>>(from, r.mats, ps, eps, f);
+    k_mat_small<PARTS, From><<<g.count, kSmallThreads, g.small_lds, h->stream>>>(from, r.mats + g.first, ps, eps, f);
     return;
   }
-  k_mat_begin<PARTS, From><<<r.begin.count, 256, 0, h->stream>>>(from, r.tiles + r.begin.at, r.sums, eps, h->mem);
+  k_mat_begin<PARTS, From><<<g.begin.count, 256, 0, h->stream>>>(from, r.tiles + g.begin.at, r.sums, eps, h->mem);
   int x = 0;  // which X
   auto square = [&](int k, int in, int out) {
-    product<PARTS, kSquare>(h, r, r.square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2]}, f);
+    product<PARTS, kSquare>(h, r, g, g.square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2]}, f);
   };
-  auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, r, r.square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
+  auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, r, g, g.square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
   for (int k = 0; k < st.count;) {
-    product<PARTS, kGram>(h, r, r.gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
-    if (r.join.count) kTileOf[r.gram.cls] == 64 ? join_shares<64, PARTS>(h, r) : join_shares<128, PARTS>(h, r);
+    product<PARTS, kGram>(h, r, g, g.gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
+    if (g.join.count) kTileOf[g.gram.cls] == 64 ? join_shares<64, PARTS>(h, r, g) : join_shares<128, PARTS>(h, r, g);
     square(k, 0, 1);
     int q = 1;
-    if (r.pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {
+    if (g.pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {
       times(1, 0, 2);      // Q_1 A_0
       times(2, 1, 0);      // A_1
       square(k + 1, 0, 2);  // Q_2
@@ -533,19 +551,27 @@ void polar(const artopk_matrices* h, const Route& r, From from, const Steps& st,
     ++k;
     const ProductArgs a = {x, q, 0, 0, 0, 0, 0};
     if (k < st.count)
-      product<PARTS, kApply>(h, r, r.apply, a, f);
+      product<PARTS, kApply>(h, r, g, g.apply, a, f);
     else
-      product<PARTS, kFinal>(h, r, r.apply, a, f);
+      product<PARTS, kFinal>(h, r, g, g.apply, a, f);
     x ^= 1;
   }
 }
 
+// What the squares' or the momentum's launch leaves to do.
 template <class From>
 void polar(const artopk_matrices* h, const Route& r, From from, const Steps& st, float eps, const FinishArgs& f) {
-  if (r.parts == 2)
-    polar<2>(h, r, from, st, eps, f);
-  else
-    polar<1>(h, r, from, st, eps, f);
+  if (st.count == 0) {
+    k_mat_scaled<From><<<r.nchunks, 256, 0, h->stream>>>(from, r.mats, r.chunks, r.sums, eps, f);
+    return;
+  }
+  for (int i = 0; i < r.ngroups; ++i) {
+    const Group& g = r.groups[i];
+    if (g.parts == 2)
+      polar<2>(h, r, g, from, st, eps, f);
+    else
+      polar<1>(h, r, g, from, st, eps, f);
+  }
 }
 
 // Calls f with a null pointer of the handle's element type.
@@ -622,16 +648,9 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
   for (int i = 0; i < plans.count && e == hipSuccess; ++i) {
     const MatPlan& plan = plans.plan[i];
     Route& r = i == 0 ? h->own : h->weights;
-    r.parts = plan.parts;
     r.nchunks = (int)plan.chunks.size();
-    r.begin = plan.begin;
-    r.gram = plan.gram;
-    r.square = plan.square;
-    r.apply = plan.apply;
-    r.join = plan.join;
-    r.count = (int)plan.mats.size();
-    r.pairs = plan.pairs;
-    r.small_lds = plan.small ? plan.small_lds : 0;
+    r.ngroups = plan.ngroups;
+    for (int g = 0; g < plan.ngroups; ++g) r.groups[g] = plan.groups[g];
     r.mats = reinterpret_cast<const MatDesc*>(h->slab + plans.o_mats[i]);
     r.chunks = reinterpret_cast<const MatChunk*>(h->slab + plans.o_chunks[i]);
     r.tiles = reinterpret_cast<const MatTile*>(h->slab + plans.o_tiles[i]);
@@ -643,7 +662,8 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
     fill(plans.o_mats[i], plan.mats.data(), plan.mats.size() * sizeof(MatDesc));
     fill(plans.o_chunks[i], plan.chunks.data(), plan.chunks.size() * sizeof(MatChunk));
     fill(plans.o_tiles[i], plan.tiles.data(), plan.tiles.size() * sizeof(MatTile));
-    if (e == hipSuccess && r.small_lds) e = r.parts == 2 ? allow_small<2>(h) : allow_small<1>(h);
+    for (int g = 0; g < r.ngroups; ++g)
+      if (e == hipSuccess && r.groups[g].small_lds) e = r.groups[g].parts == 2 ? allow_small<2>(h) : allow_small<1>(h);
   }
   if (plans.count == 1) h->weights = h->own;
   if (e != hipSuccess) {
@@ -683,7 +703,9 @@ int artopk_orthogonalize(artopk_matrices* m, const void* x, void* out, int32_t s
   with_type(m->type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     const Route& r = m->own;
-    if (!r.small_lds || steps == 0) k_mat_squares<T><<<r.nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), r.chunks, r.sums);
+    bool sums = steps == 0;  // (small matrices' blocks sum for themselves)
+    for (int i = 0; i < r.ngroups; ++i) sums |= r.groups[i].small_lds == 0;
+    if (sums) k_mat_squares<T><<<r.nchunks, 256, 0, m->stream>>>(static_cast<const T*>(x), r.chunks, r.sums);
     polar(m, r, FromVector<T>{static_cast<const T*>(x)}, st, eps, f);
   });
   MAT_TRY(m, hipGetLastError());
