@@ -320,7 +320,7 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
       d.scale = m.scale;
       d.mp = (d.m + 63) / 64 * 64;
       d.np = (d.n + 63) / 64 * 64;
-      place[i] = (int)plan->mats.size();
+      place[i] = d.id = (int)plan->mats.size();
       plan->mats.push_back(d);
     }
     g.count = (int)plan->mats.size() - g.first;
@@ -362,6 +362,7 @@ struct Route {
   const MatChunk* chunks = nullptr;
   const MatTile* tiles = nullptr;
   double* sums = nullptr;
+  float* sizes = nullptr;  // of every matrix, s with ||X_0|| < 2^s
   float* partial = nullptr;
 };
 
@@ -393,7 +394,7 @@ std::vector<int> parts_for(const artopk_matrix* mats, int32_t count, int32_t typ
 struct Plans {
   MatPlan plan[2];
   int count = 1;  // 1: they are the same
-  size_t o_mats[2], o_chunks[2], o_tiles[2], o_sums[2], o_partial[2], o_mem = 0, total = 0;
+  size_t o_mats[2], o_chunks[2], o_tiles[2], o_sums[2], o_sizes[2], o_partial[2], o_mem = 0, total = 0;
 };
 
 int make_plans(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products, Plans* p, char* err) {
@@ -418,6 +419,7 @@ int make_plans(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type
     p->o_chunks[i] = take(plan.chunks.size() * sizeof(MatChunk));
     p->o_tiles[i] = take(plan.tiles.size() * sizeof(MatTile));
     p->o_sums[i] = take((size_t)plan.sums * sizeof(double));
+    p->o_sizes[i] = take(plan.mats.size() * sizeof(float));
     p->o_partial[i] = take((size_t)plan.partial * sizeof(float));
     halves = std::max(halves, plan.halves);
   }
@@ -452,6 +454,7 @@ struct Steps {
   int count = 0;
   float co[ARTOPK_MAX_POLAR_STEPS][3];
   double factor[ARTOPK_MAX_POLAR_STEPS];  // the largest |a + b s^2 + c s^4|
+  float grown[ARTOPK_MAX_POLAR_STEPS + 1];  // log2 of the factors before each step and behind the last, multiplied
 };
 constexpr double kMostFactor = 15.0;
 
@@ -461,8 +464,9 @@ constexpr double kMostFactor = 15.0;
 int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficients, Steps* st) {
   if (steps < 0 || steps > ARTOPK_MAX_POLAR_STEPS)
     return fail_text(h->err, ARTOPK_EINVAL, "steps=%d outside [0, %d]", steps, ARTOPK_MAX_POLAR_STEPS);
-  double most = 1.0;
+  double most = 1.0, grown = 0.0;
   st->count = steps;
+  st->grown[0] = 0.0f;
   for (int k = 0; k < steps; ++k) {
     float* out = st->co[k];
     for (int i = 0; i < 3; ++i) out[i] = coefficients ? coefficients[3 * k + i] : kUsual[i];
@@ -487,6 +491,8 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
     }
     if (b != 0.0) look(-a / (3.0 * b));  // (c = 0; an extra point otherwise)
     st->factor[k] = factor;
+    grown += std::log2(factor);  // (minus infinity where nothing is left)
+    st->grown[k + 1] = (float)grown;
     if (next > 2.0 || factor > kMostFactor)
       return fail_text(h->err, ARTOPK_EINVAL,
                        "step %d would take singular values up to %.4g to %.4g, with a factor of %.4g; at most 2 and 15 are taken", k,
@@ -499,7 +505,7 @@ int take_coefficients(artopk_matrices* h, int32_t steps, const float* coefficien
 template <int TILE, int PARTS, int MODE>
 void product(const artopk_matrices* h, const Route& r, const Group& g, const Span& s, const ProductArgs& a, const FinishArgs& f) {
   k_mat_product<TILE, PARTS, MODE><<<s.count, ProductShape<TILE, PARTS>::kThreads, 0, h->stream>>>(r.tiles + s.at, h->mem, a, f,
-                                                                                                  r.partial + g.partial);
+                                                                                                  r.partial + g.partial, r.sizes);
 }
 
 template <int PARTS, int MODE>
@@ -526,30 +532,34 @@ void polar(const artopk_matrices* h, const Route& r, const Group& g, From from, 
     PolarSteps ps = {};
     ps.steps = st.count;
     memcpy(ps.co, st.co, sizeof(float) * 3 * st.count);
+    memcpy(ps.grown, st.grown, sizeof(float) * st.count);
     k_mat_small<PARTS, From><<<g.count, kSmallThreads, g.small_lds, h->stream>>>(from, r.mats + g.first, ps, eps, f);
     return;
   }
-  k_mat_begin<PARTS, From><<<g.begin.count, 256, 0, h->stream>>>(from, r.tiles + g.begin.at, r.sums, eps, h->mem);
+  k_mat_begin<PARTS, From><<<g.begin.count, 256, 0, h->stream>>>(from, r.tiles + g.begin.at, r.sums, eps, h->mem, r.sizes);
   int x = 0;  // which X
   auto square = [&](int k, int in, int out) {
-    product<PARTS, kSquare>(h, r, g, g.square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2]}, f);
+    product<PARTS, kSquare>(h, r, g, g.square, ProductArgs{x, in, in, out, st.co[k][0], st.co[k][1], st.co[k][2], st.grown[k], 0}, f);
   };
-  auto times = [&](int in, int in2, int out) { product<PARTS, kTimes>(h, r, g, g.square, ProductArgs{x, in, in2, out, 0, 0, 0}, f); };
+  auto times = [&](int in, int in2, int out, float grown, float then) {
+    product<PARTS, kTimes>(h, r, g, g.square, ProductArgs{x, in, in2, out, 0, 0, 0, grown, then}, f);
+  };
   for (int k = 0; k < st.count;) {
-    product<PARTS, kGram>(h, r, g, g.gram, ProductArgs{x, 0, 0, 0, 0, 0, 0}, f);
+    const float grown = st.grown[k];
+    product<PARTS, kGram>(h, r, g, g.gram, ProductArgs{x, 0, 0, 0, 0, 0, 0, 0, 0}, f);
     if (g.join.count) kTileOf[g.gram.cls] == 64 ? join_shares<64, PARTS>(h, r, g) : join_shares<128, PARTS>(h, r, g);
     square(k, 0, 1);
     int q = 1;
     if (g.pairs && k + 1 < st.count && st.factor[k] * st.factor[k + 1] <= kMostFactor) {
-      times(1, 0, 2);      // Q_1 A_0
-      times(2, 1, 0);      // A_1
-      square(k + 1, 0, 2);  // Q_2
-      times(2, 1, 0);      // Q_2 Q_1
+      times(1, 0, 2, 0, 0);                    // Q_1 A_0, as large as A_0 is stored
+      times(2, 1, 0, grown, st.grown[k + 1]);  // A_1
+      square(k + 1, 0, 2);                     // Q_2
+      times(2, 1, 0, 0, 0);                    // Q_2 Q_1
       q = 0;
       ++k;
     }
     ++k;
-    const ProductArgs a = {x, q, 0, 0, 0, 0, 0};
+    const ProductArgs a = {x, q, 0, 0, 0, 0, 0, grown, st.grown[k]};
     if (k < st.count)
       product<PARTS, kApply>(h, r, g, g.apply, a, f);
     else
@@ -655,6 +665,7 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
     r.chunks = reinterpret_cast<const MatChunk*>(h->slab + plans.o_chunks[i]);
     r.tiles = reinterpret_cast<const MatTile*>(h->slab + plans.o_tiles[i]);
     r.sums = reinterpret_cast<double*>(h->slab + plans.o_sums[i]);
+    r.sizes = reinterpret_cast<float*>(h->slab + plans.o_sizes[i]);
     r.partial = reinterpret_cast<float*>(h->slab + plans.o_partial[i]);
     auto fill = [&](size_t to, const void* from, size_t bytes) {
       if (e == hipSuccess && bytes) e = hipMemcpy(h->slab + to, from, bytes, hipMemcpyHostToDevice);

@@ -18,6 +18,10 @@
 // the steps multiply small singular values, and what roundings put there, by up to a^5 = 485.  With one part an operand
 // keeps 11 bits; with two (hi + lo, and hi hi + hi lo + lo hi for a product) 22, which leaves the result as exact as
 // float32 products do.
+// A matrix whose X is small, since its norm is below eps or its coefficients shrink it, would sink into float16's smallest
+// numbers so.  Its X_k is stored times another 2^e_k, A times 2^(2 e_k): with g the power of two above ||X_0|| times the largest
+// factors of the steps before, which ||X_k|| does not pass, e_k is the whole part of -log2(g), or 0 (as it is for every matrix
+// whose norm is above eps: growing iterates never need it).  Powers of two round nothing.
 //
 // Layout.  X X^T and A A^T (A is symmetric) have both operands' rows along the summed index, as the matrix cores take
 // them; in Q X the second operand's lie across it, and are turned on their way from LDS to registers.  (A second copy of
@@ -47,6 +51,7 @@ struct MatDesc {
   int64_t x[2];   // X before and after a step, in turn
   int64_t sq[3];  // A, Q and their products, m x m
   int32_t part, parts;  // its sums of squares
+  int32_t id;           // its own place in the table
 };
 
 // A piece of the flat vector inside one matrix, or of none (mat < 0).
@@ -151,12 +156,27 @@ __global__ __launch_bounds__(256) void k_mat_momentum(T* __restrict__ w, float* 
 __device__ __forceinline__ double inverse_of_norm(double squares, float eps) { return 1.0 / (sqrt(squares) + (double)eps); }
 __device__ __forceinline__ float normalised(float v, double by) { return static_cast<float>((double)v * by); }
 
-// The same from the sums of the matrix's pieces, in every thread of a block of 256.
-__device__ __forceinline__ double inverse_norm(const MatDesc& d, const double* sums, float eps, double* room) {
+// A matrix's sum of squares from those of its pieces, in every thread of a block of 256.
+__device__ __forceinline__ double all_squares(const MatDesc& d, const double* sums, double* room) {
   double s = 0.0;
   for (int i = threadIdx.x; i < d.parts; i += 256) s += sums[d.part + i];
-  return inverse_of_norm(block_sum(s, room), eps);
+  return block_sum(s, room);
 }
+
+// The whole number s with 2^(s - 1) <= ||X_0|| < 2^s, from the sum of squares and the inverse above.
+__device__ __forceinline__ float size_of(double squares, double inverse) {
+  int s;
+  (void)frexp(sqrt(squares) * inverse, &s);
+  return (float)s;
+}
+
+// e_k of a matrix with ||X_0|| < 2^size; `grown` is log2 of the largest factors of the steps before.  (Not beyond 110: 2^e
+// and its inverse times 2^12 stay ordinary float32 numbers.)
+__device__ __forceinline__ int exponent_of(float size, float grown) {
+  const float e = floorf(-(size + grown));
+  return e > 0.0f ? (int)fminf(e, 110.0f) : 0;  // (0 for NaN, too)
+}
+__device__ __forceinline__ float power_of_two(int e) { return ldexpf(1.0f, e); }
 
 template <int PARTS>
 __device__ __forceinline__ void split_half(float v, _Float16 (&out)[PARTS]) {
@@ -179,15 +199,18 @@ struct FromMomentum {
   }
 };
 
-// X_0, 64 x 64 elements a block, zeros beyond the true sizes.
+// X_0, 64 x 64 elements a block, zeros beyond the true sizes, and how large its norm is.
 template <int PARTS, class From>
 __global__ __launch_bounds__(256) void k_mat_begin(From from, const MatTile* __restrict__ tiles, const double* __restrict__ sums,
-                                                   float eps, _Float16* __restrict__ mem) {
+                                                   float eps, _Float16* __restrict__ mem, float* __restrict__ sizes) {
   __shared__ float tile[64][65];
   __shared__ double room[4];
   const MatTile& t = tiles[blockIdx.x];
   const MatDesc& d = t.d;
-  const double by = inverse_norm(d, sums, eps, room) * (double)kOperandScale;
+  const double squares = all_squares(d, sums, room), inverse = inverse_of_norm(squares, eps);
+  const float size = size_of(squares, inverse);
+  const double by = ldexp(inverse * (double)kOperandScale, exponent_of(size, 0.0f));
+  if (t.i == 0 && t.j == 0 && threadIdx.x == 0) sizes[d.id] = size;
   const int rows = d.tall ? d.n : d.m, cols = d.tall ? d.m : d.n;  // as they lie
   const int r0 = (d.tall ? t.j : t.i) * 64, c0 = (d.tall ? t.i : t.j) * 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -284,7 +307,7 @@ __global__ __launch_bounds__(256) void k_mat_scaled(From from, const MatDesc* __
   const MatChunk c = chunks[blockIdx.x];
   if (c.mat < 0) return;
   const MatDesc d = mats[c.mat];
-  const double by = inverse_norm(d, sums, eps, room);
+  const double by = inverse_of_norm(all_squares(d, sums, room), eps);
   for (int64_t i = c.begin + threadIdx.x; i < c.end; i += 256) {
     finish(f, i, normalised(from(i), by) * d.scale);
   }
@@ -298,6 +321,7 @@ struct ProductArgs {
   int32_t from;  // which X
   int32_t in, in2, out;
   float ca, cb, cc;
+  float grown, then;  // log2 of the largest factors of the steps before what is read, and before what is written
 };
 
 // The shape of a product's tile: TILE x TILE elements by WM x WN waves, the summed index in stages of kDepth, kStages of
@@ -695,7 +719,7 @@ constexpr int store_room() {
 // so, and with faster sums, 311).
 template <int FM, int FN, bool TALL>
 __device__ __forceinline__ void finish_rows(const f32x4 (&acc)[FM][FN], float* fl, int row0, int col0, const MatDesc& d,
-                                            const FinishArgs& f) {
+                                            const FinishArgs& f, float down) {
   const int lane = threadIdx.x & 63;
   constexpr int CC = FN * 16, HM = FM > 1 ? 2 : 1, HR = HM * 16;  // rows at a time
   constexpr int RUN = TALL ? HR : CC, PITCH = RUN + 4;            // as they lie
@@ -723,7 +747,7 @@ __device__ __forceinline__ void finish_rows(const f32x4 (&acc)[FM][FN], float* f
     for (int i = 0; i < HM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
-        const f32x4 v = acc[h + i][j] * by;
+        const f32x4 v = acc[h + i][j] * by * down;
         if constexpr (TALL) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) fl[(j * 16 + (lane >> 4) * 4 + e) * PITCH + i * 16 + (lane & 15)] = v[e];
@@ -761,7 +785,8 @@ __device__ __forceinline__ void finish_rows(const f32x4 (&acc)[FM][FN], float* f
 
 template <int SHAPE, int PARTS, int MODE>
 __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductShape<SHAPE, PARTS>::kBlocks)) void k_mat_product(
-    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, ProductArgs a, FinishArgs f, float* __restrict__ partial) {
+    const MatTile* __restrict__ tiles, _Float16* __restrict__ mem, ProductArgs a, FinishArgs f, float* __restrict__ partial,
+    const float* __restrict__ sizes) {
   using S = ProductShape<SHAPE, PARTS>;
   constexpr int TILE = S::TILE, FM = S::kOutM, FN = S::kFN;
   constexpr int kRoom = store_room<FM, FN>();
@@ -772,6 +797,7 @@ __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductSha
   const MatTile& t = tiles[blockIdx.x];
   const MatDesc& d = t.d;
   const int64_t mm = (int64_t)d.mp * d.mp, mn = (int64_t)d.mp * d.np;
+  const float size = MODE == kGram ? 0.0f : sizes[d.id];
   const int i0 = t.i * TILE, j0 = t.j * TILE;
   constexpr bool kTurned = MODE == kApply || MODE == kFinal;
   const int rows = d.mp, cols = kTurned ? d.np : d.mp;
@@ -796,6 +822,7 @@ __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductSha
   const int wave2 = wave % (S::kWM * S::kWN), group = wave / (S::kWM * S::kWN);
   const int row0 = i0 + wave2 / S::kWN * S::kRowsM + group * (FM * 16), col0 = j0 + wave2 % S::kWN * S::kRowsN;
   _Float16* room = lds + wave * kRoom;
+  const int up = MODE == kGram ? 0 : exponent_of(size, a.grown);
   if constexpr (MODE == kGram) {
     if (t.shares > 1) {  // the sums of this share, for k_mat_join
       f32x4* mine = reinterpret_cast<f32x4*>(partial + ((int64_t)t.slot + t.share) * (TILE * TILE)) + threadIdx.x;
@@ -809,14 +836,16 @@ __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductSha
   if constexpr (MODE == kFinal) {
     // Elements of a tall matrix lie column by column of X.  A few rows of the wave's part at a time go through LDS as floats, in
     // the order in which they lie.
+    const float down = power_of_two(-up);
     if (d.tall)
-      finish_rows<FM, FN, true>(acc, reinterpret_cast<float*>(room), row0, col0, d, f);
+      finish_rows<FM, FN, true>(acc, reinterpret_cast<float*>(room), row0, col0, d, f, down);
     else
-      finish_rows<FM, FN, false>(acc, reinterpret_cast<float*>(room), row0, col0, d, f);
+      finish_rows<FM, FN, false>(acc, reinterpret_cast<float*>(room), row0, col0, d, f, down);
   } else if constexpr (MODE == kSquare) {
+    const float cb = ldexpf(a.cb, -2 * up), cc = ldexpf(a.cc, -4 * up) / kOperandScale;
     auto value = [&](int i, int j) {
       const int row = row0 + i * 16 + (lane & 15), col = col0 + j * 16 + (lane >> 4) * 4;
-      f32x4 v = acc[i][j] * (a.cc / kOperandScale);
+      f32x4 v = acc[i][j] * cc;
       // (a place outside is read at the edge, and not stored: no load waits behind a branch; 78.6 M bf16 weights 2298 us, so 2283)
       const _Float16* pa = mem + d.sq[a.in] + (int64_t)(row < rows ? row : rows - 1) * d.mp + (col < cols ? col : cols - 4);
       const half4 hi = *reinterpret_cast<const half4*>(pa);
@@ -824,14 +853,16 @@ __global__ __launch_bounds__((ProductShape<SHAPE, PARTS>::kThreads), (ProductSha
       for (int e = 0; e < 4; ++e) {
         float av = static_cast<float>(hi[e]);
         if constexpr (PARTS == 2) av += static_cast<float>(reinterpret_cast<const half4*>(pa + mm)[0][e]);
-        v[e] = fmaf(a.cb, av, v[e]);
+        v[e] = fmaf(cb, av, v[e]);
         if (row == col + e) v[e] += a.ca * kOperandScale;
       }
       return v;
     };
     store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.sq[a.out], d.mp, mem + d.sq[a.out], d.mp, mm, t.i != t.j);
   } else {
-    auto value = [&](int i, int j) { return acc[i][j] * (1.0f / kOperandScale); };
+    const int to = MODE == kGram ? 0 : exponent_of(size, a.then);
+    const float by = power_of_two(to - up), by2 = (MODE == kTimes ? by : 1.0f) * (1.0f / kOperandScale);
+    auto value = [&](int i, int j) { return acc[i][j] * by2 * by; };
     if constexpr (MODE == kGram || MODE == kTimes)
       store_halves<FM, FN, PARTS>(value, room, row0, col0, rows, cols, mem + d.sq[a.out], d.mp, mem + d.sq[a.out], d.mp, mm,
                                   t.i != t.j);
@@ -849,6 +880,7 @@ constexpr int kSmallHeld = kSmallElems / kSmallThreads;      // that a thread br
 struct PolarSteps {
   int32_t steps;
   float co[32][3];
+  float grown[32];  // log2 of the largest factors of the steps before each
 };
 __host__ __device__ constexpr int small_pad(int v) { return (v + 31) / 32 * 32; }
 __host__ __device__ constexpr int64_t small_halves(int m, int n, int parts) {
@@ -875,7 +907,11 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
   double sum = 0.0;
 #pragma unroll
   for (int u = 0; u < kSmallHeld; ++u) sum = fma((double)held[u], (double)held[u], sum);
-  const double by = inverse_of_norm(block_sum(sum, room), eps) * (double)kOperandScale;
+  sum = block_sum(sum, room);
+  const double inverse = inverse_of_norm(sum, eps);
+  const float norm_size = size_of(sum, inverse);
+  int up = exponent_of(norm_size, 0.0f);  // of the present X
+  const double by = ldexp(inverse * (double)kOperandScale, up);
 #pragma unroll
   for (int u = 0; u < kSmallHeld; ++u) {
     const int i = threadIdx.x + u * kSmallThreads;
@@ -968,7 +1004,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
   f32x4 v[2][2];
   for (int step = 0; step < st.steps; ++step) {
     asm volatile("" : "+v"(l15), "+v"(l4));  // (places worked out once for all steps would fill the registers)
-    const float ca = st.co[step][0], cb = st.co[step][1], cc = st.co[step][2];
+    const float ca = st.co[step][0], cb = ldexpf(st.co[step][1], -2 * up), cc = ldexpf(st.co[step][2], -4 * up);
     if (has_a) {
       block(X, xp, ai, X, xp, aj, np, kStraight, v);
       put(A, ap, ai, aj, v);
@@ -995,6 +1031,12 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
     __syncthreads();
     if (has_x) block(X, xp, xj, Q, ap, xi, mp, kTurned, v);
     if (step + 1 == st.steps) break;
+    const int to = exponent_of(norm_size, st.grown[step + 1]);
+    if (to != up) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[x >> 1][x & 1] *= power_of_two(to - up);
+      up = to;
+    }
     __syncthreads();
     if (has_x) put(X, xp, xj, xi, v);
     __syncthreads();
@@ -1005,8 +1047,8 @@ __global__ __launch_bounds__(kSmallThreads) void k_mat_small(From from, const Ma
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
     const int row = xi * 32 + (x & 1) * 16 + l15, col = xj * 32 + (x >> 1) * 16 + l4 * 4;
-    const float by = d.scale / kOperandScale;
-    const float w[4] = {v[x >> 1][x & 1][0] * by, v[x >> 1][x & 1][1] * by, v[x >> 1][x & 1][2] * by, v[x >> 1][x & 1][3] * by};
+    const f32x4 scaled = v[x >> 1][x & 1] * (d.scale / kOperandScale) * power_of_two(-up);
+    const float w[4] = {scaled[0], scaled[1], scaled[2], scaled[3]};
     if (row >= d.m || col >= d.n) continue;
     if (wide) {
       const int64_t at = d.at + (int64_t)row * d.n + col;
