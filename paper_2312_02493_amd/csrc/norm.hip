@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <new>
 
 #include "host_common.h"
@@ -238,7 +239,7 @@ int artopk_layernorm_forward(artopk_norm* norm, const void* x, int64_t x_stride,
   if (!norm) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_layernorm_forward: norm is NULL");
   int rc;
   if ((rc = check_problem(norm, type, rows, cols))) return rc;
-  if (!(eps >= 0.0f) || eps > 1e30f) return fail_text(norm->err, ARTOPK_EINVAL, "eps is negative or not finite");
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail_text(norm->err, ARTOPK_EINVAL, "eps is negative or not finite");
   if ((rc = check_rows(norm, "x", x, x_stride, type, rows, cols))) return rc;
   if ((rc = check_rows(norm, "y", y, y_stride, type, rows, cols))) return rc;
   if ((rc = check_floats(norm, "gamma", gamma)) || (rc = check_floats(norm, "beta", beta)) ||
