@@ -27,6 +27,7 @@ constexpr int kWaveCols = 512;        // what a wave's eight elements a lane hol
 constexpr int kSingleCols = 8192;  // the same in the backward pass, taken one by one
 constexpr int kMaxShares = 1024;          // blocks of a backward pass, at most
 constexpr int kLongShares = 64;
+constexpr int64_t kJoinBlocks = 1 << 20;  // a launch has fewer than 2^32 threads along an axis
 // Up to this many rows, and elements, the weight gradients are summed column by column beside the rows' blocks.
 constexpr int64_t kColumnRows = 512, kColumnElems = 1 << 20;
 
@@ -312,7 +313,7 @@ int artopk_layernorm_backward(artopk_norm* norm, const void* dy, int64_t dy_stri
     else go((_Float16*)nullptr);
   }
   if (part && (shares || rows == 0))
-    k_norm_join<<<dim3((unsigned)((cols + 63) / 64), 2), 1024, 0, norm->stream>>>(part, shares, cols, grads);
+    k_norm_join<<<dim3((unsigned)std::min<int64_t>((cols + 63) / 64, kJoinBlocks), 2), 1024, 0, norm->stream>>>(part, shares, cols, grads);
   NORM_TRY(norm, hipGetLastError());
   return ARTOPK_OK;
 }

@@ -451,24 +451,27 @@ __global__ __launch_bounds__(256) void k_norm_backward_cols(
   part[((int64_t)gridDim.y + blockIdx.y) * cols + c] = b;
 }
 
-// Sums the blocks' shares column by column, blockIdx.y = 0 dgamma, 1 dbeta; 64 columns a block, each of whose sixteen
+// Sums the blocks' shares column by column, blockIdx.y = 0 dgamma, 1 dbeta; 64 columns a block at a time, each of whose sixteen
 // waves takes every sixteenth share.
 __global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ part, int shares, int64_t cols, GradOut grads) {
   __shared__ float room[16][64];
   if (!grads.wanted(blockIdx.y)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   const float* p = part + (int64_t)blockIdx.y * shares * cols;
-  float s = 0.0f;
-  if (c < cols)
+  for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < cols; c0 += (int64_t)gridDim.x * 64) {
+    const int64_t c = c0 + lane;
+    float s = 0.0f;
+    if (c < cols)
 #pragma unroll 16
-    for (int j = wave; j < shares; j += 16) s += p[(int64_t)j * cols + c];
-  room[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && c < cols) {
+      for (int j = wave; j < shares; j += 16) s += p[(int64_t)j * cols + c];
+    room[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += room[i][lane];
-    grads.put(blockIdx.y, c, s);
+      for (int i = 1; i < 16; ++i) s += room[i][lane];
+      grads.put(blockIdx.y, c, s);
+    }
+    __syncthreads();  // read before the next columns' sums
   }
 }
 

@@ -24,3 +24,25 @@ def test_every_finite_eps_is_taken():
     for eps in (float("inf"), float("nan"), -1e-45):
         with pytest.raises(lib.ArTopkError, match="eps"):
             ctx.artopk_layernorm_forward(x, None, None, y, mean, rstd, eps=eps)
+
+
+def test_more_columns_than_a_launch_has_threads_for_at_once():
+    """2^28 and some columns: the joined weight gradients of one row, and those of none."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    cols = (1 << 28) + 77
+    ctx = lib.NormContext(1, cols)
+    b = torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    dy, x = (torch.randn(1, cols, generator=gen, device="cuda", dtype=b) for _ in range(2))
+    mean, rstd = torch.full((1,), 0.25, device="cuda"), torch.full((1,), 1.5, device="cuda")
+    dgamma, dbeta = torch.full((cols,), 7.0, device="cuda", dtype=b), torch.full((cols,), 7.0, device="cuda", dtype=b)
+    ctx.artopk_layernorm_backward(dy, x, None, mean, rstd, None, dgamma, dbeta)
+    assert torch.equal(dbeta, dy[0])
+    for at in range(0, cols, 1 << 26):  # one row: a product, rounded to float32 and then to bfloat16
+        s = slice(at, min(cols, at + (1 << 26)))
+        assert torch.equal(dgamma[s], (dy[0, s].float() * ((x[0, s].float() - 0.25) * 1.5)).to(b)), at
+    none = torch.empty(0, cols, device="cuda", dtype=b)
+    ctx.artopk_layernorm_backward(none, none, None, mean[:0], rstd[:0], none, dgamma, dbeta)
+    assert not bool(dgamma.any()) and not bool(dbeta.any())
