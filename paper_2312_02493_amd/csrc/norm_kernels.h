@@ -327,18 +327,19 @@ __global__ __launch_bounds__(NormShape<TPR>::kThreads) void k_norm_backward(
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      next_x[r].settle(x + row * x_stride, (r * TPR + t) * V, cols, last_x);
+      // Behind the row's end d is zero, and nothing may come of h there: it is the row's last piece's, or zero where that is not
+      // known ((0 - mu) rs may be beyond float32).
+      if constexpr (ANY) next_x[r].settle(x + row * x_stride, (r * TPR + t) * V, cols, last_x);
       next_d[r].settle(dy + row * dy_stride, (r * TPR + t) * V, cols, last_d);
-      const int c = (r * TPR + t) * V;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         d[r][i] = static_cast<float>(next_d[r].e[i]);
         h[r][i] = (static_cast<float>(next_x[r].e[i]) - mu) * rs;
       }
-      if (c + V > cols) {  // behind the row's end d is zero, and (0 - mu) rs may be beyond float32: h has to be zero, too
+      if (ANY && (r * TPR + t) * V + V > cols) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          if (c + i >= cols) h[r][i] = 0.0f;
+          if ((r * TPR + t) * V + i >= cols) h[r][i] = 0.0f;
       }
     }
     if (kAhead) ask(row + step);
