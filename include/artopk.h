@@ -503,7 +503,8 @@ enum { ARTOPK_PRODUCTS_HALF = 0, ARTOPK_PRODUCTS_SPLIT = 1, ARTOPK_PRODUCTS_DEFA
 /*
  * A handle for the matrices of a flat vector of n elements (1 <= n < 2^31) of `type`.  `mats` is a
  * host array of `count` matrices (1 .. 65535), each within the vector, none overlapping another,
- * rows and cols in [1, 65536], scale finite; it is read before the call returns.  The iterates' memory
+ * rows and cols in [1, 65536], scale finite; it is read before the call returns.  Padded to multiples of 64 they may be
+ * some 2^23 tiles of 64 x 64 in all (256 GiB with SPLIT; more are refused where a launch cannot hold them).  The iterates' memory
  * is allocated here: artopk_matrices_scratch_bytes(..) bytes, 4 for each element of a matrix and 6 for each of its
  * Gram matrix with HALF, of sides padded to multiples of 64, twice that for matrices that take SPLIT in an entry point, the
  * partial sums of Gram matrices that are summed in shares, and the tables

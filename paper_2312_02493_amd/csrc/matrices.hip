@@ -230,9 +230,33 @@ void list_product(MatPlan* plan, const std::vector<MatDesc>& mats, const Product
   p->tiles.count = (int)(plan->tiles.size() - p->tiles.at);
 }
 
-// Places of a group's matrices in the iterates' memory, and its lists of blocks; `mats` are those of the table from
-// group->first on.
-void plan_group(MatPlan* plan, Group* g) {
+// Threads of a product's block.
+int product_threads(int parts, int cls) {
+  constexpr int kThreads[2][kTileClasses] = {
+      {ProductShape<64, 1>::kThreads, ProductShape<128, 1>::kThreads, ProductShape<192, 1>::kThreads, ProductShape<256, 1>::kThreads,
+       ProductShape<64, 1>::kThreads},
+      {ProductShape<64, 2>::kThreads, ProductShape<128, 2>::kThreads, ProductShape<192, 2>::kThreads, ProductShape<256, 2>::kThreads,
+       ProductShape<64 + kDeep, 2>::kThreads}};
+  return kThreads[parts - 1][cls];
+}
+
+// Whether a launch holds all blocks of each kind: beyond 2^32 threads it would wrap round, without an error.
+bool launches_hold(const std::vector<MatDesc>& mats, const Group& g, const ProductKind& gram, const ProductKind& square,
+                   const ProductKind& apply, int each) {
+  int64_t begin = 0, of_gram = 0, of_square = 0, of_apply = 0;
+  for (const MatDesc& d : mats) {
+    begin += (int64_t)(d.mp / 64) * (d.np / 64);
+    of_gram += product_tiles(d, gram, kTileOf[g.gram.cls]) * product_shares(d, gram, each);
+    of_square += product_tiles(d, square, kTileOf[g.square.cls]);
+    of_apply += product_tiles(d, apply, kTileOf[g.apply.cls]);
+  }
+  return std::max({begin * 256, of_gram * product_threads(g.parts, g.gram.cls), of_square * product_threads(g.parts, g.square.cls),
+                   of_apply * product_threads(g.parts, g.apply.cls)}) < (1ll << 32);
+}
+
+// Places of a group's matrices in the iterates' memory, and its lists of blocks; its matrices are those of the table from
+// group->first on.  False where they are too many for a launch.
+bool plan_group(MatPlan* plan, Group* g) {
   const std::vector<MatDesc> bare(plan->mats.begin() + g->first, plan->mats.begin() + g->first + g->count);
   const ProductKind gram = {true, true}, square = {true, false}, apply = {false, false};
   int each = 0;
@@ -250,8 +274,9 @@ void plan_group(MatPlan* plan, Group* g) {
   }
   if (small && small_cost(bare, g->parts, lds) < cost) {
     g->small_lds = lds;
-    return;
+    return true;
   }
+  if (!launches_hold(bare, *g, gram, square, apply, each)) return false;
   for (int i = g->first; i < g->first + g->count; ++i) {
     MatDesc& d = plan->mats[i];
     const int64_t mn = (int64_t)d.mp * d.np * g->parts, mm = (int64_t)d.mp * d.mp * g->parts;
@@ -278,6 +303,7 @@ void plan_group(MatPlan* plan, Group* g) {
   plan->partial += slots * kTileOf[g->gram.cls] * kTileOf[g->gram.cls];
   list_product(plan, mats, square, &g->square, 0, &slots);
   list_product(plan, mats, apply, &g->apply, 0, &slots);
+  return true;
 }
 
 // `parts`: of each matrix's operands.  ARTOPK_OK, or ARTOPK_EINVAL with the reason in `err`.  Throws std::bad_alloc.
@@ -348,8 +374,9 @@ int make_plan(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
   }
   loose(n);
 
-  for (int i = 0; i < plan->ngroups; ++i) plan_group(plan, &plan->groups[i]);
-  if (plan->tiles.size() > (size_t)INT32_MAX) return fail_text(err, ARTOPK_EINVAL, "too many tiles");
+  for (int i = 0; i < plan->ngroups; ++i)
+    if (!plan_group(plan, &plan->groups[i]))
+      return fail_text(err, ARTOPK_EINVAL, "the matrices are more tiles of 64 x 64 than a launch holds");
   return ARTOPK_OK;
 }
 
