@@ -451,7 +451,8 @@ const char* artopk_norm_last_error(const artopk_norm* norm);
  * Layer norm of each row:  mean = sum(x) / cols,  rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps),
  * y = (x - mean) rstd gamma + beta.  Sums are float32, y is rounded once.
  *   x, y       device, rows of `cols` elements of `type`; rows lie x_stride / y_stride elements apart
- *              (at least cols where there is more than one).  Elements between rows stay untouched
+ *              (at least cols where there is more than one, at most 2^46 from the first to the last).  Elements between rows
+ *              stay untouched
  *   gamma      device, cols float32, or NULL for ones;  beta the same, or NULL for zeros
  *   eps        finite, >= 0
  *   mean_out, rstd_out   device, rows float32 each, for the backward pass; may be NULL

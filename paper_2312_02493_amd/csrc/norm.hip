@@ -28,6 +28,7 @@ constexpr int kSingleCols = 8192;  // the same in the backward pass, taken one b
 constexpr int kMaxShares = 1024;          // blocks of a backward pass, at most
 constexpr int kLongShares = 64;
 constexpr int64_t kJoinBlocks = 1 << 20;  // a launch has fewer than 2^32 threads along an axis
+constexpr int64_t kMostElems = 1ll << 46;  // between the first and the last row
 // Up to this many rows, and elements, the weight gradients are summed column by column beside the rows' blocks.
 constexpr int64_t kColumnRows = 512, kColumnElems = 1 << 20;
 
@@ -70,6 +71,9 @@ int check_rows(artopk_norm* h, const char* name, const void* p, int64_t stride, 
   if (rows > 1 && stride < cols)
     return fail_text(h->err, ARTOPK_EINVAL, "%s's rows are %lld apart and %lld long", name, (long long)stride, (long long)cols);
   if (stride < 0 || stride >= (1ll << 40)) return fail_text(h->err, ARTOPK_EINVAL, "%s's stride is outside [0, 2^40)", name);
+  // (so that places of elements, and of bytes, are far from 2^63)
+  if (rows > 1 && stride > kMostElems / (rows - 1))
+    return fail_text(h->err, ARTOPK_EINVAL, "%s's rows reach over more than 2^46 elements", name);
   return ARTOPK_OK;
 }
 

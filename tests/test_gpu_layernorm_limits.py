@@ -46,3 +46,28 @@ def test_more_columns_than_a_launch_has_threads_for_at_once():
     none = torch.empty(0, cols, device="cuda", dtype=b)
     ctx.artopk_layernorm_backward(none, none, None, mean[:0], rstd[:0], none, dgamma, dbeta)
     assert not bool(dgamma.any()) and not bool(dbeta.any())
+
+
+def test_rows_that_reach_beyond_any_memory_are_refused():
+    """2^20 rows and more at distances up to 2^40: refused on the host, before places pass 63 bits."""
+    import ctypes as C
+
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rows = (1 << 31) - 1
+    ctx = lib.NormContext(rows, 4)
+    raw = lib.load_library()
+    x, y, m = (torch.zeros(64, device="cuda") for _ in range(3))
+    px, py, pm = (C.c_void_p(t.data_ptr()) for t in (x, y, m))
+    for r, far in ((rows, (1 << 40) - 1), (rows, (1 << 33) + 4), (1 << 20, 1 << 39)):
+        assert raw.artopk_layernorm_forward(ctx._h, px, far, 0, r, 4, None, None, 1e-5, py, 4, None, None) == -1
+        assert b"2^46" in raw.artopk_norm_last_error(ctx._h)
+        assert raw.artopk_layernorm_forward(ctx._h, px, 4, 0, r, 4, None, None, 1e-5, py, far, None, None) == -1
+        for at in range(3):
+            strides = [far if i == at else 4 for i in range(3)]
+            assert raw.artopk_layernorm_backward(ctx._h, px, strides[0], px, strides[1], 0, r, 4, None, pm, pm, py, strides[2], None, None,
+                                                 0, 0) == -1
+            assert b"2^46" in raw.artopk_norm_last_error(ctx._h)
+    ctx.artopk_layernorm_forward(x[:4].view(1, 4), None, None, y[:4].view(1, 4))
+    torch.cuda.synchronize()
