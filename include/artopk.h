@@ -427,7 +427,8 @@ int artopk_select_info(artopk_ctx* ctx, int32_t* info_out, int32_t count);
  * kernels (no synchronisation, no memset; they can be recorded into a HIP graph and replayed),
  * calls on one handle must not overlap.  Buffers of these calls need only be aligned to their
  * elements; at 16-byte aligned places the loads are wider.  As everywhere, a buffer that a call
- * writes must not overlap any other of that call.
+ * writes must not overlap any other of that call.  Rows of layer norms overlap where their elements do: x and y, say,
+ * may be columns of one matrix (rows at different distances are taken to overlap wherever one could lie between the other's).
  * Element types are ARTOPK_G_F32, ARTOPK_G_BF16 and ARTOPK_G_F16; weights of a layer norm, its
  * statistics, momentum and updates are float32 whatever the elements' type.
  * ------------------------------------------------------------------------------------------ */

@@ -92,9 +92,46 @@ int check_floats(artopk_norm* h, const char* name, const void* p, size_t size = 
   return ARTOPK_OK;
 }
 
-size_t rows_bytes(int64_t stride, int64_t rows, int64_t cols, int32_t type) {
-  return rows ? ((size_t)(rows - 1) * (size_t)stride + (size_t)cols) * elem_size(type) : 0;
-}
+// The buffers of one call, as rows of bytes; those of x, dy, y and dx may be columns of one matrix and so lie between each
+// other's rows.  A buffer that is written must not share a byte with any other.
+class RowSet {
+ public:
+  void add(const void* p, int64_t stride, int64_t rows, int64_t cols, size_t size, bool written, const char* name) {
+    if (!p || rows == 0) return;
+    r_[n_++] = Rows{reinterpret_cast<uintptr_t>(p), rows > 1 ? (size_t)stride * size : 0, (size_t)cols * size, rows, written, name};
+  }
+  void add(const void* p, int64_t count, size_t size, bool written, const char* name) { add(p, 0, 1, count, size, written, name); }
+  // ARTOPK_OK, or ARTOPK_EINVAL with the first offending pair in `err`
+  int check(char* err) const {
+    for (int i = 0; i < n_; ++i)
+      for (int j = 0; j < i; ++j)
+        if ((r_[i].written || r_[j].written) && (r_[j].at < r_[i].at ? meet(r_[j], r_[i]) : meet(r_[i], r_[j])))
+          return fail_text(err, ARTOPK_EINVAL, "buffers %s and %s overlap", r_[j].name, r_[i].name);
+    return ARTOPK_OK;
+  }
+
+ private:
+  struct Rows {
+    uintptr_t at;
+    size_t pitch, width;  // pitch: 0 for one row
+    int64_t rows;
+    bool written;
+    const char* name;
+    uintptr_t end() const { return at + (size_t)(rows - 1) * pitch + width; }
+  };
+  // a begins where b does, or before
+  static bool meet(const Rows& a, const Rows& b) {
+    if (b.at >= a.end()) return false;
+    if (!a.pitch) return true;                    // b begins inside
+    const size_t in = (b.at - a.at) % a.pitch;    // b's first byte, from the row of a before it
+    if (in < a.width) return true;
+    if (b.pitch && b.pitch != a.pitch) return true;  // (may be; taken for yes)
+    // between two rows of a, or behind the last, which b.at < a.end() rules out
+    return in + b.width > a.pitch;
+  }
+  Rows r_[8];  // as many as a call has
+  int n_ = 0;
+};
 
 // Whether rows at p can be read sixteen bytes at a time.
 bool wide_rows(const void* p, int64_t stride, int64_t rows, size_t size) {
@@ -251,13 +288,13 @@ int artopk_layernorm_forward(artopk_norm* norm, const void* x, int64_t x_stride,
       (rc = check_floats(norm, "mean_out", mean_out)) || (rc = check_floats(norm, "rstd_out", rstd_out)))
     return rc;
   {
-    RangeSet rs;
-    rs.add(x, rows_bytes(x_stride, rows, cols, type), false, "x");
-    rs.add(y, rows_bytes(y_stride, rows, cols, type), true, "y");
-    rs.add(gamma, (size_t)cols * 4, false, "gamma");
-    rs.add(beta, (size_t)cols * 4, false, "beta");
-    rs.add(mean_out, (size_t)rows * 4, true, "mean_out");
-    rs.add(rstd_out, (size_t)rows * 4, true, "rstd_out");
+    RowSet rs;
+    rs.add(x, x_stride, rows, cols, elem_size(type), false, "x");
+    rs.add(y, y_stride, rows, cols, elem_size(type), true, "y");
+    rs.add(gamma, cols, 4, false, "gamma");
+    rs.add(beta, cols, 4, false, "beta");
+    rs.add(mean_out, rows, 4, true, "mean_out");
+    rs.add(rstd_out, rows, 4, true, "rstd_out");
     if ((rc = rs.check(norm->err))) return rc;
   }
   if (rows == 0) return ARTOPK_OK;
@@ -292,15 +329,15 @@ int artopk_layernorm_backward(artopk_norm* norm, const void* dy, int64_t dy_stri
       (rc = check_floats(norm, "dbeta", dbeta, gsize)))
     return rc;
   {
-    RangeSet rs;
-    rs.add(dy, rows_bytes(dy_stride, rows, cols, type), false, "dy");
-    rs.add(x, rows_bytes(x_stride, rows, cols, type), false, "x");
-    rs.add(gamma, (size_t)cols * 4, false, "gamma");
-    rs.add(mean, (size_t)rows * 4, false, "mean");
-    rs.add(rstd, (size_t)rows * 4, false, "rstd");
-    rs.add(dx, rows_bytes(dx_stride, rows, cols, type), true, "dx");
-    rs.add(dgamma, (size_t)cols * gsize, true, "dgamma");
-    rs.add(dbeta, (size_t)cols * gsize, true, "dbeta");
+    RowSet rs;
+    rs.add(dy, dy_stride, rows, cols, elem_size(type), false, "dy");
+    rs.add(x, x_stride, rows, cols, elem_size(type), false, "x");
+    rs.add(gamma, cols, 4, false, "gamma");
+    rs.add(mean, rows, 4, false, "mean");
+    rs.add(rstd, rows, 4, false, "rstd");
+    rs.add(dx, dx_stride, rows, cols, elem_size(type), true, "dx");
+    rs.add(dgamma, cols, gsize, true, "dgamma");
+    rs.add(dbeta, cols, gsize, true, "dbeta");
     if ((rc = rs.check(norm->err))) return rc;
   }
   float* part = dgamma || dbeta ? norm->part : nullptr;
