@@ -491,7 +491,7 @@ typedef struct artopk_matrices artopk_matrices;
 
 /* How many bits the operands of the matrix products keep.  HALF: 11 (float16, scaled by powers of
  * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32.  Five steps leave a
- * matrix some 1e-6 off with SPLIT; with HALF 1e-3 to 2e-3 (4e-3 where all singular values are the same), and up to 9e-3
+ * matrix some 1e-6 off with SPLIT; with HALF 1e-3 to 2e-3 (4e-3 where all singular values are the same), and up to 1e-2
  * with fewer than 64 rows or columns (the fewer of the two).
  * DEFAULT takes SPLIT for float32 and float16, and for bfloat16, whose own rounding is 1.7e-3, matrix by matrix: SPLIT for
  * those of fewer than 64 rows or columns, HALF for the others; in artopk_orthogonalize SPLIT for all where the matrices of
@@ -517,6 +517,16 @@ int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int
                            int32_t type, int32_t products, void* hip_stream);
 int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
                                       int32_t products);
+/*
+ * How a handle of these arguments works, on the host alone (for tests and tuning): artopk_orthogonalize, or with `weights`
+ * artopk_muon_step.  info_out (at least ARTOPK_MATRICES_INFO int32) becomes the number of groups of launches, at most 2, and
+ * for each the matrices in it, 1 for HALF or 2 for SPLIT, 1 where all steps are one launch, 1 where two steps are taken at
+ * once, the side of the tiles of X X^T, of the products of two square matrices and of Q X (0 in one launch), and the tiles of
+ * X X^T whose sums are cut into shares.  ARTOPK_EINVAL for arguments that create refuses.
+ */
+#define ARTOPK_MATRICES_INFO 17
+int artopk_matrices_info(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products,
+                         int32_t weights, int32_t* info_out, int32_t info_count);
 int artopk_matrices_destroy(artopk_matrices* m);
 const char* artopk_matrices_last_error(const artopk_matrices* m);
 

@@ -29,7 +29,7 @@ _SYMBOLS = (
     "artopk_scratch_bytes",
     "artopk_norm_create", "artopk_norm_scratch_bytes", "artopk_norm_destroy", "artopk_norm_last_error",
     "artopk_layernorm_forward", "artopk_layernorm_backward",
-    "artopk_matrices_create", "artopk_matrices_scratch_bytes", "artopk_matrices_destroy",
+    "artopk_matrices_create", "artopk_matrices_scratch_bytes", "artopk_matrices_info", "artopk_matrices_destroy",
     "artopk_matrices_last_error", "artopk_orthogonalize", "artopk_muon_step",
 )
 
@@ -92,6 +92,7 @@ def load_library():
     lib.artopk_layernorm_backward.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, vp, vp, vp, i64, vp, vp, i32, i32]
     lib.artopk_matrices_create.argtypes = [C.POINTER(vp), vp, i32, i64, i32, i32, vp]
     lib.artopk_matrices_scratch_bytes.argtypes = [vp, i32, i64, i32, i32]
+    lib.artopk_matrices_info.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32]
     lib.artopk_matrices_destroy.argtypes = [vp]
     lib.artopk_matrices_last_error.argtypes = [vp]
     lib.artopk_orthogonalize.argtypes = [vp, vp, vp, i32, vp, f32]
@@ -416,6 +417,19 @@ def artopk_matrices_scratch_bytes(matrices: Sequence, n: int, elem_type: int = A
     """Device bytes a MatrixContext of these arguments allocates (-1: refused); needs no GPU."""
     return int(load_library().artopk_matrices_scratch_bytes(_matrix_table(matrices), len(matrices), int(n),
                                                             int(elem_type), int(products)))
+
+
+def artopk_matrices_info(matrices: Sequence, n: int, elem_type: int = ARTOPK_G_F32, products: int = ARTOPK_PRODUCTS_DEFAULT,
+                         weights: bool = False) -> list:
+    """The groups of launches of a MatrixContext of these arguments, as dicts; needs no GPU."""
+    lib = load_library()
+    out = (C.c_int32 * 17)()
+    rc = lib.artopk_matrices_info(_matrix_table(matrices), len(matrices), int(n), int(elem_type), int(products), int(weights), out,
+                                  len(out))
+    if rc != 0:
+        raise ArTopkError(rc, lib.artopk_last_error(None).decode())
+    names = ("matrices", "parts", "one_launch", "pairs", "gram_tile", "square_tile", "apply_tile", "shared_tiles")
+    return [dict(zip(names, out[1 + 8 * i:9 + 8 * i])) for i in range(out[0])]
 
 
 class MatrixContext(_Handle):

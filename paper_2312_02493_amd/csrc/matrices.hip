@@ -658,6 +658,35 @@ int64_t artopk_matrices_scratch_bytes(const artopk_matrix* mats, int32_t count, 
   }
 }
 
+int artopk_matrices_info(const artopk_matrix* mats, int32_t count, int64_t n, int32_t type, int32_t products, int32_t weights,
+                         int32_t* info_out, int32_t info_count) {
+  if (!info_out || info_count < ARTOPK_MATRICES_INFO)
+    return fail_text(g_noctx_err, ARTOPK_EINVAL, "info_out has fewer than %d places", ARTOPK_MATRICES_INFO);
+  try {
+    Plans plans;
+    const int rc = make_plans(mats, count, n, type, products, &plans, g_noctx_err);
+    if (rc) return rc;
+    const MatPlan& plan = plans.plan[weights && plans.count == 2];
+    int32_t* o = info_out;
+    *o++ = plan.ngroups;
+    for (int i = 0; i < 2; ++i) {
+      const Group g = i < plan.ngroups ? plan.groups[i] : Group();
+      const bool tiles = i < plan.ngroups && !g.small_lds;
+      *o++ = g.count;
+      *o++ = i < plan.ngroups ? g.parts : 0;
+      *o++ = g.small_lds != 0;
+      *o++ = tiles && g.pairs;
+      *o++ = tiles ? kTileOf[g.gram.cls] : 0;
+      *o++ = tiles ? kTileOf[g.square.cls] : 0;
+      *o++ = tiles ? kTileOf[g.apply.cls] : 0;
+      *o++ = g.join.count;
+    }
+    return ARTOPK_OK;
+  } catch (const std::exception&) {
+    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "out of host memory");
+  }
+}
+
 int artopk_matrices_create(artopk_matrices** out, const artopk_matrix* mats, int32_t count, int64_t n, int32_t type,
                            int32_t products, void* hip_stream) {
   if (!out) return fail_text(g_noctx_err, ARTOPK_EINVAL, "out is NULL");
