@@ -1,0 +1,198 @@
+"""Every tile, kind of products and way through the steps against the definition in 64 bits (torch's float64 products).
+
+Tolerances are the accuracy that the library states, not a worst case: random roundings add up as their squares do.  With SPLIT a
+result is some 1e-6 off; 5e-6 is taken.  With HALF 1e-3 to 2e-3 from 64 rows on; 3e-3 is taken, and 1e-2 of fewer rows (half
+as much again of a sixth step).  To both comes the rounding of the reference itself to the output's type, and a tenth of that."""
+
+import numpy as np
+import pytest
+
+from tests.matrices_layouts import HALF, LAYOUTS, SPLIT, place
+from tests.test_gpu_matrices import EPS, USUAL, _code, _dtype
+
+pytestmark = pytest.mark.gpu
+
+OFF = {HALF: 3e-3, SPLIT: 5e-6}
+HALF_FEW = 1e-2
+
+
+def _polar(g, steps=5, eps=EPS):
+    """The definition, float64 on the GPU."""
+    tall = g.shape[0] > g.shape[1]
+    x = (g.t() if tall else g).contiguous().double()
+    x = x / (x.norm() + eps)
+    for _ in range(steps):
+        s = x @ x.t().contiguous()
+        x = USUAL[0] * x + (USUAL[1] * s + USUAL[2] * (s @ s)) @ x
+    return x.t() if tall else x
+
+
+def _inputs(mats, n, seed):
+    """A few strong directions and noise, as gradients have them."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    v = 1e-3 * torch.randn(n, generator=gen, device="cuda")
+    for at, r, c, _ in mats:
+        k = max(1, min(r, c) // 8)
+        v[at:at + r * c] += 1e-3 * (torch.randn(r, k, generator=gen, device="cuda") @
+                                    torch.randn(k, c, generator=gen, device="cuda")).view(-1) / k ** 0.5
+    return v
+
+
+def _allowed(want, products, rows, dtype, steps=5):
+    own = float((want.to(dtype).double() - want).norm())
+    off = HALF_FEW if products == HALF and rows < 64 else OFF[products]
+    return (1.5 if steps > 5 else 1.0) * off * float(want.norm()) + 1.1 * own
+
+
+def _check_orthogonalized(mats, n, t, products, steps=5, seed=60):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    dtype = _dtype(t)
+    x = _inputs(mats, n, seed).to(dtype)
+    out = torch.full_like(x, 7.0)
+    lib.MatrixContext(mats, n, _code(t), products).artopk_orthogonalize(x, out, steps=steps)
+    outside = torch.ones(n, dtype=torch.bool, device="cuda")
+    for at, r, c, scale in mats:
+        s = slice(at, at + r * c)
+        outside[s] = False
+        want = scale * _polar(x[s].view(r, c), steps)
+        off = float((out[s].view(r, c).double() - want).norm())
+        assert off <= _allowed(want, products, min(r, c), dtype, steps), (r, c, off, off / float(want.norm()))
+    assert bool((out[outside] == 7.0).all())
+
+
+def _check_step(mats, n, t, products, seed=61):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    dtype, eta, mu, decay, rest, by = _dtype(t), 0.5, 0.9, 0.1, 0.25, 0.5
+    m, u = _inputs(mats, n, seed), _inputs(mats, n, seed + 1)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    w = (0.02 * torch.randn(n, generator=gen, device="cuda")).to(dtype)
+    w0, m1 = w.double(), mu * m.double() + by * u.double()
+    v = mu * m1 + by * u.double()
+    lib.MatrixContext(mats, n, _code(t), products).artopk_muon_step(w, m, u, eta=eta, mu=mu, decay=decay, eta_rest=rest, update_scale=by)
+    assert float((m.double() - m1).norm()) <= 2.0 ** -22 * float(m1.norm())
+    outside = torch.ones(n, dtype=torch.bool, device="cuda")
+    for at, r, c, scale in mats:
+        s = slice(at, at + r * c)
+        outside[s] = False
+        step = eta * scale * _polar(v[s].view(r, c))
+        want = w0[s].view(r, c) * (1 - eta * decay) - step
+        off = float((w[s].view(r, c).double() - want).norm())
+        own = float((want.to(dtype).double() - want).norm())
+        few = HALF_FEW if products == HALF and min(r, c) < 64 else OFF[products]
+        # (float32: the update of a weight rounds a product and a sum)
+        assert off <= few * float(step.norm()) + 1.1 * own + 2.0 ** -23 * float(want.norm()), (r, c, off, own)
+    want = (w0 - rest * v)[outside]
+    own = float((want.to(dtype).double() - want).norm())
+    assert float((w.double()[outside] - want).norm()) <= 1.1 * own + 2.0 ** -22 * float(want.norm())
+
+
+@pytest.mark.parametrize("t,products", [("bf16", HALF), ("f32", SPLIT), ("f16", SPLIT)])
+@pytest.mark.parametrize("name", sorted(LAYOUTS))
+def test_orthogonalize_on_every_tile(name, t, products):
+    _check_orthogonalized(*place(LAYOUTS[name], 3), t, products)
+
+
+@pytest.mark.parametrize("t,products", [("bf16", HALF), ("f32", SPLIT)])
+@pytest.mark.parametrize("name", sorted(LAYOUTS))
+def test_weights_on_every_tile(name, t, products):
+    _check_step(*place(LAYOUTS[name], 4), t, products)
+
+
+@pytest.mark.parametrize("t,products", [("f32", HALF), ("f32", SPLIT)])
+@pytest.mark.parametrize("name", sorted(LAYOUTS))
+def test_every_element_in_its_place_on_every_tile(name, t, products):
+    """One entry to each row and column: the result has the same pattern, and exact zeros everywhere else."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    mats, n = place(LAYOUTS[name], 1)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.zeros(n, device="cuda")
+    found = []
+    for at, r, c, scale in mats:
+        k = min(r, c)
+        where = at + torch.randperm(r, generator=gen, device="cuda")[:k] * c + torch.randperm(c, generator=gen, device="cuda")[:k]
+        v = torch.randint(64, 256, (k,), generator=gen, device="cuda").double() * \
+            (2 * torch.randint(0, 2, (k,), generator=gen, device="cuda") - 1)
+        x[where] = v.float()
+        v = v / (v.norm() + EPS)
+        u = {HALF: 2.0 ** -11, SPLIT: 2.0 ** -21}[products] + 2.0 ** -22
+        off = torch.zeros_like(v)
+        for _ in range(5):  # as in tests/test_gpu_matrices.py
+            p = v * (USUAL[0] + USUAL[1] * v ** 2 + USUAL[2] * v ** 4)
+            slope = (USUAL[0] + 3 * USUAL[1] * v ** 2 + 5 * USUAL[2] * v ** 4).abs()
+            off = (slope + 0.1) * off + u * v.abs() * (slope + 2 * abs(USUAL[1]) * v ** 2 + 4 * USUAL[2] * v ** 4 + 4)
+            v = p
+        found.append((where, scale * v, 2 * scale * off + 2.0 ** -24 * v.abs()))  # (two steps at once round twice as often)
+    out = torch.zeros(n, device="cuda")
+    lib.MatrixContext(mats, n, _code(t), products).artopk_orthogonalize(x, out)
+    for where, want, off in found:
+        assert bool(((out[where].double() - want).abs() <= off).all())
+        out[where] = 0.0
+    assert not bool(out.any())
+
+
+SMALL = [(64, 64), (64, 120), (100, 60), (1, 1), (1, 30), (17, 90), (5, 3), (96, 96), (33, 31)]
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("products", [HALF, SPLIT])
+@pytest.mark.parametrize("gap", [4, 3])
+def test_small_matrices_in_one_launch(t, products, gap):
+    """Lengths of fours at places of fours (16-byte stores) and others, wide and tall; one to six steps and the weights' step."""
+    import paper_2312_02493_amd as lib
+
+    mats, n = place([s for s in SMALL if products == HALF or min(s) < 96], gap)
+    (info,) = lib.artopk_matrices_info(mats, n, _code(t), products)
+    assert info["one_launch"]
+    for steps in (1, 2, 5, 6):
+        _check_orthogonalized(mats, n, t, products, steps)
+    _check_step(mats, n, t, products)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("products", [HALF, SPLIT])
+def test_special_values_of_small_matrices_in_one_launch(t, products):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    mats, n = place([(64, 64), (30, 70), (70, 30), (20, 20)], 3)
+    assert lib.artopk_matrices_info(mats, n, _code(t), products)[0]["one_launch"]
+    x = _inputs(mats, n, 3).to(_dtype(t))
+    zero, nan, inf, last = (slice(m[0], m[0] + m[1] * m[2]) for m in mats)
+    x[zero], x[nan.start + 33], x[inf.start + 1000] = 0.0, float("nan"), float("-inf")
+    out = torch.full_like(x, 7.0)
+    ctx = lib.MatrixContext(mats, n, _code(t), products)
+    ctx.artopk_orthogonalize(x, out)
+    assert not bool(out[zero].any()) and bool(out[nan].isnan().all()) and bool(out[inf].isnan().all())
+    want = mats[3][3] * _polar(x[last].view(20, 20))
+    assert float((out[last].view(20, 20).double() - want).norm()) <= _allowed(want, products, 20, _dtype(t))
+    w, m = torch.ones_like(x), torch.zeros(n, device="cuda")
+    ctx.artopk_muon_step(w, m, x.float(), eta=0.1)
+    assert bool((w[zero] == 1.0).all()) and bool(w[nan].isnan().all()) and bool(w[inf].isnan().all())
+    assert bool(torch.isfinite(w[last]).all())
+
+
+@pytest.mark.parametrize("t", ["f16", "f32"])
+def test_default_products_of_wide_types_keep_their_bits(t):
+    """float16 and float32 take SPLIT by default, in both entry points, of any size."""
+    mats, n = place([(70, 150), (300, 77), (513, 520), (1500, 1100), (3000, 100)], 3)
+    import paper_2312_02493_amd as lib
+
+    import torch
+
+    x, dtype = _inputs(mats, n, 9).to(_dtype(t)), _dtype(t)
+    out, w = torch.zeros_like(x), torch.zeros_like(x)
+    ctx = lib.MatrixContext(mats, n, _code(t))
+    ctx.artopk_orthogonalize(x, out)
+    ctx.artopk_muon_step(w, torch.zeros(n, device="cuda"), x.float(), eta=1.0, nesterov=False)
+    for at, r, c, scale in mats:
+        want = scale * _polar(x[at:at + r * c].view(r, c))
+        for got in (out, -w):
+            assert float((got[at:at + r * c].view(r, c).double() - want).norm()) <= _allowed(want, SPLIT, min(r, c), dtype), (r, c)
