@@ -423,7 +423,8 @@ int artopk_select_info(artopk_ctx* ctx, int32_t* info_out, int32_t count);
  * What a training step does on either side of the compressed exchange: layer norm, whose weight
  * gradients land in a worker's flat gradient vector, and the update of weight matrices that lie
  * in a flat weight vector.  Both have handles of their own, made once like a context: bound to
- * one stream and the current device, all device memory allocated at creation, calls only enqueue
+ * one stream and the current device (which has to be current in later calls, too), all device
+ * memory allocated at creation, calls only enqueue
  * kernels (no synchronisation, no memset; they can be recorded into a HIP graph and replayed),
  * calls on one handle must not overlap.  Buffers of these calls need only be aligned to their
  * elements; at 16-byte aligned places the loads are wider.  As everywhere, a buffer that a call
@@ -467,7 +468,8 @@ int artopk_layernorm_forward(artopk_norm* norm, const void* x, int64_t x_stride,
  * Its gradient.  With h = (x - mean) rstd and d = dy gamma, row by row
  *   dx = rstd (d - sum(d) / cols - h sum(d h) / cols),
  * and summed over the rows  dgamma = sum(dy h),  dbeta = sum(dy).  Sums are float32, and their
- * order depends on the sizes alone: the same inputs give the same bits.
+ * order depends on nothing but sizes, types, rows' distances, where each buffer lies within sixteen bytes and the number of
+ * compute units (so do the forward pass's): the same values at such places give the same bits.
  *   dy, x, dx  device, rows of `type` as above; dx may be NULL where only the weights' gradients are wanted
  *   mean, rstd device, rows float32, as the forward pass left them
  *   dgamma, dbeta   device, cols elements of grad_type each, or NULL; they may lie anywhere in a
@@ -491,7 +493,7 @@ typedef struct artopk_matrices artopk_matrices;
 
 /* How many bits the operands of the matrix products keep.  HALF: 11 (float16, scaled by powers of
  * two); SPLIT: 22 (two float16 parts, three products for one).  Products are summed in float32.  Five steps leave a
- * matrix some 1e-6 off with SPLIT; with HALF 1e-3 to 2e-3 (4e-3 where all singular values are the same), and up to 1e-2
+ * matrix 1e-6 to 4e-6 off with SPLIT, as float32 products do; with HALF 1e-3 to 2e-3 (4e-3 where all singular values are the same), and up to 1e-2
  * with fewer than 64 rows or columns (the fewer of the two).
  * DEFAULT takes SPLIT for float32 and float16, and for bfloat16, whose own rounding is 1.7e-3, matrix by matrix: SPLIT for
  * those of fewer than 64 rows or columns, HALF for the others; in artopk_orthogonalize SPLIT for all where the matrices of

@@ -1,7 +1,7 @@
 """Every tile, kind of products and way through the steps against the definition in 64 bits (torch's float64 products).
 
 Tolerances are the accuracy that the library states, not a worst case: random roundings add up as their squares do.  With SPLIT a
-result is some 1e-6 off; 5e-6 is taken.  With HALF 1e-3 to 2e-3 from 64 rows on; 3e-3 is taken, and 1e-2 of fewer rows (half
+result is 1e-6 to 4e-6 off; 5e-6 is taken.  With HALF 1e-3 to 2e-3 from 64 rows on; 3e-3 is taken, and 1e-2 of fewer rows (half
 as much again of a sixth step).  To both comes the rounding of the reference itself to the output's type, and a tenth of that."""
 
 import numpy as np
