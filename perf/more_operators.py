@@ -148,8 +148,8 @@ def _logp_inputs(case, seed):
     s["tokens"] = torch.where((tok >= 0) & (torch.rand(rows, generator=g, device="cuda") < 0.5), hot[:, 0], tok)
     del z
     if case["call"] == "logp_grad":
-        lse, entropy = _row_sums(s["logits"], case["scale"])
-        s["lse"], s["entropy"] = lse.float(), entropy.float()
+        s["peak"], logsum, entropy = _row_sums(s["logits"], case["scale"])
+        s["logsum"], s["entropy"] = logsum.float(), entropy.float()
         mean = 1.0 if case["type"] == "f16" else 1.0 / rows  # (half precision: of a loss that is scaled by the rows)
         s["dlogp"] = -mean * (0.5 + torch.rand(rows, generator=g, device="cuda"))
         s["dlse"] = 1e-3 * mean * torch.rand(rows, generator=g, device="cuda")
@@ -158,21 +158,22 @@ def _logp_inputs(case, seed):
 
 
 def _row_sums(logits, scale):
-    """Statistics that the forward pass left, in 64 bits, some rows at a time."""
-    lse = torch.empty(logits.shape[0], dtype=torch.float64, device="cuda")
-    entropy = torch.empty_like(lse)
+    """Statistics that the forward pass left: the largest logit, and the logarithm of the sum relative to it and the entropy
+    in 64 bits, some rows at a time."""
+    peak = logits.float().amax(1)
+    logsum = torch.empty(logits.shape[0], dtype=torch.float64, device="cuda")
+    entropy = torch.empty_like(logsum)
     some = max(1, 100000000 // logits.shape[1])
     for at in range(0, logits.shape[0], some):
-        z = logits[at:at + some].double() * float(np.float32(scale))
-        top = z.amax(1, keepdim=True)
-        top = torch.where(top == -math.inf, torch.zeros_like(top), top)
-        d = z.sub_(top)
+        top = peak[at:at + some].double().view(-1, 1)
+        none = top.view(-1) == -math.inf
+        d = logits[at:at + some].double().sub_(torch.where(top == -math.inf, torch.zeros_like(top), top)).mul_(float(np.float32(scale)))
         e = torch.exp(d)
         total = e.sum(1)
         weighted = e.mul_(d.clamp_(min=-1e30)).sum(1)
-        lse[at:at + some] = top.view(-1) + torch.log(total)
-        entropy[at:at + some] = torch.where(total > 0, torch.log(total) - weighted / total, torch.zeros_like(total))
-    return lse, entropy
+        logsum[at:at + some] = torch.where(none, 0.0, torch.log(total))
+        entropy[at:at + some] = torch.where(none, 0.0, torch.log(total) - weighted / total)
+    return peak, logsum, entropy
 
 
 def _tensors(case):
@@ -252,7 +253,7 @@ def prepare(case, seed):
         s.update(_logp_inputs(case, seed))
         if case["call"] == "logp":
             rows, top = case["rows"], case["top"]
-            s["logp"], s["lse"], s["entropy"] = (torch.zeros(rows, device="cuda") for _ in range(3))
+            s["logp"], s["peak"], s["logsum"], s["entropy"] = (torch.zeros(rows, device="cuda") for _ in range(4))
             s["top_ids"] = torch.zeros(rows, top, dtype=torch.int32, device="cuda") if top else None
             s["top_logp"] = torch.zeros(rows, top, device="cuda") if top else None
         else:
@@ -360,7 +361,7 @@ def _plain_logp(s):
         base = torch.where(none.view(-1), zero, log).view(-1, 1)
         logp = torch.where(tok >= 0, (d.gather(1, at) - base).view(-1), zero)
         weighted = torch.where(e > 0, e * d, zero).sum(1)
-        out = {"logp": logp, "lse": top.view(-1) * scale + log,
+        out = {"logp": logp, "peak": top.view(-1), "logsum": base.view(-1),
                "entropy": torch.where(none.view(-1), zero, log - weighted / (1.0 + rest))}
         if case["top"]:
             bits = (x + 0.0).view(torch.int32)
@@ -369,14 +370,14 @@ def _plain_logp(s):
             ids = 0x7FFFFFFF - (torch.topk(order, case["top"], 1).values & 0xFFFFFFFF)
             out["top_ids"], out["top_logp"] = ids.int(), d.gather(1, ids) - base
         return out
-    none = s["lse"].view(-1, 1) == -math.inf
-    lse, dent = torch.where(none, zero, s["lse"].view(-1, 1)), s["dentropy"].view(-1, 1)
+    none = s["peak"].view(-1, 1) == -math.inf
+    top, logsum, dent = torch.where(none, zero, s["peak"].view(-1, 1)), s["logsum"].view(-1, 1), s["dentropy"].view(-1, 1)
     dlogp, h = torch.where(tok >= 0, s["dlogp"], zero).view(-1, 1), s["entropy"].view(-1, 1)
-    d = x * scale - lse
+    d = (x - top) * scale - logsum
     p = torch.exp(d)
     grad = p * (s["dlse"].view(-1, 1) - dlogp) - dent * torch.where(p > 0, p * (d + h), zero)
     # at the token itself 1 - p, from 64 bits where p is close to 1
-    d = x.gather(1, at).double() * scale - lse
+    d = (x.gather(1, at).double() - top) * scale - logsum
     p = torch.exp(d)
     own_ = -dlogp * torch.expm1(d) + s["dlse"].view(-1, 1) * p - dent * torch.where(p > 0, p * (d + h), 0.0)
     grad.scatter_(1, at, own_.float())
@@ -432,13 +433,13 @@ def run(s):
         plan.artopk_embedding_backward(s["dy"], s["tokens"], s["dtable"], scale=case["scale"], accumulate=case["accumulate"])
         return {"dtable": s["dtable"]}
     if case["call"] == "logp":
-        plan.artopk_token_logprobs(s["logits"], s["tokens"], s["logp"], s["lse"], s["entropy"], s["top_ids"], s["top_logp"],
-                                   scale=case["scale"])
-        out = {"logp": s["logp"], "lse": s["lse"], "entropy": s["entropy"]}
+        plan.artopk_token_logprobs(s["logits"], s["tokens"], s["logp"], s["peak"], s["logsum"], s["entropy"], s["top_ids"],
+                                   s["top_logp"], scale=case["scale"])
+        out = {"logp": s["logp"], "peak": s["peak"], "logsum": s["logsum"], "entropy": s["entropy"]}
         return {**out, "top_ids": s["top_ids"], "top_logp": s["top_logp"]} if case["top"] else out
     if case["call"] == "logp_grad":
-        plan.artopk_token_logprobs_backward(s["logits"], s["tokens"], s["lse"], s["dlogits"], dlogp=s["dlogp"], dlse=s["dlse"],
-                                            entropy=s["entropy"], dentropy=s["dentropy"], scale=case["scale"])
+        plan.artopk_token_logprobs_backward(s["logits"], s["tokens"], s["peak"], s["logsum"], s["dlogits"], dlogp=s["dlogp"],
+                                            dlse=s["dlse"], entropy=s["entropy"], dentropy=s["dentropy"], scale=case["scale"])
         return {"dlogits": s["dlogits"]}
     plan.artopk_adamw_step(s["weights"], s["update"], s["first"], s["second"], s["scales"], step=case["step"], eta=ETA,
                            beta1=BETA1, beta2=BETA2, eps=ADAM_EPS, update_scale=UPDATE_SCALE, seed=s.get("seed", 0))
@@ -464,8 +465,8 @@ def work(case):
     if case["call"].startswith("logp"):
         rows, elems = case["rows"], case["rows"] * case["vocab"]
         if case["call"] == "logp":
-            return {"bytes": elems * _size(case["type"]) + rows * (20 + 8 * case["top"]), "flops": 8 * elems}
-        return {"bytes": 2 * elems * _size(case["type"]) + 28 * rows, "flops": 10 * elems}
+            return {"bytes": elems * _size(case["type"]) + rows * (24 + 8 * case["top"]), "flops": 8 * elems}
+        return {"bytes": 2 * elems * _size(case["type"]) + 32 * rows, "flops": 10 * elems}
     n = sum(count for _, count, _, _ in _tensors(case)[0])
     moved = 2 * _size(case["type"]) + 4 + (16 if case["bits"] == 32 else 4 + 4 / BLOCK + 4)  # (8 bits: and their values)
     return {"bytes": moved * n, "flops": (15 if case["bits"] == 32 else 40) * n}
@@ -498,10 +499,10 @@ def _exact_logp(case, seed):
     tok, x, scale = s["tokens"], s["logits"], float(np.float32(case["scale"]))
     row = torch.arange(case["rows"], device="cuda")
     if case["call"] == "logp":
-        lse, entropy = _row_sums(x, scale)
-        base = torch.nan_to_num(lse, neginf=0.0)
+        peak, logsum, entropy = _row_sums(x, scale)
+        base = logsum + torch.nan_to_num(peak.double(), neginf=0.0) * scale
         logp = torch.where(tok >= 0, x[row, tok.clamp(min=0)].double() * scale - base, 0.0)
-        out = {"logp": logp, "lse": lse, "entropy": entropy}
+        out = {"logp": logp, "peak": peak, "logsum": logsum, "entropy": entropy}
         if case["top"]:
             k = case["top"]
             out["top_ids"] = None
@@ -511,16 +512,17 @@ def _exact_logp(case, seed):
     some = max(1, 100000000 // case["vocab"])
     for at in range(0, case["rows"], some):
         cut = slice(at, at + some)
-        lse, h = s["lse"][cut].double().view(-1, 1), s["entropy"][cut].double().view(-1, 1)
+        lse, h = s["peak"][cut].double().view(-1, 1) * scale + s["logsum"][cut].double().view(-1, 1), s["entropy"][cut].double().view(-1, 1)
         dead = lse == -math.inf
+        dlse = s["dlse"][cut].double().view(-1, 1)
         lp = (x[cut].double() * scale - lse.masked_fill(dead, 0.0)).clamp(min=-1e4)  # (e^-1e4 is 0 in 64 bits)
         one = torch.zeros_like(lp)
         live = torch.nonzero(tok[cut] >= 0).view(-1)
         one[live, tok[cut][live]] = 1.0
-        dlogp = torch.zeros_like(lse)
+        dlogp = torch.zeros_like(dlse)
         dlogp[live] = s["dlogp"][cut].double().view(-1, 1)[live]
         p = torch.exp(lp)
-        grad = dlogp * (one - p) + s["dlse"][cut].double().view(-1, 1) * p - s["dentropy"][cut].double().view(-1, 1) * p * (lp + h)
+        grad = dlogp * (one - p) + dlse * p - s["dentropy"][cut].double().view(-1, 1) * p * (lp + h)
         out[cut] = (grad * scale).masked_fill(dead, 0.0)
     return {"dlogits": out}
 
