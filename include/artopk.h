@@ -566,6 +566,155 @@ int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const f
                      float mu, int32_t nesterov, float eta, float decay, float eta_rest, int32_t steps,
                      const float* coefficients, float eps);
 
+/* ------------------------------------------------------------------------------------------
+ * Both ends of a language model, and the optimiser of what is no matrix: embedding rows of tokens
+ * and their gradient (which lands in a worker's flat vector, like a layer norm's weights'), log
+ * probabilities of given tokens and their gradient, and AdamW over many tensors of a flat vector.
+ * Two more handles, with the rules of those above (one stream, one device, memory at creation only,
+ * calls that only enqueue kernels and can be recorded into a HIP graph, no overlapping calls on
+ * one handle, buffers aligned to their elements unless stated).
+ * ------------------------------------------------------------------------------------------ */
+
+typedef struct artopk_tokens artopk_tokens;
+
+#define ARTOPK_MAX_TOP 64
+
+/*
+ * A handle for up to max_tokens tokens (rows) a call of vocabularies up to max_vocab (each in
+ * [1, 2^31)), and embedding rows of up to max_width elements (in [1, 65536]).  It allocates
+ * artopk_tokens_scratch_bytes(..) bytes (sorted tokens, shares of heavy tokens' sums; -1 for limits
+ * that create refuses).
+ *
+ * In every call on it `tokens` is a device array of token numbers of token_bits (32 or 64) bits, signed.
+ * A negative number is no token: padding, a place behind the last sequence.  A number that is not
+ * below vocab is an error that only the device sees: no memory is touched for it, what it would have
+ * given is NaN (nothing is added to a gradient), and artopk_tokens_status reports it.
+ */
+int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vocab, int64_t max_width, void* hip_stream);
+int64_t artopk_tokens_scratch_bytes(int64_t max_tokens, int64_t max_vocab, int64_t max_width);
+/* Free the scratch.  The caller must have synchronised the stream. */
+int artopk_tokens_destroy(artopk_tokens* h);
+const char* artopk_tokens_last_error(const artopk_tokens* h);
+/* Synchronise the handle's stream and report whether a token was not below vocab since the last call
+ * (ARTOPK_ESTATE, and the report is cleared), ARTOPK_OK otherwise. */
+int artopk_tokens_status(artopk_tokens* h);
+
+/*
+ * y[i] = scale table[tokens[i]], computed in float32 and rounded once; zeros where there is no token.
+ *   table    device, vocab rows of `width` elements of table_type, table_stride apart (as a layer norm's rows); it may
+ *            lie anywhere in a flat weight vector
+ *   y        device, `count` rows of `width` elements of `type`, y_stride apart; elements between rows stay untouched
+ *   scale    finite
+ * count may be 0.
+ */
+int artopk_embedding_forward(artopk_tokens* h, const void* table, int64_t table_stride, int32_t table_type, int64_t vocab,
+                             int64_t width, const void* tokens, int32_t token_bits, int64_t count, float scale, void* y,
+                             int64_t y_stride, int32_t type);
+
+/*
+ * Its gradient:  dtable[v] = scale (sum of dy[i] over the places i with tokens[i] = v), zero rows for tokens that do not occur.
+ * Sums are float32 and their order depends on nothing but the tokens and the sizes: the same calls give the same bits.
+ *   dy       device, `count` rows of `width` elements of `type`, dy_stride apart
+ *   dtable   device, vocab rows of `width` elements of grad_type, grad_stride apart; it may lie anywhere in a worker's flat
+ *            gradient vector
+ *   accumulate 0: all rows are overwritten; otherwise the sums are added to what is there, in float32, and rows of
+ *            tokens that do not occur are not touched
+ */
+int artopk_embedding_backward(artopk_tokens* h, const void* dy, int64_t dy_stride, int32_t type, const void* tokens,
+                              int32_t token_bits, int64_t count, int64_t width, float scale, void* dtable, int64_t grad_stride,
+                              int32_t grad_type, int64_t vocab, int32_t accumulate);
+
+/*
+ * Log probabilities of each row of logits, at a temperature of 1 / scale:
+ *   peak = max x,  logsum = log(sum e^(scale (x - peak))),  log p = scale (x - peak) - logsum,
+ *   logp = log p[tokens[row]],  entropy = -sum p log p.          (log sum e^(scale x) is scale peak + logsum)
+ *   logits   device, `rows` rows of vocab elements of `type`, `stride` apart
+ *   tokens   device, `rows`, or NULL where logp_out is NULL; logp is 0 where there is no token
+ *   scale    finite, > 0; scale times the difference of two finite logits of a row has to be below 2^127
+ *   logp_out, peak_out, logsum_out, entropy_out   device, `rows` float32 each, or NULL
+ *   top      0 .. ARTOPK_MAX_TOP, at most vocab: how many of the row's largest elements to give, in descending order, the
+ *            lower index first among equal ones (-0 equals +0)
+ *   top_ids_out, top_logp_out   device, rows x top int32 and float32: their indices and log p
+ * Logits of -infinity have probability zero.  A row of nothing else has peak -infinity, logsum 0, entropy 0 and log p
+ * -infinity; rows of the type's lowest finite value are ordinary rows of equal logits.  A row with NaN or +infinity gives
+ * NaN, and top_ids -1.  rows may be 0.
+ */
+int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, int32_t type, int64_t rows, int64_t vocab,
+                          const void* tokens, int32_t token_bits, float scale, float* logp_out, float* peak_out,
+                          float* logsum_out, float* entropy_out, int32_t top, int32_t* top_ids_out, float* top_logp_out);
+
+/*
+ * Its gradient, with p, log p, lse = scale peak + logsum and the entropy as above:
+ *   dlogits = scale (dlogp ([index = token] - p) + dlse p - dentropy p (log p + entropy)),  each rounded once.
+ *   logits, tokens, scale   as in the forward pass;  peak, logsum (and with dentropy, entropy) as it left them
+ *   dlogp, dlse, dentropy   device, `rows` float32 each, or NULL for zeros (one of them at least); dlogp of a row without a
+ *            token is not read
+ *   dlogits  device, `rows` rows of vocab elements of `type`, dstride apart; it may be logits itself (with the same
+ *            distance of rows), which is then overwritten
+ * Rows with nothing left (peak -infinity) get zeros, rows with NaN statistics NaN.
+ */
+int artopk_token_logprobs_backward(artopk_tokens* h, const void* logits, int64_t stride, int32_t type, int64_t rows,
+                                   int64_t vocab, const void* tokens, int32_t token_bits, float scale, const float* peak,
+                                   const float* logsum, const float* entropy, const float* dlogp, const float* dlse,
+                                   const float* dentropy, void* dlogits, int64_t dstride);
+
+/* One tensor of a flat vector: `count` elements from `offset` on. */
+typedef struct artopk_tensor {
+  int64_t offset, count;
+  float eta_scale; /* its learning rate is eta times this                      */
+  float decay;     /* decoupled decay: w is multiplied by 1 - eta eta_scale decay */
+} artopk_tensor;
+
+typedef struct artopk_adamw artopk_adamw;
+
+/*
+ * A handle for the tensors of a flat vector of n elements (1 <= n < 2^31) of `type`.  `tensors` is a host array of `count`
+ * (1 .. 65535), each within the vector, none overlapping another; it is read before the call returns and its tables are
+ * copied to the device synchronously.  state_bits: 32 or 8, what the moments are held in.
+ *
+ * The moments are the caller's: two device arrays `first` and `second` of artopk_adamw_state_elems(tensors, count, n) elements
+ * (float32, or one byte), 16-byte aligned, tensor by tensor in the order of the table, each filled up with zeros to a multiple of
+ * 256 elements; with 8 bits also `scales`, two bytes for each 256 of these elements, 16-byte aligned.  Zeros everywhere
+ * are the state before the first step.  (-1 for arguments that create refuses.)
+ *
+ * Moments of 8 bits: the 256 elements share their largest float32 exponent field E (one byte for each moment) and hold an
+ * exponent field f and three bits of mantissa b each, 2^(f - top + E - 127) (1 + b / 8), and 2^(1 - top + E - 127) b / 8 for
+ * f = 0; the first moment with a sign and four bits of f, top = 14, the second with five and top = 30.  They are rounded
+ * up or down at random so that their mean is exact (to 2^-17 of the distance of two codes), by bits that depend on
+ * seed, step and place alone; a second moment other than zero below the least normal code becomes that code.  Infinity or NaN in
+ * a moment makes the moments of its 256 elements NaN from the next step on.
+ */
+int artopk_adamw_create(artopk_adamw** out, const artopk_tensor* tensors, int32_t count, int64_t n, int32_t type,
+                        int32_t state_bits, void* hip_stream);
+int64_t artopk_adamw_scratch_bytes(const artopk_tensor* tensors, int32_t count, int64_t n);
+int64_t artopk_adamw_state_elems(const artopk_tensor* tensors, int32_t count, int64_t n);
+int artopk_adamw_destroy(artopk_adamw* h);
+const char* artopk_adamw_last_error(const artopk_adamw* h);
+
+/*
+ * One step on all tensors; elements of no tensor stay as they are.  With g = update_scale update:
+ *   first  <- m = beta1 first + (1 - beta1) g
+ *   second <- v = beta2 second + (1 - beta2) g^2
+ *   w <- w (1 - eta eta_scale decay) - (eta eta_scale / (1 - beta1^t)) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * computed in float32; w is rounded once, and uses m and v as they are before they are rounded to 8 bits.
+ *   weights  device, n elements of the handle's type, updated in place
+ *   update   device, n float32: a step's update_out; update_scale 1 / W makes its sum a mean
+ *   first, second, scales   device, the moments, updated in place (scales NULL with 32 bits)
+ *   step     t >= 1, or 0: t is a counter on the device that this call first adds one to, for steps replayed from a graph.
+ *            artopk_adamw_set_step sets it (0 in a new handle), enqueued like any call
+ *   eta, update_scale finite; beta1, beta2 in [0, 1) (float64: 1 - beta is taken before rounding); eps > 0, finite
+ *   seed     of the random rounding (8 bits)
+ */
+int artopk_adamw_step(artopk_adamw* h, void* weights, const float* update, void* first, void* second, uint8_t* scales,
+                      int64_t step, float update_scale, float eta, double beta1, double beta2, float eps, uint64_t seed);
+int artopk_adamw_set_step(artopk_adamw* h, int64_t step);
+/*
+ * Moments of 8 bits as the values they stand for, which float32 and bfloat16 (`type`) hold exactly above the least normal number:
+ * first_out and second_out, device, artopk_adamw_state_elems elements, 16-byte aligned; one of them may be NULL.
+ */
+int artopk_adamw_values(artopk_adamw* h, const void* first, const void* second, const uint8_t* scales, int32_t type,
+                        void* first_out, void* second_out);
+
 /* Library version, major*10000 + minor*100 + patch. */
 int32_t artopk_version(void);
 

@@ -18,6 +18,7 @@ ARTOPK_G_F32, ARTOPK_G_BF16, ARTOPK_G_F16 = 0, 1, 2
 ARTOPK_OPT_GUESS_MIN_N, ARTOPK_OPT_UPDATE_TILES_MIN_N, ARTOPK_OPT_LEADER_FIRST, ARTOPK_OPT_NONTEMPORAL = 0, 1, 2, 3
 ARTOPK_OPT_STAGE_TILES, ARTOPK_OPT_SHORT_MAX_N = 4, 5
 ARTOPK_PRODUCTS_HALF, ARTOPK_PRODUCTS_SPLIT, ARTOPK_PRODUCTS_DEFAULT = 0, 1, -1
+ARTOPK_MAX_TOP = 64
 PROF_NAMES = ("pass_a", "select", "gather", "update", "total")
 
 _SYMBOLS = (
@@ -31,6 +32,11 @@ _SYMBOLS = (
     "artopk_layernorm_forward", "artopk_layernorm_backward",
     "artopk_matrices_create", "artopk_matrices_scratch_bytes", "artopk_matrices_info", "artopk_matrices_destroy",
     "artopk_matrices_last_error", "artopk_orthogonalize", "artopk_muon_step",
+    "artopk_tokens_create", "artopk_tokens_scratch_bytes", "artopk_tokens_destroy", "artopk_tokens_last_error",
+    "artopk_tokens_status", "artopk_embedding_forward", "artopk_embedding_backward", "artopk_token_logprobs",
+    "artopk_token_logprobs_backward",
+    "artopk_adamw_create", "artopk_adamw_scratch_bytes", "artopk_adamw_state_elems", "artopk_adamw_destroy",
+    "artopk_adamw_last_error", "artopk_adamw_step", "artopk_adamw_set_step", "artopk_adamw_values",
 )
 
 
@@ -97,9 +103,25 @@ def load_library():
     lib.artopk_matrices_last_error.argtypes = [vp]
     lib.artopk_orthogonalize.argtypes = [vp, vp, vp, i32, vp, f32]
     lib.artopk_muon_step.argtypes = [vp, vp, vp, vp, f32, f32, i32, f32, f32, f32, i32, vp, f32]
+    f64 = C.c_double
+    lib.artopk_tokens_create.argtypes = [C.POINTER(vp), i64, i64, i64, vp]
+    lib.artopk_tokens_scratch_bytes.argtypes = [i64, i64, i64]
+    for name in ("artopk_tokens_destroy", "artopk_tokens_last_error", "artopk_tokens_status", "artopk_adamw_destroy",
+                 "artopk_adamw_last_error"):
+        getattr(lib, name).argtypes = [vp]
+    lib.artopk_embedding_forward.argtypes = [vp, vp, i64, i32, i64, i64, vp, i32, i64, f32, vp, i64, i32]
+    lib.artopk_embedding_backward.argtypes = [vp, vp, i64, i32, vp, i32, i64, i64, f32, vp, i64, i32, i64, i32]
+    lib.artopk_token_logprobs.argtypes = [vp, vp, i64, i32, i64, i64, vp, i32, f32, vp, vp, vp, vp, i32, vp, vp]
+    lib.artopk_token_logprobs_backward.argtypes = [vp, vp, i64, i32, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, vp, vp, i64]
+    lib.artopk_adamw_create.argtypes = [C.POINTER(vp), vp, i32, i64, i32, i32, vp]
+    lib.artopk_adamw_scratch_bytes.argtypes = [vp, i32, i64]
+    lib.artopk_adamw_state_elems.argtypes = [vp, i32, i64]
+    lib.artopk_adamw_step.argtypes = [vp, vp, vp, vp, vp, vp, i64, f32, f32, f64, f64, f32, u64]
+    lib.artopk_adamw_set_step.argtypes = [vp, i64]
+    lib.artopk_adamw_values.argtypes = [vp, vp, vp, vp, i32, vp, vp]
     lib.artopk_version.restype = i32
     for name in _SYMBOLS:
-        if name.endswith("_scratch_bytes"):
+        if name.endswith(("_scratch_bytes", "_state_elems")):
             getattr(lib, name).restype = i64
         elif name.endswith("_last_error"):
             getattr(lib, name).restype = C.c_char_p
@@ -459,3 +481,166 @@ class MatrixContext(_Handle):
             _vector(update, "update", self.n, self._device, ARTOPK_G_F32), update_scale, mu, int(nesterov),
             eta, decay, eta_rest, int(steps), _coefficients(int(steps), coefficients),
             eps))
+
+
+def artopk_tokens_scratch_bytes(max_tokens: int, max_vocab: int, max_width: int = 1) -> int:
+    """Device bytes a TokenContext of these limits allocates (-1: limits refused); needs no GPU."""
+    return int(load_library().artopk_tokens_scratch_bytes(int(max_tokens), int(max_vocab), int(max_width)))
+
+
+def _token_bits(t) -> int:
+    import torch
+
+    bits = {torch.int32: 32, torch.int64: 64}.get(t.dtype)
+    if bits is None:
+        raise ArTopkError(-1, f"tokens are {t.dtype}: int32 or int64 are taken")
+    return bits
+
+
+def _matrix_of(t, name: str, rows: int, cols: int, device: int, dtype: str) -> Optional[int]:
+    """Address of a contiguous rows x cols matrix of torch's `dtype` on the device."""
+    import torch
+
+    if t.get_device() != device:
+        raise ArTopkError(-1, f"{name} is on {t.device}, not on the handle's device {device}")
+    if tuple(t.shape) != (rows, cols) or not t.is_contiguous() or t.dtype != getattr(torch, dtype):
+        raise ArTopkError(-1, f"{name} is not a contiguous {rows} x {cols} matrix of {dtype}")
+    return t.data_ptr()
+
+
+class TokenContext(_Handle):
+    """Owns one artopk_tokens: embedding rows and log probabilities of up to max_tokens tokens of up to max_vocab."""
+
+    _name = "tokens"
+
+    def __init__(self, max_tokens: int, max_vocab: int, max_width: int = 1, stream: Optional[int] = None):
+        self._open(stream, int(max_tokens), int(max_vocab), int(max_width))
+
+    def status(self):
+        self._check(self._lib.artopk_tokens_status(self._h))
+
+    def artopk_embedding_forward(self, table, tokens, y, scale: float = 1.0):
+        dev = self._device
+        pt, st, vocab, width = _rows(table, "table", dev)
+        py, sy, count, width_y = _rows(y, "y", dev)
+        if width_y != width:
+            raise ArTopkError(-1, "y's rows are not as long as table's")
+        self._check(self._lib.artopk_embedding_forward(
+            self._h, pt, st, _elem_type(table), vocab, width, _vector(tokens, "tokens", count, dev), _token_bits(tokens), count,
+            scale, py, sy, _elem_type(y)))
+
+    def artopk_embedding_backward(self, dy, tokens, dtable, scale: float = 1.0, accumulate: bool = False):
+        dev = self._device
+        pd, sd, count, width = _rows(dy, "dy", dev)
+        pt, st, vocab, width_t = _rows(dtable, "dtable", dev)
+        if width_t != width:
+            raise ArTopkError(-1, "dtable's rows are not as long as dy's")
+        self._check(self._lib.artopk_embedding_backward(
+            self._h, pd, sd, _elem_type(dy), _vector(tokens, "tokens", count, dev), _token_bits(tokens), count, width, scale, pt,
+            st, _elem_type(dtable), vocab, int(accumulate)))
+
+    def artopk_token_logprobs(self, logits, tokens=None, logp_out=None, peak_out=None, logsum_out=None, entropy_out=None,
+                              top_ids_out=None, top_logp_out=None, scale: float = 1.0):
+        dev = self._device
+        p, s, rows, vocab = _rows(logits, "logits", dev)
+        top, ids, lps = 0, None, None
+        if top_ids_out is not None or top_logp_out is not None:
+            if top_ids_out is None or top_logp_out is None or len(top_ids_out.shape) != 2:
+                raise ArTopkError(-1, "top_ids_out and top_logp_out are not two matrices")
+            top = top_ids_out.shape[1]
+            ids = _matrix_of(top_ids_out, "top_ids_out", rows, top, dev, "int32")
+            lps = _matrix_of(top_logp_out, "top_logp_out", rows, top, dev, "float32")
+        self._check(self._lib.artopk_token_logprobs(
+            self._h, p, s, _elem_type(logits), rows, vocab, _vector(tokens, "tokens", rows, dev),
+            32 if tokens is None else _token_bits(tokens), scale, _vector(logp_out, "logp_out", rows, dev, ARTOPK_G_F32),
+            _vector(peak_out, "peak_out", rows, dev, ARTOPK_G_F32), _vector(logsum_out, "logsum_out", rows, dev, ARTOPK_G_F32),
+            _vector(entropy_out, "entropy_out", rows, dev, ARTOPK_G_F32), top, ids, lps))
+
+    def artopk_token_logprobs_backward(self, logits, tokens, peak, logsum, dlogits, dlogp=None, dlse=None, entropy=None,
+                                       dentropy=None, scale: float = 1.0):
+        dev = self._device
+        p, s, rows, vocab = _rows(logits, "logits", dev)
+        pd, sd, rows_d, vocab_d = _rows(dlogits, "dlogits", dev)
+        if rows_d != rows or vocab_d != vocab or dlogits.dtype != logits.dtype:
+            raise ArTopkError(-1, "dlogits' shape or type is not logits'")
+        kind = _elem_type(logits)
+        f = [_vector(t, name, rows, dev, ARTOPK_G_F32) for t, name in (
+            (peak, "peak"), (logsum, "logsum"), (entropy, "entropy"), (dlogp, "dlogp"), (dlse, "dlse"), (dentropy, "dentropy"))]
+        self._check(self._lib.artopk_token_logprobs_backward(
+            self._h, p, s, kind, rows, vocab, _vector(tokens, "tokens", rows, dev), 32 if tokens is None else _token_bits(tokens),
+            scale, *f, pd, sd))
+
+
+class _Tensor(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("count", C.c_int64), ("eta_scale", C.c_float), ("decay", C.c_float)]
+
+
+def _tensor_table(tensors: Sequence):
+    table = (_Tensor * max(1, len(tensors)))()
+    for i, t in enumerate(tensors):
+        table[i] = _Tensor(int(t[0]), int(t[1]), float(t[2]) if len(t) > 2 else 1.0, float(t[3]) if len(t) > 3 else 0.0)
+    return table
+
+
+def artopk_adamw_scratch_bytes(tensors: Sequence, n: int) -> int:
+    """Device bytes an AdamWContext of these arguments allocates (-1: refused); needs no GPU."""
+    return int(load_library().artopk_adamw_scratch_bytes(_tensor_table(tensors), len(tensors), int(n)))
+
+
+def artopk_adamw_state_elems(tensors: Sequence, n: int) -> int:
+    """Elements of each moment (-1: refused); with 8 bits a byte each, and two bytes of scales for every 256; needs no GPU."""
+    return int(load_library().artopk_adamw_state_elems(_tensor_table(tensors), len(tensors), int(n)))
+
+
+class AdamWContext(_Handle):
+    """Owns one artopk_adamw: tensors (offset, count[, eta_scale[, decay]]) of a flat vector of n elements."""
+
+    _name = "adamw"
+
+    def __init__(self, tensors: Sequence, n: int, elem_type: int = ARTOPK_G_F32, state_bits: int = 32,
+                 stream: Optional[int] = None):
+        self.n, self.elem_type, self.state_bits = int(n), int(elem_type), int(state_bits)
+        table = _tensor_table(tensors)
+        self._open(stream, table, len(tensors), self.n, self.elem_type, self.state_bits)
+        self.state_elems = int(self._lib.artopk_adamw_state_elems(table, len(tensors), self.n))
+
+    def new_state(self):
+        """(first, second, scales) before the first step, on the handle's device; scales is None with 32 bits."""
+        import torch
+
+        dev = torch.device("cuda", self._device)
+        kind = torch.uint8 if self.state_bits == 8 else torch.float32
+        first, second = (torch.zeros(self.state_elems, dtype=kind, device=dev) for _ in range(2))
+        return first, second, torch.zeros(self.state_elems // 256, 2, dtype=kind, device=dev) if self.state_bits == 8 else None
+
+    def _moments(self, first, second, scales):
+        import torch
+
+        kind = torch.uint8 if self.state_bits == 8 else torch.float32
+        out = []
+        for t, name, length in ((first, "first", self.state_elems), (second, "second", self.state_elems),
+                                (scales, "scales", self.state_elems // 128)):
+            if t is not None and t.dtype != (torch.uint8 if name == "scales" else kind):
+                raise ArTopkError(-1, f"{name} is {t.dtype}, which is not what is taken")
+            out.append(_vector(t, name, length, self._device))
+        return out
+
+    def set_step(self, step: int):
+        self._check(self._lib.artopk_adamw_set_step(self._h, int(step)))
+
+    def artopk_adamw_step(self, weights, update, first, second, scales=None, step: int = 0, eta: float = 1e-3,
+                          beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, update_scale: float = 1.0, seed: int = 0):
+        if _elem_type(weights) != self.elem_type:
+            raise ArTopkError(-1, f"weights is {weights.dtype}, which is not the handle's type")
+        self._check(self._lib.artopk_adamw_step(
+            self._h, _vector(weights, "weights", self.n, self._device), _vector(update, "update", self.n, self._device, ARTOPK_G_F32),
+            *self._moments(first, second, scales), int(step), update_scale, eta, beta1, beta2, eps, int(seed) & (1 << 64) - 1))
+
+    def artopk_adamw_values(self, first, second, scales, first_out=None, second_out=None):
+        outs = [t for t in (first_out, second_out) if t is not None]
+        kinds = {_elem_type(t) for t in outs}
+        if len(kinds) > 1:
+            raise ArTopkError(-1, "first_out and second_out are of different types")
+        self._check(self._lib.artopk_adamw_values(
+            self._h, *self._moments(first, second, scales), kinds.pop() if kinds else ARTOPK_G_F32,
+            *[_vector(t, name, self.state_elems, self._device) for t, name in ((first_out, "first_out"), (second_out, "second_out"))]))

@@ -23,7 +23,7 @@ HIPCC_FLAGS = [
 
 
 # operators around the step, in both libraries
-PART_SOURCES = ("norm.hip", "matrices.hip")
+PART_SOURCES = ("norm.hip", "matrices.hip", "tokens.hip", "adamw.hip")
 
 
 def _run_all(runs, verbose: bool):

@@ -43,4 +43,12 @@ __device__ __forceinline__ void store_elems(T* p, const float (&in)[V]) {
   }
 }
 
+// Calls f with a null pointer of the element type.
+template <class F>
+void with_type(int32_t type, F&& f) {
+  if (type == kTypeF32) f((float*)nullptr);
+  else if (type == kTypeBf16) f((__bf16*)nullptr);
+  else f((_Float16*)nullptr);
+}
+
 }  // namespace artopk

@@ -78,4 +78,63 @@ class RangeSet {
   int n_ = 0;
 };
 
+inline size_t elem_size(int32_t type) { return type == ARTOPK_G_F32 ? 4 : 2; }
+
+inline bool known_type(int32_t type) { return type == ARTOPK_G_F32 || type == ARTOPK_G_BF16 || type == ARTOPK_G_F16; }
+
+constexpr int64_t kMostElems = 1ll << 46;  // between the first and the last row
+
+inline int check_rows(char* err, const char* name, const void* p, int64_t stride, size_t size, int64_t rows, int64_t cols) {
+  if (!p && rows > 0) return fail_text(err, ARTOPK_EINVAL, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % size) return fail_text(err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
+  if (rows > 1 && stride < cols)
+    return fail_text(err, ARTOPK_EINVAL, "%s's rows are %lld apart and %lld long", name, (long long)stride, (long long)cols);
+  if (stride < 0 || stride >= (1ll << 40)) return fail_text(err, ARTOPK_EINVAL, "%s's stride is outside [0, 2^40)", name);
+  // (so that places of elements, and of bytes, are far from 2^63)
+  if (rows > 1 && stride > kMostElems / (rows - 1))
+    return fail_text(err, ARTOPK_EINVAL, "%s's rows reach over more than 2^46 elements", name);
+  return ARTOPK_OK;
+}
+
+// The buffers of one call, as rows of bytes; those of x, dy, y and dx may be columns of one matrix and so lie between each
+// other's rows.  A buffer that is written must not share a byte with any other.
+class RowSet {
+ public:
+  void add(const void* p, int64_t stride, int64_t rows, int64_t cols, size_t size, bool written, const char* name) {
+    if (!p || rows == 0) return;
+    r_[n_++] = Rows{reinterpret_cast<uintptr_t>(p), rows > 1 ? (size_t)stride * size : 0, (size_t)cols * size, rows, written, name};
+  }
+  void add(const void* p, int64_t count, size_t size, bool written, const char* name) { add(p, 0, 1, count, size, written, name); }
+  // ARTOPK_OK, or ARTOPK_EINVAL with the first offending pair in `err`
+  int check(char* err) const {
+    for (int i = 0; i < n_; ++i)
+      for (int j = 0; j < i; ++j)
+        if ((r_[i].written || r_[j].written) && (r_[j].at < r_[i].at ? meet(r_[j], r_[i]) : meet(r_[i], r_[j])))
+          return fail_text(err, ARTOPK_EINVAL, "buffers %s and %s overlap", r_[j].name, r_[i].name);
+    return ARTOPK_OK;
+  }
+
+ private:
+  struct Rows {
+    uintptr_t at;
+    size_t pitch, width;  // pitch: 0 for one row
+    int64_t rows;
+    bool written;
+    const char* name;
+    uintptr_t end() const { return at + (size_t)(rows - 1) * pitch + width; }
+  };
+  // a begins where b does, or before
+  static bool meet(const Rows& a, const Rows& b) {
+    if (b.at >= a.end()) return false;
+    if (!a.pitch) return true;                    // b begins inside
+    const size_t in = (b.at - a.at) % a.pitch;    // b's first byte, from the row of a before it
+    if (in < a.width) return true;
+    if (b.pitch && b.pitch != a.pitch) return true;  // (may be; taken for yes)
+    // between two rows of a, or behind the last, which b.at < a.end() rules out
+    return in + b.width > a.pitch;
+  }
+  Rows r_[12];  // as many as a call has, and more
+  int n_ = 0;
+};
+
 }  // namespace artopk

@@ -611,16 +611,6 @@ void polar(const artopk_matrices* h, const Route& r, From from, const Steps& st,
   }
 }
 
-// Calls f with a null pointer of the handle's element type.
-template <class F>
-void with_type(int32_t type, F&& f) {
-  if (type == ARTOPK_G_F32) f((float*)nullptr);
-  else if (type == ARTOPK_G_BF16) f((__bf16*)nullptr);
-  else f((_Float16*)nullptr);
-}
-
-size_t elem_size(int32_t type) { return type == ARTOPK_G_F32 ? 4 : 2; }
-
 int check_vector(artopk_matrices* h, const char* name, const void* p, size_t size) {
   if (!p) return fail_text(h->err, ARTOPK_EINVAL, "%s is NULL", name);
   if (reinterpret_cast<uintptr_t>(p) % size) return fail_text(h->err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);

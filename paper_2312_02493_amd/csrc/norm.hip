@@ -28,7 +28,6 @@ constexpr int kSingleCols = 8192;  // the same in the backward pass, taken one b
 constexpr int kMaxShares = 1024;          // blocks of a backward pass, at most
 constexpr int kLongShares = 64;
 constexpr int64_t kJoinBlocks = 1 << 20;  // a launch has fewer than 2^32 threads along an axis
-constexpr int64_t kMostElems = 1ll << 46;  // between the first and the last row
 // Up to this many rows, and elements, the weight gradients are summed column by column beside the rows' blocks.
 constexpr int64_t kColumnRows = 512, kColumnElems = 1 << 20;
 
@@ -60,23 +59,6 @@ int64_t part_floats(int64_t max_rows, int64_t max_cols) {
   return f;
 }
 
-size_t elem_size(int32_t type) { return type == ARTOPK_G_F32 ? 4 : 2; }
-
-bool known_type(int32_t type) { return type == ARTOPK_G_F32 || type == ARTOPK_G_BF16 || type == ARTOPK_G_F16; }
-
-int check_rows(artopk_norm* h, const char* name, const void* p, int64_t stride, int32_t type, int64_t rows, int64_t cols) {
-  if (!p && rows > 0) return fail_text(h->err, ARTOPK_EINVAL, "%s is NULL", name);
-  if (reinterpret_cast<uintptr_t>(p) % elem_size(type))
-    return fail_text(h->err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
-  if (rows > 1 && stride < cols)
-    return fail_text(h->err, ARTOPK_EINVAL, "%s's rows are %lld apart and %lld long", name, (long long)stride, (long long)cols);
-  if (stride < 0 || stride >= (1ll << 40)) return fail_text(h->err, ARTOPK_EINVAL, "%s's stride is outside [0, 2^40)", name);
-  // (so that places of elements, and of bytes, are far from 2^63)
-  if (rows > 1 && stride > kMostElems / (rows - 1))
-    return fail_text(h->err, ARTOPK_EINVAL, "%s's rows reach over more than 2^46 elements", name);
-  return ARTOPK_OK;
-}
-
 int check_problem(artopk_norm* h, int32_t type, int64_t rows, int64_t cols) {
   if (!known_type(type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type %d", type);
   if (rows < 0 || rows > h->max_rows)
@@ -91,47 +73,6 @@ int check_floats(artopk_norm* h, const char* name, const void* p, size_t size = 
     return fail_text(h->err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
   return ARTOPK_OK;
 }
-
-// The buffers of one call, as rows of bytes; those of x, dy, y and dx may be columns of one matrix and so lie between each
-// other's rows.  A buffer that is written must not share a byte with any other.
-class RowSet {
- public:
-  void add(const void* p, int64_t stride, int64_t rows, int64_t cols, size_t size, bool written, const char* name) {
-    if (!p || rows == 0) return;
-    r_[n_++] = Rows{reinterpret_cast<uintptr_t>(p), rows > 1 ? (size_t)stride * size : 0, (size_t)cols * size, rows, written, name};
-  }
-  void add(const void* p, int64_t count, size_t size, bool written, const char* name) { add(p, 0, 1, count, size, written, name); }
-  // ARTOPK_OK, or ARTOPK_EINVAL with the first offending pair in `err`
-  int check(char* err) const {
-    for (int i = 0; i < n_; ++i)
-      for (int j = 0; j < i; ++j)
-        if ((r_[i].written || r_[j].written) && (r_[j].at < r_[i].at ? meet(r_[j], r_[i]) : meet(r_[i], r_[j])))
-          return fail_text(err, ARTOPK_EINVAL, "buffers %s and %s overlap", r_[j].name, r_[i].name);
-    return ARTOPK_OK;
-  }
-
- private:
-  struct Rows {
-    uintptr_t at;
-    size_t pitch, width;  // pitch: 0 for one row
-    int64_t rows;
-    bool written;
-    const char* name;
-    uintptr_t end() const { return at + (size_t)(rows - 1) * pitch + width; }
-  };
-  // a begins where b does, or before
-  static bool meet(const Rows& a, const Rows& b) {
-    if (b.at >= a.end()) return false;
-    if (!a.pitch) return true;                    // b begins inside
-    const size_t in = (b.at - a.at) % a.pitch;    // b's first byte, from the row of a before it
-    if (in < a.width) return true;
-    if (b.pitch && b.pitch != a.pitch) return true;  // (may be; taken for yes)
-    // between two rows of a, or behind the last, which b.at < a.end() rules out
-    return in + b.width > a.pitch;
-  }
-  Rows r_[8];  // as many as a call has
-  int n_ = 0;
-};
 
 // Whether rows at p can be read sixteen bytes at a time.
 bool wide_rows(const void* p, int64_t stride, int64_t rows, size_t size) {
@@ -282,8 +223,8 @@ int artopk_layernorm_forward(artopk_norm* norm, const void* x, int64_t x_stride,
   int rc;
   if ((rc = check_problem(norm, type, rows, cols))) return rc;
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail_text(norm->err, ARTOPK_EINVAL, "eps is negative or not finite");
-  if ((rc = check_rows(norm, "x", x, x_stride, type, rows, cols))) return rc;
-  if ((rc = check_rows(norm, "y", y, y_stride, type, rows, cols))) return rc;
+  if ((rc = check_rows(norm->err, "x", x, x_stride, elem_size(type), rows, cols))) return rc;
+  if ((rc = check_rows(norm->err, "y", y, y_stride, elem_size(type), rows, cols))) return rc;
   if ((rc = check_floats(norm, "gamma", gamma)) || (rc = check_floats(norm, "beta", beta)) ||
       (rc = check_floats(norm, "mean_out", mean_out)) || (rc = check_floats(norm, "rstd_out", rstd_out)))
     return rc;
@@ -319,9 +260,9 @@ int artopk_layernorm_backward(artopk_norm* norm, const void* dy, int64_t dy_stri
   if ((rc = check_problem(norm, type, rows, cols))) return rc;
   if (!known_type(grad_type)) return fail_text(norm->err, ARTOPK_EINVAL, "unknown gradient element type %d", grad_type);
   if (!dx && !dgamma && !dbeta) return fail_text(norm->err, ARTOPK_EINVAL, "dx, dgamma and dbeta are all NULL");
-  if ((rc = check_rows(norm, "dy", dy, dy_stride, type, rows, cols))) return rc;
-  if ((rc = check_rows(norm, "x", x, x_stride, type, rows, cols))) return rc;
-  if (dx && (rc = check_rows(norm, "dx", dx, dx_stride, type, rows, cols))) return rc;
+  if ((rc = check_rows(norm->err, "dy", dy, dy_stride, elem_size(type), rows, cols))) return rc;
+  if ((rc = check_rows(norm->err, "x", x, x_stride, elem_size(type), rows, cols))) return rc;
+  if (dx && (rc = check_rows(norm->err, "dx", dx, dx_stride, elem_size(type), rows, cols))) return rc;
   if (rows > 0 && (!mean || !rstd)) return fail_text(norm->err, ARTOPK_EINVAL, "mean or rstd is NULL");
   const size_t gsize = elem_size(grad_type);
   if ((rc = check_floats(norm, "gamma", gamma)) || (rc = check_floats(norm, "mean", mean)) ||

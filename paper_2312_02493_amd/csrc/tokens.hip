@@ -1,0 +1,391 @@
+// Host side of the token entry points (embedding and log probabilities): argument checks, the choice of a kernel's shape, launches.
+
+#include "artopk.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+
+#include "host_common.h"
+#include "logprobs_kernels.h"
+
+using namespace artopk;
+
+struct artopk_tokens {
+  hipStream_t stream = nullptr;
+  int num_cu = 256;
+  int64_t max_tokens = 0, max_vocab = 0, max_width = 0;
+  uint8_t* slab = nullptr;
+  // within the slab: sorted tokens and their places (two of each, one pass reads what the other wrote), how often tiles have
+  // digits, shares of tokens' sums, the error word
+  uint32_t *key[2] = {nullptr, nullptr}, *pos[2] = {nullptr, nullptr}, *counts = nullptr;
+  float* part = nullptr;
+  int* error = nullptr;
+  char err[kErrText] = {0};
+};
+
+namespace {
+
+constexpr int64_t kMostWidth = 65536;
+constexpr int64_t kMostBlocks = 1 << 20;
+
+#define TOKENS_TRY(h, expr)                                                                                    \
+  do {                                                                                                         \
+    hipError_t e_ = (expr);                                                                                    \
+    if (e_ != hipSuccess)                                                                                      \
+      return fail_text((h)->err, ARTOPK_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, \
+                       __LINE__);                                                                              \
+  } while (0)
+
+bool valid_limits(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
+  return max_tokens >= 1 && max_tokens < (1ll << 31) && max_vocab >= 1 && max_vocab < (1ll << 31) && max_width >= 1 &&
+         max_width <= kMostWidth;
+}
+
+int64_t runs_of(int64_t count) { return (count + kSumRun - 1) / kSumRun; }
+
+struct Layout {
+  size_t key[2], pos[2], counts, part, error, bytes;
+  Layout(int64_t tokens, int64_t width) {
+    size_t at = 0;
+    auto take = [&](size_t n) {
+      const size_t here = at;
+      at = align_up(at + n, 256);
+      return here;
+    };
+    for (int i = 0; i < 2; ++i) {
+      key[i] = take((size_t)tokens * 4);
+      pos[i] = take((size_t)tokens * 4);
+    }
+    counts = take((size_t)kSortTiles * kSortDigits * 4);
+    part = take((size_t)runs_of(tokens) * 2 * (size_t)width * 4);
+    error = take(4);
+    bytes = at;
+  }
+};
+
+int check_vector(char* err, const char* name, const void* p, size_t size) {
+  if (reinterpret_cast<uintptr_t>(p) % size) return fail_text(err, ARTOPK_EINVAL, "%s is not aligned to its elements", name);
+  return ARTOPK_OK;
+}
+
+int check_tokens(artopk_tokens* h, const void* tokens, int32_t bits, int64_t count, int64_t vocab) {
+  if (count < 0 || count > h->max_tokens)
+    return fail_text(h->err, ARTOPK_EINVAL, "%lld tokens are outside [0, %lld]", (long long)count, (long long)h->max_tokens);
+  if (vocab < 1 || vocab > h->max_vocab)
+    return fail_text(h->err, ARTOPK_EINVAL, "vocab=%lld outside [1, %lld]", (long long)vocab, (long long)h->max_vocab);
+  if (bits != 32 && bits != 64) return fail_text(h->err, ARTOPK_EINVAL, "tokens of %d bits: 32 or 64 are taken", bits);
+  return check_vector(h->err, "tokens", tokens, bits / 8);
+}
+
+int check_scale(artopk_tokens* h, float scale) {
+  if (!std::isfinite(scale)) return fail_text(h->err, ARTOPK_EINVAL, "scale is not finite");
+  return ARTOPK_OK;
+}
+
+template <class TT, class TY, int V>
+void embed(artopk_tokens* h, const TT* table, int64_t table_stride, int64_t vocab, int64_t cols, const Tokens& tokens, int64_t count,
+           float scale, TY* y, int64_t y_stride) {
+  const int64_t pieces = (cols + V - 1) / V;
+  int lg = 0;
+  while (lg < 6 && (kEmbedPieces << lg) < pieces) ++lg;
+  const int64_t tiles = (pieces + (kEmbedPieces << lg) - 1) / (kEmbedPieces << lg), per = 64 >> lg;
+  const int64_t units = (count + per - 1) / per * tiles;
+  const unsigned blocks = (unsigned)std::min<int64_t>((units + 3) / 4, kMostBlocks);
+  k_embed<TT, TY, V><<<blocks, 256, 0, h->stream>>>(table, table_stride, vocab, tokens, count, cols, scale, y, y_stride, lg, units,
+                                                    tiles, h->error);
+}
+
+// Sorts the places of `count` tokens by token; the result is in key[r], pos[r], r returned.
+int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t vocab) {
+  int all = 1;
+  while (vocab >> all) ++all;  // bits of 0 .. vocab, which stands for no token
+  const int passes = (all + kSortBits - 1) / kSortBits;
+  const int64_t round = kSortThreads * 4;
+  const int64_t per = std::max<int64_t>(1, (count + round * kSortTiles - 1) / (round * kSortTiles)) * round;
+  const int tiles = (int)((count + per - 1) / per);
+  int from = 1, shift = 0;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int bits = (all - shift + passes - pass - 1) / (passes - pass);
+    const SortKeys in = {tokens, h->key[from], h->pos[from], (uint32_t)vocab, pass == 0};
+    k_sort_count<<<tiles, kSortThreads, 0, h->stream>>>(in, count, per, shift, bits, h->counts, h->error);
+    k_sort_place<<<tiles, kSortThreads, 0, h->stream>>>(in, count, per, shift, bits, h->counts, tiles, h->key[1 - from],
+                                                        h->pos[1 - from]);
+    shift += bits;
+    from = 1 - from;
+  }
+  return from;
+}
+
+template <class TD, class TG, int V>
+void embed_sums(artopk_tokens* h, const uint32_t* key, const uint32_t* pos, int64_t count, int64_t vocab, const TD* dy,
+                int64_t dy_stride, int64_t cols, float scale, TG* dtable, int64_t grad_stride, int add) {
+  const int64_t tiles = (cols + 64 * V - 1) / (64 * V), units = runs_of(count) * tiles;
+  const unsigned blocks = (unsigned)std::min<int64_t>((units + 3) / 4, kMostBlocks);
+  k_embed_sum<TD, TG, V><<<blocks, 256, 0, h->stream>>>(key, pos, count, (uint32_t)vocab, dy, dy_stride, cols, scale, dtable,
+                                                        grad_stride, add, h->part, units, tiles);
+}
+
+}  // namespace
+
+int64_t artopk_tokens_scratch_bytes(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
+  if (!valid_limits(max_tokens, max_vocab, max_width)) return -1;
+  return (int64_t)Layout(max_tokens, max_width).bytes;
+}
+
+int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vocab, int64_t max_width, void* hip_stream) {
+  if (!out) return fail_text(g_noctx_err, ARTOPK_EINVAL, "out is NULL");
+  if (!valid_limits(max_tokens, max_vocab, max_width))
+    return fail_text(g_noctx_err, ARTOPK_EINVAL,
+                     "max_tokens=%lld and max_vocab=%lld have to be in [1, 2^31), max_width=%lld in [1, %lld]", (long long)max_tokens,
+                     (long long)max_vocab, (long long)max_width, (long long)kMostWidth);
+  artopk_tokens* h = new (std::nothrow) artopk_tokens();
+  if (!h) return fail_text(g_noctx_err, ARTOPK_ENOMEM, "out of host memory");
+  h->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  h->max_tokens = max_tokens;
+  h->max_vocab = max_vocab;
+  h->max_width = max_width;
+  int dev = 0, cus = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) {
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "no device: %s", hipGetErrorString(e));
+  }
+  if (cus > 0) h->num_cu = cus;
+  const Layout at(max_tokens, max_width);
+  void* p = nullptr;
+  e = hipMalloc(&p, at.bytes);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_ENOMEM, "hipMalloc failed: %s", hipGetErrorString(e));
+  }
+  h->slab = static_cast<uint8_t*>(p);
+  for (int i = 0; i < 2; ++i) {
+    h->key[i] = reinterpret_cast<uint32_t*>(h->slab + at.key[i]);
+    h->pos[i] = reinterpret_cast<uint32_t*>(h->slab + at.pos[i]);
+  }
+  h->counts = reinterpret_cast<uint32_t*>(h->slab + at.counts);
+  h->part = reinterpret_cast<float*>(h->slab + at.part);
+  h->error = reinterpret_cast<int*>(h->slab + at.error);
+  const int zero = 0;
+  e = hipMemcpy(h->error, &zero, sizeof(zero), hipMemcpyHostToDevice);
+  if (e != hipSuccess) {
+    (void)hipFree(h->slab);
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "hipMemcpy failed: %s", hipGetErrorString(e));
+  }
+  *out = h;
+  return ARTOPK_OK;
+}
+
+int artopk_tokens_destroy(artopk_tokens* tokens) {
+  if (!tokens) return ARTOPK_EINVAL;
+  if (tokens->slab) (void)hipFree(tokens->slab);
+  delete tokens;
+  return ARTOPK_OK;
+}
+
+const char* artopk_tokens_last_error(const artopk_tokens* tokens) { return tokens ? tokens->err : g_noctx_err; }
+
+int artopk_tokens_status(artopk_tokens* tokens) {
+  if (!tokens) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_tokens_status: tokens is NULL");
+  TOKENS_TRY(tokens, hipStreamSynchronize(tokens->stream));
+  int word = 0;
+  TOKENS_TRY(tokens, hipMemcpy(&word, tokens->error, sizeof(word), hipMemcpyDeviceToHost));
+  if (!word) return ARTOPK_OK;
+  const int zero = 0;
+  TOKENS_TRY(tokens, hipMemcpy(tokens->error, &zero, sizeof(zero), hipMemcpyHostToDevice));
+  return fail_text(tokens->err, ARTOPK_ESTATE, "a token was not below vocab");
+}
+
+int artopk_embedding_forward(artopk_tokens* h, const void* table, int64_t table_stride, int32_t table_type, int64_t vocab,
+                             int64_t width, const void* tokens, int32_t token_bits, int64_t count, float scale, void* y,
+                             int64_t y_stride, int32_t type) {
+  if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_embedding_forward: handle is NULL");
+  int rc;
+  if (!known_type(type) || !known_type(table_type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type");
+  if ((rc = check_tokens(h, tokens, token_bits, count, vocab)) || (rc = check_scale(h, scale))) return rc;
+  if (width < 1 || width > h->max_width)
+    return fail_text(h->err, ARTOPK_EINVAL, "width=%lld outside [1, %lld]", (long long)width, (long long)h->max_width);
+  if ((rc = check_rows(h->err, "table", table, table_stride, elem_size(table_type), vocab, width))) return rc;
+  if ((rc = check_rows(h->err, "y", y, y_stride, elem_size(type), count, width))) return rc;
+  if (!tokens && count > 0) return fail_text(h->err, ARTOPK_EINVAL, "tokens is NULL");
+  {
+    RowSet rs;
+    rs.add(table, table_stride, vocab, width, elem_size(table_type), false, "table");
+    rs.add(tokens, count, token_bits / 8, false, "tokens");
+    rs.add(y, y_stride, count, width, elem_size(type), true, "y");
+    if ((rc = rs.check(h->err))) return rc;
+  }
+  if (count == 0) return ARTOPK_OK;
+  const Tokens tok = {tokens, token_bits == 64};
+  with_type(table_type, [&](auto* tt) {
+    using TT = std::remove_pointer_t<decltype(tt)>;
+    with_type(type, [&](auto* ty) {
+      using TY = std::remove_pointer_t<decltype(ty)>;
+      constexpr int kWide = 16 / (sizeof(TT) < sizeof(TY) ? sizeof(TT) : sizeof(TY));
+      auto go = [&](auto V) {
+        embed<TT, TY, V()>(h, static_cast<const TT*>(table), table_stride, vocab, width, tok, count, scale, static_cast<TY*>(y),
+                           y_stride);
+      };
+      if (width >= kWide) go(std::integral_constant<int, kWide>());
+      else go(std::integral_constant<int, 1>());
+    });
+  });
+  TOKENS_TRY(h, hipGetLastError());
+  return ARTOPK_OK;
+}
+
+int artopk_embedding_backward(artopk_tokens* h, const void* dy, int64_t dy_stride, int32_t type, const void* tokens,
+                              int32_t token_bits, int64_t count, int64_t width, float scale, void* dtable, int64_t grad_stride,
+                              int32_t grad_type, int64_t vocab, int32_t accumulate) {
+  if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_embedding_backward: handle is NULL");
+  int rc;
+  if (!known_type(type) || !known_type(grad_type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type");
+  if ((rc = check_tokens(h, tokens, token_bits, count, vocab)) || (rc = check_scale(h, scale))) return rc;
+  if (width < 1 || width > h->max_width)
+    return fail_text(h->err, ARTOPK_EINVAL, "width=%lld outside [1, %lld]", (long long)width, (long long)h->max_width);
+  if ((rc = check_rows(h->err, "dy", dy, dy_stride, elem_size(type), count, width))) return rc;
+  if ((rc = check_rows(h->err, "dtable", dtable, grad_stride, elem_size(grad_type), vocab, width))) return rc;
+  if (!tokens && count > 0) return fail_text(h->err, ARTOPK_EINVAL, "tokens is NULL");
+  {
+    RowSet rs;
+    rs.add(dy, dy_stride, count, width, elem_size(type), false, "dy");
+    rs.add(tokens, count, token_bits / 8, false, "tokens");
+    rs.add(dtable, grad_stride, vocab, width, elem_size(grad_type), true, "dtable");
+    if ((rc = rs.check(h->err))) return rc;
+  }
+  const Tokens tok = {tokens, token_bits == 64};
+  int sorted = 0;
+  if (count > 0) sorted = sort_places(h, tok, count, vocab);
+  with_type(grad_type, [&](auto* tg) {
+    using TG = std::remove_pointer_t<decltype(tg)>;
+    TG* out = static_cast<TG*>(dtable);
+    if (!accumulate)
+      k_embed_zero<TG><<<(unsigned)std::min<int64_t>(vocab, kMostBlocks), 256, 0, h->stream>>>(out, grad_stride, vocab, width);
+    if (count == 0) return;
+    with_type(type, [&](auto* td) {
+      using TD = std::remove_pointer_t<decltype(td)>;
+      constexpr int kWide = 16 / sizeof(TD);
+      auto go = [&](auto V) {
+        embed_sums<TD, TG, V()>(h, h->key[sorted], h->pos[sorted], count, vocab, static_cast<const TD*>(dy), dy_stride, width, scale,
+                                out, grad_stride, accumulate != 0);
+      };
+      if (width >= kWide) go(std::integral_constant<int, kWide>());
+      else go(std::integral_constant<int, 1>());
+    });
+    const int64_t runs = runs_of(count);
+    if (runs > 1)
+      k_embed_join<TG><<<dim3((unsigned)std::min<int64_t>(runs - 1, kMostBlocks), (unsigned)((width + 63) / 64)), 1024, 0, h->stream>>>(
+          h->key[sorted], count, (uint32_t)vocab, h->part, width, scale, out, grad_stride, accumulate != 0, runs);
+  });
+  TOKENS_TRY(h, hipGetLastError());
+  return ARTOPK_OK;
+}
+
+int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, int32_t type, int64_t rows, int64_t vocab,
+                          const void* tokens, int32_t token_bits, float scale, float* logp_out, float* peak_out, float* logsum_out,
+                          float* entropy_out, int32_t top, int32_t* top_ids_out, float* top_logp_out) {
+  if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_token_logprobs: handle is NULL");
+  int rc;
+  if (!known_type(type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type %d", type);
+  if ((rc = check_tokens(h, tokens, token_bits, rows, vocab)) || (rc = check_scale(h, scale))) return rc;
+  if (!(scale > 0.0f)) return fail_text(h->err, ARTOPK_EINVAL, "scale is not positive");
+  if ((rc = check_rows(h->err, "logits", logits, stride, elem_size(type), rows, vocab))) return rc;
+  if (logp_out && !tokens && rows > 0) return fail_text(h->err, ARTOPK_EINVAL, "tokens is NULL");
+  if (top < 0 || top > ARTOPK_MAX_TOP || top > vocab)
+    return fail_text(h->err, ARTOPK_EINVAL, "top=%d outside [0, %d] or more than vocab", top, ARTOPK_MAX_TOP);
+  if (top && rows > 0 && (!top_ids_out || !top_logp_out))
+    return fail_text(h->err, ARTOPK_EINVAL, "top_ids_out or top_logp_out is NULL");
+  if (rows > 0 && !logp_out && !peak_out && !logsum_out && !entropy_out && !top)
+    return fail_text(h->err, ARTOPK_EINVAL, "nothing is asked for");
+  if ((rc = check_vector(h->err, "logp_out", logp_out, 4)) || (rc = check_vector(h->err, "peak_out", peak_out, 4)) ||
+      (rc = check_vector(h->err, "logsum_out", logsum_out, 4)) || (rc = check_vector(h->err, "entropy_out", entropy_out, 4)) ||
+      (rc = check_vector(h->err, "top_ids_out", top_ids_out, 4)) || (rc = check_vector(h->err, "top_logp_out", top_logp_out, 4)))
+    return rc;
+  {
+    RowSet rs;
+    rs.add(logits, stride, rows, vocab, elem_size(type), false, "logits");
+    rs.add(tokens, rows, token_bits / 8, false, "tokens");
+    rs.add(logp_out, rows, 4, true, "logp_out");
+    rs.add(peak_out, rows, 4, true, "peak_out");
+    rs.add(logsum_out, rows, 4, true, "logsum_out");
+    rs.add(entropy_out, rows, 4, true, "entropy_out");
+    rs.add(top ? top_ids_out : nullptr, rows * top, 4, true, "top_ids_out");
+    rs.add(top ? top_logp_out : nullptr, rows * top, 4, true, "top_logp_out");
+    if ((rc = rs.check(h->err))) return rc;
+  }
+  if (rows == 0) return ARTOPK_OK;
+  const Tokens tok = {tokens, token_bits == 64};
+  const LogpOut out = {logp_out, peak_out, logsum_out, entropy_out, top_ids_out, top_logp_out};
+  with_type(type, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    const unsigned blocks = (unsigned)std::min<int64_t>(rows, kMostBlocks);
+    auto go = [&](auto TOP) {
+      k_logp<T, TOP()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok, logp_out != nullptr,
+                                                      scale, scale * kLog2e, top, out, h->error);
+    };
+    if (top) go(std::true_type());
+    else go(std::false_type());
+  });
+  TOKENS_TRY(h, hipGetLastError());
+  return ARTOPK_OK;
+}
+
+int artopk_token_logprobs_backward(artopk_tokens* h, const void* logits, int64_t stride, int32_t type, int64_t rows, int64_t vocab,
+                                   const void* tokens, int32_t token_bits, float scale, const float* peak, const float* logsum,
+                                   const float* entropy, const float* dlogp, const float* dlse, const float* dentropy,
+                                   void* dlogits, int64_t dstride) {
+  if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_token_logprobs_backward: handle is NULL");
+  int rc;
+  if (!known_type(type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type %d", type);
+  if ((rc = check_tokens(h, tokens, token_bits, rows, vocab)) || (rc = check_scale(h, scale))) return rc;
+  if (!(scale > 0.0f)) return fail_text(h->err, ARTOPK_EINVAL, "scale is not positive");
+  const size_t size = elem_size(type);
+  if ((rc = check_rows(h->err, "logits", logits, stride, size, rows, vocab))) return rc;
+  if ((rc = check_rows(h->err, "dlogits", dlogits, dstride, size, rows, vocab))) return rc;
+  if (rows > 0 && (!peak || !logsum)) return fail_text(h->err, ARTOPK_EINVAL, "peak or logsum is NULL");
+  if (rows > 0 && !dlogp && !dlse && !dentropy) return fail_text(h->err, ARTOPK_EINVAL, "dlogp, dlse and dentropy are all NULL");
+  if (dlogp && !tokens && rows > 0) return fail_text(h->err, ARTOPK_EINVAL, "tokens is NULL");
+  if (dentropy && !entropy && rows > 0) return fail_text(h->err, ARTOPK_EINVAL, "dentropy is given without entropy");
+  const struct {
+    const char* name;
+    const float* p;
+  } vectors[] = {{"peak", peak}, {"logsum", logsum}, {"entropy", entropy}, {"dlogp", dlogp}, {"dlse", dlse}, {"dentropy", dentropy}};
+  RowSet rs;
+  for (const auto& v : vectors) {
+    if ((rc = check_vector(h->err, v.name, v.p, 4))) return rc;
+    rs.add(v.p, rows, 4, false, v.name);
+  }
+  rs.add(tokens, rows, token_bits / 8, false, "tokens");
+  // (in place: the same rows of the same matrix)
+  const bool in_place = logits == dlogits && (rows <= 1 || stride == dstride);
+  if (!in_place) rs.add(logits, stride, rows, vocab, size, false, "logits");
+  rs.add(dlogits, dstride, rows, vocab, size, true, "dlogits");
+  if ((rc = rs.check(h->err))) return rc;
+  if (rows == 0) return ARTOPK_OK;
+  const Tokens tok = {tokens, token_bits == 64};
+  const LogpGrads in = {peak, logsum, entropy, dlogp, dlse, dentropy};
+  // pieces of both at the same places within sixteen bytes
+  const bool same = (reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(dlogits)) % 16 == 0 &&
+                    (rows <= 1 || (stride - dstride) * (int64_t)size % 16 == 0);
+  with_type(type, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    const int64_t pieces = (vocab + 2 * (RowPieces<T>::V - 1)) / RowPieces<T>::V;  // at most, wherever rows begin
+    const int tiles = (int)((pieces + 1023) / 1024);
+    const int64_t units = rows * tiles;
+    const unsigned blocks = (unsigned)std::min<int64_t>(units, kMostBlocks);
+    auto go = [&](auto SAME) {
+      k_logp_backward<T, SAME()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok,
+                                                                dlogp != nullptr, scale, scale * kLog2e, in, static_cast<T*>(dlogits),
+                                                                dstride, units, tiles, h->error);
+    };
+    if (same) go(std::true_type());
+    else go(std::false_type());
+  });
+  TOKENS_TRY(h, hipGetLastError());
+  return ARTOPK_OK;
+}

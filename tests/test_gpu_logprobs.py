@@ -1,0 +1,491 @@
+"""Log probabilities of given tokens, entropy, top alternatives, and their gradient, against the definition in 64 bits.
+
+Tolerances, u = 2^-24.  With d = scale (x - peak) and e = e^d for each element beside the largest: an exponent in units of
+log2 is a difference, a product with c = scale log2(e) (itself three roundings off) and a power of two good to 2 u; the
+difference may be taken in two parts, from a reference up to 16 (in those units, 11.1 in natural ones) below the thread's largest
+element on.  So e is off by at most (6 (|d| + 2 * 11.1) + 2) u of itself: FIXED = 136 and 6 |d|.  A sum over n elements is made
+of at most `depth` additions one after the other (the thread's own, then eight halvings, with a factor good to 4 u each, and up
+to 24 rescalings of a thread's sum, of 4 u each).  Each quantity's own operations add a few u of its size.
+"""
+
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+OUT_U = {"f32": U, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -25}
+FIXED = 136.0
+
+
+def _dtype(t):
+    import torch
+
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[t]
+
+
+def _gen(seed):
+    import torch
+
+    return torch.Generator().manual_seed(seed)
+
+
+def _placed(a, pad, shift, dtype):
+    import torch
+
+    rows, cols = a.shape
+    mem = torch.full((shift + rows * (cols + pad) + 8,), 77.0, dtype=dtype, device="cuda")
+    view = mem[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    view.copy_(a)
+    return mem, view
+
+
+def _rest(mem, rows, cols, pad, shift):
+    import torch
+
+    keep = torch.ones(mem.numel(), dtype=torch.bool, device="cuda")
+    keep[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols] = False
+    return bool((mem[keep] == 77.0).all())
+
+
+def _logits(rows, vocab, seed, kind):
+    """kind: plain; masked (some -inf, every third row nothing else); lowest (the type's lowest value instead); sure (one
+    element far above); rising and falling (in order, as no real row is); equal; few (many equal values); wide (far apart)."""
+    import torch
+
+    g = _gen(seed)
+    x = 3.0 * torch.randn(rows, vocab, generator=g)
+    if kind == "sure":
+        x[torch.arange(rows), torch.randint(0, vocab, (rows,), generator=g)] = 25.0
+    if kind == "rising":
+        x = torch.sort(x, 1).values
+    if kind == "falling":
+        x = torch.sort(x, 1, descending=True).values
+    if kind == "equal":
+        x = torch.full_like(x, -1.5)
+    if kind == "few":
+        x = torch.randint(-2, 3, (rows, vocab), generator=g).float() * 0.0 + torch.randint(-2, 3, (rows, vocab), generator=g)
+        x[x == 0] = -0.0
+        x[:, ::3][x[:, ::3] == 0] = 0.0
+    if kind == "wide":
+        x = x * 300.0
+    if kind in ("masked", "lowest"):
+        x[torch.rand(rows, vocab, generator=g) < 0.5] = -math.inf
+        x[::3] = -math.inf
+    return x
+
+
+def _typed(x, t, kind):
+    import torch
+
+    y = x.to(_dtype(t))
+    return torch.where(torch.isinf(y), torch.full_like(y, torch.finfo(y.dtype).min), y) if kind == "lowest" else y
+
+
+class Row64:
+    """The definition in 64 bits, with the sums that the tolerances need."""
+
+    def __init__(self, x, scale):
+        import torch
+
+        self.scale = scale
+        self.x = x.double()
+        self.peak = self.x.amax(1, keepdim=True)
+        self.none = self.peak == -math.inf
+        base = torch.where(self.none, torch.zeros_like(self.peak), self.peak)
+        self.d = scale * (self.x - base)
+        e = torch.exp(self.d)
+        e.scatter_(1, self.x.argmax(1, keepdim=True), 0.0)
+        ad = torch.where(e > 0, self.d.abs(), torch.zeros_like(self.d))
+        self.r, self.e1, self.e2 = e.sum(1), (e * ad).sum(1), (e * ad * ad).sum(1)
+        self.logsum = torch.log1p(self.r)
+        self.entropy = self.logsum + self.e1 / (1.0 + self.r)
+        self.entropy[self.none.view(-1)] = 0.0
+        self.logsum[self.none.view(-1)] = 0.0
+        self.logp = self.d - self.logsum.view(-1, 1)
+        vocab = x.shape[1]
+        depth = 8.0 * (-(-vocab // 2048) + 1) + 8 + 4 * 8 + 24 * 4  # (2048: four elements a thread at least)
+        per = FIXED + depth
+        dr = U * (per * self.r + 6.0 * self.e1)
+        # (powers of two below 2^-126 are zero: at most so much of each element, in the entropy times |d| <= 88)
+        lost = vocab * 2.0 ** -126
+        self.tol_logsum = dr / (1.0 + self.r) + 4.0 * U * self.logsum + lost
+        du = U * ((per + 4.0) * self.e1 + 6.0 * self.e2 + FIXED * self.r)
+        self.tol_entropy = (self.tol_logsum + du / (1.0 + self.r) + self.e1 * dr / (1.0 + self.r) ** 2
+                            + 6.0 * U * self.entropy + 88.0 * lost)
+
+    def tol_logp(self, d):
+        return 4.0 * U * d.abs() + self.tol_logsum.view(-1, 1) + U * (d - self.logsum.view(-1, 1)).abs()
+
+
+def _forward(x, tok, top, scale, pad, shift, t, wide=True):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    rows, vocab = x.shape
+    mem, view = _placed(x, pad, shift, _dtype(t))
+    ctx = lib.TokenContext(rows, vocab)
+    logp, peak, logsum, entropy = (torch.full((rows,), 9.0, device="cuda") for _ in range(4))
+    ids, lps = torch.full((rows, top), -9, dtype=torch.int32, device="cuda"), torch.full((rows, top), 9.0, device="cuda")
+    ctx.artopk_token_logprobs(view, tok.to("cuda", torch.int64 if wide else torch.int32), logp, peak, logsum, entropy,
+                              ids if top else None, lps if top else None, scale=scale)
+    ctx.status()
+    return ctx, mem, view, logp, peak, logsum, entropy, ids, lps
+
+
+def _near(got, want, tol, what):
+    import torch
+
+    got = got.cpu().double()
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    bad = ~(same | ((got - want).abs() <= tol))
+    n = int(bad.sum())
+    assert n == 0, (what, n, got[bad][:4], want[bad][:4], tol.expand_as(got)[bad][:4])
+
+
+def _check_forward(rows, vocab, t, kind, top, scale=1.0, pad=0, shift=0, seed=0, wide=True):
+    import torch
+
+    x = _typed(_logits(rows, vocab, seed, kind), t, kind)
+    g = _gen(seed + 1)
+    tok = torch.randint(0, vocab, (rows,), generator=g)
+    tok[1::4] = -1 - 5 * (seed % 2)
+    tok[2::4] = x.float().argmax(1)[2::4]
+    s = float(np.float32(scale))
+    ref = Row64(x, s)
+    _, mem, view, logp, peak, logsum, entropy, ids, lps = _forward(x, tok, top, scale, pad, shift, t, wide)
+    assert torch.equal(view.cpu(), x) and _rest(mem, rows, vocab, pad, shift)
+    assert torch.equal(peak.cpu().double(), ref.peak.view(-1))
+    _near(logsum, ref.logsum, ref.tol_logsum, "logsum")
+    _near(entropy, ref.entropy, ref.tol_entropy, "entropy")
+    d = ref.d.gather(1, tok.clamp(min=0).view(-1, 1))
+    want = torch.where(tok.view(-1, 1) >= 0, d - ref.logsum.view(-1, 1), torch.zeros_like(d))
+    want = torch.where((tok.view(-1, 1) >= 0) & ref.none, torch.full_like(d, -math.inf), want)
+    _near(logp, want.view(-1), ref.tol_logp(d.clamp(min=-1e30)).view(-1), "logp")
+    if top:
+        order = torch.sort(x.float() + 0.0, dim=1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(ids.cpu().long(), order), (ids[:2], order[:2])
+        d = ref.d.gather(1, order)
+        want = torch.where(ref.none, torch.full_like(d, -math.inf), d - ref.logsum.view(-1, 1))
+        _near(lps, want, ref.tol_logp(d.clamp(min=-1e30)), "top_logp")
+
+
+KINDS = ["plain", "masked", "lowest", "sure", "rising", "falling", "equal", "few", "wide"]
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 3, 7, 8, 9, 63, 64, 65, 255, 257, 1000, 2047, 2048, 2049, 4103, 10007, 33000])
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_forward_sizes(vocab, t):
+    rows = 5 if vocab > 5000 else 13
+    for i, top in enumerate(sorted({0, 1, min(vocab, 5), min(vocab, 64)})):
+        _check_forward(rows, vocab, t, "plain", top, pad=i, shift=(vocab + i) % 8, seed=vocab + i, wide=i % 2 == 0)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("top", [0, 1, 20, 64])
+def test_forward_kinds(kind, t, top):
+    _check_forward(7, 5003, t, kind, top, shift=1, seed=top)
+    _check_forward(300, 130, t, kind, top, shift=2, pad=1, seed=top + 1)
+
+
+@pytest.mark.parametrize("scale", [1e-3, 0.5, 1.4, 7.0])
+def test_forward_scales(scale):
+    _check_forward(9, 3001, "f32", "plain", 5, scale=scale)
+    _check_forward(9, 3001, "f16", "masked", 5, scale=scale)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 5, 40])
+@pytest.mark.parametrize("kind", ["plain", "rising", "falling", "masked", "equal"])
+def test_forward_few_long_rows(rows, kind):
+    _check_forward(rows, 131_001, "bf16", kind, 20, shift=3, pad=5, seed=rows)
+    _check_forward(rows, 200_000, "f32", kind, 33, seed=rows + 9)
+
+
+def test_forward_many_rows():
+    _check_forward(5000, 257, "bf16", "plain", 3, pad=1)
+    _check_forward(70_000, 12, "f16", "few", 2)
+
+
+def test_forward_parts_of_the_outputs():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    x = _logits(6, 500, 1, "plain").cuda()
+    tok = torch.arange(6).cuda()
+    ctx = lib.TokenContext(6, 500)
+    full = [torch.zeros(6).cuda() for _ in range(4)]
+    ctx.artopk_token_logprobs(x, tok, *full)
+    for i in range(4):
+        one = torch.zeros(6).cuda()
+        args = [None] * 4
+        args[i] = one
+        ctx.artopk_token_logprobs(x, tok if i == 0 else None, *args)
+        assert torch.equal(one, full[i])
+    ids, lps = torch.zeros(6, 2, dtype=torch.int32).cuda(), torch.zeros(6, 2).cuda()
+    ctx.artopk_token_logprobs(x, top_ids_out=ids, top_logp_out=lps)
+    assert torch.equal(ids.cpu().long(), torch.topk(x, 2, 1).indices.cpu())
+    ctx.artopk_token_logprobs(x[:0], tok[:0], *[f[:0] for f in full])
+    ctx.artopk_token_logprobs_backward(x[:0], tok[:0], full[1][:0], full[2][:0], x[:0].clone(), dlogp=full[0][:0])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_forward_nan_and_infinity(t):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    x = _logits(8, 3000, 2, "plain").to(_dtype(t)).cuda()
+    x[1, 77], x[3, 2999], x[5, 0], x[6] = math.nan, math.inf, -math.nan, math.nan
+    x[7, 100:] = -math.inf
+    tok = torch.full((8,), 5).cuda()
+    ctx = lib.TokenContext(8, 3000)
+    out = [torch.zeros(8).cuda() for _ in range(4)]
+    ids, lps = torch.full((8, 9), 4, dtype=torch.int32).cuda(), torch.zeros(8, 9).cuda()
+    ctx.artopk_token_logprobs(x, tok, *out, ids, lps)
+    broken = torch.tensor([False, True, False, True, False, True, True, False])
+    for o in [*out, lps[:, 0], lps[:, 8]]:
+        assert torch.equal(torch.isnan(o.cpu()), broken)
+    assert bool((ids[broken.cuda()] == -1).all()) and bool((ids[~broken.cuda()] >= 0).all())
+    dx = torch.zeros_like(x)
+    one = torch.ones(8).cuda()
+    ctx.artopk_token_logprobs_backward(x, tok, out[1], out[2], dx, dlogp=one, dentropy=one, entropy=out[3])
+    assert torch.equal(torch.isnan(dx.cpu()).all(1), broken) and torch.equal(torch.isnan(dx.cpu()).any(1), broken)
+
+
+def _check_backward(rows, vocab, t, kind, scale=1.0, pad=0, shift=0, dpad=None, dshift=None, seed=0, which="ple", in_place=False):
+    """which: p dlogp, l dlse, e dentropy."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    x = _typed(_logits(rows, vocab, seed, kind), t, kind)
+    g = _gen(seed + 5)
+    tok = torch.randint(0, vocab, (rows,), generator=g)
+    tok[1::4] = -1
+    tok[2::4] = x.float().argmax(1)[2::4]
+    s = float(np.float32(scale))
+    ref = Row64(x, s)
+    peak, logsum, entropy = ref.peak.view(-1).float(), ref.logsum.float(), ref.entropy.float()
+    dlogp, dlse, dent = (torch.randn(rows, generator=g) * f for f in (1.0, 0.3, 0.2))
+    dlogp[tok < 0] = math.nan  # not read
+    _, view = _placed(x, pad, shift, _dtype(t))
+    dpad, dshift = pad if dpad is None else dpad, shift if dshift is None else dshift
+    dmem, dview = _placed(torch.zeros(rows, vocab), dpad, dshift, _dtype(t))
+    if in_place:
+        dview.copy_(x)
+        view = dview
+    ctx = lib.TokenContext(rows, vocab)
+    dev = [v.cuda() for v in (peak, logsum, entropy, dlogp, dlse, dent)]
+    ctx.artopk_token_logprobs_backward(view, tok.cuda(), dev[0], dev[1], dview, dlogp=dev[3] if "p" in which else None,
+                                       dlse=dev[4] if "l" in which else None, entropy=dev[2] if "e" in which else None,
+                                       dentropy=dev[5] if "e" in which else None, scale=scale)
+    ctx.status()
+    zero = torch.zeros(rows, 1, dtype=torch.float64)
+    gp = torch.where(tok.view(-1, 1) >= 0, dlogp.double().view(-1, 1), zero) if "p" in which else zero
+    gl = dlse.double().view(-1, 1) if "l" in which else zero
+    ge, h = (dent.double().view(-1, 1), entropy.double().view(-1, 1)) if "e" in which else (zero, zero)
+    lp = (ref.d - logsum.double().view(-1, 1)).clamp(min=-1e4)
+    p = torch.exp(lp)
+    one = torch.zeros_like(p)
+    live = tok >= 0
+    one[live, tok[live]] = 1.0
+    minus = torch.where(one > 0, -torch.expm1(lp), -p)  # [index = token] - p
+    want = s * (gp * minus + gl * p - ge * p * (lp + h))
+    want = torch.where(ref.none, torch.zeros_like(want), want)
+    # log p: three roundings of c, a difference, a product, less logsum's own (three) and the sum's; p: two more
+    e = U * (6.0 * ref.d.abs().clamp(max=1e4) + 6.0 * logsum.double().view(-1, 1).abs() + 2.0 * lp.abs()) + 3.0 * U
+    size = s * (gl.abs() + gp.abs() + ge.abs() * (h.abs() + lp.abs()))
+    tol = p * (e + 10.0 * U) * size + s * ge.abs() * p * e + 10.0 * U * want.abs()
+    tol = tol + OUT_U[t] * (want.abs() + tol) + TINY[t] + 1e-35
+    _near(dview, want, tol, "dlogits")
+    assert _rest(dmem, rows, vocab, dpad, dshift)
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 9, 64, 65, 255, 1000, 2049, 8191, 8192, 8193, 16400])
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_backward_sizes(vocab, t):
+    _check_backward(6, vocab, t, "plain", shift=vocab % 8, pad=vocab % 3, seed=vocab)
+    _check_backward(6, vocab, t, "plain", shift=vocab % 8, pad=1, dpad=2, dshift=3, seed=vocab)
+    _check_backward(6, vocab, t, "plain", shift=1, in_place=True, seed=vocab)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_backward_kinds(kind, t):
+    _check_backward(12, 2501, t, kind, shift=1)
+    _check_backward(12, 333, t, kind, scale=0.6, pad=2)
+
+
+@pytest.mark.parametrize("which", ["p", "l", "e", "pl", "pe", "le"])
+def test_backward_parts(which):
+    _check_backward(9, 1001, "f32", "masked", which=which)
+    _check_backward(9, 1001, "bf16", "plain", which=which)
+
+
+def test_backward_many_rows():
+    _check_backward(40_000, 40, "f16", "plain", pad=1)
+
+
+def test_gradient_against_differences():
+    """The gradient of a weighted sum of logp, lse and entropy against central differences in 64 bits: with h = 1e-5 these
+    are off by h^2 times third derivatives (below 1e-9) and by 64-bit roundings over h."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g = _gen(3)
+    x = torch.randn(3, 11, generator=g)
+    tok = torch.tensor([4, -1, 0])
+    a, b, c = (torch.randn(3, generator=g) for _ in range(3))
+    scale = 0.75
+    ctx = lib.TokenContext(3, 11)
+    out = [torch.zeros(3).cuda() for _ in range(4)]
+    ctx.artopk_token_logprobs(x.cuda(), tok.cuda(), *out, scale=scale)
+    dx = torch.zeros(3, 11).cuda()
+    ctx.artopk_token_logprobs_backward(x.cuda(), tok.cuda(), out[1], out[2], dx, dlogp=a.cuda(), dlse=b.cuda(), entropy=out[3],
+                                       dentropy=c.cuda(), scale=scale)
+
+    def loss(v):
+        z = scale * v
+        lse = torch.logsumexp(z, 1)
+        lp = z - lse.view(-1, 1)
+        own = torch.where(tok >= 0, lp.gather(1, tok.clamp(min=0).view(-1, 1)).view(-1), torch.zeros(3, dtype=torch.float64))
+        return float((a * own + b * lse - c * (lp.exp() * lp).sum(1)).sum())
+
+    for i in range(3):
+        for j in range(11):
+            up, down = x.double(), x.double()
+            up[i, j] += 1e-5
+            down[i, j] -= 1e-5
+            assert abs((loss(up) - loss(down)) / 2e-5 - float(dx[i, j])) < 1e-8 + 200 * U
+
+
+def test_tokens_beyond_the_vocabulary():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    x = _logits(4, 100, 4, "plain").cuda()
+    ctx = lib.TokenContext(4, 100)
+    out = [torch.zeros(4).cuda() for _ in range(4)]
+    for tok in (torch.tensor([5, 100, -1, 3]), torch.tensor([5, 1 << 35, -(1 << 35), 3])):
+        ctx.artopk_token_logprobs(x, tok.cuda(), *out)
+        with pytest.raises(lib.ArTopkError) as e:
+            ctx.status()
+        assert e.value.code == -4
+        ctx.status()
+        assert torch.isnan(out[0]).tolist() == [False, True, False, False]
+        assert not bool(torch.isnan(torch.stack(out[1:])).any())
+        dx = torch.zeros(4, 100).cuda()
+        ctx.artopk_token_logprobs_backward(x, tok.cuda(), out[1], out[2], dx, dlogp=torch.ones(4).cuda())
+        with pytest.raises(lib.ArTopkError):
+            ctx.status()
+        assert torch.isnan(dx).all(1).tolist() == torch.isnan(dx).any(1).tolist() == [False, True, False, False]
+
+
+def test_places_beyond_32_bits():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    far = (1 << 31) + 1000
+    mem = torch.zeros(2 * far, dtype=torch.bfloat16, device="cuda")
+    x = mem.view(2, far)[:, :3000]
+    x[0, 7], x[1, 2999] = 5.0, 6.0
+    dx = torch.zeros(2 * far, dtype=torch.bfloat16, device="cuda").view(2, far)[:, :3000]
+    ctx = lib.TokenContext(2, 3000)
+    out = [torch.zeros(2).cuda() for _ in range(4)]
+    ids, lps = torch.zeros(2, 1, dtype=torch.int32).cuda(), torch.zeros(2, 1).cuda()
+    tok = torch.tensor([7, 2999]).cuda()
+    ctx.artopk_token_logprobs(x, tok, *out, ids, lps)
+    assert ids.view(-1).tolist() == [7, 2999] and torch.equal(out[0], lps.view(-1))
+    ctx.artopk_token_logprobs_backward(x, tok, out[1], out[2], dx, dlogp=torch.ones(2).cuda())
+    assert float(dx[0, 7]) > 0 > float(dx[1, 0]) and float(dx[1, 2999]) > 0
+
+
+def test_another_stream_and_graph_replays():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g = _gen(12)
+    for rows, vocab in ((3, 20_000), (400, 1003)):
+        x, tok = torch.randn(rows, vocab).to(torch.bfloat16).cuda(), torch.randint(-1, vocab, (rows,), generator=g).cuda()
+        out = [torch.zeros(rows).cuda() for _ in range(4)]
+        ids, lps = torch.zeros(rows, 6, dtype=torch.int32).cuda(), torch.zeros(rows, 6).cuda()
+        dx, one = torch.zeros_like(x), torch.ones(rows).cuda()
+
+        def both(ctx):
+            ctx.artopk_token_logprobs(x, tok, *out, ids, lps)
+            ctx.artopk_token_logprobs_backward(x, tok, out[1], out[2], dx, dlogp=one, entropy=out[3], dentropy=one)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            ctx = lib.TokenContext(rows, vocab)
+            both(ctx)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                both(ctx)
+        for turn in range(4):
+            x.copy_(torch.randn(rows, vocab, generator=g))
+            tok.copy_(torch.randint(-1, vocab, (rows,), generator=g))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            kept = [v.clone() for v in (*out, ids, lps, dx)]
+            for v in (*out, ids, lps, dx):
+                v.zero_()
+            both(lib.TokenContext(rows, vocab))
+            for a, b in zip(kept, (*out, ids, lps, dx)):
+                assert torch.equal(a, b), turn
+
+
+def test_refusals():
+    import torch
+    import paper_2312_02493_amd as lib
+
+    ctx = lib.TokenContext(10, 200)
+    x, tok = torch.zeros(10, 200).cuda(), torch.zeros(10, dtype=torch.int64).cuda()
+    v = [torch.zeros(10).cuda() for _ in range(4)]
+    ids, lps = torch.zeros(10, 3, dtype=torch.int32).cuda(), torch.zeros(10, 3).cuda()
+
+    def refused(f, *args, **kw):
+        with pytest.raises(lib.ArTopkError) as e:
+            f(*args, **kw)
+        assert e.value.code == -1
+        return str(e.value)
+
+    fwd, bwd = ctx.artopk_token_logprobs, ctx.artopk_token_logprobs_backward
+    assert "nothing" in refused(fwd, x, tok)
+    assert "tokens" in refused(fwd, x, None, v[0])
+    assert "tokens" in refused(fwd, x, tok.cpu(), v[0])
+    assert "scale" in refused(fwd, x, tok, v[0], scale=0.0)
+    assert "scale" in refused(fwd, x, tok, v[0], scale=-1.0)
+    assert "scale" in refused(fwd, x, tok, v[0], scale=float("nan"))
+    assert "overlap" in refused(fwd, x, tok, v[0], v[0])
+    assert "overlap" in refused(fwd, x, tok, x.view(-1)[5:15])
+    assert "logp_out" in refused(fwd, x, tok, v[0][:9])
+    assert "vocab" in refused(fwd, torch.zeros(10, 201).cuda(), tok, v[0])
+    assert "outside" in refused(fwd, torch.zeros(11, 200).cuda(), torch.zeros(11, dtype=torch.int64).cuda(), torch.zeros(11).cuda())
+    assert "top" in refused(fwd, x, tok, v[0], top_ids_out=ids)
+    assert "top" in refused(fwd, x, tok, v[0], top_ids_out=ids, top_logp_out=lps[:, :2])
+    assert "top" in refused(fwd, x, tok, v[0], top_ids_out=ids.long(), top_logp_out=lps)
+    big = [torch.zeros(10, 65, dtype=k).cuda() for k in (torch.int32, torch.float32)]
+    assert "top" in refused(fwd, x, tok, v[0], top_ids_out=big[0], top_logp_out=big[1])
+    assert "top" in refused(fwd, x[:, :2], tok, v[0], top_ids_out=ids, top_logp_out=lps)
+    assert "NULL" in refused(bwd, x, tok, v[0], v[1], torch.zeros_like(x))
+    assert "entropy" in refused(bwd, x, tok, v[0], v[1], torch.zeros_like(x), dentropy=v[2])
+    assert "tokens" in refused(bwd, x, None, v[0], v[1], torch.zeros_like(x), dlogp=v[2])
+    assert "NULL" in refused(bwd, x, tok, None, v[1], torch.zeros_like(x), dlogp=v[2])
+    assert "shape" in refused(bwd, x, tok, v[0], v[1], torch.zeros(10, 199).cuda(), dlogp=v[2])
+    assert "overlap" in refused(bwd, x[:9], tok[:9], v[0][:9], v[1][:9], x[1:], dlogp=v[2][:9])
+    assert "overlap" in refused(bwd, x, tok, v[0], v[1], x, dlogp=x.view(-1)[:10])
+    raw, h = ctx._lib, ctx._h
+    assert raw.artopk_token_logprobs(h, x.data_ptr(), 200, 0, 10, 200, tok.data_ptr(), 64, 1.0, None, None, None, None, -1, None,
+                                     None) == -1
+    assert raw.artopk_token_logprobs(h, x.data_ptr(), 200, 0, 10, 200, tok.data_ptr(), 64, 1.0, v[0].data_ptr() + 2, None, None,
+                                     None, 0, None, None) == -1
+    assert raw.artopk_token_logprobs(h, x.data_ptr(), 200, 7, 10, 200, tok.data_ptr(), 64, 1.0, v[0].data_ptr(), None, None,
+                                     None, 0, None, None) == -1
+    fwd(x, tok, v[0])
+    ctx.status()
