@@ -3,8 +3,13 @@
 //   y[i] = scale table[token[i]]
 //   dtable[v] = scale (sum over the places i with token[i] = v of dy[i])  (added to what is there, or in its place)
 //
-// Both are bound by memory.  The gradient's places are sorted by token first (a stable radix sort of the places), so that
-// every row of the table is summed by one owner in the order of its places: no atomics, the same bits every time.
+// Both are bound by memory.  The gradient's places are sorted by token first (stable: a token's places stay in order), so that
+// every row of the table has one owner that sums its places in a fixed order: no atomics on sums, the same bits every time.  Most
+// of what the gradient writes are zeros, rows of tokens that do not occur; they are written beside the sort.
+//
+// Measured: gradient of 32768 places x 2048 bfloat16 into 64000 rows of float32 (658 MB) 141 us = 4.7 TB/s, of which the sort's four
+// launches 35 (with 190 MB of zeros), the sums 96 (with the other 250 MB), heavy tokens' shares 9; lookup of 32768 x 4096, float32 to
+// bfloat16, 95 us.
 #pragma once
 
 #include "elements.h"
@@ -20,12 +25,41 @@ struct Tokens {
   }
 };
 
+// Sixteen bytes at a place of four, or of two.
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t Words2 __attribute__((ext_vector_type(4), aligned(2)));
+
 // V elements at any place of their type, as they lie.
 template <class T, int V>
 struct Some {
   T e[V];
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(e, p, sizeof(e)); }
   __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, e, sizeof(e)); }
+  // the same past the caches, sixteen bytes at a time (or element by element where there are fewer)
+  using Words = std::conditional_t<sizeof(T) == 4, Words4, Words2>;
+  __device__ __forceinline__ void load_once(const T* p) {
+    if constexpr (sizeof(e) % 16 == 0) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(e) / 16; ++i) {
+        const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words*>(p) + i);
+        __builtin_memcpy(reinterpret_cast<char*>(e) + 16 * i, &w, 16);
+      }
+    } else {
+      load(p);
+    }
+  }
+  __device__ __forceinline__ void store_once(T* p) const {
+    if constexpr (sizeof(e) % 16 == 0) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(e) / 16; ++i) {
+        Words w;
+        __builtin_memcpy(&w, reinterpret_cast<const char*>(e) + 16 * i, 16);
+        __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p) + i);
+      }
+    } else {
+      store(p);
+    }
+  }
 };
 
 constexpr int kEmbedPieces = 4;  // a lane has under way
@@ -70,6 +104,47 @@ __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int
   }
 }
 
+// ---- rows of zeros --------------------------------------------------------------------------------
+// Rows of a table that no token names, in bytes (zero is all bits zero in every type).  They are most of what a gradient has to
+// write, so the launches that sort, which fill a few compute units, write them beside it: blocks from a launch's own on call
+// zero_rows.  Which rows are named says a byte each (`marks`), or, once they are sorted, the keys.
+struct ZeroRows {
+  uint8_t* at;  // NULL: none
+  int64_t pitch;
+  int32_t bytes, lg;  // of a row; lanes a row, as a power of two
+  int64_t begin, end;  // the rows of this launch
+  const uint8_t* marks;
+  const uint32_t* key;  // where marks is NULL: `count` sorted keys
+  int64_t count;
+};
+
+__device__ __forceinline__ bool row_named(const ZeroRows& z, int64_t r) {
+  if (z.marks) return z.marks[r] != 0;
+  int64_t a = 0, b = z.count;
+  while (a < b) {
+    const int64_t m = (a + b) >> 1;
+    if (z.key[m] < r) a = m + 1; else b = m;
+  }
+  return a < z.count && z.key[a] == r;
+}
+
+__device__ __forceinline__ void zero_rows(const ZeroRows& z, int64_t wave, int64_t waves) {
+  const int lane = threadIdx.x & 63, sub = lane >> z.lg, at = lane & ((1 << z.lg) - 1), per = 64 >> z.lg;
+  for (int64_t r0 = z.begin + wave * per; r0 < z.end; r0 += waves * per) {
+    const int64_t r = r0 + sub;
+    if (r >= z.end || row_named(z, r)) continue;
+    uint8_t* row = z.at + r * z.pitch;
+    const int lead = (int)(-reinterpret_cast<uintptr_t>(row) & 15), head = lead < z.bytes ? lead : z.bytes;
+    const int pieces = (z.bytes - head) / 16, tail = head + pieces * 16;
+    for (int j = at * 2; j < head; j += 2 << z.lg) *reinterpret_cast<uint16_t*>(row + j) = 0;
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words* p = reinterpret_cast<words*>(row + head);
+#pragma unroll 4
+    for (int j = at; j < pieces; j += 1 << z.lg) __builtin_nontemporal_store((words)(0), p + j);
+    for (int j = tail + at * 2; j < z.bytes; j += 2 << z.lg) *reinterpret_cast<uint16_t*>(row + j) = 0;
+  }
+}
+
 // ---- places sorted by token ----------------------------------------------------------------------
 // One pass of a radix sort takes `bits` bits of the keys, from `shift` on: how often each tile has each digit, then every key
 // to its place.  A tile is a run of tokens of one block, `per` of them; keys of the first pass are the tokens themselves, places
@@ -82,6 +157,8 @@ struct SortKeys {
   const uint32_t *key, *pos;
   uint32_t vocab;
   int first;
+  uint32_t* heavy_count;  // the first pass's first thread makes it zero
+  uint8_t* marks;  // NULL, or where the first pass marks the rows that are named
   __device__ __forceinline__ void get(int64_t i, uint32_t& k, uint32_t& p) const {
     if (first) {
       const int64_t t = tokens[i];
@@ -94,21 +171,20 @@ struct SortKeys {
   }
 };
 
-__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortKeys in, int64_t count, int64_t per, int shift, int bits,
-                                                             uint32_t* __restrict__ counts, int* __restrict__ error) {
-  __shared__ uint32_t hist[kSortDigits];
-  const uint32_t mask = (1u << bits) - 1;
-  for (int d = threadIdx.x; d <= (int)mask; d += kSortThreads) hist[d] = 0;
-  __syncthreads();
-  const int64_t lo = (int64_t)blockIdx.x * per, hi = lo + per < count ? lo + per : count;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
-    uint32_t k, p;
-    in.get(i, k, p);
-    if (in.first && in.tokens[i] >= (int64_t)in.vocab) *error = 1;
-    atomicAdd(&hist[(k >> shift) & mask], 1u);  // (whole numbers: the order does not matter)
+// Lanes of a wave see what the others wrote to LDS before.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The lanes among `live` that have the same digit.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool live) {
+  uint64_t same = __ballot(live);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t one = __ballot((d >> b) & 1);
+    same &= (d >> b) & 1 ? one : ~one;
   }
-  __syncthreads();
-  for (int d = threadIdx.x; d <= (int)mask; d += kSortThreads) counts[(size_t)blockIdx.x * (mask + 1) + d] = hist[d];
+  return same;
 }
 
 // Sums over the block of the values before each thread's own; `room` holds one value a wave.
@@ -123,241 +199,380 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* room) {
   if (lane == 63) room[wave] = s;
   __syncthreads();
   uint32_t before = 0;
-  for (int w = 0; w < wave; ++w) before += room[w];
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) before += w < wave ? room[w] : 0;
   return before + s - v;
 }
 
-// Lanes of a wave see what the others wrote to LDS before.
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortKeys in, int64_t count, int64_t per, int shift, int bits, int tiles,
+                                                             uint32_t* __restrict__ counts, int* __restrict__ error, ZeroRows zero) {
+  __shared__ uint32_t hist[kSortDigits];
+  if ((int)blockIdx.x >= tiles) {
+    zero_rows(zero, (int64_t)(blockIdx.x - tiles) * kSortWaves + (threadIdx.x >> 6), (int64_t)(gridDim.x - tiles) * kSortWaves);
+    return;
+  }
+  const uint32_t mask = (1u << bits) - 1;
+  if (in.first && blockIdx.x == 0 && threadIdx.x == 0) *in.heavy_count = 0;
+  for (int d = threadIdx.x; d <= (int)mask; d += kSortThreads) hist[d] = 0;
+  __syncthreads();
+  const int64_t lo = (int64_t)blockIdx.x * per, hi = lo + per < count ? lo + per : count;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
+    uint32_t k, p;
+    in.get(i, k, p);
+    if (in.first) {
+      if (k < in.vocab) {
+        if (in.marks) in.marks[k] = 1;
+      } else if (in.tokens[i] >= 0) {
+        *error = 1;
+      }
+    }
+    atomicAdd(&hist[(k >> shift) & mask], 1u);  // (whole numbers: the order does not matter)
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d <= (int)mask; d += kSortThreads) counts[(size_t)blockIdx.x * (mask + 1) + d] = hist[d];
 }
 
+// R keys a thread in a round.
+template <int R>
 __global__ __launch_bounds__(kSortThreads) void k_sort_place(SortKeys in, int64_t count, int64_t per, int shift, int bits,
                                                              const uint32_t* __restrict__ counts, int tiles,
-                                                             uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out) {
-  __shared__ uint32_t base[kSortDigits];              // where the tile's next key of each digit goes
-  __shared__ uint16_t seen[kSortWaves][kSortDigits];  // keys of each digit that a wave has in this round
+                                                             uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out,
+                                                             ZeroRows zero) {
+  __shared__ uint32_t base[kSortDigits];           // where the tile's next key of each digit goes
+  __shared__ uint16_t seen[kSortWaves * kSortDigits];  // keys of each digit that a wave has in this round
   __shared__ uint32_t room[kSortWaves];
+  if ((int)blockIdx.x >= tiles) {
+    zero_rows(zero, (int64_t)(blockIdx.x - tiles) * kSortWaves + (threadIdx.x >> 6), (int64_t)(gridDim.x - tiles) * kSortWaves);
+    return;
+  }
   const int digits = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t mask = digits - 1;
+  uint16_t* mine = seen + wave * digits;
   {
     // two digits a thread, side by side, so that the sum over threads runs over the digits in order
     const int d = threadIdx.x * 2;
     uint32_t all[2] = {0, 0}, before[2] = {0, 0};
-    for (int t = 0; t < tiles; ++t)
+    if (d < digits) {
+#pragma unroll 8
+      for (int t = 0; t < tiles; ++t)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t n = d + j < digits ? counts[(size_t)t * digits + d + j] : 0;
-        all[j] += n;
-        if (t < (int)blockIdx.x) before[j] += n;
-      }
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t n = counts[(size_t)t * digits + (d + j < digits ? d + j : d)];
+          all[j] += n;
+          before[j] += t < (int)blockIdx.x ? n : 0;
+        }
+      if (digits == 1) all[1] = 0;
+    }
     const uint32_t lower = block_before(all[0] + all[1], room);
     if (d < digits) base[d] = lower + before[0];
     if (d + 1 < digits) base[d + 1] = lower + all[0] + before[1];
   }
   const int64_t lo = (int64_t)blockIdx.x * per, hi = lo + per < count ? lo + per : count;
-  // A round: each wave has four times 64 keys side by side, in order.
-  for (int64_t at = lo; at < hi; at += kSortThreads * 4) {
-    for (int d = threadIdx.x; d < kSortWaves * kSortDigits / 2; d += kSortThreads)
-      if ((d * 2) % kSortDigits < digits) reinterpret_cast<uint32_t*>(seen)[d] = 0;
-    __syncthreads();
-    uint32_t key[4], pos[4], rank[4];
+  // A round: each wave has R times 64 keys side by side, in order.
+  for (int64_t at = lo; at < hi; at += kSortThreads * R) {
+    for (int d = threadIdx.x; d < kSortWaves * digits / 2; d += kSortThreads) reinterpret_cast<uint32_t*>(seen)[d] = 0;
+    uint32_t key[R], pos[R], rank[R];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t i = at + wave * 256 + r * 64 + lane;
-      const bool live = i < hi;
-      in.get(live ? i : hi - 1, key[r], pos[r]);
+    for (int r = 0; r < R; ++r) {
+      const int64_t i = at + wave * (64 * R) + r * 64 + lane;
+      in.get(i < hi ? i : hi - 1, key[r], pos[r]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool live = at + wave * (64 * R) + r * 64 + lane < hi;
       const uint32_t d = (key[r] >> shift) & mask;
-      // lanes with the same digit
-      uint64_t same = __ballot(live);
-      for (int b = 0; b < bits; ++b) {
-        const uint64_t one = __ballot((d >> b) & 1);
-        same &= (d >> b) & 1 ? one : ~one;
-      }
-      const uint32_t mine = __popcll(same & ((1ull << lane) - 1));
-      if (live) rank[r] = seen[wave][d] + mine;
+      const uint64_t same = same_digit(d, bits, live);
+      const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+      if (live) rank[r] = mine[d] + before;
       wave_fence();
-      if (live && mine == 0) seen[wave][d] += (uint16_t)__popcll(same);
+      if (live && before == 0) mine[d] += (uint16_t)__popcll(same);
       wave_fence();
     }
     __syncthreads();
     // where each wave's keys of a digit begin
     for (int d = threadIdx.x; d < digits; d += kSortThreads) {
       uint32_t next = 0;
+#pragma unroll
       for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t n = seen[w][d];
-        seen[w][d] = (uint16_t)next;
+        const uint32_t n = seen[w * digits + d];
+        seen[w * digits + d] = (uint16_t)next;
         next += n;
       }
-      seen[0][d] = (uint16_t)next;  // (wave 0 begins at 0 anyway: in its place how far base moves on behind this round)
+      seen[d] = (uint16_t)next;  // (wave 0 begins at 0 anyway: in its place how far base moves on behind this round)
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t i = at + wave * 256 + r * 64 + lane;
-      if (i < hi) {
+    for (int r = 0; r < R; ++r) {
+      if (at + wave * (64 * R) + r * 64 + lane < hi) {
         const uint32_t d = (key[r] >> shift) & mask;
-        const uint32_t to = base[d] + (wave ? seen[wave][d] : 0) + rank[r];
+        const uint32_t to = base[d] + (wave ? mine[d] : 0) + rank[r];
         key_out[to] = key[r];
         pos_out[to] = pos[r];
       }
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) base[d] += seen[0][d];
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) base[d] += seen[d];
     __syncthreads();
+  }
+}
+
+// Few tokens: each one's place is the number of smaller keys and of equal ones before it.  A block has B tokens, and 1024 / B
+// threads for each, which compare it with as many shares of all keys, read from LDS (4099 tokens 8.4 us; two passes over their
+// digits by one block 19, by several in four launches 20).
+template <int B>
+__global__ __launch_bounds__(kSortThreads) void k_sort_few(SortKeys in, int count, uint32_t* __restrict__ key_out,
+                                                           uint32_t* __restrict__ pos_out, int* __restrict__ error) {
+  constexpr int kParts = kSortThreads / B;
+  extern __shared__ uint4 keys4[];  // count keys, filled up with the largest number to a multiple of 4 kParts
+  __shared__ uint32_t below[kParts][B];
+  uint32_t* keys = reinterpret_cast<uint32_t*>(keys4);
+  const int each = (count + 4 * kParts - 1) / (4 * kParts) * 4;  // of a share
+  if (blockIdx.x == 0 && threadIdx.x == 0) *in.heavy_count = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < each * kParts; i += kSortThreads) {
+    uint32_t k, p;
+    in.get(i < count ? i : count - 1, k, p);
+    keys[i] = i < count ? k : 0xffffffffu;
+  }
+  __syncthreads();
+  const int t = threadIdx.x % B, part = threadIdx.x / B, i = blockIdx.x * B + t;
+  const uint32_t mine = keys[i < count ? i : count - 1];
+  // keys before the block's tokens count up to equality, those behind only below it; beside them places decide
+  const int first = blockIdx.x * B, lo = part * each, hi = lo + each;
+  const int mid = first < lo ? lo : first < hi ? first : hi, end = first + B < lo ? lo : first + B < hi ? first + B : hi;
+  uint32_t n = 0;
+  auto all = [&](int from, int to, uint32_t limit) {
+#pragma unroll 4
+    for (int j = from; j < to; j += 4) {
+      const uint4 k = keys4[j >> 2];
+      n += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
+    }
+  };
+  all(lo, mid, mine + 1);  // (keys are below 2^31)
+  for (int j = mid; j < end; ++j) n += keys[j] < mine || (keys[j] == mine && j < i);
+  all(end, hi, mine);
+  below[part][t] = n;
+  __syncthreads();
+  if (threadIdx.x < B && i < count) {
+    uint32_t to = 0;
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) to += below[q][t];
+    key_out[to] = mine;
+    pos_out[to] = i;
+    if (mine >= in.vocab && in.tokens[i] >= 0) *error = 1;
   }
 }
 
 // ---- sums over the sorted places -------------------------------------------------------------------
-// A wave takes kSumRun places side by side, and 64 V columns of their rows.  A token whose places all lie in the run is summed
-// and written by it.  Of one that reaches beyond, the run's share goes to part[run][0] (it began before the run) or
-// part[run][1] (it begins in it), float32, and k_embed_join adds the shares up, run by run.
-constexpr int kSumRun = 32, kSumAhead = 8;
+// A block takes the tokens that begin in its run of kSumRun sorted places.  One of at most kSumMost places is summed there and
+// written; a heavier one is summed run by run, and k_embed_join adds the runs' shares up: part[run][1] of the run that it begins in
+// (its places in that run), part[run][0] of the others, float32; its first run is put on the list `heavy` (whose order does not
+// matter).  Waves take a token and 64 V columns at a time; `split` blocks share a run.  `zero_blocks` more
+// write zeros, spread among the others, so that both kinds are under way at any time.
+constexpr int kSumRun = 32, kSumMost = 32, kSumWaves = 8;
+
+// What run `lo / kSumRun` has to do, the same in every lane.
+struct RunItems {
+  uint32_t starts;  // bit e: a token begins at place lo + e
+  int live;         // places of the run that hold a token
+  bool heavy;       // the run begins inside a heavy token
+};
+
+__device__ __forceinline__ RunItems run_items(const uint32_t* key, int64_t count, uint32_t vocab, int64_t lo, uint32_t& my_key) {
+  const int lane = threadIdx.x & 63;
+  // (a lane beyond the run has the places after it)
+  my_key = lo + lane < count ? key[lo + lane] : 0xffffffffu;
+  const uint32_t prev = lo + lane > 0 && lo + lane - 1 < count ? key[lo + lane - 1] : 0xffffffffu;
+  const uint32_t back = lo - 1 - lane >= 0 ? key[lo - 1 - lane] : 0xffffffffu;
+  RunItems it;
+  const uint64_t live = __ballot(lane < kSumRun && my_key < vocab);
+  it.live = __popcll(live);
+  it.starts = (uint32_t)__ballot(lane < kSumRun && my_key < vocab && my_key != prev);
+  const uint32_t first = __builtin_amdgcn_readfirstlane(my_key);
+  // places of the first token from here on, and before, up to 64 each
+  const int on = __popcll(__ballot(my_key == first)), before = __popcll(__ballot(back == first));
+  it.heavy = it.live > 0 && !(it.starts & 1) && on + before > kSumMost;
+  return it;
+}
 
 // dtable's row `v`, columns from c on: scale times the sums, added or not.
 template <class TG, int V>
-__device__ __forceinline__ void put_sums(TG* row, int64_t c, int64_t cols, const float (&s)[V], float scale, bool add) {
+__device__ __forceinline__ void put_sums(TG* row, int64_t c, int64_t cols, const float (&s)[V], float scale, bool add,
+                                         const Some<TG, V>& old) {
   Some<TG, V> o;
-  if (c + V <= cols) {
-    if (add) o.load(row + c);
 #pragma unroll
-    for (int j = 0; j < V; ++j) o.e[j] = static_cast<TG>(add ? static_cast<float>(o.e[j]) + s[j] * scale : s[j] * scale);
+  for (int j = 0; j < V; ++j) o.e[j] = static_cast<TG>(add ? static_cast<float>(old.e[j]) + s[j] * scale : s[j] * scale);
+  if (c + V <= cols) {
     o.store(row + c);
-  } else {
+  } else {  // (o's elements are those of the row's last V columns)
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (c + j < cols) row[c + j] = static_cast<TG>(add ? static_cast<float>(row[c + j]) + s[j] * scale : s[j] * scale);
+      if (cols - V + j >= c) row[cols - V + j] = o.e[j];
   }
 }
 
-template <int V>
-__device__ __forceinline__ void put_part(float* row, int64_t c, int64_t cols, const float (&s)[V]) {
-  if (c + V <= cols) {
-    Some<float, V> o;
-#pragma unroll
-    for (int j = 0; j < V; ++j) o.e[j] = s[j];
-    o.store(row + c);
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (c + j < cols) row[c + j] = s[j];
-  }
-}
-
-template <class TD, class TG, int V>
-__global__ __launch_bounds__(256) void k_embed_sum(const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                                                   int64_t count, uint32_t vocab, const TD* __restrict__ dy, int64_t dy_stride,
-                                                   int64_t cols, float scale, TG* __restrict__ dtable, int64_t grad_stride,
-                                                   int add, float* __restrict__ part, int64_t units, int64_t tiles) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); unit < units; unit += (int64_t)gridDim.x * 4) {
-    const int64_t run = unit / tiles, c = (unit % tiles * 64 + lane) * V;
-    const int64_t from = c + V <= cols ? c : cols - V;  // behind the row's end its last elements, shifted into place below
-    const int64_t lo = run * kSumRun;
-    const int n = count - lo < kSumRun ? (int)(count - lo) : kSumRun;
-    const uint32_t my_key = key[lo + (lane < n ? lane : n - 1)], my_pos = pos[lo + (lane < n ? lane : n - 1)];
-    const uint32_t first = __builtin_amdgcn_readfirstlane(my_key);
-    if (first >= vocab) continue;  // (nothing but places without a token from here on)
-    const bool head = lo > 0 && key[lo - 1] == first;
-    const uint32_t last = __shfl(my_key, n - 1, 64);
-    const bool tail = lo + n < count && key[lo + n] == last;
-    float s[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) s[j] = 0.0f;
-    uint32_t now = first;
-    bool began = !head;  // whether the token being summed begins in this run
-    for (int e0 = 0; e0 < n; e0 += kSumAhead) {
-      Some<TD, V> in[kSumAhead];
-#pragma unroll
-      for (int e = 0; e < kSumAhead; ++e) {
-        const uint32_t p = __builtin_amdgcn_readlane(my_pos, e0 + e < n ? e0 + e : n - 1);
-        in[e].load(dy + (int64_t)p * dy_stride + from);
-      }
-#pragma unroll
-      for (int e = 0; e < kSumAhead; ++e) {
-        if (e0 + e >= n) break;
-        const uint32_t k = __builtin_amdgcn_readlane(my_key, e0 + e);
-        if (k != now) {
-          if (began)
-            put_sums<TG, V>(dtable + (int64_t)now * grad_stride, c, cols, s, scale, add);
-          else
-            put_part<V>(part + (run * 2) * cols, c, cols, s);
-          began = true;
-          now = k;
-#pragma unroll
-          for (int j = 0; j < V; ++j) s[j] = 0.0f;
-          if (k >= vocab) break;
-        }
-        if (c + V <= cols) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) s[j] += static_cast<float>(in[e].e[j]);
-        } else {
-          // (the loaded piece begins at `from`: element j of ours is element c - from + j of it)
-#pragma unroll
-          for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int q = 0; q < V; ++q)
-              if (c + j < cols && c - from + j == q) s[j] += static_cast<float>(in[e].e[q]);
-        }
-      }
-      if (now >= vocab) break;
+template <class TD, class TG, int V, bool ONCE>  // ONCE: rows of dy lie at 16-byte boundaries and go past the caches
+__global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
+                                                              int64_t count, uint32_t vocab, const TD* __restrict__ dy,
+                                                              int64_t dy_stride, int64_t cols, float scale, TG* __restrict__ dtable,
+                                                              int64_t grad_stride, int add, float* __restrict__ part, int64_t runs,
+                                                              int split, int tiles, uint32_t* __restrict__ heavy,
+                                                              uint32_t* __restrict__ heavy_count, int zero_blocks,
+                                                              ZeroRows zero) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int mine = blockIdx.x;
+  if (zero_blocks > 0) {
+    // zero_blocks of all blocks, evenly: those where the share of the blocks up to here passes a whole number
+    const int turn = (int)((uint64_t)blockIdx.x * zero_blocks / gridDim.x);
+    if ((int)((uint64_t)(blockIdx.x + 1) * zero_blocks / gridDim.x) > turn) {
+      zero_rows(zero, (int64_t)turn * kSumWaves + wave, (int64_t)zero_blocks * kSumWaves);
+      return;
     }
-    if (now >= vocab) continue;
-    if (!began)
-      put_part<V>(part + (run * 2) * cols, c, cols, s);
-    else if (tail)
-      put_part<V>(part + (run * 2 + 1) * cols, c, cols, s);
-    else
-      put_sums<TG, V>(dtable + (int64_t)now * grad_stride, c, cols, s, scale, add);
+    mine -= turn;
+  }
+  const int share = mine % split;
+  const int64_t step = (gridDim.x - zero_blocks) / split;
+  for (int64_t run = mine / split; run < runs; run += step) {
+    const int64_t lo = run * kSumRun;
+    uint32_t my_key;
+    const RunItems it = run_items(key, count, vocab, lo, my_key);
+    if (it.live == 0) return;  // (nor have the runs behind it)
+    // the run's places, and those behind that its last token may have (it begins at most 31 places on and has at most 32)
+    const uint32_t my_pos = pos[lo + lane < count ? lo + lane : count - 1];
+    const int items = __popc(it.starts) + it.heavy;
+    for (int w = share * kSumWaves + wave; w < items * tiles; w += kSumWaves * split) {
+      const int item = w / tiles, tile = w % tiles;
+      int e0, e1;         // places lo + e0 .. lo + e1 - 1
+      int slot = -1;      // of part, or the table itself
+      if (it.heavy && item == 0) {
+        e0 = 0;
+        e1 = it.starts ? __ffs(it.starts) - 1 : it.live;
+        slot = 0;
+      } else {
+        uint32_t m = it.starts;
+        for (int j = it.heavy; j < item; ++j) m &= m - 1;
+        e0 = __ffs(m) - 1;
+        m &= m - 1;
+        if (m) {
+          e1 = __ffs(m) - 1;
+        } else {
+          // the run's last token: how far it goes on
+          const uint32_t k = __builtin_amdgcn_readlane(my_key, e0);
+          const int n = __popcll(__ballot(my_key == k));
+          e1 = e0 + n;
+          if (n > kSumMost) {
+            e1 = it.live;
+            slot = 1;
+            if (tile == 0 && lane == 0) heavy[atomicAdd(heavy_count, 1u)] = (uint32_t)run;
+          }
+        }
+      }
+      const uint32_t tok = __builtin_amdgcn_readlane(my_key, e0);
+      const int64_t c = ((int64_t)tile * 64 + lane) * V;
+      const int64_t from = c + V <= cols ? c : cols - V;  // (behind the row's end its last elements)
+      TG* row = dtable + (int64_t)tok * grad_stride;
+      Some<TG, V> old;
+      if (add && slot < 0) old.load(row + from);
+      float s[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] = 0.0f;
+      // as many rows under way at a time as there are, up to sixteen
+      int e = e0;
+      auto rows = [&](auto N, bool all) {
+        Some<TD, V> in[N()];
+#pragma unroll
+        for (int i = 0; i < N(); ++i) {
+          const uint32_t p = __builtin_amdgcn_readlane(my_pos, all || e + i < e1 ? e + i : e1 - 1);
+          const TD* at = dy + (int64_t)p * dy_stride + from;
+          if (ONCE) in[i].load_once(at); else in[i].load(at);
+        }
+#pragma unroll
+        for (int i = 0; i < N(); ++i)
+          if (all || e + i < e1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] += static_cast<float>(in[i].e[j]);
+          }
+        e += N();
+      };
+      while (e1 - e >= 16) rows(std::integral_constant<int, 16>(), true);
+      if (e1 - e > 4) rows(std::integral_constant<int, 8>(), false);
+      if (e1 - e > 2) rows(std::integral_constant<int, 4>(), false);
+      if (e1 - e > 1) rows(std::integral_constant<int, 2>(), true);
+      if (e1 - e > 0) rows(std::integral_constant<int, 1>(), true);
+      if (c < cols && slot < 0) {
+        put_sums<TG, V>(row, c, cols, s, scale, add, old);
+      } else if (c < cols) {
+        float* to = part + (run * 2 + slot) * cols;
+        Some<float, V> one;
+#pragma unroll
+        for (int j = 0; j < V; ++j) one.e[j] = s[j];
+        put_sums<float, V>(to, c, cols, s, 1.0f, false, one);
+      }
+    }
   }
 }
 
-// Tokens that reach over several runs, each by the block of the run that it begins in: blockIdx.x the run, blockIdx.y 64
-// columns, sixteen waves that take every sixteenth share.
+// Heavy tokens from their list: blockIdx.y 256 columns, sixteen waves that take every sixteenth share.  Clears the marks, too.
 template <class TG>
 __global__ __launch_bounds__(1024) void k_embed_join(const uint32_t* __restrict__ key, int64_t count, uint32_t vocab,
                                                      const float* __restrict__ part, int64_t cols, float scale,
-                                                     TG* __restrict__ dtable, int64_t grad_stride, int add, int64_t runs) {
-  __shared__ float room[16][64];
+                                                     TG* __restrict__ dtable, int64_t grad_stride, int add,
+                                                     const uint32_t* __restrict__ heavy, const uint32_t* __restrict__ heavy_count,
+                                                     uint8_t* __restrict__ marks) {
+  __shared__ float room[16][256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t run = blockIdx.x; run < runs; run += gridDim.x) {
-    const int64_t end = (run + 1) * kSumRun;
-    if (end >= count) return;
-    const uint32_t k = key[end - 1];
-    if (k >= vocab) return;
-    if (key[end] != k) continue;
-    if (key[run * kSumRun] == k && run > 0 && key[run * kSumRun - 1] == k) continue;  // it began before
-    // the first place behind `end` with another token
-    int64_t a = end, b = count;
+  if (marks && blockIdx.y == 0)
+    for (int64_t v = (int64_t)blockIdx.x * 1024 + threadIdx.x; v < vocab; v += (int64_t)gridDim.x * 1024) marks[v] = 0;
+  const uint32_t n = *heavy_count;
+  for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int64_t run = heavy[i], at = (run + 1) * kSumRun;
+    const uint32_t k = key[at - 1];
+    // the first place with another token: a wave looks at 64 places at a time, ever closer ones
+    int64_t a = at, b = count;
     while (a < b) {
-      const int64_t m = (a + b) >> 1;
-      if (key[m] == k) a = m + 1; else b = m;
+      const int64_t apart = (b - a + 63) / 64, look = a + lane * apart;
+      const int same = __popcll(__ballot(look < b && key[look < b ? look : a] == k));
+      if (same == 0) break;
+      b = a + same * apart < b ? a + same * apart : b;
+      a += (same - 1) * apart + 1;
     }
     const int64_t stop = (a + kSumRun - 1) / kSumRun;  // runs run + 1 .. stop - 1 hold shares
-    const int64_t c = (int64_t)blockIdx.y * 64 + lane;
-    float s = 0.0f;
+    const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < cols) {
-      if (wave == 0) s = part[(run * 2 + 1) * cols + c];
-#pragma unroll 8
-      for (int64_t r = run + 1 + wave; r < stop; r += 16) s += part[(r * 2) * cols + c];
+      if (wave == 0)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + j < cols) s[j] = part[(run * 2 + 1) * cols + c + j];
+      if (c + 4 <= cols) {
+#pragma unroll 4
+        for (int64_t r = run + 1 + wave; r < stop; r += 16) {
+          Some<float, 4> v;
+          v.load(part + (r * 2) * cols + c);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j] += v.e[j];
+        }
+      } else {
+        for (int64_t r = run + 1 + wave; r < stop; r += 16)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (c + j < cols) s[j] += part[(r * 2) * cols + c + j];
+      }
     }
-    room[wave][lane] = s;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) room[wave][lane * 4 + j] = s[j];
     __syncthreads();
-    if (wave == 0 && c < cols) {
-      for (int w = 1; w < 16; ++w) s += room[w][lane];
-      const float one[1] = {s};
-      put_sums<TG, 1>(dtable + (int64_t)k * grad_stride, c, cols, one, scale, add);
+    const int64_t mine_c = (int64_t)blockIdx.y * 256 + threadIdx.x;
+    if (threadIdx.x < 256 && mine_c < cols) {
+      float t = room[0][threadIdx.x];
+#pragma unroll
+      for (int w = 1; w < 16; ++w) t += room[w][threadIdx.x];
+      TG* to = dtable + (int64_t)k * grad_stride + mine_c;
+      *to = static_cast<TG>(add ? static_cast<float>(*to) + t * scale : t * scale);
     }
     __syncthreads();
   }
-}
-
-// Rows of zeros.
-template <class TG>
-__global__ __launch_bounds__(256) void k_embed_zero(TG* __restrict__ dtable, int64_t grad_stride, int64_t rows, int64_t cols) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int64_t c = threadIdx.x; c < cols; c += 256) dtable[r * grad_stride + c] = static_cast<TG>(0.0f);
 }
 
 }  // namespace artopk

@@ -18,9 +18,11 @@ struct artopk_tokens {
   int64_t max_tokens = 0, max_vocab = 0, max_width = 0;
   uint8_t* slab = nullptr;
   // within the slab: sorted tokens and their places (two of each, one pass reads what the other wrote), how often tiles have
-  // digits, shares of tokens' sums, the error word
+  // digits, shares of heavy tokens' sums, the error word
   uint32_t *key[2] = {nullptr, nullptr}, *pos[2] = {nullptr, nullptr}, *counts = nullptr;
   float* part = nullptr;
+  uint8_t* marks = nullptr;  // rows of a table that are named; zeros between calls
+  uint32_t *heavy = nullptr, *heavy_count = nullptr;  // runs in which heavy tokens begin
   int* error = nullptr;
   char err[kErrText] = {0};
 };
@@ -38,6 +40,8 @@ constexpr int64_t kMostBlocks = 1 << 20;
                        __LINE__);                                                                              \
   } while (0)
 
+constexpr int64_t kFewTokens = 8192, kFewTokensAlone = 14336;  // (at most what LDS holds beside the counts, 14336 keys)
+
 bool valid_limits(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
   return max_tokens >= 1 && max_tokens < (1ll << 31) && max_vocab >= 1 && max_vocab < (1ll << 31) && max_width >= 1 &&
          max_width <= kMostWidth;
@@ -46,8 +50,8 @@ bool valid_limits(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
 int64_t runs_of(int64_t count) { return (count + kSumRun - 1) / kSumRun; }
 
 struct Layout {
-  size_t key[2], pos[2], counts, part, error, bytes;
-  Layout(int64_t tokens, int64_t width) {
+  size_t key[2], pos[2], counts, part, marks, heavy, error, bytes;
+  Layout(int64_t tokens, int64_t vocab, int64_t width) {
     size_t at = 0;
     auto take = [&](size_t n) {
       const size_t here = at;
@@ -59,8 +63,10 @@ struct Layout {
       pos[i] = take((size_t)tokens * 4);
     }
     counts = take((size_t)kSortTiles * kSortDigits * 4);
-    part = take((size_t)runs_of(tokens) * 2 * (size_t)width * 4);
-    error = take(4);
+    part = tokens > kSumMost ? take((size_t)runs_of(tokens) * 2 * (size_t)width * 4) : 0;
+    marks = tokens > kFewTokens ? take((size_t)vocab) : 0;
+    heavy = take((size_t)(tokens / kSumMost + 1) * 4);
+    error = take(8);  // and the list's length
     bytes = at;
   }
 };
@@ -97,41 +103,89 @@ void embed(artopk_tokens* h, const TT* table, int64_t table_stride, int64_t voca
                                                     tiles, h->error);
 }
 
-// Sorts the places of `count` tokens by token; the result is in key[r], pos[r], r returned.
-int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t vocab) {
+// Bytes of zeros that a launch of the sort writes beside its own work: as much as takes no longer than that does.
+constexpr int64_t kBesideCount = 32 << 20, kBesidePlace = 80 << 20;
+constexpr int64_t kZeroShare = 64 << 10;  // and a block of the sums' launch
+constexpr int64_t kSumBlocks = 4096;      // of it, to be reached where columns can be shared
+constexpr int kZeroBlocks = 448;  // with the sort's own two on a compute unit
+
+// Sorts the places of `count` tokens by token; the result is in key[r], pos[r], r returned.  `zero` are the table's rows that
+// have to be zeros, of which some are written on the way; those left are in it afterwards.
+int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t vocab, ZeroRows& zero) {
+  // (with zeros to write beside them the passes cost nothing more)
+  if (count <= (zero.at ? kFewTokens : kFewTokensAlone)) {
+    const SortKeys in = {tokens, nullptr, nullptr, (uint32_t)vocab, 1, h->heavy_count, nullptr};
+    auto go = [&](auto B) {
+      constexpr int kParts = kSortThreads / B();
+      const int each = (int)((count + 4 * kParts - 1) / (4 * kParts) * 4);
+      k_sort_few<B()><<<(unsigned)((count + B() - 1) / B()), kSortThreads, (size_t)each * kParts * 4, h->stream>>>(
+          in, (int)count, h->key[0], h->pos[0], h->error);
+    };
+    if (count <= kFewTokens) go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 64>());
+    zero.key = h->key[0];
+    zero.count = count;
+    return 0;
+  }
   int all = 1;
   while (vocab >> all) ++all;  // bits of 0 .. vocab, which stands for no token
   const int passes = (all + kSortBits - 1) / kSortBits;
-  const int64_t round = kSortThreads * 4;
+  const int keys = count <= 65536 ? 1 : 4;  // a thread has in a round
+  const int64_t round = kSortThreads * keys;
   const int64_t per = std::max<int64_t>(1, (count + round * kSortTiles - 1) / (round * kSortTiles)) * round;
   const int tiles = (int)((count + per - 1) / per);
+  zero.marks = zero.at ? h->marks : nullptr;
+  int64_t next = 0;
+  auto beside = [&](int64_t bytes) {
+    ZeroRows z = zero;
+    if (z.at) {
+      z.begin = next;
+      z.end = next = std::min(zero.end, next + std::max<int64_t>(1, bytes / z.bytes));
+    }
+    return z;
+  };
   int from = 1, shift = 0;
   for (int pass = 0; pass < passes; ++pass) {
     const int bits = (all - shift + passes - pass - 1) / (passes - pass);
-    const SortKeys in = {tokens, h->key[from], h->pos[from], (uint32_t)vocab, pass == 0};
-    k_sort_count<<<tiles, kSortThreads, 0, h->stream>>>(in, count, per, shift, bits, h->counts, h->error);
-    k_sort_place<<<tiles, kSortThreads, 0, h->stream>>>(in, count, per, shift, bits, h->counts, tiles, h->key[1 - from],
-                                                        h->pos[1 - from]);
+    const SortKeys in = {tokens, h->key[from], h->pos[from], (uint32_t)vocab, pass == 0, h->heavy_count, zero.at ? h->marks : nullptr};
+    // (the first launch finds out which rows are named)
+    const bool fill = zero.at && pass > 0;
+    k_sort_count<<<tiles + (fill ? kZeroBlocks : 0), kSortThreads, 0, h->stream>>>(in, count, per, shift, bits, tiles, h->counts,
+                                                                                  h->error, fill ? beside(kBesideCount) : zero);
+    auto go = [&](auto R) {
+      k_sort_place<R()><<<tiles + (zero.at ? kZeroBlocks : 0), kSortThreads, 0, h->stream>>>(
+          in, count, per, shift, bits, h->counts, tiles, h->key[1 - from], h->pos[1 - from], beside(kBesidePlace));
+    };
+    if (keys == 1) go(std::integral_constant<int, 1>());
+    else go(std::integral_constant<int, 4>());
     shift += bits;
     from = 1 - from;
   }
+  zero.begin = next;
   return from;
 }
 
-template <class TD, class TG, int V>
+template <class TD, class TG, int V, bool ONCE>
 void embed_sums(artopk_tokens* h, const uint32_t* key, const uint32_t* pos, int64_t count, int64_t vocab, const TD* dy,
-                int64_t dy_stride, int64_t cols, float scale, TG* dtable, int64_t grad_stride, int add) {
-  const int64_t tiles = (cols + 64 * V - 1) / (64 * V), units = runs_of(count) * tiles;
-  const unsigned blocks = (unsigned)std::min<int64_t>((units + 3) / 4, kMostBlocks);
-  k_embed_sum<TD, TG, V><<<blocks, 256, 0, h->stream>>>(key, pos, count, (uint32_t)vocab, dy, dy_stride, cols, scale, dtable,
-                                                        grad_stride, add, h->part, units, tiles);
+                int64_t dy_stride, int64_t cols, float scale, TG* dtable, int64_t grad_stride, int add, const ZeroRows& zero) {
+  const int tiles = (int)((cols + 64 * V - 1) / (64 * V));
+  const int64_t rows = zero.at ? std::max<int64_t>(0, zero.end - zero.begin) : 0;
+  const int zeros = (int)std::min<int64_t>((rows * zero.bytes + kZeroShare - 1) / kZeroShare, 16384);
+  const int64_t runs = runs_of(count);
+  // as many blocks to a run as its tokens and column tiles can occupy, until there are enough of them
+  const int most = (kSumRun / 4 * tiles + kSumWaves - 1) / kSumWaves;
+  const int split = (int)std::max<int64_t>(1, std::min<int64_t>(most, kSumBlocks / std::max<int64_t>(1, runs)));
+  const int64_t blocks = std::min<int64_t>(runs, kMostBlocks) * split;
+  k_embed_sum<TD, TG, V, ONCE><<<(unsigned)(blocks + zeros), kSumWaves * 64, 0, h->stream>>>(
+      key, pos, count, (uint32_t)vocab, dy, dy_stride, cols, scale, dtable, grad_stride, add, h->part, runs, split, tiles, h->heavy,
+      h->heavy_count, zeros, zero);
 }
 
 }  // namespace
 
 int64_t artopk_tokens_scratch_bytes(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
   if (!valid_limits(max_tokens, max_vocab, max_width)) return -1;
-  return (int64_t)Layout(max_tokens, max_width).bytes;
+  return (int64_t)Layout(max_tokens, max_vocab, max_width).bytes;
 }
 
 int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vocab, int64_t max_width, void* hip_stream) {
@@ -154,7 +208,7 @@ int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vo
     return fail_text(g_noctx_err, ARTOPK_EHIP, "no device: %s", hipGetErrorString(e));
   }
   if (cus > 0) h->num_cu = cus;
-  const Layout at(max_tokens, max_width);
+  const Layout at(max_tokens, max_vocab, max_width);
   void* p = nullptr;
   e = hipMalloc(&p, at.bytes);
   if (e != hipSuccess) {
@@ -169,13 +223,17 @@ int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vo
   }
   h->counts = reinterpret_cast<uint32_t*>(h->slab + at.counts);
   h->part = reinterpret_cast<float*>(h->slab + at.part);
+  h->marks = h->slab + at.marks;
+  h->heavy = reinterpret_cast<uint32_t*>(h->slab + at.heavy);
+  h->heavy_count = reinterpret_cast<uint32_t*>(h->slab + at.error) + 1;
   h->error = reinterpret_cast<int*>(h->slab + at.error);
-  const int zero = 0;
-  e = hipMemcpy(h->error, &zero, sizeof(zero), hipMemcpyHostToDevice);
+  e = hipMemset(h->error, 0, sizeof(int));
+  if (e == hipSuccess && max_tokens > kFewTokens) e = hipMemset(h->marks, 0, (size_t)max_vocab);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     (void)hipFree(h->slab);
     delete h;
-    return fail_text(g_noctx_err, ARTOPK_EHIP, "hipMemcpy failed: %s", hipGetErrorString(e));
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "hipMemset failed: %s", hipGetErrorString(e));
   }
   *out = h;
   return ARTOPK_OK;
@@ -259,28 +317,38 @@ int artopk_embedding_backward(artopk_tokens* h, const void* dy, int64_t dy_strid
     if ((rc = rs.check(h->err))) return rc;
   }
   const Tokens tok = {tokens, token_bits == 64};
+  ZeroRows zero = {};
+  if (!accumulate) {
+    zero.at = static_cast<uint8_t*>(dtable);
+    zero.pitch = grad_stride * (int64_t)elem_size(grad_type);
+    zero.bytes = (int32_t)(width * (int64_t)elem_size(grad_type));
+    zero.end = vocab;
+    while (zero.lg < 6 && (64 << zero.lg) < zero.bytes) ++zero.lg;
+  }
   int sorted = 0;
-  if (count > 0) sorted = sort_places(h, tok, count, vocab);
+  if (count > 0) sorted = sort_places(h, tok, count, vocab, zero);
   with_type(grad_type, [&](auto* tg) {
     using TG = std::remove_pointer_t<decltype(tg)>;
     TG* out = static_cast<TG*>(dtable);
-    if (!accumulate)
-      k_embed_zero<TG><<<(unsigned)std::min<int64_t>(vocab, kMostBlocks), 256, 0, h->stream>>>(out, grad_stride, vocab, width);
-    if (count == 0) return;
+    if (count == 0 && accumulate) return;
     with_type(type, [&](auto* td) {
       using TD = std::remove_pointer_t<decltype(td)>;
       constexpr int kWide = 16 / sizeof(TD);
-      auto go = [&](auto V) {
-        embed_sums<TD, TG, V()>(h, h->key[sorted], h->pos[sorted], count, vocab, static_cast<const TD*>(dy), dy_stride, width, scale,
-                                out, grad_stride, accumulate != 0);
+      auto go = [&](auto V, auto ONCE) {
+        embed_sums<TD, TG, V(), ONCE()>(h, h->key[sorted], h->pos[sorted], count, vocab, static_cast<const TD*>(dy), dy_stride, width,
+                                        scale, out, grad_stride, accumulate != 0, zero);
       };
-      if (width >= kWide) go(std::integral_constant<int, kWide>());
-      else go(std::integral_constant<int, 1>());
+      using Wide = std::integral_constant<int, kWide>;
+      if (width < kWide) go(std::integral_constant<int, 1>(), std::false_type());
+      else if (width % kWide == 0 && aligned16(dy) && dy_stride % kWide == 0) go(Wide(), std::true_type());
+      else go(Wide(), std::false_type());
     });
-    const int64_t runs = runs_of(count);
-    if (runs > 1)
-      k_embed_join<TG><<<dim3((unsigned)std::min<int64_t>(runs - 1, kMostBlocks), (unsigned)((width + 63) / 64)), 1024, 0, h->stream>>>(
-          h->key[sorted], count, (uint32_t)vocab, h->part, width, scale, out, grad_stride, accumulate != 0, runs);
+    if (count <= kSumMost) return;
+    const unsigned tiles = (unsigned)((width + 255) / 256);
+    const unsigned groups = (unsigned)std::max<int64_t>(1, std::min<int64_t>(count / kSumMost, 2 * h->num_cu / tiles));
+    k_embed_join<TG><<<dim3(groups, tiles), 1024, 0, h->stream>>>(h->key[sorted], count, (uint32_t)vocab, h->part, width, scale, out,
+                                                                  grad_stride, accumulate != 0, h->heavy, h->heavy_count,
+                                                                  zero.marks ? h->marks : nullptr);
   });
   TOKENS_TRY(h, hipGetLastError());
   return ARTOPK_OK;

@@ -2,8 +2,8 @@
 
 The lookup is one product in float32 and one rounding: the host's bits.  The gradient's sums are compared with 64 bits.  A sum
 of n float32 terms in any order with at most `depth` additions one after the other is off by at most depth u sum|terms|,
-u = 2^-24.  Here a run of 32 places is summed one by one (32), a token's runs by sixteen waves (runs / 16 + 1), then these
-(16); scaling and adding to what is there are one rounding each, and the output type's own comes last.
+u = 2^-24.  Here up to 32 places of a token are summed one by one; more go run by run of 32, a token's runs by sixteen waves
+(runs / 16 + 1), then these (16); scaling and adding to what is there are one rounding each, and the output type's own comes last.
 """
 
 import numpy as np
@@ -130,7 +130,8 @@ def _check_backward(count, vocab, width, grad, t, how, accumulate, pad=0, shift=
     assert torch.equal(again, mem)  # the same bits
 
 
-@pytest.mark.parametrize("count", [1, 2, 31, 32, 33, 63, 64, 65, 200, 1000, 4095, 4096, 4097, 9000])
+@pytest.mark.parametrize("count", [1, 2, 31, 32, 33, 63, 64, 65, 66, 95, 96, 97, 128, 200, 1000, 1024, 1025, 2049, 4095, 4096, 4097, 8192,
+                                   8193, 8194, 9000, 14336, 14338])
 @pytest.mark.parametrize("how", ["mixed", "one", "few"])
 def test_backward_counts(count, how):
     _check_backward(count, 50, 40, "f32", "f32", how, count % 2 == 0, wide=count % 3 != 0)
@@ -157,6 +158,29 @@ def test_backward_vocabularies(vocab):
 @pytest.mark.parametrize("how", ["mixed", "one", "few"])
 def test_backward_many_tokens(how):
     _check_backward(300_000, 70_000, 24, "f32", "bf16", how, True)
+
+
+@pytest.mark.parametrize("how", ["mixed", "few", "none"])
+@pytest.mark.parametrize("grad,width,pad,shift", [("f32", 801, 0, 1), ("bf16", 1024, 8, 0), ("f16", 515, 1, 3)])
+def test_backward_large_tables_overwritten(how, grad, width, pad, shift):
+    """Tables whose zeros are written by every launch of the sort and by the sums'."""
+    _check_backward(9000, 60_000, width, grad, "bf16", how, False, pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("vocab", [40, 70_000])
+def test_backward_calls_in_a_row(vocab):
+    """A handle's calls leave nothing behind: other tokens, counts and kinds of calls in between."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    ctx = lib.TokenContext(20_000, vocab, 20)
+    for i, count in enumerate((20_000, 9000, 100, 20_000, 0, 8193, 64, 12_000)):
+        tok = _tokens(count, vocab, i, "few" if i % 2 else "mixed").cuda()
+        dy = torch.ones(count, 20).cuda()
+        grad = torch.full((vocab, 20), 5.0).cuda()
+        ctx.artopk_embedding_backward(dy, tok, grad, accumulate=i % 3 == 2)
+        want = torch.bincount(tok[tok >= 0], minlength=vocab).float() + (5.0 if i % 3 == 2 else 0.0)
+        assert torch.equal(grad, want.view(-1, 1).expand(-1, 20)), i
 
 
 def test_backward_no_token_and_none_at_all():
