@@ -6,10 +6,14 @@
 //
 // Both are bound by memory: forward reads a row once, backward reads and writes it once.  Two numbers of a row are kept for the
 // backward pass, not lse alone: beside a large peak (a row that is masked with the type's lowest value) lse would hold nothing of
-// logsum.  Exponentials are powers of two of c (x - ..), c = scale log2(e).  A thread's largest element M stays out of its sum
-// R = sum over the others of 2^(c (x - M)): then log(1 + R) loses nothing where one token is nearly sure, as it would beside the
-// largest element's own 1.  Exponents are taken relative to a reference that lies at most 16 below M's (sums stay below 2^50) and
-// so rarely moves.
+// logsum.  Exponentials are powers of two of c (x - ..), c = scale log2(e).  The largest element stays out of the sum
+// r = sum over the others of 2^(c (x - peak)): then log(1 + r) loses nothing where one token is nearly sure, as it would beside
+// the largest element's own 1.
+//
+// Forward has to stay below some twelve instruction slots an element (64 lanes a cycle and compute unit, an exponential takes
+// four) to be bound by memory in 16-bit types.  A wave keeps one largest element for all its lanes: 32 elements a lane at a time are
+// added with nothing but their own maximum besides, and only where some lane has a larger one (once, then ever more rarely)
+// the sums move to it: 9.5 slots.
 #pragma once
 
 #include "embedding_kernels.h"
@@ -42,49 +46,99 @@ __device__ __forceinline__ RowSum join(const RowSum& a, const RowSum& b, float c
   return {hi.m, hi.r + more * f, hi.u + (lo.u - more * d) * f};
 }
 
-// A thread's share of a row, element by element.
+// The largest of N values; NaN counts for nothing.
+template <int N>
+__device__ __forceinline__ float largest(const float* x) {
+  float m = x[0];
+  if constexpr (N % 2 == 0) m = fmaxf(x[0], x[1]);
+#pragma unroll
+  for (int i = N % 2 == 0 ? 2 : 1; i < N; i += 2) m = fmaxf(fmaxf(x[i], x[i + 1]), m);
+  return m;
+}
+
+__device__ __forceinline__ float wave_largest(float v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_total(float v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// A wave's share of a row: m is the largest element so far, the same in all lanes, r and u a lane's sums over its other ones
+// with exponents c x - ref.  ref is c m rounded (the same for all, so it costs nothing but its distance from c m in the end), or
+// with c m near float32's end exponents are c (x - m).
 struct Gather {
-  float m = -INFINITY, r = 0.0f, u = 0.0f, ref = 0.0f, most = -INFINITY;
-  bool bad = false;
-  // V elements; with one of them NaN nothing but `bad` counts
-  template <int V>
-  __device__ __forceinline__ void add(float (&x)[V], float c) {
-    if constexpr (V == 1) {
-      bad |= x[0] != x[0];
-      const float lo = fminf(x[0], m);
-      m = fmaxf(x[0], m);
-      x[0] = lo;
+  float m = -INFINITY, ref = 0.0f, r = 0.0f, u = 0.0f;
+  bool far = false;
+  __device__ __forceinline__ float exponent(float x, float c) const { return far ? (x - m) * c : fmaf(x, c, -ref); }
+  // N elements a lane, `top` their largest; all lanes of the wave call it together
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N], float top, float c) {
+    if (__any(top > m)) {
+      move(x, top, c);
+    } else if (far) {
+      sum<N>(x, [&](float v) { return (v - m) * c; });
     } else {
-#pragma unroll
-      for (int i = 0; i < V; i += 2) {
-        bad |= __builtin_isunordered(x[i], x[i + 1]);
-        const float hi = fmaxf(fmaxf(x[i], x[i + 1]), m);
-        const float mid = __builtin_amdgcn_fmed3f(x[i], x[i + 1], m), lo = fminf(fminf(x[i], x[i + 1]), m);
-        m = hi;
-        x[i] = mid;
-        x[i + 1] = lo;
-      }
+      sum<N>(x, [&](float v) { return fmaf(v, c, -ref); });
     }
-    if (m > most) {  // the reference moves (the first time from nothing)
-      if (most > -INFINITY) {
-        const float d = fminf((m - ref) * c, 200.0f), f = pow2(-d);
-        u = (u - r * d) * f;
-        r *= f;
-      }
-      ref = m;
-      most = m + 16.0f / c;
+  }
+  template <int N, class F>
+  __device__ __forceinline__ void sum(const float (&x)[N], F&& f) {
+    constexpr int S = N % 4 == 0 ? 4 : 1;  // sums side by side
+    float a[S], b[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) a[i] = b[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float d = f(x[i]), e = pow2(d);  // (NaN stays NaN and ends up in r)
+      a[i % S] += e;
+      b[i % S] = fmaf(e, fmaxf(d, -200.0f), b[i % S]);
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float d = fmaxf((x[i] - ref) * c, -200.0f), e = pow2(d);
+    for (int i = 1; i < S; ++i) {
+      a[0] += a[i];
+      b[0] += b[i];
+    }
+    r += a[0];
+    u += b[0];
+  }
+  // the same where some lane has a larger element: the first lane that has the largest leaves it out, and adds the one before
+  template <int N>
+  __device__ __forceinline__ void move(const float (&x)[N], float top, float c) {
+    const float to = wave_largest(top), before = m, next = to * c;
+    const int owner = __ffsll((unsigned long long)__ballot(top == to)) - 1;
+    bool mine = (int)(threadIdx.x & 63) == owner;
+    const bool was_far = far;
+    far = !(fabsf(next) < 0x1p120f);
+    if (before > -INFINITY) {
+      const float d = fminf(far || was_far ? (to - before) * c : next - ref, 200.0f), f = pow2(-d);
+      u = (u - r * d) * f;
+      r *= f;
+    }
+    m = to;
+    ref = next;
+    if (mine && before > -INFINITY) {
+      const float d = fmaxf(exponent(before, c), -200.0f), e = pow2(d);
       r += e;
       u = fmaf(e, d, u);
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool out = mine && x[i] == to;
+      mine = mine && !out;
+      const float d = exponent(x[i], c), e = out ? 0.0f : pow2(d);
+      r += e;
+      u = fmaf(e, fmaxf(d, -200.0f), u);
+    }
   }
-  __device__ __forceinline__ RowSum sum(float c) const {
-    if (!(m > -INFINITY)) return {-INFINITY, 0.0f, 0.0f};
-    const float d = (m - ref) * c, f = pow2(-d);
-    return {m, r * f, (u - r * d) * f};
+  // over the wave
+  __device__ __forceinline__ RowSum total(float c) const {
+    if (!(m > -INFINITY)) return {m, wave_total(r), 0.0f};  // (r may be NaN)
+    const float d = far ? 0.0f : fmaf(m, c, -ref), f = pow2(-d);
+    return {m, wave_total(r * f), wave_total((u - r * d) * f)};
   }
 };
 
@@ -120,21 +174,6 @@ struct LogpOut {
   float* top_logp;
 };
 
-// Thread t of a block of 256 has pieces whole0 + t + 256 i; thread 255 the part in front, thread 254 the part behind.  `i` runs
-// to steps() - 1.
-template <class T>
-struct Share {
-  const RowPieces<T>& p;
-  __device__ __forceinline__ int steps() const { return (p.whole1 - p.whole0 + 255) / 256 + 2; }
-  __device__ __forceinline__ int piece(int t, int i) const {  // -1: none
-    const int n = steps();
-    if (i == n - 2) return t == 255 && p.whole0 > 0 ? 0 : -1;
-    if (i == n - 1) return t == 254 && p.count > p.whole1 ? p.count - 1 : -1;
-    const int j = p.whole0 + t + 256 * i;
-    return j < p.whole1 ? j : -1;
-  }
-};
-
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
@@ -144,144 +183,251 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
   return v;
 }
 
-// One row a block.
-template <class T, bool TOP>
+// What a row's outputs come from, once its sums are known.
+struct RowEnd {
+  RowSum s;
+  float scale, log;
+  bool broken, none;  // NaN or infinity in the row; nothing left in it
+  __device__ __forceinline__ RowEnd(const RowSum& sum, float by) : s(sum), scale(by) {
+    broken = s.r != s.r || s.m == INFINITY;
+    none = s.m == -INFINITY;
+    log = log1pf(s.r);
+  }
+  __device__ __forceinline__ float logp(float x) const {
+    return broken ? __builtin_nanf("") : none ? -INFINITY : (x - s.m) * scale - log;
+  }
+  __device__ __forceinline__ void put(const LogpOut& out, int64_t row, int64_t tok, int cols, float xt) const {
+    const float nan = __builtin_nanf("");
+    if (out.peak) out.peak[row] = broken ? nan : s.m;
+    if (out.logsum) out.logsum[row] = broken ? nan : log;
+    if (out.entropy) out.entropy[row] = broken ? nan : none ? 0.0f : log - s.u * kLn2 / (1.0f + s.r);
+    if (out.logp) out.logp[row] = tok >= cols ? nan : tok < 0 ? (broken ? nan : 0.0f) : logp(xt);
+  }
+  // one of the alternatives; its key is its value's order and the complement of its place
+  __device__ __forceinline__ void put_top(const LogpOut& out, int64_t at, uint64_t key) const {
+    out.top_ids[at] = broken ? -1 : (int32_t)~(uint32_t)key;
+    out.top_logp[at] = logp(from_ordered((uint32_t)(key >> 32)));
+  }
+};
+
+// A team of WAVES waves (1: four teams a block) has a row, or with `split` > 1 one of as many parts of it, whose sums and
+// alternatives then go to parts and part_keys for k_logp_join.  Thread t has the part's whole pieces t, t + 64 WAVES, ..; the last
+// thread but one has the row's last piece, the last one the first, where these are not whole.
+//
+// Alternatives.  Every thread notes its largest element (the first among equal ones).  The `top` largest of these are a bound:
+// the row's alternatives are not below the last of them, and all lie with the threads that have them.  So those threads' elements
+// are read once more, those that reach the bound listed, and a listed one's place is the number of larger ones.  Should there be
+// more than kListRoom (a row in order), the alternatives are found one after the other.
+struct LogpPart {
+  RowSum s;
+  float unused;
+};
+
+template <class T, int WAVES, bool TOP>
 __global__ __launch_bounds__(256) void k_logp(const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, Tokens tokens,
-                                              int has_tokens, float scale, float c, int top, LogpOut out, int* __restrict__ error) {
-  constexpr int V = RowPieces<T>::V;
+                                              int has_tokens, float scale, float c, int top, LogpOut out, int split,
+                                              LogpPart* __restrict__ parts, uint64_t* __restrict__ part_keys, int* __restrict__ error) {
+  constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES, kBatch = 32 / V, kRoom = kListRoom / kTeams;
   __shared__ RowSum sums[4];
-  __shared__ int bads[4];
-  __shared__ uint64_t keys[TOP ? 256 : 1], list[TOP ? kListRoom : 1], bound, best[4];
-  __shared__ int chosen[TOP ? kMostTop : 1], chosen_count, list_count;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+  __shared__ uint64_t keys[TOP ? 256 : 1], lists[TOP ? kListRoom : 1], bests[4], bounds[4];
+  __shared__ int chosens[TOP ? kTeams * kMostTop : 1], chosen_counts[4], list_counts[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int team = wave / WAVES, t = threadIdx.x % NT, team_wave = wave % WAVES;
+  auto meet = [] {
+    if constexpr (WAVES == 1) wave_fence(); else __syncthreads();
+  };
+  const int64_t units = rows * split;
+  for (int64_t unit = (int64_t)blockIdx.x * kTeams + team; unit < units; unit += (int64_t)gridDim.x * kTeams) {
+    const int64_t row = unit / split;
+    const int part = (int)(unit % split);
     const RowPieces<T> p(x + row * x_stride, cols);
-    const Share<T> share{p};
+    const int64_t whole = p.whole1 - p.whole0;
+    const int q0 = p.whole0 + (int)(whole * part / split), q1 = p.whole0 + (int)(whole * (part + 1) / split);
+    const bool front = part == 0 && p.whole0 > 0, behind = part == split - 1 && p.count > p.whole1;
     int64_t tok = -1;
     float xt = 0.0f;
-    if (t == 0 && has_tokens) {
+    if (t == 0 && part == 0 && has_tokens) {
       tok = tokens[row];
       if (tok >= cols) *error = 1;
       if (tok >= 0 && tok < cols) xt = static_cast<float>(p.row[tok]);
     }
     Gather g;
-    int where = -1;  // the first piece with the thread's largest element
-    auto piece = [&](float(&v)[V], int j) {
-      const float before = g.m;
-      g.add(v, c);
-      if (TOP && (g.m > before || where < 0)) where = j;
+    float own = -INFINITY;  // the thread's largest element, and the first piece that has it
+    int where = -1;
+    auto note = [&](float v, int j) {
+      if (TOP && (v > own || where < 0)) {
+        own = fmaxf(v, own);
+        where = j;
+      }
     };
-    if (t == 255 && p.whole0 > 0) {
+    auto lone = [&](int j, int thread) {  // a piece of which there is only a part
       float v[V];
-      p.load_part(v, 0, -INFINITY);
-      piece(v, 0);
-    }
-    for (int j = p.whole0 + t; j < p.whole1; j += 256) {
-      float v[V];
-      p.load_whole(v, j);
-      piece(v, j);
-    }
-    if (t == 254 && p.count > p.whole1) {
-      float v[V];
-      p.load_part(v, p.count - 1, -INFINITY);
-      piece(v, p.count - 1);
-    }
-    RowSum s = g.sum(c);
+      if (t == thread) {
+        p.load_part(v, j, -INFINITY);
+      } else {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) s = join(s, RowSum{__shfl_xor(s.m, off, 64), __shfl_xor(s.r, off, 64), __shfl_xor(s.u, off, 64)}, c);
-    const int bad = __any(g.bad);
-    if (lane == 0) {
-      sums[wave] = s;
-      bads[wave] = bad;
-    }
+        for (int i = 0; i < V; ++i) v[i] = -INFINITY;
+      }
+      const float most = largest<V>(v);
+      if (t == thread) note(most, j);
+      g.add<V>(v, most, c);
+    };
+    if (front && team_wave == WAVES - 1) lone(0, NT - 1);
+    auto batch = [&](int j, bool all) {
+      Vec16<T> raw[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int at = j + i * NT;
+        raw[i] = *reinterpret_cast<const Vec16<T>*>(p.row + ((int64_t)(all || at < q1 ? at : q1 - 1) * V - p.shift));
+      }
+      float v[kBatch * V], most[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[i * V + k] = all || j + i * NT < q1 ? static_cast<float>(raw[i].e[k]) : -INFINITY;
+        most[i] = largest<V>(v + i * V);
+        if (all || j + i * NT < q1) note(most[i], j + i * NT);
+      }
+      g.add<kBatch * V>(v, largest<kBatch>(most), c);
+    };
+    int j = q0 + t;
+    const int last = q1 - kBatch * NT;  // (the same for all lanes: full batches begin up to here)
+    int base = q0;
+    for (; base <= last; base += kBatch * NT, j += kBatch * NT) batch(j, true);
+    if (base + team_wave * 64 < q1) batch(j, false);
+    if (behind && team_wave == (NT - 2) / 64) lone(p.count - 1, NT - 2);
+    RowSum s = g.total(c);
     if (TOP) {
       // a thread's key: its largest element, the lower place first; 0 where it has none
-      keys[t] = where < 0 ? 0 : (uint64_t)ordered(g.m) << 32 | (uint32_t)~where;
+      keys[threadIdx.x] = where < 0 ? 0 : (uint64_t)ordered(own) << 32 | (uint32_t)~where;
       if (t == 0) {
-        bound = 0;
-        chosen_count = list_count = 0;
+        bounds[team] = 0;
+        chosen_counts[team] = list_counts[team] = 0;
       }
     }
-    __syncthreads();
-    s = join(join(sums[0], sums[1], c), join(sums[2], sums[3], c), c);
-    const bool broken = bads[0] | bads[1] | bads[2] | bads[3] || s.m == INFINITY;  // NaN or infinity in the row
-    const bool none = s.m == -INFINITY;
-    const float log = log1pf(s.r), nan = __builtin_nanf("");
+    if constexpr (WAVES > 1) {
+      if (lane == 0) sums[wave] = s;
+      meet();
+      s = join(join(sums[0], sums[1], c), join(sums[2], sums[3], c), c);
+    } else if (TOP) {
+      meet();
+    }
+    const RowEnd end(s, scale);
     if (t == 0) {
-      if (out.peak) out.peak[row] = broken ? nan : s.m;
-      if (out.logsum) out.logsum[row] = broken ? nan : log;
-      if (out.entropy) out.entropy[row] = broken ? nan : none ? 0.0f : log - s.u * kLn2 / (1.0f + s.r);
-      if (out.logp)
-        out.logp[row] = broken || tok >= cols ? nan : tok < 0 ? 0.0f : none ? -INFINITY : (xt - s.m) * scale - log;
+      if (split == 1) end.put(out, row, tok, cols, xt);
+      else parts[unit].s = s;
     }
-    if (TOP && broken) {
-      if (t < top) {
-        out.top_ids[row * top + t] = -1;
-        out.top_logp[row * top + t] = nan;
-      }
-    } else if constexpr (TOP) {
+    if constexpr (TOP) {
       auto put = [&](int at, uint64_t key) {
-        const float v = from_ordered((uint32_t)(key >> 32));
-        out.top_ids[row * top + at] = (int32_t)~(uint32_t)key;
-        out.top_logp[row * top + at] = none ? -INFINITY : (v - s.m) * scale - log;
+        if (split == 1) end.put_top(out, row * top + at, key);
+        else part_keys[unit * top + at] = key;
       };
-      // The row's alternatives are elements of the threads with the `top` largest keys, and not below the last of these.
-      const uint64_t mine = keys[t];
+      const uint64_t* mine = keys + team * NT;
+      uint64_t* list = lists + team * kRoom;
+      int* chosen = chosens + team * kMostTop;
+      const uint64_t key = keys[threadIdx.x];
       int rank = 0;
-      for (int i = 0; i < 256; ++i) rank += keys[i] > mine;
-      if (mine && rank < top) {
-        chosen[atomicAdd(&chosen_count, 1)] = t;
-        if (rank == top - 1) bound = mine;
+#pragma unroll 8
+      for (int i = 0; i < NT; ++i) rank += mine[i] > key;
+      if (key && rank < top) {
+        chosen[atomicAdd(&chosen_counts[team], 1)] = t;
+        if (rank == top - 1) bounds[team] = key;
       }
-      __syncthreads();
-      const uint64_t least = bound;
-      const int steps = share.steps(), work = chosen_count * steps;
+      if (end.broken || split > 1)
+        for (int i = t; i < top; i += NT) put(i, 0);  // (a part may have fewer elements)
+      meet();
+      const uint64_t least = bounds[team];
+      const int steps = (q1 - q0 + NT - 1) / NT + 2, work = end.broken ? 0 : chosen_counts[team] * steps;
       auto each = [&](auto&& f) {
-        for (int w = t; w < work; w += 256) {
-          const int j = share.piece(chosen[w / steps], w % steps);
+        for (int w = t; w < work; w += NT) {
+          const int who = chosen[w / steps], i = w % steps;
+          int j = q0 + who + NT * i;
+          if (i == steps - 2) j = front && who == NT - 1 ? 0 : -1;
+          else if (i == steps - 1) j = behind && who == NT - 2 ? p.count - 1 : -1;
+          else if (j >= q1) j = -1;
           if (j < 0) continue;
           float v[V];
           if (p.is_whole(j)) p.load_whole(v, j); else p.load_part(v, j, 0.0f);
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const int64_t e = (int64_t)j * V - p.shift + i;
+          for (int k = 0; k < V; ++k) {
+            const int64_t e = (int64_t)j * V - p.shift + k;
             if (e < 0 || e >= cols) continue;
-            const uint64_t o = (uint64_t)ordered(v[i]) << 32;
+            const uint64_t o = (uint64_t)ordered(v[k]) << 32;
             if ((o | (uint32_t)~j) >= least) f(o | (uint32_t)~(uint32_t)e);
           }
         }
       };
-      each([&](uint64_t key) {
-        const int at = atomicAdd(&list_count, 1);
-        if (at < kListRoom) list[at] = key;
+      each([&](uint64_t k) {
+        const int at = atomicAdd(&list_counts[team], 1);
+        if (at < kRoom) list[at] = k;
       });
-      __syncthreads();
-      const int n = list_count;
-      if (n <= kListRoom) {
-        for (int i = t; i < n; i += 256) {
-          const uint64_t key = list[i];
+      meet();
+      const int n = list_counts[team];
+      if (n <= kRoom) {
+        for (int i = t; i < n; i += NT) {
+          const uint64_t k = list[i];
           int above = 0;
-          for (int j = 0; j < n; ++j) above += list[j] > key;
-          if (above < top) put(above, key);
+          for (int q = 0; q < n; ++q) above += list[q] > k;
+          if (above < top) put(above, k);
         }
       } else {
-        // too many candidates (a row in ascending order, say): one alternative after the other
-        uint64_t last = ~0ull;
-        for (int k = 0; k < top; ++k) {
+        uint64_t bound = ~0ull;
+        for (int a = 0; a < top; ++a) {
           uint64_t b = 0;
-          each([&](uint64_t key) { b = key < last && key > b ? key : b; });
+          each([&](uint64_t k) { b = k < bound && k > b ? k : b; });
           b = wave_max(b);
-          if (lane == 0) best[wave] = b;
-          __syncthreads();
-          last = best[0];
-          for (int i = 1; i < 4; ++i) last = best[i] > last ? best[i] : last;
-          if (t == 0) put(k, last);
-          __syncthreads();
+          if (lane == 0) bests[wave] = b;
+          meet();
+          bound = 0;
+          for (int i = 0; i < WAVES; ++i) bound = bests[team * WAVES + i] > bound ? bests[team * WAVES + i] : bound;
+          if (t == 0 && bound) put(a, bound);
+          meet();
         }
       }
     }
-    __syncthreads();  // read before the next row's
+    meet();  // read before the next row's
   }
+}
+
+// Parts of rows put together, one wave to a row: sums by lane, alternatives from the parts' lists, which are in order, one after
+// the other.
+__global__ __launch_bounds__(64) void k_logp_join(const LogpPart* __restrict__ parts, const uint64_t* __restrict__ part_keys, int split,
+                                                  int64_t x_stride, const void* __restrict__ x, int type, int cols, Tokens tokens,
+                                                  int has_tokens, float scale, float c, int top, LogpOut out) {
+  const int lane = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const bool live = lane < split;
+  RowSum s = live ? parts[row * split + lane].s : RowSum{-INFINITY, 0.0f, 0.0f};
+  const uint64_t* list = part_keys + (row * split + (live ? lane : 0)) * top;
+  uint64_t head = live && top ? list[0] : 0;
+  int64_t tok = -1;
+  float xt = 0.0f;
+  if (lane == 0 && has_tokens) {
+    tok = tokens[row];
+    if (tok >= 0 && tok < cols) {
+      const int64_t at = row * x_stride + tok;
+      xt = type == kTypeF32 ? static_cast<const float*>(x)[at]
+           : type == kTypeBf16 ? static_cast<float>(static_cast<const __bf16*>(x)[at])
+                               : static_cast<float>(static_cast<const _Float16*>(x)[at]);
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1)
+    s = join(s, RowSum{__shfl_xor(s.m, off, 64), __shfl_xor(s.r, off, 64), __shfl_xor(s.u, off, 64)}, c);
+  const RowEnd end(s, scale);
+  if (lane == 0) end.put(out, row, tok, cols, xt);
+  int next = 1;
+  uint64_t kept = 0;  // the lane's own alternative
+  for (int a = 0; a < top; ++a) {
+    const uint64_t ahead = live && next < top ? list[next] : 0;
+    const uint64_t most = wave_max(head);
+    if (lane == a) kept = most;
+    if (head == most && most) {
+      head = ahead;
+      ++next;
+    }
+  }
+  if (lane < top) end.put_top(out, row * top + lane, kept);
 }
 
 struct LogpGrads {

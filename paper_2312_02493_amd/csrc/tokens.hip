@@ -22,6 +22,8 @@ struct artopk_tokens {
   uint32_t *key[2] = {nullptr, nullptr}, *pos[2] = {nullptr, nullptr}, *counts = nullptr;
   float* part = nullptr;
   uint8_t* marks = nullptr;  // rows of a table that are named; zeros between calls
+  LogpPart* parts = nullptr;     // of rows that several blocks share, and their alternatives
+  uint64_t* part_keys = nullptr;
   uint32_t *heavy = nullptr, *heavy_count = nullptr;  // runs in which heavy tokens begin
   int* error = nullptr;
   char err[kErrText] = {0};
@@ -40,6 +42,9 @@ constexpr int64_t kMostBlocks = 1 << 20;
                        __LINE__);                                                                              \
   } while (0)
 
+constexpr int64_t kShortRow = 2048;
+constexpr int64_t kMostParts = 4096;   // of all rows of a call
+constexpr int64_t kPartBlocks = 2048;  // that parts of rows make, at most
 constexpr int64_t kFewTokens = 8192, kFewTokensAlone = 14336;  // (at most what LDS holds beside the counts, 14336 keys)
 
 bool valid_limits(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
@@ -50,7 +55,7 @@ bool valid_limits(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
 int64_t runs_of(int64_t count) { return (count + kSumRun - 1) / kSumRun; }
 
 struct Layout {
-  size_t key[2], pos[2], counts, part, marks, heavy, error, bytes;
+  size_t key[2], pos[2], counts, part, marks, heavy, parts, part_keys, error, bytes;
   Layout(int64_t tokens, int64_t vocab, int64_t width) {
     size_t at = 0;
     auto take = [&](size_t n) {
@@ -66,6 +71,8 @@ struct Layout {
     part = tokens > kSumMost ? take((size_t)runs_of(tokens) * 2 * (size_t)width * 4) : 0;
     marks = tokens > kFewTokens ? take((size_t)vocab) : 0;
     heavy = take((size_t)(tokens / kSumMost + 1) * 4);
+    parts = take((size_t)kMostParts * sizeof(LogpPart));
+    part_keys = take((size_t)kMostParts * kMostTop * 8);
     error = take(8);  // and the list's length
     bytes = at;
   }
@@ -224,6 +231,8 @@ int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vo
   h->counts = reinterpret_cast<uint32_t*>(h->slab + at.counts);
   h->part = reinterpret_cast<float*>(h->slab + at.part);
   h->marks = h->slab + at.marks;
+  h->parts = reinterpret_cast<LogpPart*>(h->slab + at.parts);
+  h->part_keys = reinterpret_cast<uint64_t*>(h->slab + at.part_keys);
   h->heavy = reinterpret_cast<uint32_t*>(h->slab + at.heavy);
   h->heavy_count = reinterpret_cast<uint32_t*>(h->slab + at.error) + 1;
   h->error = reinterpret_cast<int*>(h->slab + at.error);
@@ -391,13 +400,30 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
   const LogpOut out = {logp_out, peak_out, logsum_out, entropy_out, top_ids_out, top_logp_out};
   with_type(type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    const unsigned blocks = (unsigned)std::min<int64_t>(rows, kMostBlocks);
-    auto go = [&](auto TOP) {
-      k_logp<T, TOP()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok, logp_out != nullptr,
-                                                      scale, scale * kLog2e, top, out, h->error);
+    constexpr int V = RowPieces<T>::V;
+    const T* at = static_cast<const T*>(logits);
+    const float c = scale * kLog2e;
+    const int has_tokens = logp_out != nullptr;
+    // short rows a wave each; few long ones in as many parts as keep every compute unit busy, each a piece a thread or more
+    const bool short_rows = vocab <= kShortRow;
+    int split = 1;
+    if (!short_rows && rows * 4 <= kPartBlocks)
+      split = (int)std::max<int64_t>(1, std::min<int64_t>({64, kPartBlocks / rows, vocab / V / 256}));
+    const int64_t units = short_rows ? (rows + 3) / 4 : rows * split;
+    const unsigned blocks = (unsigned)std::min<int64_t>(units, kMostBlocks);
+    auto go = [&](auto WAVES, auto TOP) {
+      k_logp<T, WAVES(), TOP()><<<blocks, 256, 0, h->stream>>>(at, stride, rows, (int)vocab, tok, has_tokens, scale, c, top, out, split,
+                                                               h->parts, h->part_keys, h->error);
     };
-    if (top) go(std::true_type());
-    else go(std::false_type());
+    auto with_top = [&](auto WAVES) {
+      if (top) go(WAVES, std::true_type());
+      else go(WAVES, std::false_type());
+    };
+    if (short_rows) with_top(std::integral_constant<int, 1>());
+    else with_top(std::integral_constant<int, 4>());
+    if (split > 1)
+      k_logp_join<<<(unsigned)rows, 64, 0, h->stream>>>(h->parts, h->part_keys, split, stride, logits, type, (int)vocab, tok, has_tokens,
+                                                        scale, c, top, out);
   });
   TOKENS_TRY(h, hipGetLastError());
   return ARTOPK_OK;

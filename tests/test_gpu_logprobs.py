@@ -1,11 +1,13 @@
 """Log probabilities of given tokens, entropy, top alternatives, and their gradient, against the definition in 64 bits.
 
 Tolerances, u = 2^-24.  With d = scale (x - peak) and e = e^d for each element beside the largest: an exponent in units of
-log2 is a difference, a product with c = scale log2(e) (itself three roundings off) and a power of two good to 2 u; the
-difference may be taken in two parts, from a reference up to 16 (in those units, 11.1 in natural ones) below the thread's largest
-element on.  So e is off by at most (6 (|d| + 2 * 11.1) + 2) u of itself: FIXED = 136 and 6 |d|.  A sum over n elements is made
-of at most `depth` additions one after the other (the thread's own, then eight halvings, with a factor good to 4 u each, and up
-to 24 rescalings of a thread's sum, of 4 u each).  Each quantity's own operations add a few u of its size.
+log2 is c x less a reference, c = scale log2(e) (itself three roundings off), rounded once, and its power of two is good to 2 u.
+The reference is c times the largest element so far, rounded, the same number wherever it is used; where it moves, an element's
+exponent is the sum of its parts, each rounded once, which together are as long as |d|.  So e is off by at most
+(6 |d| + FIXED) u of itself, FIXED = 20 (the power, the factors of the last conversion and a few more).  A sum over n elements is
+made of at most `depth` additions one after the other: a thread's batches of 32 and within them, halvings (8), and factors good to
+4 u each where the reference moves (at most once in 8192 elements, and a few times more) and where parts are put together (9).
+Each quantity's own operations add a few u of its size.
 """
 
 import math
@@ -18,7 +20,7 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 OUT_U = {"f32": U, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
 TINY = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -25}
-FIXED = 136.0
+FIXED = 20.0
 
 
 def _dtype(t):
@@ -107,7 +109,7 @@ class Row64:
         self.logsum[self.none.view(-1)] = 0.0
         self.logp = self.d - self.logsum.view(-1, 1)
         vocab = x.shape[1]
-        depth = 8.0 * (-(-vocab // 2048) + 1) + 8 + 4 * 8 + 24 * 4  # (2048: four elements a thread at least)
+        depth = 8.0 * (-(-vocab // 2048) + 1) + 8 + 4 * 9 + 4 * (vocab / 8192 + 4)
         per = FIXED + depth
         dr = U * (per * self.r + 6.0 * self.e1)
         # (powers of two below 2^-126 are zero: at most so much of each element, in the entropy times |d| <= 88)
