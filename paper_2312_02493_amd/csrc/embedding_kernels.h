@@ -33,31 +33,33 @@ typedef uint32_t Words2 __attribute__((ext_vector_type(4), aligned(2)));
 template <class T, int V>
 struct Some {
   T e[V];
-  __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(e, p, sizeof(e)); }
-  __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, e, sizeof(e)); }
-  // the same past the caches, sixteen bytes at a time (or element by element where there are fewer)
   using Words = std::conditional_t<sizeof(T) == 4, Words4, Words2>;
-  __device__ __forceinline__ void load_once(const T* p) {
+  // sixteen bytes at a time (as such: of single elements the compiler may make single loads), or all there is; with ONCE past
+  // the caches
+  template <bool ONCE = false>
+  __device__ __forceinline__ void load(const T* p) {
     if constexpr (sizeof(e) % 16 == 0) {
 #pragma unroll
       for (int i = 0; i < (int)sizeof(e) / 16; ++i) {
-        const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words*>(p) + i);
+        const Words* at = reinterpret_cast<const Words*>(p) + i;
+        Words w;
+        if constexpr (ONCE) w = __builtin_nontemporal_load(at); else w = *at;
         __builtin_memcpy(reinterpret_cast<char*>(e) + 16 * i, &w, 16);
       }
     } else {
-      load(p);
+      __builtin_memcpy(e, p, sizeof(e));
     }
   }
-  __device__ __forceinline__ void store_once(T* p) const {
+  __device__ __forceinline__ void store(T* p) const {
     if constexpr (sizeof(e) % 16 == 0) {
 #pragma unroll
       for (int i = 0; i < (int)sizeof(e) / 16; ++i) {
         Words w;
         __builtin_memcpy(&w, reinterpret_cast<const char*>(e) + 16 * i, 16);
-        __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p) + i);
+        reinterpret_cast<Words*>(p)[i] = w;
       }
     } else {
-      store(p);
+      __builtin_memcpy(p, e, sizeof(e));
     }
   }
 };
@@ -485,7 +487,7 @@ __global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __
         for (int i = 0; i < N(); ++i) {
           const uint32_t p = __builtin_amdgcn_readlane(my_pos, all || e + i < e1 ? e + i : e1 - 1);
           const TD* at = dy + (int64_t)p * dy_stride + from;
-          if (ONCE) in[i].load_once(at); else in[i].load(at);
+          in[i].template load<ONCE>(at);
         }
 #pragma unroll
         for (int i = 0; i < N(); ++i)

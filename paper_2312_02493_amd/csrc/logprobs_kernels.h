@@ -56,15 +56,50 @@ __device__ __forceinline__ float largest(const float* x) {
   return m;
 }
 
+// Values of other lanes by data-parallel moves: a lane that has no source keeps `other`.  A row is sixteen lanes.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t other) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float moved(float v, float other) {
+  return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(v), __float_as_uint(other)));
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t moved(uint64_t v, uint64_t other) {
+  return (uint64_t)moved<CTRL, ROWS>((uint32_t)(v >> 32), (uint32_t)(other >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v, (uint32_t)other);
+}
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(lane_value(__float_as_uint(v), lane)); }
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+  return (uint64_t)lane_value((uint32_t)(v >> 32), lane) << 32 | lane_value((uint32_t)v, lane);
+}
+
+// f over all lanes of a wave, `zero` its neutral value: towards the end of each row, then of the rows, then from the last lane.
+template <class T, class F>
+__device__ __forceinline__ T over_wave(T v, T zero, F&& f) {
+  v = f(v, moved<0x111>(v, zero));  // one lane, two, four and eight lanes back
+  v = f(v, moved<0x112>(v, zero));
+  v = f(v, moved<0x114>(v, zero));
+  v = f(v, moved<0x118>(v, zero));
+  v = f(v, moved<0x142, 0xa>(v, zero));  // rows 0 and 2 into 1 and 3
+  v = f(v, moved<0x143, 0xc>(v, zero));  // row 1 into 2 and 3
+  return lane_value(v, 63);
+}
 __device__ __forceinline__ float wave_largest(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-  return v;
+  return over_wave(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float wave_total(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  return over_wave(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+  return over_wave(v, (uint64_t)0, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+}
+// The largest of four lanes side by side, in each of them.
+__device__ __forceinline__ uint64_t four_max(uint64_t v) {
+  auto f = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
+  v = f(v, moved<0xb1>(v, v));  // the neighbour, then the other pair
+  return f(v, moved<0x4e>(v, v));
 }
 
 // A wave's share of a row: m is the largest element so far, the same in all lanes, r and u a lane's sums over its other ones
@@ -142,6 +177,33 @@ struct Gather {
   }
 };
 
+// A row in pieces of sixteen bytes from its first element on, wherever that lies.  The last one may be part of one: it is read as
+// the row's last V elements, of which those that belong to the piece before it count as -infinity.
+template <class T>
+struct RowRun {
+  static constexpr int V = 16 / sizeof(T);
+  const T* row;
+  int cols, count;
+  __device__ __forceinline__ RowRun(const T* r, int c) : row(r), cols(c), count((int)(((int64_t)c + V - 1) / V)) {}
+  // (a row shorter than a piece is read element by element)
+  __device__ __forceinline__ int begin(int j) const { return cols < V ? 0 : j * V + V <= cols ? j * V : cols - V; }
+  // of rows of V elements or more; ONCE: nothing reads it again, so past the caches (16384 x 64000 bfloat16 355 us, so 337)
+  template <bool ONCE>
+  __device__ __forceinline__ void ask(Some<T, V>& raw, int j, bool whole) const {
+    raw.template load<ONCE>(row + (whole ? j * V : begin(j)));
+  }
+  // `all`: the piece is there and whole
+  __device__ __forceinline__ void take(float* x, const Some<T, V>& raw, int j, bool all) const {
+    const int skip = all ? 0 : j * V - begin(j);
+#pragma unroll
+    for (int k = 0; k < V; ++k) x[k] = all || (j < count && k >= skip) ? static_cast<float>(raw.e[k]) : -INFINITY;
+  }
+  __device__ __forceinline__ void take_short(float* x, bool there) const {
+#pragma unroll
+    for (int k = 0; k < V; ++k) x[k] = there && k < cols ? static_cast<float>(row[k]) : -INFINITY;
+  }
+};
+
 // A row in pieces of sixteen bytes that begin at aligned places; the first and the last may be part of one.  Piece j holds the
 // elements from V j - shift on.
 template <class T>
@@ -174,15 +236,6 @@ struct LogpOut {
   float* top_logp;
 };
 
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const uint64_t o = __shfl_xor(v, off, 64);
-    v = o > v ? o : v;
-  }
-  return v;
-}
-
 // What a row's outputs come from, once its sums are known.
 struct RowEnd {
   RowSum s;
@@ -210,27 +263,30 @@ struct RowEnd {
   }
 };
 
-// A team of WAVES waves (1: four teams a block) has a row, or with `split` > 1 one of as many parts of it, whose sums and
-// alternatives then go to parts and part_keys for k_logp_join.  Thread t has the part's whole pieces t, t + 64 WAVES, ..; the last
-// thread but one has the row's last piece, the last one the first, where these are not whole.
+// A team of WAVES waves (4, or 1: four teams a block) has a row, or with `split` > 1 one of as many parts of it, whose sums and
+// alternatives then go to parts and part_keys for k_logp_join.  Thread t has the part's pieces t, t + 64 WAVES, ..
 //
-// Alternatives.  Every thread notes its largest element (the first among equal ones).  The `top` largest of these are a bound:
-// the row's alternatives are not below the last of them, and all lie with the threads that have them.  So those threads' elements
-// are read once more, those that reach the bound listed, and a listed one's place is the number of larger ones.  Should there be
-// more than kListRoom (a row in order), the alternatives are found one after the other.
+// Alternatives.  Every thread notes its largest element (the first among equal ones), groups of WAVES threads the largest of
+// theirs.  The `top`-th largest of these 64 is a bound: the row's alternatives are not below it, and all lie with the threads whose
+// largest element reaches it (some 24 for 20).  So those threads' elements are read once more, those that reach the bound listed
+// (64 ln(64 / (64 - top)) of them in a row without an order), and a listed one's place is the number of larger ones.  Should there
+// be more than kListRoom (a row in order), the alternatives are found one after the other.
 struct LogpPart {
   RowSum s;
   float unused;
 };
 
 template <class T, int WAVES, bool TOP>
-__global__ __launch_bounds__(256) void k_logp(const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, Tokens tokens,
-                                              int has_tokens, float scale, float c, int top, LogpOut out, int split,
-                                              LogpPart* __restrict__ parts, uint64_t* __restrict__ part_keys, int* __restrict__ error) {
-  constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES, kBatch = 32 / V, kRoom = kListRoom / kTeams;
+__global__ __launch_bounds__(256) void k_logp(
+    const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, Tokens tokens, int has_tokens, float scale, float c, int top,
+    LogpOut out, int split, LogpPart* __restrict__ parts, uint64_t* __restrict__ part_keys, int* __restrict__ error) {
+  constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES, kBatch = 16 / V;
+  constexpr int kRoom = kListRoom / kTeams;
   __shared__ RowSum sums[4];
-  __shared__ uint64_t keys[TOP ? 256 : 1], lists[TOP ? kListRoom : 1], bests[4], bounds[4];
-  __shared__ int chosens[TOP ? kTeams * kMostTop : 1], chosen_counts[4], list_counts[4];
+  __shared__ uint64_t keys[TOP ? kTeams * 64 : 1], lists[TOP ? kListRoom : 1], bests[4];
+  __shared__ uint8_t chosens[TOP ? 256 : 1];
+  __shared__ uint64_t bounds[kTeams];
+  __shared__ int list_counts[kTeams], chosen_counts[kTeams];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int team = wave / WAVES, t = threadIdx.x % NT, team_wave = wave % WAVES;
   auto meet = [] {
@@ -238,77 +294,65 @@ __global__ __launch_bounds__(256) void k_logp(const T* __restrict__ x, int64_t x
   };
   const int64_t units = rows * split;
   for (int64_t unit = (int64_t)blockIdx.x * kTeams + team; unit < units; unit += (int64_t)gridDim.x * kTeams) {
-    const int64_t row = unit / split;
-    const int part = (int)(unit % split);
-    const RowPieces<T> p(x + row * x_stride, cols);
-    const int64_t whole = p.whole1 - p.whole0;
-    const int q0 = p.whole0 + (int)(whole * part / split), q1 = p.whole0 + (int)(whole * (part + 1) / split);
-    const bool front = part == 0 && p.whole0 > 0, behind = part == split - 1 && p.count > p.whole1;
-    int64_t tok = -1;
-    float xt = 0.0f;
-    if (t == 0 && part == 0 && has_tokens) {
-      tok = tokens[row];
-      if (tok >= cols) *error = 1;
-      if (tok >= 0 && tok < cols) xt = static_cast<float>(p.row[tok]);
-    }
+    const int64_t row = split == 1 ? unit : unit / split;
+    const int part = split == 1 ? 0 : (int)(unit % split);
+    const RowRun<T> p(x + row * x_stride, cols);
+    const int q0 = split == 1 ? 0 : (int)((int64_t)p.count * part / split);
+    const int q1 = split == 1 ? p.count : (int)((int64_t)p.count * (part + 1) / split);
+    const int64_t tok = has_tokens && split == 1 ? tokens[row] : -1;
     Gather g;
-    float own = -INFINITY;  // the thread's largest element, and the first piece that has it
-    int where = -1;
+    // the thread's largest element, and the first piece that has it: to begin with its first piece
+    float own = -INFINITY;
+    int where = q0 + t < q1 ? q0 + t : -1;
     auto note = [&](float v, int j) {
-      if (TOP && (v > own || where < 0)) {
-        own = fmaxf(v, own);
+      if (TOP && v > own) {
+        own = v;
         where = j;
       }
     };
-    auto lone = [&](int j, int thread) {  // a piece of which there is only a part
-      float v[V];
-      if (t == thread) {
-        p.load_part(v, j, -INFINITY);
-      } else {
+    auto batch = [&](int j, bool all) {  // pieces j, j + NT, ..; with `all` they are all there and whole
+      Some<T, V> raw[kBatch];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = -INFINITY;
-      }
-      const float most = largest<V>(v);
-      if (t == thread) note(most, j);
-      g.add<V>(v, most, c);
-    };
-    if (front && team_wave == WAVES - 1) lone(0, NT - 1);
-    auto batch = [&](int j, bool all) {
-      Vec16<T> raw[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int at = j + i * NT;
-        raw[i] = *reinterpret_cast<const Vec16<T>*>(p.row + ((int64_t)(all || at < q1 ? at : q1 - 1) * V - p.shift));
-      }
+      for (int i = 0; i < kBatch; ++i) p.template ask<!TOP>(raw[i], all || j + i * NT < q1 ? j + i * NT : q1 - 1, all);
+      __builtin_amdgcn_sched_barrier(0);  // (all loads go out before one is waited for)
       float v[kBatch * V], most[kBatch];
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[i * V + k] = all || j + i * NT < q1 ? static_cast<float>(raw[i].e[k]) : -INFINITY;
+        const bool there = all || j + i * NT < q1;
+        p.take(v + i * V, raw[i], there ? j + i * NT : p.count, all);
         most[i] = largest<V>(v + i * V);
-        if (all || j + i * NT < q1) note(most[i], j + i * NT);
+        if (there) note(most[i], j + i * NT);
       }
       g.add<kBatch * V>(v, largest<kBatch>(most), c);
     };
-    int j = q0 + t;
-    const int last = q1 - kBatch * NT;  // (the same for all lanes: full batches begin up to here)
-    int base = q0;
+    // (the same for all lanes: full batches of whole pieces begin up to here)
+    const int last = (q1 * (int64_t)V <= cols ? q1 : q1 - 1) - kBatch * NT;
+    if (cols < V) {
+      float v[V];
+      p.take_short(v, t == 0 && q0 < q1);
+      const float most = largest<V>(v);
+      if (t == 0 && q0 < q1) note(most, 0);
+      g.add<V>(v, most, c);
+    }
+    int j = q0 + t, base = cols < V ? q1 : q0;
     for (; base <= last; base += kBatch * NT, j += kBatch * NT) batch(j, true);
-    if (base + team_wave * 64 < q1) batch(j, false);
-    if (behind && team_wave == (NT - 2) / 64) lone(p.count - 1, NT - 2);
+    for (; base + team_wave * 64 < q1; base += kBatch * NT, j += kBatch * NT) batch(j, false);
+    // (read behind the row, of which it is a part, and needed behind the sums)
+    const float xt = tok >= 0 && tok < cols ? static_cast<float>(p.row[tok]) : 0.0f;
     RowSum s = g.total(c);
+    // a thread's key: its largest element, the lower place first; 0 where it has none
+    const uint64_t own_key = where < 0 ? 0 : (uint64_t)ordered(own) << 32 | (uint32_t)~where;
     if (TOP) {
-      // a thread's key: its largest element, the lower place first; 0 where it has none
-      keys[threadIdx.x] = where < 0 ? 0 : (uint64_t)ordered(own) << 32 | (uint32_t)~where;
-      if (t == 0) {
-        bounds[team] = 0;
-        chosen_counts[team] = list_counts[team] = 0;
-      }
+      const uint64_t key = WAVES == 4 ? four_max(own_key) : own_key;
+      if (t % WAVES == 0) keys[team * 64 + t / WAVES] = key;
+      if (t == 0) list_counts[team] = chosen_counts[team] = 0;
     }
     if constexpr (WAVES > 1) {
       if (lane == 0) sums[wave] = s;
       meet();
-      s = join(join(sums[0], sums[1], c), join(sums[2], sums[3], c), c);
+      s = sums[0];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) s = join(s, sums[w], c);
     } else if (TOP) {
       meet();
     }
@@ -316,44 +360,54 @@ __global__ __launch_bounds__(256) void k_logp(const T* __restrict__ x, int64_t x
     if (t == 0) {
       if (split == 1) end.put(out, row, tok, cols, xt);
       else parts[unit].s = s;
+      if (tok >= cols) *error = 1;
     }
     if constexpr (TOP) {
       auto put = [&](int at, uint64_t key) {
         if (split == 1) end.put_top(out, row * top + at, key);
         else part_keys[unit * top + at] = key;
       };
-      const uint64_t* mine = keys + team * NT;
       uint64_t* list = lists + team * kRoom;
-      int* chosen = chosens + team * kMostTop;
-      const uint64_t key = keys[threadIdx.x];
-      int rank = 0;
-#pragma unroll 8
-      for (int i = 0; i < NT; ++i) rank += mine[i] > key;
-      if (key && rank < top) {
-        chosen[atomicAdd(&chosen_counts[team], 1)] = t;
-        if (rank == top - 1) bounds[team] = key;
+      uint8_t* chosen = chosens + team * NT;
+      if (team_wave == 0) {  // the bound
+        const uint64_t key = keys[team * 64 + lane];
+        int rank = 0;
+#pragma unroll 16
+        for (int i = 0; i < 64; ++i) rank += keys[team * 64 + i] > key;
+        if (lane == 0 && __popcll(__ballot(key != 0)) < top) bounds[team] = 0;
+        if (key != 0 && rank == top - 1) bounds[team] = key;
       }
       if (end.broken || split > 1)
         for (int i = t; i < top; i += NT) put(i, 0);  // (a part may have fewer elements)
       meet();
       const uint64_t least = bounds[team];
-      const int steps = (q1 - q0 + NT - 1) / NT + 2, work = end.broken ? 0 : chosen_counts[team] * steps;
+      const float least_value = from_ordered((uint32_t)(least >> 32));
+      if (own_key && own_key >= least && !end.broken) chosen[atomicAdd(&chosen_counts[team], 1)] = (uint8_t)t;
+      meet();
+      const int count = chosen_counts[team], pieces = (q1 - q0 + NT - 1) / NT;  // of a thread
+      // lanes side by side have a thread's pieces, and where these are few several threads'
+      int lg = 6;
+      while (lg > 0 && pieces << 1 <= 1 << lg) --lg;
+      const int with = lane & ((1 << lg) - 1);
       auto each = [&](auto&& f) {
-        for (int w = t; w < work; w += NT) {
-          const int who = chosen[w / steps], i = w % steps;
-          int j = q0 + who + NT * i;
-          if (i == steps - 2) j = front && who == NT - 1 ? 0 : -1;
-          else if (i == steps - 1) j = behind && who == NT - 2 ? p.count - 1 : -1;
-          else if (j >= q1) j = -1;
-          if (j < 0) continue;
-          float v[V];
-          if (p.is_whole(j)) p.load_whole(v, j); else p.load_part(v, j, 0.0f);
+        for (int i = team_wave * (64 >> lg) + (lane >> lg); i < count; i += WAVES * (64 >> lg)) {
+          for (int j = q0 + chosen[i] + with * NT; j < q1; j += NT << lg) {
+            float v[V];
+            if (cols < V) {
+              p.take_short(v, true);
+            } else {
+              Some<T, V> raw;
+              p.template ask<false>(raw, j, false);
+              p.take(v, raw, j, false);
+            }
+            if (!(largest<V>(v) >= least_value) && least) continue;
+            const int begin = p.begin(j);
 #pragma unroll
-          for (int k = 0; k < V; ++k) {
-            const int64_t e = (int64_t)j * V - p.shift + k;
-            if (e < 0 || e >= cols) continue;
-            const uint64_t o = (uint64_t)ordered(v[k]) << 32;
-            if ((o | (uint32_t)~j) >= least) f(o | (uint32_t)~(uint32_t)e);
+            for (int k = 0; k < V; ++k) {
+              if (begin + k < j * V || begin + k >= cols) continue;
+              const uint64_t o = (uint64_t)ordered(v[k]) << 32;
+              if ((o | (uint32_t)~j) >= least) f(o | (uint32_t)~(uint32_t)(begin + k));
+            }
           }
         }
       };
@@ -367,6 +421,7 @@ __global__ __launch_bounds__(256) void k_logp(const T* __restrict__ x, int64_t x
         for (int i = t; i < n; i += NT) {
           const uint64_t k = list[i];
           int above = 0;
+#pragma unroll 4
           for (int q = 0; q < n; ++q) above += list[q] > k;
           if (above < top) put(above, k);
         }
@@ -389,21 +444,26 @@ __global__ __launch_bounds__(256) void k_logp(const T* __restrict__ x, int64_t x
   }
 }
 
-// Parts of rows put together, one wave to a row: sums by lane, alternatives from the parts' lists, which are in order, one after
-// the other.
-__global__ __launch_bounds__(64) void k_logp_join(const LogpPart* __restrict__ parts, const uint64_t* __restrict__ part_keys, int split,
+// Parts of rows put together: sums by lane, alternatives from the parts' lists, which are in order, one after the other.  One wave
+// works, the others help it to read the lists.
+__global__ __launch_bounds__(1024) void k_logp_join(const LogpPart* __restrict__ parts, const uint64_t* __restrict__ part_keys, int split,
                                                   int64_t x_stride, const void* __restrict__ x, int type, int cols, Tokens tokens,
-                                                  int has_tokens, float scale, float c, int top, LogpOut out) {
+                                                  int has_tokens, float scale, float c, int top, LogpOut out,
+                                                    int* __restrict__ error) {
+  __shared__ uint64_t lists[64 * (kMostTop + 1)];
   const int lane = threadIdx.x;
   const int64_t row = blockIdx.x;
+  // (a list ends with 0, below every key)
+  for (int i = threadIdx.x; i < split * top; i += 1024)
+    lists[i / top * (kMostTop + 1) + i % top] = part_keys[row * split * top + i];
+  if (lane < split) lists[lane * (kMostTop + 1) + top] = 0;
   const bool live = lane < split;
   RowSum s = live ? parts[row * split + lane].s : RowSum{-INFINITY, 0.0f, 0.0f};
-  const uint64_t* list = part_keys + (row * split + (live ? lane : 0)) * top;
-  uint64_t head = live && top ? list[0] : 0;
   int64_t tok = -1;
   float xt = 0.0f;
   if (lane == 0 && has_tokens) {
     tok = tokens[row];
+    if (tok >= cols) *error = 1;
     if (tok >= 0 && tok < cols) {
       const int64_t at = row * x_stride + tok;
       xt = type == kTypeF32 ? static_cast<const float*>(x)[at]
@@ -411,19 +471,23 @@ __global__ __launch_bounds__(64) void k_logp_join(const LogpPart* __restrict__ p
                                : static_cast<float>(static_cast<const _Float16*>(x)[at]);
     }
   }
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1)
     s = join(s, RowSum{__shfl_xor(s.m, off, 64), __shfl_xor(s.r, off, 64), __shfl_xor(s.u, off, 64)}, c);
   const RowEnd end(s, scale);
   if (lane == 0) end.put(out, row, tok, cols, xt);
-  int next = 1;
+  const uint64_t* list = lists + (live ? lane : 0) * (kMostTop + 1);
+  uint64_t head = live ? list[0] : 0, ahead = live && top ? list[1] : 0;
+  int next = 2;
   uint64_t kept = 0;  // the lane's own alternative
   for (int a = 0; a < top; ++a) {
-    const uint64_t ahead = live && next < top ? list[next] : 0;
     const uint64_t most = wave_max(head);
     if (lane == a) kept = most;
     if (head == most && most) {
       head = ahead;
+      ahead = next <= top ? list[next] : 0;
       ++next;
     }
   }

@@ -42,7 +42,7 @@ constexpr int64_t kMostBlocks = 1 << 20;
                        __LINE__);                                                                              \
   } while (0)
 
-constexpr int64_t kShortRow = 2048;
+constexpr int64_t kShortRow = 2048, kLongerRow = 16384, kManyRows = 2048;
 constexpr int64_t kMostParts = 4096;   // of all rows of a call
 constexpr int64_t kPartBlocks = 2048;  // that parts of rows make, at most
 constexpr int64_t kFewTokens = 8192, kFewTokensAlone = 14336;  // (at most what LDS holds beside the counts, 14336 keys)
@@ -400,12 +400,12 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
   const LogpOut out = {logp_out, peak_out, logsum_out, entropy_out, top_ids_out, top_logp_out};
   with_type(type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    constexpr int V = RowPieces<T>::V;
+    constexpr int V = RowRun<T>::V;
     const T* at = static_cast<const T*>(logits);
     const float c = scale * kLog2e;
     const int has_tokens = logp_out != nullptr;
     // short rows a wave each; few long ones in as many parts as keep every compute unit busy, each a piece a thread or more
-    const bool short_rows = vocab <= kShortRow;
+    const bool short_rows = vocab <= kShortRow || (vocab <= kLongerRow && rows >= kManyRows);
     int split = 1;
     if (!short_rows && rows * 4 <= kPartBlocks)
       split = (int)std::max<int64_t>(1, std::min<int64_t>({64, kPartBlocks / rows, vocab / V / 256}));
@@ -422,8 +422,8 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
     if (short_rows) with_top(std::integral_constant<int, 1>());
     else with_top(std::integral_constant<int, 4>());
     if (split > 1)
-      k_logp_join<<<(unsigned)rows, 64, 0, h->stream>>>(h->parts, h->part_keys, split, stride, logits, type, (int)vocab, tok, has_tokens,
-                                                        scale, c, top, out);
+      k_logp_join<<<(unsigned)rows, 1024, 0, h->stream>>>(h->parts, h->part_keys, split, stride, logits, type, (int)vocab, tok, has_tokens,
+                                                          scale, c, top, out, h->error);
   });
   TOKENS_TRY(h, hipGetLastError());
   return ARTOPK_OK;
