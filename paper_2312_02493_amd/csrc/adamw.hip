@@ -258,7 +258,7 @@ int artopk_adamw_values(artopk_adamw* h, const void* first, const void* second, 
   const int64_t blocks = h->elems / kAdamBlock;
   auto go = [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    k_adamw_values<T><<<(unsigned)std::min<int64_t>((blocks + 3) / 4, 1 << 20), 256, 0, h->stream>>>(
+    k_adamw_values<T><<<dim3((unsigned)std::min<int64_t>((blocks + 15) / 16, 1 << 20), 2), 256, 0, h->stream>>>(
         static_cast<const uint32_t*>(first), static_cast<const uint32_t*>(second), scales, blocks, static_cast<T*>(first_out),
         static_cast<T*>(second_out));
   };

@@ -17,6 +17,7 @@
 #pragma once
 
 #include "elements.h"
+#include "lanes.h"
 
 namespace artopk {
 
@@ -52,42 +53,95 @@ __device__ __forceinline__ uint32_t adam_random(uint32_t place, uint32_t key) {
   return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float decode1(uint32_t code, int e) {
-  if (e == 255) return __builtin_nanf("");
-  return ldexpf(__uint_as_float((code & 127) << 20 | (code & 128) << 24), e - kTop1);
-}
-__device__ __forceinline__ float decode2(uint32_t code, int e) {
-  if (e == 255) return __builtin_nanf("");
-  return ldexpf(__uint_as_float(code << 20), e - kTop2);
-}
-
-// `e` is the block's exponent field, at least top + 1 (so that field 1 is a normal number); `half` 16 random bits.
-__device__ __forceinline__ uint32_t encode1(float m, int e, uint32_t half) {
-  const uint32_t bits = __float_as_uint(m), mag = bits & 0x7fffffffu, rnd = half << 4 | 8;
-  const int32_t t = (int32_t)mag - ((e - kTop1) << 23);
-  const float step = ldexpf(__uint_as_float(mag), 127 + kTop1 + 2 - e);  // in steps of field 0
-  uint32_t low = (uint32_t)fmaf((float)rnd, 0x1p-20f, step);
-  low = low > 8 ? 8 : low;
-  return (t >= 1 << 23 ? (uint32_t)(t + (int32_t)rnd) >> 20 : low) | (bits >> 31) << 7;
-}
-__device__ __forceinline__ uint32_t encode2(float v, int e, uint32_t half) {
-  const uint32_t bits = __float_as_uint(v), rnd = half << 4 | 8;
-  const int32_t t = (int32_t)bits - ((e - kTop2) << 23);
-  return t >= 1 << 23 ? (uint32_t)(t + (int32_t)rnd) >> 20 : bits ? 8u : 0u;
-}
-
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+// Four codes of a word as values; e, the block's exponent field, is the same in all lanes.
+__device__ __forceinline__ void decode1(float (&m)[4], uint32_t codes, int e) {
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const uint32_t o = __shfl_xor(v, off, 64);
-    v = o > v ? o : v;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t c = i < 3 ? codes << (20 - 8 * i) : codes >> 4;  // the code in bits 20 to 27
+    m[i] = ldexpf(__uint_as_float((c & 0x07f00000u) | (c << 4 & 0x80000000u)), e - kTop1);
   }
-  return v;
+  if (e == 255)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = __builtin_nanf("");
+}
+__device__ __forceinline__ void decode2(float (&v)[4], uint32_t codes, int e) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t c = i < 3 ? codes << (20 - 8 * i) : codes >> 4;
+    v[i] = ldexpf(__uint_as_float(c & 0x0ff00000u), e - kTop2);
+  }
+  if (e == 255)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_nanf("");
 }
 
+// The top bytes of four words as one.
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
+  const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0703), hi = __builtin_amdgcn_perm(x[3], x[2], 0x07030c0c);
+  return lo | hi;
+}
+
+// `e` is the block's exponent field, at least top + 1 (so that field 1 is a normal number); the random bits' lower half.
+__device__ __forceinline__ uint32_t encode1(const float (&m)[4], int e, const uint32_t (&random)[4]) {
+  uint32_t x[4];
+  bool low = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t bits = __float_as_uint(m[i]), t = (bits & 0x7fffffffu) - ((uint32_t)(e - kTop1) << 23);
+    low |= (int32_t)t < 1 << 23;
+    x[i] = ((t + ((random[i] & 0xffffu) << 4 | 8u)) << 4 & 0x7fffffffu) | (bits & 0x80000000u);
+  }
+  if (__any(low)) {  // steps of field 0; rare: below 2^-13 of the block's largest
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t bits = __float_as_uint(m[i]), mag = bits & 0x7fffffffu;
+      if ((int32_t)mag - (int32_t)((uint32_t)(e - kTop1) << 23) < 1 << 23) {
+        const uint32_t rnd = (random[i] & 0xffffu) << 4 | 8u;
+        const uint32_t code = (uint32_t)fmaf((float)rnd, 0x1p-20f, ldexpf(__uint_as_float(mag), 127 + kTop1 + 2 - e));
+        x[i] = (code > 8 ? 8 : code) << 24 | (bits & 0x80000000u);
+      }
+    }
+  }
+  return top_bytes(x);
+}
+// The same for the second moment, by the upper half.
+__device__ __forceinline__ uint32_t encode2(const float (&v)[4], int e, const uint32_t (&random)[4]) {
+  uint32_t x[4];
+  bool low = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = __float_as_uint(v[i]) - ((uint32_t)(e - kTop2) << 23);
+    low |= (int32_t)t < 1 << 23;
+    x[i] = (t + ((random[i] >> 12 & 0xffff0u) | 8u)) << 4;
+  }
+  if (__any(low))
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((int32_t)(__float_as_uint(v[i]) - ((uint32_t)(e - kTop2) << 23)) < 1 << 23) x[i] = v[i] != 0.0f ? 8u << 24 : 0;
+  return top_bytes(x);
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return over_wave(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
+// Four elements; at a place of their type only by get and put (words at once: of single elements the compiler may make
+// single loads).
 template <class T>
 struct alignas(4 * sizeof(T)) Four {
   T e[4];
+  typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t Words2 __attribute__((ext_vector_type(2), aligned(2)));
+  using Words = std::conditional_t<sizeof(T) == 4, Words4, Words2>;
+  __device__ __forceinline__ void get(const T* p) {
+    const Words w = *reinterpret_cast<const Words*>(p);
+    __builtin_memcpy(e, &w, sizeof(e));
+  }
+  __device__ __forceinline__ void put(T* p) const {
+    Words w;
+    __builtin_memcpy(&w, e, sizeof(e));
+    *reinterpret_cast<Words*>(p) = w;
+  }
 };
 
 // Steps a counter on the device and works out the step's terms, for steps that are replayed from a graph.
@@ -107,123 +161,143 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamChunk* __restrict__ chu
                                                const float* __restrict__ update, void* __restrict__ first,
                                                void* __restrict__ second, uint8_t* __restrict__ scales, AdamFixed f, AdamTerms terms,
                                                const AdamTerms* __restrict__ later) {
+  constexpr int kAhead = CODES ? 2 : 1;  // blocks a wave has under way
   const AdamChunk chunk = chunks[blockIdx.x];
   if (later) terms = *later;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float rate = terms.rate * chunk.factor, keep = 1.0f - f.eta * chunk.factor * chunk.decay;
+  for (int b0 = wave * (kAdamBlocks / 4); b0 < (wave + 1) * (kAdamBlocks / 4) && b0 * kAdamBlock < chunk.count; b0 += kAhead) {
+    Four<T> in_w[kAhead];
+    Four<float> in_g[kAhead], in_m[kAhead], in_v[kAhead];
+    uint32_t in_c1[kAhead], in_c2[kAhead];
+    int in_e[kAhead];
 #pragma unroll
-  for (int q = 0; q < kAdamBlocks / 4; ++q) {
-    const int b = wave * (kAdamBlocks / 4) + q, c = b * kAdamBlock + lane * 4;
-    if (b * kAdamBlock >= chunk.count) continue;
-    const uint32_t block = chunk.block + b;
-    const int64_t place = (int64_t)block * kAdamBlock + lane * 4;
-    const int64_t at = chunk.at + c;
-    const int n = chunk.count - c;  // elements from here on
-    float w[4], g[4], m[4], v[4];
-    if (n >= 4) {
-      Four<T> x;
-      Four<float> u;
-      __builtin_memcpy(&x, weights + at, sizeof(x));
-      __builtin_memcpy(&u, update + at, sizeof(u));
+    for (int q = 0; q < kAhead; ++q) {
+      // (blocks behind the tensor's end: its last one again, which is not written)
+      const int b = (b0 + q) * kAdamBlock < chunk.count ? b0 + q : (chunk.count - 1) / kAdamBlock, n = chunk.count - b * kAdamBlock;
+      const uint32_t block = chunk.block + b;
+      const int64_t at = chunk.at + b * kAdamBlock + lane * 4;
+      if (n >= kAdamBlock || lane * 4 + 4 <= n) {
+        in_w[q].get(weights + at);
+        in_g[q].get(update + at);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = static_cast<float>(x.e[i]);
-        g[i] = u.e[i];
+        for (int i = 0; i < 4; ++i) {
+          in_w[q].e[i] = lane * 4 + i < n ? weights[at + i] : static_cast<T>(0.0f);
+          in_g[q].e[i] = lane * 4 + i < n ? update[at + i] : 0.0f;
+        }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = i < n ? static_cast<float>(weights[at + i]) : 0.0f;
-        g[i] = i < n ? update[at + i] : 0.0f;
-      }
-    }
-    if constexpr (CODES) {
-      const uint32_t c1 = static_cast<const uint32_t*>(first)[place >> 2], c2 = static_cast<const uint32_t*>(second)[place >> 2];
-      const int e1 = scales[2 * (size_t)block], e2 = scales[2 * (size_t)block + 1];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        m[i] = decode1(c1 >> (8 * i) & 255, e1);
-        v[i] = decode2(c2 >> (8 * i) & 255, e2);
-      }
-    } else {
-      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(first) + place);
-      const float4 d = *reinterpret_cast<const float4*>(static_cast<const float*>(second) + place);
-      m[0] = a.x, m[1] = a.y, m[2] = a.z, m[3] = a.w;
-      v[0] = d.x, v[1] = d.y, v[2] = d.z, v[3] = d.w;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = g[i] * f.scale;
-      m[i] = m[i] * f.b1 + x * f.c1;
-      v[i] = v[i] * f.b2 + (x * x) * f.c2;
-      const float way = m[i] / fmaf(sqrtf(v[i]), terms.root, f.eps);
-      w[i] = fmaf(-rate, way, w[i] * keep);
-    }
-    if (n >= 4) {
-      Four<T> x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x.e[i] = static_cast<T>(w[i]);
-      __builtin_memcpy(weights + at, &x, sizeof(x));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i < n) weights[at + i] = static_cast<T>(w[i]);
-        else m[i] = v[i] = 0.0f;  // (places behind the tensor's end hold zeros)
+      const size_t word = (size_t)block * (kAdamBlock / 4) + lane;
+      if constexpr (CODES) {
+        in_c1[q] = static_cast<const uint32_t*>(first)[word];
+        in_c2[q] = static_cast<const uint32_t*>(second)[word];
+        in_e[q] = reinterpret_cast<const uint16_t*>(scales)[block];
+      } else {
+        in_m[q] = static_cast<const Four<float>*>(first)[word];
+        in_v[q] = static_cast<const Four<float>*>(second)[word];
       }
     }
-    if constexpr (CODES) {
-      uint32_t big1 = 0, big2 = 0;
+    __builtin_amdgcn_sched_barrier(0);  // (all loads go out before one is waited for)
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      const int b = b0 + q, n = chunk.count - b * kAdamBlock - lane * 4;  // elements from the lane's first on
+      if (b * kAdamBlock >= chunk.count) break;
+      const uint32_t block = chunk.block + b;
+      const int64_t at = chunk.at + b * kAdamBlock + lane * 4;
+      const size_t word = (size_t)block * (kAdamBlock / 4) + lane;
+      float w[4], m[4], v[4];
+      if constexpr (CODES) {
+        const int e = __builtin_amdgcn_readfirstlane(in_e[q]);
+        decode1(m, in_c1[q], e & 255);
+        decode2(v, in_c2[q], e >> 8);
+      }
+      bool tiny = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t a = __float_as_uint(m[i]) & 0x7fffffffu, d = __float_as_uint(v[i]) & 0x7fffffffu;
-        big1 = a > big1 ? a : big1;
-        big2 = d > big2 ? d : big2;
+        const float x = in_g[q].e[i] * f.scale;
+        m[i] = (CODES ? m[i] : in_m[q].e[i]) * f.b1 + x * f.c1;
+        v[i] = (CODES ? v[i] : in_v[q].e[i]) * f.b2 + (x * x) * f.c2;
+        w[i] = static_cast<float>(in_w[q].e[i]) * keep;
+        tiny |= v[i] < 0x1p-96f;
       }
-      int e1 = (int)(wave_max_u32(big1) >> 23), e2 = (int)(wave_max_u32(big2) >> 23);
-      e1 = e1 > kTop1 + 1 ? e1 : kTop1 + 1;
-      e2 = e2 > kTop2 + 1 ? e2 : kTop2 + 1;
-      uint32_t c1 = 0, c2 = 0;
+      if (__any(tiny)) {  // (the quick square root and reciprocal do not know numbers below the normal ones)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t r = adam_random((uint32_t)place + i, terms.key);
-        c1 |= encode1(m[i], e1, r & 0xffff) << (8 * i);
-        c2 |= encode2(v[i], e2, r >> 16) << (8 * i);
+        for (int i = 0; i < 4; ++i) w[i] = fmaf(-rate, m[i] / fmaf(sqrtf(v[i]), terms.root, f.eps), w[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = fmaf(-rate, m[i] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), terms.root, f.eps)), w[i]);
       }
-      static_cast<uint32_t*>(first)[place >> 2] = c1;
-      static_cast<uint32_t*>(second)[place >> 2] = c2;
-      if (lane == 0) {
-        scales[2 * (size_t)block] = (uint8_t)e1;
-        scales[2 * (size_t)block + 1] = (uint8_t)e2;
+      if (n >= 4) {
+        Four<T> o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.e[i] = static_cast<T>(w[i]);
+        o.put(weights + at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i < n) weights[at + i] = static_cast<T>(w[i]);
+          else m[i] = v[i] = 0.0f;  // (places behind the tensor's end hold zeros)
+        }
       }
-    } else {
-      *reinterpret_cast<float4*>(static_cast<float*>(first) + place) = make_float4(m[0], m[1], m[2], m[3]);
-      *reinterpret_cast<float4*>(static_cast<float*>(second) + place) = make_float4(v[0], v[1], v[2], v[3]);
+      if constexpr (CODES) {
+        uint32_t big1 = 0, big2 = 0, random[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a = __float_as_uint(m[i]) & 0x7fffffffu, d = __float_as_uint(v[i]) & 0x7fffffffu;
+          big1 = a > big1 ? a : big1;
+          big2 = d > big2 ? d : big2;
+          random[i] = adam_random((uint32_t)word * 4 + i, terms.key);
+        }
+        int e1 = (int)(wave_max(big1) >> 23), e2 = (int)(wave_max(big2) >> 23);
+        e1 = e1 > kTop1 + 1 ? e1 : kTop1 + 1;
+        e2 = e2 > kTop2 + 1 ? e2 : kTop2 + 1;
+        static_cast<uint32_t*>(first)[word] = encode1(m, e1, random);
+        static_cast<uint32_t*>(second)[word] = encode2(v, e2, random);
+        if (lane == 0) reinterpret_cast<uint16_t*>(scales)[block] = (uint16_t)(e1 | e2 << 8);
+      } else {
+        Four<float> o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.e[i] = m[i];
+        static_cast<Four<float>*>(first)[word] = o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.e[i] = v[i];
+        static_cast<Four<float>*>(second)[word] = o;
+      }
     }
   }
 }
 
-// Moments of 8 bits as values.
+// Moments of 8 bits as values: blockIdx.y = 0 the first, 1 the second.  A wave takes four blocks at a time.
 template <class T>
 __global__ __launch_bounds__(256) void k_adamw_values(const uint32_t* __restrict__ first, const uint32_t* __restrict__ second,
                                                       const uint8_t* __restrict__ scales, int64_t blocks, T* __restrict__ first_out,
                                                       T* __restrict__ second_out) {
   const int lane = threadIdx.x & 63;
-  for (int64_t b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); b < blocks; b += (int64_t)gridDim.x * 4) {
-    const int64_t place = b * kAdamBlock + lane * 4;
-    Four<T> o;
-    if (first_out) {
-      const uint32_t c = first[place >> 2];
-      const int e = scales[2 * b];
+  const bool one = blockIdx.y == 0;
+  const uint32_t* codes = one ? first : second;
+  T* out = one ? first_out : second_out;
+  if (!out) return;
+  for (int64_t b = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 4; b < blocks; b += (int64_t)gridDim.x * 16) {
+    uint32_t c[4];
+    int e[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o.e[i] = static_cast<T>(decode1(c >> (8 * i) & 255, e));
-      *reinterpret_cast<Four<T>*>(first_out + place) = o;
+    for (int q = 0; q < 4; ++q) {
+      const int64_t from = b + q < blocks ? b + q : blocks - 1;
+      c[q] = codes[from * (kAdamBlock / 4) + lane];
+      e[q] = scales[2 * from + (one ? 0 : 1)];
     }
-    if (second_out) {
-      const uint32_t c = second[place >> 2];
-      const int e = scales[2 * b + 1];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o.e[i] = static_cast<T>(decode2(c >> (8 * i) & 255, e));
-      *reinterpret_cast<Four<T>*>(second_out + place) = o;
+    for (int q = 0; q < 4; ++q) {
+      if (b + q >= blocks) break;
+      float v[4];
+      const int at = __builtin_amdgcn_readfirstlane(e[q]);
+      if (one) decode1(v, c[q], at); else decode2(v, c[q], at);
+      Four<T> o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o.e[i] = static_cast<T>(v[i]);
+      reinterpret_cast<Four<T>*>(out)[(b + q) * (kAdamBlock / 4) + lane] = o;
     }
   }
 }

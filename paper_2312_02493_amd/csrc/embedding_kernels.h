@@ -50,13 +50,15 @@ struct Some {
       __builtin_memcpy(e, p, sizeof(e));
     }
   }
+  template <bool ONCE = false>
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (sizeof(e) % 16 == 0) {
 #pragma unroll
       for (int i = 0; i < (int)sizeof(e) / 16; ++i) {
         Words w;
         __builtin_memcpy(&w, reinterpret_cast<const char*>(e) + 16 * i, 16);
-        reinterpret_cast<Words*>(p)[i] = w;
+        if constexpr (ONCE) __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p) + i);
+        else reinterpret_cast<Words*>(p)[i] = w;
       }
     } else {
       __builtin_memcpy(p, e, sizeof(e));
@@ -98,7 +100,7 @@ __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int
       if (c[u] + V <= cols) {
 #pragma unroll
         for (int j = 0; j < V; ++j) o.e[j] = static_cast<TY>(good ? static_cast<float>(in[u].e[j]) * scale : other);
-        o.store(out + c[u]);
+        o.template store<true>(out + c[u]);
       } else {
         for (int64_t j = c[u]; j < cols; ++j) out[j] = static_cast<TY>(good ? static_cast<float>(row[j]) * scale : other);
       }

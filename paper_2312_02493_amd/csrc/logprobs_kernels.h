@@ -17,6 +17,7 @@
 #pragma once
 
 #include "embedding_kernels.h"
+#include "lanes.h"
 
 namespace artopk {
 
@@ -56,36 +57,6 @@ __device__ __forceinline__ float largest(const float* x) {
   return m;
 }
 
-// Values of other lanes by data-parallel moves: a lane that has no source keeps `other`.  A row is sixteen lanes.
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t other) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)v, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ float moved(float v, float other) {
-  return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(v), __float_as_uint(other)));
-}
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ uint64_t moved(uint64_t v, uint64_t other) {
-  return (uint64_t)moved<CTRL, ROWS>((uint32_t)(v >> 32), (uint32_t)(other >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v, (uint32_t)other);
-}
-__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
-__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(lane_value(__float_as_uint(v), lane)); }
-__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
-  return (uint64_t)lane_value((uint32_t)(v >> 32), lane) << 32 | lane_value((uint32_t)v, lane);
-}
-
-// f over all lanes of a wave, `zero` its neutral value: towards the end of each row, then of the rows, then from the last lane.
-template <class T, class F>
-__device__ __forceinline__ T over_wave(T v, T zero, F&& f) {
-  v = f(v, moved<0x111>(v, zero));  // one lane, two, four and eight lanes back
-  v = f(v, moved<0x112>(v, zero));
-  v = f(v, moved<0x114>(v, zero));
-  v = f(v, moved<0x118>(v, zero));
-  v = f(v, moved<0x142, 0xa>(v, zero));  // rows 0 and 2 into 1 and 3
-  v = f(v, moved<0x143, 0xc>(v, zero));  // row 1 into 2 and 3
-  return lane_value(v, 63);
-}
 __device__ __forceinline__ float wave_largest(float v) {
   return over_wave(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
 }
@@ -498,21 +469,24 @@ struct LogpGrads {
   const float *peak, *logsum, *entropy, *dlogp, *dlse, *dentropy;  // rows each; dlogp, dlse, and entropy with dentropy may be NULL
 };
 
-// 1024 pieces of a row a block.  dx may be x itself: a thread reads its elements before it writes them.
-template <class T, bool SAME>  // SAME: dx's rows lie within sixteen bytes as x's do
+// Four pieces of a row a thread: of one row a block (a row has `tiles` blocks), or with WAVES = 1, for short rows, of one row a
+// wave.  dx may be x itself: a thread reads its elements before it writes them.  It goes past the caches, which it
+// would only fill (8192 x 128000 bfloat16 722 us, so 707); x is better left to them (2047 x 10007 float16 26 us past them, so 19).
+template <class T, bool SAME, int WAVES>  // SAME: dx's rows lie within sixteen bytes as x's do
 __global__ __launch_bounds__(256) void k_logp_backward(const T* x, int64_t x_stride, int64_t rows, int cols, Tokens tokens,
                                                        int has_tokens, float scale, float c, LogpGrads in, T* dx,
                                                        int64_t dx_stride, int64_t units, int tiles, int* error) {
-  constexpr int V = RowPieces<T>::V;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t row = unit / tiles;
-    const int tile = (int)(unit % tiles);
+  constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES;
+  const int t = threadIdx.x % NT, team = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  for (int64_t unit = (int64_t)blockIdx.x * kTeams + team; unit < units; unit += (int64_t)gridDim.x * kTeams) {
+    const int64_t row = WAVES == 1 ? unit : unit / tiles;
+    const int tile = WAVES == 1 ? 0 : (int)(unit % tiles);
     const RowPieces<T> p(x + row * x_stride, cols);
     T* out = dx + row * dx_stride;
     int64_t tok = has_tokens ? tokens[row] : -1;
     const float peak = in.peak[row], logsum = in.logsum[row], dent = in.dentropy ? in.dentropy[row] : 0.0f, h = in.dentropy ? in.entropy[row] : 0.0f;
     const float dlogp = in.dlogp && tok >= 0 ? in.dlogp[row] : 0.0f, dlse = in.dlse ? in.dlse[row] : 0.0f;
-    if (tok >= cols && tile == 0 && threadIdx.x == 0) *error = 1;
+    if (tok >= cols && tile == 0 && t == 0) *error = 1;
     // grad = p (a + b d), d = log2 p
     const bool broken = peak != peak || tok >= cols, none = peak == -INFINITY;
     const float top = none ? 0.0f : peak, less = logsum * kLog2e;
@@ -544,21 +518,17 @@ __global__ __launch_bounds__(256) void k_logp_backward(const T* x, int64_t x_str
     };
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int j = tile * 1024 + u * 256 + threadIdx.x;
+      const int j = (tile * 4 + u) * NT + t;
       if (j >= p.count) continue;
       float v[V];
       if (p.is_whole(j)) {
         p.load_whole(v, j);
         piece(v, j);
         T* to = out + ((int64_t)j * V - p.shift);
-        if constexpr (SAME) {
-          store_elems<V>(to, v);
-        } else {
-          Some<T, V> o;
+        Some<T, V> o;
 #pragma unroll
-          for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(v[i]);
-          o.store(to);
-        }
+        for (int i = 0; i < V; ++i) o.e[i] = static_cast<T>(v[i]);
+        o.template store<SAME>(to);
       } else {
         p.load_part(v, j, 0.0f);
         piece(v, j);

@@ -468,17 +468,25 @@ int artopk_token_logprobs_backward(artopk_tokens* h, const void* logits, int64_t
                     (rows <= 1 || (stride - dstride) * (int64_t)size % 16 == 0);
   with_type(type, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    const int64_t pieces = (vocab + 2 * (RowPieces<T>::V - 1)) / RowPieces<T>::V;  // at most, wherever rows begin
-    const int tiles = (int)((pieces + 1023) / 1024);
+    constexpr int V = RowPieces<T>::V;
+    // at most, wherever rows begin
+    const bool whole = vocab % V == 0 && aligned16(logits) && (rows <= 1 || stride % V == 0);
+    const int64_t pieces = whole ? vocab / V : (vocab + 2 * (V - 1)) / V;
+    const bool short_rows = pieces <= 256;
+    const int tiles = short_rows ? 1 : (int)((pieces + 1023) / 1024);
     const int64_t units = rows * tiles;
-    const unsigned blocks = (unsigned)std::min<int64_t>(units, kMostBlocks);
-    auto go = [&](auto SAME) {
-      k_logp_backward<T, SAME()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok,
-                                                                dlogp != nullptr, scale, scale * kLog2e, in, static_cast<T*>(dlogits),
-                                                                dstride, units, tiles, h->error);
+    const unsigned blocks = (unsigned)std::min<int64_t>(short_rows ? (rows + 3) / 4 : units, kMostBlocks);
+    auto go = [&](auto SAME, auto WAVES) {
+      k_logp_backward<T, SAME(), WAVES()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok,
+                                                                         dlogp != nullptr, scale, scale * kLog2e, in,
+                                                                         static_cast<T*>(dlogits), dstride, units, tiles, h->error);
     };
-    if (same) go(std::true_type());
-    else go(std::false_type());
+    auto with_waves = [&](auto SAME) {
+      if (short_rows) go(SAME, std::integral_constant<int, 1>());
+      else go(SAME, std::integral_constant<int, 4>());
+    };
+    if (same) with_waves(std::true_type());
+    else with_waves(std::false_type());
   });
   TOKENS_TRY(h, hipGetLastError());
   return ARTOPK_OK;
