@@ -287,6 +287,7 @@ class Context:
 
 
 _types = {}  # torch's element types -> ARTOPK_G_*, filled when torch is there
+_whole = {}  # torch's types of whole numbers -> bits, the same
 
 
 def _elem_types():
@@ -294,6 +295,7 @@ def _elem_types():
         import torch
 
         _types.update({torch.float32: ARTOPK_G_F32, torch.bfloat16: ARTOPK_G_BF16, torch.float16: ARTOPK_G_F16})
+        _whole.update({torch.uint8: 8, torch.int32: 32, torch.int64: 64})
     return _types
 
 
@@ -352,6 +354,7 @@ class _Handle:
         if not torch.cuda.is_available():
             raise RuntimeError("the AR-Topk library needs a GPU; there is no CPU path")
         self._lib = load_library()
+        _elem_types()
         if stream is None:
             stream = torch.cuda.current_stream().cuda_stream
         self._device = torch.cuda.current_device()
@@ -489,22 +492,18 @@ def artopk_tokens_scratch_bytes(max_tokens: int, max_vocab: int, max_width: int 
 
 
 def _token_bits(t) -> int:
-    import torch
-
-    bits = {torch.int32: 32, torch.int64: 64}.get(t.dtype)
-    if bits is None:
+    bits = _whole.get(t.dtype, 0)
+    if bits < 32:
         raise ArTopkError(-1, f"tokens are {t.dtype}: int32 or int64 are taken")
     return bits
 
 
-def _matrix_of(t, name: str, rows: int, cols: int, device: int, dtype: str) -> Optional[int]:
-    """Address of a contiguous rows x cols matrix of torch's `dtype` on the device."""
-    import torch
-
+def _top_rows(t, name: str, rows: int, top: int, device: int, right: bool) -> int:
+    """Address of a contiguous rows x top matrix of the right type on the device."""
     if t.get_device() != device:
         raise ArTopkError(-1, f"{name} is on {t.device}, not on the handle's device {device}")
-    if tuple(t.shape) != (rows, cols) or not t.is_contiguous() or t.dtype != getattr(torch, dtype):
-        raise ArTopkError(-1, f"{name} is not a contiguous {rows} x {cols} matrix of {dtype}")
+    if tuple(t.shape) != (rows, top) or not t.is_contiguous() or not right:
+        raise ArTopkError(-1, f"{name}, {t.dtype} {tuple(t.shape)}, is not a contiguous {rows} x {top} matrix of what is taken")
     return t.data_ptr()
 
 
@@ -548,8 +547,8 @@ class TokenContext(_Handle):
             if top_ids_out is None or top_logp_out is None or len(top_ids_out.shape) != 2:
                 raise ArTopkError(-1, "top_ids_out and top_logp_out are not two matrices")
             top = top_ids_out.shape[1]
-            ids = _matrix_of(top_ids_out, "top_ids_out", rows, top, dev, "int32")
-            lps = _matrix_of(top_logp_out, "top_logp_out", rows, top, dev, "float32")
+            ids = _top_rows(top_ids_out, "top_ids_out", rows, top, dev, _whole.get(top_ids_out.dtype) == 32)
+            lps = _top_rows(top_logp_out, "top_logp_out", rows, top, dev, _types.get(top_logp_out.dtype) == ARTOPK_G_F32)
         self._check(self._lib.artopk_token_logprobs(
             self._h, p, s, _elem_type(logits), rows, vocab, _vector(tokens, "tokens", rows, dev),
             32 if tokens is None else _token_bits(tokens), scale, _vector(logp_out, "logp_out", rows, dev, ARTOPK_G_F32),
@@ -614,13 +613,11 @@ class AdamWContext(_Handle):
         return first, second, torch.zeros(self.state_elems // 256, 2, dtype=kind, device=dev) if self.state_bits == 8 else None
 
     def _moments(self, first, second, scales):
-        import torch
-
-        kind = torch.uint8 if self.state_bits == 8 else torch.float32
+        eight = self.state_bits == 8
         out = []
-        for t, name, length in ((first, "first", self.state_elems), (second, "second", self.state_elems),
-                                (scales, "scales", self.state_elems // 128)):
-            if t is not None and t.dtype != (torch.uint8 if name == "scales" else kind):
+        for t, name, length, codes in ((first, "first", self.state_elems, eight), (second, "second", self.state_elems, eight),
+                                       (scales, "scales", self.state_elems // 128, True)):
+            if t is not None and (_whole.get(t.dtype) != 8 if codes else _types.get(t.dtype) != ARTOPK_G_F32):
                 raise ArTopkError(-1, f"{name} is {t.dtype}, which is not what is taken")
             out.append(_vector(t, name, length, self._device))
         return out

@@ -371,9 +371,10 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortKeys in, int coun
 // ---- sums over the sorted places -------------------------------------------------------------------
 // A block takes the tokens that begin in its run of kSumRun sorted places.  One of at most kSumMost places is summed there and
 // written; a heavier one is summed run by run, and k_embed_join adds the runs' shares up: part[run][1] of the run that it begins in
-// (its places in that run), part[run][0] of the others, float32; its first run is put on the list `heavy` (whose order does not
+// (its places in that run), part[run][0] of the others, float32, rows of part_pitch(cols); its first run is put on the list `heavy` (whose order does not
 // matter).  Waves take a token and 64 V columns at a time; `split` blocks share a run.  `zero_blocks` more
 // write zeros, spread among the others, so that both kinds are under way at any time.
+__host__ __device__ constexpr int64_t part_pitch(int64_t cols) { return (cols + 3) / 4 * 4; }  // rows at sixteen bytes
 constexpr int kSumRun = 32, kSumMost = 32, kSumWaves = 8;
 
 // What run `lo / kSumRun` has to do, the same in every lane.
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __
       if (c < cols && slot < 0) {
         put_sums<TG, V>(row, c, cols, s, scale, add, old);
       } else if (c < cols) {
-        float* to = part + (run * 2 + slot) * cols;
+        float* to = part + (run * 2 + slot) * part_pitch(cols);
         Some<float, V> one;
 #pragma unroll
         for (int j = 0; j < V; ++j) one.e[j] = s[j];
@@ -542,18 +543,18 @@ __global__ __launch_bounds__(1024) void k_embed_join(const uint32_t* __restrict_
       a += (same - 1) * apart + 1;
     }
     const int64_t stop = (a + kSumRun - 1) / kSumRun;  // runs run + 1 .. stop - 1 hold shares
-    const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4;
+    const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4, pitch = part_pitch(cols);
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < cols) {
       if (wave == 0)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (c + j < cols) s[j] = part[(run * 2 + 1) * cols + c + j];
+          if (c + j < cols) s[j] = part[(run * 2 + 1) * pitch + c + j];
       if (c + 4 <= cols) {
 #pragma unroll 4
         for (int64_t r = run + 1 + wave; r < stop; r += 16) {
           Some<float, 4> v;
-          v.load(part + (r * 2) * cols + c);
+          v.load(part + (r * 2) * pitch + c);
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[j] += v.e[j];
         }
@@ -561,7 +562,7 @@ __global__ __launch_bounds__(1024) void k_embed_join(const uint32_t* __restrict_
         for (int64_t r = run + 1 + wave; r < stop; r += 16)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (c + j < cols) s[j] += part[(r * 2) * cols + c + j];
+            if (c + j < cols) s[j] += part[(r * 2) * pitch + c + j];
       }
     }
 #pragma unroll

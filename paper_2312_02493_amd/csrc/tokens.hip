@@ -68,7 +68,7 @@ struct Layout {
       pos[i] = take((size_t)tokens * 4);
     }
     counts = take((size_t)kSortTiles * kSortDigits * 4);
-    part = tokens > kSumMost ? take((size_t)runs_of(tokens) * 2 * (size_t)width * 4) : 0;
+    part = tokens > kSumMost ? take((size_t)runs_of(tokens) * 2 * (size_t)part_pitch(width) * 4) : 0;
     marks = tokens > kFewTokens ? take((size_t)vocab) : 0;
     heavy = take((size_t)(tokens / kSumMost + 1) * 4);
     parts = take((size_t)kMostParts * sizeof(LogpPart));
@@ -112,6 +112,7 @@ void embed(artopk_tokens* h, const TT* table, int64_t table_stride, int64_t voca
 
 // Bytes of zeros that a launch of the sort writes beside its own work: as much as takes no longer than that does.
 constexpr int64_t kBesideCount = 32 << 20, kBesidePlace = 80 << 20;
+constexpr int64_t kFewZeros = 16 << 20;   // up to here the sums' launch writes them all
 constexpr int64_t kZeroShare = 64 << 10;  // and a block of the sums' launch
 constexpr int64_t kSumBlocks = 4096;      // of it, to be reached where columns can be shared
 constexpr int kZeroBlocks = 448;  // with the sort's own two on a compute unit
@@ -141,11 +142,12 @@ int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t v
   const int64_t round = kSortThreads * keys;
   const int64_t per = std::max<int64_t>(1, (count + round * kSortTiles - 1) / (round * kSortTiles)) * round;
   const int tiles = (int)((count + per - 1) / per);
-  zero.marks = zero.at ? h->marks : nullptr;
+  const bool beside_sort = zero.at && zero.end * zero.bytes >= kFewZeros;
+  zero.marks = beside_sort ? h->marks : nullptr;
   int64_t next = 0;
   auto beside = [&](int64_t bytes) {
     ZeroRows z = zero;
-    if (z.at) {
+    if (beside_sort) {
       z.begin = next;
       z.end = next = std::min(zero.end, next + std::max<int64_t>(1, bytes / z.bytes));
     }
@@ -154,13 +156,13 @@ int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t v
   int from = 1, shift = 0;
   for (int pass = 0; pass < passes; ++pass) {
     const int bits = (all - shift + passes - pass - 1) / (passes - pass);
-    const SortKeys in = {tokens, h->key[from], h->pos[from], (uint32_t)vocab, pass == 0, h->heavy_count, zero.at ? h->marks : nullptr};
+    const SortKeys in = {tokens, h->key[from], h->pos[from], (uint32_t)vocab, pass == 0, h->heavy_count, zero.marks ? h->marks : nullptr};
     // (the first launch finds out which rows are named)
-    const bool fill = zero.at && pass > 0;
+    const bool fill = beside_sort && pass > 0;
     k_sort_count<<<tiles + (fill ? kZeroBlocks : 0), kSortThreads, 0, h->stream>>>(in, count, per, shift, bits, tiles, h->counts,
                                                                                   h->error, fill ? beside(kBesideCount) : zero);
     auto go = [&](auto R) {
-      k_sort_place<R()><<<tiles + (zero.at ? kZeroBlocks : 0), kSortThreads, 0, h->stream>>>(
+      k_sort_place<R()><<<tiles + (beside_sort ? kZeroBlocks : 0), kSortThreads, 0, h->stream>>>(
           in, count, per, shift, bits, h->counts, tiles, h->key[1 - from], h->pos[1 - from], beside(kBesidePlace));
     };
     if (keys == 1) go(std::integral_constant<int, 1>());
@@ -169,6 +171,10 @@ int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t v
     from = 1 - from;
   }
   zero.begin = next;
+  if (!beside_sort) {
+    zero.key = h->key[from];
+    zero.count = count;
+  }
   return from;
 }
 
