@@ -15,6 +15,7 @@ using namespace artopk;
 
 struct artopk_adamw {
   hipStream_t stream = nullptr;
+  int device = 0;
   int64_t n = 0, elems = 0;
   int32_t type = 0, bits = 32;
   unsigned chunk_count = 0;
@@ -26,6 +27,14 @@ struct artopk_adamw {
 };
 
 namespace {
+
+// A handle's memory and stream belong to the device that was current when it was made.
+int check_device(char* err, int device) {
+  int now = -1;
+  if (hipGetDevice(&now) != hipSuccess || now != device)
+    return fail_text(err, ARTOPK_EINVAL, "the current device is %d, the handle's %d", now, device);
+  return ARTOPK_OK;
+}
 
 constexpr int64_t kMostTensors = 65535;
 constexpr int64_t kChunk = kAdamBlock * kAdamBlocks;
@@ -119,7 +128,12 @@ int create(artopk_adamw** out, const artopk_tensor* tensors, int32_t count, int6
   h->chunk_count = (unsigned)chunks.size();
   const size_t table = align_up(chunks.size() * sizeof(AdamChunk), 256);
   void* p = nullptr;
-  hipError_t e = hipMalloc(&p, table + 512);
+  hipError_t e = hipGetDevice(&h->device);
+  if (e != hipSuccess) {
+    delete h;
+    return fail_text(g_noctx_err, ARTOPK_EHIP, "no device: %s", hipGetErrorString(e));
+  }
+  e = hipMalloc(&p, table + 512);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     delete h;
@@ -178,6 +192,8 @@ const char* artopk_adamw_last_error(const artopk_adamw* h) { return h ? h->err :
 int artopk_adamw_set_step(artopk_adamw* h, int64_t step) {
   if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_adamw_set_step: handle is NULL");
   if (step < 0) return fail_text(h->err, ARTOPK_EINVAL, "step is negative");
+  int rc;
+  if ((rc = check_device(h->err, h->device))) return rc;
   k_adamw_counter<<<1, 1, 0, h->stream>>>(h->counter, step);
   ADAMW_TRY(h, hipGetLastError());
   return ARTOPK_OK;
@@ -187,6 +203,7 @@ int artopk_adamw_step(artopk_adamw* h, void* weights, const float* update, void*
                       float update_scale, float eta, double beta1, double beta2, float eps, uint64_t seed) {
   if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_adamw_step: handle is NULL");
   int rc;
+  if ((rc = check_device(h->err, h->device))) return rc;
   if (!weights || !update) return fail_text(h->err, ARTOPK_EINVAL, "weights or update is NULL");
   const size_t size = elem_size(h->type);
   if (reinterpret_cast<uintptr_t>(weights) % size) return fail_text(h->err, ARTOPK_EINVAL, "weights is not aligned to its elements");
@@ -239,6 +256,7 @@ int artopk_adamw_values(artopk_adamw* h, const void* first, const void* second, 
                         void* second_out) {
   if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_adamw_values: handle is NULL");
   int rc;
+  if ((rc = check_device(h->err, h->device))) return rc;
   if (h->bits != 8) return fail_text(h->err, ARTOPK_EINVAL, "moments of 32 bits are values already");
   if ((rc = check_moments(h, first, second, scales))) return rc;
   if (type != ARTOPK_G_F32 && type != ARTOPK_G_BF16)

@@ -9,7 +9,7 @@
 //
 // Measured: gradient of 32768 places x 2048 bfloat16 into 64000 rows of float32 (658 MB) 141 us = 4.7 TB/s, of which the sort's four
 // launches 35 (with 190 MB of zeros), the sums 96 (with the other 250 MB), heavy tokens' shares 9; lookup of 32768 x 4096, float32 to
-// bfloat16, 95 us.
+// bfloat16, 87 us (results through the caches 95).
 #pragma once
 
 #include "elements.h"
@@ -265,7 +265,6 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(SortKeys in, int64_
           all[j] += n;
           before[j] += t < (int)blockIdx.x ? n : 0;
         }
-      if (digits == 1) all[1] = 0;
     }
     const uint32_t lower = block_before(all[0] + all[1], room);
     if (d < digits) base[d] = lower + before[0];
@@ -333,7 +332,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortKeys in, int coun
   uint32_t* keys = reinterpret_cast<uint32_t*>(keys4);
   const int each = (count + 4 * kParts - 1) / (4 * kParts) * 4;  // of a share
   if (blockIdx.x == 0 && threadIdx.x == 0) *in.heavy_count = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = threadIdx.x; i < each * kParts; i += kSortThreads) {
     uint32_t k, p;
     in.get(i < count ? i : count - 1, k, p);
@@ -371,9 +370,13 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortKeys in, int coun
 // ---- sums over the sorted places -------------------------------------------------------------------
 // A block takes the tokens that begin in its run of kSumRun sorted places.  One of at most kSumMost places is summed there and
 // written; a heavier one is summed run by run, and k_embed_join adds the runs' shares up: part[run][1] of the run that it begins in
-// (its places in that run), part[run][0] of the others, float32, rows of part_pitch(cols); its first run is put on the list `heavy` (whose order does not
-// matter).  Waves take a token and 64 V columns at a time; `split` blocks share a run.  `zero_blocks` more
+// (its places in that run), part[run][0] of the others, float32, rows of part_pitch(cols); its first run is put on the list `heavy`
+// (whose order does not matter).  Waves take a token and 64 V columns at a time; `split` blocks share a run.  `zero_blocks` more
 // write zeros, spread among the others, so that both kinds are under way at any time.
+//
+// Measured on 32768 places x 2048 bfloat16 into 64000 rows of float32: zeros through the caches leave 256 MB behind that the sums then
+// wait for (171 us in all, past them 157), dy through them 157 (past them 151; only where its rows lie at sixteen bytes: neighbours
+// share lines otherwise, 4099 x 1111 float32 14 us and past them 17), more blocks than 4096 or sixteen waves a block 166 to 169.
 __host__ __device__ constexpr int64_t part_pitch(int64_t cols) { return (cols + 3) / 4 * 4; }  // rows at sixteen bytes
 constexpr int kSumRun = 32, kSumMost = 32, kSumWaves = 8;
 

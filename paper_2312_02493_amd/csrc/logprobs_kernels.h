@@ -157,15 +157,18 @@ struct RowRun {
   int cols, count;
   __device__ __forceinline__ RowRun(const T* r, int c) : row(r), cols(c), count((int)(((int64_t)c + V - 1) / V)) {}
   // (a row shorter than a piece is read element by element)
-  __device__ __forceinline__ int begin(int j) const { return cols < V ? 0 : j * V + V <= cols ? j * V : cols - V; }
+  __device__ __forceinline__ int64_t begin(int j) const {
+    const int64_t at = (int64_t)j * V;
+    return cols < V ? 0 : at + V <= cols ? at : cols - V;
+  }
   // of rows of V elements or more; ONCE: nothing reads it again, so past the caches (16384 x 64000 bfloat16 355 us, so 337)
   template <bool ONCE>
   __device__ __forceinline__ void ask(Some<T, V>& raw, int j, bool whole) const {
-    raw.template load<ONCE>(row + (whole ? j * V : begin(j)));
+    raw.template load<ONCE>(row + (whole ? (int64_t)j * V : begin(j)));
   }
   // `all`: the piece is there and whole
   __device__ __forceinline__ void take(float* x, const Some<T, V>& raw, int j, bool all) const {
-    const int skip = all ? 0 : j * V - begin(j);
+    const int skip = all ? 0 : (int)((int64_t)j * V - begin(j));
 #pragma unroll
     for (int k = 0; k < V; ++k) x[k] = all || (j < count && k >= skip) ? static_cast<float>(raw.e[k]) : -INFINITY;
   }
@@ -372,10 +375,10 @@ __global__ __launch_bounds__(256) void k_logp(
               p.take(v, raw, j, false);
             }
             if (!(largest<V>(v) >= least_value) && least) continue;
-            const int begin = p.begin(j);
+            const int64_t begin = p.begin(j);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-              if (begin + k < j * V || begin + k >= cols) continue;
+              if (begin + k < (int64_t)j * V || begin + k >= cols) continue;
               const uint64_t o = (uint64_t)ordered(v[k]) << 32;
               if ((o | (uint32_t)~j) >= least) f(o | (uint32_t)~(uint32_t)(begin + k));
             }

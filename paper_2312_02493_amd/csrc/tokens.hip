@@ -14,6 +14,7 @@ using namespace artopk;
 
 struct artopk_tokens {
   hipStream_t stream = nullptr;
+  int device = 0;
   int num_cu = 256;
   int64_t max_tokens = 0, max_vocab = 0, max_width = 0;
   uint8_t* slab = nullptr;
@@ -30,6 +31,14 @@ struct artopk_tokens {
 };
 
 namespace {
+
+// A handle's memory and stream belong to the device that was current when it was made.
+int check_device(char* err, int device) {
+  int now = -1;
+  if (hipGetDevice(&now) != hipSuccess || now != device)
+    return fail_text(err, ARTOPK_EINVAL, "the current device is %d, the handle's %d", now, device);
+  return ARTOPK_OK;
+}
 
 constexpr int64_t kMostWidth = 65536;
 constexpr int64_t kMostBlocks = 1 << 20;
@@ -84,6 +93,8 @@ int check_vector(char* err, const char* name, const void* p, size_t size) {
 }
 
 int check_tokens(artopk_tokens* h, const void* tokens, int32_t bits, int64_t count, int64_t vocab) {
+  int rc;
+  if ((rc = check_device(h->err, h->device))) return rc;
   if (count < 0 || count > h->max_tokens)
     return fail_text(h->err, ARTOPK_EINVAL, "%lld tokens are outside [0, %lld]", (long long)count, (long long)h->max_tokens);
   if (vocab < 1 || vocab > h->max_vocab)
@@ -221,6 +232,7 @@ int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vo
     return fail_text(g_noctx_err, ARTOPK_EHIP, "no device: %s", hipGetErrorString(e));
   }
   if (cus > 0) h->num_cu = cus;
+  h->device = dev;
   const Layout at(max_tokens, max_vocab, max_width);
   void* p = nullptr;
   e = hipMalloc(&p, at.bytes);
