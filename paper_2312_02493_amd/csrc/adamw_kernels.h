@@ -121,10 +121,6 @@ __device__ __forceinline__ uint32_t encode2(const float (&v)[4], int e, const ui
   return top_bytes(x);
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-  return over_wave(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-}
-
 // Four elements; at a place of their type only by get and put (words at once: of single elements the compiler may make
 // single loads).
 template <class T>

@@ -37,4 +37,11 @@ __device__ __forceinline__ T over_wave(T v, T zero, F&& f) {
   return lane_value(v, 63);
 }
 
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return over_wave(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+  return over_wave(v, (uint64_t)0, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+}
+
 }  // namespace artopk

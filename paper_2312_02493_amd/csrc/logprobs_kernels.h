@@ -63,9 +63,6 @@ __device__ __forceinline__ float wave_largest(float v) {
 __device__ __forceinline__ float wave_total(float v) {
   return over_wave(v, 0.0f, [](float a, float b) { return a + b; });
 }
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-  return over_wave(v, (uint64_t)0, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-}
 // The largest of four lanes side by side, in each of them.
 __device__ __forceinline__ uint64_t four_max(uint64_t v) {
   auto f = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
@@ -457,7 +454,14 @@ __global__ __launch_bounds__(1024) void k_logp_join(const LogpPart* __restrict__
   int next = 2;
   uint64_t kept = 0;  // the lane's own alternative
   for (int a = 0; a < top; ++a) {
-    const uint64_t most = wave_max(head);
+    // the upper halves (values) first: two lists' first values are rarely the same
+    const uint32_t value = (uint32_t)(head >> 32), place = (uint32_t)head, top_value = wave_max(value);
+    uint64_t who = __ballot(value == top_value);
+    if (__popcll(who) > 1) {
+      const uint32_t top_place = wave_max(value == top_value ? place : 0u);
+      who = __ballot(value == top_value && place == top_place);
+    }
+    const uint64_t most = lane_value(head, __ffsll((unsigned long long)who) - 1);
     if (lane == a) kept = most;
     if (head == most && most) {
       head = ahead;

@@ -52,8 +52,7 @@ constexpr int64_t kMostBlocks = 1 << 20;
   } while (0)
 
 constexpr int64_t kShortRow = 2048, kLongerRow = 16384, kManyRows = 2048;
-constexpr int64_t kMostParts = 4096;   // of all rows of a call
-constexpr int64_t kPartBlocks = 2048;  // that parts of rows make, at most
+constexpr int64_t kPartBlocks = 1024;  // that parts of rows make, at most
 constexpr int64_t kFewTokens = 8192, kFewTokensAlone = 14336;  // (at most what LDS holds beside the counts, 14336 keys)
 
 bool valid_limits(int64_t max_tokens, int64_t max_vocab, int64_t max_width) {
@@ -80,8 +79,8 @@ struct Layout {
     part = tokens > kSumMost ? take((size_t)runs_of(tokens) * 2 * (size_t)part_pitch(width) * 4) : 0;
     marks = tokens > kFewTokens ? take((size_t)vocab) : 0;
     heavy = take((size_t)(tokens / kSumMost + 1) * 4);
-    parts = take((size_t)kMostParts * sizeof(LogpPart));
-    part_keys = take((size_t)kMostParts * kMostTop * 8);
+    parts = take((size_t)kPartBlocks * sizeof(LogpPart));
+    part_keys = take((size_t)kPartBlocks * kMostTop * 8);
     error = take(8);  // and the list's length
     bytes = at;
   }
@@ -422,10 +421,12 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
     const T* at = static_cast<const T*>(logits);
     const float c = scale * kLog2e;
     const int has_tokens = logp_out != nullptr;
-    // short rows a wave each; few long ones in as many parts as keep every compute unit busy, each a piece a thread or more
+    // Short rows a wave each.  Few long ones in parts, as many as keep every compute unit busy, from sixteen pieces a thread on, where
+    // that saves more than the second launch costs: 8 x 40000 bfloat16 14.3 us, so 11.1, 8 x 20000 8.1 and 11.3; 300 x 128000 36 and 25,
+    // 400 x 100000 float32 33 and 35.
     const bool short_rows = vocab <= kShortRow || (vocab <= kLongerRow && rows >= kManyRows);
     int split = 1;
-    if (!short_rows && rows * 4 <= kPartBlocks)
+    if (!short_rows && rows * 3 <= kPartBlocks && vocab / V / 256 >= 16)
       split = (int)std::max<int64_t>(1, std::min<int64_t>({64, kPartBlocks / rows, vocab / V / 256}));
     const int64_t units = short_rows ? (rows + 3) / 4 : rows * split;
     const unsigned blocks = (unsigned)std::min<int64_t>(units, kMostBlocks);
