@@ -570,9 +570,10 @@ int artopk_muon_step(artopk_matrices* m, void* weights, float* momentum, const f
  * Both ends of a language model, and the optimiser of what is no matrix: embedding rows of tokens
  * and their gradient (which lands in a worker's flat vector, like a layer norm's weights'), log
  * probabilities of given tokens and their gradient, and AdamW over many tensors of a flat vector.
- * Two more handles, with the rules of those above (one stream, one device, memory at creation only,
- * calls that only enqueue kernels and can be recorded into a HIP graph, no overlapping calls on
- * one handle, buffers aligned to their elements unless stated).
+ * Two more handles, with the rules of those above (one stream, one device, which these refuse to
+ * be called without, memory at creation only, calls that only enqueue kernels and can be recorded
+ * into a HIP graph, no overlapping calls on one handle, buffers aligned to their elements unless
+ * stated).
  * ------------------------------------------------------------------------------------------ */
 
 typedef struct artopk_tokens artopk_tokens;
@@ -637,7 +638,7 @@ int artopk_embedding_backward(artopk_tokens* h, const void* dy, int64_t dy_strid
  *   top_ids_out, top_logp_out   device, rows x top int32 and float32: their indices and log p
  * Logits of -infinity have probability zero.  A row of nothing else has peak -infinity, logsum 0, entropy 0 and log p
  * -infinity; rows of the type's lowest finite value are ordinary rows of equal logits.  A row with NaN or +infinity gives
- * NaN, and top_ids -1.  rows may be 0.
+ * NaN, and top_ids -1.  Sums are float32, in an order that depends on rows, vocab, top and the type alone.  rows may be 0.
  */
 int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, int32_t type, int64_t rows, int64_t vocab,
                           const void* tokens, int32_t token_bits, float scale, float* logp_out, float* peak_out,
@@ -701,7 +702,8 @@ const char* artopk_adamw_last_error(const artopk_adamw* h);
  *   update   device, n float32: a step's update_out; update_scale 1 / W makes its sum a mean
  *   first, second, scales   device, the moments, updated in place (scales NULL with 32 bits)
  *   step     t >= 1, or 0: t is a counter on the device that this call first adds one to, for steps replayed from a graph.
- *            artopk_adamw_set_step sets it (0 in a new handle), enqueued like any call
+ *            artopk_adamw_set_step sets it (0 in a new handle), enqueued like any call.  The two powers are then taken
+ *            on the device, whose last bit may be another than the host's
  *   eta, update_scale finite; beta1, beta2 in [0, 1) (float64: 1 - beta is taken before rounding); eps > 0, finite
  *   seed     of the random rounding (8 bits)
  */

@@ -40,6 +40,8 @@ int check_device(char* err, int device) {
   return ARTOPK_OK;
 }
 
+static_assert(kMostTop == ARTOPK_MAX_TOP, "");
+
 constexpr int64_t kMostWidth = 65536;
 constexpr int64_t kMostBlocks = 1 << 20;
 
@@ -255,7 +257,7 @@ int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vo
   h->error = reinterpret_cast<int*>(h->slab + at.error);
   e = hipMemset(h->error, 0, sizeof(int));
   if (e == hipSuccess && max_tokens > kFewTokens) e = hipMemset(h->marks, 0, (size_t)max_vocab);
-  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
   if (e != hipSuccess) {
     (void)hipFree(h->slab);
     delete h;

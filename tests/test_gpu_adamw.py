@@ -29,11 +29,11 @@ def _kind(t):
     return {"f32": lib.ARTOPK_G_F32, "bf16": lib.ARTOPK_G_BF16, "f16": lib.ARTOPK_G_F16}[t]
 
 
-def _random(count, seed, step):
+def _random(count, seed, step, start=0):
     wide = (seed + step * 0x9E3779B97F4A7C15) % (1 << 64)
     key = np.uint64((wide ^ (wide >> 32)) % (1 << 32))
     m = np.uint64(0xFFFFFFFF)
-    x = (np.arange(count, dtype=np.uint64) * np.uint64(0x9E3779B1) + key) & m
+    x = (np.arange(start, start + count, dtype=np.uint64) * np.uint64(0x9E3779B1) + key) & m
     x = ((x ^ (x >> np.uint64(16))) * np.uint64(0x6A09E667)) & m
     x = ((x ^ (x >> np.uint64(15))) * np.uint64(0xBB67AE85)) & m
     return (x ^ (x >> np.uint64(16))).astype(np.int64)
@@ -305,6 +305,35 @@ def test_counted_steps_in_a_graph():
             eager.artopk_adamw_step(w2, g, *state2, step=step, seed=3)
             for a, b in zip([w, *state], [w2, *state2]):
                 assert a is None or torch.equal(a, b), (bits, step)
+
+
+def test_longest_vector():
+    """All of 2^31 - 1 elements: the last blocks' codes, and weights at the vector's end."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    n, tail = (1 << 31) - 1, 700
+    ctx = lib.AdamWContext([(0, 1000), (1000, n - 1000)], n, _kind("bf16"), 8)
+    assert ctx.state_elems == 1024 + -(-(n - 1000) // 256) * 256
+    w = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, device="cuda")
+    g[-tail:] = torch.randn(tail, generator=torch.Generator().manual_seed(1)).cuda()
+    first, second, scales = ctx.new_state()
+    ctx.artopk_adamw_step(w, g, first, second, scales, step=1, eta=0.125, seed=9)
+    # beta1 = 0.9: the first step moves a weight by eta times its gradient's sign, but for eps and roundings
+    assert torch.equal(w[-tail:], -0.125 * torch.sign(g[-tail:]).bfloat16())
+    assert not bool(w[:-tail].view(torch.int16)[::4097].any())
+    blocks = 4
+    start = ctx.state_elems - blocks * 256
+    x = np.zeros(blocks * 256, F)
+    pad = -(n - 1000) % 256
+    x[-tail - pad:len(x) - pad] = g[-tail:].cpu().numpy()
+    r = _random(blocks * 256, 9, 1, start)
+    for got, e, m, half, top in ((first, scales[-blocks:, 0], x * F(1.0 - 0.9), r & 0xFFFF, 14),
+                                 (second, scales[-blocks:, 1], (x * x) * F(1.0 - 0.999), r >> 16, 30)):
+        code, want = _encode(m, half, top)
+        assert np.array_equal(e.cpu().numpy().astype(np.int64), want[:, 0])
+        assert np.array_equal(got[-blocks * 256:].cpu().numpy().astype(np.int64).reshape(-1, 256), code)
 
 
 def test_two_handles_share_a_vector():

@@ -291,6 +291,44 @@ def test_another_stream_and_graph_replays():
         assert torch.equal(got_y, y) and torch.equal(got, grad), turn
 
 
+def test_two_graphs_of_one_handle():
+    """Two recordings share the handle's scratch; replayed in turn, with other calls between, each gives its own result."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g = _gen(13)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ctx = lib.TokenContext(20_000, 30_000, 160)
+        sets = []
+        for count, vocab in ((20_000, 30_000), (500, 90)):
+            tok = torch.randint(-1, vocab, (count,), generator=g).cuda()
+            sets.append((torch.randn(count, 160, generator=g).cuda(), tok, torch.zeros(vocab, 160).cuda()))
+        graphs = []
+        for s in sets:
+            ctx.artopk_embedding_backward(*s)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                ctx.artopk_embedding_backward(*s)
+            graphs.append(graph)
+        for turn in range(6):
+            for dy, tok, grad in sets:
+                dy.normal_()
+                grad.fill_(9.0)
+            order = (0, 1) if turn % 2 else (1, 0)
+            for i in order:
+                graphs[i].replay()
+            side.synchronize()
+            got = [s[2].clone() for s in sets]
+            for s in sets:
+                ctx.artopk_embedding_backward(*s)
+            side.synchronize()
+            for a, s in zip(got, sets):
+                assert torch.equal(a, s[2]), turn
+
+
 def test_refusals():
     import torch
     import paper_2312_02493_amd as lib
