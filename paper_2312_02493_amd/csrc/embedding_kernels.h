@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(SortKeys in, int64_
                                                              uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out,
                                                              ZeroRows zero) {
   __shared__ uint32_t base[kSortDigits];           // where the tile's next key of each digit goes
-  __shared__ uint16_t seen[kSortWaves * kSortDigits];  // keys of each digit that a wave has in this round
+  __shared__ alignas(8) uint16_t seen[kSortWaves * kSortDigits];  // keys of each digit that a wave has in this round
   __shared__ uint32_t room[kSortWaves];
   if ((int)blockIdx.x >= tiles) {
     zero_rows(zero, (int64_t)(blockIdx.x - tiles) * kSortWaves + (threadIdx.x >> 6), (int64_t)(gridDim.x - tiles) * kSortWaves);
@@ -253,22 +253,40 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(SortKeys in, int64_
   const uint32_t mask = digits - 1;
   uint16_t* mine = seen + wave * digits;
   {
-    // two digits a thread, side by side, so that the sum over threads runs over the digits in order
-    const int d = threadIdx.x * 2;
-    uint32_t all[2] = {0, 0}, before[2] = {0, 0};
-    if (d < digits) {
+    // Two digits a thread, side by side, so that the sum over threads runs over the digits in order; up to sixteen groups of
+    // threads share the tiles (one alone waits 5 us for 64 tiles' counts).
+    const int pairs = digits / 2, groups = kSortThreads / pairs < 16 ? kSortThreads / pairs : 16;
+    const int group = threadIdx.x / pairs, d = threadIdx.x % pairs * 2;
+    uint2* sums = reinterpret_cast<uint2*>(seen);  // [group][digit]: keys of all tiles, and of those before this one
+    if (group < groups) {
+      uint2 s[2] = {{0, 0}, {0, 0}};
 #pragma unroll 8
-      for (int t = 0; t < tiles; ++t)
+      for (int t = group; t < tiles; t += groups) {
+        const uint2 n = *reinterpret_cast<const uint2*>(counts + (size_t)t * digits + d);
+        s[0].x += n.x;
+        s[1].x += n.y;
+        s[0].y += t < (int)blockIdx.x ? n.x : 0;
+        s[1].y += t < (int)blockIdx.x ? n.y : 0;
+      }
+      sums[group * digits + d] = s[0];
+      sums[group * digits + d + 1] = s[1];
+    }
+    __syncthreads();
+    uint2 s[2] = {{0, 0}, {0, 0}};
+    if (group == 0)
+      for (int g = 0; g < groups; ++g)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t n = counts[(size_t)t * digits + (d + j < digits ? d + j : d)];
-          all[j] += n;
-          before[j] += t < (int)blockIdx.x ? n : 0;
+          const uint2 one = sums[g * digits + d + j];
+          s[j].x += one.x;
+          s[j].y += one.y;
         }
+    const uint32_t lower = block_before(s[0].x + s[1].x, room);
+    if (group == 0) {
+      base[d] = lower + s[0].y;
+      base[d + 1] = lower + s[0].x + s[1].y;
     }
-    const uint32_t lower = block_before(all[0] + all[1], room);
-    if (d < digits) base[d] = lower + before[0];
-    if (d + 1 < digits) base[d + 1] = lower + all[0] + before[1];
+    // (block_before has a barrier behind the reads of sums)
   }
   const int64_t lo = (int64_t)blockIdx.x * per, hi = lo + per < count ? lo + per : count;
   // A round: each wave has R times 64 keys side by side, in order.
@@ -295,12 +313,13 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(SortKeys in, int64_
     __syncthreads();
     // where each wave's keys of a digit begin
     for (int d = threadIdx.x; d < digits; d += kSortThreads) {
-      uint32_t next = 0;
+      uint32_t n[kSortWaves], next = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) n[w] = seen[w * digits + d];
 #pragma unroll
       for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t n = seen[w * digits + d];
         seen[w * digits + d] = (uint16_t)next;
-        next += n;
+        next += n[w];
       }
       seen[d] = (uint16_t)next;  // (wave 0 begins at 0 anyway: in its place how far base moves on behind this round)
     }
@@ -380,6 +399,11 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortKeys in, int coun
 __host__ __device__ constexpr int64_t part_pitch(int64_t cols) { return (cols + 3) / 4 * 4; }  // rows at sixteen bytes
 constexpr int kSumRun = 32, kSumMost = 32, kSumWaves = 8;
 
+// A heavy token: the run that it begins in, the first one without a share of it, itself.
+struct HeavyToken {
+  uint32_t run, stop, token;
+};
+
 // What run `lo / kSumRun` has to do, the same in every lane.
 struct RunItems {
   uint32_t starts;  // bit e: a token begins at place lo + e
@@ -425,7 +449,7 @@ __global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __
                                                               int64_t count, uint32_t vocab, const TD* __restrict__ dy,
                                                               int64_t dy_stride, int64_t cols, float scale, TG* __restrict__ dtable,
                                                               int64_t grad_stride, int add, float* __restrict__ part, int64_t runs,
-                                                              int split, int tiles, uint32_t* __restrict__ heavy,
+                                                              int split, int tiles, HeavyToken* __restrict__ heavy,
                                                               uint32_t* __restrict__ heavy_count, int zero_blocks,
                                                               ZeroRows zero) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -472,7 +496,19 @@ __global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __
           if (n > kSumMost) {
             e1 = it.live;
             slot = 1;
-            if (tile == 0 && lane == 0) heavy[atomicAdd(heavy_count, 1u)] = (uint32_t)run;
+            if (tile == 0) {
+              // the first place with another token: 64 places are looked at at a time, ever closer ones
+              int64_t a = lo + kSumRun, b = count;
+              while (a < b) {
+                const int64_t apart = (b - a + 63) / 64, look = a + lane * apart;
+                const int same = __popcll(__ballot(look < b && key[look < b ? look : a] == k));
+                if (same == 0) break;
+                b = a + same * apart < b ? a + same * apart : b;
+                a += (same - 1) * apart + 1;
+              }
+              if (lane == 0)
+                heavy[atomicAdd(heavy_count, 1u)] = {(uint32_t)run, (uint32_t)((a + kSumRun - 1) / kSumRun), k};
+            }
           }
         }
       }
@@ -523,10 +559,9 @@ __global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __
 
 // Heavy tokens from their list: blockIdx.y 256 columns, sixteen waves that take every sixteenth share.  Clears the marks, too.
 template <class TG>
-__global__ __launch_bounds__(1024) void k_embed_join(const uint32_t* __restrict__ key, int64_t count, uint32_t vocab,
-                                                     const float* __restrict__ part, int64_t cols, float scale,
+__global__ __launch_bounds__(1024) void k_embed_join(const float* __restrict__ part, int64_t vocab, int64_t cols, float scale,
                                                      TG* __restrict__ dtable, int64_t grad_stride, int add,
-                                                     const uint32_t* __restrict__ heavy, const uint32_t* __restrict__ heavy_count,
+                                                     const HeavyToken* __restrict__ heavy, const uint32_t* __restrict__ heavy_count,
                                                      uint8_t* __restrict__ marks) {
   __shared__ float room[16][256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -534,18 +569,8 @@ __global__ __launch_bounds__(1024) void k_embed_join(const uint32_t* __restrict_
     for (int64_t v = (int64_t)blockIdx.x * 1024 + threadIdx.x; v < vocab; v += (int64_t)gridDim.x * 1024) marks[v] = 0;
   const uint32_t n = *heavy_count;
   for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
-    const int64_t run = heavy[i], at = (run + 1) * kSumRun;
-    const uint32_t k = key[at - 1];
-    // the first place with another token: a wave looks at 64 places at a time, ever closer ones
-    int64_t a = at, b = count;
-    while (a < b) {
-      const int64_t apart = (b - a + 63) / 64, look = a + lane * apart;
-      const int same = __popcll(__ballot(look < b && key[look < b ? look : a] == k));
-      if (same == 0) break;
-      b = a + same * apart < b ? a + same * apart : b;
-      a += (same - 1) * apart + 1;
-    }
-    const int64_t stop = (a + kSumRun - 1) / kSumRun;  // runs run + 1 .. stop - 1 hold shares
+    const HeavyToken token = heavy[i];
+    const int64_t run = token.run, stop = token.stop;  // runs run + 1 .. stop - 1 hold shares
     const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4, pitch = part_pitch(cols);
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < cols) {
@@ -576,7 +601,7 @@ __global__ __launch_bounds__(1024) void k_embed_join(const uint32_t* __restrict_
       float t = room[0][threadIdx.x];
 #pragma unroll
       for (int w = 1; w < 16; ++w) t += room[w][threadIdx.x];
-      TG* to = dtable + (int64_t)k * grad_stride + mine_c;
+      TG* to = dtable + (int64_t)token.token * grad_stride + mine_c;
       *to = static_cast<TG>(add ? static_cast<float>(*to) + t * scale : t * scale);
     }
     __syncthreads();

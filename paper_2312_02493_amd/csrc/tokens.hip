@@ -25,7 +25,8 @@ struct artopk_tokens {
   uint8_t* marks = nullptr;  // rows of a table that are named; zeros between calls
   LogpPart* parts = nullptr;     // of rows that several blocks share, and their alternatives
   uint64_t* part_keys = nullptr;
-  uint32_t *heavy = nullptr, *heavy_count = nullptr;  // runs in which heavy tokens begin
+  HeavyToken* heavy = nullptr;
+  uint32_t* heavy_count = nullptr;
   int* error = nullptr;
   char err[kErrText] = {0};
 };
@@ -80,7 +81,7 @@ struct Layout {
     counts = take((size_t)kSortTiles * kSortDigits * 4);
     part = tokens > kSumMost ? take((size_t)runs_of(tokens) * 2 * (size_t)part_pitch(width) * 4) : 0;
     marks = tokens > kFewTokens ? take((size_t)vocab) : 0;
-    heavy = take((size_t)(tokens / kSumMost + 1) * 4);
+    heavy = take((size_t)(tokens / kSumMost + 1) * sizeof(HeavyToken));
     parts = take((size_t)kPartBlocks * sizeof(LogpPart));
     part_keys = take((size_t)kPartBlocks * kMostTop * 8);
     error = take(8);  // and the list's length
@@ -150,7 +151,7 @@ int sort_places(artopk_tokens* h, const Tokens& tokens, int64_t count, int64_t v
   int all = 1;
   while (vocab >> all) ++all;  // bits of 0 .. vocab, which stands for no token
   const int passes = (all + kSortBits - 1) / kSortBits;
-  const int keys = count <= 65536 ? 1 : 4;  // a thread has in a round
+  const int keys = count <= 131072 ? 1 : 4;  // a thread has in a round
   const int64_t round = kSortThreads * keys;
   const int64_t per = std::max<int64_t>(1, (count + round * kSortTiles - 1) / (round * kSortTiles)) * round;
   const int tiles = (int)((count + per - 1) / per);
@@ -252,7 +253,7 @@ int artopk_tokens_create(artopk_tokens** out, int64_t max_tokens, int64_t max_vo
   h->marks = h->slab + at.marks;
   h->parts = reinterpret_cast<LogpPart*>(h->slab + at.parts);
   h->part_keys = reinterpret_cast<uint64_t*>(h->slab + at.part_keys);
-  h->heavy = reinterpret_cast<uint32_t*>(h->slab + at.heavy);
+  h->heavy = reinterpret_cast<HeavyToken*>(h->slab + at.heavy);
   h->heavy_count = reinterpret_cast<uint32_t*>(h->slab + at.error) + 1;
   h->error = reinterpret_cast<int*>(h->slab + at.error);
   e = hipMemset(h->error, 0, sizeof(int));
@@ -374,9 +375,8 @@ int artopk_embedding_backward(artopk_tokens* h, const void* dy, int64_t dy_strid
     if (count <= kSumMost) return;
     const unsigned tiles = (unsigned)((width + 255) / 256);
     const unsigned groups = (unsigned)std::max<int64_t>(1, std::min<int64_t>(count / kSumMost, 2 * h->num_cu / tiles));
-    k_embed_join<TG><<<dim3(groups, tiles), 1024, 0, h->stream>>>(h->key[sorted], count, (uint32_t)vocab, h->part, width, scale, out,
-                                                                  grad_stride, accumulate != 0, h->heavy, h->heavy_count,
-                                                                  zero.marks ? h->marks : nullptr);
+    k_embed_join<TG><<<dim3(groups, tiles), 1024, 0, h->stream>>>(h->part, vocab, width, scale, out, grad_stride, accumulate != 0,
+                                                                  h->heavy, h->heavy_count, zero.marks ? h->marks : nullptr);
   });
   TOKENS_TRY(h, hipGetLastError());
   return ARTOPK_OK;
