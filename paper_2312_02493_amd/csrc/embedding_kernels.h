@@ -7,8 +7,8 @@
 // every row of the table has one owner that sums its places in a fixed order: no atomics on sums, the same bits every time.  Most
 // of what the gradient writes are zeros, rows of tokens that do not occur; they are written beside the sort.
 //
-// Measured: gradient of 32768 places x 2048 bfloat16 into 64000 rows of float32 (658 MB) 141 us = 4.7 TB/s, of which the sort's four
-// launches 35 (with 190 MB of zeros), the sums 96 (with the other 250 MB), heavy tokens' shares 9; lookup of 32768 x 4096, float32 to
+// Measured: gradient of 32768 places x 2048 bfloat16 into 64000 rows of float32 (658 MB) 136 us = 4.8 TB/s, of which the sort's four
+// launches 35 (with 190 MB of zeros), the sums 96 (with the other 250 MB), heavy tokens' shares 5; lookup of 32768 x 4096, float32 to
 // bfloat16, 87 us (results through the caches 95).
 #pragma once
 
