@@ -37,6 +37,15 @@ __device__ __forceinline__ T over_wave(T v, T zero, F&& f) {
   return lane_value(v, 63);
 }
 
+// f over sixteen lanes side by side, in each of them; f's order of arguments must not matter.
+template <class T, class F>
+__device__ __forceinline__ T over_sixteen(T v, F&& f) {
+  v = f(v, moved<0xb1>(v, v));   // the neighbour
+  v = f(v, moved<0x4e>(v, v));   // the other pair
+  v = f(v, moved<0x141>(v, v));  // the eight backwards, then the sixteen
+  return f(v, moved<0x140>(v, v));
+}
+
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return over_wave(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }

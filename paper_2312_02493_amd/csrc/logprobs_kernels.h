@@ -22,6 +22,7 @@
 namespace artopk {
 
 constexpr int kMostTop = 64;
+constexpr int kGroupTop = 32;    // alternatives, at most, that are bounded by groups of four threads
 constexpr int kListRoom = 1024;  // candidates for a row's alternatives that are held on chip
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -63,12 +64,7 @@ __device__ __forceinline__ float wave_largest(float v) {
 __device__ __forceinline__ float wave_total(float v) {
   return over_wave(v, 0.0f, [](float a, float b) { return a + b; });
 }
-// The largest of four lanes side by side, in each of them.
-__device__ __forceinline__ uint64_t four_max(uint64_t v) {
-  auto f = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
-  v = f(v, moved<0xb1>(v, v));  // the neighbour, then the other pair
-  return f(v, moved<0x4e>(v, v));
-}
+__device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 // A wave's share of a row: m is the largest element so far, the same in all lanes, r and u a lane's sums over its other ones
 // with exponents c x - ref.  ref is c m rounded (the same for all, so it costs nothing but its distance from c m in the end), or
@@ -237,11 +233,13 @@ struct RowEnd {
 // A team of WAVES waves (4, or 1: four teams a block) has a row, or with `split` > 1 one of as many parts of it, whose sums and
 // alternatives then go to parts and part_keys for k_logp_join.  Thread t has the part's pieces t, t + 64 WAVES, ..
 //
-// Alternatives.  Every thread notes its largest element (the first among equal ones), groups of WAVES threads the largest of
-// theirs.  The `top`-th largest of these 64 is a bound: the row's alternatives are not below it, and all lie with the threads whose
+// Alternatives.  Every thread notes its largest element (the first among equal ones), groups of threads the largest of theirs.  The
+// `top`-th largest of these n keys is a bound: the row's alternatives are not below it, and all lie with the threads whose
 // largest element reaches it (some 24 for 20).  So those threads' elements are read once more, those that reach the bound listed
-// (64 ln(64 / (64 - top)) of them in a row without an order), and a listed one's place is the number of larger ones.  Should there
-// be more than kListRoom (a row in order), the alternatives are found one after the other.
+// (n ln(n / (n - top)) of them in a row without an order), and a listed one's place is the number of larger ones.  n is 64 for up to
+// kGroupTop alternatives; more are bounded by 128, of which a comparison costs more but leaves fewer (32768 x 8000 bfloat16, 64
+// alternatives: 64 keys 632 us, 128 326).  Should there be more than kListRoom (a row in order), the alternatives are found one
+// after the other.
 struct LogpPart {
   RowSum s;
   float unused;
@@ -252,9 +250,11 @@ __global__ __launch_bounds__(256) void k_logp(
     const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, Tokens tokens, int has_tokens, float scale, float c, int top,
     LogpOut out, int split, LogpPart* __restrict__ parts, uint64_t* __restrict__ part_keys, int* __restrict__ error) {
   constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES, kBatch = 16 / V;
+  using Full = std::integral_constant<int, kBatch>;
+  using One = std::integral_constant<int, 1>;
   constexpr int kRoom = kListRoom / kTeams;
   __shared__ RowSum sums[4];
-  __shared__ uint64_t keys[TOP ? kTeams * 64 : 1], lists[TOP ? kListRoom : 1], bests[4];
+  __shared__ uint64_t keys[TOP ? 256 : 1], lists[TOP ? kListRoom : 1], bests[4];
   __shared__ uint8_t chosens[TOP ? 256 : 1];
   __shared__ uint64_t bounds[kTeams];
   __shared__ int list_counts[kTeams], chosen_counts[kTeams];
@@ -271,6 +271,7 @@ __global__ __launch_bounds__(256) void k_logp(
     const int q0 = split == 1 ? 0 : (int)((int64_t)p.count * part / split);
     const int q1 = split == 1 ? p.count : (int)((int64_t)p.count * (part + 1) / split);
     const int64_t tok = has_tokens && split == 1 ? tokens[row] : -1;
+    const int group = WAVES == 1 ? 0 : top <= kGroupTop ? 2 : q1 - q0 >= NT ? 1 : 0;  // of so many threads' logarithm
     Gather g;
     // the thread's largest element, and the first piece that has it: to begin with its first piece
     float own = -INFINITY;
@@ -281,20 +282,21 @@ __global__ __launch_bounds__(256) void k_logp(
         where = j;
       }
     };
-    auto batch = [&](int j, bool all) {  // pieces j, j + NT, ..; with `all` they are all there and whole
-      Some<T, V> raw[kBatch];
+    auto batch = [&](auto pieces, int j, bool all) {  // pieces j, j + NT, ..; with `all` they are all there and whole
+      constexpr int N = pieces();
+      Some<T, V> raw[N];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) p.template ask<!TOP>(raw[i], all || j + i * NT < q1 ? j + i * NT : q1 - 1, all);
+      for (int i = 0; i < N; ++i) p.template ask<!TOP>(raw[i], all || j + i * NT < q1 ? j + i * NT : q1 - 1, all);
       __builtin_amdgcn_sched_barrier(0);  // (all loads go out before one is waited for)
-      float v[kBatch * V], most[kBatch];
+      float v[N * V], most[N];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
+      for (int i = 0; i < N; ++i) {
         const bool there = all || j + i * NT < q1;
         p.take(v + i * V, raw[i], there ? j + i * NT : p.count, all);
         most[i] = largest<V>(v + i * V);
         if (there) note(most[i], j + i * NT);
       }
-      g.add<kBatch * V>(v, largest<kBatch>(most), c);
+      g.add<N * V>(v, largest<N>(most), c);
     };
     // (the same for all lanes: full batches of whole pieces begin up to here)
     const int last = (q1 * (int64_t)V <= cols ? q1 : q1 - 1) - kBatch * NT;
@@ -306,17 +308,23 @@ __global__ __launch_bounds__(256) void k_logp(
       g.add<V>(v, most, c);
     }
     int j = q0 + t, base = cols < V ? q1 : q0;
-    for (; base <= last; base += kBatch * NT, j += kBatch * NT) batch(j, true);
-    for (; base + team_wave * 64 < q1; base += kBatch * NT, j += kBatch * NT) batch(j, false);
+    for (; base <= last; base += kBatch * NT, j += kBatch * NT) batch(Full(), j, true);
+    for (; base + NT < q1; base += kBatch * NT, j += kBatch * NT) batch(Full(), j, false);
+    if (base + team_wave * 64 < q1) batch(One(), j, false);
     // (read behind the row, of which it is a part, and needed behind the sums)
     const float xt = tok >= 0 && tok < cols ? static_cast<float>(p.row[tok]) : 0.0f;
     RowSum s = g.total(c);
     // a thread's key: its largest element, the lower place first; 0 where it has none
     const uint64_t own_key = where < 0 ? 0 : (uint64_t)ordered(own) << 32 | (uint32_t)~where;
     if (TOP) {
-      const uint64_t key = WAVES == 4 ? four_max(own_key) : own_key;
-      if (t % WAVES == 0) keys[team * 64 + t / WAVES] = key;
-      if (t == 0) list_counts[team] = chosen_counts[team] = 0;
+      uint64_t key = own_key;
+      if (group >= 1) key = larger(key, moved<0xb1>(key, key));  // of the neighbour
+      if (group == 2) key = larger(key, moved<0x4e>(key, key));  // of the other pair
+      if ((t & ((1 << group) - 1)) == 0) keys[team * NT + (t >> group)] = key;
+      if (t == 0) {
+        list_counts[team] = chosen_counts[team] = 0;
+        bounds[team] = 0;
+      }
     }
     if constexpr (WAVES > 1) {
       if (lane == 0) sums[wave] = s;
@@ -340,12 +348,20 @@ __global__ __launch_bounds__(256) void k_logp(
       };
       uint64_t* list = lists + team * kRoom;
       uint8_t* chosen = chosens + team * NT;
-      if (team_wave == 0) {  // the bound
-        const uint64_t key = keys[team * 64 + lane];
+      const int some = group ? NT >> group : q1 - q0 < NT ? q1 - q0 : NT;  // keys
+      if (team_wave * 64 < some) {  // the bound; 0 where there are fewer keys
+        const uint64_t* all = keys + team * NT;
+        const uint64_t key = all[t];
         int rank = 0;
+        int i = 0;
+        for (; i + 64 <= some; i += 64) {
 #pragma unroll 16
-        for (int i = 0; i < 64; ++i) rank += keys[team * 64 + i] > key;
-        if (lane == 0 && __popcll(__ballot(key != 0)) < top) bounds[team] = 0;
+          for (int k = 0; k < 64; ++k) rank += all[i + k] > key;
+        }
+        for (; i < some; i += 16) {  // (keys behind the last are 0)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) rank += all[i + k] > key;
+        }
         if (key != 0 && rank == top - 1) bounds[team] = key;
       }
       if (end.broken || split > 1)
@@ -415,6 +431,86 @@ __global__ __launch_bounds__(256) void k_logp(
   }
 }
 
+// Narrow rows: sixteen lanes have a row, each of them N of its pieces, which stay in registers.  All elements equal to the largest
+// are counted, one of them stays out of the sum.  Alternatives are found one after the other.  What bounds it is a row's own
+// instructions, reductions and ends, which four rows share: 32768 x 130 bfloat16 9.1 us (a wave a row 26.4), 5 alternatives 17.9
+// (53.2), 32768 x 512 float32 16.6 (27.7); 32768 x 1000 bfloat16 25.3 (28.1), x 1024 float32 31.6 (28.6).
+template <class T, int N, bool TOP>
+__global__ __launch_bounds__(256) void k_logp_narrow(const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols, Tokens tokens,
+                                                     int has_tokens, float scale, float c, int top, LogpOut out,
+                                                     int* __restrict__ error) {
+  constexpr int V = RowRun<T>::V, E = N * V;
+  const int lane = threadIdx.x & 15;
+  for (int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); row < rows; row += (int64_t)gridDim.x * 16) {
+    const RowRun<T> p(x + row * x_stride, cols);
+    const int64_t tok = has_tokens ? tokens[row] : -1;
+    float v[E];
+    if (cols < V) {
+#pragma unroll
+      for (int i = 1; i < N; ++i) p.take_short(v + i * V, false);
+      p.take_short(v, lane == 0);
+    } else {
+      Some<T, V> raw[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) p.template ask<true>(raw[i], lane + i * 16 < p.count ? lane + i * 16 : p.count - 1, false);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) p.take(v + i * V, raw[i], lane + i * 16, false);
+    }
+    const float xt = tok >= 0 && tok < cols ? static_cast<float>(p.row[tok]) : 0.0f;
+    RowSum s;
+    s.m = over_sixteen(largest<E>(v), [](float a, float b) { return fmaxf(a, b); });
+    const float peak = s.m > -INFINITY ? s.m : 0.0f;
+    float r[4] = {}, u[4] = {}, equal = 0.0f;  // (sums side by side)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float d = (v[e] - peak) * c;
+      const bool same = v[e] == s.m;
+      const float f = same ? 0.0f : pow2(d);  // (NaN stays NaN)
+      r[e % 4] += f;
+      u[e % 4] = fmaf(f, fmaxf(d, -200.0f), u[e % 4]);
+      equal += same ? 1.0f : 0.0f;
+    }
+    auto plus = [](float a, float b) { return a + b; };
+    s.r = over_sixteen((r[0] + r[1]) + (r[2] + r[3]), plus);
+    s.u = over_sixteen((u[0] + u[1]) + (u[2] + u[3]), plus);
+    if (s.m > -INFINITY) s.r += over_sixteen(equal, plus) - 1.0f;
+    const RowEnd end(s, scale);
+    if (lane == 0) {
+      end.put(out, row, tok, cols, xt);
+      if (tok >= cols) *error = 1;
+    }
+    if constexpr (TOP) {
+      uint32_t o[E];  // 0: not there, or taken
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int j = lane + e / V * 16;
+        const int64_t at = p.begin(j) + e % V;
+        o[e] = j < p.count && at >= (int64_t)j * V && at < cols ? ordered(v[e]) : 0;
+      }
+      uint64_t kept = 0;
+      for (int a = 0; a < top; ++a) {
+        uint32_t most = o[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) most = o[e] > most ? o[e] : most;
+        most = over_sixteen(most, [](uint32_t f, uint32_t g) { return f > g ? f : g; });
+        int own = E;  // the lane's first one
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e) own = o[e] == most ? e : own;
+        const uint32_t at = own < E ? (uint32_t)p.begin(lane + own / V * 16) + own % V : 0xffffffffu;
+        const uint32_t first = over_sixteen(at, [](uint32_t f, uint32_t g) { return f < g ? f : g; });
+        if (at != first) own = E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = e == own ? 0 : o[e];
+        if ((a & 15) == lane) kept = (uint64_t)most << 32 | (uint32_t)~first;
+        if ((a & 15) == 15 || a == top - 1) {
+          if (lane <= (a & 15)) end.put_top(out, row * top + (a & ~15) + lane, kept);
+        }
+      }
+    }
+  }
+}
+
 // Parts of rows put together: sums by lane, alternatives from the parts' lists, which are in order, one after the other.  One wave
 // works, the others help it to read the lists.
 __global__ __launch_bounds__(1024) void k_logp_join(const LogpPart* __restrict__ parts, const uint64_t* __restrict__ part_keys, int split,
@@ -476,18 +572,20 @@ struct LogpGrads {
   const float *peak, *logsum, *entropy, *dlogp, *dlse, *dentropy;  // rows each; dlogp, dlse, and entropy with dentropy may be NULL
 };
 
-// Four pieces of a row a thread: of one row a block (a row has `tiles` blocks), or with WAVES = 1, for short rows, of one row a
-// wave.  dx may be x itself: a thread reads its elements before it writes them.  It goes past the caches, which it
-// would only fill (8192 x 128000 bfloat16 722 us, so 707); x is better left to them (2047 x 10007 float16 26 us past them, so 19).
-template <class T, bool SAME, int WAVES>  // SAME: dx's rows lie within sixteen bytes as x's do
+// Four pieces of a row a thread: of one row a block (a row has `tiles` blocks), or for short rows of one row a wave or
+// sixteen lanes (32768 x 130 bfloat16 a wave a row 27.5 us, so 15.1).  dx may be x itself: a thread reads its elements before it
+// writes them.  It goes past the caches, which it would only fill (8192 x 128000 bfloat16 722 us, so 707); x is better left to them
+// (2047 x 10007 float16 26 us past them, so 19).
+template <class T, bool SAME, int LANES>  // SAME: dx's rows lie within sixteen bytes as x's do
 __global__ __launch_bounds__(256) void k_logp_backward(const T* x, int64_t x_stride, int64_t rows, int cols, Tokens tokens,
                                                        int has_tokens, float scale, float c, LogpGrads in, T* dx,
                                                        int64_t dx_stride, int64_t units, int tiles, int* error) {
-  constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES;
-  const int t = threadIdx.x % NT, team = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  constexpr int V = RowPieces<T>::V, kTeams = 256 / LANES;
+  const int t = threadIdx.x % LANES;
+  const int team = LANES == 256 ? 0 : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / LANES;
   for (int64_t unit = (int64_t)blockIdx.x * kTeams + team; unit < units; unit += (int64_t)gridDim.x * kTeams) {
-    const int64_t row = WAVES == 1 ? unit : unit / tiles;
-    const int tile = WAVES == 1 ? 0 : (int)(unit % tiles);
+    const int64_t row = LANES < 256 ? unit : unit / tiles;
+    const int tile = LANES < 256 ? 0 : (int)(unit % tiles);
     const RowPieces<T> p(x + row * x_stride, cols);
     T* out = dx + row * dx_stride;
     int64_t tok = has_tokens ? tokens[row] : -1;
@@ -525,7 +623,7 @@ __global__ __launch_bounds__(256) void k_logp_backward(const T* x, int64_t x_str
     };
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int j = (tile * 4 + u) * NT + t;
+      const int j = (tile * 4 + u) * LANES + t;
       if (j >= p.count) continue;
       float v[V];
       if (p.is_whole(j)) {

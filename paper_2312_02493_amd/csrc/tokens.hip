@@ -54,7 +54,7 @@ constexpr int64_t kMostBlocks = 1 << 20;
                        __LINE__);                                                                              \
   } while (0)
 
-constexpr int64_t kShortRow = 2048, kLongerRow = 16384, kManyRows = 2048;
+constexpr int64_t kNarrowRow = 512, kSomeTop = 56, kShortRow = 2048, kLongerRow = 16384, kManyRows = 2048;
 constexpr int64_t kPartBlocks = 1024;  // that parts of rows make, at most
 constexpr int64_t kFewTokens = 8192, kFewTokensAlone = 14336;  // (at most what LDS holds beside the counts, 14336 keys)
 
@@ -423,10 +423,28 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
     const T* at = static_cast<const T*>(logits);
     const float c = scale * kLog2e;
     const int has_tokens = logp_out != nullptr;
-    // Short rows a wave each.  Few long ones in parts, as many as keep every compute unit busy, from sixteen pieces a thread on, where
+    // Narrow rows four a wave, but some alternatives of 257 to 512 columns, which come faster all at once (8192 x 512 bfloat16: 8 14.3 us
+    // and 17.3, 20 22.9 and 18.4, 57 48.8 and 34.7, 64 54 and 165).
+    if (vocab <= kNarrowRow / 2 || (vocab <= kNarrowRow && (top <= 8 || top > kSomeTop))) {
+      const unsigned blocks = (unsigned)std::min<int64_t>((rows + 15) / 16, kMostBlocks);
+      auto go = [&](auto PIECES, auto TOP) {
+        k_logp_narrow<T, PIECES(), TOP()><<<blocks, 256, 0, h->stream>>>(at, stride, rows, (int)vocab, tok, has_tokens, scale, c, top, out,
+                                                                         h->error);
+      };
+      auto with_top = [&](auto PIECES) {
+        if (top) go(PIECES, std::true_type());
+        else go(PIECES, std::false_type());
+      };
+      if (vocab <= 128) with_top(std::integral_constant<int, 8 / V>());
+      else if (vocab <= 256) with_top(std::integral_constant<int, 16 / V>());
+      else with_top(std::integral_constant<int, 32 / V>());
+      return;
+    }
+    // Short rows a wave each, unless its 64 keys bound the alternatives badly (32768 x 1000 bfloat16: 50 93 us, 64 1020, by four
+    // waves 216).  Few long ones in parts, as many as keep every compute unit busy, from sixteen pieces a thread on, where
     // that saves more than the second launch costs: 8 x 40000 bfloat16 14.3 us, so 11.1, 8 x 20000 8.1 and 11.3; 300 x 128000 36 and 25,
     // 400 x 100000 float32 33 and 35.
-    const bool short_rows = vocab <= kShortRow || (vocab <= kLongerRow && rows >= kManyRows);
+    const bool short_rows = top <= kSomeTop && (vocab <= kShortRow || (vocab <= kLongerRow && rows >= kManyRows));
     int split = 1;
     if (!short_rows && rows * 3 <= kPartBlocks && vocab / V / 256 >= 16)
       split = (int)std::max<int64_t>(1, std::min<int64_t>({64, kPartBlocks / rows, vocab / V / 256}));
@@ -493,21 +511,22 @@ int artopk_token_logprobs_backward(artopk_tokens* h, const void* logits, int64_t
     // at most, wherever rows begin
     const bool whole = vocab % V == 0 && aligned16(logits) && (rows <= 1 || stride % V == 0);
     const int64_t pieces = whole ? vocab / V : (vocab + 2 * (V - 1)) / V;
-    const bool short_rows = pieces <= 256;
-    const int tiles = short_rows ? 1 : (int)((pieces + 1023) / 1024);
+    const int lanes = pieces <= 64 ? 16 : pieces <= 256 ? 64 : 256;
+    const int tiles = lanes < 256 ? 1 : (int)((pieces + 1023) / 1024);
     const int64_t units = rows * tiles;
-    const unsigned blocks = (unsigned)std::min<int64_t>(short_rows ? (rows + 3) / 4 : units, kMostBlocks);
-    auto go = [&](auto SAME, auto WAVES) {
-      k_logp_backward<T, SAME(), WAVES()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok,
+    const unsigned blocks = (unsigned)std::min<int64_t>((units * lanes + 255) / 256, kMostBlocks);
+    auto go = [&](auto SAME, auto LANES) {
+      k_logp_backward<T, SAME(), LANES()><<<blocks, 256, 0, h->stream>>>(static_cast<const T*>(logits), stride, rows, (int)vocab, tok,
                                                                          dlogp != nullptr, scale, scale * kLog2e, in,
                                                                          static_cast<T*>(dlogits), dstride, units, tiles, h->error);
     };
-    auto with_waves = [&](auto SAME) {
-      if (short_rows) go(SAME, std::integral_constant<int, 1>());
-      else go(SAME, std::integral_constant<int, 4>());
+    auto with_lanes = [&](auto SAME) {
+      if (lanes == 16) go(SAME, std::integral_constant<int, 16>());
+      else if (lanes == 64) go(SAME, std::integral_constant<int, 64>());
+      else go(SAME, std::integral_constant<int, 256>());
     };
-    if (same) with_waves(std::true_type());
-    else with_waves(std::false_type());
+    if (same) with_lanes(std::true_type());
+    else with_lanes(std::false_type());
   });
   TOKENS_TRY(h, hipGetLastError());
   return ARTOPK_OK;

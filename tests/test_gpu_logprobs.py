@@ -207,6 +207,21 @@ def test_forward_few_long_rows(rows, kind):
     _check_forward(rows, 200_000, "f32", kind, 33, seed=rows + 9)
 
 
+@pytest.mark.parametrize("vocab", [1, 2, 5, 16, 17, 63, 127, 128, 129, 130, 255, 256, 257, 400, 511, 512, 513])
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_forward_narrow_rows(vocab, t):
+    for kind in KINDS:
+        for top in sorted({min(vocab, n) for n in (1, 8, 9, 17, 56, 57, 64)}):
+            _check_forward(19, vocab, t, kind, top, pad=vocab % 3, shift=vocab % 2, seed=vocab)
+
+
+@pytest.mark.parametrize("vocab", [514, 1000, 1024, 1025, 2047, 2056, 4103, 8200, 33000])
+@pytest.mark.parametrize("kind", ["plain", "rising", "masked", "equal", "few"])
+def test_forward_most_alternatives(vocab, kind):
+    for t, rows, top in (("bf16", 3, 64), ("f32", 3, 33), ("f16", 345, 57)):
+        _check_forward(rows, vocab, t, kind, top, pad=1, seed=vocab)
+
+
 def test_forward_many_rows():
     _check_forward(5000, 257, "bf16", "plain", 3, pad=1)
     _check_forward(70_000, 12, "f16", "few", 2)
@@ -324,6 +339,16 @@ def test_backward_kinds(kind, t):
 def test_backward_parts(which):
     _check_backward(9, 1001, "f32", "masked", which=which)
     _check_backward(9, 1001, "bf16", "plain", which=which)
+
+
+@pytest.mark.parametrize("vocab", [1, 15, 57, 63, 129, 250, 256, 257, 504, 505, 512, 513])
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_backward_narrow_rows(vocab, t):
+    for kind in ("plain", "masked", "sure"):
+        for shift, dshift in ((0, 0), (1, 1), (3, 4)):
+            _check_backward(37, vocab, t, kind, pad=shift, shift=shift, dpad=dshift, dshift=dshift, seed=vocab)
+            if shift == dshift:
+                _check_backward(37, vocab, t, kind, pad=shift, shift=shift, seed=vocab, in_place=True)
 
 
 def test_backward_many_rows():
