@@ -196,7 +196,10 @@ void embed_sums(artopk_tokens* h, const uint32_t* key, const uint32_t* pos, int6
                 int64_t dy_stride, int64_t cols, float scale, TG* dtable, int64_t grad_stride, int add, const ZeroRows& zero) {
   const int tiles = (int)((cols + 64 * V - 1) / (64 * V));
   const int64_t rows = zero.at ? std::max<int64_t>(0, zero.end - zero.begin) : 0;
-  const int zeros = (int)std::min<int64_t>((rows * zero.bytes + kZeroShare - 1) / kZeroShare, 16384);
+  // (of narrow rows two rounds of the block's lanes: looking up whether a row is named takes longer than its zeros:
+  // 500 tokens, 131072 rows of 4 bytes 62 us, so 14)
+  const int64_t each = std::min<int64_t>(std::max<int64_t>(1, kZeroShare / std::max(1, zero.bytes)), 2 * kSumWaves * (64 >> zero.lg));
+  const int zeros = (int)std::min<int64_t>((rows + each - 1) / each, 16384);
   const int64_t runs = runs_of(count);
   // as many blocks to a run as its tokens and column tiles can occupy, until there are enough of them
   const int most = (kSumRun / 4 * tiles + kSumWaves - 1) / kSumWaves;
@@ -424,8 +427,9 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
     const float c = scale * kLog2e;
     const int has_tokens = logp_out != nullptr;
     // Narrow rows four a wave, but some alternatives of 257 to 512 columns, which come faster all at once (8192 x 512 bfloat16: 8 14.3 us
-    // and 17.3, 20 22.9 and 18.4, 57 48.8 and 34.7, 64 54 and 165).
-    if (vocab <= kNarrowRow / 2 || (vocab <= kNarrowRow && (top <= 8 || top > kSomeTop))) {
+    // and 17.3, 20 22.9 and 18.4, 57 48.8 and 34.7, 64 54 and 165) as long as the wave has keys
+    // enough to bound them (8192 x 257, 48 with 33 keys: 42.6 and 161).
+    if (vocab <= kNarrowRow / 2 || (vocab <= kNarrowRow && (top <= 8 || top > std::min(kSomeTop, vocab / V * 15 / 16)))) {
       const unsigned blocks = (unsigned)std::min<int64_t>((rows + 15) / 16, kMostBlocks);
       auto go = [&](auto PIECES, auto TOP) {
         k_logp_narrow<T, PIECES(), TOP()><<<blocks, 256, 0, h->stream>>>(at, stride, rows, (int)vocab, tok, has_tokens, scale, c, top, out,

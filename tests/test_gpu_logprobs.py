@@ -222,6 +222,13 @@ def test_forward_most_alternatives(vocab, kind):
         _check_forward(rows, vocab, t, kind, top, pad=1, seed=vocab)
 
 
+@pytest.mark.parametrize("vocab", [257, 264, 400, 448])
+def test_forward_alternatives_next_to_a_waves_keys(vocab):
+    for top in (31, 32, 33, 34, 49, 50, 51, 55):
+        for kind in ("plain", "few", "masked"):
+            _check_forward(13, vocab, "bf16", kind, top, seed=top)
+
+
 def test_forward_many_rows():
     _check_forward(5000, 257, "bf16", "plain", 3, pad=1)
     _check_forward(70_000, 12, "f16", "few", 2)
