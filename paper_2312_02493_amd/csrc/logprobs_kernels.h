@@ -23,7 +23,10 @@ namespace artopk {
 
 constexpr int kMostTop = 64;
 constexpr int kGroupTop = 32;    // alternatives, at most, that are bounded by groups of four threads
-constexpr int kListRoom = 1024;  // candidates for a row's alternatives that are held on chip
+// Candidates for a row's alternatives that are held on chip.  In a row of equal elements (or one with fewer than `top` others left) the
+// bound is an element of the last of `top` keys' pieces, so all before it are candidates, and the larger ones: up to 128 pieces of 8
+// and 64 more with four waves, 56 pieces with one.
+constexpr int kListRoom = 128 * 8 + 64, kWaveRoom = 56 * 8 + 64;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float pow2(float v) { return __builtin_amdgcn_exp2f(v); }  // (0 below the normal range)
@@ -238,7 +241,7 @@ struct RowEnd {
 // largest element reaches it (some 24 for 20).  So those threads' elements are read once more, those that reach the bound listed
 // (n ln(n / (n - top)) of them in a row without an order), and a listed one's place is the number of larger ones.  n is 64 for up to
 // kGroupTop alternatives; more are bounded by 128, of which a comparison costs more but leaves fewer (32768 x 8000 bfloat16, 64
-// alternatives: 64 keys 632 us, 128 326).  Should there be more than kListRoom (a row in order), the alternatives are found one
+// alternatives: 64 keys 632 us, 128 326).  Should there be more than there is room for, the alternatives are found one
 // after the other.
 struct LogpPart {
   RowSum s;
@@ -252,9 +255,9 @@ __global__ __launch_bounds__(256) void k_logp(
   constexpr int V = RowPieces<T>::V, kTeams = 4 / WAVES, NT = 64 * WAVES, kBatch = 16 / V;
   using Full = std::integral_constant<int, kBatch>;
   using One = std::integral_constant<int, 1>;
-  constexpr int kRoom = kListRoom / kTeams;
+  constexpr int kRoom = WAVES == 1 ? kWaveRoom : kListRoom;
   __shared__ RowSum sums[4];
-  __shared__ uint64_t keys[TOP ? 256 : 1], lists[TOP ? kListRoom : 1], bests[4];
+  __shared__ uint64_t keys[TOP ? 256 : 1], lists[TOP ? kTeams * kRoom : 1], bests[4];
   __shared__ uint8_t chosens[TOP ? 256 : 1];
   __shared__ uint64_t bounds[kTeams];
   __shared__ int list_counts[kTeams], chosen_counts[kTeams];

@@ -229,6 +229,29 @@ def test_forward_alternatives_next_to_a_waves_keys(vocab):
             _check_forward(13, vocab, "bf16", kind, top, seed=top)
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [700, 2048, 5000, 40000])
+def test_forward_alternatives_of_rows_with_little_left(t, vocab):
+    """Fewer elements above the others than alternatives: the rest are ties."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g, rows = _gen(vocab), 7
+    for left in (0, 1, 10, 31, 55, 63):
+        for rest in (-math.inf, -2.0):
+            x = torch.full((rows, vocab), rest)
+            at = torch.rand(rows, vocab, generator=g).argsort(1)[:, :left]
+            x.scatter_(1, at, torch.randn(rows, left, generator=g).abs())
+            x = x.to(_dtype(t))
+            for top in (20, 32, 33, 56, 64):
+                ids = torch.empty(rows, top, dtype=torch.int32, device="cuda")
+                lps = torch.empty(rows, top, device="cuda")
+                ctx = lib.TokenContext(rows, vocab)
+                ctx.artopk_token_logprobs(x.cuda(), top_ids_out=ids, top_logp_out=lps)
+                order = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :top]
+                assert torch.equal(ids.cpu().long(), order), (left, rest, top)
+
+
 def test_forward_many_rows():
     _check_forward(5000, 257, "bf16", "plain", 3, pad=1)
     _check_forward(70_000, 12, "f16", "few", 2)
