@@ -70,11 +70,15 @@ __device__ __forceinline__ float wave_total(float v) {
 __device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 // A wave's share of a row: m is the largest element so far, the same in all lanes, r and u a lane's sums over its other ones
-// with exponents c x - ref.  ref is c m rounded (the same for all, so it costs nothing but its distance from c m in the end), or
-// with c m near float32's end exponents are c (x - m).
+// with exponents c x - ref.  ref is c m rounded (the same for all, so it costs nothing but its distance from c m in the end).  That
+// distance is half a step of float32 at c m: at most 1/2 below kNear, but it grows with c m, and from 2^31 on two to its power is
+// no float32 any more.  So from kNear on exponents are c (x - m), one more operation an element.
 struct Gather {
+  static constexpr float kNear = 0x1p24f;
   float m = -INFINITY, ref = 0.0f, r = 0.0f, u = 0.0f;
   bool far = false;
+  // c m less what exponents are relative to, exact
+  __device__ __forceinline__ float apart(float c) const { return far ? 0.0f : fmaf(m, c, -ref); }
   __device__ __forceinline__ float exponent(float x, float c) const { return far ? (x - m) * c : fmaf(x, c, -ref); }
   // N elements a lane, `top` their largest; all lanes of the wave call it together
   template <int N>
@@ -114,14 +118,15 @@ struct Gather {
     const int owner = __ffsll((unsigned long long)__ballot(top == to)) - 1;
     bool mine = (int)(threadIdx.x & 63) == owner;
     const bool was_far = far;
-    far = !(fabsf(next) < 0x1p120f);
+    const float step = next - ref, was_apart = apart(c);
+    far = !(fabsf(next) < kNear);
+    m = to;
+    ref = next;
     if (before > -INFINITY) {
-      const float d = fminf(far || was_far ? (to - before) * c : next - ref, 200.0f), f = pow2(-d);
+      const float d = fminf(far || was_far ? (to - before) * c + (was_apart - apart(c)) : step, 200.0f), f = pow2(-d);
       u = (u - r * d) * f;
       r *= f;
     }
-    m = to;
-    ref = next;
     if (mine && before > -INFINITY) {
       const float d = fmaxf(exponent(before, c), -200.0f), e = pow2(d);
       r += e;
@@ -139,7 +144,7 @@ struct Gather {
   // over the wave
   __device__ __forceinline__ RowSum total(float c) const {
     if (!(m > -INFINITY)) return {m, wave_total(r), 0.0f};  // (r may be NaN)
-    const float d = far ? 0.0f : fmaf(m, c, -ref), f = pow2(-d);
+    const float d = apart(c), f = pow2(-d);
     return {m, wave_total(r * f), wave_total((u - r * d) * f)};
   }
 };
