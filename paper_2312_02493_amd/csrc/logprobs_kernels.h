@@ -222,7 +222,9 @@ struct RowEnd {
     log = log1pf(s.r);
   }
   __device__ __forceinline__ float logp(float x) const {
-    return broken ? __builtin_nanf("") : none ? -INFINITY : (x - s.m) * scale - log;
+    const float apart = x - s.m;  // (or beyond float32, where its product with scale may not be)
+    const float d = apart == -INFINITY && x > -INFINITY ? x * scale - s.m * scale : apart * scale;
+    return broken ? __builtin_nanf("") : none ? -INFINITY : d - log;
   }
   __device__ __forceinline__ void put(const LogpOut& out, int64_t row, int64_t tok, int cols, float xt) const {
     const float nan = __builtin_nanf("");

@@ -38,13 +38,15 @@ def _check(x, t, top, scale=1.0):
     assert torch.equal(peak.cpu().double(), ref.peak.view(-1))
     _near(logsum, ref.logsum, ref.tol_logsum, "logsum")
     _near(entropy, ref.entropy, ref.tol_entropy, "entropy")
+    # (log p beyond float32 is -infinity there)
+    below = lambda v: torch.where(v <= -(2.0 ** 128), torch.full_like(v, -math.inf), v)
     d = ref.d.gather(1, tok.view(-1, 1))
-    _near(logp, (d - ref.logsum.view(-1, 1)).view(-1), ref.tol_logp(d).view(-1), "logp")
+    _near(logp, below(d - ref.logsum.view(-1, 1)).view(-1), ref.tol_logp(d).view(-1), "logp")
     if top:
         order = torch.sort(x.float() + 0.0, dim=1, descending=True, stable=True).indices[:, :top]
         assert torch.equal(ids.cpu().long(), order)
         d = ref.d.gather(1, order)
-        _near(lps, d - ref.logsum.view(-1, 1), ref.tol_logp(d), "top_logp")
+        _near(lps, below(d - ref.logsum.view(-1, 1)), ref.tol_logp(d), "top_logp")
 
 
 def _rows(rows, vocab, kind, far, seed=5):
@@ -110,3 +112,53 @@ def test_low_and_high_temperatures(rows, vocab, t):
         _check(torch.full_like(x, 10.0), t, 5, scale)
     for size in (1e9, 1e20, 1e30):  # (ordinary logits, once they are scaled)
         _check(x * size, t, 5, 1.0 / size)
+
+
+LEAST = 2.0 ** -120
+
+
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_differences_beyond_float32(rows, vocab, t):
+    """Logits at both ends of float32: their difference is not in it, scaled it is."""
+    import torch
+
+    g = torch.Generator().manual_seed(13)
+    x = 3e38 * (2.0 * torch.rand(rows, vocab, generator=g) - 1.0)
+    x[:, 5], x[:, 7] = 3.2e38, -3.2e38
+    for scale in (LEAST, 1e-30, 1e-3, 0.4):
+        _check(x, t, 5, scale)
+        y = torch.full_like(x, -3.2e38)
+        y[:, -3:] = 3.1e38
+        _check(y, t, 5, scale)
+
+
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_gradient_of_rows_far_from_zero(rows, vocab):
+    """dlogits = scale dlogp ([index = token] - p): p is off by (6 |d| + 20) u of itself and its sum's share, the product by 4 u."""
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g = torch.Generator().manual_seed(14)
+    for scale, far in ((1.0, 1e10), (1.0, -1e10), (1e9, 10.0), (1e-3, 3e38), (LEAST, 3e38)):
+        for kind in ("equal", "peak", "half", "ends"):
+            x = _rows(rows, vocab, kind, far)
+            if kind == "ends":
+                x = far * (2.0 * torch.rand(rows, vocab, generator=g) - 1.0)
+            tok = torch.randint(0, vocab, (rows,), generator=g)
+            s = float(np.float32(scale))
+            d = s * (x.double() - x.double().amax(1, keepdim=True))
+            logsum = torch.logsumexp(d, 1)
+            out = [torch.empty(rows, device="cuda") for _ in range(2)]
+            dx, one = torch.empty(rows, vocab, device="cuda"), torch.ones(rows, device="cuda")
+            ctx = lib.TokenContext(rows, vocab)
+            ctx.artopk_token_logprobs(x.cuda(), None, None, *out, scale=scale)
+            ctx.artopk_token_logprobs_backward(x.cuda(), tok.cuda(), *out, dx, dlogp=one, scale=scale)
+            lp = d - logsum.view(-1, 1)
+            want = -torch.exp(lp)
+            want[torch.arange(rows), tok] = -torch.expm1(lp[torch.arange(rows), tok])
+            depth = 20.0 + 8.0 * (vocab / 2048 + 2) + 44 + 8 * (vocab / 1024 + 4)
+            tol = s * U * torch.exp(lp) * (6.0 * d.abs().clamp(max=1e4) + 4.0 * logsum.view(-1, 1) + depth) + 4.0 * U * s * want.abs()
+            got = dx.cpu().double()
+            bad = (got - s * want).abs() > tol + 2.0 ** -126 * (1.0 + s)
+            assert not bool(bad.any()), (scale, far, kind, got[bad][:4], (s * want)[bad][:4])
