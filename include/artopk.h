@@ -631,7 +631,7 @@ int artopk_embedding_backward(artopk_tokens* h, const void* dy, int64_t dy_strid
  *   logp = log p[tokens[row]],  entropy = -sum p log p.          (log sum e^(scale x) is scale peak + logsum)
  *   logits   device, `rows` rows of vocab elements of `type`, `stride` apart
  *   tokens   device, `rows`, or NULL where logp_out is NULL; logp is 0 where there is no token
- *   scale    finite, > 0; a log p beyond float32 is -infinity
+ *   scale    from 2^-120 to 2^127; a log p beyond float32 is -infinity
  *   logp_out, peak_out, logsum_out, entropy_out   device, `rows` float32 each, or NULL
  *   top      0 .. ARTOPK_MAX_TOP, at most vocab: how many of the row's largest elements to give, in descending order, the
  *            lower index first among equal ones (-0 equals +0)

@@ -110,6 +110,13 @@ int check_scale(artopk_tokens* h, float scale) {
   return ARTOPK_OK;
 }
 
+// Of log probabilities.  Below 2^-120 an element counts though its difference from the row's peak may be beyond float32 (2^128 scaled
+// is at least 256 otherwise, and e^-256 is zero there); above 2^127, scale log2(e) may be.
+int check_logp_scale(artopk_tokens* h, float scale) {
+  if (!(scale >= 0x1p-120f && scale <= 0x1p127f)) return fail_text(h->err, ARTOPK_EINVAL, "scale=%g outside [2^-120, 2^127]", scale);
+  return ARTOPK_OK;
+}
+
 template <class TT, class TY, int V>
 void embed(artopk_tokens* h, const TT* table, int64_t table_stride, int64_t vocab, int64_t cols, const Tokens& tokens, int64_t count,
            float scale, TY* y, int64_t y_stride) {
@@ -391,8 +398,7 @@ int artopk_token_logprobs(artopk_tokens* h, const void* logits, int64_t stride, 
   if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_token_logprobs: handle is NULL");
   int rc;
   if (!known_type(type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type %d", type);
-  if ((rc = check_tokens(h, tokens, token_bits, rows, vocab)) || (rc = check_scale(h, scale))) return rc;
-  if (!(scale > 0.0f)) return fail_text(h->err, ARTOPK_EINVAL, "scale is not positive");
+  if ((rc = check_tokens(h, tokens, token_bits, rows, vocab)) || (rc = check_logp_scale(h, scale))) return rc;
   if ((rc = check_rows(h->err, "logits", logits, stride, elem_size(type), rows, vocab))) return rc;
   if (logp_out && !tokens && rows > 0) return fail_text(h->err, ARTOPK_EINVAL, "tokens is NULL");
   if (top < 0 || top > ARTOPK_MAX_TOP || top > vocab)
@@ -479,8 +485,7 @@ int artopk_token_logprobs_backward(artopk_tokens* h, const void* logits, int64_t
   if (!h) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_token_logprobs_backward: handle is NULL");
   int rc;
   if (!known_type(type)) return fail_text(h->err, ARTOPK_EINVAL, "unknown element type %d", type);
-  if ((rc = check_tokens(h, tokens, token_bits, rows, vocab)) || (rc = check_scale(h, scale))) return rc;
-  if (!(scale > 0.0f)) return fail_text(h->err, ARTOPK_EINVAL, "scale is not positive");
+  if ((rc = check_tokens(h, tokens, token_bits, rows, vocab)) || (rc = check_logp_scale(h, scale))) return rc;
   const size_t size = elem_size(type);
   if ((rc = check_rows(h->err, "logits", logits, stride, size, rows, vocab))) return rc;
   if ((rc = check_rows(h->err, "dlogits", dlogits, dstride, size, rows, vocab))) return rc;

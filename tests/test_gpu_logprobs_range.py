@@ -114,7 +114,8 @@ def test_low_and_high_temperatures(rows, vocab, t):
         _check(x * size, t, 5, 1.0 / size)
 
 
-LEAST = 2.0 ** -120
+#: The scales that are taken: below, elements whose difference from the peak float32 does not hold would count; above, c is beyond it.
+LEAST, MOST = 2.0 ** -120, 2.0 ** 127
 
 
 @pytest.mark.parametrize("rows,vocab", SHAPES)
@@ -162,3 +163,26 @@ def test_gradient_of_rows_far_from_zero(rows, vocab):
             got = dx.cpu().double()
             bad = (got - s * want).abs() > tol + 2.0 ** -126 * (1.0 + s)
             assert not bool(bad.any()), (scale, far, kind, got[bad][:4], (s * want)[bad][:4])
+
+
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_ends_of_the_scales(rows, vocab):
+    import torch
+    import paper_2312_02493_amd as lib
+
+    g = torch.Generator().manual_seed(15)
+    for size in (1.0, 1e-30, 2.0 ** -127):
+        x = size * torch.randint(-6, 7, (rows, vocab), generator=g).float()  # (many equal ones)
+        _check(x, "f32", 5, MOST)
+        _check(x, "f32", 5, LEAST)
+    ctx = lib.TokenContext(rows, vocab)
+    dev, out = x.cuda(), [torch.zeros(rows, device="cuda") for _ in range(2)]
+    for scale in (float(np.nextafter(np.float32(LEAST), np.float32(0))), float(np.nextafter(np.float32(MOST), np.float32(np.inf))),
+                  1e-45, 3e38):
+        with pytest.raises(lib.ArTopkError) as e:
+            ctx.artopk_token_logprobs(dev, None, None, *out, scale=scale)
+        assert e.value.code == -1 and "scale" in str(e.value)
+        with pytest.raises(lib.ArTopkError) as e:
+            ctx.artopk_token_logprobs_backward(dev, None, *out, dev.clone(), dlse=out[0].clone(), scale=scale)
+        assert e.value.code == -1 and "scale" in str(e.value)
+    ctx.status()
