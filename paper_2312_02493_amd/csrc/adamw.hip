@@ -166,11 +166,13 @@ int check_moments(artopk_adamw* h, const void* first, const void* second, const 
 
 }  // namespace
 
-int64_t artopk_adamw_state_elems(const artopk_tensor* tensors, int32_t count, int64_t n) { return checked_elems(tensors, count, n); }
+int64_t artopk_adamw_state_elems(const artopk_tensor* tensors, int32_t count, int64_t n) {
+  const int64_t elems = checked_elems(tensors, count, n);
+  return elems < 0 || guarded([&] { return check_apart(tensors, count); }) ? -1 : elems;
+}
 
 int64_t artopk_adamw_scratch_bytes(const artopk_tensor* tensors, int32_t count, int64_t n) {
-  if (checked_elems(tensors, count, n) < 0) return -1;
-  if (guarded([&] { return check_apart(tensors, count); })) return -1;
+  if (artopk_adamw_state_elems(tensors, count, n) < 0) return -1;
   return (int64_t)(align_up((size_t)chunks_of(tensors, count) * sizeof(AdamChunk), 256) + 512);
 }
 

@@ -54,3 +54,10 @@ def test_no_cpu_fallback():
         lib.TokenContext(4, 4)
     with pytest.raises(RuntimeError):
         lib.AdamWContext([(0, 2)], 4)
+
+
+def test_adamw_sizes_of_overlapping_tensors():
+    for tensors, n in (([(0, 5), (4, 3)], 20), ([(4, 3), (0, 5)], 20), ([(0, 9), (3, 2)], 9), ([(2, 1), (2, 1)], 4)):
+        assert lib.artopk_adamw_state_elems(tensors, n) == lib.artopk_adamw_scratch_bytes(tensors, n) == -1, tensors
+        assert b"overlap" in lib.load_library().artopk_last_error(None)
+    assert lib.artopk_adamw_state_elems([(5, 4), (0, 5)], 9) == 512  # side by side, in any order
