@@ -289,6 +289,8 @@ const char* artopk_tokens_last_error(const artopk_tokens* tokens) { return token
 
 int artopk_tokens_status(artopk_tokens* tokens) {
   if (!tokens) return fail_text(g_noctx_err, ARTOPK_EINVAL, "artopk_tokens_status: tokens is NULL");
+  int rc;
+  if ((rc = check_device(tokens->err, tokens->device))) return rc;  // (a NULL stream would be another device's)
   TOKENS_TRY(tokens, hipStreamSynchronize(tokens->stream));
   int word = 0;
   TOKENS_TRY(tokens, hipMemcpy(&word, tokens->error, sizeof(word), hipMemcpyDeviceToHost));
