@@ -249,7 +249,7 @@ struct RowEnd {
 // (n ln(n / (n - top)) of them in a row without an order), and a listed one's place is the number of larger ones.  n is 64 for up to
 // kGroupTop alternatives; more are bounded by 128, of which a comparison costs more but leaves fewer (32768 x 8000 bfloat16, 64
 // alternatives: 64 keys 632 us, 128 326).  Should there be more than there is room for, the alternatives are found one
-// after the other.
+// after the other.  Columns are at least V (k_logp_narrow has up to 256).
 struct LogpPart {
   RowSum s;
   float unused;
@@ -310,14 +310,7 @@ __global__ __launch_bounds__(256) void k_logp(
     };
     // (the same for all lanes: full batches of whole pieces begin up to here)
     const int last = (q1 * (int64_t)V <= cols ? q1 : q1 - 1) - kBatch * NT;
-    if (cols < V) {
-      float v[V];
-      p.take_short(v, t == 0 && q0 < q1);
-      const float most = largest<V>(v);
-      if (t == 0 && q0 < q1) note(most, 0);
-      g.add<V>(v, most, c);
-    }
-    int j = q0 + t, base = cols < V ? q1 : q0;
+    int j = q0 + t, base = q0;
     for (; base <= last; base += kBatch * NT, j += kBatch * NT) batch(Full(), j, true);
     for (; base + NT < q1; base += kBatch * NT, j += kBatch * NT) batch(Full(), j, false);
     if (base + team_wave * 64 < q1) batch(One(), j, false);
@@ -390,18 +383,14 @@ __global__ __launch_bounds__(256) void k_logp(
         for (int i = team_wave * (64 >> lg) + (lane >> lg); i < count; i += WAVES * (64 >> lg)) {
           for (int j = q0 + chosen[i] + with * NT; j < q1; j += NT << lg) {
             float v[V];
-            if (cols < V) {
-              p.take_short(v, true);
-            } else {
-              Some<T, V> raw;
-              p.template ask<false>(raw, j, false);
-              p.take(v, raw, j, false);
-            }
+            Some<T, V> raw;
+            p.template ask<false>(raw, j, false);
+            p.take(v, raw, j, false);
             if (!(largest<V>(v) >= least_value) && least) continue;
             const int64_t begin = p.begin(j);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-              if (begin + k < (int64_t)j * V || begin + k >= cols) continue;
+              if (begin + k < (int64_t)j * V) continue;  // (the piece's before it)
               const uint64_t o = (uint64_t)ordered(v[k]) << 32;
               if ((o | (uint32_t)~j) >= least) f(o | (uint32_t)~(uint32_t)(begin + k));
             }

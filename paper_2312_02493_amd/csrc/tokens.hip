@@ -55,6 +55,7 @@ constexpr int64_t kMostBlocks = 1 << 20;
   } while (0)
 
 constexpr int64_t kNarrowRow = 512, kSomeTop = 56, kShortRow = 2048, kLongerRow = 16384, kManyRows = 2048;
+static_assert(kNarrowRow / 2 >= RowRun<__bf16>::V, "k_logp's rows have a whole piece");
 constexpr int64_t kPartBlocks = 1024;  // that parts of rows make, at most
 constexpr int64_t kFewTokens = 8192, kFewTokensAlone = 14336;  // (at most what LDS holds beside the counts, 14336 keys)
 
