@@ -226,7 +226,9 @@ int artopk_adamw_step(artopk_adamw* h, void* weights, const float* update, void*
     rs.add(scales, (size_t)h->elems / kAdamBlock * 2, true, "scales");
     if ((rc = rs.check(h->err))) return rc;
   }
-  const AdamFixed f = {update_scale, eta, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), eps};
+  const AdamFixed f = {update_scale, eta, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), eps,
+                       // (the root's part of the divisor stays below 2^92, so eps alone can make its reciprocal that small)
+                       eps > 0x1p100f ? INFINITY : 0x1p-96f};
   AdamTerms terms = {0.0f, 0.0f, 0};
   const AdamTerms* later = nullptr;
   if (step > 0) {

@@ -42,6 +42,7 @@ struct AdamTerms {
 
 struct AdamFixed {
   float scale, eta, b1, c1, b2, c2, eps;  // c1 = 1 - b1, c2 = 1 - b2, each rounded once
+  float quick;  // second moments from here on take the quick square root and reciprocal: 2^-96, or infinity for a large eps
 };
 
 // 32 random bits of a place: two rounds of multiplying and folding the upper bits onto the lower ones.  The factors are odd whole
@@ -214,9 +215,9 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamChunk* __restrict__ chu
         m[i] = (CODES ? m[i] : in_m[q].e[i]) * f.b1 + x * f.c1;
         v[i] = (CODES ? v[i] : in_v[q].e[i]) * f.b2 + (x * x) * f.c2;
         w[i] = static_cast<float>(in_w[q].e[i]) * keep;
-        tiny |= v[i] < 0x1p-96f;
+        tiny |= v[i] < f.quick;
       }
-      if (__any(tiny)) {  // (the quick square root and reciprocal do not know numbers below the normal ones)
+      if (__any(tiny)) {  // (the quick square root and reciprocal neither take nor give numbers below the normal ones)
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = fmaf(-rate, m[i] / fmaf(sqrtf(v[i]), terms.root, f.eps), w[i]);
       } else {
