@@ -682,8 +682,8 @@ typedef struct artopk_adamw artopk_adamw;
  * exponent field f and three bits of mantissa b each, 2^(f - top + E - 127) (1 + b / 8), and 2^(1 - top + E - 127) b / 8 for
  * f = 0; the first moment with a sign and four bits of f, top = 14, the second with five and top = 30.  They are rounded
  * up or down at random so that their mean is exact (to 2^-17 of the distance of two codes), by bits that depend on
- * seed, step and place alone; a second moment other than zero below the least normal code becomes that code.  Infinity or NaN in
- * a moment makes the moments of its 256 elements NaN from the next step on.
+ * seed, step and place alone; a second moment other than zero below the least normal code becomes that code.  Infinity (also of
+ * a moment above 1.875 2^127 that is rounded up) or NaN in a moment makes the moments of its 256 elements NaN from the next step on.
  */
 int artopk_adamw_create(artopk_adamw** out, const artopk_tensor* tensors, int32_t count, int64_t n, int32_t type,
                         int32_t state_bits, void* hip_stream);

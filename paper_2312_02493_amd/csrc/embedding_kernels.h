@@ -340,7 +340,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(SortKeys in, int64_
 }
 
 // Few tokens: each one's place is the number of smaller keys and of equal ones before it.  A block has B tokens, and 1024 / B
-// threads for each, which compare it with as many shares of all keys, read from LDS (4099 tokens 8.4 us; two passes over their
+// threads for each, which compare it with as many shares of all keys, read from LDS (4099 tokens 7.7 us; two passes over their
 // digits by one block 19, by several in four launches 20).
 template <int B>
 __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortKeys in, int count, uint32_t* __restrict__ key_out,
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(kSumWaves * 64) void k_embed_sum(const uint32_t* __
       float s[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) s[j] = 0.0f;
-      // as many rows under way at a time as there are, up to sixteen
+      // sixteen rows under way at a time; of those left over up to eight, four, two and one, so 15 take four rounds of loads
       int e = e0;
       auto rows = [&](auto N, bool all) {
         Some<TD, V> in[N()];
